@@ -357,6 +357,113 @@ lbt_status lbt_grad_diagnostics(const float *dY, uint64_t n, const void *q_codes
                                 size_t ws_bytes, void *cuda_stream);
 
 /*
+ * Transformer-side operators (the paper trains convolutional networks; these carry its low-bit training to a residual block
+ * of a language model): a linear layer on 8-bit integers, the norms, gate and residual sum between two blocks, and the
+ * optimizer's step.  Element types of their tensors: */
+enum { LBT_F32 = 0, LBT_BF16 = 1, LBT_F16 = 2 };
+/*
+ * Matrices are row-major with a leading dimension ld (elements from one row to the next, >= the row's length).  Activation and
+ * gradient tensors need only their element type's alignment; rows that begin on 32-byte (fp32) or 16-byte boundaries are read
+ * in wide accesses.  Zero tokens (M = 0) are valid.
+ *
+ * 8-bit rows: q[m,i] = rint(x[m,i] * fl(127 fl(1 / a_m))), a_m = max_i |x[m,i]|, scale[m] = fl(a_m fl(1/127)); ties to even,
+ * codes in [-127, 127].  a_m <= 1e-36: scale 0, codes 0.  A row that holds an infinity or NaN: scale NaN, codes 0 (its row of
+ * a product is NaN and no other).  Code rows are 16-byte aligned, ldq a multiple of 16; columns up to the next multiple of 16 hold 0.
+ * Weights [O,I] give one scale per output channel, activations [M,I] one per token.
+ */
+lbt_status lbt_rows8_quantize(const void *x, int x_type, int64_t rows, int64_t cols, int64_t ld, void *q, int64_t ldq,
+                              float *scale, void *cuda_stream);
+
+/*
+ * Y[m,o] = s_x[m] s_w[o] sum_i q_x[m,i] q_w[o,i] (+ bias[o], fp32, may be NULL).  q_x, q_w: code rows with ldq = I rounded up
+ * to 16.  lbt_linear8_forward quantizes x first and leaves its codes and scales in q_x and s_x (caller's buffers: scratch, or
+ * kept for the backward pass); lbt_linear8_matmul starts from codes.  I <= 133144 (127 * 127 * I < 2^31), else
+ * LBT_ERR_ACC_RANGE.  dev_status (device int32, may be NULL) receives LBT_ERR_TIMEOUT if a bounded on-chip wait ran out.
+ */
+lbt_status lbt_linear8_forward(const void *x, int x_type, int64_t ldx, const void *q_w, const float *s_w, const float *bias,
+                               void *y, int y_type, int64_t ldy, int64_t M, int64_t O, int64_t I, void *q_x, float *s_x,
+                               int32_t *dev_status, void *cuda_stream);
+lbt_status lbt_linear8_matmul(const void *q_x, const float *s_x, const void *q_w, const float *s_w, const float *bias, void *y,
+                              int y_type, int64_t ldy, int64_t M, int64_t O, int64_t I, int32_t *dev_status, void *cuda_stream);
+
+/*
+ * Gradients of that layer, every product on 8-bit codes.  The scale of the reduced index is multiplied into dY before dY is
+ * quantized:
+ *   dX[m,i] = s_r[m] sum_o q_r[m,o] q_w[o,i]   (q_r, s_r) = 8-bit rows    of fl(dY[m,o] s_w[o])
+ *   dW[o,i] = s_c[o] sum_m q_c[m,o] q_x[m,i]   (q_c, s_c) = 8-bit columns of fl(dY[m,o] s_x[m])
+ *   dbias[o] = sum_m dY[m,o] (fp32)
+ * Any of dX, dW, dbias may be NULL.  q_x, s_x: what the forward pass left.  O <= 133144 for dX, M <= 133144 for dW
+ * (LBT_ERR_ACC_RANGE), M <= 4194240 in any case.  ws: lbt_linear8_workspace_bytes(M, O, I).
+ */
+size_t lbt_linear8_workspace_bytes(int64_t M, int64_t O, int64_t I);
+lbt_status lbt_linear8_backward(const void *dY, int dy_type, int64_t lddy, const void *q_w, const float *s_w, const void *q_x,
+                                const float *s_x, void *dX, int dx_type, int64_t lddx, void *dW, int dw_type, int64_t lddw,
+                                float *dbias, int64_t M, int64_t O, int64_t I, int32_t *dev_status, void *ws, size_t ws_bytes,
+                                void *cuda_stream);
+
+/*
+ * Between two residual blocks: u = N_post(h), r = scale_x x + scale_h gate u, y = N_pre(r), for M rows of D columns (D <= 32768).
+ *   N(v) = w (v - mu) rstd + b; LBT_NORM_LAYER: mu = mean v, rstd = (mean (v - mu)^2 + eps)^(-1/2); LBT_NORM_RMS: mu = 0.
+ * y is formed from r before r is rounded to its type.  Optional (NULL): gate (1), w_* (1), b_* (0), y and q (no second norm),
+ * stats.  gate: [ceil(M / rows_per_gate), D], gate row m / rows_per_gate for row m; rows_per_gate 0 = one gate row for all.
+ * q, q_scale: y's 8-bit rows as lbt_linear8_matmul takes them (codes of the fp32 y; q and y may both be asked for).
+ * stats: [M,4] floats, 16-byte aligned, kept for the backward pass (mu and rstd of both norms).  r may be x, y may be h.
+ */
+enum { LBT_NORM_RMS = 0, LBT_NORM_LAYER = 1 };
+typedef struct lbt_resnorm_desc {   /* HOST struct */
+    int64_t M, D, rows_per_gate;
+    int32_t type, param_type;       /* of x, h, r, y and their gradients; of gate, w, b and their gradients */
+    int32_t kind, post_norm;        /* LBT_NORM_*; post_norm 0: u = h                                       */
+    float eps_post, eps_pre, scale_x, scale_h;
+    int64_t ld_x, ld_h, ld_r, ld_y, ld_dr, ld_dy, ld_dx, ld_dh;   /* 0 = D */
+} lbt_resnorm_desc;
+lbt_status lbt_resnorm_forward(const lbt_resnorm_desc *d, const void *x, const void *h, const void *gate, const void *w_post,
+                               const void *b_post, const void *w_pre, const void *b_pre, void *r, void *y, void *q, int64_t ldq,
+                               float *q_scale, float *stats, void *cuda_stream);
+
+/*
+ * Its gradients, from dr (of r) and dy (of y); either may be NULL (0).  x, h, gate, the parameters and stats are the forward
+ * pass's (x and h unchanged: r is formed again in fp32).  dx, dh: [M,D]; dgate (needs gate), dw_post, db_post, dw_pre, db_pre:
+ * param_type, NULL where not wanted; a gate row's gradient is the sum over its rows.  dx may be dr, dh may be dy.
+ * ws: lbt_resnorm_workspace_bytes(d).  Sums are fp32 in an order fixed by M and D.
+ */
+size_t lbt_resnorm_workspace_bytes(const lbt_resnorm_desc *d);
+lbt_status lbt_resnorm_backward(const lbt_resnorm_desc *d, const void *dr, const void *dy, const void *x, const void *h,
+                                const void *gate, const void *w_post, const void *b_post, const void *w_pre, const float *stats,
+                                void *dx, void *dh, void *dgate, void *dw_post, void *db_post, void *dw_pre, void *db_pre,
+                                void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * One AdamW step (decoupled weight decay) over `count` tensors, one launch per 400 of them:
+ *   g' = g * *d_grad_scale (1 if NULL);  m = b1 m + (1 - b1) g';  v = b2 v + (1 - b2) g'^2;
+ *   p = (1 - lr wd) p - (lr / (1 - b1^step)) m / (sqrt(v) / sqrt(1 - b2^step) + eps)
+ * in fp32, every operation rounded once; p is rounded to its type once.  step counts from 1.  *d_skip != 0 (device int32, may be
+ * NULL): nothing changes (a step whose gradients overflowed).
+ * state_bits 32: m, v fp32.  state_bits 8: m and the root of v as e4m3 codes, one byte an element, in blocks of 256 consecutive
+ * elements of a tensor: value = code * scale, scale = fl(max / 448) over the block's finite values, m_scale / v_scale:
+ * ceil(n / 256) floats.  A positive root is never stored as code 0.  All-zero codes and scales are the state before step 1.
+ * A non-finite gradient makes its own element's p, m and v non-finite and no other element's.
+ * `tensors` (HOST) is read during the call.  Tensors need their element type's alignment; 32 bytes (fp32), 16 (16-bit) and
+ * 8 (codes) are read in wide accesses.  n = 0 is valid.
+ */
+typedef struct lbt_adamw_tensor {
+    void *p;            /* parameters, p_type          */
+    const void *g;      /* gradients, g_type           */
+    void *m, *v;        /* moments                     */
+    float *m_scale, *v_scale;
+    uint64_t n;
+    double lr, weight_decay;
+    int32_t p_type, g_type;
+} lbt_adamw_tensor;     /* 80 bytes */
+typedef struct lbt_adamw_hyper {
+    double beta1, beta2, eps;
+    int64_t step;
+    int32_t state_bits, reserved;
+} lbt_adamw_hyper;      /* 40 bytes */
+lbt_status lbt_adamw_step(const lbt_adamw_tensor *tensors, int count, const lbt_adamw_hyper *h, const float *d_grad_scale,
+                          const int32_t *d_skip, void *cuda_stream);
+
+/*
  * Measurement taps (no counterpart in the paper).  After this call the library records the two
  * events (cudaEvent_t passed as void*, created by the caller) on the call's stream immediately
  * before and after every launch of the named kernel class, so that a benchmark can time one

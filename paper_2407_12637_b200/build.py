@@ -10,7 +10,7 @@ LIB = os.path.join(_HERE, "liblbt.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+    "-Xcompiler", "-fPIC", "-shared", "-t", "0", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 
 

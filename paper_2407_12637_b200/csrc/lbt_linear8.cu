@@ -1,0 +1,926 @@
+// Linear layer on 8-bit integers with a scale for each token and channel.
+//
+//   forward   Y[m,o]  = s_x[m] s_w[o] sum_i q_x[m,i] q_w[o,i] + bias[o]
+//   backward  dX[m,i] = s_r[m] sum_o q_r[m,o] q_w[o,i]     (q_r, s_r): rows of dY[m,o] s_w[o]
+//             dW[o,i] = s_c[o] sum_m q_c[m,o] q_x[m,i]     (q_c, s_c): columns of dY[m,o] s_x[m]
+//
+// A scale that sits on the reduced index cannot leave the integer sum, so the backward pass multiplies it into dY before
+// dY is quantized: all three products are then exact sums of int8 products in int32, scaled once.
+//
+// Three products, one main loop: C[R, N] = sum_k A B with each operand either K-major ([row][k]) or MN-major ([k][row]);
+// both are what TMA writes with the 128-byte swizzle and what a tcgen05 descriptor can name, so nothing is transposed.
+#include <cuda.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "lbt_sm100.cuh"
+#include "lbt_types.cuh"
+
+namespace lbt {
+
+using namespace sm100;
+
+namespace {
+
+constexpr int kStep = 128;                       // reduction bytes of one pipeline stage
+constexpr int kBox = kStep * 128;                // a 128 x 128-byte operand tile
+constexpr uint64_t kLimitNs = 2000000000ull;     // every on-chip wait gives up after 2 s
+constexpr int kMaxStages = 8;
+constexpr int kRing = 6 * kBox;                  // operand ring of the 128 x 128 kernel: two CTAs fit one SM
+constexpr int kPairStages = 6;
+constexpr int kPairRing = kPairStages * 2 * kBox;
+constexpr int kPairThreads = 320;                // TMA warp, MMA warp, 8 epilogue warps
+constexpr int64_t kMaxReduction = 133144;        // 127 * 127 * k < 2^31
+
+enum { kForward = 0, kDgrad = 1, kWgrad = 2 };   // A, B: K-major, K-major | K-major, MN-major | MN-major, MN-major
+
+struct L8Args {
+    int mode;
+    int tiles_m, tiles_n, total, band;
+    int steps;             // reduction steps of 128
+    int splits;            // 128 x 128 kernel: CTAs of a cluster that share a tile, a slice of the reduction each
+    int swapped;           // 128 x 128 kernel, forward: A = weights (128 channels), B = tokens (mma_n of them)
+    int mma_n;             // 128 x 128 kernel: columns of the accumulator
+    int stage_bytes, stages;
+    int rows, cols;        // of the output as stored
+    const float* row_scale;
+    const float* col_scale;   // may be null: 1
+    const float* bias;        // per column, may be null
+    void* out;
+    int64_t ldo;
+    int out_type;
+    int vec;               // rows of the output begin on 32-byte boundaries
+    int wait_prev;         // chained behind the kernel that writes the operands
+    int32_t* status;
+};
+
+struct Bars {
+    uint64_t full[kMaxStages], empty[kMaxStages], tmem_full[2], tmem_empty[2];
+    uint32_t tmem_base;
+    volatile uint32_t abort;
+};
+
+__device__ __forceinline__ bool wait_for(Bars* b, uint64_t* bar, uint32_t parity, int32_t* status, bool relaxed = false) {
+    if (b->abort) return false;
+    if (relaxed ? mbar_wait_bounded_relaxed(bar, parity, kLimitNs) : mbar_wait_bounded(bar, parity, kLimitNs)) return true;
+    b->abort = 1u;
+    if (status != nullptr) atomicCAS(status, (int32_t)LBT_OK, (int32_t)LBT_ERR_TIMEOUT);
+    return false;
+}
+
+// Tiles are walked in bands of `band` row tiles, rows fastest, so that the CTAs at work share few strips of A and B in L2.
+__device__ __forceinline__ void tile_at(const L8Args& a, int t, int& m, int& n) {
+    const int per_band = a.band * a.tiles_n;
+    const int b = t / per_band, within = t - b * per_band;
+    const int rows = min(a.band, a.tiles_m - b * a.band);
+    n = within / rows;
+    m = b * a.band + (within - n * rows);
+}
+
+// Stores columns [c, c + 8) of output row `row`; f holds the finished values.
+template <typename T>
+__device__ __forceinline__ void put8(const L8Args& a, int64_t row, int c, const float (&f)[8]) {
+    T* dst = static_cast<T*>(a.out) + row * a.ldo + c;
+    if (a.vec && c + 8 <= a.cols) {
+        store8(dst, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < a.cols) dst[i] = from_f32<T>(f[i]);
+    }
+}
+
+// 32 consecutive columns of one row (lane = row) from the accumulator: scale, bias, round, store.  `cs`: this warp's shared
+// copy of the 32 columns' scales and biases.
+template <typename T>
+__device__ __forceinline__ void put_row(const L8Args& a, int64_t row, int c0, const uint32_t (&v)[32], float rs, const float* cs) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 16) {
+        // 16 columns at a time: a 32-byte sector of a 16-bit type
+        float f[16];
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const float4 s = *reinterpret_cast<const float4*>(cs + j + e), b = *reinterpret_cast<const float4*>(cs + 32 + j + e);
+            f[e] = __fadd_rn(__fmul_rn(__int2float_rn((int)v[j + e]), __fmul_rn(rs, s.x)), b.x);
+            f[e + 1] = __fadd_rn(__fmul_rn(__int2float_rn((int)v[j + e + 1]), __fmul_rn(rs, s.y)), b.y);
+            f[e + 2] = __fadd_rn(__fmul_rn(__int2float_rn((int)v[j + e + 2]), __fmul_rn(rs, s.z)), b.z);
+            f[e + 3] = __fadd_rn(__fmul_rn(__int2float_rn((int)v[j + e + 3]), __fmul_rn(rs, s.w)), b.w);
+        }
+        const int c = c0 + j;
+        if (row >= a.rows || c >= a.cols) continue;
+        T* dst = static_cast<T*>(a.out) + row * a.ldo + c;
+        if (a.vec && c + 16 <= a.cols) {
+            float lo[8], hi[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { lo[i] = f[i]; hi[i] = f[8 + i]; }
+            if (sizeof(T) == 2) {
+                Vec8<T> p, q;
+                pack(lo, p); pack(hi, q);
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { w[i] = p.w[i]; w[4 + i] = q.w[i]; }
+                st_global_cs_v8(dst, w);
+            } else {
+                Vec8<T> p, q;
+                pack(lo, p); pack(hi, q);
+                st_vec(dst, p.w);
+                st_vec(dst + 8, q.w);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (c + i < a.cols) dst[i] = from_f32<T>(f[i]);
+        }
+    }
+}
+
+__device__ __forceinline__ void put_row_any(const L8Args& a, int64_t row, int c0, const uint32_t (&v)[32], float rs, const float* cs) {
+    if (a.out_type == LBT_BF16) put_row<__nv_bfloat16>(a, row, c0, v, rs, cs);
+    else if (a.out_type == LBT_F16) put_row<__half>(a, row, c0, v, rs, cs);
+    else put_row<float>(a, row, c0, v, rs, cs);
+}
+
+__device__ __forceinline__ void put_one(const L8Args& a, int64_t row, int64_t col, float f) {
+    const int64_t i = row * a.ldo + col;
+    if (a.out_type == LBT_BF16) static_cast<__nv_bfloat16*>(a.out)[i] = __float2bfloat16_rn(f);
+    else if (a.out_type == LBT_F16) static_cast<__half*>(a.out)[i] = __float2half_rn(f);
+    else static_cast<float*>(a.out)[i] = f;
+}
+
+// The scales and biases of 32 columns into a warp's 64 floats of shared memory.
+__device__ __forceinline__ void stage_columns(const L8Args& a, int c0, float* cs, int lane) {
+    __syncwarp();
+    const int c = c0 + lane;
+    cs[lane] = c < a.cols && a.col_scale != nullptr ? __ldg(a.col_scale + c) : 1.0f;
+    cs[32 + lane] = c < a.cols && a.bias != nullptr ? __ldg(a.bias + c) : 0.0f;
+    __syncwarp();
+}
+
+// ------------------------------------------------------------------------------------------ 128 x 128 tiles
+// One tile per CTA, two CTAs per SM (one drains while the other multiplies).  With few tiles a cluster of `splits` CTAs shares a
+// tile: each takes a slice of the reduction, leaves its int32 accumulator in shared memory, and finishes a slice of the
+// columns from all of them (integer sums: any order gives the same bits).
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(128, 2)
+l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ L8Args a) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    __shared__ Bars bars;
+    __shared__ alignas(16) float columns[4][64];
+    Bars* b = &bars;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = a.splits > 1 ? (int)cluster_ctarank() : 0;
+    int tm, tn;
+    tile_at(a, (int)blockIdx.x / a.splits, tm, tn);
+    const int per = (a.steps + a.splits - 1) / a.splits;
+    const int k0 = split * per, k1 = min(k0 + per, a.steps), n_steps = max(k1 - k0, 0);
+    const int m0 = tm * 128, n0 = tn * a.mma_n;
+    const bool a_mn = a.mode == kWgrad, b_mn = a.mode != kForward;
+
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&tmA);
+        prefetch_tensormap(&tmB);
+        for (int s = 0; s < a.stages; ++s) { mbar_init(&b->full[s], 1); mbar_init(&b->empty[s], 1); }
+        mbar_init(&b->tmem_full[0], 1);
+        b->abort = 0u;
+        fence_mbar_init();
+    }
+    if (warp == 1) { tmem_alloc(&b->tmem_base, 128); tmem_relinquish(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = b->tmem_base;
+
+    if (warp == 0) {
+        if (elect_one()) {
+            auto load_a = [&](int i, int s) {
+                const int k = (k0 + i) * kStep;
+                uint8_t* dst = ring + s * a.stage_bytes;
+                if (a_mn) tma_load_2d(dst, &tmA, &b->full[s], m0, k); else tma_load_2d(dst, &tmA, &b->full[s], k, m0);
+            };
+            auto load_b = [&](int i, int s) {
+                const int k = (k0 + i) * kStep;
+                uint8_t* dst = ring + s * a.stage_bytes + kBox;
+                if (b_mn) tma_load_2d(dst, &tmB, &b->full[s], n0, k); else tma_load_2d(dst, &tmB, &b->full[s], k, n0);
+            };
+            // The weights (A of the swapped form) do not come from the kernel ahead: their first loads do not wait for it.
+            const int ahead = a.wait_prev && a.swapped ? min(a.stages, n_steps) : 0;
+            for (int i = 0; i < ahead; ++i) {
+                mbar_arrive_expect_tx(&b->full[i], (uint32_t)a.stage_bytes);
+                load_a(i, i);
+            }
+            if (a.wait_prev) griddep_wait();
+            for (int i = 0; i < ahead; ++i) load_b(i, i);
+            for (int i = ahead; i < n_steps; ++i) {
+                const int s = i % a.stages;
+                if (!wait_for(b, &b->empty[s], (uint32_t)((i / a.stages) & 1) ^ 1u, a.status)) break;
+                mbar_arrive_expect_tx(&b->full[s], (uint32_t)a.stage_bytes);
+                load_a(i, s);
+                load_b(i, s);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (elect_one()) {
+            const uint32_t idesc = idesc_i8(128, a.mma_n, true, true, a_mn, b_mn);
+            bool ok = true;
+            for (int i = 0; i < n_steps && ok; ++i) {
+                const int s = i % a.stages;
+                ok = wait_for(b, &b->full[s], (uint32_t)(i / a.stages) & 1u, a.status);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t pa = smem_u32(ring + s * a.stage_bytes), pb = pa + kBox;
+                const uint64_t da = a_mn ? smem_desc_sw128(pa, kBox, 1024) : smem_desc_sw128(pa, 16, 1024);
+                const uint64_t db = b_mn ? smem_desc_sw128(pb, kBox, 1024) : smem_desc_sw128(pb, 16, 1024);
+#pragma unroll
+                for (int k = 0; k < kStep / 32; ++k)
+                    mma_i8_ss(tmem, da + (uint64_t)(k * (a_mn ? 256 : 2)), db + (uint64_t)(k * (b_mn ? 256 : 2)), idesc, (i > 0 || k > 0) ? 1u : 0u);
+                mma_commit(&b->empty[s]);
+            }
+            if (ok) mma_commit(&b->tmem_full[0]);
+        }
+        __syncwarp();
+    }
+    if (a.wait_prev) griddep_wait();   // the scales come from the kernel ahead too, and nothing is written before it has ended
+    bool ok = true;
+    if (n_steps > 0) ok = wait_for(b, &b->tmem_full[0], 0u, a.status);
+    ok = __syncthreads_and(ok) != 0;   // uniform; without it a lost signal ends in the error word and no output
+    tc_fence_after_sync();
+    const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+    int c_lo = 0, c_hi = a.mma_n;
+    if (a.splits > 1) {
+        // accumulator -> own shared memory, [column][row]
+        uint32_t* park = reinterpret_cast<uint32_t*>(ring);
+        for (int c = 0; c < a.mma_n && ok; c += 32) {
+            uint32_t v[32];
+            if (n_steps > 0) { tmem_ld_32x32(lanes + (uint32_t)c, v); tmem_ld_wait(); }
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (c + j < a.mma_n) park[(c + j) * 128 + threadIdx.x] = n_steps > 0 ? v[j] : 0u;
+        }
+        cluster_sync_all();
+        const int per_rank = a.mma_n / a.splits;
+        c_lo = split * per_rank;
+        c_hi = c_lo + per_rank;
+    }
+    const int64_t row = m0 + (int)threadIdx.x;
+    if (ok && a.splits > 1) {
+        uint32_t from[8];
+        for (int r = 0; r < a.splits; ++r) from[r] = map_to_cta(smem_u32(ring), (uint32_t)r);
+        auto total = [&](int c) {
+            int sum = 0;
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < a.splits) sum += (int)ld_cluster_u32(from[r] + (uint32_t)(c * 128 + (int)threadIdx.x) * 4u);
+            return sum;
+        };
+        if (a.swapped) {
+            const float cs = row < a.cols ? __ldg(a.col_scale + row) : 0.0f, bias = a.bias != nullptr && row < a.cols ? __ldg(a.bias + row) : 0.0f;
+            for (int c = c_lo; c < c_hi; ++c) {
+                const int m = n0 + c;
+                const int sum = total(c);
+                if (m < a.rows && row < a.cols) put_one(a, m, row, __fadd_rn(__fmul_rn(__int2float_rn(sum), __fmul_rn(a.row_scale[m], cs)), bias));
+            }
+        } else {
+            const float rs = row < a.rows ? a.row_scale[row] : 0.0f;
+            for (int c = c_lo; c < c_hi; c += 8) {   // (a slice of the columns is a multiple of 16 here)
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int n = n0 + c + i;
+                    const float cs = a.col_scale != nullptr && n < a.cols ? __ldg(a.col_scale + n) : 1.0f;
+                    const float bias = a.bias != nullptr && n < a.cols ? __ldg(a.bias + n) : 0.0f;
+                    f[i] = __fadd_rn(__fmul_rn(__int2float_rn(total(c + i)), __fmul_rn(rs, cs)), bias);
+                }
+                if (row < a.rows && n0 + c < a.cols) {
+                    if (a.out_type == LBT_BF16) put8<__nv_bfloat16>(a, row, n0 + c, f);
+                    else if (a.out_type == LBT_F16) put8<__half>(a, row, n0 + c, f);
+                    else put8<float>(a, row, n0 + c, f);
+                }
+            }
+        }
+    } else if (ok) {
+        const float rs = !a.swapped && row < a.rows ? a.row_scale[row] : 0.0f;
+        const float cs = a.swapped && row < a.cols ? __ldg(a.col_scale + row) : 0.0f;
+        const float bias = a.swapped && a.bias != nullptr && row < a.cols ? __ldg(a.bias + row) : 0.0f;
+        for (int c = 0; c < a.mma_n; c += 32) {
+            uint32_t v[32];
+            tmem_ld_32x32(lanes + (uint32_t)c, v);
+            tmem_ld_wait();
+            if (a.swapped) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const int m = n0 + c + j;
+                    if (c + j < a.mma_n && m < a.rows && row < a.cols)
+                        put_one(a, m, row, __fadd_rn(__fmul_rn(__int2float_rn((int)v[j]), __fmul_rn(a.row_scale[m], cs)), bias));
+                }
+            } else {
+                stage_columns(a, n0 + c, columns[warp], lane);
+                put_row_any(a, row, n0 + c, v, rs, columns[warp]);
+            }
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (b->abort && threadIdx.x == 0) {   // copies in flight land before the CTA's shared memory goes
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 20000000ull) __nanosleep(1000);
+    }
+    if (a.splits > 1) cluster_sync_all();   // no CTA leaves while another reads its shared memory
+    else __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, 128);
+}
+
+// ------------------------------------------------------------------------------------------ 256 x 256 tiles, CTA pairs
+// Persistent: pair p works on tiles p, p + pairs, ...; two accumulators of 256 TMEM columns let the epilogue of one tile run under
+// the main loop of the next.  Each CTA loads its 128 rows of A and its half of B's columns (32 KB a step), rank 0 issues the MMAs
+// of both: 8 KB of shared-memory operand reads per SM and MMA instead of the 12 KB a single CTA would need.
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+l8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ L8Args a) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    __shared__ Bars bars;
+    __shared__ alignas(16) float columns[8][64];
+    Bars* b = &bars;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+    const bool a_mn = a.mode == kWgrad, b_mn = a.mode != kForward;
+
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&tmA);
+        prefetch_tensormap(&tmB);
+        for (int s = 0; s < kPairStages; ++s) { mbar_init(&b->full[s], 1); mbar_init(&b->empty[s], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&b->tmem_full[i], 1); mbar_init(&b->tmem_empty[i], 16); }
+        b->abort = 0u;
+        fence_mbar_init();
+    }
+    if (warp == 1) { tmem_alloc_pair(&b->tmem_base, 512); tmem_relinquish_pair(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after_sync();
+    if (a.wait_prev) griddep_wait();
+    const uint32_t tmem = b->tmem_base;
+
+    if (warp == 0) {
+        if (elect_one()) {
+            int s = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (int t = pair; t < a.total && ok; t += pairs) {
+                int tm, tn;
+                tile_at(a, t, tm, tn);
+                const int m0 = tm * 256 + (int)rank * 128, n0 = tn * 256 + (int)rank * 128;
+                for (int i = 0; i < a.steps; ++i) {
+                    ok = wait_for(b, &b->empty[s], ph ^ 1u, a.status);
+                    if (!ok) break;
+                    uint8_t* dst = ring + s * 2 * kBox;
+                    if (rank == 0) mbar_arrive_expect_tx(&b->full[s], 4u * kBox);   // the bytes of both CTAs
+                    const uint32_t full0 = map_to_cta(smem_u32(&b->full[s]), 0);
+                    const int k = i * kStep;
+                    if (a_mn) tma_load_2d_pair(dst, &tmA, full0, m0, k); else tma_load_2d_pair(dst, &tmA, full0, k, m0);
+                    if (b_mn) tma_load_2d_pair(dst + kBox, &tmB, full0, n0, k); else tma_load_2d_pair(dst + kBox, &tmB, full0, k, n0);
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0 && elect_one()) {
+            const uint32_t idesc = idesc_i8(256, 256, true, true, a_mn, b_mn);
+            const uint32_t base = smem_u32(ring);
+            const uint64_t da0 = a_mn ? smem_desc_sw128(base, kBox, 1024) : smem_desc_sw128(base, 16, 1024);
+            const uint64_t db0 = b_mn ? smem_desc_sw128(base + kBox, kBox, 1024) : smem_desc_sw128(base + kBox, 16, 1024);
+            const uint64_t ka = a_mn ? 256 : 2, kb = b_mn ? 256 : 2;
+            int s = 0;
+            uint32_t ph = 0, acc = 0;
+            bool ok = true;
+            for (int t = pair; t < a.total && ok; t += pairs, ++acc) {
+                const uint32_t buf = acc & 1u;
+                ok = wait_for(b, &b->tmem_empty[buf], ((acc >> 1) & 1u) ^ 1u, a.status);
+                if (!ok) break;
+                tc_fence_after_sync();
+                for (int i = 0; i < a.steps; ++i) {
+                    ok = wait_for(b, &b->full[s], ph, a.status);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint64_t da = da0 + (uint64_t)(s * (2 * kBox >> 4)), db = db0 + (uint64_t)(s * (2 * kBox >> 4));
+#pragma unroll
+                    for (int k = 0; k < kStep / 32; ++k)
+                        mma_i8_ss_pair(tmem + buf * 256u, da + k * ka, db + k * kb, idesc, (i > 0 || k > 0) ? 1u : 0u);
+                    mma_commit_pair(&b->empty[s]);
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+                if (ok) mma_commit_pair(&b->tmem_full[buf]);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;   // the TMEM lanes a warp may read; half of the columns each
+        float* cs = columns[warp - 2];
+        uint32_t acc = 0;
+        for (int t = pair; t < a.total; t += pairs, ++acc) {
+            int tm, tn;
+            tile_at(a, t, tm, tn);
+            const uint32_t buf = acc & 1u;
+            bool ok = wait_for(b, &b->tmem_full[buf], (acc >> 1) & 1u, a.status, true);
+            ok = __all_sync(0xFFFFFFFFu, ok) != 0;
+            if (!ok) break;
+            tc_fence_after_sync();
+            const int64_t row = (int64_t)tm * 256 + rank * 128 + quarter * 32 + lane;
+            const float rs = row < a.rows ? a.row_scale[row] : 0.0f;
+            for (int c = half * 128; c < half * 128 + 128; c += 32) {
+                uint32_t v[32];
+                tmem_ld_32x32(tmem + buf * 256u + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
+                stage_columns(a, tn * 256 + c, cs, lane);
+                tmem_ld_wait();
+                put_row_any(a, row, tn * 256 + c, v, rs, cs);
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&b->tmem_empty[buf]), 0));
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (b->abort && threadIdx.x == 0) {
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 20000000ull) __nanosleep(1000);
+    }
+    cluster_sync_all();
+    if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
+// ------------------------------------------------------------------------------------------ quantizers
+// Eight consecutive elements [c, c + 8) of a row of `cols`, zeros behind its end.
+template <typename T>
+__device__ __forceinline__ void load_group(const T* row, int64_t c, int64_t cols, bool vec, float (&f)[8]) {
+    if (vec && c + 8 <= cols) {
+        load8(row + c, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = c + i < cols ? to_f32(row[c + i]) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ uint2 codes8(const float (&f)[8], float factor) {
+    return make_uint2(pack4(code8(f[0], factor), code8(f[1], factor), code8(f[2], factor), code8(f[3], factor)),
+                      pack4(code8(f[4], factor), code8(f[5], factor), code8(f[6], factor), code8(f[7], factor)));
+}
+
+// Row quantizer: kPerRow threads (a warp or the block of 256) own a row, eight columns at a time; the first four groups of a
+// thread stay in registers between the maximum and the codes (8192 columns for a block), the rest is read again.
+// One reading of the elements and one byte written for each: bound by memory.
+template <typename T, int kPerRow>
+__global__ void __launch_bounds__(256)
+rows8_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, bool vec, uint8_t* __restrict__ q, int64_t ldq,
+             float* __restrict__ scale) {
+    constexpr int kHeld = 4;
+    griddep_launch_dependents();
+    const int64_t row = kPerRow == 256 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int t = kPerRow == 256 ? threadIdx.x : threadIdx.x & 31;
+    if (row >= rows) return;
+    const T* src = x + row * ld;
+    float f[kHeld][8];
+    uint32_t most = 0;
+#pragma unroll
+    for (int g = 0; g < kHeld; ++g) {
+        const int64_t c = (int64_t)(g * kPerRow + t) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[g][i] = 0.0f;
+        if (c < cols) load_group(src, c, cols, vec, f[g]);
+    }
+#pragma unroll
+    for (int g = 0; g < kHeld; ++g)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max(most, abs_bits(f[g][i]));
+    for (int64_t c = (int64_t)(kHeld * kPerRow + t) * 8; c < cols; c += kPerRow * 8) {
+        float e[8];
+        load_group(src, c, cols, vec, e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max(most, abs_bits(e[i]));
+    }
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    if (kPerRow == 256) {
+        __shared__ uint32_t part[8];
+        if ((t & 31) == 0) part[t >> 5] = most;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max(most, part[i]);
+    }
+    float s, factor;
+    scale8(most, s, factor);
+    if (t == 0) scale[row] = s;
+    uint8_t* dst = q + row * ldq;
+#pragma unroll
+    for (int g = 0; g < kHeld; ++g) {
+        const int64_t c = (int64_t)(g * kPerRow + t) * 8;
+        if (c < ldq) *reinterpret_cast<uint2*>(dst + c) = codes8(f[g], factor);
+    }
+    for (int64_t c = (int64_t)(kHeld * kPerRow + t) * 8; c < ldq; c += kPerRow * 8) {
+        float e[8];
+        load_group(src, c, cols, vec, e);
+        *reinterpret_cast<uint2*>(dst + c) = codes8(e, factor);
+    }
+}
+
+// Gradient quantizer, two passes over dY in tiles of 256 columns x `strip` rows (a warp owns 256 columns and every eighth row).
+// First pass: the largest |dY s_w| of each row, the largest |dY s_x| of each column (as integers: order-free), and with
+// dbias the column sums of each strip.  Second pass: both code matrices and their scales.
+constexpr int kStrip = 64;
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+grad8_stats_kernel(const T* __restrict__ dY, int64_t M, int64_t O, int64_t ld, bool vec, const float* __restrict__ s_w,
+                   const float* __restrict__ s_x, uint32_t* __restrict__ row_most, uint32_t* __restrict__ col_most, float* __restrict__ sums) {
+    __shared__ uint32_t most[8][256];
+    __shared__ float sum[8][256];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t c = (int64_t)blockIdx.x * 256 + lane * 8, m0 = (int64_t)blockIdx.y * kStrip, m1 = min(m0 + kStrip, M);
+    float w[8], total[8];
+    uint32_t cm[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { w[i] = c + i < O ? s_w[c + i] : 0.0f; total[i] = 0.0f; cm[i] = 0u; }
+    for (int64_t m = m0 + warp; m < m1; m += 8) {
+        float f[8];
+        load_group(dY + m * ld, c, O, vec, f);
+        const float sx = s_x[m];
+        uint32_t rm = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (c + i < O) {
+                rm = max(rm, abs_bits(__fmul_rn(f[i], w[i])));
+                cm[i] = max(cm[i], abs_bits(__fmul_rn(f[i], sx)));
+            }
+            total[i] += f[i];
+        }
+        rm = __reduce_max_sync(0xFFFFFFFFu, rm);
+        if (lane == 0) atomicMax(row_most + m, rm);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { most[warp][lane * 8 + i] = cm[i]; sum[warp][lane * 8 + i] = total[i]; }
+    __syncthreads();
+    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (col >= O) return;
+    uint32_t top = 0;
+    float all = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { top = max(top, most[i][threadIdx.x]); all += sum[i][threadIdx.x]; }
+    atomicMax(col_most + col, top);
+    if (sums != nullptr) sums[(int64_t)blockIdx.y * O + col] = all;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+grad8_codes_kernel(const T* __restrict__ dY, int64_t M, int64_t O, int64_t ld, bool vec, const float* __restrict__ s_w,
+                   const float* __restrict__ s_x, const uint32_t* __restrict__ row_most, const uint32_t* __restrict__ col_most,
+                   const float* __restrict__ sums, uint8_t* __restrict__ q_r, uint8_t* __restrict__ q_c, int64_t ldq,
+                   float* __restrict__ s_r, float* __restrict__ s_c, float* __restrict__ dbias) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t c = (int64_t)blockIdx.x * 256 + lane * 8, m0 = (int64_t)blockIdx.y * kStrip, m1 = min(m0 + kStrip, M);
+    float w[8], fc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float s = 0.0f;
+        w[i] = fc[i] = 0.0f;
+        if (c + i < O) { w[i] = s_w[c + i]; scale8(col_most[c + i], s, fc[i]); }
+        if (blockIdx.y == 0 && warp == 0 && c + i < O) s_c[c + i] = s;
+    }
+    if (sums != nullptr && blockIdx.y == 0) {
+        const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        if (col < O) {
+            float all = 0.0f;
+            for (int64_t z = 0; z * kStrip < M; ++z) all += sums[z * O + col];
+            dbias[col] = all;
+        }
+    }
+    if (c >= ldq) return;
+    for (int64_t m = m0 + warp; m < m1; m += 8) {
+        float f[8], r[8], fr, s;
+        load_group(dY + m * ld, c, O, vec, f);
+        scale8(row_most[m], s, fr);
+        if (c == 0) s_r[m] = s;
+        const float sx = s_x[m];
+        uint32_t k[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            r[i] = __fmul_rn(f[i], w[i]);
+            k[i] = code8(__fmul_rn(f[i], sx), fc[i]);
+        }
+        if (q_r != nullptr) *reinterpret_cast<uint2*>(q_r + m * ldq + c) = codes8(r, fr);
+        if (q_c != nullptr) *reinterpret_cast<uint2*>(q_c + m * ldq + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
+    }
+}
+
+// ------------------------------------------------------------------------------------------ host
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                             CUtensorMapFloatOOBfill);
+
+EncodeFn encoder() {
+    static EncodeFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeFn>(p);
+    });
+    return fn;
+}
+
+// int8 codes [rows][pitch], boxes of `box_rows` rows x 128 bytes, 128-byte swizzle, zeros outside
+bool code_map(CUtensorMap* tm, const void* base, int64_t pitch, int64_t rows, int box_rows) {
+    EncodeFn fn = encoder();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kTileSmem = kRing + 1024;
+constexpr int kPairSmem = kPairRing + 1024;
+
+lbt_status allow_smem() {
+    constexpr int kDevices = 64;
+    static std::mutex mu;
+    static bool known[kDevices];
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return LBT_ERR_CUDA;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!known[dev]) {
+        if (cudaFuncSetAttribute(l8_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmem) != cudaSuccess ||
+            cudaFuncSetAttribute(l8_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem) != cudaSuccess)
+            return LBT_ERR_CUDA;
+        known[dev] = true;
+    }
+    return LBT_OK;
+}
+
+int64_t pitch16(int64_t n) { return (n + 15) / 16 * 16; }
+
+struct Product {
+    int mode;
+    const void* A; int64_t a_pitch, a_rows;   // as stored
+    const void* B; int64_t b_pitch, b_rows;
+    int64_t rows, cols, red;                  // C[rows, cols] = sum over red
+    const float *row_scale, *col_scale, *bias;
+    void* out; int out_type; int64_t ldo;
+    bool behind;                              // the launch ahead writes operands of this one
+};
+
+lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
+    lbt_status rc = allow_smem();
+    if (rc != LBT_OK) return rc;
+    L8Args a{};
+    a.mode = p.mode;
+    a.steps = (int)((p.red + kStep - 1) / kStep);
+    a.rows = (int)p.rows; a.cols = (int)p.cols;
+    a.row_scale = p.row_scale; a.col_scale = p.col_scale; a.bias = p.bias;
+    a.out = p.out; a.out_type = p.out_type; a.ldo = p.ldo; a.status = status;
+    a.vec = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0 && (p.ldo * type_size(p.out_type)) % 32 == 0;
+    a.wait_prev = p.behind ? 1 : 0;
+    a.splits = 1;
+    CUtensorMap tmA, tmB;
+    const int64_t big = ((p.rows + 255) / 256) * ((p.cols + 255) / 256);
+    cudaLaunchAttribute attr[2];
+    int n_attr = 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    if (p.behind) {
+        attr[n_attr].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n_attr++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (big > kNumSMs / 2) {
+        a.tiles_m = (int)((p.rows + 255) / 256);
+        a.tiles_n = (int)((p.cols + 255) / 256);
+        a.total = a.tiles_m * a.tiles_n;
+        a.band = std::min(a.tiles_m, 8);
+        if (!code_map(&tmA, p.A, p.a_pitch, p.a_rows, 128) || !code_map(&tmB, p.B, p.b_pitch, p.b_rows, 128)) return LBT_ERR_CUDA;
+        cfg.gridDim = dim3((unsigned)(2 * std::min(a.total, kNumSMs / 2)));
+        cfg.blockDim = dim3(kPairThreads);
+        cfg.dynamicSmemBytes = kPairSmem;
+        cfg.numAttrs = n_attr;
+        return cudaLaunchKernelEx(&cfg, l8_pair_kernel, tmA, tmB, a) == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
+    }
+    a.swapped = p.mode == kForward && p.rows <= 128;
+    a.mma_n = a.swapped ? (int)std::min<int64_t>(128, pitch16(p.rows)) : 128;
+    a.stage_bytes = kBox + a.mma_n * kStep;
+    a.stages = std::min(kMaxStages, kRing / a.stage_bytes);
+    a.tiles_m = (int)(((a.swapped ? p.cols : p.rows) + 127) / 128);
+    a.tiles_n = a.swapped ? 1 : (int)((p.cols + 127) / 128);
+    a.total = a.tiles_m * a.tiles_n;
+    a.band = std::min(a.tiles_m, 8);
+    // clusters share a tile until the CTAs fill two per SM, as long as each has four steps of the reduction
+    while (a.splits < 8 && a.total * a.splits * 2 <= 2 * kNumSMs && a.steps >= a.splits * 2 * 4) a.splits *= 2;
+    const void* A = a.swapped ? p.B : p.A;
+    const void* B = a.swapped ? p.A : p.B;
+    if (!code_map(&tmA, A, a.swapped ? p.b_pitch : p.a_pitch, a.swapped ? p.b_rows : p.a_rows, 128) ||
+        !code_map(&tmB, B, a.swapped ? p.a_pitch : p.b_pitch, a.swapped ? p.a_rows : p.b_rows, a.mma_n))
+        return LBT_ERR_CUDA;
+    if (a.splits > 1) {
+        attr[n_attr].id = cudaLaunchAttributeClusterDimension;
+        attr[n_attr].val.clusterDim.x = (unsigned)a.splits;
+        attr[n_attr].val.clusterDim.y = attr[n_attr].val.clusterDim.z = 1;
+        ++n_attr;
+    }
+    cfg.gridDim = dim3((unsigned)(a.total * a.splits));
+    cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = kTileSmem;
+    cfg.numAttrs = n_attr;
+    return cudaLaunchKernelEx(&cfg, l8_tile_kernel, tmA, tmB, a) == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
+}
+
+bool vec_rows(const void* p, int64_t ld, int type) {
+    const size_t bytes = 8 * type_size(type);
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (ld * type_size(type)) % bytes == 0;
+}
+
+template <typename T>
+lbt_status quantize_rows(const T* x, int type, int64_t rows, int64_t cols, int64_t ld, void* q, int64_t ldq, float* scale, cudaStream_t stream) {
+    const bool vec = vec_rows(x, ld, type);
+    uint8_t* dst = static_cast<uint8_t*>(q);
+    if (cols <= 1024) rows8_kernel<T, 32><<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(x, rows, cols, ld, vec, dst, ldq, scale);
+    else rows8_kernel<T, 256><<<(unsigned)rows, 256, 0, stream>>>(x, rows, cols, ld, vec, dst, ldq, scale);
+    return launch_status();
+}
+
+lbt_status quantize_rows_any(const void* x, int type, int64_t rows, int64_t cols, int64_t ld, void* q, int64_t ldq, float* scale, cudaStream_t stream) {
+    if (rows == 0) return LBT_OK;
+    if (type == LBT_F32) return quantize_rows(static_cast<const float*>(x), type, rows, cols, ld, q, ldq, scale, stream);
+    if (type == LBT_BF16) return quantize_rows(static_cast<const __nv_bfloat16*>(x), type, rows, cols, ld, q, ldq, scale, stream);
+    return quantize_rows(static_cast<const __half*>(x), type, rows, cols, ld, q, ldq, scale, stream);
+}
+
+bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+lbt_status check_sizes(int64_t M, int64_t O, int64_t I) {
+    if (M < 0 || O <= 0 || I <= 0) return LBT_ERR_INVALID_ARG;
+    if (M >= (1ll << 31) - 256 || O >= (1ll << 31) - 256 || I >= (1ll << 31) - 256) return LBT_ERR_UNSUPPORTED;
+    return LBT_OK;
+}
+
+struct BackwardSpace {
+    size_t row_most, col_most, cleared, s_r, s_c, sums, q_r, q_c, total;
+};
+
+BackwardSpace backward_space(int64_t M, int64_t O) {
+    auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+    BackwardSpace w{};
+    size_t at = 256;   // slack to align the caller's pointer
+    w.row_most = at; at += up((size_t)M * 4);
+    w.col_most = at; at += up((size_t)O * 4);
+    w.cleared = at - w.row_most;
+    w.s_r = at; at += up((size_t)M * 4);
+    w.s_c = at; at += up((size_t)O * 4);
+    w.sums = at; at += up((size_t)((M + kStrip - 1) / kStrip) * O * 4);
+    w.q_r = at; at += up((size_t)M * pitch16(O));
+    w.q_c = at; at += up((size_t)M * pitch16(O));
+    w.total = at;
+    return w;
+}
+
+template <typename T>
+lbt_status quantize_gradient(const T* dY, int type, int64_t M, int64_t O, int64_t ld, const float* s_w, const float* s_x, uint8_t* base,
+                             const BackwardSpace& w, bool need_r, bool need_c, float* dbias, cudaStream_t stream) {
+    const int64_t ldq = pitch16(O);
+    const bool vec = vec_rows(dY, ld, type);
+    uint32_t* row_most = reinterpret_cast<uint32_t*>(base + w.row_most);
+    uint32_t* col_most = reinterpret_cast<uint32_t*>(base + w.col_most);
+    float* sums = dbias != nullptr ? reinterpret_cast<float*>(base + w.sums) : nullptr;
+    LBT_CUDA_TRY(cudaMemsetAsync(row_most, 0, w.cleared, stream));
+    const dim3 grid((unsigned)((ldq + 255) / 256), (unsigned)((M + kStrip - 1) / kStrip));
+    grad8_stats_kernel<T><<<grid, 256, 0, stream>>>(dY, M, O, ld, vec, s_w, s_x, row_most, col_most, sums);
+    grad8_codes_kernel<T><<<grid, 256, 0, stream>>>(dY, M, O, ld, vec, s_w, s_x, row_most, col_most, sums, need_r ? base + w.q_r : nullptr,
+                                                    need_c ? base + w.q_c : nullptr, ldq, reinterpret_cast<float*>(base + w.s_r),
+                                                    reinterpret_cast<float*>(base + w.s_c), dbias);
+    return launch_status();
+}
+
+}  // namespace
+}  // namespace lbt
+
+using namespace lbt;
+
+extern "C" lbt_status lbt_rows8_quantize(const void* x, int x_type, int64_t rows, int64_t cols, int64_t ld, void* q, int64_t ldq,
+                                         float* scale, void* cuda_stream) {
+    if (rows < 0 || cols <= 0 || ld < cols || ldq < cols || !type_ok(x_type)) return LBT_ERR_INVALID_ARG;
+    if (rows > 0 && (x == nullptr || q == nullptr || scale == nullptr)) return LBT_ERR_INVALID_ARG;
+    if (ldq % 16 != 0 || misaligned(q, 16) || misaligned(x, type_size(x_type)) || misaligned(scale, 4)) return LBT_ERR_ALIGNMENT;
+    if (rows >= (1ll << 31) || cols >= (1ll << 31) - 256) return LBT_ERR_UNSUPPORTED;
+    return quantize_rows_any(x, x_type, rows, cols, ld, q, ldq, scale, as_stream(cuda_stream));
+}
+
+static lbt_status forward_product(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, void* y, int y_type,
+                                  int64_t ldy, int64_t M, int64_t O, int64_t I, bool behind, int32_t* status, cudaStream_t stream) {
+    Product p{};
+    p.mode = kForward;
+    p.A = q_x; p.a_pitch = pitch16(I); p.a_rows = M;
+    p.B = q_w; p.b_pitch = pitch16(I); p.b_rows = O;
+    p.rows = M; p.cols = O; p.red = I;
+    p.row_scale = s_x; p.col_scale = s_w; p.bias = bias;
+    p.out = y; p.out_type = y_type; p.ldo = ldy;
+    p.behind = behind;
+    return launch(p, status, stream);
+}
+
+static lbt_status check_forward(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, const void* y,
+                                int y_type, int64_t ldy, int64_t M, int64_t O, int64_t I) {
+    const lbt_status rc = check_sizes(M, O, I);
+    if (rc != LBT_OK) return rc;
+    if (!type_ok(y_type) || ldy < O || q_w == nullptr || s_w == nullptr) return LBT_ERR_INVALID_ARG;
+    if (M > 0 && (q_x == nullptr || s_x == nullptr || y == nullptr)) return LBT_ERR_INVALID_ARG;
+    if (misaligned(q_x, 16) || misaligned(q_w, 16) || misaligned(s_x, 4) || misaligned(s_w, 4) || misaligned(bias, 4) ||
+        misaligned(y, type_size(y_type)))
+        return LBT_ERR_ALIGNMENT;
+    return I > kMaxReduction ? LBT_ERR_ACC_RANGE : LBT_OK;
+}
+
+extern "C" lbt_status lbt_linear8_forward(const void* x, int x_type, int64_t ldx, const void* q_w, const float* s_w, const float* bias,
+                                          void* y, int y_type, int64_t ldy, int64_t M, int64_t O, int64_t I, void* q_x, float* s_x,
+                                          int32_t* dev_status, void* cuda_stream) {
+    lbt_status rc = check_forward(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I);
+    if (rc != LBT_OK) return rc;
+    if (!type_ok(x_type) || ldx < I || (M > 0 && x == nullptr)) return LBT_ERR_INVALID_ARG;
+    if (misaligned(x, type_size(x_type))) return LBT_ERR_ALIGNMENT;
+    if (M == 0) return LBT_OK;
+    const cudaStream_t stream = as_stream(cuda_stream);
+    rc = quantize_rows_any(x, x_type, M, I, ldx, q_x, pitch16(I), s_x, stream);
+    if (rc != LBT_OK) return rc;
+    return forward_product(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I, true, dev_status, stream);
+}
+
+extern "C" lbt_status lbt_linear8_matmul(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, void* y,
+                                         int y_type, int64_t ldy, int64_t M, int64_t O, int64_t I, int32_t* dev_status, void* cuda_stream) {
+    const lbt_status rc = check_forward(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I);
+    if (rc != LBT_OK || M == 0) return rc;
+    return forward_product(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I, false, dev_status, as_stream(cuda_stream));
+}
+
+extern "C" size_t lbt_linear8_workspace_bytes(int64_t M, int64_t O, int64_t I) {
+    return check_sizes(M, O, I) == LBT_OK ? backward_space(M, O).total : 0;
+}
+
+extern "C" lbt_status lbt_linear8_backward(const void* dY, int dy_type, int64_t lddy, const void* q_w, const float* s_w, const void* q_x,
+                                           const float* s_x, void* dX, int dx_type, int64_t lddx, void* dW, int dw_type, int64_t lddw,
+                                           float* dbias, int64_t M, int64_t O, int64_t I, int32_t* dev_status, void* ws, size_t ws_bytes,
+                                           void* cuda_stream) {
+    lbt_status rc = check_sizes(M, O, I);
+    if (rc != LBT_OK) return rc;
+    if (!type_ok(dy_type) || lddy < O || (dX == nullptr && dW == nullptr && dbias == nullptr)) return LBT_ERR_INVALID_ARG;
+    if (s_w == nullptr || (M > 0 && (dY == nullptr || s_x == nullptr))) return LBT_ERR_INVALID_ARG;
+    if (dX != nullptr && (!type_ok(dx_type) || lddx < I || q_w == nullptr)) return LBT_ERR_INVALID_ARG;
+    if (dW != nullptr && (!type_ok(dw_type) || lddw < I || (M > 0 && q_x == nullptr))) return LBT_ERR_INVALID_ARG;
+    if (misaligned(dY, type_size(dy_type)) || misaligned(q_w, 16) || misaligned(q_x, 16) || misaligned(s_w, 4) || misaligned(s_x, 4) ||
+        (dX != nullptr && misaligned(dX, type_size(dx_type))) || (dW != nullptr && misaligned(dW, type_size(dw_type))) || misaligned(dbias, 4))
+        return LBT_ERR_ALIGNMENT;
+    if ((dX != nullptr && O > kMaxReduction) || (dW != nullptr && M > kMaxReduction)) return LBT_ERR_ACC_RANGE;
+    const BackwardSpace w = backward_space(M, O);
+    if (ws == nullptr || ws_bytes < w.total) return LBT_ERR_WORKSPACE;
+    const cudaStream_t stream = as_stream(cuda_stream);
+    if (M > 65535 * (int64_t)kStrip) return LBT_ERR_UNSUPPORTED;
+    if (M == 0) {   // no tokens: dX is empty, the sums are zero
+        if (dW != nullptr) LBT_CUDA_TRY(cudaMemset2DAsync(dW, (size_t)lddw * type_size(dw_type), 0, (size_t)I * type_size(dw_type), (size_t)O, stream));
+        if (dbias != nullptr) LBT_CUDA_TRY(cudaMemsetAsync(dbias, 0, (size_t)O * 4, stream));
+        return LBT_OK;
+    }
+    uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255) - 256;   // offsets begin at 256
+    if (dy_type == LBT_F32)
+        rc = quantize_gradient(static_cast<const float*>(dY), dy_type, M, O, lddy, s_w, s_x, base, w, dX != nullptr, dW != nullptr, dbias, stream);
+    else if (dy_type == LBT_BF16)
+        rc = quantize_gradient(static_cast<const __nv_bfloat16*>(dY), dy_type, M, O, lddy, s_w, s_x, base, w, dX != nullptr, dW != nullptr, dbias, stream);
+    else
+        rc = quantize_gradient(static_cast<const __half*>(dY), dy_type, M, O, lddy, s_w, s_x, base, w, dX != nullptr, dW != nullptr, dbias, stream);
+    if (rc != LBT_OK) return rc;
+    Product p{};
+    if (dX != nullptr) {
+        p.mode = kDgrad;
+        p.A = base + w.q_r; p.a_pitch = pitch16(O); p.a_rows = M;
+        p.B = q_w; p.b_pitch = pitch16(I); p.b_rows = O;
+        p.rows = M; p.cols = I; p.red = O;
+        p.row_scale = reinterpret_cast<const float*>(base + w.s_r);
+        p.out = dX; p.out_type = dx_type; p.ldo = lddx;
+        rc = launch(p, dev_status, stream);
+        if (rc != LBT_OK) return rc;
+    }
+    if (dW != nullptr) {
+        p = Product{};
+        p.mode = kWgrad;
+        p.A = base + w.q_c; p.a_pitch = pitch16(O); p.a_rows = M;
+        p.B = q_x; p.b_pitch = pitch16(I); p.b_rows = M;
+        p.rows = O; p.cols = I; p.red = M;
+        p.row_scale = reinterpret_cast<const float*>(base + w.s_c);
+        p.out = dW; p.out_type = dw_type; p.ldo = lddw;
+        rc = launch(p, dev_status, stream);
+    }
+    return rc;
+}

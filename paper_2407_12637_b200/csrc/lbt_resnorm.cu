@@ -1,0 +1,646 @@
+// The norm after a block, the block's gate and residual scale, the residual sum and the norm before the next block:
+//
+//   u = N_post(h),   r = scale_x x + scale_h gate u,   y = N_pre(r)
+//   N(v) = w k + b,  k = (v - mu) rstd;  layer norm: mu = mean v, rstd = (mean (v - mu)^2 + eps)^-1/2;  RMS: mu = 0
+//
+// forward: x and h are read once, r and y (or the 8-bit codes and the scale of each row of y) written once.
+// backward: from x, h and the statistics the forward pass kept (four floats a token) everything else is formed again in fp32:
+//   d = dr + N_pre'(dy),  dx = scale_x d,  du = scale_h gate d,  dh = N_post'(du),
+//   N'(g) = rstd (e - [mean e] - k mean(e k)),  e = g w   (the bracket for the layer norm)
+//   dw = sum_rows g k,  db = sum_rows g,  dgate = sum over the gate's rows of scale_h u d.
+// Everything is bound by memory: two reads and two writes an element forward, four and two backward.
+//
+// One group of threads (a warp up to 1024 columns, a block above) owns a row, eight columns of it per thread and vector, so a
+// row's sums are the group's reduction and nothing is read twice.  Sums over rows: a group owns consecutive rows and keeps
+// its columns' sums in registers; a second kernel adds the groups' sums in a fixed order (no atomics: a run repeats bit for bit).
+#include <algorithm>
+
+#include "lbt_types.cuh"
+#include "lbt_sm100.cuh"
+
+namespace lbt {
+
+namespace {
+
+struct Params {   // a parameter vector (weights, biases, gate rows)
+    const void* p;
+    int type;
+    bool vec;
+};
+
+struct NormArgs {
+    int64_t M;
+    int D;
+    int64_t rows_per_gate;
+    bool layer, post, vec;
+    float eps_post, eps_pre, scale_x, scale_h, inv_d;
+    const void *x, *h, *dr, *dy;
+    void *r, *y, *dx, *dh;
+    int64_t ld_x, ld_h, ld_r, ld_y, ld_dr, ld_dy, ld_dx, ld_dh;
+    Params gate, w_post, b_post, w_pre, b_pre;
+    uint8_t* q;
+    int64_t ldq;
+    float* q_scale;
+    float4* stats;
+    // backward
+    int64_t rows_each;      // consecutive rows of a group
+    int64_t parts;          // groups
+    float *part_w_post, *part_b_post, *part_w_pre, *part_b_pre;   // [blocks][D], null where not asked for
+    float *part_gate;       // [parts][2][D]
+    void* dgate;
+};
+
+// Columns [c, c + 8) of an activation row / a parameter vector as fp32 (`fill` behind the end or where there is no vector).
+template <typename T>
+__device__ __forceinline__ void row_load(const T* row, int c, int D, bool vec, float (&f)[8]) {
+    if (vec && c + 8 <= D) {
+        load8(row + c, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = c + i < D ? to_f32(row[c + i]) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void row_store(T* row, int c, int D, bool vec, const float (&f)[8]) {
+    if (vec && c + 8 <= D) {
+        store8(row + c, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < D) row[c + i] = from_f32<T>(f[i]);
+    }
+}
+__device__ __forceinline__ void param_load(const Params& p, int64_t at, int c, int D, float fill, float (&f)[8]) {
+    if (p.p == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = fill;
+    } else if (p.type == LBT_F32) {
+        row_load(static_cast<const float*>(p.p) + at, c, D, p.vec, f);
+    } else if (p.type == LBT_BF16) {
+        row_load(static_cast<const __nv_bfloat16*>(p.p) + at, c, D, p.vec, f);
+    } else {
+        row_load(static_cast<const __half*>(p.p) + at, c, D, p.vec, f);
+    }
+}
+__device__ __forceinline__ void param_store(void* p, int type, int64_t i, float v) {
+    if (type == LBT_F32) static_cast<float*>(p)[i] = v;
+    else if (type == LBT_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+    else static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+
+// Sums (and a maximum) over the kG threads that own a row.  Blocks alternate between two rows of shared memory, so one
+// barrier a reduction is enough.
+template <int kG>
+struct Group {
+    float (*slots)[2][32];   // [2 buffers][2 values][warps]
+    int turn;
+    __device__ __forceinline__ float2 sum(float a, float b) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+            b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+        }
+        if (kG > 32) {
+            float (*s)[32] = slots[turn & 1];
+            ++turn;
+            if ((threadIdx.x & 31) == 0) { s[0][threadIdx.x >> 5] = a; s[1][threadIdx.x >> 5] = b; }
+            __syncthreads();
+            a = b = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kG / 32; ++i) { a += s[0][i]; b += s[1][i]; }
+        }
+        return make_float2(a, b);
+    }
+    __device__ __forceinline__ float sum(float a) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+        if (kG > 32) {
+            float* s = slots[turn & 1][0];
+            ++turn;
+            if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = a;
+            __syncthreads();
+            a = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kG / 32; ++i) a += s[i];
+        }
+        return a;
+    }
+    __device__ __forceinline__ uint32_t most(uint32_t v) {
+        v = __reduce_max_sync(0xFFFFFFFFu, v);
+        if (kG > 32) {
+            uint32_t* s = reinterpret_cast<uint32_t*>(slots[turn & 1][0]);
+            ++turn;
+            if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+            __syncthreads();
+            v = 0;
+#pragma unroll
+            for (int i = 0; i < kG / 32; ++i) v = max(v, s[i]);
+        }
+        return v;
+    }
+};
+
+// Mean and reciprocal deviation of a row held in registers (columns past D hold zeros and are masked).
+template <int kG, int kNV>
+__device__ __forceinline__ void row_stats(Group<kG>& grp, const float (&v)[kNV][8], int t, int D, bool layer, float inv_d, float eps, float& mu, float& rstd) {
+    float s = 0.0f;
+    mu = 0.0f;
+    if (layer) {
+#pragma unroll
+        for (int g = 0; g < kNV; ++g)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[g][i];
+        mu = grp.sum(s) * inv_d;
+        s = 0.0f;
+    }
+#pragma unroll
+    for (int g = 0; g < kNV; ++g)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e = (g * kG + t) * 8 + i < D ? v[g][i] - mu : 0.0f;
+            s += e * e;
+        }
+    rstd = 1.0f / sqrtf(grp.sum(s) * inv_d + eps);
+}
+
+template <typename T, int kG, int kNV>
+__global__ void __launch_bounds__(kG < 256 ? 256 : kG) resnorm_forward_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int kThreads = kG < 256 ? 256 : kG, kRows = kThreads / kG;
+    __shared__ float slots[2][2][32];
+    Group<kG> grp{slots, 0};
+    const int t = threadIdx.x % kG, D = a.D;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kG; row < a.M; row += (int64_t)gridDim.x * kRows) {
+        const T* xs = static_cast<const T*>(a.x) + row * a.ld_x;
+        const T* hs = static_cast<const T*>(a.h) + row * a.ld_h;
+        float h[kNV][8], r[kNV][8];
+#pragma unroll
+        for (int g = 0; g < kNV; ++g) {
+            const int c = (g * kG + t) * 8;
+            row_load(hs, c, D, a.vec, h[g]);
+            row_load(xs, c, D, a.vec, r[g]);
+        }
+        float mu1 = 0.0f, rstd1 = 1.0f, mu2 = 0.0f, rstd2 = 1.0f;
+        if (a.post) row_stats<kG, kNV>(grp, h, t, D, a.layer, a.inv_d, a.eps_post, mu1, rstd1);
+        const int64_t gate_row = row / a.rows_per_gate * D;
+#pragma unroll
+        for (int g = 0; g < kNV; ++g) {
+            const int c = (g * kG + t) * 8;
+            float w[8], b[8], gt[8];
+            param_load(a.w_post, 0, c, D, 1.0f, w);
+            param_load(a.b_post, 0, c, D, 0.0f, b);
+            param_load(a.gate, gate_row, c, D, 1.0f, gt);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float u = a.post ? (h[g][i] - mu1) * rstd1 * w[i] + b[i] : h[g][i];
+                r[g][i] = c + i < D ? a.scale_x * r[g][i] + a.scale_h * (gt[i] * u) : 0.0f;
+            }
+            if (c < D) row_store(static_cast<T*>(a.r) + row * a.ld_r, c, D, a.vec, r[g]);
+        }
+        if (a.y != nullptr || a.q != nullptr) {
+            row_stats<kG, kNV>(grp, r, t, D, a.layer, a.inv_d, a.eps_pre, mu2, rstd2);
+            uint32_t most = 0;
+#pragma unroll
+            for (int g = 0; g < kNV; ++g) {
+                const int c = (g * kG + t) * 8;
+                float w[8], b[8];
+                param_load(a.w_pre, 0, c, D, 1.0f, w);
+                param_load(a.b_pre, 0, c, D, 0.0f, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    r[g][i] = c + i < D ? (r[g][i] - mu2) * rstd2 * w[i] + b[i] : 0.0f;
+                    most = max(most, abs_bits(r[g][i]));
+                }
+                if (a.y != nullptr && c < D) row_store(static_cast<T*>(a.y) + row * a.ld_y, c, D, a.vec, r[g]);
+            }
+            if (a.q != nullptr) {
+                float s, factor;
+                scale8(grp.most(most), s, factor);
+                if (t == 0) a.q_scale[row] = s;
+#pragma unroll
+                for (int g = 0; g < kNV; ++g) {
+                    const int c = (g * kG + t) * 8;
+                    uint32_t k[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) k[i] = code8(r[g][i], factor);
+                    if (c < a.ldq)
+                        *reinterpret_cast<uint2*>(a.q + row * a.ldq + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
+                }
+            }
+        }
+        if (a.stats != nullptr && t == 0) a.stats[row] = make_float4(mu1, rstd1, mu2, rstd2);
+    }
+}
+
+// Adds a group's column sums of one array into what the second kernel adds up: a block's warps (groups of one warp) first meet in
+// shared memory, in order.
+template <int kG, int kNV>
+__device__ __forceinline__ void publish(float* part, const float (&acc)[kNV][8], int t, int D, float* meet) {
+    if (part == nullptr) return;   // uniform
+    constexpr int kRows = kG < 256 ? 256 / kG : 1;
+    float* dst = part + (int64_t)blockIdx.x * D;
+    if constexpr (kRows == 1) {
+#pragma unroll
+        for (int g = 0; g < kNV; ++g)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((g * kG + t) * 8 + i < D) dst[(g * kG + t) * 8 + i] = acc[g][i];
+    } else {
+        for (int w = 0; w < kRows; ++w) {
+            __syncthreads();
+            if ((int)threadIdx.x / kG == w) {
+#pragma unroll
+                for (int g = 0; g < kNV; ++g)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int c = (g * kG + t) * 8 + i;
+                        meet[c] = w == 0 ? acc[g][i] : meet[c] + acc[g][i];
+                    }
+            }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < D; c += blockDim.x) dst[c] = meet[c];
+    }
+}
+
+template <typename T, int kG, int kNV, bool kLayer>
+__global__ void __launch_bounds__(kG < 256 ? 256 : kG) resnorm_backward_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int kThreads = kG < 256 ? 256 : kG, kRows = kThreads / kG;
+    __shared__ float slots[2][2][32];
+    __shared__ float meet[kRows > 1 ? kG * kNV * 8 : 1];
+    Group<kG> grp{slots, 0};
+    const int t = threadIdx.x % kG, D = a.D;
+    const int64_t part = (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
+    const int64_t first = part * a.rows_each, last = min(first + a.rows_each, a.M);
+    float dw1[kNV][8], dw2[kNV][8], dg[kNV][8], db1[kLayer ? kNV : 1][8], db2[kLayer ? kNV : 1][8];
+#pragma unroll
+    for (int g = 0; g < kNV; ++g)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dw1[g][i] = dw2[g][i] = dg[g][i] = 0.0f;
+            if (kLayer) db1[g][i] = db2[g][i] = 0.0f;
+        }
+    for (int64_t row = first; row < last; ++row) {
+        const float4 st = a.stats[row];
+        const int64_t gate_i = row / a.rows_per_gate;
+        float k1[kNV][8], k2[kNV][8], e[kNV][8], d[kNV][8];   // normalised h, normalised r, dy w_pre, dr
+        float s_e = 0.0f, s_ek = 0.0f;
+#pragma unroll
+        for (int g = 0; g < kNV; ++g) {
+            const int c = (g * kG + t) * 8;
+            row_load(static_cast<const T*>(a.h) + row * a.ld_h, c, D, a.vec, k1[g]);
+            row_load(static_cast<const T*>(a.x) + row * a.ld_x, c, D, a.vec, k2[g]);
+            if (a.dy != nullptr) row_load(static_cast<const T*>(a.dy) + row * a.ld_dy, c, D, a.vec, e[g]);
+            if (a.dr != nullptr) row_load(static_cast<const T*>(a.dr) + row * a.ld_dr, c, D, a.vec, d[g]);
+        }
+#pragma unroll
+        for (int g = 0; g < kNV; ++g) {
+            const int c = (g * kG + t) * 8;
+            float w[8], b[8], gt[8], w2[8];
+            param_load(a.w_post, 0, c, D, 1.0f, w);
+            param_load(a.b_post, 0, c, D, 0.0f, b);
+            param_load(a.gate, gate_i * D, c, D, 1.0f, gt);
+            param_load(a.w_pre, 0, c, D, 1.0f, w2);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (a.post) k1[g][i] = (k1[g][i] - st.x) * st.y;
+                const float u = a.post ? k1[g][i] * w[i] + b[i] : k1[g][i];
+                const float r = a.scale_x * k2[g][i] + a.scale_h * (gt[i] * u);
+                k2[g][i] = (r - st.z) * st.w;
+                if (a.dy == nullptr) e[g][i] = 0.0f;
+                if (a.dr == nullptr) d[g][i] = 0.0f;
+                dw2[g][i] += e[g][i] * k2[g][i];
+                if (kLayer) db2[g][i] += e[g][i];
+                e[g][i] *= w2[i];
+                if (c + i < D) {   // columns past the end hold no element
+                    s_e += e[g][i];
+                    s_ek += e[g][i] * k2[g][i];
+                }
+            }
+        }
+        if (a.dy != nullptr) {
+            float mean_e = 0.0f, mean_ek;
+            if (kLayer) {
+                const float2 s = grp.sum(s_e, s_ek);
+                mean_e = s.x * a.inv_d;
+                mean_ek = s.y * a.inv_d;
+            } else {
+                mean_ek = grp.sum(s_ek) * a.inv_d;
+            }
+#pragma unroll
+            for (int g = 0; g < kNV; ++g)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[g][i] += st.w * ((kLayer ? e[g][i] - mean_e : e[g][i]) - k2[g][i] * mean_ek);
+        }
+        s_e = s_ek = 0.0f;
+#pragma unroll
+        for (int g = 0; g < kNV; ++g) {
+            const int c = (g * kG + t) * 8;
+            float w[8], b[8], gt[8], out[8];
+            param_load(a.w_post, 0, c, D, 1.0f, w);
+            param_load(a.b_post, 0, c, D, 0.0f, b);
+            param_load(a.gate, gate_i * D, c, D, 1.0f, gt);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                out[i] = a.scale_x * d[g][i];
+                const float u = a.post ? k1[g][i] * w[i] + b[i] : k1[g][i];
+                const float du = a.scale_h * (gt[i] * d[g][i]);
+                dg[g][i] += a.scale_h * (u * d[g][i]);
+                dw1[g][i] += du * k1[g][i];
+                if (kLayer) db1[g][i] += du;
+                e[g][i] = a.post ? du * w[i] : du;
+                if (c + i < D) {
+                    s_e += e[g][i];
+                    s_ek += e[g][i] * k1[g][i];
+                }
+            }
+            if (c < D) row_store(static_cast<T*>(a.dx) + row * a.ld_dx, c, D, a.vec, out);
+        }
+        float mean_e = 0.0f, mean_ek = 0.0f;
+        if (a.post) {
+            if (kLayer) {
+                const float2 s = grp.sum(s_e, s_ek);
+                mean_e = s.x * a.inv_d;
+                mean_ek = s.y * a.inv_d;
+            } else {
+                mean_ek = grp.sum(s_ek) * a.inv_d;
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < kNV; ++g) {
+            const int c = (g * kG + t) * 8;
+            float out[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[i] = a.post ? st.y * ((kLayer ? e[g][i] - mean_e : e[g][i]) - k1[g][i] * mean_ek) : e[g][i];
+            if (c < D) row_store(static_cast<T*>(a.dh) + row * a.ld_dh, c, D, a.vec, out);
+        }
+        // the gate row's last row, or the group's: its sum leaves (whole gate rows at once, shared ones through the second kernel)
+        if (a.dgate != nullptr && (row + 1 == last || (row + 1) / a.rows_per_gate != gate_i)) {
+            const int64_t g0 = gate_i * a.rows_per_gate, g1 = min(g0 + a.rows_per_gate, a.M);
+            const bool whole = g0 >= first && g1 <= last;
+            float* shared_part = a.part_gate + (part * 2 + (gate_i == first / a.rows_per_gate ? 0 : 1)) * D;
+#pragma unroll
+            for (int g = 0; g < kNV; ++g)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = (g * kG + t) * 8 + i;
+                    if (c < D) {
+                        if (whole) param_store(a.dgate, a.gate.type, gate_i * D + c, dg[g][i]);
+                        else shared_part[c] = dg[g][i];
+                    }
+                    dg[g][i] = 0.0f;
+                }
+        }
+    }
+    publish<kG, kNV>(a.part_w_pre, dw2, t, D, meet);
+    publish<kG, kNV>(a.part_w_post, dw1, t, D, meet);
+    if (kLayer) {
+        publish<kLayer ? kG : 32, kLayer ? kNV : 1>(a.part_b_pre, db2, t, D, meet);
+        publish<kLayer ? kG : 32, kLayer ? kNV : 1>(a.part_b_post, db1, t, D, meet);
+    }
+}
+
+// Second kernel of the backward pass: column sums over the blocks' partial sums, and the gate rows that several groups share.
+// blockIdx.y: which array, then which border between two groups (a shared gate row belongs to the first border inside it);
+// 32 columns a block, eight threads a column, added in a fixed order.
+struct FinishArgs {
+    int D;
+    int blocks;
+    const float* part[4];
+    void* out[4];
+    int arrays;
+    int type;
+    // gates
+    const float* part_gate;
+    void* dgate;
+    int gate_type;
+    int64_t M, rows_per_gate, rows_each;
+};
+
+__global__ void __launch_bounds__(256) resnorm_finish_kernel(const __grid_constant__ FinishArgs f) {
+    __shared__ float meet[8][33];
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    int64_t gate = 0;
+    if ((int)blockIdx.y < f.arrays) {
+        const float* p = f.part[blockIdx.y];
+        if (c < f.D)
+            for (int b = y; b < f.blocks; b += 8) s += p[(int64_t)b * f.D + c];
+    } else {
+        const int64_t border = (int64_t)blockIdx.y - f.arrays + 1;
+        gate = border * f.rows_each / f.rows_per_gate;
+        const int64_t g0 = gate * f.rows_per_gate, g1 = min(g0 + f.rows_per_gate, f.M);
+        const int64_t p0 = g0 / f.rows_each, p1 = (g1 - 1) / f.rows_each;
+        if (g0 == border * f.rows_each || p0 != border - 1) return;   // it begins here, or an earlier border is inside it
+        if (c < f.D)
+            for (int64_t p = p0 + y; p <= p1; p += 8) s += f.part_gate[(p * 2 + (gate == p * f.rows_each / f.rows_per_gate ? 0 : 1)) * f.D + c];
+    }
+    meet[y][lane] = s;
+    __syncthreads();
+    if (y != 0 || c >= f.D) return;
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += meet[i][lane];
+    if ((int)blockIdx.y < f.arrays) param_store(f.out[blockIdx.y], f.type, c, s);
+    else param_store(f.dgate, f.gate_type, gate * f.D + c, s);
+}
+
+// ------------------------------------------------------------------------------------------ host
+constexpr int kMaxD = 32768;
+
+// Threads of a row and blocks in flight per SM.
+int group_threads(int D) { return D <= 1024 ? 32 : D <= 4096 ? 256 : D <= 8192 ? 512 : 1024; }
+
+struct Split {
+    int64_t rows_each, parts;
+    int blocks;
+};
+// How the backward pass deals rows out: consecutive rows to each group, about two blocks per SM.
+Split split_rows(int64_t M, int D) {
+    const int g = group_threads(D), rows = g < 256 ? 256 / g : 1;
+    const int64_t most = (int64_t)kNumSMs * (g >= 512 ? 1 : 2) * rows;
+    Split s;
+    s.rows_each = std::max<int64_t>(1, (M + most - 1) / most);
+    s.parts = (M + s.rows_each - 1) / s.rows_each;
+    s.blocks = (int)((s.parts + rows - 1) / rows);
+    return s;
+}
+
+struct NormSpace {
+    size_t w_post, b_post, w_pre, b_pre, gate, total;
+};
+NormSpace norm_space(int64_t M, int D) {
+    const Split s = split_rows(M, D);
+    auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+    const size_t one = up((size_t)s.blocks * D * 4);
+    NormSpace w{};
+    size_t at = 256;
+    w.w_post = at; at += one;
+    w.b_post = at; at += one;
+    w.w_pre = at; at += one;
+    w.b_pre = at; at += one;
+    w.gate = at; at += up((size_t)s.parts * 2 * D * 4);
+    w.total = at;
+    return w;
+}
+
+template <typename T>
+lbt_status run_forward(const NormArgs& a, cudaStream_t stream) {
+    const int g = group_threads(a.D), threads = g < 256 ? 256 : g, rows = threads / g;
+    const int64_t blocks = std::min<int64_t>((a.M + rows - 1) / rows, 1 << 30);
+    const dim3 grid((unsigned)blocks), block((unsigned)threads);
+    if (a.D <= 256) resnorm_forward_kernel<T, 32, 1><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 512) resnorm_forward_kernel<T, 32, 2><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 1024) resnorm_forward_kernel<T, 32, 4><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 2048) resnorm_forward_kernel<T, 256, 1><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 4096) resnorm_forward_kernel<T, 256, 2><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 8192) resnorm_forward_kernel<T, 512, 2><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 16384) resnorm_forward_kernel<T, 1024, 2><<<grid, block, 0, stream>>>(a);
+    else resnorm_forward_kernel<T, 1024, 4><<<grid, block, 0, stream>>>(a);
+    return launch_status();
+}
+
+template <typename T, bool kLayer>
+lbt_status run_backward(const NormArgs& a, const Split& s, cudaStream_t stream) {
+    const int g = group_threads(a.D);
+    const dim3 grid((unsigned)s.blocks), block((unsigned)(g < 256 ? 256 : g));
+    if (a.D <= 256) resnorm_backward_kernel<T, 32, 1, kLayer><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 512) resnorm_backward_kernel<T, 32, 2, kLayer><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 1024) resnorm_backward_kernel<T, 32, 4, kLayer><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 2048) resnorm_backward_kernel<T, 256, 1, kLayer><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 4096) resnorm_backward_kernel<T, 256, 2, kLayer><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 8192) resnorm_backward_kernel<T, 512, 2, kLayer><<<grid, block, 0, stream>>>(a);
+    else if (a.D <= 16384) resnorm_backward_kernel<T, 1024, 2, kLayer><<<grid, block, 0, stream>>>(a);
+    else resnorm_backward_kernel<T, 1024, 4, kLayer><<<grid, block, 0, stream>>>(a);
+    return launch_status();
+}
+
+bool off(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+// What forward and backward check and set up alike.
+lbt_status common(const lbt_resnorm_desc* d, NormArgs* a) {
+    if (d == nullptr || d->M < 0 || d->D <= 0 || !type_ok(d->type) || !type_ok(d->param_type)) return LBT_ERR_INVALID_ARG;
+    if (d->kind != LBT_NORM_RMS && d->kind != LBT_NORM_LAYER) return LBT_ERR_INVALID_ARG;
+    if (d->rows_per_gate < 0 || !(d->eps_post >= 0.0f) || !(d->eps_pre >= 0.0f)) return LBT_ERR_INVALID_ARG;
+    if (d->D > kMaxD || d->M >= (1ll << 40)) return LBT_ERR_UNSUPPORTED;
+    a->M = d->M;
+    a->D = (int)d->D;
+    a->rows_per_gate = d->rows_per_gate == 0 ? std::max<int64_t>(d->M, 1) : d->rows_per_gate;
+    a->layer = d->kind == LBT_NORM_LAYER;
+    a->post = d->post_norm != 0;
+    a->eps_post = d->eps_post; a->eps_pre = d->eps_pre; a->scale_x = d->scale_x; a->scale_h = d->scale_h;
+    a->inv_d = 1.0f / (float)d->D;
+    const int64_t* ld = &d->ld_x;
+    int64_t* to[8] = {&a->ld_x, &a->ld_h, &a->ld_r, &a->ld_y, &a->ld_dr, &a->ld_dy, &a->ld_dx, &a->ld_dh};
+    for (int i = 0; i < 8; ++i) {
+        if (ld[i] != 0 && ld[i] < d->D) return LBT_ERR_INVALID_ARG;
+        *to[i] = ld[i] != 0 ? ld[i] : d->D;
+    }
+    a->vec = true;
+    return LBT_OK;
+}
+
+bool vec_ok(const void* p, int64_t ld, int type) {
+    const size_t bytes = 8 * type_size(type);
+    return p == nullptr || (!off(p, bytes) && (ld * type_size(type)) % bytes == 0);
+}
+Params make_param(const void* p, int type, int64_t D) {
+    return Params{p, type, vec_ok(p, D, type)};
+}
+
+}  // namespace
+}  // namespace lbt
+
+using namespace lbt;
+
+extern "C" lbt_status lbt_resnorm_forward(const lbt_resnorm_desc* d, const void* x, const void* h, const void* gate, const void* w_post,
+                                          const void* b_post, const void* w_pre, const void* b_pre, void* r, void* y, void* q, int64_t ldq,
+                                          float* q_scale, float* stats, void* cuda_stream) {
+    NormArgs a{};
+    const lbt_status rc = common(d, &a);
+    if (rc != LBT_OK) return rc;
+    if (q != nullptr && (q_scale == nullptr || ldq < a.D)) return LBT_ERR_INVALID_ARG;
+    if (a.M > 0 && (x == nullptr || h == nullptr || r == nullptr)) return LBT_ERR_INVALID_ARG;
+    const size_t e = type_size(d->type), pe = type_size(d->param_type);
+    if (off(x, e) || off(h, e) || off(r, e) || off(y, e) || off(gate, pe) || off(w_post, pe) || off(b_post, pe) || off(w_pre, pe) ||
+        off(b_pre, pe) || off(q, 16) || (q != nullptr && ldq % 16 != 0) || off(q_scale, 4) || off(stats, 16))
+        return LBT_ERR_ALIGNMENT;
+    if (a.M == 0) return LBT_OK;
+    a.x = x; a.h = h; a.r = r; a.y = y;
+    a.vec = vec_ok(x, a.ld_x, d->type) && vec_ok(h, a.ld_h, d->type) && vec_ok(r, a.ld_r, d->type) && vec_ok(y, a.ld_y, d->type);
+    a.gate = make_param(gate, d->param_type, a.D);
+    a.w_post = make_param(w_post, d->param_type, a.D); a.b_post = make_param(b_post, d->param_type, a.D);
+    a.w_pre = make_param(w_pre, d->param_type, a.D); a.b_pre = make_param(b_pre, d->param_type, a.D);
+    // codes: a row is padded with zeros up to the next multiple of 16 columns
+    a.q = static_cast<uint8_t*>(q); a.ldq = ldq; a.q_scale = q_scale;
+    a.stats = reinterpret_cast<float4*>(stats);
+    const cudaStream_t stream = as_stream(cuda_stream);
+    if (d->type == LBT_F32) return run_forward<float>(a, stream);
+    if (d->type == LBT_BF16) return run_forward<__nv_bfloat16>(a, stream);
+    return run_forward<__half>(a, stream);
+}
+
+extern "C" size_t lbt_resnorm_workspace_bytes(const lbt_resnorm_desc* d) {
+    NormArgs a{};
+    return common(d, &a) == LBT_OK ? norm_space(a.M, a.D).total : 0;
+}
+
+extern "C" lbt_status lbt_resnorm_backward(const lbt_resnorm_desc* d, const void* dr, const void* dy, const void* x, const void* h,
+                                           const void* gate, const void* w_post, const void* b_post, const void* w_pre, const float* stats,
+                                           void* dx, void* dh, void* dgate, void* dw_post, void* db_post, void* dw_pre, void* db_pre,
+                                           void* ws, size_t ws_bytes, void* cuda_stream) {
+    NormArgs a{};
+    lbt_status rc = common(d, &a);
+    if (rc != LBT_OK) return rc;
+    if (a.M > 0 && (x == nullptr || h == nullptr || stats == nullptr || dx == nullptr || dh == nullptr || (dr == nullptr && dy == nullptr)))
+        return LBT_ERR_INVALID_ARG;
+    if (dgate != nullptr && gate == nullptr) return LBT_ERR_INVALID_ARG;
+    if (!a.post && (dw_post != nullptr || db_post != nullptr)) return LBT_ERR_INVALID_ARG;
+    if (!a.layer && (db_post != nullptr || db_pre != nullptr)) return LBT_ERR_INVALID_ARG;
+    const size_t e = type_size(d->type), pe = type_size(d->param_type);
+    if (off(dr, e) || off(dy, e) || off(x, e) || off(h, e) || off(dx, e) || off(dh, e) || off(gate, pe) || off(w_post, pe) || off(b_post, pe) ||
+        off(w_pre, pe) || off(dgate, pe) || off(dw_post, pe) || off(db_post, pe) || off(dw_pre, pe) || off(db_pre, pe) || off(stats, 16))
+        return LBT_ERR_ALIGNMENT;
+    const NormSpace w = norm_space(a.M, a.D);
+    if (ws == nullptr || ws_bytes < w.total) return LBT_ERR_WORKSPACE;
+    const cudaStream_t stream = as_stream(cuda_stream);
+    void* outs[4] = {dw_post, db_post, dw_pre, db_pre};
+    if (a.M == 0) {   // no rows: the sums are zero (and there are no gate rows)
+        for (void* o : outs)
+            if (o != nullptr) LBT_CUDA_TRY(cudaMemsetAsync(o, 0, (size_t)a.D * pe, stream));
+        return LBT_OK;
+    }
+    uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255) - 256;
+    const Split s = split_rows(a.M, a.D);
+    a.dr = dr; a.dy = dy; a.x = x; a.h = h; a.dx = dx; a.dh = dh;
+    a.vec = vec_ok(dr, a.ld_dr, d->type) && vec_ok(dy, a.ld_dy, d->type) && vec_ok(x, a.ld_x, d->type) && vec_ok(h, a.ld_h, d->type) &&
+            vec_ok(dx, a.ld_dx, d->type) && vec_ok(dh, a.ld_dh, d->type);
+    a.gate = make_param(gate, d->param_type, a.D);
+    a.w_post = make_param(w_post, d->param_type, a.D); a.b_post = make_param(b_post, d->param_type, a.D);
+    a.w_pre = make_param(w_pre, d->param_type, a.D);
+    a.stats = reinterpret_cast<float4*>(const_cast<float*>(stats));
+    a.rows_each = s.rows_each; a.parts = s.parts;
+    auto at = [&](size_t o, void* wanted) { return wanted != nullptr ? reinterpret_cast<float*>(base + o) : nullptr; };
+    a.part_w_post = at(w.w_post, dw_post); a.part_b_post = at(w.b_post, db_post);
+    a.part_w_pre = at(w.w_pre, dw_pre); a.part_b_pre = at(w.b_pre, db_pre);
+    a.part_gate = reinterpret_cast<float*>(base + w.gate);
+    a.dgate = dgate;
+    if (d->type == LBT_F32) rc = a.layer ? run_backward<float, true>(a, s, stream) : run_backward<float, false>(a, s, stream);
+    else if (d->type == LBT_BF16) rc = a.layer ? run_backward<__nv_bfloat16, true>(a, s, stream) : run_backward<__nv_bfloat16, false>(a, s, stream);
+    else rc = a.layer ? run_backward<__half, true>(a, s, stream) : run_backward<__half, false>(a, s, stream);
+    if (rc != LBT_OK) return rc;
+    FinishArgs f{};
+    f.D = a.D; f.blocks = s.blocks; f.type = d->param_type;
+    const float* parts[4] = {a.part_w_post, a.part_b_post, a.part_w_pre, a.part_b_pre};
+    for (int i = 0; i < 4; ++i)
+        if (outs[i] != nullptr) { f.part[f.arrays] = parts[i]; f.out[f.arrays++] = outs[i]; }
+    int64_t borders = 0;   // between two groups: at most one gate row each
+    if (dgate != nullptr) {
+        borders = s.parts - 1;
+        f.part_gate = a.part_gate; f.dgate = dgate; f.gate_type = d->param_type;
+        f.M = a.M; f.rows_per_gate = a.rows_per_gate; f.rows_each = a.rows_each;
+    }
+    if (f.arrays + borders == 0) return LBT_OK;
+    resnorm_finish_kernel<<<dim3((unsigned)((a.D + 31) / 32), (unsigned)(f.arrays + borders)), 256, 0, stream>>>(f);
+    return launch_status();
+}

@@ -30,6 +30,8 @@ EXPORTS = (
     "lbt_quantize_weight", "lbt_quantize_act", "lbt_qgemm_forward", "lbt_qconv_forward",
     "lbt_quantize_grad_shard", "lbt_dequantize_acc", "lbt_quantize_grad_fused",
     "lbt_grad_diagnostics", "lbt_diagnostics_workspace_bytes",
+    "lbt_rows8_quantize", "lbt_linear8_forward", "lbt_linear8_matmul", "lbt_linear8_backward", "lbt_linear8_workspace_bytes",
+    "lbt_resnorm_forward", "lbt_resnorm_backward", "lbt_resnorm_workspace_bytes", "lbt_adamw_step",
     "lbt_set_timing_events", "lbt_selftest_wait_timeout", "lbt_selftest_barrier_timeout", "lbt_status_string",
 )
 TIME_STATS, TIME_QUANTIZE, TIME_EXPAND, TIME_DGRAD, TIME_WGRAD, TIME_FORWARD, TIME_FWD_QUANT = range(7)
@@ -56,6 +58,33 @@ class GradDiag(C.Structure):
                 ("sum_all", C.c_double), ("sum_large_in", C.c_double), ("sum_large_out", C.c_double),
                 ("e_all", C.c_double), ("e_large", C.c_double), ("u_large", C.c_double),
                 ("threshold", C.c_float), ("reserved", C.c_uint32)]
+
+
+F32, BF16, F16 = range(3)
+TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+NORM_RMS, NORM_LAYER = range(2)
+MAX_REDUCTION8 = 133144   # longest sum of products of 8-bit codes that fits int32
+ADAMW_BLOCK = 256         # elements that share a scale of 8-bit moments
+
+
+class ResnormDesc(C.Structure):
+    """Mirror of `lbt_resnorm_desc`; leading dimensions 0 = D."""
+    _fields_ = [("M", C.c_int64), ("D", C.c_int64), ("rows_per_gate", C.c_int64),
+                ("type", C.c_int32), ("param_type", C.c_int32), ("kind", C.c_int32), ("post_norm", C.c_int32),
+                ("eps_post", C.c_float), ("eps_pre", C.c_float), ("scale_x", C.c_float), ("scale_h", C.c_float),
+                *[("ld_" + k, C.c_int64) for k in ("x", "h", "r", "y", "dr", "dy", "dx", "dh")]]
+
+
+class AdamwTensor(C.Structure):
+    """Mirror of `lbt_adamw_tensor` (80 bytes)."""
+    _fields_ = [*[(k, C.c_void_p) for k in ("p", "g", "m", "v", "m_scale", "v_scale")], ("n", C.c_uint64),
+                ("lr", C.c_double), ("weight_decay", C.c_double), ("p_type", C.c_int32), ("g_type", C.c_int32)]
+
+
+class AdamwHyper(C.Structure):
+    """Mirror of `lbt_adamw_hyper` (40 bytes)."""
+    _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
+                ("state_bits", C.c_int32), ("reserved", C.c_int32)]
 
 
 class GemmDesc(C.Structure):
@@ -114,13 +143,20 @@ def lib() -> C.CDLL:
         l.lbt_qconv_dgrad_wgrad.argtypes = [vp] * 11 + [i32, i32, i32, vp, vp, sz, vp]
         l.lbt_qconv_backward.argtypes = [vp] * 13 + [i32, vp, sz, vp]
         l.lbt_qconv_backward_ex.argtypes = [vp] * 13 + [i32, vp, sz, i32, vp, vp]
+        l.lbt_rows8_quantize.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp]
+        l.lbt_linear8_forward.argtypes = [vp, i32, i64, vp, vp, vp, vp, i32, i64, i64, i64, i64, vp, vp, vp, vp]
+        l.lbt_linear8_matmul.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, vp, vp]
+        l.lbt_linear8_backward.argtypes = [vp, i32, i64, vp, vp, vp, vp, vp, i32, i64, vp, i32, i64, vp, i64, i64, i64, vp, vp, sz, vp]
+        l.lbt_linear8_workspace_bytes.argtypes = [i64, i64, i64]
+        l.lbt_resnorm_forward.argtypes = [vp] * 11 + [i64, vp, vp, vp]
+        l.lbt_resnorm_backward.argtypes = [vp] * 18 + [sz, vp]
+        l.lbt_resnorm_workspace_bytes.argtypes = [vp]
+        l.lbt_adamw_step.argtypes = [vp, i32, vp, vp, vp, vp]
         l.lbt_set_timing_events.argtypes = [i32, vp, vp]
         l.lbt_selftest_wait_timeout.argtypes = [vp, C.c_uint32, vp]
         l.lbt_selftest_barrier_timeout.argtypes = [vp, C.c_uint32, vp]
         for name in EXPORTS:
-            if name not in ("lbt_workspace_bytes", "lbt_status_string", "lbt_diagnostics_workspace_bytes"):
-                getattr(l, name).restype = C.c_int32
-        l.lbt_diagnostics_workspace_bytes.restype = sz
+            getattr(l, name).restype = sz if name.endswith("workspace_bytes") else C.c_int32
         l.lbt_status_string.restype = C.c_char_p
         l.lbt_status_string.argtypes = [C.c_int32]
         _lib = l
@@ -290,6 +326,118 @@ def quantize_grad_fused(dY, state, stats, q_out, stream=None):
     """Statistics, quantization and the clipping-factor update in one cooperative launch."""
     _check(lib().lbt_quantize_grad_fused(_p(dY), dY.numel(), _p(state), _p(stats), _p(q_out), _stream(stream)),
            "lbt_quantize_grad_fused")
+
+
+def _rows(t, name, cols=None):
+    """Address, element type and leading dimension of a [rows, cols] CUDA tensor whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 2 or t.dtype not in TYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows")
+    if cols is not None and t.shape[1] != cols:
+        raise ValueError(f"{name}: {t.shape[1]} columns, {cols} expected")
+    # (one row, or rows that overlap by a stride of 0 as an expanded tensor has: the latter is refused by the library)
+    return t.data_ptr(), TYPES[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _scratch(nbytes, device, stream):
+    """Workspace from torch's allocator, which hands it on in the order of the stream that uses it."""
+    with torch.cuda.stream(stream):   # None: the current stream
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def pitch8(cols: int) -> int:
+    """Bytes of one row of 8-bit codes: `cols` rounded up to 16."""
+    return (cols + 15) // 16 * 16
+
+
+def _codes(q, rows, cols, name):
+    if q.dtype != torch.int8 or tuple(q.shape) != (rows, pitch8(cols)):
+        raise ValueError(f"{name}: an int8 tensor of {rows} x {pitch8(cols)} codes")
+    return _p(q)
+
+
+def _floats(t, n, name):
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or t.numel() != n:
+        raise ValueError(f"{name}: {n} fp32 values")
+    return _p(t)
+
+
+def rows8_quantize(x, q, scale, stream=None):
+    """8-bit codes and a scale of each row of x [rows, cols]; q: int8 [rows, pitch8(cols)], scale: fp32 [rows]."""
+    px, tx, ld = _rows(x, "x")
+    rows, cols = x.shape
+    _check(lib().lbt_rows8_quantize(px, tx, rows, cols, ld, _codes(q, rows, cols, "q"), pitch8(cols), _floats(scale, rows, "scale"),
+                                    _stream(stream)), "lbt_rows8_quantize")
+
+
+def linear8_forward(x, q_w, s_w, y, q_x, s_x, bias=None, dev_status=None, stream=None):
+    """y = x W^T (+ bias) on 8-bit codes; leaves x's codes and scales in q_x, s_x."""
+    M, I = x.shape
+    O = s_w.numel()
+    px, tx, ldx = _rows(x, "x")
+    py, ty, ldy = _rows(y, "y", O)
+    if y.shape[0] != M:
+        raise ValueError("y: one row per row of x")
+    _check(lib().lbt_linear8_forward(px, tx, ldx, _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"), _floats(bias, O, "bias"), py, ty, ldy,
+                                     M, O, I, _codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _p(dev_status), _stream(stream)),
+           "lbt_linear8_forward")
+
+
+def linear8_matmul(q_x, s_x, q_w, s_w, y, I, bias=None, dev_status=None, stream=None):
+    """y from codes: q_x [M, pitch8(I)], s_x [M], q_w [O, pitch8(I)], s_w [O]."""
+    M, O = s_x.numel(), s_w.numel()
+    py, ty, ldy = _rows(y, "y", O)
+    if y.shape[0] != M:
+        raise ValueError("y: one row per row of codes")
+    _check(lib().lbt_linear8_matmul(_codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"),
+                                    _floats(bias, O, "bias"), py, ty, ldy, M, O, I, _p(dev_status), _stream(stream)), "lbt_linear8_matmul")
+
+
+def linear8_workspace_bytes(M, O, I) -> int:
+    return int(lib().lbt_linear8_workspace_bytes(M, O, I))
+
+
+def linear8_backward(dY, q_w, s_w, q_x, s_x, I, dX=None, dW=None, dbias=None, ws=None, dev_status=None, stream=None):
+    """Gradients of linear8_forward from the codes it left; outputs that are None are not computed.  ws None: from torch's allocator."""
+    M, O = dY.shape
+    pg, tg, ldg = _rows(dY, "dY", s_w.numel())
+    px, tx, ldx = _rows(dX, "dX", I) if dX is not None else (0, F32, I)
+    pw, tw, ldw = _rows(dW, "dW", I) if dW is not None else (0, F32, I)
+    if (dX is not None and dX.shape[0] != M) or (dW is not None and dW.shape[0] != O):
+        raise ValueError("dX: one row per row of dY; dW: one row per column of dY")
+    if ws is None:
+        ws = _scratch(linear8_workspace_bytes(M, O, I), dY.device, stream)
+    _check(lib().lbt_linear8_backward(pg, tg, ldg, _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"), _codes(q_x, M, I, "q_x"),
+                                      _floats(s_x, M, "s_x"), px, tx, ldx, pw, tw, ldw, _floats(dbias, O, "dbias"), M, O, I, _p(dev_status),
+                                      _p(ws), ws.numel(), _stream(stream)), "lbt_linear8_backward")
+
+
+def resnorm_forward(desc, x, h, gate, w_post, b_post, w_pre, b_pre, r, y=None, q=None, q_scale=None, stats=None, stream=None):
+    """`lbt_resnorm_forward` on tensors that match `desc` (marshalling only: lm.ResNorm builds and checks them)."""
+    _check(lib().lbt_resnorm_forward(C.addressof(desc), x.data_ptr(), h.data_ptr(), _p(gate), _p(w_post), _p(b_post), _p(w_pre), _p(b_pre),
+                                     r.data_ptr(), y.data_ptr() if y is not None else 0, _p(q), q.shape[1] if q is not None else 0, _p(q_scale),
+                                     _p(stats), _stream(stream)), "lbt_resnorm_forward")
+
+
+def resnorm_workspace_bytes(desc) -> int:
+    return int(lib().lbt_resnorm_workspace_bytes(C.addressof(desc)))
+
+
+def resnorm_backward(desc, dr, dy, x, h, gate, w_post, b_post, w_pre, stats, dx, dh, dgate=None, dw_post=None, db_post=None, dw_pre=None,
+                     db_pre=None, ws=None, stream=None):
+    """`lbt_resnorm_backward` on tensors that match `desc`.  ws None: from torch's allocator."""
+    if ws is None:
+        ws = _scratch(resnorm_workspace_bytes(desc), x.device, stream)
+    _check(lib().lbt_resnorm_backward(C.addressof(desc), dr.data_ptr() if dr is not None else 0, dy.data_ptr() if dy is not None else 0,
+                                      x.data_ptr(), h.data_ptr(), _p(gate), _p(w_post), _p(b_post), _p(w_pre), _p(stats), dx.data_ptr(),
+                                      dh.data_ptr(), _p(dgate), _p(dw_post), _p(db_post), _p(dw_pre), _p(db_pre), _p(ws), ws.numel(),
+                                      _stream(stream)), "lbt_resnorm_backward")
+
+
+def adamw_step(table, hyper, grad_scale=None, skip=None, stream=None):
+    """One AdamW step over a ctypes array of AdamwTensor."""
+    _check(lib().lbt_adamw_step(table, len(table), C.addressof(hyper), _p(grad_scale), _p(skip), _stream(stream)), "lbt_adamw_step")
 
 
 def grad_diagnostics(dY, q_codes, bits, alpha, stats, ws=None, stream=None) -> "GradDiag":

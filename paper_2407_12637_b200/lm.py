@@ -1,0 +1,232 @@
+"""Layers of a transformer's residual block on the library's kernels: `Linear8`, `ResNorm` and `AdamW`.
+
+Each object keeps what a program keeps between calls (weight codes, parameters, moments) and the plan of its calls; every
+step of arithmetic runs in the library (`lbt`).  Outputs may be handed in (`out`); otherwise they come from torch's
+allocator.  Work is enqueued on `stream` (default: torch's current stream); tensors that another stream made need that
+stream's event first, as with any torch call.
+"""
+from __future__ import annotations
+
+import contextlib
+
+import torch
+
+from . import lbt
+
+
+def _on(stream):
+    """Scratch and outputs of a call belong to the stream that uses them."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+class Linear8:
+    """A linear layer y = x W^T + b whose three products run on 8-bit integers, with a scale for each output channel of W and
+    for each token of x (and of the gradient)."""
+
+    def __init__(self, in_features: int, out_features: int, bias=None, weight=None, device="cuda"):
+        if in_features < 1 or out_features < 1:
+            raise ValueError("in_features and out_features are positive")
+        self.I, self.O, self.bias = int(in_features), int(out_features), bias
+        self.q_w = torch.zeros(self.O, lbt.pitch8(self.I), dtype=torch.int8, device=device)
+        self.s_w = torch.zeros(self.O, dtype=torch.float32, device=device)
+        self.kept = None
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)   # lbt.ERR_TIMEOUT if a bounded on-chip wait ran out
+        if weight is not None:
+            self.load_weight(weight)
+
+    @classmethod
+    def from_codes(cls, q_w, s_w, in_features: int, bias=None):
+        """A served layer: codes [O, in_features rounded up to 16] (zeros behind in_features) and scales [O] as they are."""
+        self = cls.__new__(cls)
+        self.I, self.O, self.bias = int(in_features), s_w.numel(), bias
+        lbt._codes(q_w, self.O, self.I, "q_w")
+        lbt._floats(s_w, self.O, "s_w")
+        lbt._floats(bias, self.O, "bias")
+        self.q_w, self.s_w, self.kept = q_w, s_w, None
+        self.status = torch.zeros(1, dtype=torch.int32, device=q_w.device)
+        return self
+
+    def load_weight(self, weight, stream=None):
+        """Quantizes the weights [O, I] (after each optimizer step)."""
+        if tuple(weight.shape) != (self.O, self.I):
+            raise ValueError(f"weight: {self.O} x {self.I}")
+        lbt.rows8_quantize(weight, self.q_w, self.s_w, stream)
+
+    def forward(self, x, out=None, keep=False, stream=None):
+        """y for x [M, I]; keep: the codes of x stay for `backward`."""
+        if x.dim() != 2 or x.shape[1] != self.I:
+            raise ValueError(f"x: rows of {self.I} values")
+        M = x.shape[0]
+        with _on(stream):
+            y = torch.empty(M, self.O, dtype=x.dtype, device=x.device) if out is None else out
+            q_x = torch.empty(M, lbt.pitch8(self.I), dtype=torch.int8, device=x.device)
+            s_x = torch.empty(M, dtype=torch.float32, device=x.device)
+        lbt.linear8_forward(x, self.q_w, self.s_w, y, q_x, s_x, self.bias, self.status, stream)
+        if keep:
+            self.kept = (q_x, s_x)
+        return y
+
+    def forward_codes(self, q_x, s_x, out=None, dtype=torch.bfloat16, keep=False, stream=None):
+        """y from codes and scales that another operator made (ResNorm.forward_codes)."""
+        with _on(stream):
+            y = torch.empty(s_x.numel(), self.O, dtype=dtype, device=q_x.device) if out is None else out
+        lbt.linear8_matmul(q_x, s_x, self.q_w, self.s_w, y, self.I, self.bias, self.status, stream)
+        if keep:
+            self.kept = (q_x, s_x)
+        return y
+
+    def backward(self, dy, need_dx=True, need_dw=True, dw_dtype=torch.float32, dx=None, dw=None, dbias=None, stream=None):
+        """{"dx", "dw", "dbias"} of the last forward pass with keep=True (dx, dw, dbias: buffers to write into)."""
+        if self.kept is None:
+            raise RuntimeError("backward needs a forward pass with keep=True")
+        q_x, s_x = self.kept
+        if dy.shape[0] != s_x.numel():
+            raise ValueError("dy: one row per token of the forward pass")
+        new = lambda rows, cols, dtype: torch.empty(rows, cols, dtype=dtype, device=dy.device)  # noqa: E731
+        out = {}
+        with _on(stream):
+            if need_dx or dx is not None:
+                out["dx"] = dx if dx is not None else new(dy.shape[0], self.I, dy.dtype)
+            if need_dw or dw is not None:
+                out["dw"] = dw if dw is not None else new(self.O, self.I, dw_dtype)
+                if self.bias is not None:
+                    out["dbias"] = dbias if dbias is not None else torch.empty(self.O, dtype=torch.float32, device=dy.device)
+        lbt.linear8_backward(dy, self.q_w, self.s_w, q_x, s_x, self.I, out.get("dx"), out.get("dw"), out.get("dbias"), None, self.status, stream)
+        return out
+
+
+class ResNorm:
+    """What happens between two blocks: r = scale_x x + scale_h gate N_post(h), y = N_pre(r), in one pass.
+
+    kind: "rms" or "layer"; post_norm False: h enters as it is.  Parameters are vectors of `dim` values of one type (None: ones,
+    or zeros for the biases).  A gate is passed to each call: [dim], [1, dim] for all rows, or [ceil(rows / rows_per_gate), dim]."""
+
+    def __init__(self, dim: int, kind="rms", w_post=None, b_post=None, w_pre=None, b_pre=None, eps=1e-6, scale_x=1.0, scale_h=1.0,
+                 post_norm=True):
+        if kind not in ("rms", "layer"):
+            raise ValueError('kind: "rms" or "layer"')
+        self.dim, self.layer, self.post = int(dim), kind == "layer", bool(post_norm)
+        self.w_post, self.b_post, self.w_pre, self.b_pre = w_post, b_post, w_pre, b_pre
+        given = [p for p in (w_post, b_post, w_pre, b_pre) if p is not None]
+        if any(p.numel() != dim or p.dtype != given[0].dtype or p.dtype not in lbt.TYPES for p in given):
+            raise ValueError(f"parameters are vectors of {dim} values of one type")
+        if not self.layer and (b_post is not None or b_pre is not None):
+            raise ValueError("an RMS norm has no bias")
+        self.param_dtype = given[0].dtype if given else None
+        self.eps, self.scale_x, self.scale_h = float(eps), float(scale_x), float(scale_h)
+        self.kept = None
+
+    def _desc(self, like, gate, rows_per_gate, **acts):
+        M, dtype = like.shape[0], like.dtype
+        pd = self.param_dtype or (gate.dtype if gate is not None else dtype)
+        if gate is not None:
+            rows = -(-M // rows_per_gate) if rows_per_gate else 1
+            if gate.dtype != pd or gate.numel() != rows * self.dim:
+                raise ValueError(f"gate: {rows} x {self.dim} values of the parameters' type")
+        d = lbt.ResnormDesc(M, self.dim, rows_per_gate or 0, lbt.TYPES[dtype], lbt.TYPES[pd], lbt.NORM_LAYER if self.layer else lbt.NORM_RMS,
+                            1 if self.post else 0, self.eps, self.eps, self.scale_x, self.scale_h)
+        for name, t in acts.items():
+            if t is None:
+                continue
+            _, _, ld = lbt._rows(t, name, self.dim)
+            if t.shape[0] != M or t.dtype != dtype:
+                raise ValueError(f"{name}: {M} rows of {dtype}")
+            setattr(d, "ld_" + name, ld)
+        return d
+
+    def forward(self, x, h, gate=None, rows_per_gate=0, out=None, keep=False, stream=None):
+        """(r, y); keep: the statistics stay for `backward`, which also needs x and h unchanged."""
+        with _on(stream):
+            new = lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device)  # noqa: E731
+            r, y = out if out is not None else (new(), new())
+            stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device) if keep else None
+        d = self._desc(x, gate, rows_per_gate, x=x, h=h, r=r, y=y)
+        lbt.resnorm_forward(d, x, h, gate, self.w_post, self.b_post, self.w_pre, self.b_pre, r, y=y, stats=stats, stream=stream)
+        if keep:
+            self.kept = (x, h, gate, rows_per_gate, stats)
+        return r, y
+
+    def forward_codes(self, x, h, gate=None, rows_per_gate=0, out=None, keep=False, stream=None):
+        """(r, q, scale): y as the 8-bit rows that Linear8.forward_codes takes."""
+        with _on(stream):
+            r = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+            q = torch.empty(x.shape[0], lbt.pitch8(self.dim), dtype=torch.int8, device=x.device)
+            scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+            stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device) if keep else None
+        d = self._desc(x, gate, rows_per_gate, x=x, h=h, r=r)
+        lbt.resnorm_forward(d, x, h, gate, self.w_post, self.b_post, self.w_pre, self.b_pre, r, q=q, q_scale=scale, stats=stats, stream=stream)
+        if keep:
+            self.kept = (x, h, gate, rows_per_gate, stats)
+        return r, q, scale
+
+    def backward(self, dr, dy, stream=None):
+        """Gradients of the last forward pass with keep=True: {"dx", "dh"} and those of the parameters and the gate that there are."""
+        if self.kept is None:
+            raise RuntimeError("backward needs a forward pass with keep=True")
+        x, h, gate, rows_per_gate, stats = self.kept
+        with _on(stream):
+            out = {k: torch.empty(x.shape, dtype=x.dtype, device=x.device) for k in ("dx", "dh")}
+            for name, p in (("dgate", gate), ("dw_post", self.w_post if self.post else None), ("db_post", self.b_post if self.post else None),
+                            ("dw_pre", self.w_pre), ("db_pre", self.b_pre)):
+                if p is not None:
+                    out[name] = torch.empty(p.shape, dtype=p.dtype, device=x.device)
+        d = self._desc(x, gate, rows_per_gate, x=x, h=h, dr=dr, dy=dy, dx=out["dx"], dh=out["dh"])
+        lbt.resnorm_backward(d, dr, dy, x, h, gate, self.w_post, self.b_post, self.w_pre, stats, stream=stream, **out)
+        return out
+
+
+class AdamW:
+    """AdamW over lists of parameter and gradient tensors (fixed storage, as the library's other calls write it), all in one launch.
+
+    m, v: the moments' tensors; None: new ones, in fp32 or (state_bits=8) as e4m3 codes with a scale for each block of 256 elements
+    (m, and the root of v).  With moments given, their type decides.  lr and weight_decay: one value, or one for each tensor."""
+
+    def __init__(self, params, grads, m=None, v=None, m_scale=None, v_scale=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
+                 step=0, state_bits=8):
+        n = len(params)
+        if len(grads) != n:
+            raise ValueError("one gradient for each parameter")
+        if m is not None:
+            state_bits = 32 if all(t.dtype == torch.float32 for t in m) else 8
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits: 8 or 32")
+        state = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        blocks = [-(-p.numel() // lbt.ADAMW_BLOCK) for p in params]
+        new = lambda kind, sizes: [torch.zeros(s, dtype=kind, device=p.device) for s, p in zip(sizes, params)]  # noqa: E731
+        self.params, self.grads = list(params), list(grads)
+        self.m = list(m) if m is not None else new(state, [p.numel() for p in params])
+        self.v = list(v) if v is not None else new(state, [p.numel() for p in params])
+        self.m_scale = (list(m_scale) if m_scale is not None else new(torch.float32, blocks)) if state_bits == 8 else [None] * n
+        self.v_scale = (list(v_scale) if v_scale is not None else new(torch.float32, blocks)) if state_bits == 8 else [None] * n
+        lrs, wds = (list(x) if isinstance(x, (list, tuple)) else [x] * n for x in (lr, weight_decay))
+        if any(len(x) != n for x in (self.m, self.v, self.m_scale, self.v_scale, lrs, wds)):
+            raise ValueError("one of each for each parameter")
+        self.table = (lbt.AdamwTensor * n)()
+        for i, (p, g) in enumerate(zip(self.params, self.grads)):
+            if p.dtype not in lbt.TYPES or g.dtype not in lbt.TYPES or g.numel() != p.numel():
+                raise ValueError("parameters and gradients: fp32, bf16 or fp16, of equal sizes")
+            for t, size, kind in ((self.m[i], p.numel(), state), (self.v[i], p.numel(), state), (self.m_scale[i], blocks[i], torch.float32),
+                                  (self.v_scale[i], blocks[i], torch.float32)):
+                if t is not None and (t.numel() != size or t.dtype != kind):
+                    raise ValueError(f"moments: {p.numel()} values of {state}; with 8 bits one fp32 scale for each {lbt.ADAMW_BLOCK}")
+            e = self.table[i]
+            e.p, e.g, e.m, e.v, e.m_scale, e.v_scale = (lbt._p(t) for t in (p, g, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i]))
+            e.n, e.lr, e.weight_decay, e.p_type, e.g_type = p.numel(), lrs[i], wds[i], lbt.TYPES[p.dtype], lbt.TYPES[g.dtype]
+        self.hyper = lbt.AdamwHyper(betas[0], betas[1], eps, step, state_bits, 0)
+
+    def set_lr(self, lr):
+        """One learning rate for all tensors, or one for each."""
+        for e, x in zip(self.table, lr if isinstance(lr, (list, tuple)) else [lr] * len(self.table)):
+            e.lr = x
+
+    def step(self, grad_scale=None, skip=None, stream=None):
+        """One step.  grad_scale: device float the gradients are multiplied by; skip: device int32, non-zero = leave everything."""
+        self.hyper.step += 1
+        lbt.adamw_step(self.table, self.hyper, grad_scale, skip, stream)
+
+    def moments(self):
+        """The moments (m, v) as fp32 values, one tensor for each parameter (a checkpoint reader's view)."""
+        if self.hyper.state_bits == 32:
+            return self.m, self.v
+        wide = lambda q, s: q.float() * s.repeat_interleave(lbt.ADAMW_BLOCK)[:q.numel()].view(q.shape)  # noqa: E731
+        return ([wide(q, s) for q, s in zip(self.m, self.m_scale)], [wide(q, s).square() for q, s in zip(self.v, self.v_scale)])

@@ -1,0 +1,128 @@
+"""Host side of the transformer operators (no GPU): struct mirrors, workspace sizes, and every refusal that needs no device.
+
+The addresses handed to the library here are never read: each call is refused (or has nothing to do) before a launch.
+"""
+import ctypes as C
+
+import pytest
+
+from paper_2407_12637_b200 import build as lib_build
+from paper_2407_12637_b200 import lbt
+
+A = 1 << 20   # an aligned address
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    lib_build.build()
+
+
+def test_struct_sizes():
+    assert (C.sizeof(lbt.AdamwTensor), C.sizeof(lbt.AdamwHyper), C.sizeof(lbt.ResnormDesc)) == (80, 40, 120)
+    assert lbt.ResnormDesc.ld_x.offset == 56 and lbt.ResnormDesc.ld_dh.offset == 112
+
+
+def test_pitch_of_code_rows():
+    assert [lbt.pitch8(n) for n in (1, 15, 16, 17, 4096)] == [16, 16, 16, 32, 4096]
+    assert 127 * 127 * lbt.MAX_REDUCTION8 < 2 ** 31 <= 127 * 127 * (lbt.MAX_REDUCTION8 + 1)
+
+
+@pytest.mark.parametrize("change,want", [
+    ({}, lbt.OK), ({"rows": -1}, lbt.ERR_INVALID_ARG), ({"cols": 0}, lbt.ERR_INVALID_ARG), ({"ld": 63}, lbt.ERR_INVALID_ARG),
+    ({"type": 3}, lbt.ERR_INVALID_ARG), ({"ldq": 48}, lbt.ERR_INVALID_ARG), ({"ldq": 72}, lbt.ERR_ALIGNMENT), ({"q": A + 8}, lbt.ERR_ALIGNMENT),
+    ({"x": A + 2}, lbt.ERR_ALIGNMENT), ({"rows": 4, "x": None}, lbt.ERR_INVALID_ARG), ({"rows": 4, "scale": None}, lbt.ERR_INVALID_ARG),
+    ({"rows": 1 << 31}, lbt.ERR_UNSUPPORTED)])
+def test_rows8(change, want):
+    a = {"x": A, "type": lbt.F32, "rows": 0, "cols": 64, "ld": 64, "q": A, "ldq": 64, "scale": A, **change}
+    assert lbt.lib().lbt_rows8_quantize(a["x"], a["type"], a["rows"], a["cols"], a["ld"], a["q"], a["ldq"], a["scale"], None) == want
+
+
+@pytest.mark.parametrize("change,want", [
+    ({}, lbt.OK), ({"M": -1}, lbt.ERR_INVALID_ARG), ({"O": 0}, lbt.ERR_INVALID_ARG), ({"I": 0}, lbt.ERR_INVALID_ARG), ({"ldy": 31}, lbt.ERR_INVALID_ARG),
+    ({"ldx": 63}, lbt.ERR_INVALID_ARG), ({"x_type": -1}, lbt.ERR_INVALID_ARG), ({"y_type": 7}, lbt.ERR_INVALID_ARG), ({"q_w": None}, lbt.ERR_INVALID_ARG),
+    ({"s_w": None}, lbt.ERR_INVALID_ARG), ({"q_w": A + 4}, lbt.ERR_ALIGNMENT), ({"q_x": A + 8}, lbt.ERR_ALIGNMENT), ({"bias": A + 2}, lbt.ERR_ALIGNMENT),
+    ({"y": A + 1}, lbt.ERR_ALIGNMENT), ({"M": 4, "y": None}, lbt.ERR_INVALID_ARG), ({"M": 4, "q_x": None}, lbt.ERR_INVALID_ARG),
+    ({"I": 133145, "ldx": 133145}, lbt.ERR_ACC_RANGE), ({"M": 1 << 31}, lbt.ERR_UNSUPPORTED)])
+def test_linear8_forward(change, want):
+    a = {"x": A, "x_type": lbt.BF16, "ldx": 64, "q_w": A, "s_w": A, "bias": None, "y": A, "y_type": lbt.BF16, "ldy": 32, "M": 0, "O": 32, "I": 64,
+         "q_x": A, "s_x": A, **change}
+    assert lbt.lib().lbt_linear8_forward(a["x"], a["x_type"], a["ldx"], a["q_w"], a["s_w"], a["bias"], a["y"], a["y_type"], a["ldy"], a["M"], a["O"],
+                                         a["I"], a["q_x"], a["s_x"], None, None) == want
+    if not set(change) & {"ldx", "x_type"} or "I" in change:
+        assert lbt.lib().lbt_linear8_matmul(a["q_x"], a["s_x"], a["q_w"], a["s_w"], a["bias"], a["y"], a["y_type"], a["ldy"], a["M"], a["O"], a["I"],
+                                            None, None) == want
+
+
+@pytest.mark.parametrize("change,want", [
+    ({"dX": None, "dW": None, "dbias": None}, lbt.ERR_INVALID_ARG), ({"lddy": 31}, lbt.ERR_INVALID_ARG), ({"lddx": 63}, lbt.ERR_INVALID_ARG),
+    ({"lddw": 63}, lbt.ERR_INVALID_ARG), ({"dw_type": 5}, lbt.ERR_INVALID_ARG), ({"q_w": None}, lbt.ERR_INVALID_ARG), ({"q_x": None}, lbt.ERR_INVALID_ARG),
+    ({"s_x": None}, lbt.ERR_INVALID_ARG), ({"dY": None}, lbt.ERR_INVALID_ARG), ({"dY": A + 1}, lbt.ERR_ALIGNMENT), ({"q_x": A + 1}, lbt.ERR_ALIGNMENT),
+    ({"M": 133145}, lbt.ERR_ACC_RANGE), ({"O": 133145, "lddy": 133145}, lbt.ERR_ACC_RANGE), ({"ws": None}, lbt.ERR_WORKSPACE),
+    ({"ws_bytes": 1000}, lbt.ERR_WORKSPACE), ({"M": 4194241, "dW": None}, lbt.ERR_UNSUPPORTED)])
+def test_linear8_backward(change, want):
+    a = {"dY": A, "lddy": 32, "q_w": A, "s_w": A, "q_x": A, "s_x": A, "dX": A, "lddx": 64, "dW": A, "dw_type": lbt.F32, "lddw": 64, "dbias": A, "M": 8, "O": 32,
+         "I": 64, "ws": A, "ws_bytes": 1 << 40, **change}
+    assert lbt.lib().lbt_linear8_backward(a["dY"], lbt.BF16, a["lddy"], a["q_w"], a["s_w"], a["q_x"], a["s_x"], a["dX"], lbt.BF16, a["lddx"], a["dW"],
+                                          a["dw_type"], a["lddw"], a["dbias"], a["M"], a["O"], a["I"], None, a["ws"], a["ws_bytes"], None) == want
+
+
+def test_linear8_workspace():
+    assert lbt.linear8_workspace_bytes(0, 32, 64) > 0 and lbt.linear8_workspace_bytes(-1, 32, 64) == 0
+    # two code matrices, scales and maxima of rows and columns
+    assert lbt.linear8_workspace_bytes(1000, 50, 64) >= 2 * 1000 * 64 + 8 * (1000 + 50)
+
+
+def _desc(**change):
+    d = lbt.ResnormDesc(0, 64, 0, lbt.BF16, lbt.F32, lbt.NORM_RMS, 1, 1e-6, 1e-6, 1.0, 1.0)
+    for k, v in change.items():
+        setattr(d, k, v)
+    return d
+
+
+@pytest.mark.parametrize("change,want", [
+    ({}, lbt.OK), ({"M": -1}, lbt.ERR_INVALID_ARG), ({"D": 0}, lbt.ERR_INVALID_ARG), ({"type": 9}, lbt.ERR_INVALID_ARG), ({"param_type": -1}, lbt.ERR_INVALID_ARG),
+    ({"kind": 2}, lbt.ERR_INVALID_ARG), ({"rows_per_gate": -1}, lbt.ERR_INVALID_ARG), ({"eps_pre": -1.0}, lbt.ERR_INVALID_ARG),
+    ({"eps_post": float("nan")}, lbt.ERR_INVALID_ARG), ({"ld_h": 63}, lbt.ERR_INVALID_ARG), ({"D": 32769}, lbt.ERR_UNSUPPORTED)])
+def test_resnorm_desc(change, want):
+    d = _desc(**change)
+    assert lbt.lib().lbt_resnorm_forward(C.addressof(d), A, A, None, A, None, A, None, A, A, None, 0, None, None, None) == want
+    assert (lbt.resnorm_workspace_bytes(d) > 0) == (want == lbt.OK)
+
+
+def test_resnorm_pointers():
+    f, b = lbt.lib().lbt_resnorm_forward, lbt.lib().lbt_resnorm_backward
+    d, at = _desc(M=4), lambda d: C.addressof(d)  # noqa: E731
+    assert f(None, A, A, None, A, None, A, None, A, A, None, 0, None, None, None) == lbt.ERR_INVALID_ARG
+    assert f(at(d), None, A, None, A, None, A, None, A, A, None, 0, None, None, None) == lbt.ERR_INVALID_ARG
+    assert f(at(d), A, A, None, A, None, A, None, None, A, None, 0, None, None, None) == lbt.ERR_INVALID_ARG
+    assert f(at(d), A + 1, A, None, A, None, A, None, A, A, None, 0, None, None, None) == lbt.ERR_ALIGNMENT
+    assert f(at(d), A, A, A + 2, A, None, A, None, A, A, None, 0, None, None, None) == lbt.ERR_ALIGNMENT
+    assert f(at(d), A, A, None, A, None, A, None, A, None, A, 48, A, None, None) == lbt.ERR_INVALID_ARG    # codes narrower than the row
+    assert f(at(d), A, A, None, A, None, A, None, A, None, A, 72, A, None, None) == lbt.ERR_ALIGNMENT
+    assert f(at(d), A, A, None, A, None, A, None, A, None, A, 64, None, None, None) == lbt.ERR_INVALID_ARG  # codes without scales
+    assert f(at(d), A, A, None, A, None, A, None, A, A, None, 0, None, A + 4, None) == lbt.ERR_ALIGNMENT
+    tail = lambda **k: [k.get(n) for n in ("dgate", "dw_post", "db_post", "dw_pre", "db_pre")]  # noqa: E731
+    big = 1 << 40
+    assert b(at(d), None, None, A, A, None, A, None, A, A, A, A, *tail(), A, big, None) == lbt.ERR_INVALID_ARG   # no gradient comes in
+    assert b(at(d), A, A, A, A, None, A, None, A, None, A, A, *tail(), A, big, None) == lbt.ERR_INVALID_ARG      # no statistics
+    assert b(at(d), A, A, A, A, None, A, None, A, A, A, A, *tail(dgate=A), A, big, None) == lbt.ERR_INVALID_ARG  # no gate
+    assert b(at(d), A, A, A, A, None, A, None, A, A, A, A, *tail(db_pre=A), A, big, None) == lbt.ERR_INVALID_ARG  # an RMS norm's bias
+    assert b(at(d), A, A, A, A, None, A, None, A, A, A, A, *tail(), None, big, None) == lbt.ERR_WORKSPACE
+    assert b(at(d), A, A, A, A, None, A, None, A, A, A, A, *tail(), A, 512, None) == lbt.ERR_WORKSPACE
+    d = _desc(M=4, post_norm=0)
+    assert b(at(d), A, A, A, A, None, A, None, A, A, A, A, *tail(dw_post=A), A, big, None) == lbt.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("change,want", [
+    ({}, lbt.OK), ({"step": 0}, lbt.ERR_INVALID_ARG), ({"beta1": 1.0}, lbt.ERR_INVALID_ARG), ({"beta2": -0.5}, lbt.ERR_INVALID_ARG),
+    ({"eps": float("nan")}, lbt.ERR_INVALID_ARG), ({"state_bits": 16}, lbt.ERR_UNSUPPORTED_BITS), ({"n": 5, "p": None}, lbt.ERR_INVALID_ARG),
+    ({"n": 5, "m_scale": None}, lbt.ERR_INVALID_ARG), ({"n": 5, "p_type": 4}, lbt.ERR_INVALID_ARG), ({"n": 5, "p": A + 2}, lbt.ERR_ALIGNMENT),
+    ({"n": 5, "v_scale": A + 2}, lbt.ERR_ALIGNMENT), ({"n": 5, "state_bits": 32, "m": A + 1}, lbt.ERR_ALIGNMENT), ({"n": (1 << 40) + 1}, lbt.ERR_UNSUPPORTED)])
+def test_adamw(change, want):
+    h = lbt.AdamwHyper(0.9, 0.999, 1e-8, 1, 8, 0)
+    t = (lbt.AdamwTensor * 1)(lbt.AdamwTensor(A, A, A, A, A, A, 0, 1e-3, 0.0, lbt.F32, lbt.F32))
+    for k, v in change.items():
+        setattr(h if hasattr(h, k) else t[0], k, v)
+    assert lbt.lib().lbt_adamw_step(t, 1, C.addressof(h), None, None, None) == want
+    assert lbt.lib().lbt_adamw_step(None, 1, C.addressof(h), None, None, None) == lbt.ERR_INVALID_ARG
+    assert lbt.lib().lbt_adamw_step(t, 0, None, None, None, None) == lbt.ERR_INVALID_ARG
