@@ -10,9 +10,11 @@
 //   dw = sum_rows g k,  db = sum_rows g,  dgate = sum over the gate's rows of scale_h u d.
 // Everything is bound by memory: two reads and two writes an element forward, four and two backward.
 //
-// One group of threads (a warp up to 1024 columns, a block above) owns a row, eight columns of it per thread and vector, so a
-// row's sums are the group's reduction and nothing is read twice.  Sums over rows: a group owns consecutive rows and keeps
-// its columns' sums in registers; a second kernel adds the groups' sums in a fixed order (no atomics: a run repeats bit for bit).
+// One group of threads (a warp up to 512 columns, a block above) owns a row, eight columns of it per thread and vector, so a row's
+// sums are the group's reduction and nothing is read twice.  A group works through several rows: each thread copies its own columns
+// of the rows to come into its own slots of shared memory (cp.async, up to three rows ahead), so the reductions of one row run
+// under the loads of the next ones and no thread waits for another's copies.  Sums over rows: a group owns consecutive rows and
+// keeps its columns' sums in registers; a second kernel adds the groups' sums in a fixed order (no atomics: a run repeats bit for bit).
 #include <algorithm>
 
 #include "lbt_types.cuh"
@@ -33,6 +35,7 @@ struct NormArgs {
     int D;
     int64_t rows_per_gate;
     bool layer, post, vec;
+    int depth;              // rows a thread copies ahead
     float eps_post, eps_pre, scale_x, scale_h, inv_d;
     const void *x, *h, *dr, *dy;
     void *r, *y, *dx, *dh;
@@ -140,6 +143,64 @@ struct Group {
     }
 };
 
+// The rows ahead of a thread: its own columns of kArrays tensors, `depth` rows deep (0: every load is direct).  Only whole
+// vectors of aligned rows go through it; what the thread copies only the thread reads, so its own wait is all it needs.
+template <typename T, int kThreads, int kG, int kNV, int kArrays>
+struct Ahead {
+    static constexpr int kPieces = (int)sizeof(T) / 2;   // 16-byte pieces of eight elements
+    static constexpr int kRowBytes = kThreads * kArrays * kNV * kPieces * 16;
+    const T* base[kArrays];
+    int64_t ld[kArrays];
+    uint8_t* slots;
+    int depth, D, t;
+    bool vec;
+
+    __device__ __forceinline__ uint8_t* slot(int stage, int array, int g, int piece) const {
+        return slots + (((stage * kArrays + array) * kNV + g) * kPieces + piece) * (kThreads * 16) + threadIdx.x * 16;
+    }
+    // starts the copies of `row` into `stage` (nothing past the last row: an empty group keeps the count)
+    __device__ __forceinline__ void start(int64_t row, int64_t end, int stage) const {
+        if (row < end && vec) {
+#pragma unroll
+            for (int k = 0; k < kArrays; ++k)
+#pragma unroll
+                for (int g = 0; g < kNV; ++g) {
+                    const int c = (g * kG + t) * 8;
+                    if (base[k] != nullptr && c + 8 <= D) {
+                        const uint8_t* src = reinterpret_cast<const uint8_t*>(base[k] + row * ld[k] + c);
+#pragma unroll
+                        for (int p = 0; p < kPieces; ++p)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(slot(stage, k, g, p))), "l"(src + 16 * p) : "memory");
+                    }
+                }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // waits for the oldest of the rows ahead
+    __device__ __forceinline__ void wait() const {
+        if (depth >= 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    __device__ __forceinline__ void read(int64_t row, int stage, int array, int g, float (&f)[8]) const {
+        const int c = (g * kG + t) * 8;
+        if (base[array] == nullptr) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+        } else if (depth > 0 && vec && c + 8 <= D) {
+            Vec8<T> v;
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                const uint4 w = *reinterpret_cast<const uint4*>(slot(stage, array, g, p));
+                v.w[4 * p] = w.x; v.w[4 * p + 1] = w.y; v.w[4 * p + 2] = w.z; v.w[4 * p + 3] = w.w;
+            }
+            unpack(v, f);
+        } else {
+            row_load(base[array] + row * ld[array], c, D, vec, f);
+        }
+    }
+};
+
 // Mean and reciprocal deviation of a row held in registers (columns past D hold zeros and are masked).
 template <int kG, int kNV>
 __device__ __forceinline__ void row_stats(Group<kG>& grp, const float (&v)[kNV][8], int t, int D, bool layer, float inv_d, float eps, float& mu, float& rstd) {
@@ -163,21 +224,30 @@ __device__ __forceinline__ void row_stats(Group<kG>& grp, const float (&v)[kNV][
     rstd = 1.0f / sqrtf(grp.sum(s) * inv_d + eps);
 }
 
+template <int kG> constexpr int kBlock = kG < 128 ? 256 : kG;   // threads of a block: groups of a warp share one
+
 template <typename T, int kG, int kNV>
-__global__ void __launch_bounds__(kG < 256 ? 256 : kG) resnorm_forward_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int kThreads = kG < 256 ? 256 : kG, kRows = kThreads / kG;
+__global__ void __launch_bounds__(kBlock<kG>, 1024 / kBlock<kG>) resnorm_forward_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int kThreads = kBlock<kG>, kRows = kThreads / kG;
+    extern __shared__ uint8_t ahead_slots[];
     __shared__ float slots[2][2][32];
     Group<kG> grp{slots, 0};
     const int t = threadIdx.x % kG, D = a.D;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kG; row < a.M; row += (int64_t)gridDim.x * kRows) {
-        const T* xs = static_cast<const T*>(a.x) + row * a.ld_x;
-        const T* hs = static_cast<const T*>(a.h) + row * a.ld_h;
+    const int64_t step = (int64_t)gridDim.x * kRows, first = (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
+    const Ahead<T, kThreads, kG, kNV, 2> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h)}, {a.ld_x, a.ld_h}, ahead_slots, a.depth, D, t, a.vec};
+    for (int s = 0; s < a.depth; ++s) in.start(first + s * step, a.M, s);
+    int stage = 0;
+    for (int64_t row = first; row < a.M; row += step) {
         float h[kNV][8], r[kNV][8];
+        if (a.depth > 0) in.wait();
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
-            const int c = (g * kG + t) * 8;
-            row_load(hs, c, D, a.vec, h[g]);
-            row_load(xs, c, D, a.vec, r[g]);
+            in.read(row, stage, 1, g, h[g]);
+            in.read(row, stage, 0, g, r[g]);
+        }
+        if (a.depth > 0) {
+            in.start(row + a.depth * step, a.M, stage);
+            stage = stage + 1 == a.depth ? 0 : stage + 1;
         }
         float mu1 = 0.0f, rstd1 = 1.0f, mu2 = 0.0f, rstd2 = 1.0f;
         if (a.post) row_stats<kG, kNV>(grp, h, t, D, a.layer, a.inv_d, a.eps_post, mu1, rstd1);
@@ -236,7 +306,7 @@ __global__ void __launch_bounds__(kG < 256 ? 256 : kG) resnorm_forward_kernel(co
 template <int kG, int kNV>
 __device__ __forceinline__ void publish(float* part, const float (&acc)[kNV][8], int t, int D, float* meet) {
     if (part == nullptr) return;   // uniform
-    constexpr int kRows = kG < 256 ? 256 / kG : 1;
+    constexpr int kRows = kBlock<kG> / kG;
     float* dst = part + (int64_t)blockIdx.x * D;
     if constexpr (kRows == 1) {
 #pragma unroll
@@ -263,14 +333,19 @@ __device__ __forceinline__ void publish(float* part, const float (&acc)[kNV][8],
 }
 
 template <typename T, int kG, int kNV, bool kLayer>
-__global__ void __launch_bounds__(kG < 256 ? 256 : kG) resnorm_backward_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int kThreads = kG < 256 ? 256 : kG, kRows = kThreads / kG;
+__global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<kG> : 1) resnorm_backward_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int kThreads = kBlock<kG>, kRows = kThreads / kG;
+    extern __shared__ uint8_t ahead_slots[];
     __shared__ float slots[2][2][32];
     __shared__ float meet[kRows > 1 ? kG * kNV * 8 : 1];
     Group<kG> grp{slots, 0};
     const int t = threadIdx.x % kG, D = a.D;
     const int64_t part = (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
     const int64_t first = part * a.rows_each, last = min(first + a.rows_each, a.M);
+    const Ahead<T, kThreads, kG, kNV, 4> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h), static_cast<const T*>(a.dy), static_cast<const T*>(a.dr)},
+                                            {a.ld_x, a.ld_h, a.ld_dy, a.ld_dr}, ahead_slots, a.depth, D, t, a.vec};
+    for (int s = 0; s < a.depth; ++s) in.start(first + s, last, s);
+    int stage = 0;
     float dw1[kNV][8], dw2[kNV][8], dg[kNV][8], db1[kLayer ? kNV : 1][8], db2[kLayer ? kNV : 1][8];
 #pragma unroll
     for (int g = 0; g < kNV; ++g)
@@ -284,13 +359,17 @@ __global__ void __launch_bounds__(kG < 256 ? 256 : kG) resnorm_backward_kernel(c
         const int64_t gate_i = row / a.rows_per_gate;
         float k1[kNV][8], k2[kNV][8], e[kNV][8], d[kNV][8];   // normalised h, normalised r, dy w_pre, dr
         float s_e = 0.0f, s_ek = 0.0f;
+        if (a.depth > 0) in.wait();
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
-            const int c = (g * kG + t) * 8;
-            row_load(static_cast<const T*>(a.h) + row * a.ld_h, c, D, a.vec, k1[g]);
-            row_load(static_cast<const T*>(a.x) + row * a.ld_x, c, D, a.vec, k2[g]);
-            if (a.dy != nullptr) row_load(static_cast<const T*>(a.dy) + row * a.ld_dy, c, D, a.vec, e[g]);
-            if (a.dr != nullptr) row_load(static_cast<const T*>(a.dr) + row * a.ld_dr, c, D, a.vec, d[g]);
+            in.read(row, stage, 1, g, k1[g]);
+            in.read(row, stage, 0, g, k2[g]);
+            in.read(row, stage, 2, g, e[g]);
+            in.read(row, stage, 3, g, d[g]);
+        }
+        if (a.depth > 0) {
+            in.start(row + a.depth, last, stage);
+            stage = stage + 1 == a.depth ? 0 : stage + 1;
         }
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
@@ -306,8 +385,6 @@ __global__ void __launch_bounds__(kG < 256 ? 256 : kG) resnorm_backward_kernel(c
                 const float u = a.post ? k1[g][i] * w[i] + b[i] : k1[g][i];
                 const float r = a.scale_x * k2[g][i] + a.scale_h * (gt[i] * u);
                 k2[g][i] = (r - st.z) * st.w;
-                if (a.dy == nullptr) e[g][i] = 0.0f;
-                if (a.dr == nullptr) d[g][i] = 0.0f;
                 dw2[g][i] += e[g][i] * k2[g][i];
                 if (kLayer) db2[g][i] += e[g][i];
                 e[g][i] *= w2[i];
@@ -400,8 +477,8 @@ __global__ void __launch_bounds__(kG < 256 ? 256 : kG) resnorm_backward_kernel(c
 }
 
 // Second kernel of the backward pass: column sums over the blocks' partial sums, and the gate rows that several groups share.
-// blockIdx.y: which array, then which border between two groups (a shared gate row belongs to the first border inside it);
-// 32 columns a block, eight threads a column, added in a fixed order.
+// blockIdx.y: which array, then which gate row (or, where there are fewer of them, which border between two groups: a shared gate
+// row belongs to the first border inside it); 32 columns a block, 32 threads a column, added in a fixed order.
 struct FinishArgs {
     int D;
     int blocks;
@@ -412,53 +489,57 @@ struct FinishArgs {
     // gates
     const float* part_gate;
     void* dgate;
-    int gate_type;
+    int gate_type, by_border;
     int64_t M, rows_per_gate, rows_each;
 };
 
-__global__ void __launch_bounds__(256) resnorm_finish_kernel(const __grid_constant__ FinishArgs f) {
-    __shared__ float meet[8][33];
+__global__ void __launch_bounds__(1024) resnorm_finish_kernel(const __grid_constant__ FinishArgs f) {
+    __shared__ float meet[32][33];
     const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
-    int64_t gate = 0;
-    if ((int)blockIdx.y < f.arrays) {
+    int64_t gate = (int64_t)blockIdx.y - f.arrays;
+    if (gate < 0) {
         const float* p = f.part[blockIdx.y];
         if (c < f.D)
-            for (int b = y; b < f.blocks; b += 8) s += p[(int64_t)b * f.D + c];
+#pragma unroll 4
+            for (int b = y; b < f.blocks; b += 32) s += p[(int64_t)b * f.D + c];
     } else {
-        const int64_t border = (int64_t)blockIdx.y - f.arrays + 1;
-        gate = border * f.rows_each / f.rows_per_gate;
+        const int64_t border = f.by_border ? gate + 1 : 0;
+        if (f.by_border) gate = border * f.rows_each / f.rows_per_gate;
         const int64_t g0 = gate * f.rows_per_gate, g1 = min(g0 + f.rows_per_gate, f.M);
         const int64_t p0 = g0 / f.rows_each, p1 = (g1 - 1) / f.rows_each;
-        if (g0 == border * f.rows_each || p0 != border - 1) return;   // it begins here, or an earlier border is inside it
+        if (p0 == p1 || (f.by_border && (g0 == border * f.rows_each || p0 != border - 1))) return;   // one group's alone, or another border's
         if (c < f.D)
-            for (int64_t p = p0 + y; p <= p1; p += 8) s += f.part_gate[(p * 2 + (gate == p * f.rows_each / f.rows_per_gate ? 0 : 1)) * f.D + c];
+#pragma unroll 4
+            for (int64_t p = p0 + y; p <= p1; p += 32) s += f.part_gate[(p * 2 + (gate == p * f.rows_each / f.rows_per_gate ? 0 : 1)) * f.D + c];
     }
     meet[y][lane] = s;
     __syncthreads();
-    if (y != 0 || c >= f.D) return;
-    s = 0.0f;
+    // column `y` of the block is added up by warp y: lane by lane in a fixed tree
+    s = meet[lane][y];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += meet[i][lane];
-    if ((int)blockIdx.y < f.arrays) param_store(f.out[blockIdx.y], f.type, c, s);
-    else param_store(f.dgate, f.gate_type, gate * f.D + c, s);
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    const int64_t col = (int64_t)blockIdx.x * 32 + y;
+    if (lane != 0 || col >= f.D) return;
+    if ((int)blockIdx.y < f.arrays) param_store(f.out[blockIdx.y], f.type, col, s);
+    else param_store(f.dgate, f.gate_type, gate * f.D + col, s);
 }
 
 // ------------------------------------------------------------------------------------------ host
 constexpr int kMaxD = 32768;
 
-// Threads of a row and blocks in flight per SM.
-int group_threads(int D) { return D <= 1024 ? 32 : D <= 4096 ? 256 : D <= 8192 ? 512 : 1024; }
+// Threads of a row in the backward pass.
+int group_threads(int D) { return D <= 512 ? 32 : D <= 1024 ? 128 : D <= 2048 ? 256 : D <= 8192 ? 512 : 1024; }
 
 struct Split {
     int64_t rows_each, parts;
     int blocks;
 };
-// How the backward pass deals rows out: consecutive rows to each group, about two blocks per SM.
+// How the backward pass deals rows out: consecutive rows to each group, 512 threads (of 128 registers) to an SM.
 Split split_rows(int64_t M, int D) {
-    const int g = group_threads(D), rows = g < 256 ? 256 / g : 1;
-    const int64_t most = (int64_t)kNumSMs * (g >= 512 ? 1 : 2) * rows;
+    const int g = group_threads(D), threads = g < 128 ? 256 : g, rows = threads / g;
+    const int64_t most = (int64_t)kNumSMs * std::max(1, 512 / threads) * rows;
     Split s;
     s.rows_each = std::max<int64_t>(1, (M + most - 1) / most);
     s.parts = (M + s.rows_each - 1) / s.rows_each;
@@ -484,35 +565,64 @@ NormSpace norm_space(int64_t M, int D) {
     return w;
 }
 
+// Rows ahead that fit the shared memory of a block when `resident` of them share an SM.
+int depth_for(int row_bytes, int resident, bool vec, int64_t rows_each) {
+    if (!vec || rows_each < 2) return 0;   // (one row a group: nothing to run ahead of)
+    return (int)std::min<int64_t>(3, 200 * 1024 / resident / row_bytes);
+}
+
+// The attribute for more than 48 KB of shared memory, once per kernel and device.
+template <typename K>
+lbt_status allow_smem(K kernel, int bytes) {
+    if (bytes <= 40 * 1024) return LBT_OK;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
+}
+
+template <typename T, int kG, int kNV>
+lbt_status forward_launch(NormArgs a, cudaStream_t stream) {
+    constexpr int threads = kBlock<kG>, rows = threads / kG, resident = 1024 / threads;
+    const int64_t blocks = std::min<int64_t>((a.M + rows - 1) / rows, (int64_t)kNumSMs * resident);
+    constexpr int row_bytes = Ahead<T, threads, kG, kNV, 2>::kRowBytes;
+    a.depth = depth_for(row_bytes, resident, a.vec, (a.M + blocks * rows - 1) / (blocks * rows));
+    const lbt_status rc = allow_smem(resnorm_forward_kernel<T, kG, kNV>, a.depth * row_bytes);
+    if (rc != LBT_OK) return rc;
+    resnorm_forward_kernel<T, kG, kNV><<<(unsigned)blocks, threads, a.depth * row_bytes, stream>>>(a);
+    return launch_status();
+}
+
 template <typename T>
 lbt_status run_forward(const NormArgs& a, cudaStream_t stream) {
-    const int g = group_threads(a.D), threads = g < 256 ? 256 : g, rows = threads / g;
-    const int64_t blocks = std::min<int64_t>((a.M + rows - 1) / rows, 1 << 30);
-    const dim3 grid((unsigned)blocks), block((unsigned)threads);
-    if (a.D <= 256) resnorm_forward_kernel<T, 32, 1><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 512) resnorm_forward_kernel<T, 32, 2><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 1024) resnorm_forward_kernel<T, 32, 4><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 2048) resnorm_forward_kernel<T, 256, 1><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 4096) resnorm_forward_kernel<T, 256, 2><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 8192) resnorm_forward_kernel<T, 512, 2><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 16384) resnorm_forward_kernel<T, 1024, 2><<<grid, block, 0, stream>>>(a);
-    else resnorm_forward_kernel<T, 1024, 4><<<grid, block, 0, stream>>>(a);
+    if (a.D <= 256) return forward_launch<T, 32, 1>(a, stream);
+    if (a.D <= 512) return forward_launch<T, 32, 2>(a, stream);
+    if (a.D <= 1024) return forward_launch<T, 128, 1>(a, stream);
+    if (a.D <= 2048) return forward_launch<T, 256, 1>(a, stream);
+    if (a.D <= 4096) return forward_launch<T, 512, 1>(a, stream);
+    if (a.D <= 8192) return forward_launch<T, 1024, 1>(a, stream);
+    if (a.D <= 16384) return forward_launch<T, 1024, 2>(a, stream);
+    return forward_launch<T, 1024, 4>(a, stream);
+}
+
+template <typename T, int kG, int kNV, bool kLayer>
+lbt_status backward_launch(NormArgs a, const Split& s, cudaStream_t stream) {
+    constexpr int threads = kBlock<kG>, resident = threads <= 512 ? 512 / threads : 1;
+    constexpr int row_bytes = Ahead<T, threads, kG, kNV, 4>::kRowBytes;
+    a.depth = depth_for(row_bytes, resident, a.vec, s.rows_each);
+    const lbt_status rc = allow_smem(resnorm_backward_kernel<T, kG, kNV, kLayer>, a.depth * row_bytes);
+    if (rc != LBT_OK) return rc;
+    resnorm_backward_kernel<T, kG, kNV, kLayer><<<(unsigned)s.blocks, threads, a.depth * row_bytes, stream>>>(a);
     return launch_status();
 }
 
 template <typename T, bool kLayer>
 lbt_status run_backward(const NormArgs& a, const Split& s, cudaStream_t stream) {
-    const int g = group_threads(a.D);
-    const dim3 grid((unsigned)s.blocks), block((unsigned)(g < 256 ? 256 : g));
-    if (a.D <= 256) resnorm_backward_kernel<T, 32, 1, kLayer><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 512) resnorm_backward_kernel<T, 32, 2, kLayer><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 1024) resnorm_backward_kernel<T, 32, 4, kLayer><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 2048) resnorm_backward_kernel<T, 256, 1, kLayer><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 4096) resnorm_backward_kernel<T, 256, 2, kLayer><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 8192) resnorm_backward_kernel<T, 512, 2, kLayer><<<grid, block, 0, stream>>>(a);
-    else if (a.D <= 16384) resnorm_backward_kernel<T, 1024, 2, kLayer><<<grid, block, 0, stream>>>(a);
-    else resnorm_backward_kernel<T, 1024, 4, kLayer><<<grid, block, 0, stream>>>(a);
-    return launch_status();
+    if (a.D <= 256) return backward_launch<T, 32, 1, kLayer>(a, s, stream);
+    if (a.D <= 512) return backward_launch<T, 32, 2, kLayer>(a, s, stream);
+    if (a.D <= 1024) return backward_launch<T, 128, 1, kLayer>(a, s, stream);
+    if (a.D <= 2048) return backward_launch<T, 256, 1, kLayer>(a, s, stream);
+    if (a.D <= 4096) return backward_launch<T, 512, 1, kLayer>(a, s, stream);
+    if (a.D <= 8192) return backward_launch<T, 512, 2, kLayer>(a, s, stream);
+    if (a.D <= 16384) return backward_launch<T, 1024, 2, kLayer>(a, s, stream);
+    return backward_launch<T, 1024, 4, kLayer>(a, s, stream);
 }
 
 bool off(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
@@ -634,13 +744,15 @@ extern "C" lbt_status lbt_resnorm_backward(const lbt_resnorm_desc* d, const void
     const float* parts[4] = {a.part_w_post, a.part_b_post, a.part_w_pre, a.part_b_pre};
     for (int i = 0; i < 4; ++i)
         if (outs[i] != nullptr) { f.part[f.arrays] = parts[i]; f.out[f.arrays++] = outs[i]; }
-    int64_t borders = 0;   // between two groups: at most one gate row each
+    int64_t shared = 0;   // gate rows that may lie in several groups: all of them, or at most one for each border
     if (dgate != nullptr) {
-        borders = s.parts - 1;
+        const int64_t gates = (a.M + a.rows_per_gate - 1) / a.rows_per_gate;
+        shared = std::min(gates, s.parts - 1);
+        f.by_border = gates > s.parts - 1;
         f.part_gate = a.part_gate; f.dgate = dgate; f.gate_type = d->param_type;
         f.M = a.M; f.rows_per_gate = a.rows_per_gate; f.rows_each = a.rows_each;
     }
-    if (f.arrays + borders == 0) return LBT_OK;
-    resnorm_finish_kernel<<<dim3((unsigned)((a.D + 31) / 32), (unsigned)(f.arrays + borders)), 256, 0, stream>>>(f);
+    if (f.arrays + shared == 0) return LBT_OK;
+    resnorm_finish_kernel<<<dim3((unsigned)((a.D + 31) / 32), (unsigned)(f.arrays + shared)), 1024, 0, stream>>>(f);
     return launch_status();
 }
