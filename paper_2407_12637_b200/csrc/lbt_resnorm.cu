@@ -34,7 +34,7 @@ struct NormArgs {
     int64_t M;
     int D;
     int64_t rows_per_gate;
-    bool layer, post, vec;
+    bool layer, post, vec, one_gate;
     int depth;              // rows a thread copies ahead
     float eps_post, eps_pre, scale_x, scale_h, inv_d;
     const void *x, *h, *dr, *dy;
@@ -53,7 +53,14 @@ struct NormArgs {
     void* dgate;
 };
 
-// Columns [c, c + 8) of an activation row / a parameter vector as fp32 (`fill` behind the end or where there is no vector).
+// The kernels come in two forms.  P a type: activation rows and parameter vectors (of type P) are aligned and D is a multiple of 8,
+// so a thread's eight columns are all there or none of them is.  P void: any alignment, any D, parameters of any type, element
+// by element.  (The test for a column costs about as much as the arithmetic on it: on 8192 x 4096 bf16 the second form's
+// forward pass runs 82 instructions an element and is bound by their issue, the first form's 25.)
+template <typename P> constexpr bool kEven = true;
+template <> constexpr bool kEven<void> = false;
+
+// Columns [c, c + 8) of a row as fp32 (zeros behind the end), and back.
 template <typename T>
 __device__ __forceinline__ void row_load(const T* row, int c, int D, bool vec, float (&f)[8]) {
     if (vec && c + 8 <= D) {
@@ -63,9 +70,9 @@ __device__ __forceinline__ void row_load(const T* row, int c, int D, bool vec, f
         for (int i = 0; i < 8; ++i) f[i] = c + i < D ? to_f32(row[c + i]) : 0.0f;
     }
 }
-template <typename T>
+template <typename P, typename T>
 __device__ __forceinline__ void row_store(T* row, int c, int D, bool vec, const float (&f)[8]) {
-    if (vec && c + 8 <= D) {
+    if (kEven<P> || (vec && c + 8 <= D)) {
         store8(row + c, f);
     } else {
 #pragma unroll
@@ -73,10 +80,13 @@ __device__ __forceinline__ void row_store(T* row, int c, int D, bool vec, const 
             if (c + i < D) row[c + i] = from_f32<T>(f[i]);
     }
 }
+template <typename P>
 __device__ __forceinline__ void param_load(const Params& p, int64_t at, int c, int D, float fill, float (&f)[8]) {
     if (p.p == nullptr) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = fill;
+    } else if constexpr (kEven<P>) {
+        load8(static_cast<const P*>(p.p) + at + c, f);
     } else if (p.type == LBT_F32) {
         row_load(static_cast<const float*>(p.p) + at, c, D, p.vec, f);
     } else if (p.type == LBT_BF16) {
@@ -91,11 +101,12 @@ __device__ __forceinline__ void param_store(void* p, int type, int64_t i, float 
     else static_cast<__half*>(p)[i] = __float2half_rn(v);
 }
 
-// Sums (and a maximum) over the kG threads that own a row.  Blocks alternate between two rows of shared memory, so one
-// barrier a reduction is enough.
+// Sums (and a maximum) over the kG threads that own a row: a tree in each warp, then one over the warps' results, which every
+// warp forms for itself.  Blocks alternate between two rows of shared memory, so one barrier a reduction is enough.
 template <int kG>
 struct Group {
-    float (*slots)[2][32];   // [2 buffers][2 values][warps]
+    static constexpr int kWarps = kG / 32;
+    float2 (*slots)[32];   // [2 buffers][warps]
     int turn;
     __device__ __forceinline__ float2 sum(float a, float b) {
 #pragma unroll
@@ -103,41 +114,43 @@ struct Group {
             a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
             b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
         }
-        if (kG > 32) {
-            float (*s)[32] = slots[turn & 1];
+        if (kWarps > 1) {
+            float2* s = slots[turn & 1];
             ++turn;
-            if ((threadIdx.x & 31) == 0) { s[0][threadIdx.x >> 5] = a; s[1][threadIdx.x >> 5] = b; }
+            if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float2(a, b);
             __syncthreads();
-            a = b = 0.0f;
+            const float2 v = s[threadIdx.x & (kWarps - 1)];
+            a = v.x; b = v.y;
 #pragma unroll
-            for (int i = 0; i < kG / 32; ++i) { a += s[0][i]; b += s[1][i]; }
+            for (int o = kWarps / 2; o > 0; o >>= 1) {
+                a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+                b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+            }
         }
         return make_float2(a, b);
     }
     __device__ __forceinline__ float sum(float a) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-        if (kG > 32) {
-            float* s = slots[turn & 1][0];
+        if (kWarps > 1) {
+            float* s = reinterpret_cast<float*>(slots[turn & 1]);
             ++turn;
             if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = a;
             __syncthreads();
-            a = 0.0f;
+            a = s[threadIdx.x & (kWarps - 1)];
 #pragma unroll
-            for (int i = 0; i < kG / 32; ++i) a += s[i];
+            for (int o = kWarps / 2; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
         }
         return a;
     }
     __device__ __forceinline__ uint32_t most(uint32_t v) {
         v = __reduce_max_sync(0xFFFFFFFFu, v);
-        if (kG > 32) {
-            uint32_t* s = reinterpret_cast<uint32_t*>(slots[turn & 1][0]);
+        if (kWarps > 1) {
+            uint32_t* s = reinterpret_cast<uint32_t*>(slots[turn & 1]);
             ++turn;
             if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
             __syncthreads();
-            v = 0;
-#pragma unroll
-            for (int i = 0; i < kG / 32; ++i) v = max(v, s[i]);
+            v = __reduce_max_sync(0xFFFFFFFFu, s[threadIdx.x & (kWarps - 1)]);
         }
         return v;
     }
@@ -156,21 +169,24 @@ struct Ahead {
     bool vec;
 
     __device__ __forceinline__ uint8_t* slot(int stage, int array, int g, int piece) const {
-        return slots + (((stage * kArrays + array) * kNV + g) * kPieces + piece) * (kThreads * 16) + threadIdx.x * 16;
+        return slots + stage * kRowBytes + ((array * kNV + g) * kPieces + piece) * (kThreads * 16) + threadIdx.x * 16;
     }
     // starts the copies of `row` into `stage` (nothing past the last row: an empty group keeps the count)
     __device__ __forceinline__ void start(int64_t row, int64_t end, int stage) const {
         if (row < end && vec) {
 #pragma unroll
             for (int k = 0; k < kArrays; ++k)
+                if (base[k] != nullptr) {
+                    const T* src = base[k] + row * ld[k];
 #pragma unroll
-                for (int g = 0; g < kNV; ++g) {
-                    const int c = (g * kG + t) * 8;
-                    if (base[k] != nullptr && c + 8 <= D) {
-                        const uint8_t* src = reinterpret_cast<const uint8_t*>(base[k] + row * ld[k] + c);
+                    for (int g = 0; g < kNV; ++g) {
+                        const int c = (g * kG + t) * 8;
+                        if (c + 8 <= D) {
 #pragma unroll
-                        for (int p = 0; p < kPieces; ++p)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(slot(stage, k, g, p))), "l"(src + 16 * p) : "memory");
+                            for (int p = 0; p < kPieces; ++p)
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(slot(stage, k, g, p))),
+                                             "l"(reinterpret_cast<const uint8_t*>(src + c) + 16 * p) : "memory");
+                        }
                     }
                 }
         }
@@ -184,7 +200,7 @@ struct Ahead {
     }
     __device__ __forceinline__ void read(int64_t row, int stage, int array, int g, float (&f)[8]) const {
         const int c = (g * kG + t) * 8;
-        if (base[array] == nullptr) {
+        if (base[array] == nullptr || c >= D) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = 0.0f;
         } else if (depth > 0 && vec && c + 8 <= D) {
@@ -201,8 +217,8 @@ struct Ahead {
     }
 };
 
-// Mean and reciprocal deviation of a row held in registers (columns past D hold zeros and are masked).
-template <int kG, int kNV>
+// Mean and reciprocal deviation of a row held in registers (columns past D hold zeros and are left out).
+template <typename P, int kG, int kNV>
 __device__ __forceinline__ void row_stats(Group<kG>& grp, const float (&v)[kNV][8], int t, int D, bool layer, float inv_d, float eps, float& mu, float& rstd) {
     float s = 0.0f;
     mu = 0.0f;
@@ -213,24 +229,33 @@ __device__ __forceinline__ void row_stats(Group<kG>& grp, const float (&v)[kNV][
             for (int i = 0; i < 8; ++i) s += v[g][i];
         mu = grp.sum(s) * inv_d;
         s = 0.0f;
-    }
 #pragma unroll
-    for (int g = 0; g < kNV; ++g)
+        for (int g = 0; g < kNV; ++g) {
+            const int c = (g * kG + t) * 8;
+            if (c < D) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float e = (g * kG + t) * 8 + i < D ? v[g][i] - mu : 0.0f;
-            s += e * e;
+                for (int i = 0; i < 8; ++i) {
+                    const float e = kEven<P> || c + i < D ? v[g][i] - mu : 0.0f;
+                    s += e * e;
+                }
+            }
         }
+    } else {
+#pragma unroll
+        for (int g = 0; g < kNV; ++g)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[g][i] * v[g][i];
+    }
     rstd = 1.0f / sqrtf(grp.sum(s) * inv_d + eps);
 }
 
 template <int kG> constexpr int kBlock = kG < 128 ? 256 : kG;   // threads of a block: groups of a warp share one
 
-template <typename T, int kG, int kNV>
-__global__ void __launch_bounds__(kBlock<kG>, 1024 / kBlock<kG>) resnorm_forward_kernel(const __grid_constant__ NormArgs a) {
+template <typename T, typename P, int kG, int kNV>
+__global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<kG> : 1) resnorm_forward_kernel(const __grid_constant__ NormArgs a) {
     constexpr int kThreads = kBlock<kG>, kRows = kThreads / kG;
     extern __shared__ uint8_t ahead_slots[];
-    __shared__ float slots[2][2][32];
+    __shared__ float2 slots[2][32];
     Group<kG> grp{slots, 0};
     const int t = threadIdx.x % kG, D = a.D;
     const int64_t step = (int64_t)gridDim.x * kRows, first = (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
@@ -250,40 +275,62 @@ __global__ void __launch_bounds__(kBlock<kG>, 1024 / kBlock<kG>) resnorm_forward
             stage = stage + 1 == a.depth ? 0 : stage + 1;
         }
         float mu1 = 0.0f, rstd1 = 1.0f, mu2 = 0.0f, rstd2 = 1.0f;
-        if (a.post) row_stats<kG, kNV>(grp, h, t, D, a.layer, a.inv_d, a.eps_post, mu1, rstd1);
-        const int64_t gate_row = row / a.rows_per_gate * D;
+        if (a.post) row_stats<P, kG, kNV>(grp, h, t, D, a.layer, a.inv_d, a.eps_post, mu1, rstd1);
+        const int64_t gate_row = a.one_gate ? 0 : row / a.rows_per_gate * D;
+        T* out = static_cast<T*>(a.r) + row * a.ld_r;
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
-            float w[8], b[8], gt[8];
-            param_load(a.w_post, 0, c, D, 1.0f, w);
-            param_load(a.b_post, 0, c, D, 0.0f, b);
-            param_load(a.gate, gate_row, c, D, 1.0f, gt);
+            if (c >= D) continue;   // (r holds zeros there)
+            if (a.post) {
+                float w[8], b[8];
+                param_load<P>(a.w_post, 0, c, D, 1.0f, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float u = a.post ? (h[g][i] - mu1) * rstd1 * w[i] + b[i] : h[g][i];
-                r[g][i] = c + i < D ? a.scale_x * r[g][i] + a.scale_h * (gt[i] * u) : 0.0f;
+                for (int i = 0; i < 8; ++i) h[g][i] = (h[g][i] - mu1) * rstd1 * w[i];
+                if (a.b_post.p != nullptr) {
+                    param_load<P>(a.b_post, 0, c, D, 0.0f, b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[g][i] += b[i];
+                }
             }
-            if (c < D) row_store(static_cast<T*>(a.r) + row * a.ld_r, c, D, a.vec, r[g]);
+            if (a.gate.p != nullptr) {
+                float gt[8];
+                param_load<P>(a.gate, gate_row, c, D, 1.0f, gt);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[g][i] *= gt[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[g][i] = kEven<P> || c + i < D ? a.scale_x * r[g][i] + a.scale_h * h[g][i] : 0.0f;
+            row_store<P>(out, c, D, a.vec, r[g]);
         }
         if (a.y != nullptr || a.q != nullptr) {
-            row_stats<kG, kNV>(grp, r, t, D, a.layer, a.inv_d, a.eps_pre, mu2, rstd2);
+            row_stats<P, kG, kNV>(grp, r, t, D, a.layer, a.inv_d, a.eps_pre, mu2, rstd2);
             uint32_t most = 0;
 #pragma unroll
             for (int g = 0; g < kNV; ++g) {
                 const int c = (g * kG + t) * 8;
-                float w[8], b[8];
-                param_load(a.w_pre, 0, c, D, 1.0f, w);
-                param_load(a.b_pre, 0, c, D, 0.0f, b);
+                if (c >= D) continue;
+                float w[8];
+                param_load<P>(a.w_pre, 0, c, D, 1.0f, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    r[g][i] = c + i < D ? (r[g][i] - mu2) * rstd2 * w[i] + b[i] : 0.0f;
-                    most = max(most, abs_bits(r[g][i]));
+                for (int i = 0; i < 8; ++i) r[g][i] = (r[g][i] - mu2) * rstd2 * w[i];
+                if (a.b_pre.p != nullptr) {
+                    param_load<P>(a.b_pre, 0, c, D, 0.0f, w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) r[g][i] += w[i];
                 }
-                if (a.y != nullptr && c < D) row_store(static_cast<T*>(a.y) + row * a.ld_y, c, D, a.vec, r[g]);
+                if (!kEven<P>)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i >= D) r[g][i] = 0.0f;
+                if (a.y != nullptr) row_store<P>(static_cast<T*>(a.y) + row * a.ld_y, c, D, a.vec, r[g]);
             }
             if (a.q != nullptr) {
                 float s, factor;
+#pragma unroll
+                for (int g = 0; g < kNV; ++g)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most = max(most, abs_bits(r[g][i]));
                 scale8(grp.most(most), s, factor);
                 if (t == 0) a.q_scale[row] = s;
 #pragma unroll
@@ -332,11 +379,11 @@ __device__ __forceinline__ void publish(float* part, const float (&acc)[kNV][8],
     }
 }
 
-template <typename T, int kG, int kNV, bool kLayer>
+template <typename T, typename P, int kG, int kNV, bool kLayer>
 __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<kG> : 1) resnorm_backward_kernel(const __grid_constant__ NormArgs a) {
     constexpr int kThreads = kBlock<kG>, kRows = kThreads / kG;
     extern __shared__ uint8_t ahead_slots[];
-    __shared__ float slots[2][2][32];
+    __shared__ float2 slots[2][32];
     __shared__ float meet[kRows > 1 ? kG * kNV * 8 : 1];
     Group<kG> grp{slots, 0};
     const int t = threadIdx.x % kG, D = a.D;
@@ -354,9 +401,9 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
             dw1[g][i] = dw2[g][i] = dg[g][i] = 0.0f;
             if (kLayer) db1[g][i] = db2[g][i] = 0.0f;
         }
+    int64_t gate_i = a.one_gate ? 0 : first / a.rows_per_gate, gate_end = a.one_gate ? a.M : (gate_i + 1) * a.rows_per_gate;
     for (int64_t row = first; row < last; ++row) {
         const float4 st = a.stats[row];
-        const int64_t gate_i = row / a.rows_per_gate;
         float k1[kNV][8], k2[kNV][8], e[kNV][8], d[kNV][8];   // normalised h, normalised r, dy w_pre, dr
         float s_e = 0.0f, s_ek = 0.0f;
         if (a.depth > 0) in.wait();
@@ -374,22 +421,39 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
-            float w[8], b[8], gt[8], w2[8];
-            param_load(a.w_post, 0, c, D, 1.0f, w);
-            param_load(a.b_post, 0, c, D, 0.0f, b);
-            param_load(a.gate, gate_i * D, c, D, 1.0f, gt);
-            param_load(a.w_pre, 0, c, D, 1.0f, w2);
+            if (c >= D) continue;
+            float u[8], p[8];
+            if (a.post) {
+                param_load<P>(a.w_post, 0, c, D, 1.0f, p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    k1[g][i] = (kLayer ? k1[g][i] - st.x : k1[g][i]) * st.y;
+                    u[i] = k1[g][i] * p[i];
+                }
+                if (kLayer && a.b_post.p != nullptr) {
+                    param_load<P>(a.b_post, 0, c, D, 0.0f, p);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) u[i] += p[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = k1[g][i];
+            }
+            if (a.gate.p != nullptr) {
+                param_load<P>(a.gate, gate_i * D, c, D, 1.0f, p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] *= p[i];
+            }
+            param_load<P>(a.w_pre, 0, c, D, 1.0f, p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (a.post) k1[g][i] = (k1[g][i] - st.x) * st.y;
-                const float u = a.post ? k1[g][i] * w[i] + b[i] : k1[g][i];
-                const float r = a.scale_x * k2[g][i] + a.scale_h * (gt[i] * u);
-                k2[g][i] = (r - st.z) * st.w;
+                const float r = a.scale_x * k2[g][i] + a.scale_h * u[i];
+                k2[g][i] = (kLayer ? r - st.z : r) * st.w;
                 dw2[g][i] += e[g][i] * k2[g][i];
                 if (kLayer) db2[g][i] += e[g][i];
-                e[g][i] *= w2[i];
-                if (c + i < D) {   // columns past the end hold no element
-                    s_e += e[g][i];
+                e[g][i] *= p[i];
+                if (kEven<P> || c + i < D) {   // columns past the end hold no element
+                    if (kLayer) s_e += e[g][i];
                     s_ek += e[g][i] * k2[g][i];
                 }
             }
@@ -412,28 +476,52 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
-            float w[8], b[8], gt[8], out[8];
-            param_load(a.w_post, 0, c, D, 1.0f, w);
-            param_load(a.b_post, 0, c, D, 0.0f, b);
-            param_load(a.gate, gate_i * D, c, D, 1.0f, gt);
+            if (c >= D) continue;
+            float out[8], p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                out[i] = a.scale_x * d[g][i];
-                const float u = a.post ? k1[g][i] * w[i] + b[i] : k1[g][i];
-                const float du = a.scale_h * (gt[i] * d[g][i]);
-                dg[g][i] += a.scale_h * (u * d[g][i]);
-                dw1[g][i] += du * k1[g][i];
-                if (kLayer) db1[g][i] += du;
-                e[g][i] = a.post ? du * w[i] : du;
-                if (c + i < D) {
-                    s_e += e[g][i];
-                    s_ek += e[g][i] * k1[g][i];
+            for (int i = 0; i < 8; ++i) out[i] = a.scale_x * d[g][i];
+            row_store<P>(static_cast<T*>(a.dx) + row * a.ld_dx, c, D, a.vec, out);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[g][i] = a.scale_h * d[g][i];   // of gate * u
+            if (a.post) {
+                float w[8];
+                param_load<P>(a.w_post, 0, c, D, 1.0f, w);
+                if (a.gate.p != nullptr) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) out[i] = k1[g][i] * w[i];
+                    if (kLayer && a.b_post.p != nullptr) {
+                        param_load<P>(a.b_post, 0, c, D, 0.0f, p);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) out[i] += p[i];
+                    }
+                    param_load<P>(a.gate, gate_i * D, c, D, 1.0f, p);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        dg[g][i] += out[i] * e[g][i];
+                        e[g][i] *= p[i];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dw1[g][i] += e[g][i] * k1[g][i];
+                    if (kLayer) db1[g][i] += e[g][i];
+                    e[g][i] *= w[i];
+                    if (kEven<P> || c + i < D) {
+                        if (kLayer) s_e += e[g][i];
+                        s_ek += e[g][i] * k1[g][i];
+                    }
+                }
+            } else if (a.gate.p != nullptr) {
+                param_load<P>(a.gate, gate_i * D, c, D, 1.0f, p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dg[g][i] += k1[g][i] * e[g][i];
+                    e[g][i] *= p[i];
                 }
             }
-            if (c < D) row_store(static_cast<T*>(a.dx) + row * a.ld_dx, c, D, a.vec, out);
         }
-        float mean_e = 0.0f, mean_ek = 0.0f;
         if (a.post) {
+            float mean_e = 0.0f, mean_ek;
             if (kLayer) {
                 const float2 s = grp.sum(s_e, s_ek);
                 mean_e = s.x * a.inv_d;
@@ -441,31 +529,36 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
             } else {
                 mean_ek = grp.sum(s_ek) * a.inv_d;
             }
+#pragma unroll
+            for (int g = 0; g < kNV; ++g)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[g][i] = st.y * ((kLayer ? e[g][i] - mean_e : e[g][i]) - k1[g][i] * mean_ek);
         }
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
-            float out[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = a.post ? st.y * ((kLayer ? e[g][i] - mean_e : e[g][i]) - k1[g][i] * mean_ek) : e[g][i];
-            if (c < D) row_store(static_cast<T*>(a.dh) + row * a.ld_dh, c, D, a.vec, out);
+            if (c < D) row_store<P>(static_cast<T*>(a.dh) + row * a.ld_dh, c, D, a.vec, e[g]);
         }
         // the gate row's last row, or the group's: its sum leaves (whole gate rows at once, shared ones through the second kernel)
-        if (a.dgate != nullptr && (row + 1 == last || (row + 1) / a.rows_per_gate != gate_i)) {
-            const int64_t g0 = gate_i * a.rows_per_gate, g1 = min(g0 + a.rows_per_gate, a.M);
-            const bool whole = g0 >= first && g1 <= last;
-            float* shared_part = a.part_gate + (part * 2 + (gate_i == first / a.rows_per_gate ? 0 : 1)) * D;
+        if (row + 1 == last || row + 1 == gate_end) {
+            if (a.dgate != nullptr) {
+                const int64_t g0 = gate_i * a.rows_per_gate, g1 = min(g0 + a.rows_per_gate, a.M);
+                const bool whole = g0 >= first && g1 <= last;
+                float* shared_part = a.part_gate + (part * 2 + (gate_i == first / a.rows_per_gate ? 0 : 1)) * D;
 #pragma unroll
-            for (int g = 0; g < kNV; ++g)
+                for (int g = 0; g < kNV; ++g)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int c = (g * kG + t) * 8 + i;
-                    if (c < D) {
-                        if (whole) param_store(a.dgate, a.gate.type, gate_i * D + c, dg[g][i]);
-                        else shared_part[c] = dg[g][i];
+                    for (int i = 0; i < 8; ++i) {
+                        const int c = (g * kG + t) * 8 + i;
+                        if (c < D) {
+                            if (whole) param_store(a.dgate, a.gate.type, gate_i * D + c, dg[g][i]);
+                            else shared_part[c] = dg[g][i];
+                        }
+                        dg[g][i] = 0.0f;
                     }
-                    dg[g][i] = 0.0f;
-                }
+            }
+            ++gate_i;
+            gate_end += a.rows_per_gate;
         }
     }
     publish<kG, kNV>(a.part_w_pre, dw2, t, D, meet);
@@ -578,51 +671,79 @@ lbt_status allow_smem(K kernel, int bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
 }
 
-template <typename T, int kG, int kNV>
+template <typename T, typename P, int kG, int kNV>
 lbt_status forward_launch(NormArgs a, cudaStream_t stream) {
-    constexpr int threads = kBlock<kG>, rows = threads / kG, resident = 1024 / threads;
+    constexpr int threads = kBlock<kG>, rows = threads / kG, resident = threads <= 768 ? 768 / threads : 1;
     const int64_t blocks = std::min<int64_t>((a.M + rows - 1) / rows, (int64_t)kNumSMs * resident);
     constexpr int row_bytes = Ahead<T, threads, kG, kNV, 2>::kRowBytes;
     a.depth = depth_for(row_bytes, resident, a.vec, (a.M + blocks * rows - 1) / (blocks * rows));
-    const lbt_status rc = allow_smem(resnorm_forward_kernel<T, kG, kNV>, a.depth * row_bytes);
+    const lbt_status rc = allow_smem(resnorm_forward_kernel<T, P, kG, kNV>, a.depth * row_bytes);
     if (rc != LBT_OK) return rc;
-    resnorm_forward_kernel<T, kG, kNV><<<(unsigned)blocks, threads, a.depth * row_bytes, stream>>>(a);
+    resnorm_forward_kernel<T, P, kG, kNV><<<(unsigned)blocks, threads, a.depth * row_bytes, stream>>>(a);
     return launch_status();
 }
 
-template <typename T>
+// Sixteen columns a thread where a block owns a row: half the reductions' instructions for each element.
+template <typename T, typename P>
 lbt_status run_forward(const NormArgs& a, cudaStream_t stream) {
-    if (a.D <= 256) return forward_launch<T, 32, 1>(a, stream);
-    if (a.D <= 512) return forward_launch<T, 32, 2>(a, stream);
-    if (a.D <= 1024) return forward_launch<T, 128, 1>(a, stream);
-    if (a.D <= 2048) return forward_launch<T, 256, 1>(a, stream);
-    if (a.D <= 4096) return forward_launch<T, 512, 1>(a, stream);
-    if (a.D <= 8192) return forward_launch<T, 1024, 1>(a, stream);
-    if (a.D <= 16384) return forward_launch<T, 1024, 2>(a, stream);
-    return forward_launch<T, 1024, 4>(a, stream);
+    if (a.D <= 256) return forward_launch<T, P, 32, 1>(a, stream);
+    if (a.D <= 512) return forward_launch<T, P, 32, 2>(a, stream);
+    if (a.D <= 1024) return forward_launch<T, P, 32, 4>(a, stream);
+    if (a.D <= 2048) return forward_launch<T, P, 128, 2>(a, stream);
+    if (a.D <= 4096) return forward_launch<T, P, 256, 2>(a, stream);
+    if (a.D <= 8192) return forward_launch<T, P, 512, 2>(a, stream);
+    if (a.D <= 16384) return forward_launch<T, P, 1024, 2>(a, stream);
+    return forward_launch<T, P, 1024, 4>(a, stream);
 }
 
-template <typename T, int kG, int kNV, bool kLayer>
+template <typename T, typename P, int kG, int kNV, bool kLayer>
 lbt_status backward_launch(NormArgs a, const Split& s, cudaStream_t stream) {
     constexpr int threads = kBlock<kG>, resident = threads <= 512 ? 512 / threads : 1;
     constexpr int row_bytes = Ahead<T, threads, kG, kNV, 4>::kRowBytes;
     a.depth = depth_for(row_bytes, resident, a.vec, s.rows_each);
-    const lbt_status rc = allow_smem(resnorm_backward_kernel<T, kG, kNV, kLayer>, a.depth * row_bytes);
+    const lbt_status rc = allow_smem(resnorm_backward_kernel<T, P, kG, kNV, kLayer>, a.depth * row_bytes);
     if (rc != LBT_OK) return rc;
-    resnorm_backward_kernel<T, kG, kNV, kLayer><<<(unsigned)s.blocks, threads, a.depth * row_bytes, stream>>>(a);
+    resnorm_backward_kernel<T, P, kG, kNV, kLayer><<<(unsigned)s.blocks, threads, a.depth * row_bytes, stream>>>(a);
     return launch_status();
 }
 
-template <typename T, bool kLayer>
+template <typename T, typename P, bool kLayer>
+lbt_status run_backward_kind(const NormArgs& a, const Split& s, cudaStream_t stream) {
+    if (a.D <= 256) return backward_launch<T, P, 32, 1, kLayer>(a, s, stream);
+    if (a.D <= 512) return backward_launch<T, P, 32, 2, kLayer>(a, s, stream);
+    if (a.D <= 1024) return backward_launch<T, P, 128, 1, kLayer>(a, s, stream);
+    if (a.D <= 2048) return backward_launch<T, P, 256, 1, kLayer>(a, s, stream);
+    if (a.D <= 4096) return backward_launch<T, P, 512, 1, kLayer>(a, s, stream);
+    if (a.D <= 8192) return backward_launch<T, P, 512, 2, kLayer>(a, s, stream);
+    if (a.D <= 16384) return backward_launch<T, P, 1024, 2, kLayer>(a, s, stream);
+    return backward_launch<T, P, 1024, 4, kLayer>(a, s, stream);
+}
+template <typename T, typename P>
 lbt_status run_backward(const NormArgs& a, const Split& s, cudaStream_t stream) {
-    if (a.D <= 256) return backward_launch<T, 32, 1, kLayer>(a, s, stream);
-    if (a.D <= 512) return backward_launch<T, 32, 2, kLayer>(a, s, stream);
-    if (a.D <= 1024) return backward_launch<T, 128, 1, kLayer>(a, s, stream);
-    if (a.D <= 2048) return backward_launch<T, 256, 1, kLayer>(a, s, stream);
-    if (a.D <= 4096) return backward_launch<T, 512, 1, kLayer>(a, s, stream);
-    if (a.D <= 8192) return backward_launch<T, 512, 2, kLayer>(a, s, stream);
-    if (a.D <= 16384) return backward_launch<T, 1024, 2, kLayer>(a, s, stream);
-    return backward_launch<T, 1024, 4, kLayer>(a, s, stream);
+    return a.layer ? run_backward_kind<T, P, true>(a, s, stream) : run_backward_kind<T, P, false>(a, s, stream);
+}
+
+// The form for aligned rows where everything is aligned, D is a multiple of 8 and the parameters are fp32 or of the
+// activations' type.
+bool even(const NormArgs& a, int type, int param_type) {
+    return a.vec && a.D % 8 == 0 && a.gate.vec && a.w_post.vec && a.b_post.vec && a.w_pre.vec && a.b_pre.vec &&
+           (param_type == LBT_F32 || param_type == type);
+}
+#define LBT_RESNORM_DISPATCH(RUN, a, type, ptype, ...)                                                                        \
+    do {                                                                                                                      \
+        const bool e = even(a, type, ptype);                                                                                  \
+        if (type == LBT_F32) return e ? RUN<float, float>(a, __VA_ARGS__) : RUN<float, void>(a, __VA_ARGS__);                 \
+        if (type == LBT_BF16) {                                                                                               \
+            if (!e) return RUN<__nv_bfloat16, void>(a, __VA_ARGS__);                                                          \
+            return ptype == LBT_F32 ? RUN<__nv_bfloat16, float>(a, __VA_ARGS__) : RUN<__nv_bfloat16, __nv_bfloat16>(a, __VA_ARGS__); \
+        }                                                                                                                     \
+        if (!e) return RUN<__half, void>(a, __VA_ARGS__);                                                                     \
+        return ptype == LBT_F32 ? RUN<__half, float>(a, __VA_ARGS__) : RUN<__half, __half>(a, __VA_ARGS__);                   \
+    } while (0)
+
+lbt_status forward_any(const NormArgs& a, int type, int ptype, cudaStream_t stream) { LBT_RESNORM_DISPATCH(run_forward, a, type, ptype, stream); }
+lbt_status backward_any(const NormArgs& a, const Split& s, int type, int ptype, cudaStream_t stream) {
+    LBT_RESNORM_DISPATCH(run_backward, a, type, ptype, s, stream);
 }
 
 bool off(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
@@ -636,6 +757,7 @@ lbt_status common(const lbt_resnorm_desc* d, NormArgs* a) {
     a->M = d->M;
     a->D = (int)d->D;
     a->rows_per_gate = d->rows_per_gate == 0 ? std::max<int64_t>(d->M, 1) : d->rows_per_gate;
+    a->one_gate = a->rows_per_gate >= d->M;
     a->layer = d->kind == LBT_NORM_LAYER;
     a->post = d->post_norm != 0;
     a->eps_post = d->eps_post; a->eps_pre = d->eps_pre; a->scale_x = d->scale_x; a->scale_h = d->scale_h;
@@ -685,9 +807,7 @@ extern "C" lbt_status lbt_resnorm_forward(const lbt_resnorm_desc* d, const void*
     a.q = static_cast<uint8_t*>(q); a.ldq = ldq; a.q_scale = q_scale;
     a.stats = reinterpret_cast<float4*>(stats);
     const cudaStream_t stream = as_stream(cuda_stream);
-    if (d->type == LBT_F32) return run_forward<float>(a, stream);
-    if (d->type == LBT_BF16) return run_forward<__nv_bfloat16>(a, stream);
-    return run_forward<__half>(a, stream);
+    return forward_any(a, d->type, d->param_type, stream);
 }
 
 extern "C" size_t lbt_resnorm_workspace_bytes(const lbt_resnorm_desc* d) {
@@ -727,7 +847,7 @@ extern "C" lbt_status lbt_resnorm_backward(const lbt_resnorm_desc* d, const void
             vec_ok(dx, a.ld_dx, d->type) && vec_ok(dh, a.ld_dh, d->type);
     a.gate = make_param(gate, d->param_type, a.D);
     a.w_post = make_param(w_post, d->param_type, a.D); a.b_post = make_param(b_post, d->param_type, a.D);
-    a.w_pre = make_param(w_pre, d->param_type, a.D);
+    a.w_pre = make_param(w_pre, d->param_type, a.D); a.b_pre = make_param(nullptr, d->param_type, a.D);
     a.stats = reinterpret_cast<float4*>(const_cast<float*>(stats));
     a.rows_each = s.rows_each; a.parts = s.parts;
     auto at = [&](size_t o, void* wanted) { return wanted != nullptr ? reinterpret_cast<float*>(base + o) : nullptr; };
@@ -735,9 +855,7 @@ extern "C" lbt_status lbt_resnorm_backward(const lbt_resnorm_desc* d, const void
     a.part_w_pre = at(w.w_pre, dw_pre); a.part_b_pre = at(w.b_pre, db_pre);
     a.part_gate = reinterpret_cast<float*>(base + w.gate);
     a.dgate = dgate;
-    if (d->type == LBT_F32) rc = a.layer ? run_backward<float, true>(a, s, stream) : run_backward<float, false>(a, s, stream);
-    else if (d->type == LBT_BF16) rc = a.layer ? run_backward<__nv_bfloat16, true>(a, s, stream) : run_backward<__nv_bfloat16, false>(a, s, stream);
-    else rc = a.layer ? run_backward<__half, true>(a, s, stream) : run_backward<__half, false>(a, s, stream);
+    rc = backward_any(a, s, d->type, d->param_type, stream);
     if (rc != LBT_OK) return rc;
     FinishArgs f{};
     f.D = a.D; f.blocks = s.blocks; f.type = d->param_type;
