@@ -6,13 +6,15 @@
 // 8-bit moments: a tensor's elements fall into blocks of 256; m and u = sqrt(v) are kept as e4m3 codes of x * 448 / max|x|
 // with the block's scale max|x| / 448 in fp32.  The root is stored because its ratios are the square roots of v's: e4m3
 // spans 2^17.8 from its smallest to its largest number, so a block holds v's that differ by 2^35.  A positive root never
-// becomes code 0 (it takes the smallest one): a vanished denominator would turn a small step into m / eps.  All of the
-// arithmetic is fp32 with each operation rounded once (no contraction), so a step is reproducible operation for operation.
+// becomes code 0 (it takes the smallest one): a vanished denominator would turn a small step into m / eps.  The moments are
+// fp32 with each operation rounded once (no contraction), so their codes are reproducible operation for operation; the
+// quotient of the update is good to 2 ulp.
 //
 // The step is bound by memory: 14 bytes per element with fp32 parameters, bf16 gradients and 8-bit moments, 28 with all of
 // it in fp32.  A block of 256 elements is one warp's work (8 consecutive elements a lane: 32-byte accesses of fp32, 16 of
-// bf16, 8 of codes), so that a block's maximum is one warp reduction and nothing is shared between warps.  The table of
-// tensors travels as a kernel argument: no device memory, no copy ahead of the launch.
+// bf16, 8 of codes), so that a block's maximum is one warp reduction and nothing is shared between warps; 64 registers keep 32
+// warps on an SM, which hide the loads better than copies ahead through shared memory did with 24 (fp32 states: 57 against 80 us).  The table of tensors travels as a kernel
+// argument: no device memory, no copy ahead of the launch.
 #include <math.h>
 
 #include <algorithm>
@@ -25,6 +27,7 @@ constexpr int kAdamBlock = 256;
 constexpr int kAdamMax = 400;       // tensors per launch: the table fits the 32 764 bytes of a kernel's arguments
 constexpr int kAdamFew = 40;        // a small table for few tensors: a launch that copies 3 KB of arguments instead of 30
 constexpr int kAdamThreads = 256;
+constexpr int kAdamRun = 8;         // blocks a warp takes at a time: their scales are one 32-byte sector
 
 struct AdamEntry {
     void* p;
@@ -42,9 +45,9 @@ struct AdamEntry {
 template <int kCap>
 struct AdamTable {
     AdamEntry e[kCap];
-    uint32_t first[kCap + 1];   // first block of 256 of each tensor; first[count] = all of them
+    uint32_t first[kCap + 1];   // first run of blocks of each tensor; first[count] = all of them
     int count;
-    int run;                    // consecutive blocks a warp takes at a time
+    int run;                    // blocks of a run: kAdamRun, or 1
     float b1, omb1, b2, omb2, inv_c2, eps;
     const float* grad_scale;
     const int32_t* skip;
@@ -60,17 +63,6 @@ __device__ __forceinline__ void adam_store(void* p, int type, uint64_t i, float 
     else if (type == LBT_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
     else static_cast<__half*>(p)[i] = __float2half_rn(v);
 }
-__device__ __forceinline__ void adam_load8(const void* p, int type, uint64_t i, float (&f)[8]) {
-    if (type == LBT_F32) load8(static_cast<const float*>(p) + i, f);
-    else if (type == LBT_BF16) load8(static_cast<const __nv_bfloat16*>(p) + i, f);
-    else load8(static_cast<const __half*>(p) + i, f);
-}
-__device__ __forceinline__ void adam_store8(void* p, int type, uint64_t i, const float (&f)[8]) {
-    if (type == LBT_F32) store8(static_cast<float*>(p) + i, f);
-    else if (type == LBT_BF16) store8(static_cast<__nv_bfloat16*>(p) + i, f);
-    else store8(static_cast<__half*>(p) + i, f);
-}
-
 // e4m3 code (nearest, ties to even, saturating; NaN stays NaN) and back
 __device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
     uint16_t r;
@@ -87,13 +79,26 @@ struct AdamConst {
     float b1, omb1, b2, omb2, inv_c2, eps, gs;
 };
 
+// sqrt(v) by Markstein's correction (Computation of Elementary Functions on the IBM RISC System/6000, 1990): s = v y with y a
+// hardware reciprocal root, then s + (v - s s) y / 2 with the residual exact in one fused operation.  Rounds as sqrtf does but
+// for about one v in 2^22; below the normal range (v < 2^-126, where eps is all of the denominator) the root is underestimated.
+// sqrtf's own special cases took a fifth of the step's instructions.
+__device__ __forceinline__ float adam_root(float v) {
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(v, 1.17549435e-38f)));
+    const float s = __fmul_rn(v, y);
+    return __fmaf_rn(__fmaf_rn(-s, s, v), __fmul_rn(0.5f, y), s);
+}
+
 // one element; returns u = sqrt(v)
 __device__ __forceinline__ float adam_update(const AdamConst& c, float step_size, float decay, float g, float& p, float& m, float& v) {
     g = __fmul_rn(g, c.gs);
     m = __fadd_rn(__fmul_rn(c.b1, m), __fmul_rn(c.omb1, g));
     v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.omb2, __fmul_rn(g, g)));
-    const float u = __fsqrt_rn(v);
-    p = __fsub_rn(__fmul_rn(decay, p), __fdiv_rn(__fmul_rn(step_size, m), __fadd_rn(__fmul_rn(u, c.inv_c2), c.eps)));
+    const float u = adam_root(v);
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__fadd_rn(__fmul_rn(u, c.inv_c2), c.eps)));
+    p = __fsub_rn(__fmul_rn(decay, p), __fmul_rn(__fmul_rn(step_size, m), inv));
     return u;
 }
 
@@ -103,102 +108,91 @@ __device__ __forceinline__ void block_scale(uint32_t most_bits, float& scale, fl
     scale = __fmul_rn(most, 1.0f / 448.0f);
     factor = most > 1e-36f ? __fmul_rn(__frcp_rn(most), 448.0f) : 0.0f;
 }
-// what is stored of one element: NaN where it is not finite
-__device__ __forceinline__ float scaled(float x, float factor, bool root) {
-    if (abs_bits(x) >= kNonFinite) return __uint_as_float(0x7FC00000u);
-    const float s = __fmul_rn(x, factor);
-    return root && x > 0.0f ? fmaxf(s, 0.001953125f) : s;   // 2^-9, the smallest positive e4m3
-}
-
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-    const uint32_t b = abs_bits(x);
-    return b < kNonFinite ? b : 0u;
-}
-
-// One block of 256 elements of one tensor, kN of them present (kFull: all 256, aligned, eight consecutive ones a lane;
-// else element 32 j + lane, one by one).
-template <int kBits, bool kFull>
-__device__ __forceinline__ void adam_block(const AdamEntry& e, const AdamConst& c, uint64_t block, int lane) {
-    const uint64_t base = block * kAdamBlock;
-    const int p_type = e.types & 15, g_type = (e.types >> 4) & 15;
-    float p[8], g[8], m[8], v[8];
-    const uint64_t at = base + (kFull ? lane * 8 : lane);
-    const int have = kFull ? 8 : (e.n > at ? (int)min((e.n - at + 31) / 32, (uint64_t)8) : 0);
-    float ms = 0.0f, vs = 0.0f;
-    if (kBits == 8) { ms = e.m_scale[block]; vs = e.v_scale[block]; }
-    if (kFull) {
-        adam_load8(e.p, p_type, at, p);
-        adam_load8(e.g, g_type, at, g);
-        if (kBits == 32) {
-            load8(static_cast<const float*>(e.m) + at, m);
-            load8(static_cast<const float*>(e.v) + at, v);
-        } else {
-            const uint2 mc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(e.m) + at);
-            const uint2 vc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(e.v) + at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 a = e4m3_values(((i < 2 ? mc.x : mc.y) >> (16 * (i & 1))) & 0xFFFFu);
-                const float2 b = e4m3_values(((i < 2 ? vc.x : vc.y) >> (16 * (i & 1))) & 0xFFFFu);
-                m[2 * i] = a.x; m[2 * i + 1] = a.y; v[2 * i] = b.x; v[2 * i + 1] = b.y;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            p[i] = g[i] = m[i] = v[i] = 0.0f;
-            if (i < have) {
-                const uint64_t k = at + 32 * i;
-                p[i] = adam_load(e.p, p_type, k);
-                g[i] = adam_load(e.g, g_type, k);
-                if (kBits == 32) {
-                    m[i] = static_cast<const float*>(e.m)[k];
-                    v[i] = static_cast<const float*>(e.v)[k];
-                } else {
-                    m[i] = e4m3_values(static_cast<const uint8_t*>(e.m)[k]).x;
-                    v[i] = e4m3_values(static_cast<const uint8_t*>(e.v)[k]).x;
-                }
-            }
-        }
-    }
-    float u[8];
-    uint32_t most_m = 0, most_u = 0;
+// The moments of a lane's eight elements as the block stores them: scales, and codes ready to be rounded.  Every warp takes the
+// short way unless its block has a root of 0 or something that is not finite: then the largest finite magnitude decides the
+// scale, what is not finite is stored as NaN, and a root of 0 stays 0.
+__device__ __forceinline__ void block_codes(float (&m)[8], float (&u)[8], float& ms, float& vs) {
+    float top_m = 0.0f, low_u = 1.0f;
+    uint32_t most_u = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        if (kBits == 8) {
-            m[i] = __fmul_rn(m[i], ms);
-            v[i] = __fmul_rn(v[i], vs);
-            v[i] = __fmul_rn(v[i], v[i]);
-        }
-        u[i] = adam_update(c, e.step_size, e.decay, g[i], p[i], m[i], v[i]);
-        if (kBits == 8 && (kFull || i < have)) {
-            most_m = max(most_m, finite_bits(m[i]));
-            most_u = max(most_u, finite_bits(u[i]));
-        }
+        top_m = fmaxf(top_m, fabsf(m[i]));   // (passes over NaN)
+        most_u = max(most_u, __float_as_uint(u[i]));
+        low_u = fminf(low_u, u[i]);
     }
-    if (kFull) adam_store8(e.p, p_type, at, p);
-    else
+    uint32_t most_m = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top_m));
+    most_u = __reduce_max_sync(0xFFFFFFFFu, most_u & 0x7FFFFFFFu);
+    const bool odd = max(most_m, most_u) >= kNonFinite || __any_sync(0xFFFFFFFFu, !(low_u > 0.0f));
+    if (odd) {
+        most_m = most_u = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < have) adam_store(e.p, p_type, at + 32 * i, p[i]);
-    if (kBits == 32) {
-        if (kFull) {
-            store8(static_cast<float*>(e.m) + at, m);
-            store8(static_cast<float*>(e.v) + at, v);
-        } else
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < have) {
-                    static_cast<float*>(e.m)[at + 32 * i] = m[i];
-                    static_cast<float*>(e.v)[at + 32 * i] = v[i];
-                }
-        return;
+        for (int i = 0; i < 8; ++i) {
+            if (abs_bits(m[i]) >= kNonFinite) m[i] = __uint_as_float(0x7FC00000u); else most_m = max(most_m, abs_bits(m[i]));
+            if (abs_bits(u[i]) >= kNonFinite) u[i] = __uint_as_float(0x7FC00000u); else most_u = max(most_u, abs_bits(u[i]));
+        }
+        most_m = __reduce_max_sync(0xFFFFFFFFu, most_m);
+        most_u = __reduce_max_sync(0xFFFFFFFFu, most_u);
     }
     float fm, fu;
-    block_scale(__reduce_max_sync(0xFFFFFFFFu, most_m), ms, fm);
-    block_scale(__reduce_max_sync(0xFFFFFFFFu, most_u), vs, fu);
+    block_scale(most_m, ms, fm);
+    block_scale(most_u, vs, fu);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { m[i] = scaled(m[i], fm, false); u[i] = scaled(u[i], fu, true); }
-    if (kFull) {
+    for (int i = 0; i < 8; ++i) {
+        m[i] = __fmul_rn(m[i], fm);
+        const float s = __fmul_rn(u[i], fu);   // a positive root takes at least 2^-9, the smallest positive e4m3
+        u[i] = !odd || u[i] > 0.0f ? fmaxf(s, 0.001953125f) : s;
+    }
+}
+
+// What a lane reads of a whole, aligned block.
+template <int kBits, typename P, typename G>
+struct AdamRaw {
+    Vec8<P> p;
+    Vec8<G> g;
+    uint32_t m[kBits / 4], v[kBits / 4];   // 8 bytes of codes, or 32 of fp32
+
+    __device__ __forceinline__ void load(const AdamEntry& e, uint64_t block, int lane) {
+        const uint64_t at = block * kAdamBlock + lane * 8;
+        ld_vec(static_cast<const P*>(e.p) + at, p.w);
+        ld_vec(static_cast<const G*>(e.g) + at, g.w);
+        if constexpr (kBits == 32) {
+            ld_vec(static_cast<const float*>(e.m) + at, m);
+            ld_vec(static_cast<const float*>(e.v) + at, v);
+        } else {
+            const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(e.m) + at);
+            const uint2 b = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(e.v) + at);
+            m[0] = a.x; m[1] = a.y; v[0] = b.x; v[1] = b.y;
+        }
+    }
+};
+
+template <int kBits, typename P, typename G>
+__device__ __forceinline__ void adam_whole(const AdamEntry& e, const AdamConst& c, const AdamRaw<kBits, P, G>& raw, float& ms, float& vs, uint64_t block, int lane) {
+    const uint64_t at = block * kAdamBlock + lane * 8;
+    float p[8], g[8], m[8], v[8], u[8];
+    unpack(raw.p, p);
+    unpack(raw.g, g);
+    if constexpr (kBits == 32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { m[i] = __uint_as_float(raw.m[i]); v[i] = __uint_as_float(raw.v[i]); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = e4m3_values(raw.m[i >> 1] >> (16 * (i & 1))), b = e4m3_values(raw.v[i >> 1] >> (16 * (i & 1)));
+            m[2 * i] = __fmul_rn(a.x, ms); m[2 * i + 1] = __fmul_rn(a.y, ms);
+            v[2 * i] = __fmul_rn(b.x, vs); v[2 * i + 1] = __fmul_rn(b.y, vs);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = adam_update(c, e.step_size, e.decay, g[i], p[i], m[i], v[i]);
+    store8(static_cast<P*>(e.p) + at, p);
+    if constexpr (kBits == 32) {
+        store8(static_cast<float*>(e.m) + at, m);
+        store8(static_cast<float*>(e.v) + at, v);
+    } else {
+        block_codes(m, u, ms, vs);
         uint32_t mc[2], vc[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -207,52 +201,116 @@ __device__ __forceinline__ void adam_block(const AdamEntry& e, const AdamConst& 
         }
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.m) + at) = make_uint2(mc[0], mc[1]);
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.v) + at) = make_uint2(vc[0], vc[1]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < have) {
-                static_cast<uint8_t*>(e.m)[at + 32 * i] = (uint8_t)e4m3_pair(m[i], 0.0f);
-                static_cast<uint8_t*>(e.v)[at + 32 * i] = (uint8_t)e4m3_pair(u[i], 0.0f);
-            }
     }
-    if (lane == 0) { e.m_scale[block] = ms; e.v_scale[block] = vs; }
+}
+
+// Whole blocks [b, end) of one tensor, at most kAdamRun of them.  Their scales are read and written together, block b + l's by
+// lane l: warps that wrote four bytes each into a sector they shared with others' cost the 0.4 G element step 410 of 1315 us.
+template <int kBits, typename P, typename G>
+__device__ __forceinline__ void adam_run(const AdamEntry& e, const AdamConst& c, uint64_t b, uint64_t end, int lane) {
+    const int count = (int)(end - b);
+    float old_ms = 0.0f, old_vs = 0.0f, new_ms = 0.0f, new_vs = 0.0f;
+    if (kBits == 8 && lane < count) { old_ms = e.m_scale[b + lane]; old_vs = e.v_scale[b + lane]; }
+#pragma unroll 1
+    for (int k = 0; k < count; ++k) {
+        AdamRaw<kBits, P, G> now;
+        now.load(e, b + k, lane);
+        float ms = 0.0f, vs = 0.0f;
+        if (kBits == 8) { ms = __shfl_sync(0xFFFFFFFFu, old_ms, k); vs = __shfl_sync(0xFFFFFFFFu, old_vs, k); }
+        adam_whole(e, c, now, ms, vs, b + k, lane);
+        if (lane == k) { new_ms = ms; new_vs = vs; }
+    }
+    if (kBits == 8 && lane < count) { e.m_scale[b + lane] = new_ms; e.v_scale[b + lane] = new_vs; }
+}
+
+// A block element by element (32 j + lane): the end of a tensor, or tensors that are not aligned.
+template <int kBits>
+__device__ __noinline__ void adam_ragged(const AdamEntry& e, const AdamConst& c, uint64_t block, int lane) {
+    const int p_type = e.types & 15, g_type = (e.types >> 4) & 15;
+    const uint64_t at = block * kAdamBlock + lane;
+    const int have = e.n > at ? (int)min((e.n - at + 31) / 32, (uint64_t)8) : 0;
+    const float ms = kBits == 8 ? e.m_scale[block] : 0.0f, vs = kBits == 8 ? e.v_scale[block] : 0.0f;
+    float p[8], m[8], v[8], u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float g = 0.0f;
+        p[i] = m[i] = v[i] = u[i] = 0.0f;
+        if (i < have) {
+            const uint64_t k = at + 32 * i;
+            p[i] = adam_load(e.p, p_type, k);
+            g = adam_load(e.g, g_type, k);
+            if (kBits == 32) {
+                m[i] = static_cast<const float*>(e.m)[k];
+                v[i] = static_cast<const float*>(e.v)[k];
+            } else {
+                m[i] = __fmul_rn(e4m3_values(static_cast<const uint8_t*>(e.m)[k]).x, ms);
+                v[i] = __fmul_rn(e4m3_values(static_cast<const uint8_t*>(e.v)[k]).x, vs);
+                v[i] = __fmul_rn(v[i], v[i]);
+            }
+            u[i] = adam_update(c, e.step_size, e.decay, g, p[i], m[i], v[i]);
+            adam_store(e.p, p_type, k, p[i]);
+            if (kBits == 32) {
+                static_cast<float*>(e.m)[k] = m[i];
+                static_cast<float*>(e.v)[k] = v[i];
+            }
+        }
+    }
+    if (kBits == 32) return;
+    float new_ms, new_vs;
+    __syncwarp();
+    block_codes(m, u, new_ms, new_vs);   // (an absent element's moments are 0)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < have) {
+            static_cast<uint8_t*>(e.m)[at + 32 * i] = (uint8_t)e4m3_pair(m[i], 0.0f);
+            static_cast<uint8_t*>(e.v)[at + 32 * i] = (uint8_t)e4m3_pair(u[i], 0.0f);
+        }
+    if (lane == 0) { e.m_scale[block] = new_ms; e.v_scale[block] = new_vs; }
+}
+
+template <int kBits, typename P>
+__device__ __forceinline__ void adam_run_g(const AdamEntry& e, const AdamConst& c, uint64_t b, uint64_t end, int lane) {
+    const int g_type = (e.types >> 4) & 15;
+    if (g_type == LBT_F32) adam_run<kBits, P, float>(e, c, b, end, lane);
+    else if (g_type == LBT_BF16) adam_run<kBits, P, __nv_bfloat16>(e, c, b, end, lane);
+    else adam_run<kBits, P, __half>(e, c, b, end, lane);
 }
 
 template <int kBits, int kCap>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamTable<kCap> t) {
+__global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ AdamTable<kCap> t) {
     __shared__ uint32_t first[kCap + 1];
     if (t.skip != nullptr && *t.skip != 0) return;
     for (int i = threadIdx.x; i <= t.count; i += kAdamThreads) first[i] = t.first[i];
     __syncthreads();
     const int lane = threadIdx.x & 31;
     const AdamConst c{t.b1, t.omb1, t.b2, t.omb2, t.inv_c2, t.eps, t.grad_scale != nullptr ? *t.grad_scale : 1.0f};
-    const uint64_t all = first[t.count], stride = (uint64_t)gridDim.x * (kAdamThreads / 32) * t.run;
-    for (uint64_t b0 = ((uint64_t)blockIdx.x * (kAdamThreads / 32) + (threadIdx.x >> 5)) * t.run; b0 < all; b0 += stride) {
-        int lo = 0, hi = t.count;   // the tensor of block b0: the last with first <= b0 (empty tensors share their successor's first)
+    const uint32_t all = first[t.count];
+    const uint64_t stride = (uint64_t)gridDim.x * (kAdamThreads / 32);
+    for (uint64_t r = (uint64_t)blockIdx.x * (kAdamThreads / 32) + (threadIdx.x >> 5); r < all; r += stride) {
+        int lo = 0, hi = t.count;   // the tensor of run r: the last with first <= r (empty tensors share their successor's first)
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (first[mid] <= b0) lo = mid; else hi = mid;
+            if (first[mid] <= r) lo = mid; else hi = mid;
         }
-        const uint64_t end = min(b0 + t.run, all);
-        for (uint64_t b = b0; b < end; ++b) {
-            while (b >= first[lo + 1]) ++lo;
-            const AdamEntry& e = t.e[lo];
-            const uint64_t block = b - first[lo];
-            if ((e.types >> 8) != 0 && (block + 1) * kAdamBlock <= e.n) adam_block<kBits, true>(e, c, block, lane);
-            else adam_block<kBits, false>(e, c, block, lane);
+        const AdamEntry& e = t.e[lo];
+        const uint64_t b = (r - first[lo]) * t.run, end = min(b + t.run, (e.n + kAdamBlock - 1) / kAdamBlock);
+        const uint64_t whole = (e.types >> 8) != 0 ? max(b, min(end, e.n / kAdamBlock)) : b;
+        if (b < whole) {
+            const int p_type = e.types & 15;
+            if (p_type == LBT_F32) adam_run_g<kBits, float>(e, c, b, whole, lane);
+            else if (p_type == LBT_BF16) adam_run_g<kBits, __nv_bfloat16>(e, c, b, whole, lane);
+            else adam_run_g<kBits, __half>(e, c, b, whole, lane);
         }
+        for (uint64_t k = whole; k < end; ++k) adam_ragged<kBits>(e, c, k, lane);
     }
 }
 
 template <int kBits, int kCap>
-static lbt_status adamw_launch(AdamTable<kCap>& t, cudaStream_t stream) {
-    const uint64_t blocks = t.first[t.count];
-    if (blocks == 0) return LBT_OK;
-    // Few blocks: one a warp, spread over the SMs; many: runs of four, which amortise the search for the tensor.
+static lbt_status adamw_launch(const AdamTable<kCap>& t, cudaStream_t stream) {
+    const uint64_t runs = t.first[t.count];
+    if (runs == 0) return LBT_OK;
     constexpr int warps = kAdamThreads / 32;
-    t.run = blocks <= (uint64_t)kNumSMs * warps * 8 ? 1 : 4;
-    const uint64_t want = (blocks + (uint64_t)warps * t.run - 1) / ((uint64_t)warps * t.run);
-    const int grid = (int)std::min<uint64_t>(want, (uint64_t)kNumSMs * 32);
+    const int grid = (int)std::min<uint64_t>((runs + warps - 1) / warps, (uint64_t)kNumSMs * 32);
     adamw_kernel<kBits, kCap><<<grid, kAdamThreads, 0, stream>>>(t);
     return launch_status();
 }
@@ -269,7 +327,10 @@ static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lb
     t.grad_scale = grad_scale;
     t.skip = skip;
     t.count = count;
-    uint64_t at = 0;
+    uint64_t blocks = 0, at = 0;
+    for (int i = 0; i < count; ++i) blocks += (tensors[i].n + kAdamBlock - 1) / kAdamBlock;
+    // Few blocks: each its own warp's; enough of them to fill the SMs four times over: in runs of eight.
+    t.run = blocks <= (uint64_t)kNumSMs * 32 * 4 ? 1 : kAdamRun;
     for (int i = 0; i < count; ++i) {
         const lbt_adamw_tensor& s = tensors[i];
         AdamEntry& e = t.e[i];
@@ -282,8 +343,7 @@ static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lb
         const bool aligned = ok(s.p, 8 * type_size(s.p_type)) && ok(s.g, 8 * type_size(s.g_type)) && ok(s.m, state) && ok(s.v, state);
         e.types = s.p_type | s.g_type << 4 | (aligned ? 1 << 8 : 0);
         t.first[i] = (uint32_t)at;
-        at += (s.n + kAdamBlock - 1) / kAdamBlock;
-        if (at > 0xFFFFFFFFull) return LBT_ERR_UNSUPPORTED;
+        at += ((s.n + kAdamBlock - 1) / kAdamBlock + t.run - 1) / t.run;
     }
     t.first[count] = (uint32_t)at;
     return h->state_bits == 8 ? adamw_launch<8, kCap>(t, stream) : adamw_launch<32, kCap>(t, stream);
