@@ -437,7 +437,8 @@ lbt_status lbt_resnorm_backward(const lbt_resnorm_desc *d, const void *dr, const
  * One AdamW step (decoupled weight decay) over `count` tensors, one launch per 400 of them:
  *   g' = g * *d_grad_scale (1 if NULL);  m = b1 m + (1 - b1) g';  v = b2 v + (1 - b2) g'^2;
  *   p = (1 - lr wd) p - (lr / (1 - b1^step)) m / (sqrt(v) / sqrt(1 - b2^step) + eps)
- * in fp32, every operation rounded once; p is rounded to its type once.  step counts from 1.  *d_skip != 0 (device int32, may be
+ * in fp32: the moments with every operation rounded once, the quotient of p's update within 2 ulp (v below 2^-126 counts as
+ * nearly 0 there); p is rounded to its type once.  step counts from 1.  *d_skip != 0 (device int32, may be
  * NULL): nothing changes (a step whose gradients overflowed).
  * state_bits 32: m, v fp32.  state_bits 8: m and the root of v as e4m3 codes, one byte an element, in blocks of 256 consecutive
  * elements of a tensor: value = code * scale, scale = fl(max / 448) over the block's finite values, m_scale / v_scale:

@@ -13,7 +13,7 @@
 // The step is bound by memory: 14 bytes per element with fp32 parameters, bf16 gradients and 8-bit moments, 28 with all of
 // it in fp32.  A block of 256 elements is one warp's work (8 consecutive elements a lane: 32-byte accesses of fp32, 16 of
 // bf16, 8 of codes), so that a block's maximum is one warp reduction and nothing is shared between warps; 64 registers keep 32
-// warps on an SM, which hide the loads better than copies ahead through shared memory did with 24 (fp32 states: 57 against 80 us).  The table of tensors travels as a kernel
+// warps on an SM, which hide the loads better than copies ahead through shared memory did with 24 (fp32 states: 55 against 80 us).  The table of tensors travels as a kernel
 // argument: no device memory, no copy ahead of the launch.
 #include <math.h>
 
@@ -25,7 +25,8 @@ namespace lbt {
 
 constexpr int kAdamBlock = 256;
 constexpr int kAdamMax = 400;       // tensors per launch: the table fits the 32 764 bytes of a kernel's arguments
-constexpr int kAdamFew = 40;        // a small table for few tensors: a launch that copies 3 KB of arguments instead of 30
+constexpr int kAdamFew = 40;        // smaller tables for fewer tensors: a launch copies 3 or 10 KB of arguments instead of 30
+constexpr int kAdamSome = 128;      //   (the call takes 4.5, 5.5 and 7.5 us of the host's time)
 constexpr int kAdamThreads = 256;
 constexpr int kAdamRun = 8;         // blocks a warp takes at a time: their scales are one 32-byte sector
 
@@ -225,7 +226,7 @@ __device__ __forceinline__ void adam_run(const AdamEntry& e, const AdamConst& c,
 
 // A block element by element (32 j + lane): the end of a tensor, or tensors that are not aligned.
 template <int kBits>
-__device__ __noinline__ void adam_ragged(const AdamEntry& e, const AdamConst& c, uint64_t block, int lane) {
+__device__ __forceinline__ void adam_ragged(const AdamEntry& e, const AdamConst& c, uint64_t block, int lane) {
     const int p_type = e.types & 15, g_type = (e.types >> 4) & 15;
     const uint64_t at = block * kAdamBlock + lane;
     const int have = e.n > at ? (int)min((e.n - at + 31) / 32, (uint64_t)8) : 0;
@@ -329,8 +330,9 @@ static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lb
     t.count = count;
     uint64_t blocks = 0, at = 0;
     for (int i = 0; i < count; ++i) blocks += (tensors[i].n + kAdamBlock - 1) / kAdamBlock;
-    // Few blocks: each its own warp's; enough of them to fill the SMs four times over: in runs of eight.
-    t.run = blocks <= (uint64_t)kNumSMs * 32 * 4 ? 1 : kAdamRun;
+    // Runs of eight where there are scales and blocks enough to fill the SMs four times over (0.4 G elements: 890 us, one by one
+    // 1209 us); else block by block (fp32 states, 11.7 M elements: 55 us, in runs of eight 60 us; few blocks: all warps at work).
+    t.run = h->state_bits == 8 && blocks > (uint64_t)kNumSMs * 32 * 4 ? kAdamRun : 1;
     for (int i = 0; i < count; ++i) {
         const lbt_adamw_tensor& s = tensors[i];
         AdamEntry& e = t.e[i];
@@ -377,8 +379,9 @@ extern "C" lbt_status lbt_adamw_step(const lbt_adamw_tensor* tensors, int count,
     const cudaStream_t stream = as_stream(cuda_stream);
     for (int i = 0; i < count; i += kAdamMax) {
         const int n = std::min(count - i, kAdamMax);
-        const lbt_status rc = n <= kAdamFew ? adamw_run<kAdamFew>(tensors + i, n, h, d_grad_scale, d_skip, stream)
-                                            : adamw_run<kAdamMax>(tensors + i, n, h, d_grad_scale, d_skip, stream);
+        const lbt_status rc = n <= kAdamFew    ? adamw_run<kAdamFew>(tensors + i, n, h, d_grad_scale, d_skip, stream)
+                              : n <= kAdamSome ? adamw_run<kAdamSome>(tensors + i, n, h, d_grad_scale, d_skip, stream)
+                                               : adamw_run<kAdamMax>(tensors + i, n, h, d_grad_scale, d_skip, stream);
         if (rc != LBT_OK) return rc;
     }
     return LBT_OK;

@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 #include "lbt_sm100.cuh"
 #include "lbt_types.cuh"
@@ -531,6 +532,140 @@ rows8_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, bo
     }
 }
 
+// ------------------------------------------------------------------------------------------ few tokens
+// A handful of tokens: the time is the weights' way from memory, each byte used once.  A block owns 16 output channels, its
+// eight warps take 64-byte pieces of their rows in turn, straight into the fragments of m16n8k32 products (A: channels, B: tokens;
+// the reduction may be dealt out in any order as long as both operands agree, so a lane's 16 consecutive bytes are two
+// fragments).  Sixteen 16-byte loads a lane are in flight before the first product; the warps' integer sums meet in shared memory.
+// With T a type the block quantizes the tokens itself (x stays in L2) under the first weights' latency: one launch in all.
+constexpr int kFewTokens = 16;
+constexpr int kFewSmem = 40 * 1024;      // codes of the tokens a block quantizes itself
+constexpr int kFewBatch = 8;             // 64-byte pieces of a row in flight per lane
+
+struct FewArgs {
+    const void* x;
+    int64_t ldx;
+    bool vec;
+    uint8_t* q_x;
+    float* s_x;
+    const uint8_t* q_w;
+    int64_t pitch;
+    int I, M, tokens_pitch;   // tokens_pitch: bytes of a token's codes in shared memory
+    bool wait_prev;
+    L8Args out;               // rows, cols, scales, bias, output
+};
+
+__device__ __forceinline__ uint4 ld_stream(const uint8_t* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ void mma_16832(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <typename T, int kTiles>   // T void: codes come from q_x; kTiles: groups of eight tokens
+__global__ void __launch_bounds__(256) l8_few_kernel(const __grid_constant__ FewArgs a) {
+    constexpr bool kQuantize = !std::is_void<T>::value;
+    extern __shared__ uint8_t codes[];
+    __shared__ int sums[8][kTiles * 8][17];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int64_t o0 = (int64_t)blockIdx.x * 16;
+    const uint8_t* w0 = a.q_w + min(o0 + g, (int64_t)a.out.cols - 1) * a.pitch + 16 * t;
+    const uint8_t* w1 = a.q_w + min(o0 + g + 8, (int64_t)a.out.cols - 1) * a.pitch + 16 * t;
+    const int room = (int)a.pitch - 16 * t;   // bytes of the rows from this lane's first on
+    uint4 lo[kFewBatch], hi[kFewBatch];
+    auto fetch = [&](int piece) {
+#pragma unroll
+        for (int i = 0; i < kFewBatch; ++i) {
+            const int k = (piece + 8 * i) * 64;
+            lo[i] = hi[i] = make_uint4(0, 0, 0, 0);
+            if (k < room) { lo[i] = ld_stream(w0 + k); hi[i] = ld_stream(w1 + k); }
+        }
+    };
+    fetch(warp);
+    float scale[kQuantize ? 4 : 1];
+    if constexpr (kQuantize) {
+        __shared__ uint32_t part[4][8];
+        uint32_t most[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+            if (m < a.M) {
+                const T* row = static_cast<const T*>(a.x) + m * a.ldx;
+                for (int c = threadIdx.x * 8; c < a.I; c += 2048) {
+                    float f[8];
+                    load_group(row, c, a.I, a.vec, f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most[m] = max(most[m], abs_bits(f[i]));
+                }
+                most[m] = __reduce_max_sync(0xFFFFFFFFu, most[m]);
+                if (lane == 0) part[m][warp] = most[m];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+            if (m < a.M) {
+                float factor;
+                scale8(__reduce_max_sync(0xFFFFFFFFu, part[m][lane & 7]), scale[m], factor);
+                const T* row = static_cast<const T*>(a.x) + m * a.ldx;
+                for (int c = threadIdx.x * 8; c < a.tokens_pitch; c += 2048) {
+                    float f[8];
+                    load_group(row, c, a.I, a.vec, f);
+                    const uint2 q = codes8(f, factor);
+                    *reinterpret_cast<uint2*>(codes + m * a.tokens_pitch + c) = q;
+                    if (blockIdx.x == 0 && c < a.pitch) *reinterpret_cast<uint2*>(a.q_x + m * a.pitch + c) = q;
+                }
+                if (blockIdx.x == 0 && threadIdx.x == 0) a.s_x[m] = scale[m];
+            }
+        __syncthreads();
+    } else if (a.wait_prev) {
+        griddep_wait();
+    }
+    int acc[kTiles][4];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[n][i] = 0;
+    for (int piece = warp; piece * 64 < a.pitch; piece += 8 * kFewBatch) {
+        if (piece != warp) fetch(piece);
+#pragma unroll
+        for (int i = 0; i < kFewBatch; ++i) {
+            const int k = (piece + 8 * i) * 64 + 16 * t;
+            if ((piece + 8 * i) * 64 >= a.pitch) break;   // uniform over the warp
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) {
+                const int m = min(n * 8 + g, a.M - 1);    // (columns past M are not stored)
+                uint4 b = make_uint4(0, 0, 0, 0);
+                if (kQuantize) b = *reinterpret_cast<const uint4*>(codes + m * a.tokens_pitch + k);
+                else if (k < a.pitch) b = __ldg(reinterpret_cast<const uint4*>(a.q_x + m * a.pitch + k));
+                mma_16832(acc[n], lo[i].x, hi[i].x, lo[i].y, hi[i].y, b.x, b.y);
+                mma_16832(acc[n], lo[i].z, hi[i].z, lo[i].w, hi[i].w, b.z, b.w);
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+        sums[warp][n * 8 + 2 * t][g] = acc[n][0];
+        sums[warp][n * 8 + 2 * t + 1][g] = acc[n][1];
+        sums[warp][n * 8 + 2 * t][g + 8] = acc[n][2];
+        sums[warp][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
+    }
+    __syncthreads();
+    const int m = threadIdx.x >> 4, r = threadIdx.x & 15;
+    const int64_t o = o0 + r;
+    if (m < a.M && m < kTiles * 8 && o < a.out.cols) {
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += sums[i][m][r];
+        float rs;
+        if constexpr (kQuantize) rs = m == 0 ? scale[0] : m == 1 ? scale[1] : m == 2 ? scale[2] : scale[3];
+        else rs = a.s_x[m];
+        const float bias = a.out.bias != nullptr ? __ldg(a.out.bias + o) : 0.0f;
+        put_one(a.out, m, o, __fadd_rn(__fmul_rn(__int2float_rn(sum), __fmul_rn(rs, __ldg(a.out.col_scale + o))), bias));
+    }
+}
+
 // Gradient quantizer, two passes over dY in tiles of 256 columns x `strip` rows (a warp owns 256 columns and every eighth row).
 // First pass: the largest |dY s_w| of each row, the largest |dY s_x| of each column (as integers: order-free), and with
 // dbias the column sums of each strip.  Second pass: both code matrices and their scales.
@@ -761,6 +896,43 @@ lbt_status quantize_rows_any(const void* x, int type, int64_t rows, int64_t cols
     return quantize_rows(static_cast<const __half*>(x), type, rows, cols, ld, q, ldq, scale, stream);
 }
 
+// Few tokens, from their codes (the quantizer may be the launch ahead) or from x.
+FewArgs few_args(void* q_x, float* s_x, const void* q_w, const float* s_w, const float* bias, void* y, int y_type, int64_t ldy, int64_t M,
+                 int64_t O, int64_t I) {
+    FewArgs a{};
+    a.q_x = static_cast<uint8_t*>(q_x); a.s_x = s_x; a.q_w = static_cast<const uint8_t*>(q_w);
+    a.pitch = pitch16(I); a.I = (int)I; a.M = (int)M;
+    a.tokens_pitch = (int)((I + 63) / 64 * 64);
+    a.out.rows = (int)M; a.out.cols = (int)O; a.out.col_scale = s_w; a.out.bias = bias;
+    a.out.out = y; a.out.out_type = y_type; a.out.ldo = ldy;
+    return a;
+}
+
+lbt_status few_from_codes(FewArgs a, bool behind, cudaStream_t stream) {
+    a.wait_prev = behind;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((a.out.cols + 15) / 16));
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = behind ? 1 : 0;
+    const cudaError_t e = a.M <= 8 ? cudaLaunchKernelEx(&cfg, l8_few_kernel<void, 1>, a) : cudaLaunchKernelEx(&cfg, l8_few_kernel<void, 2>, a);
+    return e == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
+}
+
+lbt_status few_from_x(FewArgs a, const void* x, int x_type, int64_t ldx, cudaStream_t stream) {
+    a.x = x; a.ldx = ldx; a.vec = vec_rows(x, ldx, x_type);
+    const unsigned grid = (unsigned)((a.out.cols + 15) / 16);
+    const size_t smem = (size_t)a.M * a.tokens_pitch;
+    if (x_type == LBT_F32) l8_few_kernel<float, 1><<<grid, 256, smem, stream>>>(a);
+    else if (x_type == LBT_BF16) l8_few_kernel<__nv_bfloat16, 1><<<grid, 256, smem, stream>>>(a);
+    else l8_few_kernel<__half, 1><<<grid, 256, smem, stream>>>(a);
+    return launch_status();
+}
+
 bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
 
 lbt_status check_sizes(int64_t M, int64_t O, int64_t I) {
@@ -822,6 +994,8 @@ extern "C" lbt_status lbt_rows8_quantize(const void* x, int x_type, int64_t rows
 
 static lbt_status forward_product(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, void* y, int y_type,
                                   int64_t ldy, int64_t M, int64_t O, int64_t I, bool behind, int32_t* status, cudaStream_t stream) {
+    if (M <= kFewTokens)
+        return few_from_codes(few_args(const_cast<void*>(q_x), const_cast<float*>(s_x), q_w, s_w, bias, y, y_type, ldy, M, O, I), behind, stream);
     Product p{};
     p.mode = kForward;
     p.A = q_x; p.a_pitch = pitch16(I); p.a_rows = M;
@@ -854,6 +1028,9 @@ extern "C" lbt_status lbt_linear8_forward(const void* x, int x_type, int64_t ldx
     if (misaligned(x, type_size(x_type))) return LBT_ERR_ALIGNMENT;
     if (M == 0) return LBT_OK;
     const cudaStream_t stream = as_stream(cuda_stream);
+    // One to four tokens: every block quantizes them for itself, one launch.
+    if (M <= 4 && M * ((I + 63) / 64 * 64) <= kFewSmem)
+        return few_from_x(few_args(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I), x, x_type, ldx, stream);
     rc = quantize_rows_any(x, x_type, M, I, ldx, q_x, pitch16(I), s_x, stream);
     if (rc != LBT_OK) return rc;
     return forward_product(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I, true, dev_status, stream);

@@ -330,12 +330,18 @@ def quantize_grad_fused(dY, state, stats, q_out, stream=None):
 
 def _rows(t, name, cols=None):
     """Address, element type and leading dimension of a [rows, cols] CUDA tensor whose rows are contiguous."""
-    if not t.is_cuda or t.dim() != 2 or t.dtype not in TYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+    kind, shape, stride = TYPES.get(t.dtype), t.shape, t.stride()
+    if kind is None or len(shape) != 2 or not t.is_cuda or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{name}: a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows")
-    if cols is not None and t.shape[1] != cols:
-        raise ValueError(f"{name}: {t.shape[1]} columns, {cols} expected")
-    # (one row, or rows that overlap by a stride of 0 as an expanded tensor has: the latter is refused by the library)
-    return t.data_ptr(), TYPES[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if cols is not None and shape[1] != cols:
+        raise ValueError(f"{name}: {shape[1]} columns, {cols} expected")
+    # (rows that overlap, as an expanded tensor's do, are refused by the library)
+    return t.data_ptr(), kind, stride[0] if shape[0] > 1 else shape[1]
+
+
+def _raw_stream(t, stream=None) -> int:
+    """The stream a call on `t` goes to: the one given, else torch's current stream of t's device."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _scratch(nbytes, device, stream):
@@ -368,7 +374,7 @@ def rows8_quantize(x, q, scale, stream=None):
     px, tx, ld = _rows(x, "x")
     rows, cols = x.shape
     _check(lib().lbt_rows8_quantize(px, tx, rows, cols, ld, _codes(q, rows, cols, "q"), pitch8(cols), _floats(scale, rows, "scale"),
-                                    _stream(stream)), "lbt_rows8_quantize")
+                                    _raw_stream(x, stream)), "lbt_rows8_quantize")
 
 
 def linear8_forward(x, q_w, s_w, y, q_x, s_x, bias=None, dev_status=None, stream=None):
@@ -380,7 +386,7 @@ def linear8_forward(x, q_w, s_w, y, q_x, s_x, bias=None, dev_status=None, stream
     if y.shape[0] != M:
         raise ValueError("y: one row per row of x")
     _check(lib().lbt_linear8_forward(px, tx, ldx, _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"), _floats(bias, O, "bias"), py, ty, ldy,
-                                     M, O, I, _codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _p(dev_status), _stream(stream)),
+                                     M, O, I, _codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _p(dev_status), _raw_stream(x, stream)),
            "lbt_linear8_forward")
 
 
@@ -391,7 +397,7 @@ def linear8_matmul(q_x, s_x, q_w, s_w, y, I, bias=None, dev_status=None, stream=
     if y.shape[0] != M:
         raise ValueError("y: one row per row of codes")
     _check(lib().lbt_linear8_matmul(_codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"),
-                                    _floats(bias, O, "bias"), py, ty, ldy, M, O, I, _p(dev_status), _stream(stream)), "lbt_linear8_matmul")
+                                    _floats(bias, O, "bias"), py, ty, ldy, M, O, I, _p(dev_status), _raw_stream(y, stream)), "lbt_linear8_matmul")
 
 
 def linear8_workspace_bytes(M, O, I) -> int:
@@ -410,14 +416,14 @@ def linear8_backward(dY, q_w, s_w, q_x, s_x, I, dX=None, dW=None, dbias=None, ws
         ws = _scratch(linear8_workspace_bytes(M, O, I), dY.device, stream)
     _check(lib().lbt_linear8_backward(pg, tg, ldg, _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"), _codes(q_x, M, I, "q_x"),
                                       _floats(s_x, M, "s_x"), px, tx, ldx, pw, tw, ldw, _floats(dbias, O, "dbias"), M, O, I, _p(dev_status),
-                                      _p(ws), ws.numel(), _stream(stream)), "lbt_linear8_backward")
+                                      _p(ws), ws.numel(), _raw_stream(dY, stream)), "lbt_linear8_backward")
 
 
 def resnorm_forward(desc, x, h, gate, w_post, b_post, w_pre, b_pre, r, y=None, q=None, q_scale=None, stats=None, stream=None):
     """`lbt_resnorm_forward` on tensors that match `desc` (marshalling only: lm.ResNorm builds and checks them)."""
     _check(lib().lbt_resnorm_forward(C.addressof(desc), x.data_ptr(), h.data_ptr(), _p(gate), _p(w_post), _p(b_post), _p(w_pre), _p(b_pre),
                                      r.data_ptr(), y.data_ptr() if y is not None else 0, _p(q), q.shape[1] if q is not None else 0, _p(q_scale),
-                                     _p(stats), _stream(stream)), "lbt_resnorm_forward")
+                                     _p(stats), _raw_stream(x, stream)), "lbt_resnorm_forward")
 
 
 def resnorm_workspace_bytes(desc) -> int:
@@ -432,12 +438,13 @@ def resnorm_backward(desc, dr, dy, x, h, gate, w_post, b_post, w_pre, stats, dx,
     _check(lib().lbt_resnorm_backward(C.addressof(desc), dr.data_ptr() if dr is not None else 0, dy.data_ptr() if dy is not None else 0,
                                       x.data_ptr(), h.data_ptr(), _p(gate), _p(w_post), _p(b_post), _p(w_pre), _p(stats), dx.data_ptr(),
                                       dh.data_ptr(), _p(dgate), _p(dw_post), _p(db_post), _p(dw_pre), _p(db_pre), _p(ws), ws.numel(),
-                                      _stream(stream)), "lbt_resnorm_backward")
+                                      _raw_stream(x, stream)), "lbt_resnorm_backward")
 
 
 def adamw_step(table, hyper, grad_scale=None, skip=None, stream=None):
-    """One AdamW step over a ctypes array of AdamwTensor."""
-    _check(lib().lbt_adamw_step(table, len(table), C.addressof(hyper), _p(grad_scale), _p(skip), _stream(stream)), "lbt_adamw_step")
+    """One AdamW step over a ctypes array of AdamwTensor; stream: a torch stream or a raw one (None: the current stream)."""
+    raw = stream if isinstance(stream, int) else _stream(stream)
+    _check(lib().lbt_adamw_step(table, len(table), C.addressof(hyper), _p(grad_scale), _p(skip), raw), "lbt_adamw_step")
 
 
 def grad_diagnostics(dY, q_codes, bits, alpha, stats, ws=None, stream=None) -> "GradDiag":

@@ -1,22 +1,17 @@
 """Layers of a transformer's residual block on the library's kernels: `Linear8`, `ResNorm` and `AdamW`.
 
-Each object keeps what a program keeps between calls (weight codes, parameters, moments) and the plan of its calls; every
-step of arithmetic runs in the library (`lbt`).  Outputs may be handed in (`out`); otherwise they come from torch's
-allocator.  Work is enqueued on `stream` (default: torch's current stream); tensors that another stream made need that
-stream's event first, as with any torch call.
+Each object keeps what a program keeps between calls (weight codes, parameters, moments, scratch for each stream) and the
+plan of its calls; every step of arithmetic runs in the library (`lbt`).  Outputs may be handed in (`out`); otherwise they
+come from torch's allocator.  Work is enqueued on `stream` (default: torch's current stream); tensors that another stream
+made need that stream's event first, as with any torch call.
 """
 from __future__ import annotations
 
-import contextlib
+import ctypes as C
 
 import torch
 
 from . import lbt
-
-
-def _on(stream):
-    """Scratch and outputs of a call belong to the stream that uses them."""
-    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
 
 class Linear8:
@@ -26,11 +21,8 @@ class Linear8:
     def __init__(self, in_features: int, out_features: int, bias=None, weight=None, device="cuda"):
         if in_features < 1 or out_features < 1:
             raise ValueError("in_features and out_features are positive")
-        self.I, self.O, self.bias = int(in_features), int(out_features), bias
-        self.q_w = torch.zeros(self.O, lbt.pitch8(self.I), dtype=torch.int8, device=device)
-        self.s_w = torch.zeros(self.O, dtype=torch.float32, device=device)
-        self.kept = None
-        self.status = torch.zeros(1, dtype=torch.int32, device=device)   # lbt.ERR_TIMEOUT if a bounded on-chip wait ran out
+        self._set(torch.zeros(out_features, lbt.pitch8(in_features), dtype=torch.int8, device=device),
+                  torch.zeros(out_features, dtype=torch.float32, device=device), in_features, bias)
         if weight is not None:
             self.load_weight(weight)
 
@@ -38,45 +30,77 @@ class Linear8:
     def from_codes(cls, q_w, s_w, in_features: int, bias=None):
         """A served layer: codes [O, in_features rounded up to 16] (zeros behind in_features) and scales [O] as they are."""
         self = cls.__new__(cls)
-        self.I, self.O, self.bias = int(in_features), s_w.numel(), bias
-        lbt._codes(q_w, self.O, self.I, "q_w")
-        lbt._floats(s_w, self.O, "s_w")
-        lbt._floats(bias, self.O, "bias")
-        self.q_w, self.s_w, self.kept = q_w, s_w, None
-        self.status = torch.zeros(1, dtype=torch.int32, device=q_w.device)
+        self._set(q_w, s_w, in_features, bias)
         return self
+
+    def _set(self, q_w, s_w, in_features, bias):
+        self.I, self.O, self.pitch = int(in_features), s_w.numel(), lbt.pitch8(in_features)
+        # (addresses of the layer's own tensors, whose storage stays)
+        self._weights = (lbt._codes(q_w, self.O, self.I, "q_w"), lbt._floats(s_w, self.O, "s_w"), lbt._floats(bias, self.O, "bias"))
+        self.q_w, self.s_w, self.bias, self.kept = q_w, s_w, bias, None
+        self.status = torch.zeros(1, dtype=torch.int32, device=q_w.device)   # lbt.ERR_TIMEOUT if a bounded on-chip wait ran out
+        self._status = self.status.data_ptr()
+        self._scratch = {}   # stream -> (rows, codes and scales of x): never shared between streams
 
     def load_weight(self, weight, stream=None):
         """Quantizes the weights [O, I] (after each optimizer step)."""
-        if tuple(weight.shape) != (self.O, self.I):
+        if weight.shape != (self.O, self.I):
             raise ValueError(f"weight: {self.O} x {self.I}")
         lbt.rows8_quantize(weight, self.q_w, self.s_w, stream)
 
     def forward(self, x, out=None, keep=False, stream=None):
         """y for x [M, I]; keep: the codes of x stay for `backward`."""
-        if x.dim() != 2 or x.shape[1] != self.I:
-            raise ValueError(f"x: rows of {self.I} values")
+        if stream is not None:
+            with torch.cuda.stream(stream):   # outputs and scratch belong to the stream that uses them
+                return self.forward(x, out, keep)
+        px, tx, ldx = lbt._rows(x, "x", self.I)
         M = x.shape[0]
-        with _on(stream):
-            y = torch.empty(M, self.O, dtype=x.dtype, device=x.device) if out is None else out
-            q_x = torch.empty(M, lbt.pitch8(self.I), dtype=torch.int8, device=x.device)
-            s_x = torch.empty(M, dtype=torch.float32, device=x.device)
-        lbt.linear8_forward(x, self.q_w, self.s_w, y, q_x, s_x, self.bias, self.status, stream)
+        y = torch.empty(M, self.O, dtype=x.dtype, device=x.device) if out is None else out
+        py, ty, ldy = lbt._rows(y, "y", self.O)
+        if y.shape[0] != M:
+            raise ValueError("out: one row per row of x")
+        raw = lbt._raw_stream(x)
         if keep:
-            self.kept = (q_x, s_x)
+            self.kept = q_x, s_x = (torch.empty(M, self.pitch, dtype=torch.int8, device=x.device),
+                                    torch.empty(M, dtype=torch.float32, device=x.device))
+            pq, ps = q_x.data_ptr(), s_x.data_ptr()
+        else:
+            rows, _, pq, ps = self._scratch.get(raw, (0, None, 0, 0))
+            if rows < M:
+                rows = -(-M // 64) * 64
+                space = torch.empty(rows * (self.pitch + 4), dtype=torch.uint8, device=x.device)
+                pq, ps = space.data_ptr(), space.data_ptr() + rows * self.pitch
+                self._scratch[raw] = (rows, space, pq, ps)
+        q_w, s_w, bias = self._weights
+        status = lbt.lib().lbt_linear8_forward(px, tx, ldx, q_w, s_w, bias, py, ty, ldy, M, self.O, self.I, pq, ps, self._status, raw)
+        if status:
+            raise lbt.LbtError(status, "lbt_linear8_forward")
         return y
 
     def forward_codes(self, q_x, s_x, out=None, dtype=torch.bfloat16, keep=False, stream=None):
         """y from codes and scales that another operator made (ResNorm.forward_codes)."""
-        with _on(stream):
-            y = torch.empty(s_x.numel(), self.O, dtype=dtype, device=q_x.device) if out is None else out
-        lbt.linear8_matmul(q_x, s_x, self.q_w, self.s_w, y, self.I, self.bias, self.status, stream)
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.forward_codes(q_x, s_x, out, dtype, keep)
+        M = s_x.numel()
+        y = torch.empty(M, self.O, dtype=dtype, device=q_x.device) if out is None else out
+        py, ty, ldy = lbt._rows(y, "y", self.O)
+        if y.shape[0] != M:
+            raise ValueError("out: one row per row of codes")
+        q_w, s_w, bias = self._weights
+        status = lbt.lib().lbt_linear8_matmul(lbt._codes(q_x, M, self.I, "q_x"), lbt._floats(s_x, M, "s_x"), q_w, s_w, bias, py, ty, ldy,
+                                              M, self.O, self.I, self._status, lbt._raw_stream(y))
+        if status:
+            raise lbt.LbtError(status, "lbt_linear8_matmul")
         if keep:
             self.kept = (q_x, s_x)
         return y
 
     def backward(self, dy, need_dx=True, need_dw=True, dw_dtype=torch.float32, dx=None, dw=None, dbias=None, stream=None):
         """{"dx", "dw", "dbias"} of the last forward pass with keep=True (dx, dw, dbias: buffers to write into)."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.backward(dy, need_dx, need_dw, dw_dtype, dx, dw, dbias)
         if self.kept is None:
             raise RuntimeError("backward needs a forward pass with keep=True")
         q_x, s_x = self.kept
@@ -84,14 +108,13 @@ class Linear8:
             raise ValueError("dy: one row per token of the forward pass")
         new = lambda rows, cols, dtype: torch.empty(rows, cols, dtype=dtype, device=dy.device)  # noqa: E731
         out = {}
-        with _on(stream):
-            if need_dx or dx is not None:
-                out["dx"] = dx if dx is not None else new(dy.shape[0], self.I, dy.dtype)
-            if need_dw or dw is not None:
-                out["dw"] = dw if dw is not None else new(self.O, self.I, dw_dtype)
-                if self.bias is not None:
-                    out["dbias"] = dbias if dbias is not None else torch.empty(self.O, dtype=torch.float32, device=dy.device)
-        lbt.linear8_backward(dy, self.q_w, self.s_w, q_x, s_x, self.I, out.get("dx"), out.get("dw"), out.get("dbias"), None, self.status, stream)
+        if need_dx or dx is not None:
+            out["dx"] = dx if dx is not None else new(dy.shape[0], self.I, dy.dtype)
+        if need_dw or dw is not None:
+            out["dw"] = dw if dw is not None else new(self.O, self.I, dw_dtype)
+            if self.bias is not None:
+                out["dbias"] = dbias if dbias is not None else torch.empty(self.O, dtype=torch.float32, device=dy.device)
+        lbt.linear8_backward(dy, self.q_w, self.s_w, q_x, s_x, self.I, out.get("dx"), out.get("dw"), out.get("dbias"), None, self.status)
         return out
 
 
@@ -115,63 +138,98 @@ class ResNorm:
         self.param_dtype = given[0].dtype if given else None
         self.eps, self.scale_x, self.scale_h = float(eps), float(scale_x), float(scale_h)
         self.kept = None
+        self._params = tuple(lbt._p(p) for p in (w_post, b_post, w_pre, b_pre))   # (the layer's own tensors, whose storage stays)
+        self._plans = {}   # (rows, types, leading dimensions) -> descriptor and its workspace size
 
-    def _desc(self, like, gate, rows_per_gate, **acts):
-        M, dtype = like.shape[0], like.dtype
+    def _plan(self, names, acts, gate, rows_per_gate):
+        """Addresses of the activations and the descriptor of a call on tensors of these sizes (checked each time)."""
+        x = acts[0]
+        rows, dtype, addresses, lds = x.shape[0], x.dtype, [], []
+        for name, t in zip(names, acts):
+            if t is None:
+                addresses.append(0)
+                lds.append(0)
+                continue
+            p, _, ld = lbt._rows(t, name, self.dim)
+            if t.shape[0] != rows or t.dtype != dtype:
+                raise ValueError(f"{name}: {rows} rows of {dtype}")
+            addresses.append(p)
+            lds.append(ld)
         pd = self.param_dtype or (gate.dtype if gate is not None else dtype)
         if gate is not None:
-            rows = -(-M // rows_per_gate) if rows_per_gate else 1
-            if gate.dtype != pd or gate.numel() != rows * self.dim:
-                raise ValueError(f"gate: {rows} x {self.dim} values of the parameters' type")
-        d = lbt.ResnormDesc(M, self.dim, rows_per_gate or 0, lbt.TYPES[dtype], lbt.TYPES[pd], lbt.NORM_LAYER if self.layer else lbt.NORM_RMS,
-                            1 if self.post else 0, self.eps, self.eps, self.scale_x, self.scale_h)
-        for name, t in acts.items():
-            if t is None:
-                continue
-            _, _, ld = lbt._rows(t, name, self.dim)
-            if t.shape[0] != M or t.dtype != dtype:
-                raise ValueError(f"{name}: {M} rows of {dtype}")
-            setattr(d, "ld_" + name, ld)
-        return d
+            gates = -(-rows // rows_per_gate) if rows_per_gate else 1
+            if gate.dtype != pd or gate.numel() != gates * self.dim:
+                raise ValueError(f"gate: {gates} x {self.dim} values of the parameters' type")
+        key = (rows, dtype, pd, rows_per_gate, *names, *lds)
+        plan = self._plans.get(key)
+        if plan is None:
+            d = lbt.ResnormDesc(rows, self.dim, rows_per_gate or 0, lbt.TYPES[dtype], lbt.TYPES[pd],
+                                lbt.NORM_LAYER if self.layer else lbt.NORM_RMS, 1 if self.post else 0, self.eps, self.eps, self.scale_x,
+                                self.scale_h)
+            for name, ld in zip(names, lds):
+                setattr(d, "ld_" + name, ld)
+            if len(self._plans) >= 256:   # many lengths: the plans are cheap to make again
+                self._plans.clear()
+            plan = self._plans[key] = (d, C.addressof(d), lbt.resnorm_workspace_bytes(d))
+        return addresses, plan
+
+    def _forward(self, x, h, gate, rows_per_gate, r, y, q, q_scale, keep):
+        names, acts = (("x", "h", "r", "y"), (x, h, r, y)) if y is not None else (("x", "h", "r"), (x, h, r))
+        at, (_, desc, _) = self._plan(names, acts, gate, rows_per_gate)
+        stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device) if keep else None
+        w_post, b_post, w_pre, b_pre = self._params
+        status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._p(gate), w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
+                                               lbt._p(q), q.shape[1] if q is not None else 0, lbt._p(q_scale), lbt._p(stats), lbt._raw_stream(x))
+        if status:
+            raise lbt.LbtError(status, "lbt_resnorm_forward")
+        if keep:
+            self.kept = (x, h, gate, rows_per_gate, stats)
 
     def forward(self, x, h, gate=None, rows_per_gate=0, out=None, keep=False, stream=None):
         """(r, y); keep: the statistics stay for `backward`, which also needs x and h unchanged."""
-        with _on(stream):
-            new = lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device)  # noqa: E731
-            r, y = out if out is not None else (new(), new())
-            stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device) if keep else None
-        d = self._desc(x, gate, rows_per_gate, x=x, h=h, r=r, y=y)
-        lbt.resnorm_forward(d, x, h, gate, self.w_post, self.b_post, self.w_pre, self.b_pre, r, y=y, stats=stats, stream=stream)
-        if keep:
-            self.kept = (x, h, gate, rows_per_gate, stats)
+        if stream is not None:
+            with torch.cuda.stream(stream):   # outputs and scratch belong to the stream that uses them
+                return self.forward(x, h, gate, rows_per_gate, out, keep)
+        r, y = out if out is not None else (torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(x.shape, dtype=x.dtype, device=x.device))
+        self._forward(x, h, gate, rows_per_gate, r, y, None, None, keep)
         return r, y
 
     def forward_codes(self, x, h, gate=None, rows_per_gate=0, out=None, keep=False, stream=None):
         """(r, q, scale): y as the 8-bit rows that Linear8.forward_codes takes."""
-        with _on(stream):
-            r = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-            q = torch.empty(x.shape[0], lbt.pitch8(self.dim), dtype=torch.int8, device=x.device)
-            scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-            stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device) if keep else None
-        d = self._desc(x, gate, rows_per_gate, x=x, h=h, r=r)
-        lbt.resnorm_forward(d, x, h, gate, self.w_post, self.b_post, self.w_pre, self.b_pre, r, q=q, q_scale=scale, stats=stats, stream=stream)
-        if keep:
-            self.kept = (x, h, gate, rows_per_gate, stats)
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.forward_codes(x, h, gate, rows_per_gate, out, keep)
+        r = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        q = torch.empty(x.shape[0], lbt.pitch8(self.dim), dtype=torch.int8, device=x.device)
+        scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+        self._forward(x, h, gate, rows_per_gate, r, None, q, scale, keep)
         return r, q, scale
 
     def backward(self, dr, dy, stream=None):
         """Gradients of the last forward pass with keep=True: {"dx", "dh"} and those of the parameters and the gate that there are."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.backward(dr, dy)
         if self.kept is None:
             raise RuntimeError("backward needs a forward pass with keep=True")
         x, h, gate, rows_per_gate, stats = self.kept
-        with _on(stream):
-            out = {k: torch.empty(x.shape, dtype=x.dtype, device=x.device) for k in ("dx", "dh")}
-            for name, p in (("dgate", gate), ("dw_post", self.w_post if self.post else None), ("db_post", self.b_post if self.post else None),
-                            ("dw_pre", self.w_pre), ("db_pre", self.b_pre)):
-                if p is not None:
-                    out[name] = torch.empty(p.shape, dtype=p.dtype, device=x.device)
-        d = self._desc(x, gate, rows_per_gate, x=x, h=h, dr=dr, dy=dy, dx=out["dx"], dh=out["dh"])
-        lbt.resnorm_backward(d, dr, dy, x, h, gate, self.w_post, self.b_post, self.w_pre, stats, stream=stream, **out)
+        device = x.device
+        out = {"dx": torch.empty(x.shape, dtype=x.dtype, device=device), "dh": torch.empty(x.shape, dtype=x.dtype, device=device)}
+        grads = []
+        for name, p in (("dgate", gate), ("dw_post", self.w_post if self.post else None), ("db_post", self.b_post if self.post else None),
+                        ("dw_pre", self.w_pre), ("db_pre", self.b_pre)):
+            if p is not None:
+                out[name] = torch.empty(p.shape, dtype=p.dtype, device=device)
+                grads.append(out[name].data_ptr())
+            else:
+                grads.append(0)
+        at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate)
+        ws = torch.empty(size, dtype=torch.uint8, device=device)
+        w_post, b_post, w_pre, _ = self._params
+        status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._p(gate), w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
+                                                *grads, ws.data_ptr(), size, lbt._raw_stream(x))
+        if status:
+            raise lbt.LbtError(status, "lbt_resnorm_backward")
         return out
 
 
@@ -222,7 +280,8 @@ class AdamW:
     def step(self, grad_scale=None, skip=None, stream=None):
         """One step.  grad_scale: device float the gradients are multiplied by; skip: device int32, non-zero = leave everything."""
         self.hyper.step += 1
-        lbt.adamw_step(self.table, self.hyper, grad_scale, skip, stream)
+        raw = lbt._raw_stream(self.params[0], stream) if self.params else stream
+        lbt.adamw_step(self.table, self.hyper, grad_scale, skip, raw)
 
     def moments(self):
         """The moments (m, v) as fp32 values, one tensor for each parameter (a checkpoint reader's view)."""
