@@ -79,54 +79,46 @@ __device__ __forceinline__ void tile_at(const L8Args& a, int t, int& m, int& n) 
     m = b * a.band + (within - n * rows);
 }
 
-// Stores columns [c, c + 8) of output row `row`; f holds the finished values.
-template <typename T>
-__device__ __forceinline__ void put8(const L8Args& a, int64_t row, int c, const float (&f)[8]) {
-    T* dst = static_cast<T*>(a.out) + row * a.ldo + c;
-    if (a.vec && c + 8 <= a.cols) {
-        store8(dst, f);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < a.cols) dst[i] = from_f32<T>(f[i]);
-    }
+__device__ __forceinline__ void put_one(const L8Args& a, int64_t row, int64_t col, float f) {
+    const int64_t i = row * a.ldo + col;
+    if (a.out_type == LBT_BF16) static_cast<__nv_bfloat16*>(a.out)[i] = __float2bfloat16_rn(f);
+    else if (a.out_type == LBT_F16) static_cast<__half*>(a.out)[i] = __float2half_rn(f);
+    else static_cast<float*>(a.out)[i] = f;
 }
 
-// 32 consecutive columns of one row (lane = row) from the accumulator: scale, bias, round, store.  `cs`: this warp's shared
-// copy of the 32 columns' scales and biases.
+__device__ __forceinline__ float finish(int acc, float scale, float bias) { return __fadd_rn(__fmul_rn(__int2float_rn(acc), scale), bias); }
+
+// 32 consecutive columns of one row (lane = row): scale, bias, round, store in 32-byte sectors.  `cs`: this warp's shared copy of the
+// columns' scales and biases.
 template <typename T>
-__device__ __forceinline__ void put_row(const L8Args& a, int64_t row, int c0, const uint32_t (&v)[32], float rs, const float* cs) {
+__device__ __forceinline__ void put_row(const L8Args& a, int64_t row, int c0, int width, const uint32_t (&v)[32], float rs, const float* cs) {
 #pragma unroll
     for (int j = 0; j < 32; j += 16) {
-        // 16 columns at a time: a 32-byte sector of a 16-bit type
         float f[16];
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             const float4 s = *reinterpret_cast<const float4*>(cs + j + e), b = *reinterpret_cast<const float4*>(cs + 32 + j + e);
-            f[e] = __fadd_rn(__fmul_rn(__int2float_rn((int)v[j + e]), __fmul_rn(rs, s.x)), b.x);
-            f[e + 1] = __fadd_rn(__fmul_rn(__int2float_rn((int)v[j + e + 1]), __fmul_rn(rs, s.y)), b.y);
-            f[e + 2] = __fadd_rn(__fmul_rn(__int2float_rn((int)v[j + e + 2]), __fmul_rn(rs, s.z)), b.z);
-            f[e + 3] = __fadd_rn(__fmul_rn(__int2float_rn((int)v[j + e + 3]), __fmul_rn(rs, s.w)), b.w);
+            f[e] = finish((int)v[j + e], __fmul_rn(rs, s.x), b.x);
+            f[e + 1] = finish((int)v[j + e + 1], __fmul_rn(rs, s.y), b.y);
+            f[e + 2] = finish((int)v[j + e + 2], __fmul_rn(rs, s.z), b.z);
+            f[e + 3] = finish((int)v[j + e + 3], __fmul_rn(rs, s.w), b.w);
         }
         const int c = c0 + j;
-        if (row >= a.rows || c >= a.cols) continue;
+        if (row >= a.rows || c >= a.cols || j >= width) continue;
         T* dst = static_cast<T*>(a.out) + row * a.ldo + c;
-        if (a.vec && c + 16 <= a.cols) {
+        if (c + 16 <= a.cols) {
+            Vec8<T> p, q;
             float lo[8], hi[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) { lo[i] = f[i]; hi[i] = f[8 + i]; }
-            if (sizeof(T) == 2) {
-                Vec8<T> p, q;
-                pack(lo, p); pack(hi, q);
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { w[i] = p.w[i]; w[4 + i] = q.w[i]; }
+            pack(lo, p);
+            pack(hi, q);
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t w[8] = {p.w[0], p.w[1], p.w[2], p.w[3], q.w[0], q.w[1], q.w[2], q.w[3]};
                 st_global_cs_v8(dst, w);
             } else {
-                Vec8<T> p, q;
-                pack(lo, p); pack(hi, q);
-                st_vec(dst, p.w);
-                st_vec(dst + 8, q.w);
+                st_global_cs_v8(dst, p.w);
+                st_global_cs_v8(dst + 8, q.w);
             }
         } else {
 #pragma unroll
@@ -136,26 +128,34 @@ __device__ __forceinline__ void put_row(const L8Args& a, int64_t row, int c0, co
     }
 }
 
-__device__ __forceinline__ void put_row_any(const L8Args& a, int64_t row, int c0, const uint32_t (&v)[32], float rs, const float* cs) {
-    if (a.out_type == LBT_BF16) put_row<__nv_bfloat16>(a, row, c0, v, rs, cs);
-    else if (a.out_type == LBT_F16) put_row<__half>(a, row, c0, v, rs, cs);
-    else put_row<float>(a, row, c0, v, rs, cs);
-}
-
-__device__ __forceinline__ void put_one(const L8Args& a, int64_t row, int64_t col, float f) {
-    const int64_t i = row * a.ldo + col;
-    if (a.out_type == LBT_BF16) static_cast<__nv_bfloat16*>(a.out)[i] = __float2bfloat16_rn(f);
-    else if (a.out_type == LBT_F16) static_cast<__half*>(a.out)[i] = __float2half_rn(f);
-    else static_cast<float*>(a.out)[i] = f;
-}
-
-// The scales and biases of 32 columns into a warp's 64 floats of shared memory.
-__device__ __forceinline__ void stage_columns(const L8Args& a, int c0, float* cs, int lane) {
-    __syncwarp();
+// `width` (16 or 32) consecutive columns from c0 of a warp's 32 rows, lane l holding row row0 + l in v.  Rows that begin on 32-byte
+// boundaries leave straight from the registers; others are turned round in the warp's 4 KB of shared memory, so that a store covers
+// consecutive addresses of one row (a lane's own row in 4-byte stores touched 32 partly written sectors each).
+__device__ __forceinline__ void put_block(const L8Args& a, uint32_t* stage, int64_t row0, int c0, int width, const uint32_t (&v)[32], float rs, int lane) {
+    if (c0 >= a.cols || row0 >= a.rows) return;   // uniform over the warp
     const int c = c0 + lane;
-    cs[lane] = c < a.cols && a.col_scale != nullptr ? __ldg(a.col_scale + c) : 1.0f;
-    cs[32 + lane] = c < a.cols && a.bias != nullptr ? __ldg(a.bias + c) : 0.0f;
+    const float scale = c < a.cols && a.col_scale != nullptr ? __ldg(a.col_scale + c) : 1.0f;
+    const float bias = c < a.cols && a.bias != nullptr ? __ldg(a.bias + c) : 0.0f;
     __syncwarp();
+    if (a.vec) {
+        float* cs = reinterpret_cast<float*>(stage);
+        cs[lane] = scale;
+        cs[32 + lane] = bias;
+        __syncwarp();
+        if (a.out_type == LBT_BF16) put_row<__nv_bfloat16>(a, row0 + lane, c0, width, v, rs, cs);
+        else if (a.out_type == LBT_F16) put_row<__half>(a, row0 + lane, c0, width, v, rs, cs);
+        else put_row<float>(a, row0 + lane, c0, width, v, rs, cs);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) stage[lane * 32 + (j ^ lane)] = v[j];
+    __syncwarp();
+    const bool live = lane < width && c < a.cols;
+#pragma unroll 4
+    for (int r = 0; r < 32; ++r) {
+        const float s = __fmul_rn(__shfl_sync(0xFFFFFFFFu, rs, r), scale);
+        if (live && row0 + r < a.rows) put_one(a, row0 + r, c, finish((int)stage[r * 32 + (lane ^ r)], s, bias));
+    }
 }
 
 // ------------------------------------------------------------------------------------------ 128 x 128 tiles
@@ -167,13 +167,21 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+constexpr int kParkPitch = 132;                  // words of a parked accumulator row: 16-byte accesses without bank conflicts
+constexpr int kParkBytes = 128 * kParkPitch * 4;
+static_assert(kParkBytes + 4 * 4096 <= kRing, "the parked accumulator and the warps' staging share the operand ring");
 
 __global__ void __launch_bounds__(128, 2)
 l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ L8Args a) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     __shared__ Bars bars;
-    __shared__ alignas(16) float columns[4][64];
+    __shared__ float token_scale[64];
     Bars* b = &bars;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int split = a.splits > 1 ? (int)cluster_ctarank() : 0;
@@ -249,82 +257,92 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         __syncwarp();
     }
     if (a.wait_prev) griddep_wait();   // the scales come from the kernel ahead too, and nothing is written before it has ended
+    if (a.swapped && threadIdx.x < 64) token_scale[threadIdx.x] = n0 + (int)threadIdx.x < a.rows ? a.row_scale[n0 + threadIdx.x] : 0.0f;
     bool ok = true;
     if (n_steps > 0) ok = wait_for(b, &b->tmem_full[0], 0u, a.status);
     ok = __syncthreads_and(ok) != 0;   // uniform; without it a lost signal ends in the error word and no output
     tc_fence_after_sync();
     const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-    int c_lo = 0, c_hi = a.mma_n;
+    uint32_t* park = reinterpret_cast<uint32_t*>(ring);
+    uint32_t* stage = reinterpret_cast<uint32_t*>(ring + kParkBytes + warp * 4096);
     if (a.splits > 1) {
-        // accumulator -> own shared memory, [column][row]
-        uint32_t* park = reinterpret_cast<uint32_t*>(ring);
+        // accumulator -> own shared memory: [row][column], or [token][channel] for the swapped form
         for (int c = 0; c < a.mma_n && ok; c += 32) {
             uint32_t v[32];
             if (n_steps > 0) { tmem_ld_32x32(lanes + (uint32_t)c, v); tmem_ld_wait(); }
+            else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (c + j < a.mma_n) park[(c + j) * 128 + threadIdx.x] = n_steps > 0 ? v[j] : 0u;
+                for (int j = 0; j < 32; ++j) v[j] = 0u;
+            }
+            if (a.swapped) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (c + j < a.mma_n) park[(c + j) * 128 + threadIdx.x] = v[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4)
+                    *reinterpret_cast<uint4*>(park + threadIdx.x * kParkPitch + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            }
         }
         cluster_sync_all();
-        const int per_rank = a.mma_n / a.splits;
-        c_lo = split * per_rank;
-        c_hi = c_lo + per_rank;
     }
-    const int64_t row = m0 + (int)threadIdx.x;
-    if (ok && a.splits > 1) {
-        uint32_t from[8];
-        for (int r = 0; r < a.splits; ++r) from[r] = map_to_cta(smem_u32(ring), (uint32_t)r);
-        auto total = [&](int c) {
-            int sum = 0;
+    const int64_t row = m0 + (int)threadIdx.x;   // of the output, or (swapped) its column
+    uint32_t from[8];
+    if (a.splits > 1)
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
-                if (r < a.splits) sum += (int)ld_cluster_u32(from[r] + (uint32_t)(c * 128 + (int)threadIdx.x) * 4u);
-            return sum;
-        };
-        if (a.swapped) {
-            const float cs = row < a.cols ? __ldg(a.col_scale + row) : 0.0f, bias = a.bias != nullptr && row < a.cols ? __ldg(a.bias + row) : 0.0f;
-            for (int c = c_lo; c < c_hi; ++c) {
-                const int m = n0 + c;
-                const int sum = total(c);
-                if (m < a.rows && row < a.cols) put_one(a, m, row, __fadd_rn(__fmul_rn(__int2float_rn(sum), __fmul_rn(a.row_scale[m], cs)), bias));
+        for (int r = 0; r < 8; ++r) from[r] = map_to_cta(smem_u32(ring), (uint32_t)min(r, a.splits - 1));
+    if (ok && a.swapped) {
+        const float cs = row < a.cols ? __ldg(a.col_scale + row) : 0.0f, bias = a.bias != nullptr && row < a.cols ? __ldg(a.bias + row) : 0.0f;
+        if (a.splits > 1) {
+            const int each = a.mma_n / a.splits;
+#pragma unroll 2
+            for (int c = split * each; c < (split + 1) * each; ++c) {
+                uint32_t part[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < a.splits) part[r] = ld_cluster_u32(from[r] + (uint32_t)(c * 128 + (int)threadIdx.x) * 4u);
+                int sum = 0;
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < a.splits) sum += (int)part[r];
+                if (n0 + c < a.rows && row < a.cols) put_one(a, n0 + c, row, finish(sum, __fmul_rn(token_scale[c], cs), bias));
             }
         } else {
-            const float rs = row < a.rows ? a.row_scale[row] : 0.0f;
-            for (int c = c_lo; c < c_hi; c += 8) {   // (a slice of the columns is a multiple of 16 here)
-                float f[8];
+            for (int c = 0; c < a.mma_n; c += 32) {
+                uint32_t v[32];
+                tmem_ld_32x32(lanes + (uint32_t)c, v);
+                tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int n = n0 + c + i;
-                    const float cs = a.col_scale != nullptr && n < a.cols ? __ldg(a.col_scale + n) : 1.0f;
-                    const float bias = a.bias != nullptr && n < a.cols ? __ldg(a.bias + n) : 0.0f;
-                    f[i] = __fadd_rn(__fmul_rn(__int2float_rn(total(c + i)), __fmul_rn(rs, cs)), bias);
-                }
-                if (row < a.rows && n0 + c < a.cols) {
-                    if (a.out_type == LBT_BF16) put8<__nv_bfloat16>(a, row, n0 + c, f);
-                    else if (a.out_type == LBT_F16) put8<__half>(a, row, n0 + c, f);
-                    else put8<float>(a, row, n0 + c, f);
-                }
+                for (int j = 0; j < 32; ++j)
+                    if (c + j < a.mma_n && n0 + c + j < a.rows && row < a.cols)
+                        put_one(a, n0 + c + j, row, finish((int)v[j], __fmul_rn(token_scale[c + j], cs), bias));
             }
         }
     } else if (ok) {
-        const float rs = !a.swapped && row < a.rows ? a.row_scale[row] : 0.0f;
-        const float cs = a.swapped && row < a.cols ? __ldg(a.col_scale + row) : 0.0f;
-        const float bias = a.swapped && a.bias != nullptr && row < a.cols ? __ldg(a.bias + row) : 0.0f;
-        for (int c = 0; c < a.mma_n; c += 32) {
+        const float rs = row < a.rows ? a.row_scale[row] : 0.0f;
+        const int each = 128 / a.splits, width = min(each, 32);
+        for (int c = split * each; c < (split + 1) * each; c += width) {
             uint32_t v[32];
-            tmem_ld_32x32(lanes + (uint32_t)c, v);
-            tmem_ld_wait();
-            if (a.swapped) {
+            if (a.splits > 1) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const int m = n0 + c + j;
-                    if (c + j < a.mma_n && m < a.rows && row < a.cols)
-                        put_one(a, m, row, __fadd_rn(__fmul_rn(__int2float_rn((int)v[j]), __fmul_rn(a.row_scale[m], cs)), bias));
+                for (int j = 0; j < 32; j += 4) {
+                    uint4 part[8];
+                    uint4 sum = make_uint4(0, 0, 0, 0);
+                    if (j < width) {
+#pragma unroll
+                        for (int r = 0; r < 8; ++r)
+                            if (r < a.splits) part[r] = ld_cluster_v4(from[r] + (uint32_t)((int)threadIdx.x * kParkPitch + c + j) * 4u);
+#pragma unroll
+                        for (int r = 0; r < 8; ++r)
+                            if (r < a.splits) { sum.x += part[r].x; sum.y += part[r].y; sum.z += part[r].z; sum.w += part[r].w; }
+                    }
+                    v[j] = sum.x; v[j + 1] = sum.y; v[j + 2] = sum.z; v[j + 3] = sum.w;
                 }
             } else {
-                stage_columns(a, n0 + c, columns[warp], lane);
-                put_row_any(a, row, n0 + c, v, rs, columns[warp]);
+                tmem_ld_32x32(lanes + (uint32_t)c, v);
+                tmem_ld_wait();
             }
+            put_block(a, stage, m0 + warp * 32, n0 + c, width, v, rs, lane);
         }
     }
     tc_fence_before_sync();
@@ -347,7 +365,6 @@ l8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     __shared__ Bars bars;
-    __shared__ alignas(16) float columns[8][64];
     Bars* b = &bars;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -425,7 +442,7 @@ l8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         __syncwarp();
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;   // the TMEM lanes a warp may read; half of the columns each
-        float* cs = columns[warp - 2];
+        uint32_t* stage = reinterpret_cast<uint32_t*>(ring + kPairRing + (warp - 2) * 4096);
         uint32_t acc = 0;
         for (int t = pair; t < a.total; t += pairs, ++acc) {
             int tm, tn;
@@ -440,9 +457,8 @@ l8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             for (int c = half * 128; c < half * 128 + 128; c += 32) {
                 uint32_t v[32];
                 tmem_ld_32x32(tmem + buf * 256u + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
-                stage_columns(a, tn * 256 + c, cs, lane);
                 tmem_ld_wait();
-                put_row_any(a, row, tn * 256 + c, v, rs, cs);
+                put_block(a, stage, row - lane, tn * 256 + c, 32, v, rs, lane);
             }
             tc_fence_before_sync();
             __syncwarp();
@@ -533,14 +549,15 @@ rows8_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, bo
 }
 
 // ------------------------------------------------------------------------------------------ few tokens
-// A handful of tokens: the time is the weights' way from memory, each byte used once.  A block owns 16 output channels, its
-// eight warps take 64-byte pieces of their rows in turn, straight into the fragments of m16n8k32 products (A: channels, B: tokens;
-// the reduction may be dealt out in any order as long as both operands agree, so a lane's 16 consecutive bytes are two
-// fragments).  Sixteen 16-byte loads a lane are in flight before the first product; the warps' integer sums meet in shared memory.
-// With T a type the block quantizes the tokens itself (x stays in L2) under the first weights' latency: one launch in all.
+// A handful of tokens: the time is the weights' way from memory, each byte used once.  A tile is 16 output channels; a block's
+// warps take 64-byte pieces of their rows in turn as the fragments of m16n8k32 products (A: channels, B: tokens; the reduction may
+// be dealt out in any order as long as both operands agree, so a lane's 16 consecutive bytes are two fragments).  A lane copies its
+// own pieces ahead (cp.async, eight of them in flight, on into the block's next tile) into slots that only it reads: no barrier
+// but one a tile, where the warps' integer sums meet.  (Refilling registers instead halved the rate: a warp has six scoreboards.)
+// With T a type (one token) every block quantizes the token for itself under the first weights' latency: one launch in all.
 constexpr int kFewTokens = 16;
-constexpr int kFewSmem = 40 * 1024;      // codes of the tokens a block quantizes itself
-constexpr int kFewBatch = 8;             // 64-byte pieces of a row in flight per lane
+constexpr int kFewAhead = 8;               // pieces in flight per lane
+constexpr int kFewCodes = 60 * 1024;       // codes of all tokens, kept by each block
 
 struct FewArgs {
     const void* x;
@@ -550,119 +567,129 @@ struct FewArgs {
     float* s_x;
     const uint8_t* q_w;
     int64_t pitch;
-    int I, M, tokens_pitch;   // tokens_pitch: bytes of a token's codes in shared memory
+    int I, M, tokens_pitch;   // tokens_pitch: bytes of a token's codes in shared memory, an odd multiple of 64 (no bank conflicts)
     bool wait_prev;
     L8Args out;               // rows, cols, scales, bias, output
 };
 
-__device__ __forceinline__ uint4 ld_stream(const uint8_t* p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
 __device__ __forceinline__ void mma_16832(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <typename T, int kTiles>   // T void: codes come from q_x; kTiles: groups of eight tokens
-__global__ void __launch_bounds__(256) l8_few_kernel(const __grid_constant__ FewArgs a) {
+template <typename T, int kTiles, int kWarps>   // T void: codes come from q_x; kTiles: groups of eight tokens
+__global__ void __launch_bounds__(kWarps * 32) l8_few_kernel(const __grid_constant__ FewArgs a) {
     constexpr bool kQuantize = !std::is_void<T>::value;
-    extern __shared__ uint8_t codes[];
-    __shared__ int sums[8][kTiles * 8][17];
+    constexpr int kThreads = kWarps * 32;
+    extern __shared__ uint8_t few_smem[];
+    uint8_t* codes = few_smem + kFewAhead * 2 * kThreads * 16;
+    __shared__ int sums[2][kWarps][kTiles * 8][17];
+    __shared__ float scales[kTiles * 8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int64_t o0 = (int64_t)blockIdx.x * 16;
-    const uint8_t* w0 = a.q_w + min(o0 + g, (int64_t)a.out.cols - 1) * a.pitch + 16 * t;
-    const uint8_t* w1 = a.q_w + min(o0 + g + 8, (int64_t)a.out.cols - 1) * a.pitch + 16 * t;
-    const int room = (int)a.pitch - 16 * t;   // bytes of the rows from this lane's first on
-    uint4 lo[kFewBatch], hi[kFewBatch];
-    auto fetch = [&](int piece) {
-#pragma unroll
-        for (int i = 0; i < kFewBatch; ++i) {
-            const int k = (piece + 8 * i) * 64;
-            lo[i] = hi[i] = make_uint4(0, 0, 0, 0);
-            if (k < room) { lo[i] = ld_stream(w0 + k); hi[i] = ld_stream(w1 + k); }
-        }
+    const int tiles = (a.out.cols + 15) / 16;
+    const int pieces = ((int)a.pitch + 63) / 64;
+    const int mine = warp < pieces ? (pieces - warp + kWarps - 1) / kWarps : 0;   // pieces of a tile that this warp takes
+    // what is being fetched: its tile, its piece and this lane's two rows of it
+    int f_tile = blockIdx.x, f_piece = 0, f_stage = 0;
+    const uint8_t *w0, *w1;
+    auto rows_of = [&](int tile) {
+        const int64_t o = (int64_t)tile * 16 + g, last = a.out.cols - 1;   // (rows past the last channel repeat it and are not stored)
+        w0 = a.q_w + min(o, last) * a.pitch + 64 * warp + 16 * t;
+        w1 = a.q_w + min(o + 8, last) * a.pitch + 64 * warp + 16 * t;
     };
-    fetch(warp);
-    float scale[kQuantize ? 4 : 1];
+    auto slot = [&](int stage, int half) { return few_smem + ((stage * 2 + half) * kThreads + threadIdx.x) * 16; };
+    auto fetch = [&]() {
+        if (f_tile < tiles && mine > 0) {
+            const int k = f_piece * (64 * kWarps);
+            // a lane whose 16 bytes lie behind the row's end copies zeros
+            const uint32_t bytes = k + 64 * warp + 16 * t < a.pitch ? 16u : 0u;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(slot(f_stage, 0))), "l"(bytes ? w0 + k : a.q_w), "r"(bytes) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(slot(f_stage, 1))), "l"(bytes ? w1 + k : a.q_w), "r"(bytes) : "memory");
+            if (++f_piece == mine) {
+                f_piece = 0;
+                f_tile += gridDim.x;
+                rows_of(f_tile);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        f_stage = f_stage + 1 == kFewAhead ? 0 : f_stage + 1;
+    };
+    rows_of(f_tile);
+#pragma unroll
+    for (int i = 0; i < kFewAhead; ++i) fetch();
     if constexpr (kQuantize) {
-        __shared__ uint32_t part[4][8];
-        uint32_t most[4] = {0, 0, 0, 0};
+        __shared__ uint32_t part[kWarps];
+        const T* row = static_cast<const T*>(a.x);
+        uint32_t most = 0;
+        for (int c = threadIdx.x * 8; c < a.I; c += kThreads * 8) {
+            float f[8];
+            load_group(row, c, a.I, a.vec, f);
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
-            if (m < a.M) {
-                const T* row = static_cast<const T*>(a.x) + m * a.ldx;
-                for (int c = threadIdx.x * 8; c < a.I; c += 2048) {
-                    float f[8];
-                    load_group(row, c, a.I, a.vec, f);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) most[m] = max(most[m], abs_bits(f[i]));
-                }
-                most[m] = __reduce_max_sync(0xFFFFFFFFu, most[m]);
-                if (lane == 0) part[m][warp] = most[m];
-            }
+            for (int i = 0; i < 8; ++i) most = max(most, abs_bits(f[i]));
+        }
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        if (lane == 0) part[warp] = most;
         __syncthreads();
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-            if (m < a.M) {
-                float factor;
-                scale8(__reduce_max_sync(0xFFFFFFFFu, part[m][lane & 7]), scale[m], factor);
-                const T* row = static_cast<const T*>(a.x) + m * a.ldx;
-                for (int c = threadIdx.x * 8; c < a.tokens_pitch; c += 2048) {
-                    float f[8];
-                    load_group(row, c, a.I, a.vec, f);
-                    const uint2 q = codes8(f, factor);
-                    *reinterpret_cast<uint2*>(codes + m * a.tokens_pitch + c) = q;
-                    if (blockIdx.x == 0 && c < a.pitch) *reinterpret_cast<uint2*>(a.q_x + m * a.pitch + c) = q;
-                }
-                if (blockIdx.x == 0 && threadIdx.x == 0) a.s_x[m] = scale[m];
-            }
-        __syncthreads();
-    } else if (a.wait_prev) {
-        griddep_wait();
+        float scale, factor;
+        scale8(__reduce_max_sync(0xFFFFFFFFu, part[lane & (kWarps - 1)]), scale, factor);
+        for (int c = threadIdx.x * 8; c < a.tokens_pitch; c += kThreads * 8) {
+            float f[8];
+            load_group(row, c, a.I, a.vec, f);
+            const uint2 q = codes8(f, factor);
+            *reinterpret_cast<uint2*>(codes + c) = q;
+            if (blockIdx.x == 0 && c < a.pitch) *reinterpret_cast<uint2*>(a.q_x + c) = q;
+        }
+        if (threadIdx.x == 0) scales[0] = scale;
+        if (blockIdx.x == 0 && threadIdx.x == 0) a.s_x[0] = scale;
+    } else {
+        if (a.wait_prev) griddep_wait();
+        const int chunks = (int)(a.tokens_pitch >> 4);
+        for (int i = threadIdx.x; i < a.M * chunks; i += kThreads) {
+            const int m = i / chunks, c = (i - m * chunks) * 16;
+            const uint4 v = c < a.pitch ? *reinterpret_cast<const uint4*>(a.q_x + m * a.pitch + c) : make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(codes + m * a.tokens_pitch + c) = v;
+        }
+        if (threadIdx.x < a.M) scales[threadIdx.x] = a.s_x[threadIdx.x];
     }
-    int acc[kTiles][4];
+    __syncthreads();
+    int turn = 0, stage = 0;
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+        int acc[kTiles][4];
 #pragma unroll
-    for (int n = 0; n < kTiles; ++n)
+        for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[n][i] = 0;
-    for (int piece = warp; piece * 64 < a.pitch; piece += 8 * kFewBatch) {
-        if (piece != warp) fetch(piece);
-#pragma unroll
-        for (int i = 0; i < kFewBatch; ++i) {
-            const int k = (piece + 8 * i) * 64 + 16 * t;
-            if ((piece + 8 * i) * 64 >= a.pitch) break;   // uniform over the warp
+            for (int i = 0; i < 4; ++i) acc[n][i] = 0;
+        for (int i = 0; i < mine; ++i) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kFewAhead - 1) : "memory");
+            const uint4 lo = *reinterpret_cast<const uint4*>(slot(stage, 0)), hi = *reinterpret_cast<const uint4*>(slot(stage, 1));
+            const int k = (i * kWarps + warp) * 64 + 16 * t;
 #pragma unroll
             for (int n = 0; n < kTiles; ++n) {
                 const int m = min(n * 8 + g, a.M - 1);    // (columns past M are not stored)
-                uint4 b = make_uint4(0, 0, 0, 0);
-                if (kQuantize) b = *reinterpret_cast<const uint4*>(codes + m * a.tokens_pitch + k);
-                else if (k < a.pitch) b = __ldg(reinterpret_cast<const uint4*>(a.q_x + m * a.pitch + k));
-                mma_16832(acc[n], lo[i].x, hi[i].x, lo[i].y, hi[i].y, b.x, b.y);
-                mma_16832(acc[n], lo[i].z, hi[i].z, lo[i].w, hi[i].w, b.z, b.w);
+                const uint4 b = *reinterpret_cast<const uint4*>(codes + m * a.tokens_pitch + k);
+                mma_16832(acc[n], lo.x, hi.x, lo.y, hi.y, b.x, b.y);
+                mma_16832(acc[n], lo.z, hi.z, lo.w, hi.w, b.z, b.w);
             }
+            fetch();
+            stage = stage + 1 == kFewAhead ? 0 : stage + 1;
         }
-    }
 #pragma unroll
-    for (int n = 0; n < kTiles; ++n) {
-        sums[warp][n * 8 + 2 * t][g] = acc[n][0];
-        sums[warp][n * 8 + 2 * t + 1][g] = acc[n][1];
-        sums[warp][n * 8 + 2 * t][g + 8] = acc[n][2];
-        sums[warp][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
-    }
-    __syncthreads();
-    const int m = threadIdx.x >> 4, r = threadIdx.x & 15;
-    const int64_t o = o0 + r;
-    if (m < a.M && m < kTiles * 8 && o < a.out.cols) {
-        int sum = 0;
+        for (int n = 0; n < kTiles; ++n) {
+            sums[turn][warp][n * 8 + 2 * t][g] = acc[n][0];
+            sums[turn][warp][n * 8 + 2 * t + 1][g] = acc[n][1];
+            sums[turn][warp][n * 8 + 2 * t][g + 8] = acc[n][2];
+            sums[turn][warp][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
+        }
+        __syncthreads();
+        const int m = threadIdx.x >> 4, r = threadIdx.x & 15;
+        const int64_t o = (int64_t)tile * 16 + r;
+        if (m < a.M && o < a.out.cols) {
+            int sum = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += sums[i][m][r];
-        float rs;
-        if constexpr (kQuantize) rs = m == 0 ? scale[0] : m == 1 ? scale[1] : m == 2 ? scale[2] : scale[3];
-        else rs = a.s_x[m];
-        const float bias = a.out.bias != nullptr ? __ldg(a.out.bias + o) : 0.0f;
-        put_one(a.out, m, o, __fadd_rn(__fmul_rn(__int2float_rn(sum), __fmul_rn(rs, __ldg(a.out.col_scale + o))), bias));
+            for (int i = 0; i < kWarps; ++i) sum += sums[turn][i][m][r];
+            const float bias = a.out.bias != nullptr ? __ldg(a.out.bias + o) : 0.0f;
+            put_one(a.out, m, o, __fadd_rn(__fmul_rn(__int2float_rn(sum), __fmul_rn(scales[m], __ldg(a.out.col_scale + o))), bias));
+        }
     }
 }
 
@@ -782,7 +809,7 @@ bool code_map(CUtensorMap* tm, const void* base, int64_t pitch, int64_t rows, in
 }
 
 constexpr int kTileSmem = kRing + 1024;
-constexpr int kPairSmem = kPairRing + 1024;
+constexpr int kPairSmem = kPairRing + 8 * 4096 + 1024;
 
 lbt_status allow_smem() {
     constexpr int kDevices = 64;
@@ -847,8 +874,10 @@ lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
         cfg.numAttrs = n_attr;
         return cudaLaunchKernelEx(&cfg, l8_pair_kernel, tmA, tmB, a) == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
     }
-    a.swapped = p.mode == kForward && p.rows <= 128;
-    a.mma_n = a.swapped ? (int)std::min<int64_t>(128, pitch16(p.rows)) : 128;
+    // Up to 64 tokens the weights are the rows of the product and the tokens its columns: the tokens' share of the operand
+    // traffic and of the products shrinks with their number.
+    a.swapped = p.mode == kForward && p.rows <= 64;
+    a.mma_n = a.swapped ? (int)pitch16(p.rows) : 128;
     a.stage_bytes = kBox + a.mma_n * kStep;
     a.stages = std::min(kMaxStages, kRing / a.stage_bytes);
     a.tiles_m = (int)(((a.swapped ? p.cols : p.rows) + 127) / 128);
@@ -896,41 +925,59 @@ lbt_status quantize_rows_any(const void* x, int type, int64_t rows, int64_t cols
     return quantize_rows(static_cast<const __half*>(x), type, rows, cols, ld, q, ldq, scale, stream);
 }
 
+// Bytes of a token's codes in the few-token kernel's shared memory.
+int few_pitch(int64_t I) { return (int)((I + 127) / 128 * 128 + 64); }
+bool few_fits(int64_t M, int64_t I) { return M <= kFewTokens && M * ((I + 127) / 128 * 128 + 64) <= kFewCodes; }
+
 // Few tokens, from their codes (the quantizer may be the launch ahead) or from x.
 FewArgs few_args(void* q_x, float* s_x, const void* q_w, const float* s_w, const float* bias, void* y, int y_type, int64_t ldy, int64_t M,
                  int64_t O, int64_t I) {
     FewArgs a{};
     a.q_x = static_cast<uint8_t*>(q_x); a.s_x = s_x; a.q_w = static_cast<const uint8_t*>(q_w);
     a.pitch = pitch16(I); a.I = (int)I; a.M = (int)M;
-    a.tokens_pitch = (int)((I + 63) / 64 * 64);
+    a.tokens_pitch = few_pitch(I);
     a.out.rows = (int)M; a.out.cols = (int)O; a.out.col_scale = s_w; a.out.bias = bias;
     a.out.out = y; a.out.out_type = y_type; a.out.ldo = ldy;
     return a;
 }
 
-lbt_status few_from_codes(FewArgs a, bool behind, cudaStream_t stream) {
-    a.wait_prev = behind;
+// Blocks of eight warps, two to an SM, while two blocks' codes and pieces fit one; else of sixteen, one to an SM.
+constexpr int kFewCodesOfTwo = 40 * 1024;
+template <typename T, int kTiles, int kWarps>
+lbt_status few_launch(const FewArgs& a, bool behind, cudaStream_t stream) {
+    constexpr int pieces = kFewAhead * 2 * kWarps * 32 * 16;
+    static const cudaError_t allowed = cudaFuncSetAttribute(l8_few_kernel<T, kTiles, kWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                            pieces + (kWarps == 8 ? kFewCodesOfTwo : kFewCodes));
+    if (allowed != cudaSuccess) return LBT_ERR_CUDA;
+    const int smem = pieces + a.M * a.tokens_pitch;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((a.out.cols + 15) / 16));
-    cfg.blockDim = dim3(256);
+    cfg.gridDim = dim3((unsigned)std::min((a.out.cols + 15) / 16, kNumSMs * (16 / kWarps)));
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = behind ? 1 : 0;
-    const cudaError_t e = a.M <= 8 ? cudaLaunchKernelEx(&cfg, l8_few_kernel<void, 1>, a) : cudaLaunchKernelEx(&cfg, l8_few_kernel<void, 2>, a);
-    return e == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, l8_few_kernel<T, kTiles, kWarps>, a) == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
+}
+
+template <typename T, int kTiles>
+lbt_status few_any(const FewArgs& a, bool behind, cudaStream_t stream) {
+    return a.M * a.tokens_pitch <= kFewCodesOfTwo ? few_launch<T, kTiles, 8>(a, behind, stream) : few_launch<T, kTiles, 16>(a, behind, stream);
+}
+
+lbt_status few_from_codes(FewArgs a, bool behind, cudaStream_t stream) {
+    a.wait_prev = behind;
+    return a.M <= 8 ? few_any<void, 1>(a, behind, stream) : few_any<void, 2>(a, behind, stream);
 }
 
 lbt_status few_from_x(FewArgs a, const void* x, int x_type, int64_t ldx, cudaStream_t stream) {
     a.x = x; a.ldx = ldx; a.vec = vec_rows(x, ldx, x_type);
-    const unsigned grid = (unsigned)((a.out.cols + 15) / 16);
-    const size_t smem = (size_t)a.M * a.tokens_pitch;
-    if (x_type == LBT_F32) l8_few_kernel<float, 1><<<grid, 256, smem, stream>>>(a);
-    else if (x_type == LBT_BF16) l8_few_kernel<__nv_bfloat16, 1><<<grid, 256, smem, stream>>>(a);
-    else l8_few_kernel<__half, 1><<<grid, 256, smem, stream>>>(a);
-    return launch_status();
+    if (x_type == LBT_F32) return few_any<float, 1>(a, false, stream);
+    if (x_type == LBT_BF16) return few_any<__nv_bfloat16, 1>(a, false, stream);
+    return few_any<__half, 1>(a, false, stream);
 }
 
 bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
@@ -994,7 +1041,7 @@ extern "C" lbt_status lbt_rows8_quantize(const void* x, int x_type, int64_t rows
 
 static lbt_status forward_product(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, void* y, int y_type,
                                   int64_t ldy, int64_t M, int64_t O, int64_t I, bool behind, int32_t* status, cudaStream_t stream) {
-    if (M <= kFewTokens)
+    if (few_fits(M, I))
         return few_from_codes(few_args(const_cast<void*>(q_x), const_cast<float*>(s_x), q_w, s_w, bias, y, y_type, ldy, M, O, I), behind, stream);
     Product p{};
     p.mode = kForward;
@@ -1028,8 +1075,8 @@ extern "C" lbt_status lbt_linear8_forward(const void* x, int x_type, int64_t ldx
     if (misaligned(x, type_size(x_type))) return LBT_ERR_ALIGNMENT;
     if (M == 0) return LBT_OK;
     const cudaStream_t stream = as_stream(cuda_stream);
-    // One to four tokens: every block quantizes them for itself, one launch.
-    if (M <= 4 && M * ((I + 63) / 64 * 64) <= kFewSmem)
+    // One token: every block quantizes it for itself, one launch.  (Two tokens that way measured as slow as a launch ahead, four slower.)
+    if (M == 1 && few_fits(M, I))
         return few_from_x(few_args(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I), x, x_type, ldx, stream);
     rc = quantize_rows_any(x, x_type, M, I, ldx, q_x, pitch16(I), s_x, stream);
     if (rc != LBT_OK) return rc;
