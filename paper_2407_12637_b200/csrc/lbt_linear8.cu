@@ -51,7 +51,7 @@ struct L8Args {
     void* out;
     int64_t ldo;
     int out_type;
-    int vec;               // rows of the output begin on 32-byte boundaries
+    int vec, vec4;         // rows of the output begin on 32-byte boundaries; four consecutive elements can be stored at once
     int wait_prev;         // chained behind the kernel that writes the operands
     int32_t* status;
 };
@@ -161,27 +161,77 @@ __device__ __forceinline__ void put_block(const L8Args& a, uint32_t* stage, int6
 // ------------------------------------------------------------------------------------------ 128 x 128 tiles
 // One tile per CTA, two CTAs per SM (one drains while the other multiplies).  With few tiles a cluster of `splits` CTAs shares a
 // tile: each takes a slice of the reduction, leaves its int32 accumulator in shared memory, and finishes a slice of the
-// columns from all of them (integer sums: any order gives the same bits).
-__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-    return v;
-}
+// tokens from all of them (integer sums: any order gives the same bits).  The accumulator is parked as [token][channel] whichever
+// operand the tokens were, so that a warp finishes a token's 128 channels at a time: one coalesced access to each CTA's part, one
+// store of 256 or 512 consecutive bytes, and a short loop (a kernel that runs for a few us waits for its instructions, too).
 __device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
-constexpr int kParkPitch = 132;                  // words of a parked accumulator row: 16-byte accesses without bank conflicts
-constexpr int kParkBytes = 128 * kParkPitch * 4;
-static_assert(kParkBytes + 4 * 4096 <= kRing, "the parked accumulator and the warps' staging share the operand ring");
+__device__ __forceinline__ int ld_cluster_s32(uint32_t addr) {
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+constexpr int kParkPitch = 132;   // words of a parked row: 16-byte accesses of neighbouring rows without bank conflicts
+static_assert(128 * kParkPitch * 4 <= kRing, "the parked accumulator takes the operand ring's place");
+
+// Rows [first, last) of the parked tile -> rows row0 + first ... of the output, columns [col0, col0 + 128).
+template <typename T>
+__device__ __forceinline__ void finish_rows(const L8Args& a, uint32_t park, int first, int last, int64_t row0, int col0, int warp, int lane) {
+    // where rows allow it a lane has four consecutive columns, else every 32nd: consecutive lanes store to consecutive addresses either way
+    const int step = a.vec4 ? 1 : 32, c0 = col0 + (a.vec4 ? lane * 4 : lane);
+    float cs[4], bias[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = c0 + i * step;
+        cs[i] = c < a.cols && a.col_scale != nullptr ? __ldg(a.col_scale + c) : 1.0f;
+        bias[i] = c < a.cols && a.bias != nullptr ? __ldg(a.bias + c) : 0.0f;
+    }
+    uint32_t from[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) from[r] = a.splits > 1 ? map_to_cta(park, (uint32_t)min(r, a.splits - 1)) : park;
+    T* out = static_cast<T*>(a.out) + row0 * a.ldo;
+#pragma unroll 2
+    for (int m = first + warp; m < last; m += 4) {
+        const float rs = __ldg(a.row_scale + row0 + m);
+        int sum[4] = {0, 0, 0, 0};
+        if (a.vec4) {
+            const uint32_t at = (uint32_t)(m * kParkPitch + lane * 4) * 4u;
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < a.splits) {
+                    const uint4 v = ld_cluster_v4(from[r] + at);
+                    sum[0] += (int)v.x; sum[1] += (int)v.y; sum[2] += (int)v.z; sum[3] += (int)v.w;
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < a.splits) sum[i] += ld_cluster_s32(from[r] + (uint32_t)(m * kParkPitch + lane + 32 * i) * 4u);
+        }
+        T v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(finish(sum[i], __fmul_rn(rs, cs[i]), bias[i]));
+        T* dst = out + m * a.ldo;
+        if (a.vec4 && c0 + 3 < a.cols) {
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst + c0) = *reinterpret_cast<const uint2*>(v);
+            else *reinterpret_cast<uint4*>(dst + c0) = *reinterpret_cast<const uint4*>(v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c0 + i * step < a.cols) dst[c0 + i * step] = v[i];
+        }
+    }
+}
 
 __global__ void __launch_bounds__(128, 2)
 l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ L8Args a) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     __shared__ Bars bars;
-    __shared__ float token_scale[64];
     Bars* b = &bars;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int split = a.splits > 1 ? (int)cluster_ctarank() : 0;
@@ -192,13 +242,27 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const int m0 = tm * 128, n0 = tn * a.mma_n;
     const bool a_mn = a.mode == kWgrad, b_mn = a.mode != kForward;
 
+    auto load_a = [&](int i, int s) {
+        const int k = (k0 + i) * kStep;
+        uint8_t* dst = ring + s * a.stage_bytes;
+        if (a_mn) tma_load_2d(dst, &tmA, &b->full[s], m0, k); else tma_load_2d(dst, &tmA, &b->full[s], k, m0);
+    };
+    auto load_b = [&](int i, int s) {
+        const int k = (k0 + i) * kStep;
+        uint8_t* dst = ring + s * a.stage_bytes + kBox;
+        if (b_mn) tma_load_2d(dst, &tmB, &b->full[s], n0, k); else tma_load_2d(dst, &tmB, &b->full[s], k, n0);
+    };
+    // One operand (weights, or wgrad's token codes) never comes from the kernel ahead: its first loads wait for nothing.
+    const int ahead = min(a.stages, n_steps);
     if (threadIdx.x == 0) {
-        prefetch_tensormap(&tmA);
-        prefetch_tensormap(&tmB);
         for (int s = 0; s < a.stages; ++s) { mbar_init(&b->full[s], 1); mbar_init(&b->empty[s], 1); }
         mbar_init(&b->tmem_full[0], 1);
         b->abort = 0u;
         fence_mbar_init();
+        for (int i = 0; i < ahead; ++i) {
+            mbar_arrive_expect_tx(&b->full[i], (uint32_t)a.stage_bytes);
+            if (a.swapped) load_a(i, i); else load_b(i, i);
+        }
     }
     if (warp == 1) { tmem_alloc(&b->tmem_base, 128); tmem_relinquish(); }
     tc_fence_before_sync();
@@ -207,25 +271,10 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const uint32_t tmem = b->tmem_base;
 
     if (warp == 0) {
-        if (elect_one()) {
-            auto load_a = [&](int i, int s) {
-                const int k = (k0 + i) * kStep;
-                uint8_t* dst = ring + s * a.stage_bytes;
-                if (a_mn) tma_load_2d(dst, &tmA, &b->full[s], m0, k); else tma_load_2d(dst, &tmA, &b->full[s], k, m0);
-            };
-            auto load_b = [&](int i, int s) {
-                const int k = (k0 + i) * kStep;
-                uint8_t* dst = ring + s * a.stage_bytes + kBox;
-                if (b_mn) tma_load_2d(dst, &tmB, &b->full[s], n0, k); else tma_load_2d(dst, &tmB, &b->full[s], k, n0);
-            };
-            // The weights (A of the swapped form) do not come from the kernel ahead: their first loads do not wait for it.
-            const int ahead = a.wait_prev && a.swapped ? min(a.stages, n_steps) : 0;
-            for (int i = 0; i < ahead; ++i) {
-                mbar_arrive_expect_tx(&b->full[i], (uint32_t)a.stage_bytes);
-                load_a(i, i);
-            }
+        if (lane == 0) {
             if (a.wait_prev) griddep_wait();
-            for (int i = 0; i < ahead; ++i) load_b(i, i);
+            for (int i = 0; i < ahead; ++i)
+                if (a.swapped) load_b(i, i); else load_a(i, i);
             for (int i = ahead; i < n_steps; ++i) {
                 const int s = i % a.stages;
                 if (!wait_for(b, &b->empty[s], (uint32_t)((i / a.stages) & 1) ^ 1u, a.status)) break;
@@ -257,93 +306,40 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         __syncwarp();
     }
     if (a.wait_prev) griddep_wait();   // the scales come from the kernel ahead too, and nothing is written before it has ended
-    if (a.swapped && threadIdx.x < 64) token_scale[threadIdx.x] = n0 + (int)threadIdx.x < a.rows ? a.row_scale[n0 + threadIdx.x] : 0.0f;
     bool ok = true;
     if (n_steps > 0) ok = wait_for(b, &b->tmem_full[0], 0u, a.status);
     ok = __syncthreads_and(ok) != 0;   // uniform; without it a lost signal ends in the error word and no output
     tc_fence_after_sync();
     const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
     uint32_t* park = reinterpret_cast<uint32_t*>(ring);
-    uint32_t* stage = reinterpret_cast<uint32_t*>(ring + kParkBytes + warp * 4096);
-    if (a.splits > 1) {
-        // accumulator -> own shared memory: [row][column], or [token][channel] for the swapped form
-        for (int c = 0; c < a.mma_n && ok; c += 32) {
-            uint32_t v[32];
-            if (n_steps > 0) { tmem_ld_32x32(lanes + (uint32_t)c, v); tmem_ld_wait(); }
-            else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = 0u;
-            }
-            if (a.swapped) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (c + j < a.mma_n) park[(c + j) * 128 + threadIdx.x] = v[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 32; j += 4)
-                    *reinterpret_cast<uint4*>(park + threadIdx.x * kParkPitch + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-            }
-        }
-        cluster_sync_all();
-    }
-    const int64_t row = m0 + (int)threadIdx.x;   // of the output, or (swapped) its column
-    uint32_t from[8];
-    if (a.splits > 1)
-#pragma unroll
-        for (int r = 0; r < 8; ++r) from[r] = map_to_cta(smem_u32(ring), (uint32_t)min(r, a.splits - 1));
-    if (ok && a.swapped) {
-        const float cs = row < a.cols ? __ldg(a.col_scale + row) : 0.0f, bias = a.bias != nullptr && row < a.cols ? __ldg(a.bias + row) : 0.0f;
-        if (a.splits > 1) {
-            const int each = a.mma_n / a.splits;
-#pragma unroll 2
-            for (int c = split * each; c < (split + 1) * each; ++c) {
-                uint32_t part[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r)
-                    if (r < a.splits) part[r] = ld_cluster_u32(from[r] + (uint32_t)(c * 128 + (int)threadIdx.x) * 4u);
-                int sum = 0;
-#pragma unroll
-                for (int r = 0; r < 8; ++r)
-                    if (r < a.splits) sum += (int)part[r];
-                if (n0 + c < a.rows && row < a.cols) put_one(a, n0 + c, row, finish(sum, __fmul_rn(token_scale[c], cs), bias));
-            }
+#pragma unroll 1
+    for (int c = 0; c < a.mma_n && ok; c += 32) {
+        uint32_t v[32];
+        if (n_steps > 0) {
+            tmem_ld_32x32(lanes + (uint32_t)c, v);
+            tmem_ld_wait();
         } else {
-            for (int c = 0; c < a.mma_n; c += 32) {
-                uint32_t v[32];
-                tmem_ld_32x32(lanes + (uint32_t)c, v);
-                tmem_ld_wait();
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (c + j < a.mma_n && n0 + c + j < a.rows && row < a.cols)
-                        put_one(a, n0 + c + j, row, finish((int)v[j], __fmul_rn(token_scale[c + j], cs), bias));
-            }
+            for (int j = 0; j < 32; ++j) v[j] = 0u;
         }
-    } else if (ok) {
-        const float rs = row < a.rows ? a.row_scale[row] : 0.0f;
-        const int each = 128 / a.splits, width = min(each, 32);
-        for (int c = split * each; c < (split + 1) * each; c += width) {
-            uint32_t v[32];
-            if (a.splits > 1) {
+        if (a.swapped) {   // a lane holds a channel
 #pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    uint4 part[8];
-                    uint4 sum = make_uint4(0, 0, 0, 0);
-                    if (j < width) {
+            for (int j = 0; j < 32; ++j)
+                if (c + j < a.mma_n) park[(c + j) * kParkPitch + (int)threadIdx.x] = v[j];
+        } else {           // a lane holds a token
 #pragma unroll
-                        for (int r = 0; r < 8; ++r)
-                            if (r < a.splits) part[r] = ld_cluster_v4(from[r] + (uint32_t)((int)threadIdx.x * kParkPitch + c + j) * 4u);
-#pragma unroll
-                        for (int r = 0; r < 8; ++r)
-                            if (r < a.splits) { sum.x += part[r].x; sum.y += part[r].y; sum.z += part[r].z; sum.w += part[r].w; }
-                    }
-                    v[j] = sum.x; v[j + 1] = sum.y; v[j + 2] = sum.z; v[j + 3] = sum.w;
-                }
-            } else {
-                tmem_ld_32x32(lanes + (uint32_t)c, v);
-                tmem_ld_wait();
-            }
-            put_block(a, stage, m0 + warp * 32, n0 + c, width, v, rs, lane);
+            for (int j = 0; j < 32; j += 4)
+                *reinterpret_cast<uint4*>(park + (int)threadIdx.x * kParkPitch + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
         }
+    }
+    if (a.splits > 1) cluster_sync_all(); else __syncthreads();
+    if (ok) {
+        const int64_t row0 = a.swapped ? n0 : m0;
+        const int col0 = a.swapped ? m0 : n0, rows = a.swapped ? a.mma_n : 128, each = rows / a.splits;
+        const int first = split * each, last = (int)min((int64_t)(first + each), a.rows - row0);
+        if (a.out_type == LBT_BF16) finish_rows<__nv_bfloat16>(a, smem_u32(park), first, last, row0, col0, warp, lane);
+        else if (a.out_type == LBT_F16) finish_rows<__half>(a, smem_u32(park), first, last, row0, col0, warp, lane);
+        else finish_rows<float>(a, smem_u32(park), first, last, row0, col0, warp, lane);
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -492,11 +488,43 @@ __device__ __forceinline__ uint2 codes8(const float (&f)[8], float factor) {
                       pack4(code8(f[4], factor), code8(f[5], factor), code8(f[6], factor), code8(f[7], factor)));
 }
 
+// The largest magnitude of eight raw elements as fp32 bits; for 16-bit types two at a time on the bits without their signs (which
+// order like the magnitudes, infinities and NaN on top), kept apart until the end of the row.
+template <typename T> struct RowMost {
+    uint32_t v = 0;
+    __device__ __forceinline__ void add(const Vec8<T>& r) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v = max(v, r.w[i] & 0x7FFFFFFFu);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v = __vmaxu2(v, r.w[i] & 0x7FFF7FFFu);
+        }
+    }
+    __device__ __forceinline__ uint32_t bits() const {
+        if constexpr (sizeof(T) == 4) return v;
+        const uint16_t top = (uint16_t)max(v & 0xFFFFu, v >> 16);
+        return __float_as_uint(to_f32(*reinterpret_cast<const T*>(&top))) & 0x7FFFFFFFu;
+    }
+};
+
+// Eight consecutive elements [c, c + 8) as they are stored, zeros behind the row's end.
+template <typename T>
+__device__ __forceinline__ void load_raw(const T* row, int64_t c, int64_t cols, bool vec, Vec8<T>& r) {
+    if (vec && c + 8 <= cols) {
+        ld_vec(row + c, r.w);
+    } else {
+        float f[8];
+        load_group(row, c, cols, false, f);
+        pack(f, r);   // (exact: the values came from this type)
+    }
+}
+
 // Row quantizer: kPerRow threads (a warp or the block of 256) own a row, eight columns at a time; the first four groups of a
-// thread stay in registers between the maximum and the codes (8192 columns for a block), the rest is read again.
+// thread stay in registers, as stored, between the maximum and the codes (8192 columns for a block), the rest is read again.
 // One reading of the elements and one byte written for each: bound by memory.
 template <typename T, int kPerRow>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 6 : 4)
 rows8_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, bool vec, uint8_t* __restrict__ q, int64_t ldq,
              float* __restrict__ scale) {
     constexpr int kHeld = 4;
@@ -505,32 +533,27 @@ rows8_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, bo
     const int t = kPerRow == 256 ? threadIdx.x : threadIdx.x & 31;
     if (row >= rows) return;
     const T* src = x + row * ld;
-    float f[kHeld][8];
-    uint32_t most = 0;
+    Vec8<T> held[kHeld];
+    RowMost<T> top;
 #pragma unroll
     for (int g = 0; g < kHeld; ++g) {
         const int64_t c = (int64_t)(g * kPerRow + t) * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[g][i] = 0.0f;
-        if (c < cols) load_group(src, c, cols, vec, f[g]);
+        held[g] = Vec8<T>{};
+        if (c < cols) load_raw(src, c, cols, vec, held[g]);
     }
 #pragma unroll
-    for (int g = 0; g < kHeld; ++g)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = max(most, abs_bits(f[g][i]));
+    for (int g = 0; g < kHeld; ++g) top.add(held[g]);
     for (int64_t c = (int64_t)(kHeld * kPerRow + t) * 8; c < cols; c += kPerRow * 8) {
-        float e[8];
-        load_group(src, c, cols, vec, e);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = max(most, abs_bits(e[i]));
+        Vec8<T> r;
+        load_raw(src, c, cols, vec, r);
+        top.add(r);
     }
-    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    uint32_t most = __reduce_max_sync(0xFFFFFFFFu, top.bits());
     if (kPerRow == 256) {
         __shared__ uint32_t part[8];
         if ((t & 31) == 0) part[t >> 5] = most;
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = max(most, part[i]);
+        most = __reduce_max_sync(0xFFFFFFFFu, part[t & 7]);
     }
     float s, factor;
     scale8(most, s, factor);
@@ -539,12 +562,14 @@ rows8_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, bo
 #pragma unroll
     for (int g = 0; g < kHeld; ++g) {
         const int64_t c = (int64_t)(g * kPerRow + t) * 8;
-        if (c < ldq) *reinterpret_cast<uint2*>(dst + c) = codes8(f[g], factor);
+        float f[8];
+        unpack(held[g], f);
+        if (c < ldq) *reinterpret_cast<uint2*>(dst + c) = codes8(f, factor);
     }
     for (int64_t c = (int64_t)(kHeld * kPerRow + t) * 8; c < ldq; c += kPerRow * 8) {
-        float e[8];
-        load_group(src, c, cols, vec, e);
-        *reinterpret_cast<uint2*>(dst + c) = codes8(e, factor);
+        float f[8];
+        load_group(src, c, cols, vec, f);
+        *reinterpret_cast<uint2*>(dst + c) = codes8(f, factor);
     }
 }
 
@@ -693,69 +718,106 @@ __global__ void __launch_bounds__(kWarps * 32) l8_few_kernel(const __grid_consta
     }
 }
 
-// Gradient quantizer, two passes over dY in tiles of 256 columns x `strip` rows (a warp owns 256 columns and every eighth row).
-// First pass: the largest |dY s_w| of each row, the largest |dY s_x| of each column (as integers: order-free), and with
-// dbias the column sums of each strip.  Second pass: both code matrices and their scales.
+// Gradient quantizer, two passes over dY in tiles of 256 columns x 64 rows (a warp owns 256 columns and every eighth row).  First pass:
+// the largest |dY s_w| of each row, the largest |dY s_x| of each column (as integers: order-free), and with dbias the column sums of
+// each strip.  Second pass, from the last strip back (the first pass left that end in L2): both code matrices and their scales.
+// Bound by instruction issue next to memory, so: kEven (aligned rows, O a multiple of 8) has no test per column, the row's scale
+// and factor are formed once in a lane and handed round, and columns without a usable scale take a way of their own.
 constexpr int kStrip = 64;
+constexpr int kStripRows = kStrip / 8;   // rows of a warp
 
-template <typename T>
+// max(m, |a|, |b|) that keeps a NaN
+__device__ __forceinline__ float most3(float m, float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+
+template <typename T, bool kEven, bool kSums>
 __global__ void __launch_bounds__(256)
 grad8_stats_kernel(const T* __restrict__ dY, int64_t M, int64_t O, int64_t ld, bool vec, const float* __restrict__ s_w,
                    const float* __restrict__ s_x, uint32_t* __restrict__ row_most, uint32_t* __restrict__ col_most, float* __restrict__ sums) {
-    __shared__ uint32_t most[8][256];
-    __shared__ float sum[8][256];
+    __shared__ float most[8][256];
+    __shared__ float sum[kSums ? 8 : 1][256];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t c = (int64_t)blockIdx.x * 256 + lane * 8, m0 = (int64_t)blockIdx.y * kStrip, m1 = min(m0 + kStrip, M);
-    float w[8], total[8];
-    uint32_t cm[8];
+    const int64_t c = (int64_t)blockIdx.x * 256 + lane * 8, m0 = (int64_t)blockIdx.y * kStrip + warp;
+    const int rows = (int)min((int64_t)kStripRows, (M - m0 + 7) / 8);   // of this warp (may be <= 0)
+    const bool live = c < O;
+    float w[8], total[8], cm[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { w[i] = c + i < O ? s_w[c + i] : 0.0f; total[i] = 0.0f; cm[i] = 0u; }
-    for (int64_t m = m0 + warp; m < m1; m += 8) {
-        float f[8];
-        load_group(dY + m * ld, c, O, vec, f);
-        const float sx = s_x[m];
-        uint32_t rm = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (c + i < O) {
-                rm = max(rm, abs_bits(__fmul_rn(f[i], w[i])));
-                cm[i] = max(cm[i], abs_bits(__fmul_rn(f[i], sx)));
-            }
-            total[i] += f[i];
+    for (int i = 0; i < 8; ++i) { w[i] = c + i < O ? s_w[c + i] : 0.0f; total[i] = cm[i] = 0.0f; }
+    const float sx_all = lane < rows ? s_x[m0 + 8 * lane] : 0.0f;
+    const T* row = dY + m0 * ld;
+#pragma unroll 2
+    for (int k = 0; k < rows; ++k, row += 8 * ld) {
+        const float sx = __shfl_sync(0xFFFFFFFFu, sx_all, k);
+        float f[8], rm = 0.0f;
+        if (kEven) {
+            Vec8<T> r{};
+            if (live) ld_vec(row + c, r.w);
+            unpack(r, f);
+        } else {
+            load_group(row, c, O, vec, f);
         }
-        rm = __reduce_max_sync(0xFFFFFFFFu, rm);
-        if (lane == 0) atomicMax(row_most + m, rm);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            rm = most3(rm, __fmul_rn(f[i], w[i]), __fmul_rn(f[i + 1], w[i + 1]));
+            if (kEven || live) {   // (a lane behind the end: 0 times a NaN scale; its columns are not stored)
+                cm[i] = most3(cm[i], __fmul_rn(f[i], sx), 0.0f);
+                cm[i + 1] = most3(cm[i + 1], __fmul_rn(f[i + 1], sx), 0.0f);
+            }
+            if (kSums) { total[i] += f[i]; total[i + 1] += f[i + 1]; }
+        }
+        const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(rm) & 0x7FFFFFFFu);
+        if (lane == 0) atomicMax(row_most + m0 + 8 * k, top);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { most[warp][lane * 8 + i] = cm[i]; sum[warp][lane * 8 + i] = total[i]; }
+    for (int i = 0; i < 8; ++i) {
+        most[warp][lane * 8 + i] = cm[i];
+        if (kSums) sum[warp][lane * 8 + i] = total[i];
+    }
     __syncthreads();
     const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (col >= O) return;
     uint32_t top = 0;
     float all = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { top = max(top, most[i][threadIdx.x]); all += sum[i][threadIdx.x]; }
+    for (int i = 0; i < 8; ++i) {
+        top = max(top, __float_as_uint(most[i][threadIdx.x]) & 0x7FFFFFFFu);
+        if (kSums) all += sum[i][threadIdx.x];
+    }
     atomicMax(col_most + col, top);
-    if (sums != nullptr) sums[(int64_t)blockIdx.y * O + col] = all;
+    if (kSums) sums[(int64_t)blockIdx.y * O + col] = all;
 }
 
-template <typename T>
+// code8 where the factor is known not to be 0
+__device__ __forceinline__ uint32_t code8_live(float t, float factor) { return __float_as_uint(__fadd_rn(__fmul_rn(t, factor), 12582912.0f)); }
+
+template <typename T, bool kEven>
 __global__ void __launch_bounds__(256)
 grad8_codes_kernel(const T* __restrict__ dY, int64_t M, int64_t O, int64_t ld, bool vec, const float* __restrict__ s_w,
                    const float* __restrict__ s_x, const uint32_t* __restrict__ row_most, const uint32_t* __restrict__ col_most,
                    const float* __restrict__ sums, uint8_t* __restrict__ q_r, uint8_t* __restrict__ q_c, int64_t ldq,
                    float* __restrict__ s_r, float* __restrict__ s_c, float* __restrict__ dbias) {
+    griddep_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t c = (int64_t)blockIdx.x * 256 + lane * 8, m0 = (int64_t)blockIdx.y * kStrip, m1 = min(m0 + kStrip, M);
+    const int strip = gridDim.y - 1 - blockIdx.y;
+    const int64_t c = (int64_t)blockIdx.x * 256 + lane * 8, m0 = (int64_t)strip * kStrip + warp;
+    const int rows = (int)min((int64_t)kStripRows, (M - m0 + 7) / 8);
     float w[8], fc[8];
+    bool dead = false;   // a column without a usable scale
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         float s = 0.0f;
         w[i] = fc[i] = 0.0f;
-        if (c + i < O) { w[i] = s_w[c + i]; scale8(col_most[c + i], s, fc[i]); }
-        if (blockIdx.y == 0 && warp == 0 && c + i < O) s_c[c + i] = s;
+        if (c + i < O) {
+            w[i] = s_w[c + i];
+            scale8(col_most[c + i], s, fc[i]);
+            if (strip == 0 && warp == 0) s_c[c + i] = s;
+        }
+        dead |= fc[i] == 0.0f;
     }
-    if (sums != nullptr && blockIdx.y == 0) {
+    if (sums != nullptr && strip == 0) {
         const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
         if (col < O) {
             float all = 0.0f;
@@ -763,21 +825,45 @@ grad8_codes_kernel(const T* __restrict__ dY, int64_t M, int64_t O, int64_t ld, b
             dbias[col] = all;
         }
     }
-    if (c >= ldq) return;
-    for (int64_t m = m0 + warp; m < m1; m += 8) {
-        float f[8], r[8], fr, s;
-        load_group(dY + m * ld, c, O, vec, f);
-        scale8(row_most[m], s, fr);
-        if (c == 0) s_r[m] = s;
-        const float sx = s_x[m];
-        uint32_t k[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            r[i] = __fmul_rn(f[i], w[i]);
-            k[i] = code8(__fmul_rn(f[i], sx), fc[i]);
+    dead = __any_sync(0xFFFFFFFFu, dead && c < ldq);
+    float sx_all = 0.0f, fr_all = 0.0f;
+    if (lane < rows) {
+        float s;
+        sx_all = s_x[m0 + 8 * lane];
+        scale8(row_most[m0 + 8 * lane], s, fr_all);
+        if (blockIdx.x == 0) s_r[m0 + 8 * lane] = s;
+    }
+    const T* row = dY + m0 * ld;
+    uint8_t *to_r = q_r != nullptr ? q_r + m0 * ldq + c : nullptr, *to_c = q_c != nullptr ? q_c + m0 * ldq + c : nullptr;
+#pragma unroll 2
+    for (int k = 0; k < rows; ++k, row += 8 * ld) {
+        const float sx = __shfl_sync(0xFFFFFFFFu, sx_all, k), fr = __shfl_sync(0xFFFFFFFFu, fr_all, k);
+        float f[8];
+        if (kEven) {
+            Vec8<T> r{};
+            if (c < O) ld_vec(row + c, r.w);
+            unpack(r, f);
+        } else {
+            load_group(row, c, O, vec, f);
         }
-        if (q_r != nullptr) *reinterpret_cast<uint2*>(q_r + m * ldq + c) = codes8(r, fr);
-        if (q_c != nullptr) *reinterpret_cast<uint2*>(q_c + m * ldq + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
+        uint32_t q[8], p[8];
+        if (fr != 0.0f && !dead) {   // uniform over the warp
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                q[i] = code8_live(__fmul_rn(f[i], w[i]), fr);
+                p[i] = code8_live(__fmul_rn(f[i], sx), fc[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                q[i] = code8(__fmul_rn(f[i], w[i]), fr);
+                p[i] = code8(__fmul_rn(f[i], sx), fc[i]);
+            }
+        }
+        if (c < ldq) {
+            if (to_r != nullptr) *reinterpret_cast<uint2*>(to_r + k * 8 * ldq) = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+            if (to_c != nullptr) *reinterpret_cast<uint2*>(to_c + k * 8 * ldq) = make_uint2(pack4(p[0], p[1], p[2], p[3]), pack4(p[4], p[5], p[6], p[7]));
+        }
     }
 }
 
@@ -829,6 +915,8 @@ lbt_status allow_smem() {
 
 int64_t pitch16(int64_t n) { return (n + 15) / 16 * 16; }
 
+bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
 struct Product {
     int mode;
     const void* A; int64_t a_pitch, a_rows;   // as stored
@@ -849,6 +937,7 @@ lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
     a.row_scale = p.row_scale; a.col_scale = p.col_scale; a.bias = p.bias;
     a.out = p.out; a.out_type = p.out_type; a.ldo = p.ldo; a.status = status;
     a.vec = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0 && (p.ldo * type_size(p.out_type)) % 32 == 0;
+    a.vec4 = misaligned(p.out, 4 * type_size(p.out_type)) || p.ldo % 4 != 0 ? 0 : 1;
     a.wait_prev = p.behind ? 1 : 0;
     a.splits = 1;
     CUtensorMap tmA, tmB;
@@ -884,8 +973,9 @@ lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
     a.tiles_n = a.swapped ? 1 : (int)((p.cols + 127) / 128);
     a.total = a.tiles_m * a.tiles_n;
     a.band = std::min(a.tiles_m, 8);
-    // clusters share a tile until the CTAs fill two per SM, as long as each has four steps of the reduction
-    while (a.splits < 8 && a.total * a.splits * 2 <= 2 * kNumSMs && a.steps >= a.splits * 2 * 4) a.splits *= 2;
+    // Clusters share a tile while all their CTAs are resident at once (256: 288 CTAs in clusters of four left some for a second
+    // round, 11 us late) and each has four steps of the reduction.
+    while (a.splits < 8 && a.total * a.splits * 2 <= 256 && a.steps >= a.splits * 2 * 4) a.splits *= 2;
     const void* A = a.swapped ? p.B : p.A;
     const void* B = a.swapped ? p.A : p.B;
     if (!code_map(&tmA, A, a.swapped ? p.b_pitch : p.a_pitch, a.swapped ? p.b_rows : p.a_rows, 128) ||
@@ -980,8 +1070,6 @@ lbt_status few_from_x(FewArgs a, const void* x, int x_type, int64_t ldx, cudaStr
     return few_any<__half, 1>(a, false, stream);
 }
 
-bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
-
 lbt_status check_sizes(int64_t M, int64_t O, int64_t I) {
     if (M < 0 || O <= 0 || I <= 0) return LBT_ERR_INVALID_ARG;
     if (M >= (1ll << 31) - 256 || O >= (1ll << 31) - 256 || I >= (1ll << 31) - 256) return LBT_ERR_UNSUPPORTED;
@@ -1018,10 +1106,14 @@ lbt_status quantize_gradient(const T* dY, int type, int64_t M, int64_t O, int64_
     float* sums = dbias != nullptr ? reinterpret_cast<float*>(base + w.sums) : nullptr;
     LBT_CUDA_TRY(cudaMemsetAsync(row_most, 0, w.cleared, stream));
     const dim3 grid((unsigned)((ldq + 255) / 256), (unsigned)((M + kStrip - 1) / kStrip));
-    grad8_stats_kernel<T><<<grid, 256, 0, stream>>>(dY, M, O, ld, vec, s_w, s_x, row_most, col_most, sums);
-    grad8_codes_kernel<T><<<grid, 256, 0, stream>>>(dY, M, O, ld, vec, s_w, s_x, row_most, col_most, sums, need_r ? base + w.q_r : nullptr,
-                                                    need_c ? base + w.q_c : nullptr, ldq, reinterpret_cast<float*>(base + w.s_r),
-                                                    reinterpret_cast<float*>(base + w.s_c), dbias);
+    const bool even = vec && O % 8 == 0;
+    auto stats = even ? (sums != nullptr ? grad8_stats_kernel<T, true, true> : grad8_stats_kernel<T, true, false>)
+                      : (sums != nullptr ? grad8_stats_kernel<T, false, true> : grad8_stats_kernel<T, false, false>);
+    stats<<<grid, 256, 0, stream>>>(dY, M, O, ld, vec, s_w, s_x, row_most, col_most, sums);
+    auto codes = even ? grad8_codes_kernel<T, true> : grad8_codes_kernel<T, false>;
+    codes<<<grid, 256, 0, stream>>>(dY, M, O, ld, vec, s_w, s_x, row_most, col_most, sums, need_r ? base + w.q_r : nullptr,
+                                    need_c ? base + w.q_c : nullptr, ldq, reinterpret_cast<float*>(base + w.s_r),
+                                    reinterpret_cast<float*>(base + w.s_c), dbias);
     return launch_status();
 }
 
@@ -1132,6 +1224,7 @@ extern "C" lbt_status lbt_linear8_backward(const void* dY, int dy_type, int64_t 
         p.B = q_w; p.b_pitch = pitch16(I); p.b_rows = O;
         p.rows = M; p.cols = I; p.red = O;
         p.row_scale = reinterpret_cast<const float*>(base + w.s_r);
+        p.behind = true;   // (the weights, its other operand, are older)
         p.out = dX; p.out_type = dx_type; p.ldo = lddx;
         rc = launch(p, dev_status, stream);
         if (rc != LBT_OK) return rc;
@@ -1143,6 +1236,7 @@ extern "C" lbt_status lbt_linear8_backward(const void* dY, int dy_type, int64_t 
         p.B = q_x; p.b_pitch = pitch16(I); p.b_rows = M;
         p.rows = O; p.cols = I; p.red = M;
         p.row_scale = reinterpret_cast<const float*>(base + w.s_c);
+        p.behind = dX == nullptr;   // the quantizer is the launch ahead; dgrad does not release its successor early
         p.out = dW; p.out_type = dw_type; p.ldo = lddw;
         rc = launch(p, dev_status, stream);
     }
