@@ -164,70 +164,110 @@ __device__ __forceinline__ void put_block(const L8Args& a, uint32_t* stage, int6
 // tokens from all of them (integer sums: any order gives the same bits).  The accumulator is parked as [token][channel] whichever
 // operand the tokens were, so that a warp finishes a token's 128 channels at a time: one coalesced access to each CTA's part, one
 // store of 256 or 512 consecutive bytes, and a short loop (a kernel that runs for a few us waits for its instructions, too).
+// (volatile keeps these behind the cluster's barrier; no memory clobber, so that stores of finished rows do not hold them back)
 __device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
     uint4 v;
-    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
     return v;
 }
-__device__ __forceinline__ int ld_cluster_s32(uint32_t addr) {
-    int v;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ uint4 ld_cluster_words(uint32_t addr) {   // four words 128 bytes apart
+    uint4 v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v.x) : "r"(addr));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v.y) : "r"(addr + 128));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v.z) : "r"(addr + 256));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v.w) : "r"(addr + 384));
     return v;
 }
+constexpr int kTileWarps = 8;     // the last thousand instructions of a tile are its warps' latency: eight share them (four: +1.4 us)
 constexpr int kParkPitch = 132;   // words of a parked row: 16-byte accesses of neighbouring rows without bank conflicts
 static_assert(128 * kParkPitch * 4 <= kRing, "the parked accumulator takes the operand ring's place");
 
-// Rows [first, last) of the parked tile -> rows row0 + first ... of the output, columns [col0, col0 + 128).
-template <typename T>
-__device__ __forceinline__ void finish_rows(const L8Args& a, uint32_t park, int first, int last, int64_t row0, int col0, int warp, int lane) {
-    // where rows allow it a lane has four consecutive columns, else every 32nd: consecutive lanes store to consecutive addresses either way
-    const int step = a.vec4 ? 1 : 32, c0 = col0 + (a.vec4 ? lane * 4 : lane);
-    float cs[4], bias[4];
+// What a warp needs to finish its rows [first + warp, + kTileWarps, ...) of a tile, looked up while the last products run: the scales and
+// biases of the lane's four columns (consecutive ones where rows allow it, else every 32nd: neighbouring lanes store to
+// neighbouring addresses either way), and the scale of the warp's l-th row in lane l.
+struct TileFactors {
+    int first, last, c0, step;
+    float cs[4], bias[4], rows;
+};
+
+__device__ __forceinline__ TileFactors tile_factors(const L8Args& a, int first, int last, int64_t row0, int col0, int warp, int lane) {
+    TileFactors f;
+    f.first = first; f.last = last;
+    f.step = a.vec4 ? 1 : 32;
+    f.c0 = col0 + (a.vec4 ? lane * 4 : lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int c = c0 + i * step;
-        cs[i] = c < a.cols && a.col_scale != nullptr ? __ldg(a.col_scale + c) : 1.0f;
-        bias[i] = c < a.cols && a.bias != nullptr ? __ldg(a.bias + c) : 0.0f;
+        const int c = f.c0 + i * f.step;
+        f.cs[i] = c < a.cols && a.col_scale != nullptr ? __ldg(a.col_scale + c) : 1.0f;
+        f.bias[i] = c < a.cols && a.bias != nullptr ? __ldg(a.bias + c) : 0.0f;
     }
+    const int mine = first + warp + kTileWarps * lane;
+    f.rows = mine < last ? a.row_scale[row0 + mine] : 0.0f;
+    return f;
+}
+
+// Rows of the parked tile -> rows row0 + ... of the output.
+template <typename T>
+__device__ __forceinline__ void finish_rows(const L8Args& a, const TileFactors& f, const uint32_t* parked, int64_t row0, int warp, int lane) {
+    const int first = f.first, last = f.last, c0 = f.c0, step = f.step;
+    const uint32_t park = smem_u32(parked);
     uint32_t from[8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) from[r] = a.splits > 1 ? map_to_cta(park, (uint32_t)min(r, a.splits - 1)) : park;
     T* out = static_cast<T*>(a.out) + row0 * a.ldo;
-#pragma unroll 2
-    for (int m = first + warp; m < last; m += 4) {
-        const float rs = __ldg(a.row_scale + row0 + m);
-        int sum[4] = {0, 0, 0, 0};
-        if (a.vec4) {
-            const uint32_t at = (uint32_t)(m * kParkPitch + lane * 4) * 4u;
+    constexpr int kRows = 4;                    // rows whose parts are on their way together
+#pragma unroll 1
+    for (int i = 0; first + warp + kTileWarps * i < last; i += kRows) {
+        int sum[kRows][4] = {};
+        auto take = [&](int u, const uint4& v) { sum[u][0] += (int)v.x; sum[u][1] += (int)v.y; sum[u][2] += (int)v.z; sum[u][3] += (int)v.w; };
+        uint32_t at[kRows];
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
-                if (r < a.splits) {
-                    const uint4 v = ld_cluster_v4(from[r] + at);
-                    sum[0] += (int)v.x; sum[1] += (int)v.y; sum[2] += (int)v.z; sum[3] += (int)v.w;
+        for (int u = 0; u < kRows; ++u) {
+            at[u] = (uint32_t)((first + warp + kTileWarps * (i + u)) * kParkPitch + (a.vec4 ? lane * 4 : lane)) * 4u;
+        }
+        const int have = min(kRows, (last - first - warp + kTileWarps - 1) / kTileWarps - i);   // rows left (uniform over the warp)
+        if (a.splits == 1) {
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+                if (u < have) {
+                    const uint32_t* p = parked + at[u] / 4;
+                    take(u, a.vec4 ? *reinterpret_cast<const uint4*>(p) : make_uint4(p[0], p[32], p[64], p[96]));
                 }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int r = 0; r < 8; ++r)
+                if (r < a.splits) {
+                    uint4 v[kRows];
 #pragma unroll
-                for (int r = 0; r < 8; ++r)
-                    if (r < a.splits) sum[i] += ld_cluster_s32(from[r] + (uint32_t)(m * kParkPitch + lane + 32 * i) * 4u);
+                    for (int u = 0; u < kRows; ++u)
+                        if (u < have) v[u] = a.vec4 ? ld_cluster_v4(from[r] + at[u]) : ld_cluster_words(from[r] + at[u]);
+#pragma unroll
+                    for (int u = 0; u < kRows; ++u)
+                        if (u < have) take(u, v[u]);
+                }
         }
-        T v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(finish(sum[i], __fmul_rn(rs, cs[i]), bias[i]));
-        T* dst = out + m * a.ldo;
-        if (a.vec4 && c0 + 3 < a.cols) {
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst + c0) = *reinterpret_cast<const uint2*>(v);
-            else *reinterpret_cast<uint4*>(dst + c0) = *reinterpret_cast<const uint4*>(v);
-        } else {
+        for (int u = 0; u < kRows; ++u) {
+            const int m = first + warp + kTileWarps * (i + u);
+            const float rs = __shfl_sync(0xFFFFFFFFu, f.rows, (i + u) & 31);
+            if (u >= have) break;
+            alignas(16) T v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (c0 + i * step < a.cols) dst[c0 + i * step] = v[i];
+            for (int k = 0; k < 4; ++k) v[k] = from_f32<T>(finish(sum[u][k], __fmul_rn(rs, f.cs[k]), f.bias[k]));
+            T* dst = out + m * a.ldo;
+            if (a.vec4 && c0 + 3 < a.cols) {
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst + c0) = *reinterpret_cast<const uint2*>(v);
+                else *reinterpret_cast<uint4*>(dst + c0) = *reinterpret_cast<const uint4*>(v);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c0 + k * step < a.cols) dst[c0 + k * step] = v[k];
+            }
         }
     }
 }
 
-__global__ void __launch_bounds__(128, 2)
+__global__ void __launch_bounds__(kTileWarps * 32, 2)
 l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ L8Args a) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -306,14 +346,19 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         __syncwarp();
     }
     if (a.wait_prev) griddep_wait();   // the scales come from the kernel ahead too, and nothing is written before it has ended
+    const int64_t row0 = a.swapped ? n0 : m0;
+    const int each = (a.swapped ? a.mma_n : 128) / a.splits;
+    const TileFactors factors =
+        tile_factors(a, split * each, (int)min((int64_t)(split * each + each), a.rows - row0), row0, a.swapped ? m0 : n0, warp, lane);
     bool ok = true;
-    if (n_steps > 0) ok = wait_for(b, &b->tmem_full[0], 0u, a.status);
+    if (n_steps > 0 && warp == 1) ok = wait_for(b, &b->tmem_full[0], 0u, a.status);   // one warp polls, the others rest at the barrier
     ok = __syncthreads_and(ok) != 0;   // uniform; without it a lost signal ends in the error word and no output
     tc_fence_after_sync();
-    const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+    const int quarter = warp & 3, tmem_lane = quarter * 32 + lane;   // the TMEM lanes a warp may read; warps 4..7 take every other 32 columns
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     uint32_t* park = reinterpret_cast<uint32_t*>(ring);
 #pragma unroll 1
-    for (int c = 0; c < a.mma_n && ok; c += 32) {
+    for (int c = (warp >> 2) * 32; c < a.mma_n && ok; c += 64) {
         uint32_t v[32];
         if (n_steps > 0) {
             tmem_ld_32x32(lanes + (uint32_t)c, v);
@@ -325,21 +370,18 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         if (a.swapped) {   // a lane holds a channel
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-                if (c + j < a.mma_n) park[(c + j) * kParkPitch + (int)threadIdx.x] = v[j];
+                if (c + j < a.mma_n) park[(c + j) * kParkPitch + tmem_lane] = v[j];
         } else {           // a lane holds a token
 #pragma unroll
             for (int j = 0; j < 32; j += 4)
-                *reinterpret_cast<uint4*>(park + (int)threadIdx.x * kParkPitch + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                *reinterpret_cast<uint4*>(park + tmem_lane * kParkPitch + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
         }
     }
     if (a.splits > 1) cluster_sync_all(); else __syncthreads();
     if (ok) {
-        const int64_t row0 = a.swapped ? n0 : m0;
-        const int col0 = a.swapped ? m0 : n0, rows = a.swapped ? a.mma_n : 128, each = rows / a.splits;
-        const int first = split * each, last = (int)min((int64_t)(first + each), a.rows - row0);
-        if (a.out_type == LBT_BF16) finish_rows<__nv_bfloat16>(a, smem_u32(park), first, last, row0, col0, warp, lane);
-        else if (a.out_type == LBT_F16) finish_rows<__half>(a, smem_u32(park), first, last, row0, col0, warp, lane);
-        else finish_rows<float>(a, smem_u32(park), first, last, row0, col0, warp, lane);
+        if (a.out_type == LBT_BF16) finish_rows<__nv_bfloat16>(a, factors, park, row0, warp, lane);
+        else if (a.out_type == LBT_F16) finish_rows<__half>(a, factors, park, row0, warp, lane);
+        else finish_rows<float>(a, factors, park, row0, warp, lane);
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -988,7 +1030,7 @@ lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
         ++n_attr;
     }
     cfg.gridDim = dim3((unsigned)(a.total * a.splits));
-    cfg.blockDim = dim3(128);
+    cfg.blockDim = dim3(kTileWarps * 32);
     cfg.dynamicSmemBytes = kTileSmem;
     cfg.numAttrs = n_attr;
     return cudaLaunchKernelEx(&cfg, l8_tile_kernel, tmA, tmB, a) == cudaSuccess ? LBT_OK : LBT_ERR_CUDA;
