@@ -40,7 +40,9 @@ class Linear8:
         self.q_w, self.s_w, self.bias, self.kept = q_w, s_w, bias, None
         self.status = torch.zeros(1, dtype=torch.int32, device=q_w.device)   # lbt.ERR_TIMEOUT if a bounded on-chip wait ran out
         self._status = self.status.data_ptr()
-        self._scratch = {}   # stream -> (rows, codes and scales of x): never shared between streams
+        # never shared between streams: codes and scales of x that are not kept (rows, buffer, two addresses), those that were
+        # made here to be kept (shared by one forward pass after the other), and the backward pass's workspace
+        self._scratch, self._own_kept, self._space = {}, {}, {}
 
     def load_weight(self, weight, stream=None):
         """Quantizes the weights [O, I] (after each optimizer step)."""
@@ -49,7 +51,7 @@ class Linear8:
         lbt.rows8_quantize(weight, self.q_w, self.s_w, stream)
 
     def forward(self, x, out=None, keep=False, stream=None):
-        """y for x [M, I]; keep: the codes of x stay for `backward`."""
+        """y for x [M, I]; keep: the codes of x stay for `backward`, until the next forward pass with keep=True."""
         if stream is not None:
             with torch.cuda.stream(stream):   # outputs and scratch belong to the stream that uses them
                 return self.forward(x, out, keep)
@@ -61,9 +63,12 @@ class Linear8:
             raise ValueError("out: one row per row of x")
         raw = lbt._raw_stream(x)
         if keep:
-            self.kept = q_x, s_x = (torch.empty(M, self.pitch, dtype=torch.int8, device=x.device),
-                                    torch.empty(M, dtype=torch.float32, device=x.device))
-            pq, ps = q_x.data_ptr(), s_x.data_ptr()
+            mine = self._own_kept.get(raw)
+            if mine is None or mine[1].shape[0] != M:
+                mine = self._own_kept[raw] = (torch.empty(M, self.pitch, dtype=torch.int8, device=x.device),
+                                              torch.empty(M, dtype=torch.float32, device=x.device))
+            self.kept = mine
+            pq, ps = mine[0].data_ptr(), mine[1].data_ptr()
         else:
             rows, _, pq, ps = self._scratch.get(raw, (0, None, 0, 0))
             if rows < M:
@@ -114,7 +119,13 @@ class Linear8:
             out["dw"] = dw if dw is not None else new(self.O, self.I, dw_dtype)
             if self.bias is not None:
                 out["dbias"] = dbias if dbias is not None else torch.empty(self.O, dtype=torch.float32, device=dy.device)
-        lbt.linear8_backward(dy, self.q_w, self.s_w, q_x, s_x, self.I, out.get("dx"), out.get("dw"), out.get("dbias"), None, self.status)
+        raw = lbt._raw_stream(dy)
+        size, space = self._space.get(raw, (0, None))
+        need = lbt.linear8_workspace_bytes(dy.shape[0], self.O, self.I)
+        if size < need:
+            space = torch.empty(need, dtype=torch.uint8, device=dy.device)
+            self._space[raw] = (need, space)
+        lbt.linear8_backward(dy, self.q_w, self.s_w, q_x, s_x, self.I, out.get("dx"), out.get("dw"), out.get("dbias"), space, self.status)
         return out
 
 
@@ -140,6 +151,7 @@ class ResNorm:
         self.kept = None
         self._params = tuple(lbt._p(p) for p in (w_post, b_post, w_pre, b_pre))   # (the layer's own tensors, whose storage stays)
         self._plans = {}   # (rows, types, leading dimensions) -> descriptor and its workspace size
+        self._space = {}   # stream -> workspace of the backward pass
 
     def _plan(self, names, acts, gate, rows_per_gate):
         """Addresses of the activations and the descriptor of a call on tensors of these sizes (checked each time)."""
@@ -215,19 +227,24 @@ class ResNorm:
         x, h, gate, rows_per_gate, stats = self.kept
         device = x.device
         out = {"dx": torch.empty(x.shape, dtype=x.dtype, device=device), "dh": torch.empty(x.shape, dtype=x.dtype, device=device)}
-        grads = []
-        for name, p in (("dgate", gate), ("dw_post", self.w_post if self.post else None), ("db_post", self.b_post if self.post else None),
-                        ("dw_pre", self.w_pre), ("db_pre", self.b_pre)):
-            if p is not None:
-                out[name] = torch.empty(p.shape, dtype=p.dtype, device=device)
-                grads.append(out[name].data_ptr())
-            else:
-                grads.append(0)
+        if gate is not None:
+            out["dgate"] = torch.empty(gate.shape, dtype=gate.dtype, device=device)
+        named = [(name, p) for name, p in (("dw_post", self.w_post if self.post else None), ("db_post", self.b_post if self.post else None),
+                                           ("dw_pre", self.w_pre), ("db_pre", self.b_pre)) if p is not None]
+        if named:   # one allocation: rows a multiple of 16 bytes apart
+            pitch = -(-self.dim // 8) * 8
+            rows = torch.empty(len(named), pitch, dtype=self.param_dtype, device=device).unbind(0)
+            for (name, p), row in zip(named, rows):
+                out[name] = row if pitch == self.dim and p.dim() == 1 else row[:self.dim].view(p.shape)
+        grads = [out[name].data_ptr() if name in out else 0 for name in ("dgate", "dw_post", "db_post", "dw_pre", "db_pre")]
         at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate)
-        ws = torch.empty(size, dtype=torch.uint8, device=device)
+        raw = lbt._raw_stream(x)
+        ws = self._space.get(raw)
+        if ws is None or ws.numel() < size:
+            ws = self._space[raw] = torch.empty(size, dtype=torch.uint8, device=device)
         w_post, b_post, w_pre, _ = self._params
         status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._p(gate), w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
-                                                *grads, ws.data_ptr(), size, lbt._raw_stream(x))
+                                                *grads, ws.data_ptr(), size, raw)
         if status:
             raise lbt.LbtError(status, "lbt_resnorm_backward")
         return out
