@@ -34,6 +34,7 @@ struct NormArgs {
     int64_t M;
     int D;
     int64_t rows_per_gate;
+    int64_t step_gates, step_rest;   // forward: rows from one row of a group to its next = step_gates gate rows and step_rest rows
     bool layer, post, vec, one_gate;
     int depth;              // rows a thread copies ahead
     float eps_post, eps_pre, scale_x, scale_h, inv_d;
@@ -158,22 +159,28 @@ struct Group {
 
 // The rows ahead of a thread: its own columns of kArrays tensors, `depth` rows deep (0: every load is direct).  Only whole
 // vectors of aligned rows go through it; what the thread copies only the thread reads, so its own wait is all it needs.
-template <typename T, int kThreads, int kG, int kNV, int kArrays>
+template <typename T, typename P, int kThreads, int kG, int kNV, int kArrays>
 struct Ahead {
     static constexpr int kPieces = (int)sizeof(T) / 2;   // 16-byte pieces of eight elements
     static constexpr int kRowBytes = kThreads * kArrays * kNV * kPieces * 16;
     const T* base[kArrays];
     int64_t ld[kArrays];
-    uint8_t* slots;
+    uint8_t* mine;      // this thread's first slot of the row that is read next
+    uint8_t* begin;
+    uint8_t* end;
     int depth, D, t;
     bool vec;
 
-    __device__ __forceinline__ uint8_t* slot(int stage, int array, int g, int piece) const {
-        return slots + stage * kRowBytes + ((array * kNV + g) * kPieces + piece) * (kThreads * 16) + threadIdx.x * 16;
+    __device__ __forceinline__ void set(uint8_t* slots, int rows_ahead, int d, int thread, bool aligned) {
+        begin = mine = slots + threadIdx.x * 16;
+        end = begin + rows_ahead * kRowBytes;
+        depth = rows_ahead; D = d; t = thread;
+        vec = kEven<P> || aligned;
     }
-    // starts the copies of `row` into `stage` (nothing past the last row: an empty group keeps the count)
-    __device__ __forceinline__ void start(int64_t row, int64_t end, int stage) const {
-        if (row < end && vec) {
+    __device__ __forceinline__ bool whole(int c) const { return kEven<P> ? c < D : c + 8 <= D; }
+    // starts the copies of `row` into the slots at `to` (nothing past the last row: an empty group keeps the count)
+    __device__ __forceinline__ void start(int64_t row, int64_t last, uint8_t* to) const {
+        if (row < last && vec) {
 #pragma unroll
             for (int k = 0; k < kArrays; ++k)
                 if (base[k] != nullptr) {
@@ -181,10 +188,10 @@ struct Ahead {
 #pragma unroll
                     for (int g = 0; g < kNV; ++g) {
                         const int c = (g * kG + t) * 8;
-                        if (c + 8 <= D) {
+                        if (whole(c)) {
 #pragma unroll
                             for (int p = 0; p < kPieces; ++p)
-                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(slot(stage, k, g, p))),
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(to + ((k * kNV + g) * kPieces + p) * (kThreads * 16))),
                                              "l"(reinterpret_cast<const uint8_t*>(src + c) + 16 * p) : "memory");
                         }
                     }
@@ -192,22 +199,32 @@ struct Ahead {
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
+    __device__ __forceinline__ void begin_rows(int64_t first, int64_t step, int64_t last) const {
+        for (int s = 0; s < depth; ++s) start(first + s * step, last, begin + s * kRowBytes);
+    }
     // waits for the oldest of the rows ahead
     __device__ __forceinline__ void wait() const {
         if (depth >= 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else if (depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        else if (depth == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
-    __device__ __forceinline__ void read(int64_t row, int stage, int array, int g, float (&f)[8]) const {
+    // the row that has been read makes room for one `depth` rows on
+    __device__ __forceinline__ void advance(int64_t row, int64_t last) {
+        if (depth > 0) {
+            start(row, last, mine);
+            mine = mine + kRowBytes == end ? begin : mine + kRowBytes;
+        }
+    }
+    __device__ __forceinline__ void read(int64_t row, int array, int g, float (&f)[8]) const {
         const int c = (g * kG + t) * 8;
         if (base[array] == nullptr || c >= D) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = 0.0f;
-        } else if (depth > 0 && vec && c + 8 <= D) {
+        } else if (depth > 0 && vec && whole(c)) {
             Vec8<T> v;
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
-                const uint4 w = *reinterpret_cast<const uint4*>(slot(stage, array, g, p));
+                const uint4 w = *reinterpret_cast<const uint4*>(mine + ((array * kNV + g) * kPieces + p) * (kThreads * 16));
                 v.w[4 * p] = w.x; v.w[4 * p + 1] = w.y; v.w[4 * p + 2] = w.z; v.w[4 * p + 3] = w.w;
             }
             unpack(v, f);
@@ -217,9 +234,10 @@ struct Ahead {
     }
 };
 
-// Mean and reciprocal deviation of a row held in registers (columns past D hold zeros and are left out).
+// Mean and reciprocal deviation of a row held in registers (columns past D hold zeros and are left out); the layer norm's mean is
+// taken off the row in place.  rsqrtf: 2 ulp, against a row's sums of D roundings.
 template <typename P, int kG, int kNV>
-__device__ __forceinline__ void row_stats(Group<kG>& grp, const float (&v)[kNV][8], int t, int D, bool layer, float inv_d, float eps, float& mu, float& rstd) {
+__device__ __forceinline__ void row_stats(Group<kG>& grp, float (&v)[kNV][8], int t, int D, bool layer, float inv_d, float eps, float& mu, float& rstd) {
     float s = 0.0f;
     mu = 0.0f;
     if (layer) {
@@ -234,19 +252,16 @@ __device__ __forceinline__ void row_stats(Group<kG>& grp, const float (&v)[kNV][
             const int c = (g * kG + t) * 8;
             if (c < D) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float e = kEven<P> || c + i < D ? v[g][i] - mu : 0.0f;
-                    s += e * e;
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (kEven<P> || c + i < D) v[g][i] -= mu;
             }
         }
-    } else {
-#pragma unroll
-        for (int g = 0; g < kNV; ++g)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[g][i] * v[g][i];
     }
-    rstd = 1.0f / sqrtf(grp.sum(s) * inv_d + eps);
+#pragma unroll
+    for (int g = 0; g < kNV; ++g)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += v[g][i] * v[g][i];
+    rstd = rsqrtf(grp.sum(s) * inv_d + eps);
 }
 
 template <int kG> constexpr int kBlock = kG < 128 ? 256 : kG;   // threads of a block: groups of a warp share one
@@ -259,24 +274,23 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
     Group<kG> grp{slots, 0};
     const int t = threadIdx.x % kG, D = a.D;
     const int64_t step = (int64_t)gridDim.x * kRows, first = (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
-    const Ahead<T, kThreads, kG, kNV, 2> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h)}, {a.ld_x, a.ld_h}, ahead_slots, a.depth, D, t, a.vec};
-    for (int s = 0; s < a.depth; ++s) in.start(first + s * step, a.M, s);
-    int stage = 0;
+    Ahead<T, P, kThreads, kG, kNV, 2> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h)}, {a.ld_x, a.ld_h}};
+    in.set(ahead_slots, a.depth, D, t, a.vec);
+    in.begin_rows(first, step, a.M);
+    // the gate row of `row` and the row's place in it, moved on from row to row without a division
+    int64_t gate_row = 0, gate_place = 0;
+    if (!a.one_gate) { gate_row = first / a.rows_per_gate; gate_place = first - gate_row * a.rows_per_gate; }
     for (int64_t row = first; row < a.M; row += step) {
         float h[kNV][8], r[kNV][8];
-        if (a.depth > 0) in.wait();
+        in.wait();
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
-            in.read(row, stage, 1, g, h[g]);
-            in.read(row, stage, 0, g, r[g]);
+            in.read(row, 1, g, h[g]);
+            in.read(row, 0, g, r[g]);
         }
-        if (a.depth > 0) {
-            in.start(row + a.depth * step, a.M, stage);
-            stage = stage + 1 == a.depth ? 0 : stage + 1;
-        }
+        in.advance(row + a.depth * step, a.M);
         float mu1 = 0.0f, rstd1 = 1.0f, mu2 = 0.0f, rstd2 = 1.0f;
         if (a.post) row_stats<P, kG, kNV>(grp, h, t, D, a.layer, a.inv_d, a.eps_post, mu1, rstd1);
-        const int64_t gate_row = a.one_gate ? 0 : row / a.rows_per_gate * D;
         T* out = static_cast<T*>(a.r) + row * a.ld_r;
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
@@ -286,7 +300,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
                 float w[8], b[8];
                 param_load<P>(a.w_post, 0, c, D, 1.0f, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[g][i] = (h[g][i] - mu1) * rstd1 * w[i];
+                for (int i = 0; i < 8; ++i) h[g][i] = h[g][i] * rstd1 * w[i];
                 if (a.b_post.p != nullptr) {
                     param_load<P>(a.b_post, 0, c, D, 0.0f, b);
 #pragma unroll
@@ -295,7 +309,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
             }
             if (a.gate.p != nullptr) {
                 float gt[8];
-                param_load<P>(a.gate, gate_row, c, D, 1.0f, gt);
+                param_load<P>(a.gate, gate_row * D, c, D, 1.0f, gt);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[g][i] *= gt[i];
             }
@@ -313,7 +327,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
                 float w[8];
                 param_load<P>(a.w_pre, 0, c, D, 1.0f, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[g][i] = (r[g][i] - mu2) * rstd2 * w[i];
+                for (int i = 0; i < 8; ++i) r[g][i] = r[g][i] * rstd2 * w[i];
                 if (a.b_pre.p != nullptr) {
                     param_load<P>(a.b_pre, 0, c, D, 0.0f, w);
 #pragma unroll
@@ -345,6 +359,11 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
             }
         }
         if (a.stats != nullptr && t == 0) a.stats[row] = make_float4(mu1, rstd1, mu2, rstd2);
+        if (!a.one_gate) {
+            gate_row += a.step_gates;
+            gate_place += a.step_rest;
+            if (gate_place >= a.rows_per_gate) { gate_place -= a.rows_per_gate; ++gate_row; }
+        }
     }
 }
 
@@ -389,10 +408,10 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
     const int t = threadIdx.x % kG, D = a.D;
     const int64_t part = (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
     const int64_t first = part * a.rows_each, last = min(first + a.rows_each, a.M);
-    const Ahead<T, kThreads, kG, kNV, 4> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h), static_cast<const T*>(a.dy), static_cast<const T*>(a.dr)},
-                                            {a.ld_x, a.ld_h, a.ld_dy, a.ld_dr}, ahead_slots, a.depth, D, t, a.vec};
-    for (int s = 0; s < a.depth; ++s) in.start(first + s, last, s);
-    int stage = 0;
+    Ahead<T, P, kThreads, kG, kNV, 4> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h), static_cast<const T*>(a.dy), static_cast<const T*>(a.dr)},
+                                         {a.ld_x, a.ld_h, a.ld_dy, a.ld_dr}};
+    in.set(ahead_slots, a.depth, D, t, a.vec);
+    in.begin_rows(first, 1, last);
     float dw1[kNV][8], dw2[kNV][8], dg[kNV][8], db1[kLayer ? kNV : 1][8], db2[kLayer ? kNV : 1][8];
 #pragma unroll
     for (int g = 0; g < kNV; ++g)
@@ -406,18 +425,15 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
         const float4 st = a.stats[row];
         float k1[kNV][8], k2[kNV][8], e[kNV][8], d[kNV][8];   // normalised h, normalised r, dy w_pre, dr
         float s_e = 0.0f, s_ek = 0.0f;
-        if (a.depth > 0) in.wait();
+        in.wait();
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
-            in.read(row, stage, 1, g, k1[g]);
-            in.read(row, stage, 0, g, k2[g]);
-            in.read(row, stage, 2, g, e[g]);
-            in.read(row, stage, 3, g, d[g]);
+            in.read(row, 1, g, k1[g]);
+            in.read(row, 0, g, k2[g]);
+            in.read(row, 2, g, e[g]);
+            in.read(row, 3, g, d[g]);
         }
-        if (a.depth > 0) {
-            in.start(row + a.depth, last, stage);
-            stage = stage + 1 == a.depth ? 0 : stage + 1;
-        }
+        in.advance(row + a.depth, last);
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
@@ -675,8 +691,10 @@ template <typename T, typename P, int kG, int kNV>
 lbt_status forward_launch(NormArgs a, cudaStream_t stream) {
     constexpr int threads = kBlock<kG>, rows = threads / kG, resident = threads <= 768 ? 768 / threads : 1;
     const int64_t blocks = std::min<int64_t>((a.M + rows - 1) / rows, (int64_t)kNumSMs * resident);
-    constexpr int row_bytes = Ahead<T, threads, kG, kNV, 2>::kRowBytes;
+    constexpr int row_bytes = Ahead<T, P, threads, kG, kNV, 2>::kRowBytes;
     a.depth = depth_for(row_bytes, resident, a.vec, (a.M + blocks * rows - 1) / (blocks * rows));
+    a.step_gates = blocks * rows / a.rows_per_gate;
+    a.step_rest = blocks * rows % a.rows_per_gate;
     const lbt_status rc = allow_smem(resnorm_forward_kernel<T, P, kG, kNV>, a.depth * row_bytes);
     if (rc != LBT_OK) return rc;
     resnorm_forward_kernel<T, P, kG, kNV><<<(unsigned)blocks, threads, a.depth * row_bytes, stream>>>(a);
@@ -699,7 +717,7 @@ lbt_status run_forward(const NormArgs& a, cudaStream_t stream) {
 template <typename T, typename P, int kG, int kNV, bool kLayer>
 lbt_status backward_launch(NormArgs a, const Split& s, cudaStream_t stream) {
     constexpr int threads = kBlock<kG>, resident = threads <= 512 ? 512 / threads : 1;
-    constexpr int row_bytes = Ahead<T, threads, kG, kNV, 4>::kRowBytes;
+    constexpr int row_bytes = Ahead<T, P, threads, kG, kNV, 4>::kRowBytes;
     a.depth = depth_for(row_bytes, resident, a.vec, s.rows_each);
     const lbt_status rc = allow_smem(resnorm_backward_kernel<T, P, kG, kNV, kLayer>, a.depth * row_bytes);
     if (rc != LBT_OK) return rc;
