@@ -61,6 +61,10 @@ struct NormArgs {
 template <typename P> constexpr bool kEven = true;
 template <> constexpr bool kEven<void> = false;
 
+// Whether vector g of a thread, from column c on, lies in the row.  The launch picks the smallest group that covers D, so the first half
+// of a thread's vectors always does.
+template <typename P, int kNV> __device__ __forceinline__ bool live(int g, int c, int D) { return (kEven<P> && 2 * g < kNV && kNV > 1) || c < D; }
+
 // Columns [c, c + 8) of a row as fp32 (zeros behind the end), and back.
 template <typename T>
 __device__ __forceinline__ void row_load(const T* row, int c, int D, bool vec, float (&f)[8]) {
@@ -177,25 +181,25 @@ struct Ahead {
         depth = rows_ahead; D = d; t = thread;
         vec = kEven<P> || aligned;
     }
-    __device__ __forceinline__ bool whole(int c) const { return kEven<P> ? c < D : c + 8 <= D; }
+    __device__ __forceinline__ bool whole(int g, int c) const { return kEven<P> ? live<P, kNV>(g, c, D) : c + 8 <= D; }
     // starts the copies of `row` into the slots at `to` (nothing past the last row: an empty group keeps the count)
     __device__ __forceinline__ void start(int64_t row, int64_t last, uint8_t* to) const {
         if (row < last && vec) {
 #pragma unroll
-            for (int k = 0; k < kArrays; ++k)
-                if (base[k] != nullptr) {
-                    const T* src = base[k] + row * ld[k];
+            for (int g = 0; g < kNV; ++g) {
+                const int c = (g * kG + t) * 8;
+                if (whole(g, c)) {
 #pragma unroll
-                    for (int g = 0; g < kNV; ++g) {
-                        const int c = (g * kG + t) * 8;
-                        if (whole(c)) {
+                    for (int k = 0; k < kArrays; ++k)
+                        if (k < 2 || base[k] != nullptr) {
+                            const T* src = base[k] + row * ld[k];
 #pragma unroll
                             for (int p = 0; p < kPieces; ++p)
                                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(to + ((k * kNV + g) * kPieces + p) * (kThreads * 16))),
                                              "l"(reinterpret_cast<const uint8_t*>(src + c) + 16 * p) : "memory");
                         }
-                    }
                 }
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
@@ -217,10 +221,10 @@ struct Ahead {
     }
     __device__ __forceinline__ void read(int64_t row, int array, int g, float (&f)[8]) const {
         const int c = (g * kG + t) * 8;
-        if (base[array] == nullptr || c >= D) {
+        if ((array >= 2 && base[array] == nullptr) || !live<P, kNV>(g, c, D)) {   // (x and h, the first two, are always there)
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = 0.0f;
-        } else if (depth > 0 && vec && whole(c)) {
+        } else if (depth > 0 && vec && whole(g, c)) {
             Vec8<T> v;
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
@@ -272,8 +276,9 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
     extern __shared__ uint8_t ahead_slots[];
     __shared__ float2 slots[2][32];
     Group<kG> grp{slots, 0};
-    const int t = threadIdx.x % kG, D = a.D;
-    const int64_t step = (int64_t)gridDim.x * kRows, first = (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
+    // (a block that owns a row keeps everything about it uniform)
+    const int t = kRows == 1 ? threadIdx.x : threadIdx.x % kG, D = a.D;
+    const int64_t step = (int64_t)gridDim.x * kRows, first = kRows == 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
     Ahead<T, P, kThreads, kG, kNV, 2> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h)}, {a.ld_x, a.ld_h}};
     in.set(ahead_slots, a.depth, D, t, a.vec);
     in.begin_rows(first, step, a.M);
@@ -295,7 +300,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
-            if (c >= D) continue;   // (r holds zeros there)
+            if (!live<P, kNV>(g, c, D)) continue;   // (r holds zeros there)
             if (a.post) {
                 float w[8], b[8];
                 param_load<P>(a.w_post, 0, c, D, 1.0f, w);
@@ -323,7 +328,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
 #pragma unroll
             for (int g = 0; g < kNV; ++g) {
                 const int c = (g * kG + t) * 8;
-                if (c >= D) continue;
+                if (!live<P, kNV>(g, c, D)) continue;
                 float w[8];
                 param_load<P>(a.w_pre, 0, c, D, 1.0f, w);
 #pragma unroll
@@ -405,8 +410,8 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
     __shared__ float2 slots[2][32];
     __shared__ float meet[kRows > 1 ? kG * kNV * 8 : 1];
     Group<kG> grp{slots, 0};
-    const int t = threadIdx.x % kG, D = a.D;
-    const int64_t part = (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
+    const int t = kRows == 1 ? threadIdx.x : threadIdx.x % kG, D = a.D;
+    const int64_t part = kRows == 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
     const int64_t first = part * a.rows_each, last = min(first + a.rows_each, a.M);
     Ahead<T, P, kThreads, kG, kNV, 4> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h), static_cast<const T*>(a.dy), static_cast<const T*>(a.dr)},
                                          {a.ld_x, a.ld_h, a.ld_dy, a.ld_dr}};
@@ -424,6 +429,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
     for (int64_t row = first; row < last; ++row) {
         const float4 st = a.stats[row];
         float k1[kNV][8], k2[kNV][8], e[kNV][8], d[kNV][8];   // normalised h, normalised r, dy w_pre, dr
+        float u[kNV][8], gt[kNV][8];                          // N_post(h), scale_h gate
         float s_e = 0.0f, s_ek = 0.0f;
         in.wait();
 #pragma unroll
@@ -437,34 +443,34 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
-            if (c >= D) continue;
-            float u[8], p[8];
+            if (!live<P, kNV>(g, c, D)) continue;
+            float p[8];
             if (a.post) {
                 param_load<P>(a.w_post, 0, c, D, 1.0f, p);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     k1[g][i] = (kLayer ? k1[g][i] - st.x : k1[g][i]) * st.y;
-                    u[i] = k1[g][i] * p[i];
+                    u[g][i] = k1[g][i] * p[i];
                 }
                 if (kLayer && a.b_post.p != nullptr) {
                     param_load<P>(a.b_post, 0, c, D, 0.0f, p);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) u[i] += p[i];
+                    for (int i = 0; i < 8; ++i) u[g][i] += p[i];
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] = k1[g][i];
+                for (int i = 0; i < 8; ++i) u[g][i] = k1[g][i];
             }
-            if (a.gate.p != nullptr) {
-                param_load<P>(a.gate, gate_i * D, c, D, 1.0f, p);
+            param_load<P>(a.gate, gate_i * D, c, D, 1.0f, p);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] *= p[i];
+            for (int i = 0; i < 8; ++i) {
+                gt[g][i] = a.scale_h * p[i];
+                k2[g][i] = a.scale_x * k2[g][i] + gt[g][i] * u[g][i];   // r
             }
             param_load<P>(a.w_pre, 0, c, D, 1.0f, p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float r = a.scale_x * k2[g][i] + a.scale_h * u[i];
-                k2[g][i] = (kLayer ? r - st.z : r) * st.w;
+                k2[g][i] = (kLayer ? k2[g][i] - st.z : k2[g][i]) * st.w;
                 dw2[g][i] += e[g][i] * k2[g][i];
                 if (kLayer) db2[g][i] += e[g][i];
                 e[g][i] *= p[i];
@@ -492,31 +498,18 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
-            if (c >= D) continue;
-            float out[8], p[8];
+            if (!live<P, kNV>(g, c, D)) continue;
+            float out[8], w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) out[i] = a.scale_x * d[g][i];
             row_store<P>(static_cast<T*>(a.dx) + row * a.ld_dx, c, D, a.vec, out);
+            if (a.post) param_load<P>(a.w_post, 0, c, D, 1.0f, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[g][i] = a.scale_h * d[g][i];   // of gate * u
+            for (int i = 0; i < 8; ++i) {
+                dg[g][i] += u[g][i] * d[g][i];   // (scale_h comes on when the sum leaves)
+                e[g][i] = gt[g][i] * d[g][i];
+            }
             if (a.post) {
-                float w[8];
-                param_load<P>(a.w_post, 0, c, D, 1.0f, w);
-                if (a.gate.p != nullptr) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) out[i] = k1[g][i] * w[i];
-                    if (kLayer && a.b_post.p != nullptr) {
-                        param_load<P>(a.b_post, 0, c, D, 0.0f, p);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) out[i] += p[i];
-                    }
-                    param_load<P>(a.gate, gate_i * D, c, D, 1.0f, p);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        dg[g][i] += out[i] * e[g][i];
-                        e[g][i] *= p[i];
-                    }
-                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     dw1[g][i] += e[g][i] * k1[g][i];
@@ -526,13 +519,6 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
                         if (kLayer) s_e += e[g][i];
                         s_ek += e[g][i] * k1[g][i];
                     }
-                }
-            } else if (a.gate.p != nullptr) {
-                param_load<P>(a.gate, gate_i * D, c, D, 1.0f, p);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    dg[g][i] += k1[g][i] * e[g][i];
-                    e[g][i] *= p[i];
                 }
             }
         }
@@ -553,7 +539,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             const int c = (g * kG + t) * 8;
-            if (c < D) row_store<P>(static_cast<T*>(a.dh) + row * a.ld_dh, c, D, a.vec, e[g]);
+            if (live<P, kNV>(g, c, D)) row_store<P>(static_cast<T*>(a.dh) + row * a.ld_dh, c, D, a.vec, e[g]);
         }
         // the gate row's last row, or the group's: its sum leaves (whole gate rows at once, shared ones through the second kernel)
         if (row + 1 == last || row + 1 == gate_end) {
@@ -567,8 +553,8 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
                     for (int i = 0; i < 8; ++i) {
                         const int c = (g * kG + t) * 8 + i;
                         if (c < D) {
-                            if (whole) param_store(a.dgate, a.gate.type, gate_i * D + c, dg[g][i]);
-                            else shared_part[c] = dg[g][i];
+                            if (whole) param_store(a.dgate, a.gate.type, gate_i * D + c, a.scale_h * dg[g][i]);
+                            else shared_part[c] = a.scale_h * dg[g][i];
                         }
                         dg[g][i] = 0.0f;
                     }
@@ -711,7 +697,8 @@ lbt_status run_forward(const NormArgs& a, cudaStream_t stream) {
     if (a.D <= 4096) return forward_launch<T, P, 256, 2>(a, stream);
     if (a.D <= 8192) return forward_launch<T, P, 512, 2>(a, stream);
     if (a.D <= 16384) return forward_launch<T, P, 1024, 2>(a, stream);
-    return forward_launch<T, P, 1024, 4>(a, stream);
+    if constexpr (!kEven<P>) return forward_launch<T, P, 1024, 4>(a, stream);
+    return LBT_ERR_UNSUPPORTED;   // (not reached: even() refuses such rows)
 }
 
 template <typename T, typename P, int kG, int kNV, bool kLayer>
@@ -734,7 +721,8 @@ lbt_status run_backward_kind(const NormArgs& a, const Split& s, cudaStream_t str
     if (a.D <= 4096) return backward_launch<T, P, 512, 1, kLayer>(a, s, stream);
     if (a.D <= 8192) return backward_launch<T, P, 512, 2, kLayer>(a, s, stream);
     if (a.D <= 16384) return backward_launch<T, P, 1024, 2, kLayer>(a, s, stream);
-    return backward_launch<T, P, 1024, 4, kLayer>(a, s, stream);
+    if constexpr (!kEven<P>) return backward_launch<T, P, 1024, 4, kLayer>(a, s, stream);
+    return LBT_ERR_UNSUPPORTED;   // (not reached: even() refuses such rows)
 }
 template <typename T, typename P>
 lbt_status run_backward(const NormArgs& a, const Split& s, cudaStream_t stream) {
@@ -742,9 +730,9 @@ lbt_status run_backward(const NormArgs& a, const Split& s, cudaStream_t stream) 
 }
 
 // The form for aligned rows where everything is aligned, D is a multiple of 8 and the parameters are fp32 or of the
-// activations' type.
+// activations' type.  (Past 16384 columns rows are rare and the general form serves them.)
 bool even(const NormArgs& a, int type, int param_type) {
-    return a.vec && a.D % 8 == 0 && a.gate.vec && a.w_post.vec && a.b_post.vec && a.w_pre.vec && a.b_pre.vec &&
+    return a.vec && a.D % 8 == 0 && a.D <= 16384 && a.gate.vec && a.w_post.vec && a.b_post.vec && a.w_pre.vec && a.b_pre.vec &&
            (param_type == LBT_F32 || param_type == type);
 }
 #define LBT_RESNORM_DISPATCH(RUN, a, type, ptype, ...)                                                                        \
