@@ -404,7 +404,7 @@ lbt_status lbt_linear8_backward(const void *dY, int dy_type, int64_t lddy, const
 /*
  * Between two residual blocks: u = N_post(h), r = scale_x x + scale_h gate u, y = N_pre(r), for M rows of D columns (D <= 32768).
  *   N(v) = w (v - mu) rstd + b; LBT_NORM_LAYER: mu = mean v, rstd = (mean (v - mu)^2 + eps)^(-1/2); LBT_NORM_RMS: mu = 0.
- * y is formed from r before r is rounded to its type.  Optional (NULL): gate (1), w_* (1), b_* (0), y and q (no second norm),
+ * y is formed from r before r is rounded to its type.  Optional (NULL): gate (1), w_* (1), b_* (0; layer norms only), y and q (no second norm),
  * stats.  gate: [ceil(M / rows_per_gate), D], gate row m / rows_per_gate for row m; rows_per_gate 0 = one gate row for all.
  * q, q_scale: y's 8-bit rows as lbt_linear8_matmul takes them (codes of the fp32 y; q and y may both be asked for).
  * stats: [M,4] floats, 16-byte aligned, kept for the backward pass (mu and rstd of both norms).  r may be x, y may be h.

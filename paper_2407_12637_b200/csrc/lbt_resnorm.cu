@@ -240,11 +240,11 @@ struct Ahead {
 
 // Mean and reciprocal deviation of a row held in registers (columns past D hold zeros and are left out); the layer norm's mean is
 // taken off the row in place.  rsqrtf: 2 ulp, against a row's sums of D roundings.
-template <typename P, int kG, int kNV>
-__device__ __forceinline__ void row_stats(Group<kG>& grp, float (&v)[kNV][8], int t, int D, bool layer, float inv_d, float eps, float& mu, float& rstd) {
+template <typename P, bool kLayer, int kG, int kNV>
+__device__ __forceinline__ void row_stats(Group<kG>& grp, float (&v)[kNV][8], int t, int D, float inv_d, float eps, float& mu, float& rstd) {
     float s = 0.0f;
     mu = 0.0f;
-    if (layer) {
+    if (kLayer) {
 #pragma unroll
         for (int g = 0; g < kNV; ++g)
 #pragma unroll
@@ -270,7 +270,7 @@ __device__ __forceinline__ void row_stats(Group<kG>& grp, float (&v)[kNV][8], in
 
 template <int kG> constexpr int kBlock = kG < 128 ? 256 : kG;   // threads of a block: groups of a warp share one
 
-template <typename T, typename P, int kG, int kNV>
+template <typename T, typename P, int kG, int kNV, bool kLayer>
 __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<kG> : 1) resnorm_forward_kernel(const __grid_constant__ NormArgs a) {
     constexpr int kThreads = kBlock<kG>, kRows = kThreads / kG;
     extern __shared__ uint8_t ahead_slots[];
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
         }
         in.advance(row + a.depth * step, a.M);
         float mu1 = 0.0f, rstd1 = 1.0f, mu2 = 0.0f, rstd2 = 1.0f;
-        if (a.post) row_stats<P, kG, kNV>(grp, h, t, D, a.layer, a.inv_d, a.eps_post, mu1, rstd1);
+        if (a.post) row_stats<P, kLayer, kG, kNV>(grp, h, t, D, a.inv_d, a.eps_post, mu1, rstd1);
         T* out = static_cast<T*>(a.r) + row * a.ld_r;
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
                 param_load<P>(a.w_post, 0, c, D, 1.0f, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[g][i] = h[g][i] * rstd1 * w[i];
-                if (a.b_post.p != nullptr) {
+                if (kLayer && a.b_post.p != nullptr) {
                     param_load<P>(a.b_post, 0, c, D, 0.0f, b);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) h[g][i] += b[i];
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
             row_store<P>(out, c, D, a.vec, r[g]);
         }
         if (a.y != nullptr || a.q != nullptr) {
-            row_stats<P, kG, kNV>(grp, r, t, D, a.layer, a.inv_d, a.eps_pre, mu2, rstd2);
+            row_stats<P, kLayer, kG, kNV>(grp, r, t, D, a.inv_d, a.eps_pre, mu2, rstd2);
             uint32_t most = 0;
 #pragma unroll
             for (int g = 0; g < kNV; ++g) {
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
                 param_load<P>(a.w_pre, 0, c, D, 1.0f, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) r[g][i] = r[g][i] * rstd2 * w[i];
-                if (a.b_pre.p != nullptr) {
+                if (kLayer && a.b_pre.p != nullptr) {
                     param_load<P>(a.b_pre, 0, c, D, 0.0f, w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) r[g][i] += w[i];
@@ -681,9 +681,10 @@ lbt_status forward_launch(NormArgs a, cudaStream_t stream) {
     a.depth = depth_for(row_bytes, resident, a.vec, (a.M + blocks * rows - 1) / (blocks * rows));
     a.step_gates = blocks * rows / a.rows_per_gate;
     a.step_rest = blocks * rows % a.rows_per_gate;
-    const lbt_status rc = allow_smem(resnorm_forward_kernel<T, P, kG, kNV>, a.depth * row_bytes);
+    auto kernel = a.layer ? resnorm_forward_kernel<T, P, kG, kNV, true> : resnorm_forward_kernel<T, P, kG, kNV, false>;
+    const lbt_status rc = allow_smem(kernel, a.depth * row_bytes);
     if (rc != LBT_OK) return rc;
-    resnorm_forward_kernel<T, P, kG, kNV><<<(unsigned)blocks, threads, a.depth * row_bytes, stream>>>(a);
+    kernel<<<(unsigned)blocks, threads, a.depth * row_bytes, stream>>>(a);
     return launch_status();
 }
 
@@ -798,6 +799,7 @@ extern "C" lbt_status lbt_resnorm_forward(const lbt_resnorm_desc* d, const void*
     const lbt_status rc = common(d, &a);
     if (rc != LBT_OK) return rc;
     if (q != nullptr && (q_scale == nullptr || ldq < a.D)) return LBT_ERR_INVALID_ARG;
+    if (!a.layer && (b_post != nullptr || b_pre != nullptr)) return LBT_ERR_INVALID_ARG;
     if (a.M > 0 && (x == nullptr || h == nullptr || r == nullptr)) return LBT_ERR_INVALID_ARG;
     const size_t e = type_size(d->type), pe = type_size(d->param_type);
     if (off(x, e) || off(h, e) || off(r, e) || off(y, e) || off(gate, pe) || off(w_post, pe) || off(b_post, pe) || off(w_pre, pe) ||
@@ -832,7 +834,7 @@ extern "C" lbt_status lbt_resnorm_backward(const lbt_resnorm_desc* d, const void
         return LBT_ERR_INVALID_ARG;
     if (dgate != nullptr && gate == nullptr) return LBT_ERR_INVALID_ARG;
     if (!a.post && (dw_post != nullptr || db_post != nullptr)) return LBT_ERR_INVALID_ARG;
-    if (!a.layer && (db_post != nullptr || db_pre != nullptr)) return LBT_ERR_INVALID_ARG;
+    if (!a.layer && (b_post != nullptr || db_post != nullptr || db_pre != nullptr)) return LBT_ERR_INVALID_ARG;
     const size_t e = type_size(d->type), pe = type_size(d->param_type);
     if (off(dr, e) || off(dy, e) || off(x, e) || off(h, e) || off(dx, e) || off(dh, e) || off(gate, pe) || off(w_post, pe) || off(b_post, pe) ||
         off(w_pre, pe) || off(dgate, pe) || off(dw_post, pe) || off(db_post, pe) || off(dw_pre, pe) || off(db_pre, pe) || off(stats, 16))

@@ -57,7 +57,7 @@ class Linear8:
                 return self.forward(x, out, keep)
         px, tx, ldx = lbt._rows(x, "x", self.I)
         M = x.shape[0]
-        y = torch.empty(M, self.O, dtype=x.dtype, device=x.device) if out is None else out
+        y = x.new_empty((M, self.O)) if out is None else out
         py, ty, ldy = lbt._rows(y, "y", self.O)
         if y.shape[0] != M:
             raise ValueError("out: one row per row of x")
@@ -111,14 +111,13 @@ class Linear8:
         q_x, s_x = self.kept
         if dy.shape[0] != s_x.numel():
             raise ValueError("dy: one row per token of the forward pass")
-        new = lambda rows, cols, dtype: torch.empty(rows, cols, dtype=dtype, device=dy.device)  # noqa: E731
         out = {}
         if need_dx or dx is not None:
-            out["dx"] = dx if dx is not None else new(dy.shape[0], self.I, dy.dtype)
+            out["dx"] = dx if dx is not None else dy.new_empty((dy.shape[0], self.I))
         if need_dw or dw is not None:
-            out["dw"] = dw if dw is not None else new(self.O, self.I, dw_dtype)
+            out["dw"] = dw if dw is not None else dy.new_empty((self.O, self.I), dtype=dw_dtype)
             if self.bias is not None:
-                out["dbias"] = dbias if dbias is not None else torch.empty(self.O, dtype=torch.float32, device=dy.device)
+                out["dbias"] = dbias if dbias is not None else torch.empty_like(self.s_w)
         raw = lbt._raw_stream(dy)
         size, space = self._space.get(raw, (0, None))
         need = lbt.linear8_workspace_bytes(dy.shape[0], self.O, self.I)
@@ -151,7 +150,7 @@ class ResNorm:
         self.kept = None
         self._params = tuple(lbt._p(p) for p in (w_post, b_post, w_pre, b_pre))   # (the layer's own tensors, whose storage stays)
         self._plans = {}   # (rows, types, leading dimensions) -> descriptor and its workspace size
-        self._space = {}   # stream -> workspace of the backward pass
+        self._space, self._stats = {}, {}   # stream -> workspace of the backward pass, statistics that were kept
 
     def _plan(self, names, acts, gate, rows_per_gate):
         """Addresses of the activations and the descriptor of a call on tensors of these sizes (checked each time)."""
@@ -188,21 +187,26 @@ class ResNorm:
     def _forward(self, x, h, gate, rows_per_gate, r, y, q, q_scale, keep):
         names, acts = (("x", "h", "r", "y"), (x, h, r, y)) if y is not None else (("x", "h", "r"), (x, h, r))
         at, (_, desc, _) = self._plan(names, acts, gate, rows_per_gate)
-        stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device) if keep else None
+        raw, stats = lbt._raw_stream(x), None
+        if keep:   # a buffer for each stream, shared by one forward pass after the other
+            stats = self._stats.get(raw)
+            if stats is None or stats.shape[0] != x.shape[0]:
+                stats = self._stats[raw] = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device)
         w_post, b_post, w_pre, b_pre = self._params
         status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._p(gate), w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
-                                               lbt._p(q), q.shape[1] if q is not None else 0, lbt._p(q_scale), lbt._p(stats), lbt._raw_stream(x))
+                                               lbt._p(q), q.shape[1] if q is not None else 0, lbt._p(q_scale), lbt._p(stats), raw)
         if status:
             raise lbt.LbtError(status, "lbt_resnorm_forward")
         if keep:
             self.kept = (x, h, gate, rows_per_gate, stats)
 
     def forward(self, x, h, gate=None, rows_per_gate=0, out=None, keep=False, stream=None):
-        """(r, y); keep: the statistics stay for `backward`, which also needs x and h unchanged."""
+        """(r, y); keep: the statistics stay for `backward` (until the next forward pass with keep=True), which also needs x and h
+        unchanged."""
         if stream is not None:
             with torch.cuda.stream(stream):   # outputs and scratch belong to the stream that uses them
                 return self.forward(x, h, gate, rows_per_gate, out, keep)
-        r, y = out if out is not None else (torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(x.shape, dtype=x.dtype, device=x.device))
+        r, y = out if out is not None else (torch.empty_like(x), torch.empty_like(x))
         self._forward(x, h, gate, rows_per_gate, r, y, None, None, keep)
         return r, y
 
@@ -211,9 +215,9 @@ class ResNorm:
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.forward_codes(x, h, gate, rows_per_gate, out, keep)
-        r = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-        q = torch.empty(x.shape[0], lbt.pitch8(self.dim), dtype=torch.int8, device=x.device)
-        scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+        r = torch.empty_like(x) if out is None else out
+        q = x.new_empty((x.shape[0], lbt.pitch8(self.dim)), dtype=torch.int8)
+        scale = x.new_empty(x.shape[0], dtype=torch.float32)
         self._forward(x, h, gate, rows_per_gate, r, None, q, scale, keep)
         return r, q, scale
 
@@ -225,23 +229,19 @@ class ResNorm:
         if self.kept is None:
             raise RuntimeError("backward needs a forward pass with keep=True")
         x, h, gate, rows_per_gate, stats = self.kept
-        device = x.device
-        out = {"dx": torch.empty(x.shape, dtype=x.dtype, device=device), "dh": torch.empty(x.shape, dtype=x.dtype, device=device)}
-        if gate is not None:
-            out["dgate"] = torch.empty(gate.shape, dtype=gate.dtype, device=device)
-        named = [(name, p) for name, p in (("dw_post", self.w_post if self.post else None), ("db_post", self.b_post if self.post else None),
-                                           ("dw_pre", self.w_pre), ("db_pre", self.b_pre)) if p is not None]
-        if named:   # one allocation: rows a multiple of 16 bytes apart
-            pitch = -(-self.dim // 8) * 8
-            rows = torch.empty(len(named), pitch, dtype=self.param_dtype, device=device).unbind(0)
-            for (name, p), row in zip(named, rows):
-                out[name] = row if pitch == self.dim and p.dim() == 1 else row[:self.dim].view(p.shape)
-        grads = [out[name].data_ptr() if name in out else 0 for name in ("dgate", "dw_post", "db_post", "dw_pre", "db_pre")]
+        out, grads = {"dx": torch.empty_like(x), "dh": torch.empty_like(x)}, []
+        for name, p in (("dgate", gate), ("dw_post", self.w_post if self.post else None), ("db_post", self.b_post if self.post else None),
+                        ("dw_pre", self.w_pre), ("db_pre", self.b_pre)):
+            if p is not None:
+                out[name] = torch.empty_like(p)
+                grads.append(out[name].data_ptr())
+            else:
+                grads.append(0)
         at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate)
         raw = lbt._raw_stream(x)
         ws = self._space.get(raw)
         if ws is None or ws.numel() < size:
-            ws = self._space[raw] = torch.empty(size, dtype=torch.uint8, device=device)
+            ws = self._space[raw] = torch.empty(size, dtype=torch.uint8, device=x.device)
         w_post, b_post, w_pre, _ = self._params
         status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._p(gate), w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
                                                 *grads, ws.data_ptr(), size, raw)

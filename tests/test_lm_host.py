@@ -101,6 +101,7 @@ def test_resnorm_pointers():
     assert f(at(d), A, A, None, A, None, A, None, A, None, A, 72, A, None, None) == lbt.ERR_ALIGNMENT
     assert f(at(d), A, A, None, A, None, A, None, A, None, A, 64, None, None, None) == lbt.ERR_INVALID_ARG  # codes without scales
     assert f(at(d), A, A, None, A, None, A, None, A, A, None, 0, None, A + 4, None) == lbt.ERR_ALIGNMENT
+    assert f(at(d), A, A, None, A, A, A, None, A, A, None, 0, None, None, None) == lbt.ERR_INVALID_ARG     # an RMS norm has no bias
     tail = lambda **k: [k.get(n) for n in ("dgate", "dw_post", "db_post", "dw_pre", "db_pre")]  # noqa: E731
     big = 1 << 40
     assert b(at(d), None, None, A, A, None, A, None, A, A, A, A, *tail(), A, big, None) == lbt.ERR_INVALID_ARG   # no gradient comes in
