@@ -18,6 +18,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "lbt_types.cuh"
 
@@ -145,17 +146,41 @@ __device__ __forceinline__ void block_codes(float (&m)[8], float (&u)[8], float&
     }
 }
 
-// What a lane reads of a whole, aligned block.
+// What a lane reads of an aligned block.  kTail: the block that a tensor ends in; a lane past the end holds zeros, the one that the end
+// falls into reads its elements one by one.
 template <int kBits, typename P, typename G>
 struct AdamRaw {
     Vec8<P> p;
     Vec8<G> g;
     uint32_t m[kBits / 4], v[kBits / 4];   // 8 bytes of codes, or 32 of fp32
 
-    __device__ __forceinline__ void load(const AdamEntry& e, uint64_t block, int lane) {
-        const uint64_t at = block * kAdamBlock + lane * 8;
-        ld_vec(static_cast<const P*>(e.p) + at, p.w);
-        ld_vec(static_cast<const G*>(e.g) + at, g.w);
+    template <bool kTail>
+    __device__ __forceinline__ void load(const AdamEntry& e, uint64_t at) {
+        const P* ps = static_cast<const P*>(e.p) + at;
+        const G* gs = static_cast<const G*>(e.g) + at;
+        if (kTail && at + 8 > e.n) {
+            p = Vec8<P>{};
+            g = Vec8<G>{};
+#pragma unroll
+            for (int i = 0; i < kBits / 4; ++i) m[i] = v[i] = 0u;
+            const int have = e.n > at ? (int)(e.n - at) : 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) {
+                    put(p.w, i, ps[i]);
+                    put(g.w, i, gs[i]);
+                    if constexpr (kBits == 32) {
+                        m[i] = static_cast<const uint32_t*>(e.m)[at + i];
+                        v[i] = static_cast<const uint32_t*>(e.v)[at + i];
+                    } else {
+                        m[i >> 2] |= (uint32_t)static_cast<const uint8_t*>(e.m)[at + i] << (8 * (i & 3));
+                        v[i >> 2] |= (uint32_t)static_cast<const uint8_t*>(e.v)[at + i] << (8 * (i & 3));
+                    }
+                }
+            return;
+        }
+        ld_vec(ps, p.w);
+        ld_vec(gs, g.w);
         if constexpr (kBits == 32) {
             ld_vec(static_cast<const float*>(e.m) + at, m);
             ld_vec(static_cast<const float*>(e.v) + at, v);
@@ -165,11 +190,16 @@ struct AdamRaw {
             m[0] = a.x; m[1] = a.y; v[0] = b.x; v[1] = b.y;
         }
     }
+    template <typename T, int kWords>
+    static __device__ __forceinline__ void put(uint32_t (&w)[kWords], int i, T x) {
+        if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(&x);
+        else w[i >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t*>(&x) << (16 * (i & 1));
+    }
 };
 
-template <int kBits, typename P, typename G>
-__device__ __forceinline__ void adam_whole(const AdamEntry& e, const AdamConst& c, const AdamRaw<kBits, P, G>& raw, float& ms, float& vs, uint64_t block, int lane) {
-    const uint64_t at = block * kAdamBlock + lane * 8;
+template <int kBits, bool kTail, typename P, typename G>
+__device__ __forceinline__ void adam_whole(const AdamEntry& e, const AdamConst& c, const AdamRaw<kBits, P, G>& raw, float& ms, float& vs, uint64_t at) {
+    const int have = !kTail || at + 8 <= e.n ? 8 : e.n > at ? (int)(e.n - at) : 0;
     float p[8], g[8], m[8], v[8], u[8];
     unpack(raw.p, p);
     unpack(raw.g, g);
@@ -188,43 +218,70 @@ __device__ __forceinline__ void adam_whole(const AdamEntry& e, const AdamConst& 
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[i] = adam_update(c, e.step_size, e.decay, g[i], p[i], m[i], v[i]);
-    store8(static_cast<P*>(e.p) + at, p);
-    if constexpr (kBits == 32) {
-        store8(static_cast<float*>(e.m) + at, m);
-        store8(static_cast<float*>(e.v) + at, v);
+    if (kTail && have < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < have) {
+                static_cast<P*>(e.p)[at + i] = from_f32<P>(p[i]);
+                if constexpr (kBits == 32) {
+                    static_cast<float*>(e.m)[at + i] = m[i];
+                    static_cast<float*>(e.v)[at + i] = v[i];
+                }
+            }
     } else {
-        block_codes(m, u, ms, vs);
+        store8(static_cast<P*>(e.p) + at, p);
+        if constexpr (kBits == 32) {
+            store8(static_cast<float*>(e.m) + at, m);
+            store8(static_cast<float*>(e.v) + at, v);
+        }
+    }
+    if constexpr (kBits == 8) {
+        __syncwarp();
+        block_codes(m, u, ms, vs);   // (an absent element's moments are 0)
         uint32_t mc[2], vc[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             mc[i] = e4m3_pair(m[4 * i], m[4 * i + 1]) | e4m3_pair(m[4 * i + 2], m[4 * i + 3]) << 16;
             vc[i] = e4m3_pair(u[4 * i], u[4 * i + 1]) | e4m3_pair(u[4 * i + 2], u[4 * i + 3]) << 16;
         }
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.m) + at) = make_uint2(mc[0], mc[1]);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.v) + at) = make_uint2(vc[0], vc[1]);
+        if (kTail && have < 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have) {
+                    static_cast<uint8_t*>(e.m)[at + i] = (uint8_t)(mc[i >> 2] >> (8 * (i & 3)));
+                    static_cast<uint8_t*>(e.v)[at + i] = (uint8_t)(vc[i >> 2] >> (8 * (i & 3)));
+                }
+        } else {
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.m) + at) = make_uint2(mc[0], mc[1]);
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(e.v) + at) = make_uint2(vc[0], vc[1]);
+        }
     }
 }
 
-// Whole blocks [b, end) of one tensor, at most kAdamRun of them.  Their scales are read and written together, block b + l's by
-// lane l: warps that wrote four bytes each into a sector they shared with others' cost the 0.4 G element step 410 of 1315 us.
+// Blocks [b, end) of one aligned tensor, at most kAdamRun of them; the tensor may end in the last.  Their scales are read and written
+// together, block b + l's by lane l: warps that wrote four bytes each into a sector they shared with others' cost the 0.4 G
+// element step 410 of 1315 us.
 template <int kBits, typename P, typename G>
 __device__ __forceinline__ void adam_run(const AdamEntry& e, const AdamConst& c, uint64_t b, uint64_t end, int lane) {
-    const int count = (int)(end - b);
+    const int count = (int)(end - b), whole = (int)(min(end, e.n / kAdamBlock) - b);   // (end - b or one less)
     float old_ms = 0.0f, old_vs = 0.0f, new_ms = 0.0f, new_vs = 0.0f;
     if (kBits == 8 && lane < count) { old_ms = e.m_scale[b + lane]; old_vs = e.v_scale[b + lane]; }
-#pragma unroll 1
-    for (int k = 0; k < count; ++k) {
+    auto one = [&](auto tail, int k) {
+        const uint64_t at = (b + k) * kAdamBlock + lane * 8;
         AdamRaw<kBits, P, G> now;
-        now.load(e, b + k, lane);
+        now.template load<decltype(tail)::value>(e, at);
         float ms = 0.0f, vs = 0.0f;
         if (kBits == 8) { ms = __shfl_sync(0xFFFFFFFFu, old_ms, k); vs = __shfl_sync(0xFFFFFFFFu, old_vs, k); }
-        adam_whole(e, c, now, ms, vs, b + k, lane);
+        adam_whole<kBits, decltype(tail)::value>(e, c, now, ms, vs, at);
         if (lane == k) { new_ms = ms; new_vs = vs; }
-    }
+    };
+#pragma unroll 1
+    for (int k = 0; k < whole; ++k) one(std::false_type{}, k);
+    if (whole < count) one(std::true_type{}, whole);
     if (kBits == 8 && lane < count) { e.m_scale[b + lane] = new_ms; e.v_scale[b + lane] = new_vs; }
 }
 
-// A block element by element (32 j + lane): the end of a tensor, or tensors that are not aligned.
+// A block of a tensor that is not aligned, element by element (32 j + lane).
 template <int kBits>
 __device__ __forceinline__ void adam_ragged(const AdamEntry& e, const AdamConst& c, uint64_t block, int lane) {
     const int p_type = e.types & 15, g_type = (e.types >> 4) & 15;
@@ -295,14 +352,14 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_con
         }
         const AdamEntry& e = t.e[lo];
         const uint64_t b = (r - first[lo]) * t.run, end = min(b + t.run, (e.n + kAdamBlock - 1) / kAdamBlock);
-        const uint64_t whole = (e.types >> 8) != 0 ? max(b, min(end, e.n / kAdamBlock)) : b;
-        if (b < whole) {
+        if ((e.types >> 8) != 0) {
             const int p_type = e.types & 15;
-            if (p_type == LBT_F32) adam_run_g<kBits, float>(e, c, b, whole, lane);
-            else if (p_type == LBT_BF16) adam_run_g<kBits, __nv_bfloat16>(e, c, b, whole, lane);
-            else adam_run_g<kBits, __half>(e, c, b, whole, lane);
+            if (p_type == LBT_F32) adam_run_g<kBits, float>(e, c, b, end, lane);
+            else if (p_type == LBT_BF16) adam_run_g<kBits, __nv_bfloat16>(e, c, b, end, lane);
+            else adam_run_g<kBits, __half>(e, c, b, end, lane);
+        } else {
+            for (uint64_t k = b; k < end; ++k) adam_ragged<kBits>(e, c, k, lane);
         }
-        for (uint64_t k = whole; k < end; ++k) adam_ragged<kBits>(e, c, k, lane);
     }
 }
 
