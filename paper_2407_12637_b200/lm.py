@@ -221,20 +221,25 @@ class ResNorm:
         self._forward(x, h, gate, rows_per_gate, r, None, q, scale, keep)
         return r, q, scale
 
-    def backward(self, dr, dy, stream=None):
-        """Gradients of the last forward pass with keep=True: {"dx", "dh"} and those of the parameters and the gate that there are."""
+    def backward(self, dr, dy, out=None, stream=None):
+        """Gradients of the last forward pass with keep=True: {"dx", "dh"} and those of the parameters and the gate that there are
+        ("dgate", "dw_post", "db_post", "dw_pre", "db_pre").  out: buffers to write some of them into, by name."""
         if stream is not None:
             with torch.cuda.stream(stream):
-                return self.backward(dr, dy)
+                return self.backward(dr, dy, out)
         if self.kept is None:
             raise RuntimeError("backward needs a forward pass with keep=True")
         x, h, gate, rows_per_gate, stats = self.kept
-        out, grads = {"dx": torch.empty_like(x), "dh": torch.empty_like(x)}, []
+        given, out, grads = out or {}, {}, []
+        for name in ("dx", "dh"):
+            out[name] = given[name] if name in given else torch.empty_like(x)
         for name, p in (("dgate", gate), ("dw_post", self.w_post if self.post else None), ("db_post", self.b_post if self.post else None),
                         ("dw_pre", self.w_pre), ("db_pre", self.b_pre)):
             if p is not None:
-                out[name] = torch.empty_like(p)
-                grads.append(out[name].data_ptr())
+                g = out[name] = given[name] if name in given else torch.empty_like(p)
+                if g.numel() != p.numel() or g.dtype != p.dtype:
+                    raise ValueError(f"{name}: {p.numel()} values of {p.dtype}")
+                grads.append(lbt._p(g))
             else:
                 grads.append(0)
         at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate)
