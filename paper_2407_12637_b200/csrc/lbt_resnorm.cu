@@ -55,49 +55,54 @@ struct NormArgs {
 };
 
 // The kernels come in two forms.  P a type: activation rows and parameter vectors (of type P) are aligned and D is a multiple of 8,
-// so a thread's eight columns are all there or none of them is.  P void: any alignment, any D, parameters of any type, element
-// by element.  (The test for a column costs about as much as the arithmetic on it: on 8192 x 4096 bf16 the second form's
-// forward pass runs 82 instructions an element and is bound by their issue, the first form's 25.)
+// so a thread has eight consecutive columns to a vector, all there or none.  P void: any alignment, any D, parameters of any type;
+// a thread's columns are kG apart, so that a warp reads consecutive elements one by one, and each column is tested.
+// (The tests cost about as much as the arithmetic: on 8192 x 4096 bf16 an element takes 82 instructions forward with them, 36
+// without, and the kernel is bound by their issue.)
 template <typename P> constexpr bool kEven = true;
 template <> constexpr bool kEven<void> = false;
 
-// Whether vector g of a thread, from column c on, lies in the row.  The launch picks the smallest group that covers D, so the first half
-// of a thread's vectors always does.
-template <typename P, int kNV> __device__ __forceinline__ bool live(int g, int c, int D) { return (kEven<P> && 2 * g < kNV && kNV > 1) || c < D; }
+// Column of element i of thread t's vector g, and whether the vector has one in the row.  The launch picks the smallest group that
+// covers D, so the first half of a thread's vectors always does.
+template <typename P, int kG> __device__ __forceinline__ int column(int g, int i, int t) { return kEven<P> ? (g * kG + t) * 8 + i : (g * 8 + i) * kG + t; }
+template <typename P, int kG, int kNV> __device__ __forceinline__ bool live(int g, int t, int D) {
+    return (kEven<P> && 2 * g < kNV && kNV > 1) || column<P, kG>(g, 0, t) < D;
+}
+template <typename P, int kG> __device__ __forceinline__ bool inside(int g, int i, int t, int D) { return kEven<P> || column<P, kG>(g, i, t) < D; }
 
-// Columns [c, c + 8) of a row as fp32 (zeros behind the end), and back.
-template <typename T>
-__device__ __forceinline__ void row_load(const T* row, int c, int D, bool vec, float (&f)[8]) {
-    if (vec && c + 8 <= D) {
-        load8(row + c, f);
+// A vector of a row as fp32 (`fill` behind the row's end), and back.  Only for live vectors.
+template <typename P, int kG, typename T>
+__device__ __forceinline__ void row_load(const T* row, int g, int t, int D, float fill, float (&f)[8]) {
+    if constexpr (kEven<P>) {
+        load8(row + column<P, kG>(g, 0, t), f);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = c + i < D ? to_f32(row[c + i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) f[i] = inside<P, kG>(g, i, t, D) ? to_f32(row[column<P, kG>(g, i, t)]) : fill;
     }
 }
-template <typename P, typename T>
-__device__ __forceinline__ void row_store(T* row, int c, int D, bool vec, const float (&f)[8]) {
-    if (kEven<P> || (vec && c + 8 <= D)) {
-        store8(row + c, f);
+template <typename P, int kG, typename T>
+__device__ __forceinline__ void row_store(T* row, int g, int t, int D, const float (&f)[8]) {
+    if constexpr (kEven<P>) {
+        store8(row + column<P, kG>(g, 0, t), f);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c + i < D) row[c + i] = from_f32<T>(f[i]);
+            if (inside<P, kG>(g, i, t, D)) row[column<P, kG>(g, i, t)] = from_f32<T>(f[i]);
     }
 }
-template <typename P>
-__device__ __forceinline__ void param_load(const Params& p, int64_t at, int c, int D, float fill, float (&f)[8]) {
+template <typename P, int kG>
+__device__ __forceinline__ void param_load(const Params& p, int64_t at, int g, int t, int D, float fill, float (&f)[8]) {
     if (p.p == nullptr) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = fill;
     } else if constexpr (kEven<P>) {
-        load8(static_cast<const P*>(p.p) + at + c, f);
+        row_load<P, kG>(static_cast<const P*>(p.p) + at, g, t, D, fill, f);
     } else if (p.type == LBT_F32) {
-        row_load(static_cast<const float*>(p.p) + at, c, D, p.vec, f);
+        row_load<P, kG>(static_cast<const float*>(p.p) + at, g, t, D, fill, f);
     } else if (p.type == LBT_BF16) {
-        row_load(static_cast<const __nv_bfloat16*>(p.p) + at, c, D, p.vec, f);
+        row_load<P, kG>(static_cast<const __nv_bfloat16*>(p.p) + at, g, t, D, fill, f);
     } else {
-        row_load(static_cast<const __half*>(p.p) + at, c, D, p.vec, f);
+        row_load<P, kG>(static_cast<const __half*>(p.p) + at, g, t, D, fill, f);
     }
 }
 __device__ __forceinline__ void param_store(void* p, int type, int64_t i, float v) {
@@ -161,8 +166,8 @@ struct Group {
     }
 };
 
-// The rows ahead of a thread: its own columns of kArrays tensors, `depth` rows deep (0: every load is direct).  Only whole
-// vectors of aligned rows go through it; what the thread copies only the thread reads, so its own wait is all it needs.
+// The rows ahead of a thread: its own columns of kArrays tensors, `depth` rows deep (0: every load is direct, as it always is in the
+// general form).  What the thread copies only the thread reads, so its own wait is all it needs.
 template <typename T, typename P, int kThreads, int kG, int kNV, int kArrays>
 struct Ahead {
     static constexpr int kPieces = (int)sizeof(T) / 2;   // 16-byte pieces of eight elements
@@ -173,30 +178,26 @@ struct Ahead {
     uint8_t* begin;
     uint8_t* end;
     int depth, D, t;
-    bool vec;
 
-    __device__ __forceinline__ void set(uint8_t* slots, int rows_ahead, int d, int thread, bool aligned) {
+    __device__ __forceinline__ void set(uint8_t* slots, int rows_ahead, int d, int thread) {
         begin = mine = slots + threadIdx.x * 16;
         end = begin + rows_ahead * kRowBytes;
-        depth = rows_ahead; D = d; t = thread;
-        vec = kEven<P> || aligned;
+        depth = kEven<P> ? rows_ahead : 0; D = d; t = thread;
     }
-    __device__ __forceinline__ bool whole(int g, int c) const { return kEven<P> ? live<P, kNV>(g, c, D) : c + 8 <= D; }
     // starts the copies of `row` into the slots at `to` (nothing past the last row: an empty group keeps the count)
     __device__ __forceinline__ void start(int64_t row, int64_t last, uint8_t* to) const {
-        if (row < last && vec) {
+        if (row < last) {
 #pragma unroll
             for (int g = 0; g < kNV; ++g) {
-                const int c = (g * kG + t) * 8;
-                if (whole(g, c)) {
+                if (live<P, kG, kNV>(g, t, D)) {
 #pragma unroll
                     for (int k = 0; k < kArrays; ++k)
                         if (k < 2 || base[k] != nullptr) {
-                            const T* src = base[k] + row * ld[k];
+                            const uint8_t* src = reinterpret_cast<const uint8_t*>(base[k] + row * ld[k] + column<P, kG>(g, 0, t));
 #pragma unroll
                             for (int p = 0; p < kPieces; ++p)
                                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(to + ((k * kNV + g) * kPieces + p) * (kThreads * 16))),
-                                             "l"(reinterpret_cast<const uint8_t*>(src + c) + 16 * p) : "memory");
+                                             "l"(src + 16 * p) : "memory");
                         }
                 }
             }
@@ -220,11 +221,10 @@ struct Ahead {
         }
     }
     __device__ __forceinline__ void read(int64_t row, int array, int g, float (&f)[8]) const {
-        const int c = (g * kG + t) * 8;
-        if ((array >= 2 && base[array] == nullptr) || !live<P, kNV>(g, c, D)) {   // (x and h, the first two, are always there)
+        if ((array >= 2 && base[array] == nullptr) || !live<P, kG, kNV>(g, t, D)) {   // (x and h, the first two, are always there)
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = 0.0f;
-        } else if (depth > 0 && vec && whole(g, c)) {
+        } else if (depth > 0) {
             Vec8<T> v;
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
@@ -233,7 +233,7 @@ struct Ahead {
             }
             unpack(v, f);
         } else {
-            row_load(base[array] + row * ld[array], c, D, vec, f);
+            row_load<P, kG>(base[array] + row * ld[array], g, t, D, 0.0f, f);
         }
     }
 };
@@ -252,14 +252,12 @@ __device__ __forceinline__ void row_stats(Group<kG>& grp, float (&v)[kNV][8], in
         mu = grp.sum(s) * inv_d;
         s = 0.0f;
 #pragma unroll
-        for (int g = 0; g < kNV; ++g) {
-            const int c = (g * kG + t) * 8;
-            if (c < D) {
+        for (int g = 0; g < kNV; ++g)
+            if (live<P, kG, kNV>(g, t, D)) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (kEven<P> || c + i < D) v[g][i] -= mu;
+                    if (inside<P, kG>(g, i, t, D)) v[g][i] -= mu;
             }
-        }
     }
 #pragma unroll
     for (int g = 0; g < kNV; ++g)
@@ -269,9 +267,11 @@ __device__ __forceinline__ void row_stats(Group<kG>& grp, float (&v)[kNV][8], in
 }
 
 template <int kG> constexpr int kBlock = kG < 128 ? 256 : kG;   // threads of a block: groups of a warp share one
+// Blocks of the forward pass on an SM: 1024 threads of 64 registers where sixteen columns a thread fit them, else 768 of 85.
+template <int kG, int kNV> constexpr int kForwardBlocks = (kG == 128 || kG == 256) && kNV <= 2 ? 1024 / kBlock<kG> : kBlock<kG> <= 768 ? 768 / kBlock<kG> : 1;
 
 template <typename T, typename P, int kG, int kNV, bool kLayer>
-__global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<kG> : 1) resnorm_forward_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(kBlock<kG>, kForwardBlocks<kG, kNV>) resnorm_forward_kernel(const __grid_constant__ NormArgs a) {
     constexpr int kThreads = kBlock<kG>, kRows = kThreads / kG;
     extern __shared__ uint8_t ahead_slots[];
     __shared__ float2 slots[2][32];
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
     const int t = kRows == 1 ? threadIdx.x : threadIdx.x % kG, D = a.D;
     const int64_t step = (int64_t)gridDim.x * kRows, first = kRows == 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kRows + threadIdx.x / kG;
     Ahead<T, P, kThreads, kG, kNV, 2> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h)}, {a.ld_x, a.ld_h}};
-    in.set(ahead_slots, a.depth, D, t, a.vec);
+    in.set(ahead_slots, a.depth, D, t);
     in.begin_rows(first, step, a.M);
     // the gate row of `row` and the row's place in it, moved on from row to row without a division
     int64_t gate_row = 0, gate_place = 0;
@@ -299,50 +299,48 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
         T* out = static_cast<T*>(a.r) + row * a.ld_r;
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
-            const int c = (g * kG + t) * 8;
-            if (!live<P, kNV>(g, c, D)) continue;   // (r holds zeros there)
+            if (!live<P, kG, kNV>(g, t, D)) continue;   // (r holds zeros there)
             if (a.post) {
                 float w[8], b[8];
-                param_load<P>(a.w_post, 0, c, D, 1.0f, w);
+                param_load<P, kG>(a.w_post, 0, g, t, D, 1.0f, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[g][i] = h[g][i] * rstd1 * w[i];
                 if (kLayer && a.b_post.p != nullptr) {
-                    param_load<P>(a.b_post, 0, c, D, 0.0f, b);
+                    param_load<P, kG>(a.b_post, 0, g, t, D, 0.0f, b);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) h[g][i] += b[i];
                 }
             }
             if (a.gate.p != nullptr) {
                 float gt[8];
-                param_load<P>(a.gate, gate_row * D, c, D, 1.0f, gt);
+                param_load<P, kG>(a.gate, gate_row * D, g, t, D, 1.0f, gt);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[g][i] *= gt[i];
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[g][i] = kEven<P> || c + i < D ? a.scale_x * r[g][i] + a.scale_h * h[g][i] : 0.0f;
-            row_store<P>(out, c, D, a.vec, r[g]);
+            for (int i = 0; i < 8; ++i) r[g][i] = inside<P, kG>(g, i, t, D) ? a.scale_x * r[g][i] + a.scale_h * h[g][i] : 0.0f;
+            row_store<P, kG>(out, g, t, D, r[g]);
         }
         if (a.y != nullptr || a.q != nullptr) {
             row_stats<P, kLayer, kG, kNV>(grp, r, t, D, a.inv_d, a.eps_pre, mu2, rstd2);
             uint32_t most = 0;
 #pragma unroll
             for (int g = 0; g < kNV; ++g) {
-                const int c = (g * kG + t) * 8;
-                if (!live<P, kNV>(g, c, D)) continue;
+                if (!live<P, kG, kNV>(g, t, D)) continue;
                 float w[8];
-                param_load<P>(a.w_pre, 0, c, D, 1.0f, w);
+                param_load<P, kG>(a.w_pre, 0, g, t, D, 1.0f, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) r[g][i] = r[g][i] * rstd2 * w[i];
                 if (kLayer && a.b_pre.p != nullptr) {
-                    param_load<P>(a.b_pre, 0, c, D, 0.0f, w);
+                    param_load<P, kG>(a.b_pre, 0, g, t, D, 0.0f, w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) r[g][i] += w[i];
                 }
                 if (!kEven<P>)
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if (c + i >= D) r[g][i] = 0.0f;
-                if (a.y != nullptr) row_store<P>(static_cast<T*>(a.y) + row * a.ld_y, c, D, a.vec, r[g]);
+                        if (!inside<P, kG>(g, i, t, D)) r[g][i] = 0.0f;
+                if (a.y != nullptr) row_store<P, kG>(static_cast<T*>(a.y) + row * a.ld_y, g, t, D, r[g]);
             }
             if (a.q != nullptr) {
                 float s, factor;
@@ -354,12 +352,18 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
                 if (t == 0) a.q_scale[row] = s;
 #pragma unroll
                 for (int g = 0; g < kNV; ++g) {
-                    const int c = (g * kG + t) * 8;
                     uint32_t k[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) k[i] = code8(r[g][i], factor);
-                    if (c < a.ldq)
-                        *reinterpret_cast<uint2*>(a.q + row * a.ldq + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
+                    uint8_t* to = a.q + row * a.ldq;
+                    if constexpr (kEven<P>) {
+                        const int c = column<P, kG>(g, 0, t);
+                        if (c < a.ldq) *reinterpret_cast<uint2*>(to + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (column<P, kG>(g, i, t) < a.ldq) to[column<P, kG>(g, i, t)] = (uint8_t)k[i];
+                    }
                 }
             }
         }
@@ -374,7 +378,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 768 ? 768 / kBlock<k
 
 // Adds a group's column sums of one array into what the second kernel adds up: a block's warps (groups of one warp) first meet in
 // shared memory, in order.
-template <int kG, int kNV>
+template <typename P, int kG, int kNV>
 __device__ __forceinline__ void publish(float* part, const float (&acc)[kNV][8], int t, int D, float* meet) {
     if (part == nullptr) return;   // uniform
     constexpr int kRows = kBlock<kG> / kG;
@@ -384,7 +388,7 @@ __device__ __forceinline__ void publish(float* part, const float (&acc)[kNV][8],
         for (int g = 0; g < kNV; ++g)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if ((g * kG + t) * 8 + i < D) dst[(g * kG + t) * 8 + i] = acc[g][i];
+                if (column<P, kG>(g, i, t) < D) dst[column<P, kG>(g, i, t)] = acc[g][i];
     } else {
         for (int w = 0; w < kRows; ++w) {
             __syncthreads();
@@ -393,7 +397,7 @@ __device__ __forceinline__ void publish(float* part, const float (&acc)[kNV][8],
                 for (int g = 0; g < kNV; ++g)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int c = (g * kG + t) * 8 + i;
+                        const int c = column<P, kG>(g, i, t);
                         meet[c] = w == 0 ? acc[g][i] : meet[c] + acc[g][i];
                     }
             }
@@ -415,7 +419,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
     const int64_t first = part * a.rows_each, last = min(first + a.rows_each, a.M);
     Ahead<T, P, kThreads, kG, kNV, 4> in{{static_cast<const T*>(a.x), static_cast<const T*>(a.h), static_cast<const T*>(a.dy), static_cast<const T*>(a.dr)},
                                          {a.ld_x, a.ld_h, a.ld_dy, a.ld_dr}};
-    in.set(ahead_slots, a.depth, D, t, a.vec);
+    in.set(ahead_slots, a.depth, D, t);
     in.begin_rows(first, 1, last);
     float dw1[kNV][8], dw2[kNV][8], dg[kNV][8], db1[kLayer ? kNV : 1][8], db2[kLayer ? kNV : 1][8];
 #pragma unroll
@@ -442,18 +446,17 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
         in.advance(row + a.depth, last);
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
-            const int c = (g * kG + t) * 8;
-            if (!live<P, kNV>(g, c, D)) continue;
+            if (!live<P, kG, kNV>(g, t, D)) continue;
             float p[8];
             if (a.post) {
-                param_load<P>(a.w_post, 0, c, D, 1.0f, p);
+                param_load<P, kG>(a.w_post, 0, g, t, D, 1.0f, p);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     k1[g][i] = (kLayer ? k1[g][i] - st.x : k1[g][i]) * st.y;
                     u[g][i] = k1[g][i] * p[i];
                 }
                 if (kLayer && a.b_post.p != nullptr) {
-                    param_load<P>(a.b_post, 0, c, D, 0.0f, p);
+                    param_load<P, kG>(a.b_post, 0, g, t, D, 0.0f, p);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) u[g][i] += p[i];
                 }
@@ -461,20 +464,20 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
 #pragma unroll
                 for (int i = 0; i < 8; ++i) u[g][i] = k1[g][i];
             }
-            param_load<P>(a.gate, gate_i * D, c, D, 1.0f, p);
+            param_load<P, kG>(a.gate, gate_i * D, g, t, D, 1.0f, p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 gt[g][i] = a.scale_h * p[i];
                 k2[g][i] = a.scale_x * k2[g][i] + gt[g][i] * u[g][i];   // r
             }
-            param_load<P>(a.w_pre, 0, c, D, 1.0f, p);
+            param_load<P, kG>(a.w_pre, 0, g, t, D, 1.0f, p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 k2[g][i] = (kLayer ? k2[g][i] - st.z : k2[g][i]) * st.w;
                 dw2[g][i] += e[g][i] * k2[g][i];
                 if (kLayer) db2[g][i] += e[g][i];
                 e[g][i] *= p[i];
-                if (kEven<P> || c + i < D) {   // columns past the end hold no element
+                if (inside<P, kG>(g, i, t, D)) {   // columns past the end hold no element
                     if (kLayer) s_e += e[g][i];
                     s_ek += e[g][i] * k2[g][i];
                 }
@@ -497,13 +500,12 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
         s_e = s_ek = 0.0f;
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
-            const int c = (g * kG + t) * 8;
-            if (!live<P, kNV>(g, c, D)) continue;
+            if (!live<P, kG, kNV>(g, t, D)) continue;
             float out[8], w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) out[i] = a.scale_x * d[g][i];
-            row_store<P>(static_cast<T*>(a.dx) + row * a.ld_dx, c, D, a.vec, out);
-            if (a.post) param_load<P>(a.w_post, 0, c, D, 1.0f, w);
+            row_store<P, kG>(static_cast<T*>(a.dx) + row * a.ld_dx, g, t, D, out);
+            if (a.post) param_load<P, kG>(a.w_post, 0, g, t, D, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 dg[g][i] += u[g][i] * d[g][i];   // (scale_h comes on when the sum leaves)
@@ -515,7 +517,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
                     dw1[g][i] += e[g][i] * k1[g][i];
                     if (kLayer) db1[g][i] += e[g][i];
                     e[g][i] *= w[i];
-                    if (kEven<P> || c + i < D) {
+                    if (inside<P, kG>(g, i, t, D)) {
                         if (kLayer) s_e += e[g][i];
                         s_ek += e[g][i] * k1[g][i];
                     }
@@ -538,8 +540,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
         }
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
-            const int c = (g * kG + t) * 8;
-            if (live<P, kNV>(g, c, D)) row_store<P>(static_cast<T*>(a.dh) + row * a.ld_dh, c, D, a.vec, e[g]);
+            if (live<P, kG, kNV>(g, t, D)) row_store<P, kG>(static_cast<T*>(a.dh) + row * a.ld_dh, g, t, D, e[g]);
         }
         // the gate row's last row, or the group's: its sum leaves (whole gate rows at once, shared ones through the second kernel)
         if (row + 1 == last || row + 1 == gate_end) {
@@ -551,7 +552,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
                 for (int g = 0; g < kNV; ++g)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int c = (g * kG + t) * 8 + i;
+                        const int c = column<P, kG>(g, i, t);
                         if (c < D) {
                             if (whole) param_store(a.dgate, a.gate.type, gate_i * D + c, a.scale_h * dg[g][i]);
                             else shared_part[c] = a.scale_h * dg[g][i];
@@ -563,17 +564,18 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
             gate_end += a.rows_per_gate;
         }
     }
-    publish<kG, kNV>(a.part_w_pre, dw2, t, D, meet);
-    publish<kG, kNV>(a.part_w_post, dw1, t, D, meet);
+    publish<P, kG, kNV>(a.part_w_pre, dw2, t, D, meet);
+    publish<P, kG, kNV>(a.part_w_post, dw1, t, D, meet);
     if (kLayer) {
-        publish<kLayer ? kG : 32, kLayer ? kNV : 1>(a.part_b_pre, db2, t, D, meet);
-        publish<kLayer ? kG : 32, kLayer ? kNV : 1>(a.part_b_post, db1, t, D, meet);
+        publish<P, kLayer ? kG : 32, kLayer ? kNV : 1>(a.part_b_pre, db2, t, D, meet);
+        publish<P, kLayer ? kG : 32, kLayer ? kNV : 1>(a.part_b_post, db1, t, D, meet);
     }
 }
 
 // Second kernel of the backward pass: column sums over the blocks' partial sums, and the gate rows that several groups share.
 // blockIdx.y: which array, then which gate row (or, where there are fewer of them, which border between two groups: a shared gate
-// row belongs to the first border inside it); 32 columns a block, 32 threads a column, added in a fixed order.
+// row belongs to the first border inside it); 32 columns a block, eight threads a column with eight loads in flight each, added in a fixed order.
+// Launched behind the first kernel's end (its blocks are resident by then).
 struct FinishArgs {
     int D;
     int blocks;
@@ -588,37 +590,41 @@ struct FinishArgs {
     int64_t M, rows_per_gate, rows_each;
 };
 
-__global__ void __launch_bounds__(1024) resnorm_finish_kernel(const __grid_constant__ FinishArgs f) {
-    __shared__ float meet[32][33];
+__global__ void __launch_bounds__(256) resnorm_finish_kernel(const __grid_constant__ FinishArgs f) {
+    __shared__ float meet[8][33];
     const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
     int64_t gate = (int64_t)blockIdx.y - f.arrays;
+    sm100::griddep_wait();
     if (gate < 0) {
         const float* p = f.part[blockIdx.y];
         if (c < f.D)
-#pragma unroll 4
-            for (int b = y; b < f.blocks; b += 32) s += p[(int64_t)b * f.D + c];
+#pragma unroll 8
+            for (int b = y; b < f.blocks; b += 8) s += p[(int64_t)b * f.D + c];
     } else {
         const int64_t border = f.by_border ? gate + 1 : 0;
         if (f.by_border) gate = border * f.rows_each / f.rows_per_gate;
         const int64_t g0 = gate * f.rows_per_gate, g1 = min(g0 + f.rows_per_gate, f.M);
         const int64_t p0 = g0 / f.rows_each, p1 = (g1 - 1) / f.rows_each;
         if (p0 == p1 || (f.by_border && (g0 == border * f.rows_each || p0 != border - 1))) return;   // one group's alone, or another border's
-        if (c < f.D)
-#pragma unroll 4
-            for (int64_t p = p0 + y; p <= p1; p += 32) s += f.part_gate[(p * 2 + (gate == p * f.rows_each / f.rows_per_gate ? 0 : 1)) * f.D + c];
+        // only a part's first gate row can have begun before it, so of parts p0 + 1 ... it is slot 0; of part p0 it is slot 0 where
+        // that part begins with it
+        if (c < f.D) {
+            const float* p = f.part_gate + c;
+            if (y == 0) s = p[(p0 * 2 + (gate == p0 * f.rows_each / f.rows_per_gate ? 0 : 1)) * f.D];
+#pragma unroll 8
+            for (int64_t i = p0 + 1 + y; i <= p1; i += 8) s += p[i * 2 * f.D];
+        }
     }
     meet[y][lane] = s;
     __syncthreads();
-    // column `y` of the block is added up by warp y: lane by lane in a fixed tree
-    s = meet[lane][y];
+    if (y != 0 || c >= f.D) return;
+    s = 0.0f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    const int64_t col = (int64_t)blockIdx.x * 32 + y;
-    if (lane != 0 || col >= f.D) return;
-    if ((int)blockIdx.y < f.arrays) param_store(f.out[blockIdx.y], f.type, col, s);
-    else param_store(f.dgate, f.gate_type, gate * f.D + col, s);
+    for (int i = 0; i < 8; ++i) s += meet[i][lane];
+    if ((int)blockIdx.y < f.arrays) param_store(f.out[blockIdx.y], f.type, c, s);
+    else param_store(f.dgate, f.gate_type, gate * f.D + c, s);
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -661,8 +667,8 @@ NormSpace norm_space(int64_t M, int D) {
 }
 
 // Rows ahead that fit the shared memory of a block when `resident` of them share an SM.
-int depth_for(int row_bytes, int resident, bool vec, int64_t rows_each) {
-    if (!vec || rows_each < 2) return 0;   // (one row a group: nothing to run ahead of)
+int depth_for(int row_bytes, int resident, bool even, int64_t rows_each) {
+    if (!even || rows_each < 2) return 0;   // (one row a group: nothing to run ahead of)
     return (int)std::min<int64_t>(3, 200 * 1024 / resident / row_bytes);
 }
 
@@ -675,10 +681,10 @@ lbt_status allow_smem(K kernel, int bytes) {
 
 template <typename T, typename P, int kG, int kNV>
 lbt_status forward_launch(NormArgs a, cudaStream_t stream) {
-    constexpr int threads = kBlock<kG>, rows = threads / kG, resident = threads <= 768 ? 768 / threads : 1;
+    constexpr int threads = kBlock<kG>, rows = threads / kG, resident = kForwardBlocks<kG, kNV>;
     const int64_t blocks = std::min<int64_t>((a.M + rows - 1) / rows, (int64_t)kNumSMs * resident);
     constexpr int row_bytes = Ahead<T, P, threads, kG, kNV, 2>::kRowBytes;
-    a.depth = depth_for(row_bytes, resident, a.vec, (a.M + blocks * rows - 1) / (blocks * rows));
+    a.depth = depth_for(row_bytes, resident, kEven<P>, (a.M + blocks * rows - 1) / (blocks * rows));
     a.step_gates = blocks * rows / a.rows_per_gate;
     a.step_rest = blocks * rows % a.rows_per_gate;
     auto kernel = a.layer ? resnorm_forward_kernel<T, P, kG, kNV, true> : resnorm_forward_kernel<T, P, kG, kNV, false>;
@@ -706,7 +712,7 @@ template <typename T, typename P, int kG, int kNV, bool kLayer>
 lbt_status backward_launch(NormArgs a, const Split& s, cudaStream_t stream) {
     constexpr int threads = kBlock<kG>, resident = threads <= 512 ? 512 / threads : 1;
     constexpr int row_bytes = Ahead<T, P, threads, kG, kNV, 4>::kRowBytes;
-    a.depth = depth_for(row_bytes, resident, a.vec, s.rows_each);
+    a.depth = depth_for(row_bytes, resident, kEven<P>, s.rows_each);
     const lbt_status rc = allow_smem(resnorm_backward_kernel<T, P, kG, kNV, kLayer>, a.depth * row_bytes);
     if (rc != LBT_OK) return rc;
     resnorm_backward_kernel<T, P, kG, kNV, kLayer><<<(unsigned)s.blocks, threads, a.depth * row_bytes, stream>>>(a);
@@ -879,6 +885,15 @@ extern "C" lbt_status lbt_resnorm_backward(const lbt_resnorm_desc* d, const void
         f.M = a.M; f.rows_per_gate = a.rows_per_gate; f.rows_each = a.rows_each;
     }
     if (f.arrays + shared == 0) return LBT_OK;
-    resnorm_finish_kernel<<<dim3((unsigned)((a.D + 31) / 32), (unsigned)(f.arrays + shared)), 1024, 0, stream>>>(f);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((a.D + 31) / 32), (unsigned)(f.arrays + shared));
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, resnorm_finish_kernel, f) != cudaSuccess) return LBT_ERR_CUDA;
     return launch_status();
 }
