@@ -68,7 +68,18 @@ template <typename P, int kG> __device__ __forceinline__ int column(int g, int i
 template <typename P, int kG, int kNV> __device__ __forceinline__ bool live(int g, int t, int D) {
     return (kEven<P> && 2 * g < kNV && kNV > 1) || column<P, kG>(g, 0, t) < D;
 }
-template <typename P, int kG> __device__ __forceinline__ bool inside(int g, int i, int t, int D) { return kEven<P> || column<P, kG>(g, i, t) < D; }
+template <typename P, int kG> __device__ __forceinline__ bool full(int g, int t, int D) { return kEven<P> || column<P, kG>(g, 7, t) < D; }
+// Runs body(i) for the elements of a live vector that lie in the row: without a test where all do.
+template <typename P, int kG, typename Body> __device__ __forceinline__ void each(int g, int t, int D, Body body) {
+    if (full<P, kG>(g, t, D)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) body(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (column<P, kG>(g, i, t) < D) body(i);
+    }
+}
 
 // A vector of a row as fp32 (`fill` behind the row's end), and back.  Only for live vectors.
 template <typename P, int kG, typename T>
@@ -77,7 +88,8 @@ __device__ __forceinline__ void row_load(const T* row, int g, int t, int D, floa
         load8(row + column<P, kG>(g, 0, t), f);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = inside<P, kG>(g, i, t, D) ? to_f32(row[column<P, kG>(g, i, t)]) : fill;
+        for (int i = 0; i < 8; ++i) f[i] = fill;
+        each<P, kG>(g, t, D, [&](int i) { f[i] = to_f32(row[column<P, kG>(g, i, t)]); });
     }
 }
 template <typename P, int kG, typename T>
@@ -85,9 +97,7 @@ __device__ __forceinline__ void row_store(T* row, int g, int t, int D, const flo
     if constexpr (kEven<P>) {
         store8(row + column<P, kG>(g, 0, t), f);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (inside<P, kG>(g, i, t, D)) row[column<P, kG>(g, i, t)] = from_f32<T>(f[i]);
+        each<P, kG>(g, t, D, [&](int i) { row[column<P, kG>(g, i, t)] = from_f32<T>(f[i]); });
     }
 }
 template <typename P, int kG>
@@ -253,11 +263,7 @@ __device__ __forceinline__ void row_stats(Group<kG>& grp, float (&v)[kNV][8], in
         s = 0.0f;
 #pragma unroll
         for (int g = 0; g < kNV; ++g)
-            if (live<P, kG, kNV>(g, t, D)) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (inside<P, kG>(g, i, t, D)) v[g][i] -= mu;
-            }
+            if (live<P, kG, kNV>(g, t, D)) each<P, kG>(g, t, D, [&](int i) { v[g][i] -= mu; });
     }
 #pragma unroll
     for (int g = 0; g < kNV; ++g)
@@ -318,7 +324,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kForwardBlocks<kG, kNV>) resnorm_f
                 for (int i = 0; i < 8; ++i) h[g][i] *= gt[i];
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[g][i] = inside<P, kG>(g, i, t, D) ? a.scale_x * r[g][i] + a.scale_h * h[g][i] : 0.0f;
+            for (int i = 0; i < 8; ++i) r[g][i] = a.scale_x * r[g][i] + a.scale_h * h[g][i];   // (x = h = 0 past the end: so are r and y)
             row_store<P, kG>(out, g, t, D, r[g]);
         }
         if (a.y != nullptr || a.q != nullptr) {
@@ -336,10 +342,6 @@ __global__ void __launch_bounds__(kBlock<kG>, kForwardBlocks<kG, kNV>) resnorm_f
 #pragma unroll
                     for (int i = 0; i < 8; ++i) r[g][i] += w[i];
                 }
-                if (!kEven<P>)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (!inside<P, kG>(g, i, t, D)) r[g][i] = 0.0f;
                 if (a.y != nullptr) row_store<P, kG>(static_cast<T*>(a.y) + row * a.ld_y, g, t, D, r[g]);
             }
             if (a.q != nullptr) {
@@ -436,18 +438,10 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
         float u[kNV][8], gt[kNV][8];                          // N_post(h), scale_h gate
         float s_e = 0.0f, s_ek = 0.0f;
         in.wait();
-#pragma unroll
-        for (int g = 0; g < kNV; ++g) {
-            in.read(row, 1, g, k1[g]);
-            in.read(row, 0, g, k2[g]);
-            in.read(row, 2, g, e[g]);
-            in.read(row, 3, g, d[g]);
-        }
-        in.advance(row + a.depth, last);
-#pragma unroll
-        for (int g = 0; g < kNV; ++g) {
-            if (!live<P, kG, kNV>(g, t, D)) continue;
+        // h of vector g -> its norm: k1, u, and the gate beside it
+        auto norm_h = [&](int g) {
             float p[8];
+            in.read(row, 1, g, k1[g]);
             if (a.post) {
                 param_load<P, kG>(a.w_post, 0, g, t, D, 1.0f, p);
 #pragma unroll
@@ -465,24 +459,40 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
                 for (int i = 0; i < 8; ++i) u[g][i] = k1[g][i];
             }
             param_load<P, kG>(a.gate, gate_i * D, g, t, D, 1.0f, p);
+            if (full<P, kG>(g, t, D)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                gt[g][i] = a.scale_h * p[i];
-                k2[g][i] = a.scale_x * k2[g][i] + gt[g][i] * u[g][i];   // r
+                for (int i = 0; i < 8; ++i) gt[g][i] = a.scale_h * p[i];
+            } else {   // 0 past the end: what is multiplied by it stays out of the row's sums
+#pragma unroll
+                for (int i = 0; i < 8; ++i) gt[g][i] = column<P, kG>(g, i, t) < D ? a.scale_h * p[i] : 0.0f;
             }
+        };
+#pragma unroll
+        for (int g = 0; g < kNV; ++g) {
+            in.read(row, 0, g, k2[g]);
+            in.read(row, 2, g, e[g]);
+            in.read(row, 3, g, d[g]);
+            if (!live<P, kG, kNV>(g, t, D)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) k1[g][i] = u[g][i] = gt[g][i] = 0.0f;
+                continue;
+            }
+            norm_h(g);
+            float p[8];
             param_load<P, kG>(a.w_pre, 0, g, t, D, 1.0f, p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                k2[g][i] = a.scale_x * k2[g][i] + gt[g][i] * u[g][i];   // r
                 k2[g][i] = (kLayer ? k2[g][i] - st.z : k2[g][i]) * st.w;
                 dw2[g][i] += e[g][i] * k2[g][i];
                 if (kLayer) db2[g][i] += e[g][i];
-                e[g][i] *= p[i];
-                if (inside<P, kG>(g, i, t, D)) {   // columns past the end hold no element
-                    if (kLayer) s_e += e[g][i];
-                    s_ek += e[g][i] * k2[g][i];
-                }
+                e[g][i] *= p[i];   // (0 past the end, as dy is)
+                if (kLayer) s_e += e[g][i];
+                s_ek += e[g][i] * k2[g][i];
             }
         }
+        // One vector a thread keeps the norm of h in registers; several form it again from the row in shared memory.
+        if (kNV == 1) in.advance(row + a.depth, last);
         if (a.dy != nullptr) {
             float mean_e = 0.0f, mean_ek;
             if (kLayer) {
@@ -501,6 +511,7 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
 #pragma unroll
         for (int g = 0; g < kNV; ++g) {
             if (!live<P, kG, kNV>(g, t, D)) continue;
+            if (kNV > 1) norm_h(g);
             float out[8], w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) out[i] = a.scale_x * d[g][i];
@@ -517,13 +528,12 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
                     dw1[g][i] += e[g][i] * k1[g][i];
                     if (kLayer) db1[g][i] += e[g][i];
                     e[g][i] *= w[i];
-                    if (inside<P, kG>(g, i, t, D)) {
-                        if (kLayer) s_e += e[g][i];
-                        s_ek += e[g][i] * k1[g][i];
-                    }
+                    if (kLayer) s_e += e[g][i];
+                    s_ek += e[g][i] * k1[g][i];
                 }
             }
         }
+        if (kNV > 1) in.advance(row + a.depth, last);
         if (a.post) {
             float mean_e = 0.0f, mean_ek;
             if (kLayer) {
@@ -573,8 +583,8 @@ __global__ void __launch_bounds__(kBlock<kG>, kBlock<kG> <= 512 ? 512 / kBlock<k
 }
 
 // Second kernel of the backward pass: column sums over the blocks' partial sums, and the gate rows that several groups share.
-// blockIdx.y: which array, then which gate row (or, where there are fewer of them, which border between two groups: a shared gate
-// row belongs to the first border inside it); 32 columns a block, eight threads a column with eight loads in flight each, added in a fixed order.
+// blockIdx.y: which array, then which gate row -- or, where there are fewer of them, which eight borders between two groups, one for
+// each warp (a shared gate row belongs to the first border inside it, and then reaches over few groups); 32 columns a block, eight threads a column with eight loads in flight each, added in a fixed order.
 // Launched behind the first kernel's end (its blocks are resident by then).
 struct FinishArgs {
     int D;
@@ -587,7 +597,7 @@ struct FinishArgs {
     const float* part_gate;
     void* dgate;
     int gate_type, by_border;
-    int64_t M, rows_per_gate, rows_each;
+    int64_t M, rows_per_gate, rows_each, parts;
 };
 
 __global__ void __launch_bounds__(256) resnorm_finish_kernel(const __grid_constant__ FinishArgs f) {
@@ -603,16 +613,27 @@ __global__ void __launch_bounds__(256) resnorm_finish_kernel(const __grid_consta
 #pragma unroll 8
             for (int b = y; b < f.blocks; b += 8) s += p[(int64_t)b * f.D + c];
     } else {
-        const int64_t border = f.by_border ? gate + 1 : 0;
-        if (f.by_border) gate = border * f.rows_each / f.rows_per_gate;
+        const int64_t border = f.by_border ? gate * 8 + y + 1 : 0;
+        if (f.by_border) {
+            if (border >= f.parts) return;
+            gate = border * f.rows_each / f.rows_per_gate;
+        }
         const int64_t g0 = gate * f.rows_per_gate, g1 = min(g0 + f.rows_per_gate, f.M);
         const int64_t p0 = g0 / f.rows_each, p1 = (g1 - 1) / f.rows_each;
         if (p0 == p1 || (f.by_border && (g0 == border * f.rows_each || p0 != border - 1))) return;   // one group's alone, or another border's
         // only a part's first gate row can have begun before it, so of parts p0 + 1 ... it is slot 0; of part p0 it is slot 0 where
         // that part begins with it
+        const float* p = f.part_gate + c;
+        const int64_t at0 = (p0 * 2 + (gate == p0 * f.rows_each / f.rows_per_gate ? 0 : 1)) * f.D;
+        if (f.by_border) {
+            if (c >= f.D) return;
+            s = p[at0];
+            for (int64_t i = p0 + 1; i <= p1; ++i) s += p[i * 2 * f.D];
+            param_store(f.dgate, f.gate_type, gate * f.D + c, s);
+            return;
+        }
         if (c < f.D) {
-            const float* p = f.part_gate + c;
-            if (y == 0) s = p[(p0 * 2 + (gate == p0 * f.rows_each / f.rows_per_gate ? 0 : 1)) * f.D];
+            if (y == 0) s = p[at0];
 #pragma unroll 8
             for (int64_t i = p0 + 1 + y; i <= p1; i += 8) s += p[i * 2 * f.D];
         }
@@ -876,13 +897,13 @@ extern "C" lbt_status lbt_resnorm_backward(const lbt_resnorm_desc* d, const void
     const float* parts[4] = {a.part_w_post, a.part_b_post, a.part_w_pre, a.part_b_pre};
     for (int i = 0; i < 4; ++i)
         if (outs[i] != nullptr) { f.part[f.arrays] = parts[i]; f.out[f.arrays++] = outs[i]; }
-    int64_t shared = 0;   // gate rows that may lie in several groups: all of them, or at most one for each border
+    int64_t shared = 0;   // blocks for the gate rows that may lie in several groups: all of them, or at most one for each border
     if (dgate != nullptr) {
         const int64_t gates = (a.M + a.rows_per_gate - 1) / a.rows_per_gate;
-        shared = std::min(gates, s.parts - 1);
         f.by_border = gates > s.parts - 1;
+        shared = f.by_border ? (s.parts - 1 + 7) / 8 : gates;
         f.part_gate = a.part_gate; f.dgate = dgate; f.gate_type = d->param_type;
-        f.M = a.M; f.rows_per_gate = a.rows_per_gate; f.rows_each = a.rows_each;
+        f.M = a.M; f.rows_per_gate = a.rows_per_gate; f.rows_each = a.rows_each; f.parts = s.parts;
     }
     if (f.arrays + shared == 0) return LBT_OK;
     cudaLaunchAttribute attr[1];
