@@ -790,17 +790,22 @@ grad8_stats_kernel(const T* __restrict__ dY, int64_t M, int64_t O, int64_t ld, b
     for (int i = 0; i < 8; ++i) { w[i] = c + i < O ? s_w[c + i] : 0.0f; total[i] = cm[i] = 0.0f; }
     const float sx_all = lane < rows ? s_x[m0 + 8 * lane] : 0.0f;
     const T* row = dY + m0 * ld;
-#pragma unroll 2
-    for (int k = 0; k < rows; ++k, row += 8 * ld) {
+    // all rows' loads of an aligned strip are on their way before the first is looked at
+    Vec8<T> raw[kStripRows];
+    if (kEven) {
+#pragma unroll
+        for (int k = 0; k < kStripRows; ++k) {
+            raw[k] = Vec8<T>{};
+            if (live && k < rows) ld_vec(row + k * 8 * ld + c, raw[k].w);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kStripRows; ++k) {
+        if (k >= rows) break;   // uniform over the warp
         const float sx = __shfl_sync(0xFFFFFFFFu, sx_all, k);
         float f[8], rm = 0.0f;
-        if (kEven) {
-            Vec8<T> r{};
-            if (live) ld_vec(row + c, r.w);
-            unpack(r, f);
-        } else {
-            load_group(row, c, O, vec, f);
-        }
+        if (kEven) unpack(raw[k], f);
+        else load_group(row + k * 8 * ld, c, O, vec, f);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             rm = most3(rm, __fmul_rn(f[i], w[i]), __fmul_rn(f[i + 1], w[i + 1]));
@@ -877,34 +882,42 @@ grad8_codes_kernel(const T* __restrict__ dY, int64_t M, int64_t O, int64_t ld, b
     }
     const T* row = dY + m0 * ld;
     uint8_t *to_r = q_r != nullptr ? q_r + m0 * ldq + c : nullptr, *to_c = q_c != nullptr ? q_c + m0 * ldq + c : nullptr;
-#pragma unroll 2
-    for (int k = 0; k < rows; ++k, row += 8 * ld) {
-        const float sx = __shfl_sync(0xFFFFFFFFu, sx_all, k), fr = __shfl_sync(0xFFFFFFFFu, fr_all, k);
-        float f[8];
+    constexpr int kBatch = 4;   // rows whose loads are on their way together
+    for (int k0 = 0; k0 < rows; k0 += kBatch) {
+        Vec8<T> raw[kBatch];
         if (kEven) {
-            Vec8<T> r{};
-            if (c < O) ld_vec(row + c, r.w);
-            unpack(r, f);
-        } else {
-            load_group(row, c, O, vec, f);
-        }
-        uint32_t q[8], p[8];
-        if (fr != 0.0f && !dead) {   // uniform over the warp
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                q[i] = code8_live(__fmul_rn(f[i], w[i]), fr);
-                p[i] = code8_live(__fmul_rn(f[i], sx), fc[i]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                q[i] = code8(__fmul_rn(f[i], w[i]), fr);
-                p[i] = code8(__fmul_rn(f[i], sx), fc[i]);
+            for (int k = 0; k < kBatch; ++k) {
+                raw[k] = Vec8<T>{};
+                if (c < O && k0 + k < rows) ld_vec(row + (k0 + k) * 8 * ld + c, raw[k].w);
             }
         }
-        if (c < ldq) {
-            if (to_r != nullptr) *reinterpret_cast<uint2*>(to_r + k * 8 * ldq) = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
-            if (to_c != nullptr) *reinterpret_cast<uint2*>(to_c + k * 8 * ldq) = make_uint2(pack4(p[0], p[1], p[2], p[3]), pack4(p[4], p[5], p[6], p[7]));
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int k = k0 + b;
+            if (k >= rows) break;   // uniform over the warp
+            const float sx = __shfl_sync(0xFFFFFFFFu, sx_all, k), fr = __shfl_sync(0xFFFFFFFFu, fr_all, k);
+            float f[8];
+            if (kEven) unpack(raw[b], f);
+            else load_group(row + k * 8 * ld, c, O, vec, f);
+            uint32_t q[8], p[8];
+            if (fr != 0.0f && !dead) {   // uniform over the warp
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    q[i] = code8_live(__fmul_rn(f[i], w[i]), fr);
+                    p[i] = code8_live(__fmul_rn(f[i], sx), fc[i]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    q[i] = code8(__fmul_rn(f[i], w[i]), fr);
+                    p[i] = code8(__fmul_rn(f[i], sx), fc[i]);
+                }
+            }
+            if (c < ldq) {
+                if (to_r != nullptr) *reinterpret_cast<uint2*>(to_r + k * 8 * ldq) = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+                if (to_c != nullptr) *reinterpret_cast<uint2*>(to_c + k * 8 * ldq) = make_uint2(pack4(p[0], p[1], p[2], p[3]), pack4(p[4], p[5], p[6], p[7]));
+            }
         }
     }
 }
