@@ -8,10 +8,11 @@
 //   d = dr + N_pre'(dy),  dx = scale_x d,  du = scale_h gate d,  dh = N_post'(du),
 //   N'(g) = rstd (e - [mean e] - k mean(e k)),  e = g w   (the bracket for the layer norm)
 //   dw = sum_rows g k,  db = sum_rows g,  dgate = sum over the gate's rows of scale_h u d.
-// Everything is bound by memory: two reads and two writes an element forward, four and two backward.
+// Memory is the floor: two reads and two writes an element forward, four and two backward.  Next to it stands instruction issue, which
+// bounds both passes now (8192 x 4096 bf16: forward 55-59 us = 4.6-4.9 TB/s, backward 127 us = 3.2 TB/s).
 //
-// One group of threads (a warp up to 512 columns, a block above) owns a row, eight columns of it per thread and vector, so a row's
-// sums are the group's reduction and nothing is read twice.  A group works through several rows: each thread copies its own columns
+// One group of threads (a warp up to 1024 columns forward and 512 backward, a block above) owns a row, eight columns of it per
+// thread and vector, so a row's sums are the group's reduction and nothing is read twice.  A group works through several rows: each thread copies its own columns
 // of the rows to come into its own slots of shared memory (cp.async, up to three rows ahead), so the reductions of one row run
 // under the loads of the next ones and no thread waits for another's copies.  Sums over rows: a group owns consecutive rows and
 // keeps its columns' sums in registers; a second kernel adds the groups' sums in a fixed order (no atomics: a run repeats bit for bit).
