@@ -463,6 +463,13 @@ typedef struct lbt_adamw_hyper {
 } lbt_adamw_hyper;      /* 40 bytes */
 lbt_status lbt_adamw_step(const lbt_adamw_tensor *tensors, int count, const lbt_adamw_hyper *h, const float *d_grad_scale,
                           const int32_t *d_skip, void *cuda_stream);
+/*
+ * The same with the held-back steps counted on the device, where alone they are known.  d_skipped (device int64, 8-byte aligned,
+ * 0 before the first step; NULL: lbt_adamw_step): a call that *d_skip holds back adds 1 to it and changes nothing else, and a
+ * call that is taken corrects with h->step - *d_skipped in place of h->step.  So h->step counts the calls, whatever became of them.
+ */
+lbt_status lbt_adamw_step_ex(const lbt_adamw_tensor *tensors, int count, const lbt_adamw_hyper *h, const float *d_grad_scale,
+                             const int32_t *d_skip, int64_t *d_skipped, void *cuda_stream);
 
 /*
  * Measurement taps (no counterpart in the paper).  After this call the library records the two

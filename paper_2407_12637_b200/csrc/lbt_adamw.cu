@@ -39,7 +39,7 @@ struct AdamEntry {
     float* m_scale;
     float* v_scale;
     uint64_t n;
-    float step_size;   // lr / (1 - b1^t)
+    double step_size;  // lr / (1 - b1^t), t the host's step
     float decay;       // 1 - lr wd
     int types;         // p type | g type << 4 | aligned << 8
 };
@@ -53,7 +53,20 @@ struct AdamTable {
     float b1, omb1, b2, omb2, inv_c2, eps;
     const float* grad_scale;
     const int32_t* skip;
+    int64_t* skipped;           // steps held back so far (null: none), added to by this launch if `counts`
+    int counts;
+    int64_t step;               // the host's step: t = step - *skipped
+    double beta1, beta2, c1;    // c1 = 1 - b1^step
 };
+static_assert(sizeof(AdamTable<kAdamMax>) <= 32764, "the table is a kernel argument");
+
+// b^t by squaring (t >= 1): a rounding for each of its at most 2 log2 t products, in 64 bits
+__device__ __forceinline__ double adam_power(double b, int64_t t) {
+    double r = 1.0;
+    for (; t > 0; t >>= 1, b *= b)
+        if (t & 1) r *= b;
+    return r;
+}
 
 __device__ __forceinline__ float adam_load(const void* p, int type, uint64_t i) {
     if (type == LBT_F32) return static_cast<const float*>(p)[i];
@@ -79,6 +92,7 @@ __device__ __forceinline__ float2 e4m3_values(uint32_t pair) {
 
 struct AdamConst {
     float b1, omb1, b2, omb2, inv_c2, eps, gs;
+    float step_size;   // of the tensor at work
 };
 
 // sqrt(v) by Markstein's correction (Computation of Elementary Functions on the IBM RISC System/6000, 1990): s = v y with y a
@@ -93,14 +107,14 @@ __device__ __forceinline__ float adam_root(float v) {
 }
 
 // one element; returns u = sqrt(v)
-__device__ __forceinline__ float adam_update(const AdamConst& c, float step_size, float decay, float g, float& p, float& m, float& v) {
+__device__ __forceinline__ float adam_update(const AdamConst& c, float decay, float g, float& p, float& m, float& v) {
     g = __fmul_rn(g, c.gs);
     m = __fadd_rn(__fmul_rn(c.b1, m), __fmul_rn(c.omb1, g));
     v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.omb2, __fmul_rn(g, g)));
     const float u = adam_root(v);
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__fadd_rn(__fmul_rn(u, c.inv_c2), c.eps)));
-    p = __fsub_rn(__fmul_rn(decay, p), __fmul_rn(__fmul_rn(step_size, m), inv));
+    p = __fsub_rn(__fmul_rn(decay, p), __fmul_rn(__fmul_rn(c.step_size, m), inv));
     return u;
 }
 
@@ -217,7 +231,7 @@ __device__ __forceinline__ void adam_whole(const AdamEntry& e, const AdamConst& 
         for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = adam_update(c, e.step_size, e.decay, g[i], p[i], m[i], v[i]);
+    for (int i = 0; i < 8; ++i) u[i] = adam_update(c, e.decay, g[i], p[i], m[i], v[i]);
     if (kTail && have < 8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -305,7 +319,7 @@ __device__ __forceinline__ void adam_ragged(const AdamEntry& e, const AdamConst&
                 v[i] = __fmul_rn(e4m3_values(static_cast<const uint8_t*>(e.v)[k]).x, vs);
                 v[i] = __fmul_rn(v[i], v[i]);
             }
-            u[i] = adam_update(c, e.step_size, e.decay, g, p[i], m[i], v[i]);
+            u[i] = adam_update(c, e.decay, g, p[i], m[i], v[i]);
             adam_store(e.p, p_type, k, p[i]);
             if (kBits == 32) {
                 static_cast<float*>(e.m)[k] = m[i];
@@ -337,11 +351,22 @@ __device__ __forceinline__ void adam_run_g(const AdamEntry& e, const AdamConst& 
 template <int kBits, int kCap>
 __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ AdamTable<kCap> t) {
     __shared__ uint32_t first[kCap + 1];
-    if (t.skip != nullptr && *t.skip != 0) return;
+    __shared__ double correct;   // what the host's step sizes are multiplied by
+    __shared__ float inv_c2;
+    if (t.skip != nullptr && *t.skip != 0) {
+        if (t.counts && blockIdx.x == 0 && threadIdx.x == 0) *t.skipped += 1;   // (nobody reads it in a launch that is held back)
+        return;
+    }
     for (int i = threadIdx.x; i <= t.count; i += kAdamThreads) first[i] = t.first[i];
+    if (threadIdx.x == 0) {
+        // The corrections are the host's, for its own step; once steps have been held back they are formed here for the smaller t.
+        const int64_t missed = t.skipped != nullptr ? *t.skipped : 0, step = max(t.step - missed, (int64_t)1);
+        correct = missed == 0 ? 1.0 : t.c1 / (1.0 - adam_power(t.beta1, step));
+        inv_c2 = missed == 0 ? t.inv_c2 : 1.0f / (float)sqrt(1.0 - adam_power(t.beta2, step));
+    }
     __syncthreads();
     const int lane = threadIdx.x & 31;
-    const AdamConst c{t.b1, t.omb1, t.b2, t.omb2, t.inv_c2, t.eps, t.grad_scale != nullptr ? *t.grad_scale : 1.0f};
+    AdamConst c{t.b1, t.omb1, t.b2, t.omb2, inv_c2, t.eps, t.grad_scale != nullptr ? *t.grad_scale : 1.0f, 0.0f};
     const uint32_t all = first[t.count];
     const uint64_t stride = (uint64_t)gridDim.x * (kAdamThreads / 32);
     for (uint64_t r = (uint64_t)blockIdx.x * (kAdamThreads / 32) + (threadIdx.x >> 5); r < all; r += stride) {
@@ -351,6 +376,7 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_con
             if (first[mid] <= r) lo = mid; else hi = mid;
         }
         const AdamEntry& e = t.e[lo];
+        c.step_size = (float)(e.step_size * correct);
         const uint64_t b = (r - first[lo]) * t.run, end = min(b + t.run, (e.n + kAdamBlock - 1) / kAdamBlock);
         if ((e.types >> 8) != 0) {
             const int p_type = e.types & 15;
@@ -375,7 +401,7 @@ static lbt_status adamw_launch(const AdamTable<kCap>& t, cudaStream_t stream) {
 
 template <int kCap>
 static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lbt_adamw_hyper* h, const float* grad_scale,
-                            const int32_t* skip, cudaStream_t stream) {
+                            const int32_t* skip, int64_t* skipped, bool* counted, cudaStream_t stream) {
     AdamTable<kCap> t{};
     const double c1 = 1.0 - pow(h->beta1, (double)h->step), c2 = sqrt(1.0 - pow(h->beta2, (double)h->step));
     t.b1 = (float)h->beta1; t.omb1 = (float)(1.0 - h->beta1);
@@ -384,6 +410,9 @@ static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lb
     t.eps = (float)h->eps;
     t.grad_scale = grad_scale;
     t.skip = skip;
+    t.skipped = skipped;
+    t.step = h->step;
+    t.beta1 = h->beta1; t.beta2 = h->beta2; t.c1 = c1;
     t.count = count;
     uint64_t blocks = 0, at = 0;
     for (int i = 0; i < count; ++i) blocks += (tensors[i].n + kAdamBlock - 1) / kAdamBlock;
@@ -394,7 +423,7 @@ static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lb
         const lbt_adamw_tensor& s = tensors[i];
         AdamEntry& e = t.e[i];
         e.p = s.p; e.g = s.g; e.m = s.m; e.v = s.v; e.m_scale = s.m_scale; e.v_scale = s.v_scale; e.n = s.n;
-        e.step_size = (float)(s.lr / c1);
+        e.step_size = s.lr / c1;
         e.decay = (float)(1.0 - s.lr * s.weight_decay);
         // eight elements in one access: 32 bytes of fp32, 16 of a 16-bit type, 8 of codes
         auto ok = [](const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; };
@@ -405,6 +434,9 @@ static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lb
         at += ((s.n + kAdamBlock - 1) / kAdamBlock + t.run - 1) / t.run;
     }
     t.first[count] = (uint32_t)at;
+    // a step that is held back is counted once, by its first launch (the others only return)
+    t.counts = skipped != nullptr && skip != nullptr && at > 0 && !*counted;
+    *counted |= at > 0;
     return h->state_bits == 8 ? adamw_launch<8, kCap>(t, stream) : adamw_launch<32, kCap>(t, stream);
 }
 
@@ -412,11 +444,12 @@ static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lb
 
 using namespace lbt;
 
-extern "C" lbt_status lbt_adamw_step(const lbt_adamw_tensor* tensors, int count, const lbt_adamw_hyper* h,
-                                     const float* d_grad_scale, const int32_t* d_skip, void* cuda_stream) {
+extern "C" lbt_status lbt_adamw_step_ex(const lbt_adamw_tensor* tensors, int count, const lbt_adamw_hyper* h,
+                                        const float* d_grad_scale, const int32_t* d_skip, int64_t* d_skipped, void* cuda_stream) {
     if (count < 0 || (count > 0 && tensors == nullptr) || h == nullptr || h->step < 1) return LBT_ERR_INVALID_ARG;
     if (!(h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0 && h->eps >= 0.0)) return LBT_ERR_INVALID_ARG;
     if (h->state_bits != 8 && h->state_bits != 32) return LBT_ERR_UNSUPPORTED_BITS;
+    if ((reinterpret_cast<uintptr_t>(d_skipped) & 7) != 0) return LBT_ERR_ALIGNMENT;
     uint64_t blocks = 0;
     for (int i = 0; i < count; ++i) {
         const lbt_adamw_tensor& s = tensors[i];
@@ -434,12 +467,18 @@ extern "C" lbt_status lbt_adamw_step(const lbt_adamw_tensor* tensors, int count,
     }
     if (blocks > 0xFFFFFFFFull) return LBT_ERR_UNSUPPORTED;
     const cudaStream_t stream = as_stream(cuda_stream);
+    bool counted = false;
     for (int i = 0; i < count; i += kAdamMax) {
         const int n = std::min(count - i, kAdamMax);
-        const lbt_status rc = n <= kAdamFew    ? adamw_run<kAdamFew>(tensors + i, n, h, d_grad_scale, d_skip, stream)
-                              : n <= kAdamSome ? adamw_run<kAdamSome>(tensors + i, n, h, d_grad_scale, d_skip, stream)
-                                               : adamw_run<kAdamMax>(tensors + i, n, h, d_grad_scale, d_skip, stream);
+        const lbt_status rc = n <= kAdamFew    ? adamw_run<kAdamFew>(tensors + i, n, h, d_grad_scale, d_skip, d_skipped, &counted, stream)
+                              : n <= kAdamSome ? adamw_run<kAdamSome>(tensors + i, n, h, d_grad_scale, d_skip, d_skipped, &counted, stream)
+                                               : adamw_run<kAdamMax>(tensors + i, n, h, d_grad_scale, d_skip, d_skipped, &counted, stream);
         if (rc != LBT_OK) return rc;
     }
     return LBT_OK;
+}
+
+extern "C" lbt_status lbt_adamw_step(const lbt_adamw_tensor* tensors, int count, const lbt_adamw_hyper* h,
+                                     const float* d_grad_scale, const int32_t* d_skip, void* cuda_stream) {
+    return lbt_adamw_step_ex(tensors, count, h, d_grad_scale, d_skip, nullptr, cuda_stream);
 }

@@ -32,6 +32,7 @@ EXPORTS = (
     "lbt_grad_diagnostics", "lbt_diagnostics_workspace_bytes",
     "lbt_rows8_quantize", "lbt_linear8_forward", "lbt_linear8_matmul", "lbt_linear8_backward", "lbt_linear8_workspace_bytes",
     "lbt_resnorm_forward", "lbt_resnorm_backward", "lbt_resnorm_workspace_bytes", "lbt_adamw_step",
+    "lbt_adamw_step_ex",
     "lbt_set_timing_events", "lbt_selftest_wait_timeout", "lbt_selftest_barrier_timeout", "lbt_status_string",
 )
 TIME_STATS, TIME_QUANTIZE, TIME_EXPAND, TIME_DGRAD, TIME_WGRAD, TIME_FORWARD, TIME_FWD_QUANT = range(7)
@@ -152,6 +153,7 @@ def lib() -> C.CDLL:
         l.lbt_resnorm_backward.argtypes = [vp] * 18 + [sz, vp]
         l.lbt_resnorm_workspace_bytes.argtypes = [vp]
         l.lbt_adamw_step.argtypes = [vp, i32, vp, vp, vp, vp]
+        l.lbt_adamw_step_ex.argtypes = [vp, i32, vp, vp, vp, vp, vp]
         l.lbt_set_timing_events.argtypes = [i32, vp, vp]
         l.lbt_selftest_wait_timeout.argtypes = [vp, C.c_uint32, vp]
         l.lbt_selftest_barrier_timeout.argtypes = [vp, C.c_uint32, vp]
@@ -441,10 +443,11 @@ def resnorm_backward(desc, dr, dy, x, h, gate, w_post, b_post, w_pre, stats, dx,
                                       _raw_stream(x, stream)), "lbt_resnorm_backward")
 
 
-def adamw_step(table, hyper, grad_scale=None, skip=None, stream=None):
-    """One AdamW step over a ctypes array of AdamwTensor; stream: a torch stream or a raw one (None: the current stream)."""
+def adamw_step(table, hyper, grad_scale=None, skip=None, stream=None, skipped=None):
+    """One AdamW step over a ctypes array of AdamwTensor; stream: a torch stream or a raw one (None: the current stream).
+    skipped: device int64 that counts the steps held back by `skip` (None: hyper.step counts the steps that were taken)."""
     raw = stream if isinstance(stream, int) else _stream(stream)
-    _check(lib().lbt_adamw_step(table, len(table), C.addressof(hyper), _p(grad_scale), _p(skip), raw), "lbt_adamw_step")
+    _check(lib().lbt_adamw_step_ex(table, len(table), C.addressof(hyper), _p(grad_scale), _p(skip), _p(skipped), raw), "lbt_adamw_step")
 
 
 def grad_diagnostics(dY, q_codes, bits, alpha, stats, ws=None, stream=None) -> "GradDiag":

@@ -292,7 +292,9 @@ class AdamW:
             e = self.table[i]
             e.p, e.g, e.m, e.v, e.m_scale, e.v_scale = (lbt._p(t) for t in (p, g, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i]))
             e.n, e.lr, e.weight_decay, e.p_type, e.g_type = p.numel(), lrs[i], wds[i], lbt.TYPES[p.dtype], lbt.TYPES[g.dtype]
-        self.hyper = lbt.AdamwHyper(betas[0], betas[1], eps, step, state_bits, 0)
+        self.hyper = lbt.AdamwHyper(betas[0], betas[1], eps, step, state_bits, 0)   # (its step counts the calls)
+        # calls that were held back, counted once there may be some (a launch that need not look starts 0.5 us earlier)
+        self.skipped, self._counting = torch.zeros(1, dtype=torch.int64, device=self.params[0].device) if n else None, False
 
     def set_lr(self, lr):
         """One learning rate for all tensors, or one for each."""
@@ -300,10 +302,17 @@ class AdamW:
             e.lr = x
 
     def step(self, grad_scale=None, skip=None, stream=None):
-        """One step.  grad_scale: device float the gradients are multiplied by; skip: device int32, non-zero = leave everything."""
+        """One step.  grad_scale: device float the gradients are multiplied by; skip: device int32, non-zero = leave everything (the
+        step then counts for nothing: the next one corrects as this one would have)."""
         self.hyper.step += 1
+        if skip is not None:
+            self._counting = True
         raw = lbt._raw_stream(self.params[0], stream) if self.params else stream
-        lbt.adamw_step(self.table, self.hyper, grad_scale, skip, raw)
+        lbt.adamw_step(self.table, self.hyper, grad_scale, skip, raw, self.skipped if self._counting else None)
+
+    def taken(self) -> int:
+        """Steps taken so far, as `step` of a resumed optimizer (waits for the device)."""
+        return self.hyper.step - (int(self.skipped) if self.params else 0)
 
     def moments(self):
         """The moments (m, v) as fp32 values, one tensor for each parameter (a checkpoint reader's view)."""

@@ -195,3 +195,26 @@ def test_refusals():
         with pytest.raises(lbt.LbtError) as e:
             lm.AdamW([p], [g], betas=betas, eps=eps).step()
         assert e.value.status == lbt.ERR_INVALID_ARG
+
+
+def _state_bits(opt):
+    """Everything a step writes, as bytes."""
+    parts = opt.params + opt.m + opt.v + [s for s in opt.m_scale + opt.v_scale if s is not None]
+    return [t.view(torch.uint8) for t in parts]
+
+
+@pytest.mark.parametrize("count", [1, 41, 401])   # (401: two launches a step)
+@pytest.mark.parametrize("bits", [8, 32])
+def test_skipped_steps_do_not_count(bits, count):
+    """Steps that were held back leave the bias corrections where they were: what follows is bit for bit an optimizer that never saw them."""
+    ps, gs = _tensors([(37 * i) % 600 + 1 for i in range(count)], torch.float32, torch.float32, 7, Guard())
+    held, taken = lm.AdamW(ps, gs, lr=1e-2, state_bits=bits), lm.AdamW([p.clone() for p in ps], gs, lr=1e-2, state_bits=bits)
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for skipped in (1, 1, 0, 1, 0, 0, 1, 1, 1, 0):
+        for g in gs:
+            g.mul_(0.9).add_(0.001)
+        flag.fill_(skipped)
+        held.step(skip=flag)
+        if not skipped:
+            taken.step()
+        assert all(torch.equal(a, b) for a, b in zip(_state_bits(held), _state_bits(taken)))
