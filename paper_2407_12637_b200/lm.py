@@ -307,8 +307,12 @@ class AdamW:
         self.hyper.step += 1
         if skip is not None:
             self._counting = True
-        raw = lbt._raw_stream(self.params[0], stream) if self.params else stream
-        lbt.adamw_step(self.table, self.hyper, grad_scale, skip, raw, self.skipped if self._counting else None)
+        try:
+            raw = lbt._raw_stream(self.params[0], stream) if self.params else stream
+            lbt.adamw_step(self.table, self.hyper, grad_scale, skip, raw, self.skipped if self._counting else None)
+        except Exception:   # refused: nothing was enqueued
+            self.hyper.step -= 1
+            raise
 
     def taken(self) -> int:
         """Steps taken so far, as `step` of a resumed optimizer (waits for the device)."""

@@ -7,7 +7,7 @@ import ctypes as C
 import pytest
 
 from paper_2407_12637_b200 import build as lib_build
-from paper_2407_12637_b200 import lbt
+from paper_2407_12637_b200 import lbt, lm
 
 A = 1 << 20   # an aligned address
 
@@ -127,3 +127,14 @@ def test_adamw(change, want):
     assert lbt.lib().lbt_adamw_step(t, 1, C.addressof(h), None, None, None) == want
     assert lbt.lib().lbt_adamw_step(None, 1, C.addressof(h), None, None, None) == lbt.ERR_INVALID_ARG
     assert lbt.lib().lbt_adamw_step(t, 0, None, None, None, None) == lbt.ERR_INVALID_ARG
+
+
+def test_a_refused_step_does_not_count():
+    bad = lm.AdamW([], [], betas=(1.0, 0.9), step=3)
+    for _ in range(2):
+        with pytest.raises(lbt.LbtError):
+            bad.step(stream=0)
+    assert bad.hyper.step == bad.taken() == 3
+    good = lm.AdamW([], [], step=3)   # (no tensors: nothing is launched)
+    good.step(stream=0)
+    assert good.hyper.step == good.taken() == 4
