@@ -466,7 +466,8 @@ lbt_status lbt_adamw_step(const lbt_adamw_tensor *tensors, int count, const lbt_
 /*
  * The same with the held-back steps counted on the device, where alone they are known.  d_skipped (device int64, 8-byte aligned,
  * 0 before the first step; NULL: lbt_adamw_step): a call that *d_skip holds back adds 1 to it and changes nothing else, and a
- * call that is taken corrects with h->step - *d_skipped in place of h->step.  So h->step counts the calls, whatever became of them.
+ * call that is taken corrects with h->step - *d_skipped in place of h->step.  So h->step counts the calls, whatever became of them
+ * (a call in a captured graph keeps the h->step of its capture: taking 1 from *d_skipped behind it makes each replay the next step).
  */
 lbt_status lbt_adamw_step_ex(const lbt_adamw_tensor *tensors, int count, const lbt_adamw_hyper *h, const float *d_grad_scale,
                              const int32_t *d_skip, int64_t *d_skipped, void *cuda_stream);

@@ -295,6 +295,7 @@ class AdamW:
         self.hyper = lbt.AdamwHyper(betas[0], betas[1], eps, step, state_bits, 0)   # (its step counts the calls)
         # calls that were held back, counted once there may be some (a launch that need not look starts 0.5 us earlier)
         self.skipped, self._counting = torch.zeros(1, dtype=torch.int64, device=self.params[0].device) if n else None, False
+        self._replayed = False   # whether a step is in a captured graph
 
     def set_lr(self, lr):
         """One learning rate for all tensors, or one for each."""
@@ -304,15 +305,23 @@ class AdamW:
     def step(self, grad_scale=None, skip=None, stream=None):
         """One step.  grad_scale: device float the gradients are multiplied by; skip: device int32, non-zero = leave everything (the
         step then counts for nothing: the next one corrects as this one would have)."""
-        self.hyper.step += 1
-        if skip is not None:
+        if stream is not None and self.params:
+            with torch.cuda.stream(stream):
+                return self.step(grad_scale, skip)
+        if not self._replayed and self.params and torch.cuda.is_current_stream_capturing():
+            self._replayed = True
+        if skip is not None or self._replayed:
             self._counting = True
+        self.hyper.step += 1
         try:
-            raw = lbt._raw_stream(self.params[0], stream) if self.params else stream
+            raw = lbt._raw_stream(self.params[0]) if self.params else stream
             lbt.adamw_step(self.table, self.hyper, grad_scale, skip, raw, self.skipped if self._counting else None)
         except Exception:   # refused: nothing was enqueued
             self.hyper.step -= 1
             raise
+        if self._replayed:   # a graph holds this call's step: from the first capture on the host's count rests and the device's runs
+            self.hyper.step -= 1
+            self.skipped.sub_(1)
 
     def taken(self) -> int:
         """Steps taken so far, as `step` of a resumed optimizer (waits for the device)."""

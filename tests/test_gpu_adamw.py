@@ -218,3 +218,30 @@ def test_skipped_steps_do_not_count(bits, count):
         if not skipped:
             taken.step()
         assert all(torch.equal(a, b) for a, b in zip(_state_bits(held), _state_bits(taken)))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_captured_step_counts_its_replays(bits):
+    """Replays of a captured step, steps outside of the graph and held-back ones in any order: the bits of the same steps taken one by one."""
+    ps, gs = _tensors([700, 33], torch.float32, torch.float32, 9, Guard())
+    graphed, plain = lm.AdamW(ps, gs, lr=1e-2, state_bits=bits), lm.AdamW([p.clone() for p in ps], gs, lr=1e-2, state_bits=bits)
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    graphed.step(skip=flag)
+    plain.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.step(skip=flag)
+    taken = 1
+    for replay, skipped in ((1, 0), (1, 0), (0, 0), (1, 1), (1, 0), (0, 1), (0, 0), (1, 0)):
+        for g in gs:
+            g.mul_(0.9).add_(0.001)
+        flag.fill_(skipped)
+        if replay:
+            graph.replay()
+        else:
+            graphed.step(skip=flag)
+        if not skipped:
+            plain.step()
+            taken += 1
+        assert all(torch.equal(a, b) for a, b in zip(_state_bits(graphed), _state_bits(plain)))
+        assert graphed.taken() == plain.taken() == taken
