@@ -443,7 +443,8 @@ lbt_status lbt_resnorm_backward(const lbt_resnorm_desc *d, const void *dr, const
  * state_bits 32: m, v fp32.  state_bits 8: m and the root of v as e4m3 codes, one byte an element, in blocks of 256 consecutive
  * elements of a tensor: value = code * scale, scale = fl(max / 448) over the block's finite values, m_scale / v_scale:
  * ceil(n / 256) floats.  A positive root is never stored as code 0.  All-zero codes and scales are the state before step 1.
- * A non-finite gradient makes its own element's p, m and v non-finite and no other element's.
+ * A non-finite gradient makes its own element's p, m and v non-finite and no other element's.  A finite one whose square
+ * overflows makes v infinite and its element's updates 0; with state_bits 8 such a v is kept as NaN, which is read as infinity.
  * `tensors` (HOST) is read during the call.  Tensors need their element type's alignment; 32 bytes (fp32), 16 (16-bit) and
  * 8 (codes) are read in wide accesses.  n = 0 is valid.
  */

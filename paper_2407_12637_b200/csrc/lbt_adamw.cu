@@ -98,7 +98,7 @@ struct AdamConst {
 // sqrt(v) by Markstein's correction (Computation of Elementary Functions on the IBM RISC System/6000, 1990): s = v y with y a
 // hardware reciprocal root, then s + (v - s s) y / 2 with the residual exact in one fused operation.  Rounds as sqrtf does but
 // for about one v in 2^22; below the normal range (v < 2^-126, where eps is all of the denominator) the root is underestimated.
-// sqrtf's own special cases took a fifth of the step's instructions.
+// sqrtf's own special cases took a fifth of the step's instructions.  (An infinity or NaN comes out as NaN: adam_update.)
 __device__ __forceinline__ float adam_root(float v) {
     float y;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(v, 1.17549435e-38f)));
@@ -106,12 +106,15 @@ __device__ __forceinline__ float adam_root(float v) {
     return __fmaf_rn(__fmaf_rn(-s, s, v), __fmul_rn(0.5f, y), s);
 }
 
-// one element; returns u = sqrt(v)
+// One element; returns u = sqrt(v).  An infinite v (a finite gradient beyond 1.8e19 squared) has the root infinity and the update 0;
+// kRootOfInf false: its root and p come out as NaN, which the caller mends.  8 bits have no code for infinity: it is stored as
+// NaN, and a NaN there is read as infinity (a gradient that is not finite shows in m).
+template <bool kRootOfInf>
 __device__ __forceinline__ float adam_update(const AdamConst& c, float decay, float g, float& p, float& m, float& v) {
     g = __fmul_rn(g, c.gs);
     m = __fadd_rn(__fmul_rn(c.b1, m), __fmul_rn(c.omb1, g));
     v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.omb2, __fmul_rn(g, g)));
-    const float u = adam_root(v);
+    const float root = adam_root(v), u = kRootOfInf ? fminf(root, __uint_as_float(kNonFinite)) : root;   // (fminf passes over NaN)
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__fadd_rn(__fmul_rn(u, c.inv_c2), c.eps)));
     p = __fsub_rn(__fmul_rn(decay, p), __fmul_rn(__fmul_rn(c.step_size, m), inv));
@@ -124,16 +127,21 @@ __device__ __forceinline__ void block_scale(uint32_t most_bits, float& scale, fl
     scale = __fmul_rn(most, 1.0f / 448.0f);
     factor = most > 1e-36f ? __fmul_rn(__frcp_rn(most), 448.0f) : 0.0f;
 }
+// The largest of a lane's eight roots as bits (NaN above infinity above all others).
+__device__ __forceinline__ uint32_t largest(const float (&u)[8]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(u[i]));
+    return most;
+}
 // The moments of a lane's eight elements as the block stores them: scales, and codes ready to be rounded.  Every warp takes the
 // short way unless its block has a root of 0 or something that is not finite: then the largest finite magnitude decides the
 // scale, what is not finite is stored as NaN, and a root of 0 stays 0.
-__device__ __forceinline__ void block_codes(float (&m)[8], float (&u)[8], float& ms, float& vs) {
+__device__ __forceinline__ void block_codes(float (&m)[8], float (&u)[8], uint32_t most_u, float& ms, float& vs) {
     float top_m = 0.0f, low_u = 1.0f;
-    uint32_t most_u = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         top_m = fmaxf(top_m, fabsf(m[i]));   // (passes over NaN)
-        most_u = max(most_u, __float_as_uint(u[i]));
         low_u = fminf(low_u, u[i]);
     }
     uint32_t most_m = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top_m));
@@ -231,7 +239,22 @@ __device__ __forceinline__ void adam_whole(const AdamEntry& e, const AdamConst& 
         for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = adam_update(c, e.decay, g[i], p[i], m[i], v[i]);
+    for (int i = 0; i < 8; ++i) u[i] = adam_update<kBits == 32>(c, e.decay, g[i], p[i], m[i], v[i]);
+    uint32_t most_u = 0;
+    if constexpr (kBits == 8) {
+        // An instruction an element costs this form 2 % of the step (0.4 G elements), so what has no finite root is mended on a way of its own.
+        most_u = largest(u);
+        if (most_u >= kNonFinite) {
+            most_u = kNonFinite;
+            const P* old = static_cast<const P*>(e.p) + at;   // (not written yet)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < have && __float_as_uint(u[i]) >= kNonFinite) {
+                    u[i] = __uint_as_float(kNonFinite);
+                    p[i] = __fsub_rn(__fmul_rn(e.decay, to_f32(old[i])), __fmul_rn(__fmul_rn(c.step_size, m[i]), 0.0f));
+                }
+        }
+    }
     if (kTail && have < 8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -251,7 +274,7 @@ __device__ __forceinline__ void adam_whole(const AdamEntry& e, const AdamConst& 
     }
     if constexpr (kBits == 8) {
         __syncwarp();
-        block_codes(m, u, ms, vs);   // (an absent element's moments are 0)
+        block_codes(m, u, most_u, ms, vs);   // (an absent element's moments are 0)
         uint32_t mc[2], vc[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -319,7 +342,7 @@ __device__ __forceinline__ void adam_ragged(const AdamEntry& e, const AdamConst&
                 v[i] = __fmul_rn(e4m3_values(static_cast<const uint8_t*>(e.v)[k]).x, vs);
                 v[i] = __fmul_rn(v[i], v[i]);
             }
-            u[i] = adam_update(c, e.decay, g, p[i], m[i], v[i]);
+            u[i] = adam_update<true>(c, e.decay, g, p[i], m[i], v[i]);
             adam_store(e.p, p_type, k, p[i]);
             if (kBits == 32) {
                 static_cast<float*>(e.m)[k] = m[i];
@@ -330,7 +353,7 @@ __device__ __forceinline__ void adam_ragged(const AdamEntry& e, const AdamConst&
     if (kBits == 32) return;
     float new_ms, new_vs;
     __syncwarp();
-    block_codes(m, u, new_ms, new_vs);   // (an absent element's moments are 0)
+    block_codes(m, u, largest(u), new_ms, new_vs);   // (an absent element's moments are 0)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < have) {

@@ -245,3 +245,18 @@ def test_a_captured_step_counts_its_replays(bits):
             taken += 1
         assert all(torch.equal(a, b) for a, b in zip(_state_bits(graphed), _state_bits(plain)))
         assert graphed.taken() == plain.taken() == taken
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_squares_that_overflow(bits):
+    """A finite gradient whose square is infinite: v is, the update is 0 by the formula, then and in every later step; only the decay moves p."""
+    n, big = 600, [5, 300, 599]
+    p, g = torch.ones(n, device="cuda"), torch.full((n,), 0.1, device="cuda")
+    opt = lm.AdamW([p], [g], lr=1e-2, weight_decay=0.1, state_bits=bits)
+    decay, want = torch.tensor(1 - 1e-2 * 0.1, device="cuda"), torch.ones(3, device="cuda")
+    for step in range(3):
+        g[big] = torch.tensor([1e20, -3e38, 2e19] if step == 0 else [0.1, 0.0, -0.2], device="cuda")
+        opt.step()
+        want *= decay
+        assert torch.equal(p[big], want) and torch.isfinite(p).all(), step
+        assert torch.isfinite(opt.m[0].float()).all() and int((~torch.isfinite(opt.v[0].float())).sum()) == 3
