@@ -107,6 +107,7 @@ class ConvDesc(C.Structure):
 assert C.sizeof(IntervalState) == 56 and C.sizeof(GradStats) == 40
 
 _lib = None
+_device, _current_raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream   # (without the wrappers' own time)
 
 
 class LbtError(RuntimeError):
@@ -330,20 +331,46 @@ def quantize_grad_fused(dY, state, stats, q_out, stream=None):
            "lbt_quantize_grad_fused")
 
 
-def _rows(t, name, cols=None):
-    """Address, element type and leading dimension of a [rows, cols] CUDA tensor whose rows are contiguous."""
+def _rows(t, name, cols=None, device=None):
+    """Address, element type and leading dimension of a [rows, cols] tensor whose rows are contiguous, on `device` (None: the current one)."""
     kind, shape, stride = TYPES.get(t.dtype), t.shape, t.stride()
-    if kind is None or len(shape) != 2 or not t.is_cuda or (stride[1] != 1 and shape[1] > 1):
-        raise ValueError(f"{name}: a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows")
+    if kind is None or len(shape) != 2 or t.get_device() != (_device() if device is None else device) or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows, on the device of the call")
     if cols is not None and shape[1] != cols:
         raise ValueError(f"{name}: {shape[1]} columns, {cols} expected")
     # (rows that overlap, as an expanded tensor's do, are refused by the library)
     return t.data_ptr(), kind, stride[0] if shape[0] > 1 else shape[1]
 
 
+def _at(t, device=None) -> int:
+    """Address of a contiguous operand that may be left out, on `device` (None: the current one)."""
+    if t is None:
+        return 0
+    if t.get_device() != (_device() if device is None else device) or not t.is_contiguous():
+        raise ValueError("operands are contiguous CUDA tensors on the device of the call")
+    return t.data_ptr()
+
+
+def _place(t, stream=None):
+    """What a call on `t` runs in so that the library, which launches on the current device, launches on t's: the stream given, or
+    the device.  (A call that is there already need not enter anything.)"""
+    at = t.get_device()
+    if at < 0:
+        raise ValueError("operands are CUDA tensors")
+    if stream is None:
+        return torch.cuda.device(at)
+    if stream.device_index != at:
+        raise ValueError("the stream belongs to another device than the operands")
+    return torch.cuda.stream(stream)
+
+
 def _raw_stream(t, stream=None) -> int:
-    """The stream a call on `t` goes to: the one given, else torch's current stream of t's device."""
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
+    """The stream a call on `t` goes to: the one given, else torch's current stream.  The library launches on the current device,
+    so that has to be t's: the default streams of all devices share one handle."""
+    at = t.get_device()
+    if at != _device() or (stream is not None and stream.device_index != at):
+        raise ValueError("the call's tensors and stream belong to the current device (torch.cuda.device)")
+    return stream.cuda_stream if stream is not None else _current_raw_stream(at)
 
 
 def _scratch(nbytes, device, stream):
@@ -357,18 +384,18 @@ def pitch8(cols: int) -> int:
     return (cols + 15) // 16 * 16
 
 
-def _codes(q, rows, cols, name):
+def _codes(q, rows, cols, name, device=None):
     if q.dtype != torch.int8 or tuple(q.shape) != (rows, pitch8(cols)):
         raise ValueError(f"{name}: an int8 tensor of {rows} x {pitch8(cols)} codes")
-    return _p(q)
+    return _at(q, device)
 
 
-def _floats(t, n, name):
+def _floats(t, n, name, device=None):
     if t is None:
         return 0
     if t.dtype != torch.float32 or t.numel() != n:
         raise ValueError(f"{name}: {n} fp32 values")
-    return _p(t)
+    return _at(t, device)
 
 
 def rows8_quantize(x, q, scale, stream=None):
@@ -388,7 +415,7 @@ def linear8_forward(x, q_w, s_w, y, q_x, s_x, bias=None, dev_status=None, stream
     if y.shape[0] != M:
         raise ValueError("y: one row per row of x")
     _check(lib().lbt_linear8_forward(px, tx, ldx, _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"), _floats(bias, O, "bias"), py, ty, ldy,
-                                     M, O, I, _codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _p(dev_status), _raw_stream(x, stream)),
+                                     M, O, I, _codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _at(dev_status), _raw_stream(x, stream)),
            "lbt_linear8_forward")
 
 
@@ -399,7 +426,7 @@ def linear8_matmul(q_x, s_x, q_w, s_w, y, I, bias=None, dev_status=None, stream=
     if y.shape[0] != M:
         raise ValueError("y: one row per row of codes")
     _check(lib().lbt_linear8_matmul(_codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"),
-                                    _floats(bias, O, "bias"), py, ty, ldy, M, O, I, _p(dev_status), _raw_stream(y, stream)), "lbt_linear8_matmul")
+                                    _floats(bias, O, "bias"), py, ty, ldy, M, O, I, _at(dev_status), _raw_stream(y, stream)), "lbt_linear8_matmul")
 
 
 def linear8_workspace_bytes(M, O, I) -> int:
@@ -409,23 +436,24 @@ def linear8_workspace_bytes(M, O, I) -> int:
 def linear8_backward(dY, q_w, s_w, q_x, s_x, I, dX=None, dW=None, dbias=None, ws=None, dev_status=None, stream=None):
     """Gradients of linear8_forward from the codes it left; outputs that are None are not computed.  ws None: from torch's allocator."""
     M, O = dY.shape
-    pg, tg, ldg = _rows(dY, "dY", s_w.numel())
-    px, tx, ldx = _rows(dX, "dX", I) if dX is not None else (0, F32, I)
-    pw, tw, ldw = _rows(dW, "dW", I) if dW is not None else (0, F32, I)
+    raw, on = _raw_stream(dY, stream), dY.get_device()
+    pg, tg, ldg = _rows(dY, "dY", s_w.numel(), on)
+    px, tx, ldx = _rows(dX, "dX", I, on) if dX is not None else (0, F32, I)
+    pw, tw, ldw = _rows(dW, "dW", I, on) if dW is not None else (0, F32, I)
     if (dX is not None and dX.shape[0] != M) or (dW is not None and dW.shape[0] != O):
         raise ValueError("dX: one row per row of dY; dW: one row per column of dY")
     if ws is None:
         ws = _scratch(linear8_workspace_bytes(M, O, I), dY.device, stream)
-    _check(lib().lbt_linear8_backward(pg, tg, ldg, _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"), _codes(q_x, M, I, "q_x"),
-                                      _floats(s_x, M, "s_x"), px, tx, ldx, pw, tw, ldw, _floats(dbias, O, "dbias"), M, O, I, _p(dev_status),
-                                      _p(ws), ws.numel(), _raw_stream(dY, stream)), "lbt_linear8_backward")
+    _check(lib().lbt_linear8_backward(pg, tg, ldg, _codes(q_w, O, I, "q_w", on), _floats(s_w, O, "s_w", on), _codes(q_x, M, I, "q_x", on),
+                                      _floats(s_x, M, "s_x", on), px, tx, ldx, pw, tw, ldw, _floats(dbias, O, "dbias", on), M, O, I, _at(dev_status, on),
+                                      _at(ws, on), ws.numel(), raw), "lbt_linear8_backward")
 
 
 def resnorm_forward(desc, x, h, gate, w_post, b_post, w_pre, b_pre, r, y=None, q=None, q_scale=None, stats=None, stream=None):
     """`lbt_resnorm_forward` on tensors that match `desc` (marshalling only: lm.ResNorm builds and checks them)."""
-    _check(lib().lbt_resnorm_forward(C.addressof(desc), x.data_ptr(), h.data_ptr(), _p(gate), _p(w_post), _p(b_post), _p(w_pre), _p(b_pre),
-                                     r.data_ptr(), y.data_ptr() if y is not None else 0, _p(q), q.shape[1] if q is not None else 0, _p(q_scale),
-                                     _p(stats), _raw_stream(x, stream)), "lbt_resnorm_forward")
+    _check(lib().lbt_resnorm_forward(C.addressof(desc), x.data_ptr(), h.data_ptr(), _at(gate), _at(w_post), _at(b_post), _at(w_pre), _at(b_pre),
+                                     r.data_ptr(), y.data_ptr() if y is not None else 0, _at(q), q.shape[1] if q is not None else 0, _at(q_scale),
+                                     _at(stats), _raw_stream(x, stream)), "lbt_resnorm_forward")
 
 
 def resnorm_workspace_bytes(desc) -> int:
@@ -438,16 +466,16 @@ def resnorm_backward(desc, dr, dy, x, h, gate, w_post, b_post, w_pre, stats, dx,
     if ws is None:
         ws = _scratch(resnorm_workspace_bytes(desc), x.device, stream)
     _check(lib().lbt_resnorm_backward(C.addressof(desc), dr.data_ptr() if dr is not None else 0, dy.data_ptr() if dy is not None else 0,
-                                      x.data_ptr(), h.data_ptr(), _p(gate), _p(w_post), _p(b_post), _p(w_pre), _p(stats), dx.data_ptr(),
-                                      dh.data_ptr(), _p(dgate), _p(dw_post), _p(db_post), _p(dw_pre), _p(db_pre), _p(ws), ws.numel(),
+                                      x.data_ptr(), h.data_ptr(), _at(gate), _at(w_post), _at(b_post), _at(w_pre), _at(stats), dx.data_ptr(),
+                                      dh.data_ptr(), _at(dgate), _at(dw_post), _at(db_post), _at(dw_pre), _at(db_pre), _at(ws), ws.numel(),
                                       _raw_stream(x, stream)), "lbt_resnorm_backward")
 
 
 def adamw_step(table, hyper, grad_scale=None, skip=None, stream=None, skipped=None):
     """One AdamW step over a ctypes array of AdamwTensor; stream: a torch stream or a raw one (None: the current stream).
     skipped: device int64 that counts the steps held back by `skip` (None: hyper.step counts the steps that were taken)."""
-    raw = stream if isinstance(stream, int) else _stream(stream)
-    _check(lib().lbt_adamw_step_ex(table, len(table), C.addressof(hyper), _p(grad_scale), _p(skip), _p(skipped), raw), "lbt_adamw_step")
+    raw = stream if isinstance(stream, int) else _stream(stream)   # (the table's addresses are the caller's to place)
+    _check(lib().lbt_adamw_step_ex(table, len(table), C.addressof(hyper), _at(grad_scale), _at(skip), _at(skipped), raw), "lbt_adamw_step")
 
 
 def grad_diagnostics(dY, q_codes, bits, alpha, stats, ws=None, stream=None) -> "GradDiag":

@@ -7,6 +7,7 @@ made need that stream's event first, as with any torch call.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 
 import torch
@@ -35,8 +36,9 @@ class Linear8:
 
     def _set(self, q_w, s_w, in_features, bias):
         self.I, self.O, self.pitch = int(in_features), s_w.numel(), lbt.pitch8(in_features)
-        # (addresses of the layer's own tensors, whose storage stays)
-        self._weights = (lbt._codes(q_w, self.O, self.I, "q_w"), lbt._floats(s_w, self.O, "s_w"), lbt._floats(bias, self.O, "bias"))
+        self.device = q_w.get_device()
+        with lbt._place(q_w):   # (addresses of the layer's own tensors, whose storage stays)
+            self._weights = (lbt._codes(q_w, self.O, self.I, "q_w"), lbt._floats(s_w, self.O, "s_w"), lbt._floats(bias, self.O, "bias"))
         self.q_w, self.s_w, self.bias, self.kept = q_w, s_w, bias, None
         self.status = torch.zeros(1, dtype=torch.int32, device=q_w.device)   # lbt.ERR_TIMEOUT if a bounded on-chip wait ran out
         self._status = self.status.data_ptr()
@@ -48,20 +50,27 @@ class Linear8:
         """Quantizes the weights [O, I] (after each optimizer step)."""
         if weight.shape != (self.O, self.I):
             raise ValueError(f"weight: {self.O} x {self.I}")
-        lbt.rows8_quantize(weight, self.q_w, self.s_w, stream)
+        on = weight.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(weight, stream):
+                return self.load_weight(weight)
+        lbt.rows8_quantize(weight, self.q_w, self.s_w)
 
     def forward(self, x, out=None, keep=False, stream=None):
         """y for x [M, I]; keep: the codes of x stay for `backward`, until the next forward pass with keep=True."""
-        if stream is not None:
-            with torch.cuda.stream(stream):   # outputs and scratch belong to the stream that uses them
+        on = x.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(x, stream):   # outputs and scratch belong to the stream that uses them
                 return self.forward(x, out, keep)
-        px, tx, ldx = lbt._rows(x, "x", self.I)
+        if on != self.device:
+            raise ValueError(f"the layer's weights are on device {self.device}")
+        px, tx, ldx = lbt._rows(x, "x", self.I, on)
         M = x.shape[0]
         y = x.new_empty((M, self.O)) if out is None else out
-        py, ty, ldy = lbt._rows(y, "y", self.O)
+        py, ty, ldy = lbt._rows(y, "y", self.O, on)
         if y.shape[0] != M:
             raise ValueError("out: one row per row of x")
-        raw = lbt._raw_stream(x)
+        raw = lbt._current_raw_stream(on)
         if keep:
             mine = self._own_kept.get(raw)
             if mine is None or mine[1].shape[0] != M:
@@ -84,17 +93,20 @@ class Linear8:
 
     def forward_codes(self, q_x, s_x, out=None, dtype=torch.bfloat16, keep=False, stream=None):
         """y from codes and scales that another operator made (ResNorm.forward_codes)."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
+        on = q_x.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(q_x, stream):
                 return self.forward_codes(q_x, s_x, out, dtype, keep)
+        if on != self.device:
+            raise ValueError(f"the layer's weights are on device {self.device}")
         M = s_x.numel()
         y = torch.empty(M, self.O, dtype=dtype, device=q_x.device) if out is None else out
-        py, ty, ldy = lbt._rows(y, "y", self.O)
+        py, ty, ldy = lbt._rows(y, "y", self.O, on)
         if y.shape[0] != M:
             raise ValueError("out: one row per row of codes")
         q_w, s_w, bias = self._weights
-        status = lbt.lib().lbt_linear8_matmul(lbt._codes(q_x, M, self.I, "q_x"), lbt._floats(s_x, M, "s_x"), q_w, s_w, bias, py, ty, ldy,
-                                              M, self.O, self.I, self._status, lbt._raw_stream(y))
+        status = lbt.lib().lbt_linear8_matmul(lbt._codes(q_x, M, self.I, "q_x", on), lbt._floats(s_x, M, "s_x", on), q_w, s_w, bias, py, ty, ldy,
+                                              M, self.O, self.I, self._status, lbt._current_raw_stream(on))
         if status:
             raise lbt.LbtError(status, "lbt_linear8_matmul")
         if keep:
@@ -103,8 +115,9 @@ class Linear8:
 
     def backward(self, dy, need_dx=True, need_dw=True, dw_dtype=torch.float32, dx=None, dw=None, dbias=None, stream=None):
         """{"dx", "dw", "dbias"} of the last forward pass with keep=True (dx, dw, dbias: buffers to write into)."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
+        on = dy.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(dy, stream):
                 return self.backward(dy, need_dx, need_dw, dw_dtype, dx, dw, dbias)
         if self.kept is None:
             raise RuntimeError("backward needs a forward pass with keep=True")
@@ -118,7 +131,7 @@ class Linear8:
             out["dw"] = dw if dw is not None else dy.new_empty((self.O, self.I), dtype=dw_dtype)
             if self.bias is not None:
                 out["dbias"] = dbias if dbias is not None else torch.empty_like(self.s_w)
-        raw = lbt._raw_stream(dy)
+        raw = lbt._current_raw_stream(on)
         size, space = self._space.get(raw, (0, None))
         need = lbt.linear8_workspace_bytes(dy.shape[0], self.O, self.I)
         if size < need:
@@ -148,20 +161,24 @@ class ResNorm:
         self.param_dtype = given[0].dtype if given else None
         self.eps, self.scale_x, self.scale_h = float(eps), float(scale_x), float(scale_h)
         self.kept = None
-        self._params = tuple(lbt._p(p) for p in (w_post, b_post, w_pre, b_pre))   # (the layer's own tensors, whose storage stays)
+        self.device = given[0].get_device() if given else None
+        with lbt._place(given[0]) if given else contextlib.nullcontext():   # (the layer's own tensors, whose storage stays)
+            self._params = tuple(lbt._at(p) for p in (w_post, b_post, w_pre, b_pre))
         self._plans = {}   # (rows, types, leading dimensions) -> descriptor and its workspace size
         self._space, self._stats = {}, {}   # stream -> workspace of the backward pass, statistics that were kept
 
-    def _plan(self, names, acts, gate, rows_per_gate):
+    def _plan(self, names, acts, gate, rows_per_gate, on):
         """Addresses of the activations and the descriptor of a call on tensors of these sizes (checked each time)."""
         x = acts[0]
+        if self.device is not None and on != self.device:
+            raise ValueError(f"the norm's parameters are on device {self.device}")
         rows, dtype, addresses, lds = x.shape[0], x.dtype, [], []
         for name, t in zip(names, acts):
             if t is None:
                 addresses.append(0)
                 lds.append(0)
                 continue
-            p, _, ld = lbt._rows(t, name, self.dim)
+            p, _, ld = lbt._rows(t, name, self.dim, on)
             if t.shape[0] != rows or t.dtype != dtype:
                 raise ValueError(f"{name}: {rows} rows of {dtype}")
             addresses.append(p)
@@ -184,17 +201,17 @@ class ResNorm:
             plan = self._plans[key] = (d, C.addressof(d), lbt.resnorm_workspace_bytes(d))
         return addresses, plan
 
-    def _forward(self, x, h, gate, rows_per_gate, r, y, q, q_scale, keep):
+    def _forward(self, x, h, gate, rows_per_gate, r, y, q, q_scale, keep, on):
         names, acts = (("x", "h", "r", "y"), (x, h, r, y)) if y is not None else (("x", "h", "r"), (x, h, r))
-        at, (_, desc, _) = self._plan(names, acts, gate, rows_per_gate)
-        raw, stats = lbt._raw_stream(x), None
+        at, (_, desc, _) = self._plan(names, acts, gate, rows_per_gate, on)
+        raw, stats = lbt._current_raw_stream(on), None
         if keep:   # a buffer for each stream, shared by one forward pass after the other
             stats = self._stats.get(raw)
             if stats is None or stats.shape[0] != x.shape[0]:
                 stats = self._stats[raw] = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device)
         w_post, b_post, w_pre, b_pre = self._params
-        status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._p(gate), w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
-                                               lbt._p(q), q.shape[1] if q is not None else 0, lbt._p(q_scale), lbt._p(stats), raw)
+        status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._at(gate, on), w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
+                                               lbt._at(q, on), q.shape[1] if q is not None else 0, lbt._at(q_scale, on), lbt._at(stats, on), raw)
         if status:
             raise lbt.LbtError(status, "lbt_resnorm_forward")
         if keep:
@@ -203,33 +220,36 @@ class ResNorm:
     def forward(self, x, h, gate=None, rows_per_gate=0, out=None, keep=False, stream=None):
         """(r, y); keep: the statistics stay for `backward` (until the next forward pass with keep=True), which also needs x and h
         unchanged."""
-        if stream is not None:
-            with torch.cuda.stream(stream):   # outputs and scratch belong to the stream that uses them
+        on = x.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(x, stream):   # outputs and scratch belong to the stream that uses them
                 return self.forward(x, h, gate, rows_per_gate, out, keep)
         r, y = out if out is not None else (torch.empty_like(x), torch.empty_like(x))
-        self._forward(x, h, gate, rows_per_gate, r, y, None, None, keep)
+        self._forward(x, h, gate, rows_per_gate, r, y, None, None, keep, on)
         return r, y
 
     def forward_codes(self, x, h, gate=None, rows_per_gate=0, out=None, keep=False, stream=None):
         """(r, q, scale): y as the 8-bit rows that Linear8.forward_codes takes."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
+        on = x.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(x, stream):
                 return self.forward_codes(x, h, gate, rows_per_gate, out, keep)
         r = torch.empty_like(x) if out is None else out
         q = x.new_empty((x.shape[0], lbt.pitch8(self.dim)), dtype=torch.int8)
         scale = x.new_empty(x.shape[0], dtype=torch.float32)
-        self._forward(x, h, gate, rows_per_gate, r, None, q, scale, keep)
+        self._forward(x, h, gate, rows_per_gate, r, None, q, scale, keep, on)
         return r, q, scale
 
     def backward(self, dr, dy, out=None, stream=None):
         """Gradients of the last forward pass with keep=True: {"dx", "dh"} and those of the parameters and the gate that there are
         ("dgate", "dw_post", "db_post", "dw_pre", "db_pre").  out: buffers to write some of them into, by name."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return self.backward(dr, dy, out)
         if self.kept is None:
             raise RuntimeError("backward needs a forward pass with keep=True")
         x, h, gate, rows_per_gate, stats = self.kept
+        on = x.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(x, stream):
+                return self.backward(dr, dy, out)
         given, out, grads = out or {}, {}, []
         for name in ("dx", "dh"):
             out[name] = given[name] if name in given else torch.empty_like(x)
@@ -239,16 +259,16 @@ class ResNorm:
                 g = out[name] = given[name] if name in given else torch.empty_like(p)
                 if g.numel() != p.numel() or g.dtype != p.dtype:
                     raise ValueError(f"{name}: {p.numel()} values of {p.dtype}")
-                grads.append(lbt._p(g))
+                grads.append(lbt._at(g, on))
             else:
                 grads.append(0)
-        at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate)
-        raw = lbt._raw_stream(x)
+        at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate, on)
+        raw = lbt._current_raw_stream(on)
         ws = self._space.get(raw)
         if ws is None or ws.numel() < size:
             ws = self._space[raw] = torch.empty(size, dtype=torch.uint8, device=x.device)
         w_post, b_post, w_pre, _ = self._params
-        status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._p(gate), w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
+        status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._at(gate, on), w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
                                                 *grads, ws.data_ptr(), size, raw)
         if status:
             raise lbt.LbtError(status, "lbt_resnorm_backward")
@@ -281,20 +301,26 @@ class AdamW:
         lrs, wds = (list(x) if isinstance(x, (list, tuple)) else [x] * n for x in (lr, weight_decay))
         if any(len(x) != n for x in (self.m, self.v, self.m_scale, self.v_scale, lrs, wds)):
             raise ValueError("one of each for each parameter")
+        lists = (self.params, self.grads, self.m, self.v, self.m_scale, self.v_scale)
+        if len({t.get_device() for ts in lists for t in ts if t is not None}) > 1:
+            raise ValueError("parameters, gradients and moments are on one device")
+        self.device = self.params[0].get_device() if n else None
         self.table = (lbt.AdamwTensor * n)()
-        for i, (p, g) in enumerate(zip(self.params, self.grads)):
-            if p.dtype not in lbt.TYPES or g.dtype not in lbt.TYPES or g.numel() != p.numel():
-                raise ValueError("parameters and gradients: fp32, bf16 or fp16, of equal sizes")
-            for t, size, kind in ((self.m[i], p.numel(), state), (self.v[i], p.numel(), state), (self.m_scale[i], blocks[i], torch.float32),
-                                  (self.v_scale[i], blocks[i], torch.float32)):
-                if t is not None and (t.numel() != size or t.dtype != kind):
-                    raise ValueError(f"moments: {p.numel()} values of {state}; with 8 bits one fp32 scale for each {lbt.ADAMW_BLOCK}")
-            e = self.table[i]
-            e.p, e.g, e.m, e.v, e.m_scale, e.v_scale = (lbt._p(t) for t in (p, g, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i]))
-            e.n, e.lr, e.weight_decay, e.p_type, e.g_type = p.numel(), lrs[i], wds[i], lbt.TYPES[p.dtype], lbt.TYPES[g.dtype]
+        with lbt._place(self.params[0]) if n else contextlib.nullcontext():
+            for i, (p, g) in enumerate(zip(self.params, self.grads)):
+                if p.dtype not in lbt.TYPES or g.dtype not in lbt.TYPES or g.numel() != p.numel():
+                    raise ValueError("parameters and gradients: fp32, bf16 or fp16, of equal sizes")
+                for t, size, kind in ((self.m[i], p.numel(), state), (self.v[i], p.numel(), state), (self.m_scale[i], blocks[i], torch.float32),
+                                      (self.v_scale[i], blocks[i], torch.float32)):
+                    if t is not None and (t.numel() != size or t.dtype != kind):
+                        raise ValueError(f"moments: {p.numel()} values of {state}; with 8 bits one fp32 scale for each {lbt.ADAMW_BLOCK}")
+                e = self.table[i]
+                e.p, e.g, e.m, e.v, e.m_scale, e.v_scale = (lbt._at(t) for t in (p, g, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i]))
+                e.n, e.lr, e.weight_decay, e.p_type, e.g_type = p.numel(), lrs[i], wds[i], lbt.TYPES[p.dtype], lbt.TYPES[g.dtype]
         self.hyper = lbt.AdamwHyper(betas[0], betas[1], eps, step, state_bits, 0)   # (its step counts the calls)
         # calls that were held back, counted once there may be some (a launch that need not look starts 0.5 us earlier)
         self.skipped, self._counting = torch.zeros(1, dtype=torch.int64, device=self.params[0].device) if n else None, False
+        self._skipped = self.skipped.data_ptr() if n else 0
         self._replayed = False   # whether a step is in a captured graph
 
     def set_lr(self, lr):
@@ -305,17 +331,21 @@ class AdamW:
     def step(self, grad_scale=None, skip=None, stream=None):
         """One step.  grad_scale: device float the gradients are multiplied by; skip: device int32, non-zero = leave everything (the
         step then counts for nothing: the next one corrects as this one would have)."""
-        if stream is not None and self.params:
-            with torch.cuda.stream(stream):
-                return self.step(grad_scale, skip)
-        if not self._replayed and self.params and torch.cuda.is_current_stream_capturing():
-            self._replayed = True
+        if self.params:
+            if stream is not None or self.device != lbt._device():
+                with lbt._place(self.params[0], stream):
+                    return self.step(grad_scale, skip)
+            if not self._replayed and torch._C._cuda_isCurrentStreamCapturing():
+                self._replayed = True
         if skip is not None or self._replayed:
             self._counting = True
         self.hyper.step += 1
         try:
-            raw = lbt._raw_stream(self.params[0]) if self.params else stream
-            lbt.adamw_step(self.table, self.hyper, grad_scale, skip, raw, self.skipped if self._counting else None)
+            raw = lbt._current_raw_stream(self.device) if self.params else stream
+            status = lbt.lib().lbt_adamw_step_ex(self.table, len(self.params), C.addressof(self.hyper), lbt._at(grad_scale, self.device), lbt._at(skip, self.device),
+                                                 self._skipped if self._counting else 0, raw)
+            if status:
+                raise lbt.LbtError(status, "lbt_adamw_step_ex")
         except Exception:   # refused: nothing was enqueued
             self.hyper.step -= 1
             raise

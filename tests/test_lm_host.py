@@ -2,9 +2,12 @@
 
 The addresses handed to the library here are never read: each call is refused (or has nothing to do) before a launch.
 """
+import contextlib
 import ctypes as C
+import types
 
 import pytest
+import torch
 
 from paper_2407_12637_b200 import build as lib_build
 from paper_2407_12637_b200 import lbt, lm
@@ -138,3 +141,111 @@ def test_a_refused_step_does_not_count():
     good = lm.AdamW([], [], step=3)   # (no tensors: nothing is launched)
     good.step(stream=0)
     assert good.hyper.step == good.taken() == 4
+
+
+# ---------------------------------------------------------------------------------------------- several devices, without any
+class _Tensor:
+    """A contiguous tensor as the layers see one on a CUDA device: nothing behind its address."""
+
+    def __init__(self, shape, dtype, index):
+        self.shape, self.dtype, self.index = torch.Size(shape), dtype, index
+        self.device = torch.device("cpu")   # where a layer makes its scratch
+
+    def get_device(self):
+        return self.index
+
+    def stride(self):
+        return (self.shape[1], 1) if len(self.shape) == 2 else (1,)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return A
+
+
+class _Devices:
+    """Two CUDA devices as torch and the library see them: which one is current, and which one each call was made on."""
+
+    def __init__(self, monkeypatch):
+        self.current, self.calls = 0, []
+        monkeypatch.setattr(lbt, "_device", lambda: self.current)
+        monkeypatch.setattr(lbt, "_current_raw_stream", lambda index: 0)
+        monkeypatch.setattr(lbt, "lib", lambda: self)
+        monkeypatch.setattr(torch.cuda, "device", self.enter)
+        monkeypatch.setattr(torch.cuda, "stream", self.enter)
+        monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: False)
+
+    @contextlib.contextmanager
+    def enter(self, where):
+        before = self.current
+        if isinstance(where, int):
+            self.current = where
+        elif hasattr(where, "device_index"):
+            self.current = where.device_index
+        try:
+            yield
+        finally:
+            self.current = before
+
+    def __getattr__(self, name):
+        def call(*args):
+            if name.endswith("workspace_bytes"):
+                return 256
+            self.calls.append((name, self.current))
+            return lbt.OK
+        return call
+
+
+def _layer(index):
+    layer = lm.Linear8.__new__(lm.Linear8)
+    with torch.cuda.device(index):
+        layer._set(_Tensor((32, 64), torch.int8, index), _Tensor((32,), torch.float32, index), 64, None)
+    layer.status = _Tensor((1,), torch.int32, index)
+    return layer
+
+
+def test_calls_launch_on_their_tensors_device(monkeypatch):
+    devices = _Devices(monkeypatch)
+    x, y = (_Tensor(shape, torch.bfloat16, 1) for shape in ((5, 64), (5, 32)))
+    q, s = _Tensor((5, 64), torch.int8, 1), _Tensor((5,), torch.float32, 1)
+    layer = _layer(1)
+    layer._space[0] = (1 << 20, _Tensor((1 << 20,), torch.uint8, 1))
+    layer.forward(x, out=y)
+    layer.forward(x, out=y, keep=True)
+    layer.forward_codes(q, s, out=y, keep=True)   # (its codes are the ones kept)
+    layer.backward(y, dx=x, need_dw=False)
+    layer.load_weight(_Tensor((32, 64), torch.float32, 1))
+    norm = lm.ResNorm(64)
+    norm.forward(x, x, out=(x, x))
+    assert devices.calls and {index for _, index in devices.calls} == {1} and devices.current == 0
+    # on a stream: the stream's device
+    stream = types.SimpleNamespace(device_index=1, cuda_stream=7)
+    layer.forward(x, out=y, stream=stream)
+    assert {index for _, index in devices.calls} == {1} and devices.current == 0
+
+
+def test_operands_on_several_devices_are_refused(monkeypatch):
+    devices = _Devices(monkeypatch)
+    t = lambda shape, index, dtype=torch.bfloat16: _Tensor(shape, dtype, index)  # noqa: E731
+    layer = _layer(1)
+    codes = lambda index: (t((5, 64), index, torch.int8), t((5,), index, torch.float32))  # noqa: E731
+    vec = lambda index: t((64,), index, torch.float32)  # noqa: E731
+    away = types.SimpleNamespace(device_index=0, cuda_stream=7)
+    norm = lm.ResNorm(64, w_pre=vec(0))
+    q_w, s_w = t((32, 64), 1, torch.int8), t((32,), 1, torch.float32)
+    for bad in (lambda: layer.forward(t((5, 64), 0), out=t((5, 32), 0)), lambda: layer.forward(t((5, 64), 1), out=t((5, 32), 0)),
+                lambda: layer.forward(t((5, 64), 1), out=t((5, 32), 1), stream=away), lambda: layer.forward_codes(*codes(0), out=t((5, 32), 1)),
+                lambda: layer.load_weight(t((32, 64), 0, torch.float32)), lambda: layer.forward(t((5, 64), -1), out=t((5, 32), 1)),
+                lambda: norm.forward(t((5, 64), 1), t((5, 64), 1), out=(t((5, 64), 1),) * 2),
+                lambda: norm.forward(t((5, 64), 0), t((5, 64), 1), out=(t((5, 64), 0),) * 2),
+                lambda: norm.forward(t((5, 64), 0), t((5, 64), 0), vec(1), out=(t((5, 64), 0),) * 2),
+                lambda: lm.ResNorm(64, w_pre=vec(0), w_post=vec(1)), lambda: lm.AdamW([vec(0), vec(1)], [vec(0), vec(1)], [vec(0)] * 2, [vec(0)] * 2),
+                lambda: lm.AdamW([vec(0)], [vec(1)], [vec(0)], [vec(0)]),
+                lambda: lbt.rows8_quantize(t((32, 64), 1, torch.float32), q_w, s_w)):   # (the binding itself enters no device)
+        with pytest.raises(ValueError):
+            bad()
+    assert not devices.calls
