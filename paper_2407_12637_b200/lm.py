@@ -290,6 +290,8 @@ class AdamW:
             state_bits = 32 if all(t.dtype == torch.float32 for t in m) else 8
         if state_bits not in (8, 32):
             raise ValueError("state_bits: 8 or 32")
+        if state_bits == 8 and ((m is not None and m_scale is None) or (v is not None and v_scale is None)):
+            raise ValueError("moments in 8 bits come with their scales (new ones would be 0, and the moments with them)")
         state = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
         blocks = [-(-p.numel() // lbt.ADAMW_BLOCK) for p in params]
         new = lambda kind, sizes: [torch.zeros(s, dtype=kind, device=p.device) for s, p in zip(sizes, params)]  # noqa: E731

@@ -260,3 +260,14 @@ def test_squares_that_overflow(bits):
         want *= decay
         assert torch.equal(p[big], want) and torch.isfinite(p).all(), step
         assert torch.isfinite(opt.m[0].float()).all() and int((~torch.isfinite(opt.v[0].float())).sum()) == 3
+
+
+def test_moments_in_codes_need_their_scales():
+    p, g = torch.zeros(300, device="cuda"), torch.zeros(300, device="cuda")
+    codes = lambda: [torch.zeros(300, dtype=torch.float8_e4m3fn, device="cuda")]  # noqa: E731
+    scales = [torch.ones(2, device="cuda")]
+    for given in ({"m": codes()}, {"m": codes(), "v": codes()}, {"m": codes(), "v": codes(), "m_scale": scales}, {"m": codes(), "v": codes(), "v_scale": scales},
+                  {"v": codes()}):
+        with pytest.raises(ValueError):
+            lm.AdamW([p], [g], **given)
+    lm.AdamW([p], [g], codes(), codes(), scales, [scales[0].clone()]).step()
