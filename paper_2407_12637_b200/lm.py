@@ -114,7 +114,8 @@ class Linear8:
         return y
 
     def backward(self, dy, need_dx=True, need_dw=True, dw_dtype=torch.float32, dx=None, dw=None, dbias=None, stream=None):
-        """{"dx", "dw", "dbias"} of the last forward pass with keep=True (dx, dw, dbias: buffers to write into)."""
+        """{"dx", "dw", "dbias"} of the last forward pass with keep=True (dx, dw, dbias: buffers to write into; what has one
+        is computed whatever need_dx and need_dw say, and a bias's gradient comes with dw)."""
         on = dy.get_device()
         if stream is not None or on != lbt._device():
             with lbt._place(dy, stream):
@@ -129,8 +130,8 @@ class Linear8:
             out["dx"] = dx if dx is not None else dy.new_empty((dy.shape[0], self.I))
         if need_dw or dw is not None:
             out["dw"] = dw if dw is not None else dy.new_empty((self.O, self.I), dtype=dw_dtype)
-            if self.bias is not None:
-                out["dbias"] = dbias if dbias is not None else torch.empty_like(self.s_w)
+        if dbias is not None or ("dw" in out and self.bias is not None):
+            out["dbias"] = dbias if dbias is not None else torch.empty_like(self.s_w)
         raw = lbt._current_raw_stream(on)
         size, space = self._space.get(raw, (0, None))
         need = lbt.linear8_workspace_bytes(dy.shape[0], self.O, self.I)

@@ -232,3 +232,18 @@ def test_refusals():
     with pytest.raises(lbt.LbtError) as e:
         long.forward(torch.ones(1, I, device="cuda"))
     assert e.value.status == lbt.ERR_ACC_RANGE
+
+
+def test_bias_gradient_alone():
+    lin = lm.Linear8(64, 48, bias=torch.ones(48, device="cuda"), weight=torch.randn(48, 64, device="cuda"))
+    bare = lm.Linear8(64, 48, weight=torch.randn(48, 64, device="cuda"))
+    x, dy = torch.randn(70, 64, device="cuda"), torch.randn(70, 48, device="cuda")
+    for layer in (lin, bare):
+        layer.forward(x, keep=True)
+        want = layer.backward(dy, dbias=torch.full((48,), 7.0, device="cuda"))["dbias"]
+        assert ((want.double() - dy.double().sum(0)).abs() <= 70 * 2.0 ** -24 * dy.double().abs().sum(0)).all()
+        for need_dx in (True, False):
+            db = torch.full((48,), 7.0, device="cuda")
+            out = layer.backward(dy, need_dx=need_dx, need_dw=False, dbias=db)
+            assert out["dbias"] is db and torch.equal(db, want) and set(out) == {"dbias"} | ({"dx"} if need_dx else set())
+    assert set(lin.backward(dy, need_dw=False)) == {"dx"} and set(bare.backward(dy)) == {"dx", "dw"}
