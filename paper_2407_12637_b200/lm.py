@@ -3,12 +3,14 @@
 Each object keeps what a program keeps between calls (weight codes, parameters, moments, scratch for each stream) and the
 plan of its calls; every step of arithmetic runs in the library (`lbt`).  Outputs may be handed in (`out`); otherwise they
 come from torch's allocator.  Work is enqueued on `stream` (default: torch's current stream); tensors that another stream
-made need that stream's event first, as with any torch call.
+made need that stream's event first, as with any torch call.  Threads may share an object's forward passes without `keep`;
+what `keep` holds for `backward` belongs to one thread at a time.
 """
 from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import threading
 
 import torch
 
@@ -45,6 +47,7 @@ class Linear8:
         # never shared between streams: codes and scales of x that are not kept (rows, buffer, two addresses), those that were
         # made here to be kept (shared by one forward pass after the other), and the backward pass's workspace
         self._scratch, self._own_kept, self._space = {}, {}, {}
+        self._lock = threading.Lock()   # a pass uses them for as long as it enqueues (the library's call lets other threads run)
 
     def load_weight(self, weight, stream=None):
         """Quantizes the weights [O, I] (after each optimizer step)."""
@@ -71,24 +74,25 @@ class Linear8:
         if y.shape[0] != M:
             raise ValueError("out: one row per row of x")
         raw = lbt._current_raw_stream(on)
-        if keep:
-            mine = self._own_kept.get(raw)
-            if mine is None or mine[1].shape[0] != M:
-                mine = self._own_kept[raw] = (torch.empty(M, self.pitch, dtype=torch.int8, device=x.device),
-                                              torch.empty(M, dtype=torch.float32, device=x.device))
-            self.kept = mine
-            pq, ps = mine[0].data_ptr(), mine[1].data_ptr()
-        else:
-            rows, _, pq, ps = self._scratch.get(raw, (0, None, 0, 0))
-            if rows < M:
-                rows = -(-M // 64) * 64
-                space = torch.empty(rows * (self.pitch + 4), dtype=torch.uint8, device=x.device)
-                pq, ps = space.data_ptr(), space.data_ptr() + rows * self.pitch
-                self._scratch[raw] = (rows, space, pq, ps)
-        q_w, s_w, bias = self._weights
-        status = lbt.lib().lbt_linear8_forward(px, tx, ldx, q_w, s_w, bias, py, ty, ldy, M, self.O, self.I, pq, ps, self._status, raw)
-        if status:
-            raise lbt.LbtError(status, "lbt_linear8_forward")
+        with self._lock:
+            if keep:
+                mine = self._own_kept.get(raw)
+                if mine is None or mine[1].shape[0] != M:
+                    mine = self._own_kept[raw] = (torch.empty(M, self.pitch, dtype=torch.int8, device=x.device),
+                                                  torch.empty(M, dtype=torch.float32, device=x.device))
+                self.kept = mine
+                pq, ps = mine[0].data_ptr(), mine[1].data_ptr()
+            else:
+                rows, _, pq, ps = self._scratch.get(raw, (0, None, 0, 0))
+                if rows < M:
+                    rows = -(-M // 64) * 64
+                    space = torch.empty(rows * (self.pitch + 4), dtype=torch.uint8, device=x.device)
+                    pq, ps = space.data_ptr(), space.data_ptr() + rows * self.pitch
+                    self._scratch[raw] = (rows, space, pq, ps)
+            q_w, s_w, bias = self._weights
+            status = lbt.lib().lbt_linear8_forward(px, tx, ldx, q_w, s_w, bias, py, ty, ldy, M, self.O, self.I, pq, ps, self._status, raw)
+            if status:
+                raise lbt.LbtError(status, "lbt_linear8_forward")
         return y
 
     def forward_codes(self, q_x, s_x, out=None, dtype=torch.bfloat16, keep=False, stream=None):
@@ -133,12 +137,13 @@ class Linear8:
         if dbias is not None or ("dw" in out and self.bias is not None):
             out["dbias"] = dbias if dbias is not None else torch.empty_like(self.s_w)
         raw = lbt._current_raw_stream(on)
-        size, space = self._space.get(raw, (0, None))
-        need = lbt.linear8_workspace_bytes(dy.shape[0], self.O, self.I)
-        if size < need:
-            space = torch.empty(need, dtype=torch.uint8, device=dy.device)
-            self._space[raw] = (need, space)
-        lbt.linear8_backward(dy, self.q_w, self.s_w, q_x, s_x, self.I, out.get("dx"), out.get("dw"), out.get("dbias"), space, self.status)
+        with self._lock:
+            size, space = self._space.get(raw, (0, None))
+            need = lbt.linear8_workspace_bytes(dy.shape[0], self.O, self.I)
+            if size < need:
+                space = torch.empty(need, dtype=torch.uint8, device=dy.device)
+                self._space[raw] = (need, space)
+            lbt.linear8_backward(dy, self.q_w, self.s_w, q_x, s_x, self.I, out.get("dx"), out.get("dw"), out.get("dbias"), space, self.status)
         return out
 
 

@@ -3,6 +3,8 @@
 Tolerances.  y = fl(fl(acc) fl(s_x s_w)) + b: three roundings of the product and one of the sum, each within 2^-24 of its
 magnitude, then one rounding to the output's type (2^-24, 2^-8, 2^-11; fp16 also 2^-25 absolute below its normal range).
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -247,3 +249,23 @@ def test_bias_gradient_alone():
             out = layer.backward(dy, need_dx=need_dx, need_dw=False, dbias=db)
             assert out["dbias"] is db and torch.equal(db, want) and set(out) == {"dbias"} | ({"dx"} if need_dx else set())
     assert set(lin.backward(dy, need_dw=False)) == {"dx"} and set(bare.backward(dy)) == {"dx", "dw"}
+
+
+def test_two_threads_on_one_stream():
+    """Two threads that share a layer and the default stream, each with its own inputs: the bits that each gets alone."""
+    lin = lm.Linear8(300, 200, weight=torch.randn(200, 300, device="cuda"))
+    xs = [torch.randn(70, 300, device="cuda") * (i + 1) for i in range(2)]
+    want = [lin.forward(x) for x in xs]
+    got = [[], []]
+
+    def work(i):
+        for _ in range(300):
+            got[i].append(lin.forward(xs[i]))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i]) for i in range(2) for y in got[i])

@@ -4,6 +4,7 @@ The addresses handed to the library here are never read: each call is refused (o
 """
 import contextlib
 import ctypes as C
+import threading
 import types
 
 import pytest
@@ -249,3 +250,37 @@ def test_operands_on_several_devices_are_refused(monkeypatch):
         with pytest.raises(ValueError):
             bad()
     assert not devices.calls
+
+
+def test_threads_that_share_a_layer_take_turns(monkeypatch):
+    """A forward pass enqueues the quantizer and the product that reads its codes from the layer's scratch: between the two no other
+    thread's pass may use the same scratch."""
+    devices = _Devices(monkeypatch)
+    layer = _layer(0)
+    layer._space[0] = (1 << 20, _Tensor((1 << 20,), torch.uint8, 0))
+    inside, overlaps, entered = [], [], threading.Event()
+
+    def call(scratch):
+        overlaps.extend(s for s in inside if s == scratch)
+        inside.append(scratch)
+        (entered.wait if len(inside) == 1 else entered.set)(*([0.3] if len(inside) == 1 else []))   # the first one stays for the second
+        inside.remove(scratch)
+        return lbt.OK
+
+    devices.lbt_linear8_forward = lambda *a: call(a[12])    # (q_x)
+    devices.lbt_linear8_backward = lambda *a: call(a[18])   # (the workspace)
+    x, y = _Tensor((5, 64), torch.bfloat16, 0), _Tensor((5, 32), torch.bfloat16, 0)
+
+    def both(work):
+        entered.clear()
+        threads = [threading.Thread(target=work) for _ in range(2)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join(10)
+
+    both(lambda: layer.forward(x, out=y))
+    assert not overlaps
+    layer.kept = (_Tensor((5, 64), torch.int8, 0), _Tensor((5,), torch.float32, 0))
+    both(lambda: layer.backward(y, dx=x, need_dw=False))
+    assert not overlaps
