@@ -80,7 +80,6 @@ class Linear8:
                 if mine is None or mine[1].shape[0] != M:
                     mine = self._own_kept[raw] = (torch.empty(M, self.pitch, dtype=torch.int8, device=x.device),
                                                   torch.empty(M, dtype=torch.float32, device=x.device))
-                self.kept = mine
                 pq, ps = mine[0].data_ptr(), mine[1].data_ptr()
             else:
                 rows, _, pq, ps = self._scratch.get(raw, (0, None, 0, 0))
@@ -93,6 +92,8 @@ class Linear8:
             status = lbt.lib().lbt_linear8_forward(px, tx, ldx, q_w, s_w, bias, py, ty, ldy, M, self.O, self.I, pq, ps, self._status, raw)
             if status:
                 raise lbt.LbtError(status, "lbt_linear8_forward")
+            if keep:
+                self.kept = mine
         return y
 
     def forward_codes(self, q_x, s_x, out=None, dtype=torch.bfloat16, keep=False, stream=None):

@@ -269,3 +269,16 @@ def test_two_threads_on_one_stream():
         t.join()
     torch.cuda.synchronize()
     assert all(torch.equal(y, want[i]) for i in range(2) for y in got[i])
+
+
+def test_a_refused_forward_pass_leaves_what_backward_reads():
+    lin = lm.Linear8(64, 48, weight=torch.randn(48, 64, device="cuda"))
+    x, dy = torch.randn(70, 64, device="cuda"), torch.randn(70, 48, device="cuda")
+    lin.forward(x, keep=True)
+    want, kept = lin.backward(dy), lin.kept
+    wide = torch.randn(1, 64, device="cuda").expand(30, 64)   # rows that overlap
+    with pytest.raises(lbt.LbtError):
+        lin.forward(wide, keep=True)
+    assert lin.kept is kept
+    out = lin.backward(dy)
+    assert all(torch.equal(out[k], want[k]) for k in want)
