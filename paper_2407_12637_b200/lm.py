@@ -17,6 +17,15 @@ import torch
 from . import lbt
 
 
+_NO_SCRATCH = (0, None, 0, 0)
+
+
+def _capturing() -> bool:
+    """Whether the current stream is being captured.  What a captured call allocates belongs to its graph, and what a graph's
+    replays write must not be handed on: such calls neither use nor leave scratch that is kept from call to call."""
+    return torch._C._cuda_isCurrentStreamCapturing()
+
+
 class Linear8:
     """A linear layer y = x W^T + b whose three products run on 8-bit integers, with a scale for each output channel of W and
     for each token of x (and of the gradient)."""
@@ -75,19 +84,22 @@ class Linear8:
             raise ValueError("out: one row per row of x")
         raw = lbt._current_raw_stream(on)
         with self._lock:
+            held = not _capturing()
             if keep:
-                mine = self._own_kept.get(raw)
+                mine = self._own_kept.get(raw) if held else None
                 if mine is None or mine[1].shape[0] != M:
-                    mine = self._own_kept[raw] = (torch.empty(M, self.pitch, dtype=torch.int8, device=x.device),
-                                                  torch.empty(M, dtype=torch.float32, device=x.device))
+                    mine = (torch.empty(M, self.pitch, dtype=torch.int8, device=x.device), torch.empty(M, dtype=torch.float32, device=x.device))
+                    if held:
+                        self._own_kept[raw] = mine
                 pq, ps = mine[0].data_ptr(), mine[1].data_ptr()
             else:
-                rows, _, pq, ps = self._scratch.get(raw, (0, None, 0, 0))
+                rows, space, pq, ps = self._scratch.get(raw, _NO_SCRATCH) if held else _NO_SCRATCH
                 if rows < M:
                     rows = -(-M // 64) * 64
                     space = torch.empty(rows * (self.pitch + 4), dtype=torch.uint8, device=x.device)
                     pq, ps = space.data_ptr(), space.data_ptr() + rows * self.pitch
-                    self._scratch[raw] = (rows, space, pq, ps)
+                    if held:
+                        self._scratch[raw] = (rows, space, pq, ps)
             q_w, s_w, bias = self._weights
             status = lbt.lib().lbt_linear8_forward(px, tx, ldx, q_w, s_w, bias, py, ty, ldy, M, self.O, self.I, pq, ps, self._status, raw)
             if status:
@@ -139,11 +151,13 @@ class Linear8:
             out["dbias"] = dbias if dbias is not None else torch.empty_like(self.s_w)
         raw = lbt._current_raw_stream(on)
         with self._lock:
-            size, space = self._space.get(raw, (0, None))
+            held = not _capturing()
+            size, space = self._space.get(raw, (0, None)) if held else (0, None)
             need = lbt.linear8_workspace_bytes(dy.shape[0], self.O, self.I)
             if size < need:
                 space = torch.empty(need, dtype=torch.uint8, device=dy.device)
-                self._space[raw] = (need, space)
+                if held:
+                    self._space[raw] = (need, space)
             lbt.linear8_backward(dy, self.q_w, self.s_w, q_x, s_x, self.I, out.get("dx"), out.get("dw"), out.get("dbias"), space, self.status)
         return out
 
@@ -213,9 +227,12 @@ class ResNorm:
         at, (_, desc, _) = self._plan(names, acts, gate, rows_per_gate, on)
         raw, stats = lbt._current_raw_stream(on), None
         if keep:   # a buffer for each stream, shared by one forward pass after the other
-            stats = self._stats.get(raw)
+            held = not _capturing()
+            stats = self._stats.get(raw) if held else None
             if stats is None or stats.shape[0] != x.shape[0]:
-                stats = self._stats[raw] = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device)
+                stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device)
+                if held:
+                    self._stats[raw] = stats
         w_post, b_post, w_pre, b_pre = self._params
         status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._at(gate, on), w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
                                                lbt._at(q, on), q.shape[1] if q is not None else 0, lbt._at(q_scale, on), lbt._at(stats, on), raw)
@@ -271,9 +288,12 @@ class ResNorm:
                 grads.append(0)
         at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate, on)
         raw = lbt._current_raw_stream(on)
-        ws = self._space.get(raw)
+        held = not _capturing()
+        ws = self._space.get(raw) if held else None
         if ws is None or ws.numel() < size:
-            ws = self._space[raw] = torch.empty(size, dtype=torch.uint8, device=x.device)
+            ws = torch.empty(size, dtype=torch.uint8, device=x.device)
+            if held:
+                self._space[raw] = ws
         w_post, b_post, w_pre, _ = self._params
         status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._at(gate, on), w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
                                                 *grads, ws.data_ptr(), size, raw)
@@ -344,7 +364,7 @@ class AdamW:
             if stream is not None or self.device != lbt._device():
                 with lbt._place(self.params[0], stream):
                     return self.step(grad_scale, skip)
-            if not self._replayed and torch._C._cuda_isCurrentStreamCapturing():
+            if not self._replayed and _capturing():
                 self._replayed = True
         if skip is not None or self._replayed:
             self._counting = True

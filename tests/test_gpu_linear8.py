@@ -282,3 +282,29 @@ def test_a_refused_forward_pass_leaves_what_backward_reads():
     assert lin.kept is kept
     out = lin.backward(dy)
     assert all(torch.equal(out[k], want[k]) for k in want)
+
+
+def test_graphs_of_several_lengths():
+    """Captured passes of growing lengths, with calls outside between them; a graph that is gone takes no other's scratch with it."""
+    lin = lm.Linear8(300, 200, bias=torch.randn(200, device="cuda"), weight=torch.randn(200, 300, device="cuda"))
+    kept = []
+    for M in (70, 9, 400, 33):
+        x, dy = torch.randn(M, 300, device="cuda"), torch.randn(M, 200, device="cuda")
+        want = lin.forward(x, keep=True)
+        grads = lin.backward(dy)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = lin.forward(x)
+            y2 = lin.forward(x, keep=True)
+            out = lin.backward(dy)
+        kept.append((graph, y, y2, out, want, {k: v.clone() for k, v in grads.items()}, x, dy))   # (a graph reads its inputs where they are)
+    del kept[2], graph, y, y2, out
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    for graph, y, y2, out, want, grads, _, _ in kept:
+        for t in (y, y2, *out.values()):
+            t.fill_(7)
+        lin.forward(torch.randn(500, 300, device="cuda"), keep=True)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(y2, want) and all(torch.equal(out[k], grads[k]) for k in grads)

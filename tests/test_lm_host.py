@@ -284,3 +284,24 @@ def test_threads_that_share_a_layer_take_turns(monkeypatch):
     layer.kept = (_Tensor((5, 64), torch.int8, 0), _Tensor((5,), torch.float32, 0))
     both(lambda: layer.backward(y, dx=x, need_dw=False))
     assert not overlaps
+
+
+def test_a_captured_call_keeps_no_scratch(monkeypatch):
+    """Memory that a captured call takes belongs to its graph: kept for later calls it would go when they need more, or be shared with a
+    replay.  Outside of a capture it is kept."""
+    devices = _Devices(monkeypatch)
+    devices.lbt_linear8_backward = devices.lbt_resnorm_backward = lambda *a: lbt.OK
+    x, y = _Tensor((5, 64), torch.bfloat16, 0), _Tensor((5, 32), torch.bfloat16, 0)
+    monkeypatch.setattr(lbt, "linear8_backward", lambda *a: None)
+    monkeypatch.setattr(lbt, "_at", lambda t, device=None: A)
+    for capturing in (True, False):
+        monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: capturing)
+        layer, norm = _layer(0), lm.ResNorm(64)
+        layer.forward(x, out=y)
+        layer.forward(x, out=y, keep=True)
+        layer.backward(y, dx=x, need_dw=False)
+        norm.forward(x, x, out=(x, x), keep=True)
+        norm.backward(x, x, out={"dx": x, "dh": x})
+        for kept in (layer._scratch, layer._own_kept, layer._space, norm._stats, norm._space):
+            assert bool(kept) != capturing
+        assert layer.kept is not None and norm.kept is not None
