@@ -378,7 +378,8 @@ lbt_status lbt_rows8_quantize(const void *x, int x_type, int64_t rows, int64_t c
  * Y[m,o] = s_x[m] s_w[o] sum_i q_x[m,i] q_w[o,i] (+ bias[o], fp32, may be NULL).  q_x, q_w: code rows with ldq = I rounded up
  * to 16.  lbt_linear8_forward quantizes x first and leaves its codes and scales in q_x and s_x (caller's buffers: scratch, or
  * kept for the backward pass); lbt_linear8_matmul starts from codes.  I <= 133144 (127 * 127 * I < 2^31), else
- * LBT_ERR_ACC_RANGE.  dev_status (device int32, may be NULL) receives LBT_ERR_TIMEOUT if a bounded on-chip wait ran out.
+ * LBT_ERR_ACC_RANGE.  dev_status (device int32, may be NULL) receives LBT_ERR_TIMEOUT if a bounded on-chip wait ran out;
+ * the outputs that hang on it are not written.
  */
 lbt_status lbt_linear8_forward(const void *x, int x_type, int64_t ldx, const void *q_w, const float *s_w, const float *bias,
                                void *y, int y_type, int64_t ldy, int64_t M, int64_t O, int64_t I, void *q_x, float *s_x,
@@ -510,6 +511,15 @@ lbt_status lbt_selftest_wait_timeout(int32_t *dev_status, uint32_t limit_us, voi
  * *dev_status becomes LBT_ERR_TIMEOUT when the wait gives up.  Nothing faults and nothing is left running.
  */
 lbt_status lbt_selftest_barrier_timeout(int32_t *dev_status, uint32_t limit_us, void *cuda_stream);
+
+/*
+ * The same for the 8-bit layer's product whose reduction a cluster of CTAs shares: CTA `rank` of each cluster waits for a signal
+ * that never comes, with a limit of `limit_us`.  *dev_status becomes LBT_ERR_TIMEOUT and y stays as it was, in the parts that the
+ * other CTAs finish too.  y: fp32 [M,O]; codes and scales as lbt_linear8_matmul takes them.  LBT_ERR_UNSUPPORTED where the product of
+ * this size is not cut into more than `rank` slices.
+ */
+lbt_status lbt_selftest_linear8_timeout(const void *q_x, const float *s_x, const void *q_w, const float *s_w, float *y, int64_t M,
+                                        int64_t O, int64_t I, int rank, uint32_t limit_us, int32_t *dev_status, void *cuda_stream);
 
 /* Static, NUL-terminated name of a status code. */
 const char *lbt_status_string(lbt_status status);

@@ -62,6 +62,11 @@ class Stack:
             layer.load_weight(w)
         return (diff * diff).mean()
 
+    def check(self):
+        """Raises if a product's output is missing (waits for the device)."""
+        for layer in self.layers:
+            layer.check()
+
 
 def train(depth=4, dim=1024, tokens=4096, steps=50, dtype=torch.bfloat16, state_bits=8, lr=1e-3, seed=0, report=None):
     """The losses of `steps` steps on fresh synthetic batches."""
@@ -74,7 +79,9 @@ def train(depth=4, dim=1024, tokens=4096, steps=50, dtype=torch.bfloat16, state_
         target = torch.tanh(x.float() @ teacher)
         losses.append(model.step(x, target))
         if report is not None and (i % 10 == 0 or i + 1 == steps):
+            model.check()
             report(i, float(losses[-1]))
+    model.check()
     return [float(v) for v in losses]
 
 

@@ -54,6 +54,8 @@ struct L8Args {
     int out_type;
     int vec, vec4;         // rows of the output begin on 32-byte boundaries; four consecutive elements can be stored at once
     int wait_prev;         // chained behind the kernel that writes the operands
+    int lost;              // 128 x 128 kernel: the CTA of each cluster whose first load is never signalled (self-test), -1: none
+    uint64_t limit_ns;     // after which an on-chip wait gives up
     int32_t* status;
 };
 
@@ -63,11 +65,11 @@ struct Bars {
     volatile uint32_t abort;
 };
 
-__device__ __forceinline__ bool wait_for(Bars* b, uint64_t* bar, uint32_t parity, int32_t* status, bool relaxed = false) {
+__device__ __forceinline__ bool wait_for(Bars* b, uint64_t* bar, uint32_t parity, const L8Args& a, bool relaxed = false) {
     if (b->abort) return false;
-    if (relaxed ? mbar_wait_bounded_relaxed(bar, parity, kLimitNs) : mbar_wait_bounded(bar, parity, kLimitNs)) return true;
+    if (relaxed ? mbar_wait_bounded_relaxed(bar, parity, a.limit_ns) : mbar_wait_bounded(bar, parity, a.limit_ns)) return true;
     b->abort = 1u;
-    if (status != nullptr) atomicCAS(status, (int32_t)LBT_OK, (int32_t)LBT_ERR_TIMEOUT);
+    if (a.status != nullptr) atomicCAS(a.status, (int32_t)LBT_OK, (int32_t)LBT_ERR_TIMEOUT);
     return false;
 }
 
@@ -180,6 +182,11 @@ __device__ __forceinline__ uint4 ld_cluster_words(uint32_t addr) {   // four wor
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v.w) : "r"(addr + 384));
     return v;
 }
+__device__ __forceinline__ uint32_t ld_cluster_word(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
 constexpr int kTileWarps = 8;     // the last thousand instructions of a tile are its warps' latency: eight share them (four: +1.4 us)
 constexpr int kParkPitch = 132;   // words of a parked row: 16-byte accesses of neighbouring rows without bank conflicts
 static_assert(128 * kParkPitch * 4 <= kRing, "the parked accumulator takes the operand ring's place");
@@ -210,13 +217,17 @@ __device__ __forceinline__ TileFactors tile_factors(const L8Args& a, int first, 
 
 // Rows of the parked tile -> rows row0 + ... of the output.
 template <typename T>
-__device__ __forceinline__ void finish_rows(const L8Args& a, const TileFactors& f, const uint32_t* parked, int64_t row0, int warp, int lane) {
+__device__ __forceinline__ void finish_rows(const L8Args& a, const TileFactors& f, const uint32_t* parked, const volatile uint32_t* abort, int64_t row0,
+                                            int warp, int lane) {
     const int first = f.first, last = f.last, c0 = f.c0, step = f.step;
     const uint32_t park = smem_u32(parked);
     uint32_t from[8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) from[r] = a.splits > 1 ? map_to_cta(park, (uint32_t)min(r, a.splits - 1)) : park;
     T* out = static_cast<T*>(a.out) + row0 * a.ldo;
+    // whether CTA `lane` of the cluster lost a signal: then its part is not there, and no row may be stored (looked at behind the parts' loads)
+    uint32_t lost = 0u;
+    if (a.splits > 1 && lane < a.splits) lost = ld_cluster_word(map_to_cta(smem_u32(const_cast<const uint32_t*>(abort)), (uint32_t)lane));
     constexpr int kRows = 4;                    // rows whose parts are on their way together
 #pragma unroll 1
     for (int i = 0; first + warp + kTileWarps * i < last; i += kRows) {
@@ -248,6 +259,7 @@ __device__ __forceinline__ void finish_rows(const L8Args& a, const TileFactors& 
                         if (u < have) take(u, v[u]);
                 }
         }
+        if (__any_sync(0xFFFFFFFFu, lost != 0u)) return;
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
             const int m = first + warp + kTileWarps * (i + u);
@@ -302,7 +314,7 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         b->abort = 0u;
         fence_mbar_init();
         for (int i = 0; i < ahead; ++i) {
-            mbar_arrive_expect_tx(&b->full[i], (uint32_t)a.stage_bytes);
+            mbar_arrive_expect_tx(&b->full[i], (uint32_t)a.stage_bytes + (i == 0 && split == a.lost ? 16u : 0u));
             if (a.swapped) load_a(i, i); else load_b(i, i);
         }
     }
@@ -319,7 +331,7 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 if (a.swapped) load_b(i, i); else load_a(i, i);
             for (int i = ahead; i < n_steps; ++i) {
                 const int s = i % a.stages;
-                if (!wait_for(b, &b->empty[s], (uint32_t)((i / a.stages) & 1) ^ 1u, a.status)) break;
+                if (!wait_for(b, &b->empty[s], (uint32_t)((i / a.stages) & 1) ^ 1u, a)) break;
                 mbar_arrive_expect_tx(&b->full[s], (uint32_t)a.stage_bytes);
                 load_a(i, s);
                 load_b(i, s);
@@ -332,7 +344,7 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             bool ok = true;
             for (int i = 0; i < n_steps && ok; ++i) {
                 const int s = i % a.stages;
-                ok = wait_for(b, &b->full[s], (uint32_t)(i / a.stages) & 1u, a.status);
+                ok = wait_for(b, &b->full[s], (uint32_t)(i / a.stages) & 1u, a);
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint32_t pa = smem_u32(ring + s * a.stage_bytes), pb = pa + kBox;
@@ -353,8 +365,8 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const TileFactors factors =
         tile_factors(a, split * each, (int)min((int64_t)(split * each + each), a.rows - row0), row0, a.swapped ? m0 : n0, warp, lane);
     bool ok = true;
-    if (n_steps > 0 && warp == 1) ok = wait_for(b, &b->tmem_full[0], 0u, a.status);   // one warp polls, the others rest at the barrier
-    ok = __syncthreads_and(ok) != 0;   // uniform; without it a lost signal ends in the error word and no output
+    if (n_steps > 0 && warp == 1) ok = wait_for(b, &b->tmem_full[0], 0u, a);   // one warp polls, the others rest at the barrier
+    ok = __syncthreads_and(ok) != 0;   // uniform; without it a lost signal ends in the error word and no output of the cluster
     tc_fence_after_sync();
     const int quarter = warp & 3, tmem_lane = quarter * 32 + lane;   // the TMEM lanes a warp may read; warps 4..7 take every other 32 columns
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
@@ -381,9 +393,9 @@ l8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     }
     if (a.splits > 1) cluster_sync_all(); else __syncthreads();
     if (ok) {
-        if (a.out_type == LBT_BF16) finish_rows<__nv_bfloat16>(a, factors, park, row0, warp, lane);
-        else if (a.out_type == LBT_F16) finish_rows<__half>(a, factors, park, row0, warp, lane);
-        else finish_rows<float>(a, factors, park, row0, warp, lane);
+        if (a.out_type == LBT_BF16) finish_rows<__nv_bfloat16>(a, factors, park, &b->abort, row0, warp, lane);
+        else if (a.out_type == LBT_F16) finish_rows<__half>(a, factors, park, &b->abort, row0, warp, lane);
+        else finish_rows<float>(a, factors, park, &b->abort, row0, warp, lane);
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -438,7 +450,7 @@ l8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 tile_at(a, t, tm, tn);
                 const int m0 = tm * 256 + (int)rank * 128, n0 = tn * 256 + (int)rank * 128;
                 for (int i = 0; i < a.steps; ++i) {
-                    ok = wait_for(b, &b->empty[s], ph ^ 1u, a.status);
+                    ok = wait_for(b, &b->empty[s], ph ^ 1u, a);
                     if (!ok) break;
                     uint8_t* dst = ring + s * 2 * kBox;
                     if (rank == 0) mbar_arrive_expect_tx(&b->full[s], 4u * kBox);   // the bytes of both CTAs
@@ -463,11 +475,11 @@ l8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             bool ok = true;
             for (int t = pair; t < a.total && ok; t += pairs, ++acc) {
                 const uint32_t buf = acc & 1u;
-                ok = wait_for(b, &b->tmem_empty[buf], ((acc >> 1) & 1u) ^ 1u, a.status);
+                ok = wait_for(b, &b->tmem_empty[buf], ((acc >> 1) & 1u) ^ 1u, a);
                 if (!ok) break;
                 tc_fence_after_sync();
                 for (int i = 0; i < a.steps; ++i) {
-                    ok = wait_for(b, &b->full[s], ph, a.status);
+                    ok = wait_for(b, &b->full[s], ph, a);
                     if (!ok) break;
                     tc_fence_after_sync();
                     const uint64_t da = da0 + (uint64_t)(s * (2 * kBox >> 4)), db = db0 + (uint64_t)(s * (2 * kBox >> 4));
@@ -489,7 +501,7 @@ l8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             int tm, tn;
             tile_at(a, t, tm, tn);
             const uint32_t buf = acc & 1u;
-            bool ok = wait_for(b, &b->tmem_full[buf], (acc >> 1) & 1u, a.status, true);
+            bool ok = wait_for(b, &b->tmem_full[buf], (acc >> 1) & 1u, a, true);
             ok = __all_sync(0xFFFFFFFFu, ok) != 0;
             if (!ok) break;
             tc_fence_after_sync();
@@ -985,6 +997,8 @@ struct Product {
     const float *row_scale, *col_scale, *bias;
     void* out; int out_type; int64_t ldo;
     bool behind;                              // the launch ahead writes operands of this one
+    int lost = -1;                            // self-test: L8Args
+    uint64_t limit_ns = kLimitNs;
 };
 
 lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
@@ -999,6 +1013,7 @@ lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
     a.vec = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0 && (p.ldo * type_size(p.out_type)) % 32 == 0;
     a.vec4 = misaligned(p.out, 4 * type_size(p.out_type)) || p.ldo % 4 != 0 ? 0 : 1;
     a.wait_prev = p.behind ? 1 : 0;
+    a.lost = p.lost; a.limit_ns = p.limit_ns;
     a.splits = 1;
     CUtensorMap tmA, tmB;
     const int64_t big = ((p.rows + 255) / 256) * ((p.cols + 255) / 256);
@@ -1012,6 +1027,7 @@ lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
         attr[n_attr++].val.programmaticStreamSerializationAllowed = 1;
     }
     if (big > kNumSMs / 2) {
+        if (p.lost >= 0) return LBT_ERR_UNSUPPORTED;
         a.tiles_m = (int)((p.rows + 255) / 256);
         a.tiles_n = (int)((p.cols + 255) / 256);
         a.total = a.tiles_m * a.tiles_n;
@@ -1036,6 +1052,7 @@ lbt_status launch(const Product& p, int32_t* status, cudaStream_t stream) {
     // Clusters share a tile while all their CTAs are resident at once (256: 288 CTAs in clusters of four left some for a second
     // round, 11 us late) and each has four steps of the reduction.
     while (a.splits < 8 && a.total * a.splits * 2 <= 256 && a.steps >= a.splits * 2 * 4) a.splits *= 2;
+    if (p.lost >= a.splits) return LBT_ERR_UNSUPPORTED;
     const void* A = a.swapped ? p.B : p.A;
     const void* B = a.swapped ? p.A : p.B;
     if (!code_map(&tmA, A, a.swapped ? p.b_pitch : p.a_pitch, a.swapped ? p.b_rows : p.a_rows, 128) ||
@@ -1198,10 +1215,8 @@ extern "C" lbt_status lbt_rows8_quantize(const void* x, int x_type, int64_t rows
     return quantize_rows_any(x, x_type, rows, cols, ld, q, ldq, scale, as_stream(cuda_stream));
 }
 
-static lbt_status forward_product(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, void* y, int y_type,
-                                  int64_t ldy, int64_t M, int64_t O, int64_t I, bool behind, int32_t* status, cudaStream_t stream) {
-    if (few_fits(M, I))
-        return few_from_codes(few_args(const_cast<void*>(q_x), const_cast<float*>(s_x), q_w, s_w, bias, y, y_type, ldy, M, O, I), behind, stream);
+static Product forward_operands(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, void* y, int y_type,
+                                int64_t ldy, int64_t M, int64_t O, int64_t I, bool behind) {
     Product p{};
     p.mode = kForward;
     p.A = q_x; p.a_pitch = pitch16(I); p.a_rows = M;
@@ -1210,7 +1225,14 @@ static lbt_status forward_product(const void* q_x, const float* s_x, const void*
     p.row_scale = s_x; p.col_scale = s_w; p.bias = bias;
     p.out = y; p.out_type = y_type; p.ldo = ldy;
     p.behind = behind;
-    return launch(p, status, stream);
+    return p;
+}
+
+static lbt_status forward_product(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, void* y, int y_type,
+                                  int64_t ldy, int64_t M, int64_t O, int64_t I, bool behind, int32_t* status, cudaStream_t stream) {
+    if (few_fits(M, I))
+        return few_from_codes(few_args(const_cast<void*>(q_x), const_cast<float*>(s_x), q_w, s_w, bias, y, y_type, ldy, M, O, I), behind, stream);
+    return launch(forward_operands(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I, behind), status, stream);
 }
 
 static lbt_status check_forward(const void* q_x, const float* s_x, const void* q_w, const float* s_w, const float* bias, const void* y,
@@ -1247,6 +1269,18 @@ extern "C" lbt_status lbt_linear8_matmul(const void* q_x, const float* s_x, cons
     const lbt_status rc = check_forward(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I);
     if (rc != LBT_OK || M == 0) return rc;
     return forward_product(q_x, s_x, q_w, s_w, bias, y, y_type, ldy, M, O, I, false, dev_status, as_stream(cuda_stream));
+}
+
+extern "C" lbt_status lbt_selftest_linear8_timeout(const void* q_x, const float* s_x, const void* q_w, const float* s_w, float* y, int64_t M,
+                                                   int64_t O, int64_t I, int rank, uint32_t limit_us, int32_t* dev_status, void* cuda_stream) {
+    if (dev_status == nullptr || rank < 0 || limit_us == 0 || limit_us > 1000000u) return LBT_ERR_INVALID_ARG;
+    const lbt_status rc = check_forward(q_x, s_x, q_w, s_w, nullptr, y, LBT_F32, O, M, O, I);
+    if (rc != LBT_OK) return rc;
+    if (M == 0) return LBT_ERR_UNSUPPORTED;
+    Product p = forward_operands(q_x, s_x, q_w, s_w, nullptr, y, LBT_F32, O, M, O, I, false);
+    p.lost = rank;
+    p.limit_ns = (uint64_t)limit_us * 1000ull;
+    return launch(p, dev_status, as_stream(cuda_stream));
 }
 
 extern "C" size_t lbt_linear8_workspace_bytes(int64_t M, int64_t O, int64_t I) {

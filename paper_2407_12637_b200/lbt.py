@@ -33,7 +33,8 @@ EXPORTS = (
     "lbt_rows8_quantize", "lbt_linear8_forward", "lbt_linear8_matmul", "lbt_linear8_backward", "lbt_linear8_workspace_bytes",
     "lbt_resnorm_forward", "lbt_resnorm_backward", "lbt_resnorm_workspace_bytes", "lbt_adamw_step",
     "lbt_adamw_step_ex",
-    "lbt_set_timing_events", "lbt_selftest_wait_timeout", "lbt_selftest_barrier_timeout", "lbt_status_string",
+    "lbt_set_timing_events", "lbt_selftest_wait_timeout", "lbt_selftest_barrier_timeout",
+    "lbt_selftest_linear8_timeout", "lbt_status_string",
 )
 TIME_STATS, TIME_QUANTIZE, TIME_EXPAND, TIME_DGRAD, TIME_WGRAD, TIME_FORWARD, TIME_FWD_QUANT = range(7)
 
@@ -158,6 +159,7 @@ def lib() -> C.CDLL:
         l.lbt_set_timing_events.argtypes = [i32, vp, vp]
         l.lbt_selftest_wait_timeout.argtypes = [vp, C.c_uint32, vp]
         l.lbt_selftest_barrier_timeout.argtypes = [vp, C.c_uint32, vp]
+        l.lbt_selftest_linear8_timeout.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i32, C.c_uint32, vp, vp]
         for name in EXPORTS:
             getattr(l, name).restype = sz if name.endswith("workspace_bytes") else C.c_int32
         l.lbt_status_string.restype = C.c_char_p
@@ -427,6 +429,14 @@ def linear8_matmul(q_x, s_x, q_w, s_w, y, I, bias=None, dev_status=None, stream=
         raise ValueError("y: one row per row of codes")
     _check(lib().lbt_linear8_matmul(_codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"),
                                     _floats(bias, O, "bias"), py, ty, ldy, M, O, I, _at(dev_status), _raw_stream(y, stream)), "lbt_linear8_matmul")
+
+
+def selftest_linear8_timeout(q_x, s_x, q_w, s_w, y, I, rank, dev_status, limit_us: int, stream=None):
+    """linear8_matmul (fp32 y) in which CTA `rank` of each cluster waits in vain; *dev_status becomes ERR_TIMEOUT and y stays as it was."""
+    M, O = s_x.numel(), s_w.numel()
+    _check(lib().lbt_selftest_linear8_timeout(_codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"),
+                                              _floats(y, M * O, "y"), M, O, I, int(rank), int(limit_us), _at(dev_status), _raw_stream(y, stream)),
+           "lbt_selftest_linear8_timeout")
 
 
 def linear8_workspace_bytes(M, O, I) -> int:

@@ -51,12 +51,20 @@ class Linear8:
         with lbt._place(q_w):   # (addresses of the layer's own tensors, whose storage stays)
             self._weights = (lbt._codes(q_w, self.O, self.I, "q_w"), lbt._floats(s_w, self.O, "s_w"), lbt._floats(bias, self.O, "bias"))
         self.q_w, self.s_w, self.bias, self.kept = q_w, s_w, bias, None
-        self.status = torch.zeros(1, dtype=torch.int32, device=q_w.device)   # lbt.ERR_TIMEOUT if a bounded on-chip wait ran out
+        self.status = torch.zeros(1, dtype=torch.int32, device=q_w.device)   # lbt.ERR_TIMEOUT if a bounded on-chip wait ran out (check)
         self._status = self.status.data_ptr()
         # never shared between streams: codes and scales of x that are not kept (rows, buffer, two addresses), those that were
         # made here to be kept (shared by one forward pass after the other), and the backward pass's workspace
         self._scratch, self._own_kept, self._space = {}, {}, {}
         self._lock = threading.Lock()   # a pass uses them for as long as it enqueues (the library's call lets other threads run)
+
+    def check(self):
+        """Raises LbtError if a bounded on-chip wait of a product ran out since the last check (waits for the device): the outputs
+        that hang on it were not written.  Nothing else says so: a training or serving loop checks now and then."""
+        status = int(self.status)
+        if status:
+            self.status.zero_()
+            raise lbt.LbtError(status, "Linear8")
 
     def load_weight(self, weight, stream=None):
         """Quantizes the weights [O, I] (after each optimizer step)."""

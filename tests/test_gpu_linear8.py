@@ -308,3 +308,25 @@ def test_graphs_of_several_lengths():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want) and torch.equal(y2, want) and all(torch.equal(out[k], grads[k]) for k in grads)
+
+
+@pytest.mark.parametrize("M,I,O,rank", [(128, 8192, 256, 0), (128, 8192, 256, 7), (32, 4096, 300, 3), (200, 300, 257, 0)])   # (the last: one slice)
+def test_a_lost_signal_stores_nothing(M, I, O, rank):
+    """One CTA of a cluster that waits in vain: an error code, no output from the CTAs that would add its part, and a usable context."""
+    x, w, _, _ = _make(M, I, O, torch.float32, 13)
+    lin = lm.Linear8(I, O, weight=w.cuda())
+    want = lin.forward(x.cuda(), keep=True)
+    q, s = lin.kept
+    y = torch.full((M, O), 7.0, device="cuda")
+    lbt.selftest_linear8_timeout(q, s, lin.q_w, lin.s_w, y, I, rank, lin.status, 2000)
+    torch.cuda.synchronize()
+    assert (y == 7).all()
+    with pytest.raises(lbt.LbtError) as e:
+        lin.check()
+    assert e.value.status == lbt.ERR_TIMEOUT
+    lin.check()   # (said once)
+    assert torch.equal(lin.forward(x.cuda()), want)
+    lin.check()
+    with pytest.raises(lbt.LbtError) as e:
+        lbt.selftest_linear8_timeout(q, s, lin.q_w, lin.s_w, y, I, 8, lin.status, 2000)
+    assert e.value.status == lbt.ERR_UNSUPPORTED
