@@ -225,9 +225,7 @@ __device__ __forceinline__ void finish_rows(const L8Args& a, const TileFactors& 
 #pragma unroll
     for (int r = 0; r < 8; ++r) from[r] = a.splits > 1 ? map_to_cta(park, (uint32_t)min(r, a.splits - 1)) : park;
     T* out = static_cast<T*>(a.out) + row0 * a.ldo;
-    // whether CTA `lane` of the cluster lost a signal: then its part is not there, and no row may be stored (looked at behind the parts' loads)
-    uint32_t lost = 0u;
-    if (a.splits > 1 && lane < a.splits) lost = ld_cluster_word(map_to_cta(smem_u32(const_cast<const uint32_t*>(abort)), (uint32_t)lane));
+    uint32_t lost = 0u;                         // whether CTA `lane` of the cluster lost a signal: its part is not there, no row may be stored
     constexpr int kRows = 4;                    // rows whose parts are on their way together
 #pragma unroll 1
     for (int i = 0; first + warp + kTileWarps * i < last; i += kRows) {
@@ -247,6 +245,8 @@ __device__ __forceinline__ void finish_rows(const L8Args& a, const TileFactors& 
                     take(u, a.vec4 ? *reinterpret_cast<const uint4*>(p) : make_uint4(p[0], p[32], p[64], p[96]));
                 }
         } else {
+            // (loaded and looked at beside the first rows' parts: 0.1 us of 11.5; an abort word pushed to all CTAs and read behind the barrier 0.2)
+            if (i == 0 && lane < a.splits) lost = ld_cluster_word(map_to_cta(smem_u32(const_cast<const uint32_t*>(abort)), (uint32_t)lane));
 #pragma unroll
             for (int r = 0; r < 8; ++r)
                 if (r < a.splits) {
@@ -259,7 +259,7 @@ __device__ __forceinline__ void finish_rows(const L8Args& a, const TileFactors& 
                         if (u < have) take(u, v[u]);
                 }
         }
-        if (__any_sync(0xFFFFFFFFu, lost != 0u)) return;
+        if (i == 0 && __any_sync(0xFFFFFFFFu, lost != 0u)) return;
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
             const int m = first + warp + kTileWarps * (i + u);
