@@ -583,7 +583,7 @@ __device__ __forceinline__ void load_raw(const T* row, int64_t c, int64_t cols, 
 template <typename T, int kPerRow>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 6 : 4)
 rows8_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, bool vec, uint8_t* __restrict__ q, int64_t ldq,
-             float* __restrict__ scale) {
+             int64_t end, float* __restrict__ scale) {   // end: columns and padding (what lies behind them in a row is not this matrix's)
     constexpr int kHeld = 4;
     griddep_launch_dependents();
     const int64_t row = kPerRow == 256 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -621,9 +621,9 @@ rows8_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, bo
         const int64_t c = (int64_t)(g * kPerRow + t) * 8;
         float f[8];
         unpack(held[g], f);
-        if (c < ldq) *reinterpret_cast<uint2*>(dst + c) = codes8(f, factor);
+        if (c < end) *reinterpret_cast<uint2*>(dst + c) = codes8(f, factor);
     }
-    for (int64_t c = (int64_t)(kHeld * kPerRow + t) * 8; c < ldq; c += kPerRow * 8) {
+    for (int64_t c = (int64_t)(kHeld * kPerRow + t) * 8; c < end; c += kPerRow * 8) {
         float f[8];
         load_group(src, c, cols, vec, f);
         *reinterpret_cast<uint2*>(dst + c) = codes8(f, factor);
@@ -1080,8 +1080,8 @@ template <typename T>
 lbt_status quantize_rows(const T* x, int type, int64_t rows, int64_t cols, int64_t ld, void* q, int64_t ldq, float* scale, cudaStream_t stream) {
     const bool vec = vec_rows(x, ld, type);
     uint8_t* dst = static_cast<uint8_t*>(q);
-    if (cols <= 1024) rows8_kernel<T, 32><<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(x, rows, cols, ld, vec, dst, ldq, scale);
-    else rows8_kernel<T, 256><<<(unsigned)rows, 256, 0, stream>>>(x, rows, cols, ld, vec, dst, ldq, scale);
+    if (cols <= 1024) rows8_kernel<T, 32><<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(x, rows, cols, ld, vec, dst, ldq, pitch16(cols), scale);
+    else rows8_kernel<T, 256><<<(unsigned)rows, 256, 0, stream>>>(x, rows, cols, ld, vec, dst, ldq, pitch16(cols), scale);
     return launch_status();
 }
 

@@ -359,13 +359,14 @@ __global__ void __launch_bounds__(kBlock<kG>, kForwardBlocks<kG, kNV>) resnorm_f
 #pragma unroll
                     for (int i = 0; i < 8; ++i) k[i] = code8(r[g][i], factor);
                     uint8_t* to = a.q + row * a.ldq;
+                    const int q_end = (D + 15) & ~15;   // (what lies behind the padding is not this matrix's)
                     if constexpr (kEven<P>) {
                         const int c = column<P, kG>(g, 0, t);
-                        if (c < a.ldq) *reinterpret_cast<uint2*>(to + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
+                        if (c < q_end) *reinterpret_cast<uint2*>(to + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
                     } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            if (column<P, kG>(g, i, t) < a.ldq) to[column<P, kG>(g, i, t)] = (uint8_t)k[i];
+                            if (column<P, kG>(g, i, t) < q_end) to[column<P, kG>(g, i, t)] = (uint8_t)k[i];
                     }
                 }
             }

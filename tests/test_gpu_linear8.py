@@ -330,3 +330,22 @@ def test_a_lost_signal_stores_nothing(M, I, O, rank):
     with pytest.raises(lbt.LbtError) as e:
         lbt.selftest_linear8_timeout(q, s, lin.q_w, lin.s_w, y, I, 8, lin.status, 2000)
     assert e.value.status == lbt.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("cols", [1, 100, 128, 1000, 1024, 1030, 9000])
+def test_code_rows_of_a_wider_matrix(cols):
+    """Rows of codes inside a wider matrix: zeros up to the next multiple of 16 columns, what lies behind them stays as it was."""
+    rows, pitch = 5, lbt.pitch8(cols)
+    ldq = pitch + 48
+    x = torch.randn(rows, cols, device="cuda")
+    q, want = torch.full((rows, ldq), 77, dtype=torch.int8, device="cuda"), torch.empty(rows, pitch, dtype=torch.int8, device="cuda")
+    s, want_s = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    lbt.rows8_quantize(x, want, want_s)
+    assert not want[:, cols:].any()
+    for kind in (torch.float32, torch.bfloat16):
+        xk = x.to(kind)
+        lbt.rows8_quantize(xk, want, want_s)
+        q.fill_(77)
+        assert lbt.lib().lbt_rows8_quantize(xk.data_ptr(), lbt.TYPES[kind], rows, cols, cols, q.data_ptr(), ldq, s.data_ptr(), None) == lbt.OK
+        torch.cuda.synchronize()
+        assert torch.equal(q[:, :pitch], want) and torch.equal(s, want_s) and (q[:, pitch:] == 77).all()

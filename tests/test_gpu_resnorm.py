@@ -5,6 +5,7 @@ threads), every output a dozen roundings: 2^-24 (16 + sqrt(D)) of the magnitudes
 type.  Magnitudes that enter: what the formula gives with every term's absolute value, bounded here by the row's (or the
 column's) largest term.  A sum over M rows adds 2^-24 sqrt(M) per term in magnitude; types of 16 bits round once at the end.
 """
+import ctypes as C
 import math
 
 import pytest
@@ -224,3 +225,18 @@ def test_zero_rows_and_refusals():
     with pytest.raises(lbt.LbtError) as e:
         lm.ResNorm(40000).forward(wide, wide)
     assert e.value.status == lbt.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("D", [1, 100, 128, 300, 1111, 4096, 8200, 20001])
+def test_codes_in_a_wider_matrix(D):
+    M, pitch = 4, lbt.pitch8(D)
+    ldq = pitch + 48
+    c, t, norm, _, _ = _case(M, D, torch.float32, torch.float32, "rms", "one", 0, 6)
+    r, want, want_s = norm.forward_codes(t["x"], t["h"], t["gate"])
+    q, s = torch.full((M, ldq), 77, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    d = lbt.ResnormDesc(M, D, 0, lbt.F32, lbt.F32, lbt.NORM_RMS, 1, 1e-6, 1e-6, 0.9, 0.6)
+    at = lambda v: v.data_ptr()  # noqa: E731
+    assert lbt.lib().lbt_resnorm_forward(C.addressof(d), at(t["x"]), at(t["h"]), at(t["gate"]), at(t["w1"]), None, at(t["w2"]), None, at(r), None,
+                                         at(q), ldq, at(s), None, None) == lbt.OK
+    torch.cuda.synchronize()
+    assert torch.equal(q[:, :pitch], want) and torch.equal(s, want_s) and (q[:, pitch:] == 77).all()
