@@ -872,8 +872,8 @@ extern "C" lbt_status lbt_resnorm_backward(const lbt_resnorm_desc* d, const void
     if (ws == nullptr || ws_bytes < w.total) return LBT_ERR_WORKSPACE;
     const cudaStream_t stream = as_stream(cuda_stream);
     void* outs[4] = {dw_post, db_post, dw_pre, db_pre};
-    if (a.M == 0) {   // no rows: the sums are zero (and there are no gate rows)
-        for (void* o : outs)
+    if (a.M == 0) {   // no rows: the sums are zero (there is a gate row only where it is one for all)
+        for (void* o : {dw_post, db_post, dw_pre, db_pre, d->rows_per_gate == 0 ? dgate : nullptr})
             if (o != nullptr) LBT_CUDA_TRY(cudaMemsetAsync(o, 0, (size_t)a.D * pe, stream));
         return LBT_OK;
     }

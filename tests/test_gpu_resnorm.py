@@ -240,3 +240,17 @@ def test_codes_in_a_wider_matrix(D):
                                          at(q), ldq, at(s), None, None) == lbt.OK
     torch.cuda.synchronize()
     assert torch.equal(q[:, :pitch], want) and torch.equal(s, want_s) and (q[:, pitch:] == 77).all()
+
+
+def test_gradient_of_a_gate_without_rows():
+    """No tokens and one gate row for all of them: its gradient is zero, as the parameters' are."""
+    x = torch.empty(0, 64, device="cuda")
+    for kind in ("rms", "layer"):
+        norm = lm.ResNorm(64, kind, w_post=torch.ones(64, device="cuda"), w_pre=torch.ones(64, device="cuda"))
+        for gate in (torch.ones(64, device="cuda"), torch.ones(1, 64, device="cuda")):
+            norm.forward(x, x, gate, keep=True)
+            out = norm.backward(x, x, out={"dgate": torch.full_like(gate, 5.0)})
+            assert not out["dgate"].any() and not out["dw_pre"].any()
+        none = torch.empty(0, 64, device="cuda")   # (no rows, no gate rows)
+        norm.forward(x, x, none, 3, keep=True)
+        assert norm.backward(x, x)["dgate"].shape == (0, 64)
