@@ -1108,18 +1108,23 @@ FewArgs few_args(void* q_x, float* s_x, const void* q_w, const float* s_w, const
     return a;
 }
 
-// Blocks of eight warps, two to an SM, while two blocks' codes and pieces fit one; else of sixteen, one to an SM.
-constexpr int kFewCodesOfTwo = 40 * 1024;
+// Blocks of eight warps, two to an SM, while two blocks' codes, pieces and sums fit its 228 KB (each block takes 1 KB more); else of
+// sixteen, one to an SM.  (16 tokens 2048 -> 8192, just beyond: 14.4 us, in blocks of eight that lie alone 16.4; 9 tokens 4096 -> 8192:
+// 18.5 and 20.5.)
+constexpr int few_pieces(int warps) { return kFewAhead * 2 * warps * 32 * 16; }
+constexpr int few_sums(int tiles, int warps) { return 2 * warps * tiles * 8 * 17 * 4; }   // (the kernel's own)
+template <int kTiles> constexpr int kFewCodesOfTwo = 228 * 1024 / 2 - 1024 - 256 - few_pieces(8) - few_sums(kTiles, 8);
+static_assert(few_pieces(16) + few_sums(2, 16) + kFewCodes + 256 <= 227 * 1024, "one block of sixteen warps fits");
 template <typename T, int kTiles, int kWarps>
 lbt_status few_launch(const FewArgs& a, bool behind, cudaStream_t stream) {
-    constexpr int pieces = kFewAhead * 2 * kWarps * 32 * 16;
+    constexpr int pieces = few_pieces(kWarps);
     constexpr int kDevices = 64;
     static std::atomic<bool> known[kDevices];   // the attribute belongs to the device that is current when it is set
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return LBT_ERR_CUDA;
     if (!known[dev].load()) {
         if (cudaFuncSetAttribute(l8_few_kernel<T, kTiles, kWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 pieces + (kWarps == 8 ? kFewCodesOfTwo : kFewCodes)) != cudaSuccess)
+                                 pieces + (kWarps == 8 ? kFewCodesOfTwo<kTiles> : kFewCodes)) != cudaSuccess)
             return LBT_ERR_CUDA;
         known[dev].store(true);
     }
@@ -1139,7 +1144,7 @@ lbt_status few_launch(const FewArgs& a, bool behind, cudaStream_t stream) {
 
 template <typename T, int kTiles>
 lbt_status few_any(const FewArgs& a, bool behind, cudaStream_t stream) {
-    return a.M * a.tokens_pitch <= kFewCodesOfTwo ? few_launch<T, kTiles, 8>(a, behind, stream) : few_launch<T, kTiles, 16>(a, behind, stream);
+    return a.M * a.tokens_pitch <= kFewCodesOfTwo<kTiles> ? few_launch<T, kTiles, 8>(a, behind, stream) : few_launch<T, kTiles, 16>(a, behind, stream);
 }
 
 lbt_status few_from_codes(FewArgs a, bool behind, cudaStream_t stream) {

@@ -349,3 +349,20 @@ def test_code_rows_of_a_wider_matrix(cols):
         assert lbt.lib().lbt_rows8_quantize(xk.data_ptr(), lbt.TYPES[kind], rows, cols, cols, q.data_ptr(), ldq, s.data_ptr(), None) == lbt.OK
         torch.cuda.synchronize()
         assert torch.equal(q[:, :pitch], want) and torch.equal(s, want_s) and (q[:, pitch:] == 77).all()
+
+
+@pytest.mark.parametrize("M,I,O", [(1, 50000, 130), (8, 6000, 130), (16, 3000, 257), (9, 4096, 384), (16, 2112, 100), (16, 1920, 384), (3, 13500, 100), (1, 41000, 70)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=str)
+def test_few_tokens_with_long_rows(M, I, O, dtype):
+    """Codes that fill a multiprocessor's shared memory: blocks of sixteen warps, and the longest of eight."""
+    x, w, b, _ = _make(M, I, O, dtype, M + I)
+    guard = Guard()
+    lin = lm.Linear8(I, O, bias=b.cuda(), weight=w.cuda())
+    y = guard.alloc((M, O), dtype)
+    lin.forward(x.cuda(), out=y, keep=True)
+    q_w, s_w = _rows8(w)
+    q_x, s_x = _rows8(x.float())
+    assert torch.equal(lin.kept[0].cpu()[:, :I].double(), q_x) and not lin.kept[0][:, I:].any() and torch.equal(lin.kept[1].cpu(), s_x)
+    _close(y, q_x @ q_w.T, s_x.double()[:, None] * s_w.double(), b, "y")
+    lin.check()
+    guard.check()
