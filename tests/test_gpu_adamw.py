@@ -271,3 +271,38 @@ def test_moments_in_codes_need_their_scales():
         with pytest.raises(ValueError):
             lm.AdamW([p], [g], **given)
     lm.AdamW([p], [g], codes(), codes(), scales, [scales[0].clone()]).step()
+
+
+@pytest.mark.parametrize("dtype,gdtype", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float16), (torch.float16, torch.float32)], ids=str)
+def test_many_blocks_are_the_same_steps(dtype, gdtype):
+    """More than 18 944 blocks of 256 (a warp takes eight at a time): codes, scales and parameters are bit for bit those of the same
+    tensors stepped in pieces of few blocks each."""
+    sizes = [2_000_003, 256 * 9, 1, 256 * 8 - 1, 3_000_007, 17, 256 * 15 + 3, 700_001]
+    assert sum(-(-n // 256) for n in sizes) > 148 * 32 * 4
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    rand = lambda n: torch.randn(n, generator=gen, device="cuda")  # noqa: E731
+    ps, gs, ms, vs, mss, vss = [], [], [], [], [], []
+    for n in sizes:
+        b = -(-n // 256)
+        ps.append(rand(n).to(dtype))
+        gs.append((rand(n).pow(3) * 0.01).to(gdtype))
+        ms.append((rand(n) * 100).clamp(-448, 448).to(torch.float8_e4m3fn))
+        vs.append((rand(n).abs() * 100 + 0.01).clamp(max=448).to(torch.float8_e4m3fn))
+        mss.append(torch.rand(b, generator=gen, device="cuda") * 1e-4)
+        vss.append(torch.rand(b, generator=gen, device="cuda") * 1e-3)
+    copy = lambda ts: [t.clone() for t in ts]  # noqa: E731
+    whole = lm.AdamW(ps, gs, ms, vs, mss, vss, lr=1e-2, step=4)
+    apart = [copy(t) for t in (ps, ms, vs, mss, vss)]
+    cut = 256 * 1000
+    pieces = [(i, at) for i, n in enumerate(sizes) for at in range(0, n, cut)]
+    at = lambda ts: [ts[i][a:a + cut] for i, a in pieces]  # noqa: E731
+    scales_at = lambda ts: [ts[i][a // 256:a // 256 + 1000] for i, a in pieces]  # noqa: E731
+    for step in range(3):
+        for g in gs:
+            g.mul_(0.8).add_(0.001)
+        whole.step()
+        parts = [at(apart[0]), at(gs), at(apart[1]), at(apart[2]), scales_at(apart[3]), scales_at(apart[4])]
+        for k in range(len(pieces)):
+            lm.AdamW(*[[t[k]] for t in parts], lr=1e-2, step=4 + step).step()
+        for a, b in zip((ps, ms, vs, mss, vss), apart):
+            assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b)), step

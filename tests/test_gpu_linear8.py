@@ -366,3 +366,71 @@ def test_few_tokens_with_long_rows(M, I, O, dtype):
     _close(y, q_x @ q_w.T, s_x.double()[:, None] * s_w.double(), b, "y")
     lin.check()
     guard.check()
+
+
+@pytest.mark.parametrize("M,I,O", [(17, 200, 19100), (32, 256, 19200), (64, 130, 24000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=str)
+def test_few_tokens_to_many_channels(M, I, O, dtype):
+    """More channels than 74 tiles of 256 columns hold: tiles of 256 rows, few of them tokens."""
+    x, w, b, _ = _make(M, I, O, dtype, M + I)
+    guard = Guard()
+    lin = lm.Linear8(I, O, bias=b.cuda(), weight=w.cuda())
+    y = guard.alloc((M, O), dtype)
+    lin.forward(x.cuda(), out=y)
+    q_w, s_w = _rows8(w)
+    q_x, s_x = _rows8(x.float())
+    _close(y, q_x @ q_w.T, s_x.double()[:, None] * s_w.double(), b, "y")
+    guard.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16], ids=str)
+@pytest.mark.parametrize("M,I,O", [(2304, 384, 2304), (2500, 130, 2100)])
+def test_many_tiles_with_bias(M, I, O, dtype):
+    """The CTA pairs' epilogue with a bias, fp32 and fp16 outputs, a 16-bit dW."""
+    x, w, b, dy = (t.cuda() for t in _make(M, I, O, dtype, 6))
+    lin = lm.Linear8(I, O, bias=b, weight=w)
+    y = lin.forward(x, keep=True)
+    out = lin.backward(dy, dw_dtype=torch.bfloat16)
+    q_x, s_x, q_w, s_w = lin.kept[0][:, :I].double(), lin.kept[1].double(), lin.q_w[:, :I].double(), lin.s_w.double()
+    q_r, s_r = _rows8(dy.float().cpu() * lin.s_w.cpu())
+    q_c, s_c = _rows8((dy.float().cpu() * lin.kept[1].cpu()[:, None]).T.contiguous())
+    _close(y.cpu(), (q_x @ q_w.T).cpu(), (s_x[:, None] * s_w).cpu(), b.cpu(), "y")
+    _close(out["dx"].cpu(), (q_r.cuda() @ q_w).cpu(), s_r.double()[:, None], None, "dx")
+    _close(out["dw"].cpu(), (q_c.cuda() @ q_x).cpu(), s_c.double()[:, None], None, "dw")
+    s = dy.double()
+    assert ((out["dbias"].double() - s.sum(0)).abs() <= M * 2.0 ** -24 * s.abs().sum(0) + 1e-37).all()
+
+
+@pytest.mark.parametrize("M,I,O", [(0, 64, 48), (1, 200, 150), (16, 200, 150), (40, 130, 77), (300, 515, 150), (2304, 384, 2304)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=str)
+def test_from_codes(M, I, O, dtype):
+    """A product that starts from codes gives the bits of the one that makes them; rows of a wider output at an odd offset."""
+    x, w, b, dy = (t.cuda() for t in _make(M, I, O, dtype, 12))
+    lin = lm.Linear8(I, O, bias=b, weight=w)
+    y = lin.forward(x, keep=True)
+    want = lin.backward(dy)
+    served = lm.Linear8.from_codes(lin.q_w, lin.s_w, I, bias=b)
+    q, s = (t.clone() for t in lin.kept)
+    wide = torch.full((M, O + 21), 7.0, dtype=dtype, device="cuda")
+    served.forward_codes(q, s, out=wide[:, 5:5 + O], keep=True)
+    assert torch.equal(wide[:, 5:5 + O], y) and (wide[:, :5] == 7).all() and (wide[:, 5 + O:] == 7).all()
+    assert torch.equal(served.forward_codes(q, s, dtype=dtype), y)
+    got = served.backward(dy)
+    assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+def test_the_binding_gives_the_layers_bits():
+    M, I, O = 70, 300, 200
+    x, w, b, dy = (t.cuda() for t in _make(M, I, O, torch.bfloat16, 14))
+    lin = lm.Linear8(I, O, bias=b, weight=w)
+    want = lin.forward(x, keep=True)
+    grads = lin.backward(dy)
+    q, s, y = torch.empty_like(lin.kept[0]), torch.empty_like(lin.kept[1]), torch.empty_like(want)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lbt.linear8_forward(x, lin.q_w, lin.s_w, y, q, s, b, status)
+    assert torch.equal(y, want) and torch.equal(q, lin.kept[0]) and torch.equal(s, lin.kept[1])
+    lbt.linear8_matmul(q, s, lin.q_w, lin.s_w, y.zero_(), I, b, status)
+    assert torch.equal(y, want)
+    dx, dw, db = torch.empty_like(x), torch.empty(O, I, device="cuda"), torch.empty(O, device="cuda")
+    lbt.linear8_backward(dy, lin.q_w, lin.s_w, q, s, I, dx, dw, db, dev_status=status)
+    assert torch.equal(dx, grads["dx"]) and torch.equal(dw, grads["dw"]) and torch.equal(db, grads["dbias"]) and int(status) == 0

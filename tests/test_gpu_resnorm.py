@@ -254,3 +254,40 @@ def test_gradient_of_a_gate_without_rows():
         none = torch.empty(0, 64, device="cuda")   # (no rows, no gate rows)
         norm.forward(x, x, none, 3, keep=True)
         assert norm.backward(x, x)["dgate"].shape == (0, 64)
+
+
+@pytest.mark.parametrize("dtype,pdtype", [(torch.bfloat16, torch.float32), (torch.float16, torch.float16), (torch.float32, torch.bfloat16), (torch.float32, torch.float16)], ids=str)
+@pytest.mark.parametrize("M,D,kind,gate,rpg,post", [(70, 256, "rms", "one", 0, True), (300, 1111, "layer", "rows", 40, True), (64, 4096, "rms", "none", 0, False),
+                                                     (40, 2048, "layer", "rows", 7, False), (9, 8192, "rms", "rows", 3, True), (500, 512, "layer", "one", 0, True)])
+def test_types(M, D, kind, gate, rpg, post, dtype, pdtype):
+    """Whole tensors in the Euclidean norm: every element carries a relative error of a rounding to its type (2^-8, 2^-11, 2^-24 at most) and of
+    fp32 arithmetic (about 2^-24 sqrt(D) of the largest terms, well below 2^-15 of the tensor's norm)."""
+    c, t, norm, dr, dy = _case(M, D, dtype, pdtype, kind, gate, rpg, M + D, post=post)
+    r, y = norm.forward(t["x"], t["h"], t["gate"], rpg, keep=True)
+    out = norm.backward(dr, dy)
+    wide = {k: v.double().requires_grad_() if v is not None else None for k, v in t.items()}
+    r64, y64 = _formula(c, *(wide[k] for k in ("x", "h", "gate", "w1", "b1", "w2", "b2")))
+    (r64 * dr.double()).sum().add((y64 * dy.double()).sum()).backward()
+    half = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+    for got, ref in ((r, r64.detach()), (y, y64.detach()), (out["dx"], wide["x"].grad), (out["dh"], wide["h"].grad)):
+        assert (got.double() - ref).norm() <= (half[dtype] + 2.0 ** -15) * ref.norm()
+    for name, key in (("dw_post", "w1"), ("db_post", "b1"), ("dw_pre", "w2"), ("db_pre", "b2"), ("dgate", "gate")):
+        if wide[key] is not None:
+            ref = wide[key].grad
+            assert (out[name].double() - ref).norm() <= (half[pdtype] + 2.0 ** -15) * ref.norm(), name
+        else:
+            assert name not in out
+
+
+def test_the_binding_gives_the_norms_bits():
+    M, D = 70, 256
+    c, t, norm, dr, dy = _case(M, D, torch.bfloat16, torch.bfloat16, "rms", "rows", 30, 15)
+    r, y = norm.forward(t["x"], t["h"], t["gate"], 30, keep=True)
+    want = norm.backward(dr, dy)
+    d = lbt.ResnormDesc(M, D, 30, lbt.BF16, lbt.BF16, lbt.NORM_RMS, 1, 1e-6, 1e-6, 0.9, 0.6)
+    r2, y2, stats = torch.empty_like(r), torch.empty_like(y), torch.empty(M, 4, device="cuda")
+    lbt.resnorm_forward(d, t["x"], t["h"], t["gate"], t["w1"], None, t["w2"], None, r2, y2, stats=stats)
+    dx, dh, dgate, dw1, dw2 = (torch.empty_like(v) for v in (r, r, t["gate"], t["w1"], t["w2"]))
+    lbt.resnorm_backward(d, dr, dy, t["x"], t["h"], t["gate"], t["w1"], None, t["w2"], stats, dx, dh, dgate=dgate, dw_post=dw1, dw_pre=dw2)
+    for a, b in ((r2, r), (y2, y), (dx, want["dx"]), (dh, want["dh"]), (dgate, want["dgate"]), (dw1, want["dw_post"]), (dw2, want["dw_pre"])):
+        assert torch.equal(a, b)
