@@ -374,6 +374,10 @@ class AdamW:
                     return self.step(grad_scale, skip)
             if not self._replayed and _capturing():
                 self._replayed = True
+        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+            raise ValueError("grad_scale: one fp32 value")
+        if skip is not None and (skip.dtype != torch.int32 or skip.numel() != 1):
+            raise ValueError("skip: one int32 value")
         if skip is not None or self._replayed:
             self._counting = True
         self.hyper.step += 1

@@ -305,3 +305,18 @@ def test_a_captured_call_keeps_no_scratch(monkeypatch):
         for kept in (layer._scratch, layer._own_kept, layer._space, norm._stats, norm._space):
             assert bool(kept) != capturing
         assert layer.kept is not None and norm.kept is not None
+
+
+def test_scale_and_skip_of_a_step_have_their_types(monkeypatch):
+    """The kernel reads four bytes of each: a flag of one byte or a scale of another type would be read with what lies beside it."""
+    devices = _Devices(monkeypatch)
+    vec = lambda dtype=torch.float32, n=1: _Tensor((n,), dtype, 0)  # noqa: E731
+    monkeypatch.setattr(torch, "zeros", lambda *a, **k: _Tensor((1,), torch.int64, 0))
+    opt = lm.AdamW([vec(n=9)], [vec(n=9)], [vec(n=9)], [vec(n=9)])
+    for bad in ({"skip": vec(torch.bool)}, {"skip": vec(torch.float32)}, {"skip": vec(torch.int64)}, {"skip": vec(torch.int32, 2)},
+                {"grad_scale": vec(torch.float64)}, {"grad_scale": vec(torch.bfloat16)}, {"grad_scale": vec(torch.float32, 0)}):
+        with pytest.raises(ValueError):
+            opt.step(**bad)
+    assert not devices.calls and opt.hyper.step == 0
+    opt.step(grad_scale=vec(), skip=vec(torch.int32))
+    assert len(devices.calls) == 1 and opt.hyper.step == 1
