@@ -334,14 +334,18 @@ def quantize_grad_fused(dY, state, stats, q_out, stream=None):
 
 
 def _rows(t, name, cols=None, device=None):
-    """Address, element type and leading dimension of a [rows, cols] tensor whose rows are contiguous, on `device` (None: the current one)."""
-    kind, shape, stride = TYPES.get(t.dtype), t.shape, t.stride()
-    if kind is None or len(shape) != 2 or t.get_device() != (_device() if device is None else device) or (stride[1] != 1 and shape[1] > 1):
+    """Address, element type, leading dimension and rows of a [rows, cols] tensor whose rows are contiguous, on `device` (None: the
+    current one)."""
+    kind, shape = TYPES.get(t.dtype), t.shape
+    if kind is None or len(shape) != 2 or t.get_device() != (_device() if device is None else device):
         raise ValueError(f"{name}: a 2-D CUDA tensor of fp32, bf16 or fp16 with contiguous rows, on the device of the call")
-    if cols is not None and shape[1] != cols:
-        raise ValueError(f"{name}: {shape[1]} columns, {cols} expected")
+    (rows, width), (ld, step) = shape, t.stride()
+    if step != 1 and width > 1:
+        raise ValueError(f"{name}: contiguous rows")
+    if cols is not None and width != cols:
+        raise ValueError(f"{name}: {width} columns, {cols} expected")
     # (rows that overlap, as an expanded tensor's do, are refused by the library)
-    return t.data_ptr(), kind, stride[0] if shape[0] > 1 else shape[1]
+    return t.data_ptr(), kind, ld if rows > 1 else width, rows
 
 
 def _at(t, device=None) -> int:
@@ -402,7 +406,7 @@ def _floats(t, n, name, device=None):
 
 def rows8_quantize(x, q, scale, stream=None):
     """8-bit codes and a scale of each row of x [rows, cols]; q: int8 [rows, pitch8(cols)], scale: fp32 [rows]."""
-    px, tx, ld = _rows(x, "x")
+    px, tx, ld, _ = _rows(x, "x")
     rows, cols = x.shape
     _check(lib().lbt_rows8_quantize(px, tx, rows, cols, ld, _codes(q, rows, cols, "q"), pitch8(cols), _floats(scale, rows, "scale"),
                                     _raw_stream(x, stream)), "lbt_rows8_quantize")
@@ -412,9 +416,9 @@ def linear8_forward(x, q_w, s_w, y, q_x, s_x, bias=None, dev_status=None, stream
     """y = x W^T (+ bias) on 8-bit codes; leaves x's codes and scales in q_x, s_x."""
     M, I = x.shape
     O = s_w.numel()
-    px, tx, ldx = _rows(x, "x")
-    py, ty, ldy = _rows(y, "y", O)
-    if y.shape[0] != M:
+    px, tx, ldx, _ = _rows(x, "x")
+    py, ty, ldy, rows = _rows(y, "y", O)
+    if rows != M:
         raise ValueError("y: one row per row of x")
     _check(lib().lbt_linear8_forward(px, tx, ldx, _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"), _floats(bias, O, "bias"), py, ty, ldy,
                                      M, O, I, _codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _at(dev_status), _raw_stream(x, stream)),
@@ -424,8 +428,8 @@ def linear8_forward(x, q_w, s_w, y, q_x, s_x, bias=None, dev_status=None, stream
 def linear8_matmul(q_x, s_x, q_w, s_w, y, I, bias=None, dev_status=None, stream=None):
     """y from codes: q_x [M, pitch8(I)], s_x [M], q_w [O, pitch8(I)], s_w [O]."""
     M, O = s_x.numel(), s_w.numel()
-    py, ty, ldy = _rows(y, "y", O)
-    if y.shape[0] != M:
+    py, ty, ldy, rows = _rows(y, "y", O)
+    if rows != M:
         raise ValueError("y: one row per row of codes")
     _check(lib().lbt_linear8_matmul(_codes(q_x, M, I, "q_x"), _floats(s_x, M, "s_x"), _codes(q_w, O, I, "q_w"), _floats(s_w, O, "s_w"),
                                     _floats(bias, O, "bias"), py, ty, ldy, M, O, I, _at(dev_status), _raw_stream(y, stream)), "lbt_linear8_matmul")
@@ -445,12 +449,12 @@ def linear8_workspace_bytes(M, O, I) -> int:
 
 def linear8_backward(dY, q_w, s_w, q_x, s_x, I, dX=None, dW=None, dbias=None, ws=None, dev_status=None, stream=None):
     """Gradients of linear8_forward from the codes it left; outputs that are None are not computed.  ws None: from torch's allocator."""
-    M, O = dY.shape
-    raw, on = _raw_stream(dY, stream), dY.get_device()
-    pg, tg, ldg = _rows(dY, "dY", s_w.numel(), on)
-    px, tx, ldx = _rows(dX, "dX", I, on) if dX is not None else (0, F32, I)
-    pw, tw, ldw = _rows(dW, "dW", I, on) if dW is not None else (0, F32, I)
-    if (dX is not None and dX.shape[0] != M) or (dW is not None and dW.shape[0] != O):
+    O, on = s_w.numel(), dY.get_device()
+    raw = _raw_stream(dY, stream)
+    pg, tg, ldg, M = _rows(dY, "dY", O, on)
+    px, tx, ldx, rows_x = _rows(dX, "dX", I, on) if dX is not None else (0, F32, I, M)
+    pw, tw, ldw, rows_w = _rows(dW, "dW", I, on) if dW is not None else (0, F32, I, O)
+    if rows_x != M or rows_w != O:
         raise ValueError("dX: one row per row of dY; dW: one row per column of dY")
     if ws is None:
         ws = _scratch(linear8_workspace_bytes(M, O, I), dY.device, stream)

@@ -20,10 +20,11 @@ from . import lbt
 _NO_SCRATCH = (0, None, 0, 0)
 
 
-def _capturing() -> bool:
-    """Whether the current stream is being captured.  What a captured call allocates belongs to its graph, and what a graph's
-    replays write must not be handed on: such calls neither use nor leave scratch that is kept from call to call."""
-    return torch._C._cuda_isCurrentStreamCapturing()
+def _capturing(raw) -> bool:
+    """Whether `raw`, the current stream, is being captured (the default stream, 0, cannot be; asking takes 0.3 us).  What a captured
+    call allocates belongs to its graph, and what a graph's replays write must not be handed on: such calls neither use nor leave
+    scratch that is kept from call to call."""
+    return raw != 0 and torch._C._cuda_isCurrentStreamCapturing()
 
 
 class Linear8:
@@ -84,15 +85,14 @@ class Linear8:
                 return self.forward(x, out, keep)
         if on != self.device:
             raise ValueError(f"the layer's weights are on device {self.device}")
-        px, tx, ldx = lbt._rows(x, "x", self.I, on)
-        M = x.shape[0]
+        px, tx, ldx, M = lbt._rows(x, "x", self.I, on)
         y = x.new_empty((M, self.O)) if out is None else out
-        py, ty, ldy = lbt._rows(y, "y", self.O, on)
-        if y.shape[0] != M:
+        py, ty, ldy, rows = lbt._rows(y, "y", self.O, on)
+        if rows != M:
             raise ValueError("out: one row per row of x")
         raw = lbt._current_raw_stream(on)
         with self._lock:
-            held = not _capturing()
+            held = raw == 0 or not _capturing(raw)
             if keep:
                 mine = self._own_kept.get(raw) if held else None
                 if mine is None or mine[1].shape[0] != M:
@@ -126,8 +126,8 @@ class Linear8:
             raise ValueError(f"the layer's weights are on device {self.device}")
         M = s_x.numel()
         y = torch.empty(M, self.O, dtype=dtype, device=q_x.device) if out is None else out
-        py, ty, ldy = lbt._rows(y, "y", self.O, on)
-        if y.shape[0] != M:
+        py, ty, ldy, rows = lbt._rows(y, "y", self.O, on)
+        if rows != M:
             raise ValueError("out: one row per row of codes")
         q_w, s_w, bias = self._weights
         status = lbt.lib().lbt_linear8_matmul(lbt._codes(q_x, M, self.I, "q_x", on), lbt._floats(s_x, M, "s_x", on), q_w, s_w, bias, py, ty, ldy,
@@ -159,7 +159,7 @@ class Linear8:
             out["dbias"] = dbias if dbias is not None else torch.empty_like(self.s_w)
         raw = lbt._current_raw_stream(on)
         with self._lock:
-            held = not _capturing()
+            held = not _capturing(raw)
             size, space = self._space.get(raw, (0, None)) if held else (0, None)
             need = lbt.linear8_workspace_bytes(dy.shape[0], self.O, self.I)
             if size < need:
@@ -201,16 +201,17 @@ class ResNorm:
         x = acts[0]
         if self.device is not None and on != self.device:
             raise ValueError(f"the norm's parameters are on device {self.device}")
-        rows, dtype, addresses, lds = x.shape[0], x.dtype, [], []
-        for name, t in zip(names, acts):
+        address, kind, ld, rows = lbt._rows(x, names[0], self.dim, on)
+        dtype, addresses, lds = x.dtype, [address], [ld]
+        for name, t in zip(names[1:], acts[1:]):
             if t is None:
                 addresses.append(0)
                 lds.append(0)
                 continue
-            p, _, ld = lbt._rows(t, name, self.dim, on)
-            if t.shape[0] != rows or t.dtype != dtype:
+            address, t_kind, ld, t_rows = lbt._rows(t, name, self.dim, on)
+            if t_rows != rows or t_kind != kind:
                 raise ValueError(f"{name}: {rows} rows of {dtype}")
-            addresses.append(p)
+            addresses.append(address)
             lds.append(ld)
         pd = self.param_dtype or (gate.dtype if gate is not None else dtype)
         if gate is not None:
@@ -235,15 +236,16 @@ class ResNorm:
         at, (_, desc, _) = self._plan(names, acts, gate, rows_per_gate, on)
         raw, stats = lbt._current_raw_stream(on), None
         if keep:   # a buffer for each stream, shared by one forward pass after the other
-            held = not _capturing()
+            held = not _capturing(raw)
             stats = self._stats.get(raw) if held else None
             if stats is None or stats.shape[0] != x.shape[0]:
                 stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device)
                 if held:
                     self._stats[raw] = stats
         w_post, b_post, w_pre, b_pre = self._params
-        status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._at(gate, on), w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
-                                               lbt._at(q, on), q.shape[1] if q is not None else 0, lbt._at(q_scale, on), lbt._at(stats, on), raw)
+        status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._at(gate, on) if gate is not None else 0, w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
+                                               q.data_ptr() if q is not None else 0, q.shape[1] if q is not None else 0,
+                                               q_scale.data_ptr() if q is not None else 0, stats.data_ptr() if keep else 0, raw)
         if status:
             raise lbt.LbtError(status, "lbt_resnorm_forward")
         if keep:
@@ -296,14 +298,14 @@ class ResNorm:
                 grads.append(0)
         at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate, on)
         raw = lbt._current_raw_stream(on)
-        held = not _capturing()
+        held = not _capturing(raw)
         ws = self._space.get(raw) if held else None
         if ws is None or ws.numel() < size:
             ws = torch.empty(size, dtype=torch.uint8, device=x.device)
             if held:
                 self._space[raw] = ws
         w_post, b_post, w_pre, _ = self._params
-        status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._at(gate, on), w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
+        status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._at(gate, on) if gate is not None else 0, w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
                                                 *grads, ws.data_ptr(), size, raw)
         if status:
             raise lbt.LbtError(status, "lbt_resnorm_backward")
@@ -368,11 +370,13 @@ class AdamW:
     def step(self, grad_scale=None, skip=None, stream=None):
         """One step.  grad_scale: device float the gradients are multiplied by; skip: device int32, non-zero = leave everything (the
         step then counts for nothing: the next one corrects as this one would have)."""
+        raw = stream
         if self.params:
             if stream is not None or self.device != lbt._device():
                 with lbt._place(self.params[0], stream):
                     return self.step(grad_scale, skip)
-            if not self._replayed and _capturing():
+            raw = lbt._current_raw_stream(self.device)
+            if not self._replayed and raw != 0 and _capturing(raw):
                 self._replayed = True
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale: one fp32 value")
@@ -382,9 +386,8 @@ class AdamW:
             self._counting = True
         self.hyper.step += 1
         try:
-            raw = lbt._current_raw_stream(self.device) if self.params else stream
-            status = lbt.lib().lbt_adamw_step_ex(self.table, len(self.params), C.addressof(self.hyper), lbt._at(grad_scale, self.device), lbt._at(skip, self.device),
-                                                 self._skipped if self._counting else 0, raw)
+            status = lbt.lib().lbt_adamw_step_ex(self.table, len(self.params), C.addressof(self.hyper), lbt._at(grad_scale, self.device) if grad_scale is not None else 0,
+                                                 lbt._at(skip, self.device) if skip is not None else 0, self._skipped if self._counting else 0, raw)
             if status:
                 raise lbt.LbtError(status, "lbt_adamw_step_ex")
         except Exception:   # refused: nothing was enqueued

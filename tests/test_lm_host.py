@@ -294,6 +294,7 @@ def test_a_captured_call_keeps_no_scratch(monkeypatch):
     x, y = _Tensor((5, 64), torch.bfloat16, 0), _Tensor((5, 32), torch.bfloat16, 0)
     monkeypatch.setattr(lbt, "linear8_backward", lambda *a: None)
     monkeypatch.setattr(lbt, "_at", lambda t, device=None: A)
+    monkeypatch.setattr(lbt, "_current_raw_stream", lambda index: 7)
     for capturing in (True, False):
         monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: capturing)
         layer, norm = _layer(0), lm.ResNorm(64)
