@@ -439,8 +439,8 @@ static lbt_status adamw_run(const lbt_adamw_tensor* tensors, int count, const lb
     t.count = count;
     uint64_t blocks = 0, at = 0;
     for (int i = 0; i < count; ++i) blocks += (tensors[i].n + kAdamBlock - 1) / kAdamBlock;
-    // Runs of eight where there are scales and blocks enough to fill the SMs four times over (0.4 G elements: 890 us, one by one
-    // 1209 us); else block by block (fp32 states, 11.7 M elements: 55 us, in runs of eight 60 us; few blocks: all warps at work).
+    // Runs of eight where there are scales and blocks enough to fill the SMs four times over (0.4 G elements: 890 us where one
+    // by one took 1209; 940-970 us on other boards); else block by block (fp32 states, 11.7 M elements: 55 us, in runs of eight 60 us; few blocks: all warps at work).
     t.run = h->state_bits == 8 && blocks > (uint64_t)kNumSMs * 32 * 4 ? kAdamRun : 1;
     for (int i = 0; i < count; ++i) {
         const lbt_adamw_tensor& s = tensors[i];

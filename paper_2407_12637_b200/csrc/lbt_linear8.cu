@@ -94,7 +94,7 @@ __device__ __forceinline__ float finish(int acc, float scale, float bias) { retu
 // 32 consecutive columns of one row (lane = row): scale, bias, round, store in 32-byte sectors.  `cs`: this warp's shared copy of the
 // columns' scales and biases.
 template <typename T>
-__device__ __forceinline__ void put_row(const L8Args& a, int64_t row, int c0, int width, const uint32_t (&v)[32], float rs, const float* cs) {
+__device__ __forceinline__ void put_row(const L8Args& a, int64_t row, int c0, const uint32_t (&v)[32], float rs, const float* cs) {
 #pragma unroll
     for (int j = 0; j < 32; j += 16) {
         float f[16];
@@ -107,7 +107,7 @@ __device__ __forceinline__ void put_row(const L8Args& a, int64_t row, int c0, in
             f[e + 3] = finish((int)v[j + e + 3], __fmul_rn(rs, s.w), b.w);
         }
         const int c = c0 + j;
-        if (row >= a.rows || c >= a.cols || j >= width) continue;
+        if (row >= a.rows || c >= a.cols) continue;
         T* dst = static_cast<T*>(a.out) + row * a.ldo + c;
         if (c + 16 <= a.cols) {
             Vec8<T> p, q;
@@ -131,10 +131,10 @@ __device__ __forceinline__ void put_row(const L8Args& a, int64_t row, int c0, in
     }
 }
 
-// `width` (16 or 32) consecutive columns from c0 of a warp's 32 rows, lane l holding row row0 + l in v.  Rows that begin on 32-byte
+// 32 consecutive columns from c0 of a warp's 32 rows, lane l holding row row0 + l in v.  Rows that begin on 32-byte
 // boundaries leave straight from the registers; others are turned round in the warp's 4 KB of shared memory, so that a store covers
 // consecutive addresses of one row (a lane's own row in 4-byte stores touched 32 partly written sectors each).
-__device__ __forceinline__ void put_block(const L8Args& a, uint32_t* stage, int64_t row0, int c0, int width, const uint32_t (&v)[32], float rs, int lane) {
+__device__ __forceinline__ void put_block(const L8Args& a, uint32_t* stage, int64_t row0, int c0, const uint32_t (&v)[32], float rs, int lane) {
     if (c0 >= a.cols || row0 >= a.rows) return;   // uniform over the warp
     const int c = c0 + lane;
     const float scale = c < a.cols && a.col_scale != nullptr ? __ldg(a.col_scale + c) : 1.0f;
@@ -145,15 +145,15 @@ __device__ __forceinline__ void put_block(const L8Args& a, uint32_t* stage, int6
         cs[lane] = scale;
         cs[32 + lane] = bias;
         __syncwarp();
-        if (a.out_type == LBT_BF16) put_row<__nv_bfloat16>(a, row0 + lane, c0, width, v, rs, cs);
-        else if (a.out_type == LBT_F16) put_row<__half>(a, row0 + lane, c0, width, v, rs, cs);
-        else put_row<float>(a, row0 + lane, c0, width, v, rs, cs);
+        if (a.out_type == LBT_BF16) put_row<__nv_bfloat16>(a, row0 + lane, c0, v, rs, cs);
+        else if (a.out_type == LBT_F16) put_row<__half>(a, row0 + lane, c0, v, rs, cs);
+        else put_row<float>(a, row0 + lane, c0, v, rs, cs);
         return;
     }
 #pragma unroll
     for (int j = 0; j < 32; ++j) stage[lane * 32 + (j ^ lane)] = v[j];
     __syncwarp();
-    const bool live = lane < width && c < a.cols;
+    const bool live = c < a.cols;
 #pragma unroll 4
     for (int r = 0; r < 32; ++r) {
         const float s = __fmul_rn(__shfl_sync(0xFFFFFFFFu, rs, r), scale);
@@ -511,7 +511,7 @@ l8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 uint32_t v[32];
                 tmem_ld_32x32(tmem + buf * 256u + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
                 tmem_ld_wait();
-                put_block(a, stage, row - lane, tn * 256 + c, 32, v, rs, lane);
+                put_block(a, stage, row - lane, tn * 256 + c, v, rs, lane);
             }
             tc_fence_before_sync();
             __syncwarp();

@@ -8,8 +8,11 @@
 //   d = dr + N_pre'(dy),  dx = scale_x d,  du = scale_h gate d,  dh = N_post'(du),
 //   N'(g) = rstd (e - [mean e] - k mean(e k)),  e = g w   (the bracket for the layer norm)
 //   dw = sum_rows g k,  db = sum_rows g,  dgate = sum over the gate's rows of scale_h u d.
-// Memory is the floor: two reads and two writes an element forward, four and two backward.  Next to it stands instruction issue, which
-// bounds both passes now (8192 x 4096 bf16: forward 55-59 us = 4.6-4.9 TB/s, backward 127 us = 3.2 TB/s).
+// Memory is the floor: two reads and two writes an element forward, four and two backward.  Neither pass reaches it: on 8192 x 4096
+// bf16 (gate per 2048 rows) forward takes 55-59 us = 4.6-4.9 TB/s with 0.70 instructions a cycle and scheduler, eight warps each; a warp
+// waits most for its rows ahead and for its turn.  Backward takes 127 us = 3.2 TB/s with 0.56 instructions: 118 registers leave
+// four warps a scheduler (one block), too few to fill the latencies of shared memory and of the arithmetic; the barriers are a
+// twentieth of a warp's time.
 //
 // One group of threads (a warp up to 1024 columns forward and 512 backward, a block above) owns a row, eight columns of it per
 // thread and vector, so a row's sums are the group's reduction and nothing is read twice.  A group works through several rows: each thread copies its own columns
@@ -44,7 +47,7 @@ struct NormArgs {
     int64_t ld_x, ld_h, ld_r, ld_y, ld_dr, ld_dy, ld_dx, ld_dh;
     Params gate, w_post, b_post, w_pre, b_pre;
     uint8_t* q;
-    int64_t ldq;
+    int64_t ldq, q_end;     // q_end: D and its padding (what lies behind them in a row is not this matrix's)
     float* q_scale;
     float4* stats;
     // backward
@@ -59,7 +62,7 @@ struct NormArgs {
 // so a thread has eight consecutive columns to a vector, all there or none.  P void: any alignment, any D, parameters of any type;
 // a thread's columns are kG apart, so that a warp reads consecutive elements one by one, and each column is tested.
 // (The tests cost about as much as the arithmetic: on 8192 x 4096 bf16 an element takes 82 instructions forward with them, 36
-// without, and the kernel is bound by their issue.)
+// without.)
 template <typename P> constexpr bool kEven = true;
 template <> constexpr bool kEven<void> = false;
 
@@ -359,14 +362,13 @@ __global__ void __launch_bounds__(kBlock<kG>, kForwardBlocks<kG, kNV>) resnorm_f
 #pragma unroll
                     for (int i = 0; i < 8; ++i) k[i] = code8(r[g][i], factor);
                     uint8_t* to = a.q + row * a.ldq;
-                    const int q_end = (D + 15) & ~15;   // (what lies behind the padding is not this matrix's)
                     if constexpr (kEven<P>) {
                         const int c = column<P, kG>(g, 0, t);
-                        if (c < q_end) *reinterpret_cast<uint2*>(to + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
+                        if (c < a.q_end) *reinterpret_cast<uint2*>(to + c) = make_uint2(pack4(k[0], k[1], k[2], k[3]), pack4(k[4], k[5], k[6], k[7]));
                     } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            if (column<P, kG>(g, i, t) < q_end) to[column<P, kG>(g, i, t)] = (uint8_t)k[i];
+                            if (column<P, kG>(g, i, t) < a.q_end) to[column<P, kG>(g, i, t)] = (uint8_t)k[i];
                     }
                 }
             }
@@ -695,7 +697,7 @@ int depth_for(int row_bytes, int resident, bool even, int64_t rows_each) {
     return (int)std::min<int64_t>(3, 200 * 1024 / resident / row_bytes);
 }
 
-// The attribute for more than 48 KB of shared memory, once per kernel and device.
+// The attribute for more than 48 KB of shared memory (it belongs to the current device).
 template <typename K>
 lbt_status allow_smem(K kernel, int bytes) {
     if (bytes <= 40 * 1024) return LBT_OK;
@@ -841,7 +843,7 @@ extern "C" lbt_status lbt_resnorm_forward(const lbt_resnorm_desc* d, const void*
     a.w_post = make_param(w_post, d->param_type, a.D); a.b_post = make_param(b_post, d->param_type, a.D);
     a.w_pre = make_param(w_pre, d->param_type, a.D); a.b_pre = make_param(b_pre, d->param_type, a.D);
     // codes: a row is padded with zeros up to the next multiple of 16 columns
-    a.q = static_cast<uint8_t*>(q); a.ldq = ldq; a.q_scale = q_scale;
+    a.q = static_cast<uint8_t*>(q); a.ldq = ldq; a.q_end = (d->D + 15) / 16 * 16; a.q_scale = q_scale;
     a.stats = reinterpret_cast<float4*>(stats);
     const cudaStream_t stream = as_stream(cuda_stream);
     return forward_any(a, d->type, d->param_type, stream);
