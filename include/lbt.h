@@ -364,7 +364,7 @@ enum { LBT_F32 = 0, LBT_BF16 = 1, LBT_F16 = 2 };
 /*
  * Matrices are row-major with a leading dimension ld (elements from one row to the next, >= the row's length).  Activation and
  * gradient tensors need only their element type's alignment; rows that begin on 32-byte (fp32) or 16-byte boundaries are read
- * in wide accesses.  Zero tokens (M = 0) are valid.
+ * in wide accesses.  Zero tokens (M = 0) are valid.  Outputs overlap no input unless a call says so.
  *
  * 8-bit rows: q[m,i] = rint(x[m,i] * fl(127 fl(1 / a_m))), a_m = max_i |x[m,i]|, scale[m] = fl(a_m fl(1/127)); ties to even,
  * codes in [-127, 127].  a_m <= 1e-36: scale 0, codes 0.  A row that holds an infinity or NaN: scale NaN, codes 0 (its row of
