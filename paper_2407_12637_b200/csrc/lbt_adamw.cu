@@ -106,15 +106,16 @@ __device__ __forceinline__ float adam_root(float v) {
     return __fmaf_rn(__fmaf_rn(-s, s, v), __fmul_rn(0.5f, y), s);
 }
 
-// One element; returns u = sqrt(v).  An infinite v (a finite gradient beyond 1.8e19 squared) has the root infinity and the update 0;
-// kRootOfInf false: its root and p come out as NaN, which the caller mends.  8 bits have no code for infinity: it is stored as
-// NaN, and a NaN there is read as infinity (a gradient that is not finite shows in m).
-template <bool kRootOfInf>
+// One element; returns u = sqrt(v).  An infinite v (a finite gradient beyond 1.8e19 squared) has the root infinity and the update 0.
+// 8 bits have no code for infinity: it is stored as NaN, and a NaN there is read as infinity (a gradient that is not finite shows in m).
+enum RootOf { kOf32, kOf8, kLeft };   // kLeft: an infinite or NaN v leaves NaN in the root and in p, which the caller mends
+template <RootOf kOdd>
 __device__ __forceinline__ float adam_update(const AdamConst& c, float decay, float g, float& p, float& m, float& v) {
     g = __fmul_rn(g, c.gs);
     m = __fadd_rn(__fmul_rn(c.b1, m), __fmul_rn(c.omb1, g));
     v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.omb2, __fmul_rn(g, g)));
-    const float root = adam_root(v), u = kRootOfInf ? fminf(root, __uint_as_float(kNonFinite)) : root;   // (fminf passes over NaN)
+    // (fminf passes over one NaN: v + 1 is above every finite root, infinite with v, and NaN with it)
+    const float root = adam_root(v), u = kOdd == kLeft ? root : fminf(root, kOdd == kOf8 ? __uint_as_float(kNonFinite) : __fadd_rn(v, 1.0f));
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__fadd_rn(__fmul_rn(u, c.inv_c2), c.eps)));
     p = __fsub_rn(__fmul_rn(decay, p), __fmul_rn(__fmul_rn(c.step_size, m), inv));
@@ -239,7 +240,7 @@ __device__ __forceinline__ void adam_whole(const AdamEntry& e, const AdamConst& 
         for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = adam_update<kBits == 32>(c, e.decay, g[i], p[i], m[i], v[i]);
+    for (int i = 0; i < 8; ++i) u[i] = adam_update<kBits == 32 ? kOf32 : kLeft>(c, e.decay, g[i], p[i], m[i], v[i]);
     uint32_t most_u = 0;
     if constexpr (kBits == 8) {
         // An instruction an element costs this form 2 % of the step (0.4 G elements), so what has no finite root is mended on a way of its own.
@@ -342,7 +343,7 @@ __device__ __forceinline__ void adam_ragged(const AdamEntry& e, const AdamConst&
                 v[i] = __fmul_rn(e4m3_values(static_cast<const uint8_t*>(e.v)[k]).x, vs);
                 v[i] = __fmul_rn(v[i], v[i]);
             }
-            u[i] = adam_update<true>(c, e.decay, g, p[i], m[i], v[i]);
+            u[i] = adam_update<kBits == 32 ? kOf32 : kOf8>(c, e.decay, g, p[i], m[i], v[i]);
             adam_store(e.p, p_type, k, p[i]);
             if (kBits == 32) {
                 static_cast<float*>(e.m)[k] = m[i];

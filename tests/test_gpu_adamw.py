@@ -306,3 +306,12 @@ def test_many_blocks_are_the_same_steps(dtype, gdtype):
             lm.AdamW(*[[t[k]] for t in parts], lr=1e-2, step=4 + step).step()
         for a, b in zip((ps, ms, vs, mss, vss), apart):
             assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b)), step
+
+
+@pytest.mark.parametrize("shift", [0, 1])   # (aligned, and element by element)
+def test_a_second_moment_that_is_nan_shows(shift):
+    n = 600
+    p, m, v = (torch.full((n + shift,), x, device="cuda")[shift:] for x in (1.0, 0.1, 0.01))
+    v[7], v[300] = float("nan"), float("inf")
+    lm.AdamW([p], [torch.full((n,), 0.1, device="cuda")], [m], [v], step=3).step()
+    assert p[7].isnan() and v[7].isnan() and torch.isfinite(p[300]) and torch.isinf(v[300]) and int(p.isnan().sum()) == 1
