@@ -340,22 +340,20 @@ class AdamW:
         lrs, wds = (list(x) if isinstance(x, (list, tuple)) else [x] * n for x in (lr, weight_decay))
         if any(len(x) != n for x in (self.m, self.v, self.m_scale, self.v_scale, lrs, wds)):
             raise ValueError("one of each for each parameter")
-        lists = (self.params, self.grads, self.m, self.v, self.m_scale, self.v_scale)
-        if len({t.get_device() for ts in lists for t in ts if t is not None}) > 1:
-            raise ValueError("parameters, gradients and moments are on one device")
         self.device = self.params[0].get_device() if n else None
+        if n and self.device < 0:
+            raise ValueError("parameters are CUDA tensors")
         self.table = (lbt.AdamwTensor * n)()
-        with lbt._place(self.params[0]) if n else contextlib.nullcontext():
-            for i, (p, g) in enumerate(zip(self.params, self.grads)):
-                if p.dtype not in lbt.TYPES or g.dtype not in lbt.TYPES or g.numel() != p.numel():
-                    raise ValueError("parameters and gradients: fp32, bf16 or fp16, of equal sizes")
-                for t, size, kind in ((self.m[i], p.numel(), state), (self.v[i], p.numel(), state), (self.m_scale[i], blocks[i], torch.float32),
-                                      (self.v_scale[i], blocks[i], torch.float32)):
-                    if t is not None and (t.numel() != size or t.dtype != kind):
-                        raise ValueError(f"moments: {p.numel()} values of {state}; with 8 bits one fp32 scale for each {lbt.ADAMW_BLOCK}")
-                e = self.table[i]
-                e.p, e.g, e.m, e.v, e.m_scale, e.v_scale = (lbt._at(t) for t in (p, g, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i]))
-                e.n, e.lr, e.weight_decay, e.p_type, e.g_type = p.numel(), lrs[i], wds[i], lbt.TYPES[p.dtype], lbt.TYPES[g.dtype]
+        for i, (p, g) in enumerate(zip(self.params, self.grads)):
+            if p.dtype not in lbt.TYPES or g.dtype not in lbt.TYPES or g.numel() != p.numel():
+                raise ValueError("parameters and gradients: fp32, bf16 or fp16, of equal sizes")
+            for t, size, kind in ((self.m[i], p.numel(), state), (self.v[i], p.numel(), state), (self.m_scale[i], blocks[i], torch.float32),
+                                  (self.v_scale[i], blocks[i], torch.float32)):
+                if t is not None and (t.numel() != size or t.dtype != kind):
+                    raise ValueError(f"moments: {p.numel()} values of {state}; with 8 bits one fp32 scale for each {lbt.ADAMW_BLOCK}")
+            e = self.table[i]
+            e.p, e.g, e.m, e.v, e.m_scale, e.v_scale = (lbt._at(t, self.device) for t in (p, g, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i]))
+            e.n, e.lr, e.weight_decay, e.p_type, e.g_type = p.numel(), lrs[i], wds[i], lbt.TYPES[p.dtype], lbt.TYPES[g.dtype]
         self.hyper = lbt.AdamwHyper(betas[0], betas[1], eps, step, state_bits, 0)   # (its step counts the calls)
         # calls that were held back, counted once there may be some (a launch that need not look starts 0.5 us earlier)
         self.skipped, self._counting = torch.zeros(1, dtype=torch.int64, device=self.params[0].device) if n else None, False
