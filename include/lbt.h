@@ -475,6 +475,90 @@ lbt_status lbt_adamw_step_ex(const lbt_adamw_tensor *tensors, int count, const l
                              const int32_t *d_skip, int64_t *d_skipped, void *cuda_stream);
 
 /*
+ * The norm of all gradients, and clipping by it, over `count` tensors (one launch each per 800 of them):
+ *   norm = |s| (sum over all tensors of g^2)^(1/2),  s = *d_grad_scale (1 if NULL);   scale = s min(1, max_norm / norm)
+ * summed in 64 bits in an order fixed by the sizes.  out->scale and &out->skip are what lbt_adamw_step takes as d_grad_scale and
+ * d_skip: an infinity or NaN among the gradients (or as s) makes skip 1 and scale 0 (norm is then infinite or NaN), else skip is 0.
+ * max_norm > 0 (infinity: measure only).  norms (may be NULL): the norm of each tensor, without s, count floats.
+ * out (device, 4-byte aligned): `reserved` is 0 before the first call and between calls; a struct belongs to one call at a time.
+ * ws: lbt_grad_norm_workspace_bytes(tensors, count) bytes, 8-byte aligned.
+ * lbt_grad_clip: out_i = g_i * norm->scale in fp32, rounded to out's type once, for every tensor of the table; skip != 0: nothing is
+ * written.  out may be g (then a scale of 1 writes nothing) and may have another type where it is not.
+ * `tensors` (HOST) is read during the call.  Tensors need their element type's alignment; 32 bytes (fp32) and 16 (16-bit types) are
+ * read in wide accesses.  n = 0 and count = 0 are valid (the norm of nothing is 0).
+ */
+typedef struct lbt_grad_tensor {
+    const void *g;      /* gradients, g_type                    */
+    void *out;          /* clipped, out_type (lbt_grad_clip)    */
+    uint64_t n;
+    int32_t g_type, out_type;
+} lbt_grad_tensor;      /* 32 bytes */
+typedef struct lbt_grad_norm_t {
+    float norm, scale;
+    int32_t skip;
+    uint32_t reserved;
+} lbt_grad_norm_t;      /* 16 bytes */
+size_t lbt_grad_norm_workspace_bytes(const lbt_grad_tensor *tensors, int count);
+lbt_status lbt_grad_norm(const lbt_grad_tensor *tensors, int count, double max_norm, const float *d_grad_scale, lbt_grad_norm_t *out,
+                         float *norms, void *ws, size_t ws_bytes, void *cuda_stream);
+lbt_status lbt_grad_clip(const lbt_grad_tensor *tensors, int count, const lbt_grad_norm_t *norm, void *cuda_stream);
+
+/*
+ * Low-rank adapters beside one linear layer: the tokens of run k, offsets[k] <= m < offsets[k+1], take adapter i = index[k]:
+ *   h[m] = A_i x[m],  out[m,o] = base[m,o] + s_i sum_r h[m,r] B_i[r,o]
+ * a: [adapters, rank, I], b: [adapters, rank, O] (both rank first, contiguous; an adapter of lower rank has rows of zeros); scale: s, one
+ * float an adapter (NULL: ones).  x, base, out, a and b have one type.  offsets: runs + 1 ascending device ints, index: one for each run; both NULL: one run
+ * of all M tokens with adapter 0.  An index outside [0, adapters) is a run without an adapter: out = base.  Rows of no run (ahead of
+ * offsets[0], from offsets[runs] on) are not written; offsets are cut to [0, M].  out may be base.
+ * h (may be NULL): [M, rank] floats, kept for the backward pass (rows without an adapter are not written).
+ * Sums are fp32 in an order fixed by the sizes; h enters its second product with 22 bits.  rank <= 128.
+ */
+typedef struct lbt_adapters_desc {   /* HOST struct */
+    int64_t M, I, O, runs;
+    int32_t adapters, rank, type, reserved;
+    int64_t ld_x, ld_base, ld_out, ld_dy, ld_dbase, ld_dx;   /* 0 = the row's length */
+} lbt_adapters_desc;
+lbt_status lbt_adapters_forward(const lbt_adapters_desc *d, const void *x, const void *a, const void *b, const float *scale,
+                                const int32_t *offsets, const int32_t *index, const void *base, void *out, float *h, void *cuda_stream);
+
+/*
+ * Its gradients: dh[m] = B_i dy[m], dx[m] = dbase[m] + s_i dh[m] A_i (dx may be dbase; rows as for out), and over all runs of adapter i
+ * dA_i = s_i sum_m dh[m] x[m]^T, dB_i = s_i sum_m h[m] dy[m]^T: whole tensors like a and b of grad_type (LBT_F32, or the type of a), zeros
+ * for an adapter without tokens.  Any of dx, da, db may be NULL.  x, h, runs: the forward pass's.  ws: lbt_adapters_workspace_bytes(d).
+ */
+size_t lbt_adapters_workspace_bytes(const lbt_adapters_desc *d);
+lbt_status lbt_adapters_backward(const lbt_adapters_desc *d, const void *dy, const void *x, const float *h, const void *a, const void *b,
+                                 const float *scale, const int32_t *offsets, const int32_t *index, const void *dbase, void *dx, void *da,
+                                 void *db, int grad_type, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Group norm with an activation on channels-last images x[N,P,C] (P pixels, ld elements from one pixel to the next, images P ld apart):
+ * for each image and each group of C / G neighbouring channels, mean and (biased) variance over the group's P C / G values,
+ *   k = (x - mean) rstd, rstd = (var + eps)^(-1/2);  z = k w + b;  y = act(z): z, max(z, 0) or z / (1 + exp(-z)).
+ * w, b: [C] of param_type (NULL: ones, zeros).  y or q may be NULL.  q: what lbt_quantize_act makes of the fp32 y with `bits` and d_clip
+ * (dense, the storage of this header's codes: what lbt_qconv_forward takes), d_scale_out: its scale; needs C a multiple of 8 and aligned rows.
+ * stats (may be NULL): [N,G,2] floats, mean and rstd, kept for the backward pass.  ws: lbt_groupnorm_workspace_bytes(d), 8-byte aligned.
+ * No sum crosses images.  Sums are fp32 (of differences from a value of the channel) in an order fixed by the sizes.  y may be x.
+ */
+enum { LBT_ACT_NONE = 0, LBT_ACT_RELU = 1, LBT_ACT_SILU = 2 };
+typedef struct lbt_groupnorm_desc {   /* HOST struct */
+    int64_t N, P, C, G;
+    int32_t type, param_type;   /* of x, y and their gradients; of w, b and their gradients */
+    int32_t act;
+    float eps;
+    int64_t ld_x, ld_y, ld_dy, ld_dx;   /* 0 = C */
+} lbt_groupnorm_desc;
+size_t lbt_groupnorm_workspace_bytes(const lbt_groupnorm_desc *d);
+lbt_status lbt_groupnorm_forward(const lbt_groupnorm_desc *d, const void *x, const void *w, const void *b, void *y, void *q, int bits,
+                                 const float *d_clip, float *d_scale_out, float *stats, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Its gradients from dy; x, w, b, stats are the forward pass's.  dx, dw, db: any may be NULL.  dx may be dy.  The slope of a ReLU at 0 is 0.
+ */
+lbt_status lbt_groupnorm_backward(const lbt_groupnorm_desc *d, const void *dy, const void *x, const void *w, const void *b, const float *stats,
+                                  void *dx, void *dw, void *db, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
  * Measurement taps (no counterpart in the paper).  After this call the library records the two
  * events (cudaEvent_t passed as void*, created by the caller) on the call's stream immediately
  * before and after every launch of the named kernel class, so that a benchmark can time one

@@ -32,7 +32,9 @@ EXPORTS = (
     "lbt_grad_diagnostics", "lbt_diagnostics_workspace_bytes",
     "lbt_rows8_quantize", "lbt_linear8_forward", "lbt_linear8_matmul", "lbt_linear8_backward", "lbt_linear8_workspace_bytes",
     "lbt_resnorm_forward", "lbt_resnorm_backward", "lbt_resnorm_workspace_bytes", "lbt_adamw_step",
-    "lbt_adamw_step_ex",
+    "lbt_adamw_step_ex", "lbt_grad_norm", "lbt_grad_clip", "lbt_grad_norm_workspace_bytes",
+    "lbt_adapters_forward", "lbt_adapters_backward", "lbt_adapters_workspace_bytes",
+    "lbt_groupnorm_forward", "lbt_groupnorm_backward", "lbt_groupnorm_workspace_bytes",
     "lbt_set_timing_events", "lbt_selftest_wait_timeout", "lbt_selftest_barrier_timeout",
     "lbt_selftest_linear8_timeout", "lbt_status_string",
 )
@@ -65,6 +67,8 @@ class GradDiag(C.Structure):
 F32, BF16, F16 = range(3)
 TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 NORM_RMS, NORM_LAYER = range(2)
+ACT_NONE, ACT_RELU, ACT_SILU = range(3)
+MAX_RANK = 128           # of a low-rank adapter
 MAX_REDUCTION8 = 133144   # longest sum of products of 8-bit codes that fits int32
 ADAMW_BLOCK = 256         # elements that share a scale of 8-bit moments
 
@@ -87,6 +91,23 @@ class AdamwHyper(C.Structure):
     """Mirror of `lbt_adamw_hyper` (40 bytes)."""
     _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
                 ("state_bits", C.c_int32), ("reserved", C.c_int32)]
+
+
+class GradTensor(C.Structure):
+    """Mirror of `lbt_grad_tensor` (32 bytes)."""
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_uint64), ("g_type", C.c_int32), ("out_type", C.c_int32)]
+
+
+class AdaptersDesc(C.Structure):
+    """Mirror of `lbt_adapters_desc` (96 bytes); leading dimensions 0 = the row's length."""
+    _fields_ = [*[(k, C.c_int64) for k in ("M", "I", "O", "runs")], *[(k, C.c_int32) for k in ("adapters", "rank", "type", "reserved")],
+                *[("ld_" + k, C.c_int64) for k in ("x", "base", "out", "dy", "dbase", "dx")]]
+
+
+class GroupnormDesc(C.Structure):
+    """Mirror of `lbt_groupnorm_desc` (80 bytes); leading dimensions 0 = C."""
+    _fields_ = [*[(k, C.c_int64) for k in ("N", "P", "C", "G")], *[(k, C.c_int32) for k in ("type", "param_type", "act")], ("eps", C.c_float),
+                *[("ld_" + k, C.c_int64) for k in ("x", "y", "dy", "dx")]]
 
 
 class GemmDesc(C.Structure):
@@ -156,6 +177,15 @@ def lib() -> C.CDLL:
         l.lbt_resnorm_workspace_bytes.argtypes = [vp]
         l.lbt_adamw_step.argtypes = [vp, i32, vp, vp, vp, vp]
         l.lbt_adamw_step_ex.argtypes = [vp, i32, vp, vp, vp, vp, vp]
+        l.lbt_grad_norm.argtypes = [vp, i32, C.c_double, vp, vp, vp, vp, sz, vp]
+        l.lbt_grad_clip.argtypes = [vp, i32, vp, vp]
+        l.lbt_grad_norm_workspace_bytes.argtypes = [vp, i32]
+        l.lbt_adapters_forward.argtypes = [vp] * 11
+        l.lbt_adapters_backward.argtypes = [vp] * 13 + [i32, vp, sz, vp]
+        l.lbt_adapters_workspace_bytes.argtypes = [vp]
+        l.lbt_groupnorm_forward.argtypes = [vp] * 6 + [i32, vp, vp, vp, vp, sz, vp]
+        l.lbt_groupnorm_backward.argtypes = [vp] * 10 + [sz, vp]
+        l.lbt_groupnorm_workspace_bytes.argtypes = [vp]
         l.lbt_set_timing_events.argtypes = [i32, vp, vp]
         l.lbt_selftest_wait_timeout.argtypes = [vp, C.c_uint32, vp]
         l.lbt_selftest_barrier_timeout.argtypes = [vp, C.c_uint32, vp]
@@ -490,6 +520,63 @@ def adamw_step(table, hyper, grad_scale=None, skip=None, stream=None, skipped=No
     skipped: device int64 that counts the steps held back by `skip` (None: hyper.step counts the steps that were taken)."""
     raw = stream if isinstance(stream, int) else _stream(stream)   # (the table's addresses are the caller's to place)
     _check(lib().lbt_adamw_step_ex(table, len(table), C.addressof(hyper), _at(grad_scale), _at(skip), _at(skipped), raw), "lbt_adamw_step")
+
+
+def grad_norm_workspace_bytes(table) -> int:
+    return int(lib().lbt_grad_norm_workspace_bytes(table, len(table)))
+
+
+def grad_norm(table, result, max_norm=float("inf"), norms=None, grad_scale=None, ws=None, stream=None):
+    """Norm, factor and skip flag of a ctypes array of GradTensor into `result` (16 device bytes whose last four are 0 before the
+    first call).  ws None: from torch's allocator."""
+    if ws is None:
+        ws = _scratch(grad_norm_workspace_bytes(table), result.device, stream)
+    _check(lib().lbt_grad_norm(table, len(table), max_norm, _at(grad_scale), _at(result), _floats(norms, len(table), "norms"), _at(ws), ws.numel(),
+                               _raw_stream(result, stream)), "lbt_grad_norm")
+
+
+def grad_clip(table, result, stream=None):
+    """Every tensor's `out` = `g` times the factor that grad_norm left in `result`."""
+    _check(lib().lbt_grad_clip(table, len(table), _at(result), _raw_stream(result, stream)), "lbt_grad_clip")
+
+
+def adapters_workspace_bytes(desc) -> int:
+    return int(lib().lbt_adapters_workspace_bytes(C.addressof(desc)))
+
+
+def adapters_forward(desc, x, a, b, scale, offsets, index, base, out, h=None, stream=None):
+    """`lbt_adapters_forward` on tensors that match `desc` (marshalling only: lm.Adapters builds and checks them)."""
+    _check(lib().lbt_adapters_forward(C.addressof(desc), x.data_ptr(), _at(a), _at(b), _at(scale), _at(offsets), _at(index), base.data_ptr(),
+                                      out.data_ptr(), _at(h), _raw_stream(x, stream)), "lbt_adapters_forward")
+
+
+def adapters_backward(desc, dy, x, h, a, b, scale, offsets, index, dbase=None, dx=None, da=None, db=None, grad_type=F32, ws=None, stream=None):
+    """`lbt_adapters_backward` on tensors that match `desc`.  ws None: from torch's allocator."""
+    if ws is None:
+        ws = _scratch(adapters_workspace_bytes(desc), dy.device, stream)
+    _check(lib().lbt_adapters_backward(C.addressof(desc), dy.data_ptr(), x.data_ptr(), _at(h), _at(a), _at(b), _at(scale), _at(offsets), _at(index),
+                                       dbase.data_ptr() if dbase is not None else 0, dx.data_ptr() if dx is not None else 0, _at(da), _at(db),
+                                       grad_type, _at(ws), ws.numel(), _raw_stream(dy, stream)), "lbt_adapters_backward")
+
+
+def groupnorm_workspace_bytes(desc) -> int:
+    return int(lib().lbt_groupnorm_workspace_bytes(C.addressof(desc)))
+
+
+def groupnorm_forward(desc, x, w, b, y=None, q=None, bits=4, clip=None, scale_out=None, stats=None, ws=None, stream=None):
+    """`lbt_groupnorm_forward` on tensors that match `desc` (marshalling only: cnn.GroupNorm builds and checks them)."""
+    if ws is None:
+        ws = _scratch(groupnorm_workspace_bytes(desc), x.device, stream)
+    _check(lib().lbt_groupnorm_forward(C.addressof(desc), x.data_ptr(), _at(w), _at(b), y.data_ptr() if y is not None else 0, _at(q), bits, _at(clip),
+                                       _at(scale_out), _at(stats), _at(ws), ws.numel(), _raw_stream(x, stream)), "lbt_groupnorm_forward")
+
+
+def groupnorm_backward(desc, dy, x, w, b, stats, dx=None, dw=None, db=None, ws=None, stream=None):
+    """`lbt_groupnorm_backward` on tensors that match `desc`.  ws None: from torch's allocator."""
+    if ws is None:
+        ws = _scratch(groupnorm_workspace_bytes(desc), x.device, stream)
+    _check(lib().lbt_groupnorm_backward(C.addressof(desc), dy.data_ptr(), x.data_ptr(), _at(w), _at(b), _at(stats), dx.data_ptr() if dx is not None else 0,
+                                        _at(dw), _at(db), _at(ws), ws.numel(), _raw_stream(x, stream)), "lbt_groupnorm_backward")
 
 
 def grad_diagnostics(dY, q_codes, bits, alpha, stats, ws=None, stream=None) -> "GradDiag":

@@ -1,4 +1,4 @@
-"""Layers of a transformer's residual block on the library's kernels: `Linear8`, `ResNorm` and `AdamW`.
+"""Layers of a transformer's residual block on the library's kernels: `Linear8`, `Adapters`, `ResNorm`, `GradClip` and `AdamW`.
 
 Each object keeps what a program keeps between calls (weight codes, parameters, moments, scratch for each stream) and the
 plan of its calls; every step of arithmetic runs in the library (`lbt`).  Outputs may be handed in (`out`); otherwise they
@@ -170,6 +170,128 @@ class Linear8:
         return out
 
 
+class Adapters:
+    """Low-rank adapters beside a linear layer (a `Linear8` whose weights stay as they are): out[m] = base[m] + s_i (x[m] A_i^T) B_i for
+    the tokens m of each run of neighbouring tokens with adapter i.
+
+    a [adapters, rank, I], b [adapters, rank, O]: both rank first, of one type (the activations'); scale [adapters] fp32 (None: ones).
+    Runs: offsets (runs + 1 ascending int32 on the device) and index (int32 [runs], an adapter each; -1: none).  Both None: all tokens
+    are one run with adapter 0.  Rows of no run are left as they are."""
+
+    def __init__(self, a, b, scale=None):
+        if a.dim() != 3 or b.dim() != 3 or a.shape[:2] != b.shape[:2] or a.dtype != b.dtype or a.dtype not in lbt.TYPES:
+            raise ValueError("a: [adapters, rank, I], b: [adapters, rank, O], of one type: fp32, bf16 or fp16")
+        self.n, self.rank, self.I = a.shape
+        self.O = b.shape[2]
+        if not 1 <= self.rank <= lbt.MAX_RANK or min(self.n, self.I, self.O) < 1:
+            raise ValueError(f"ranks of 1 to {lbt.MAX_RANK}, at least one adapter, input and output")
+        self.a, self.b, self.scale, self.dtype, self.device = a, b, scale, a.dtype, a.get_device()
+        with lbt._place(a):   # (addresses of the adapters' own tensors, whose storage stays)
+            self._weights = (lbt._at(a), lbt._at(b), lbt._floats(scale, self.n, "scale"))
+        self.kept = None
+        self._plans, self._own_kept, self._space = {}, {}, {}   # descriptors by sizes; by stream: h that is kept, workspace of the backward pass
+
+    def _runs(self, offsets, index):
+        if offsets is None and index is None:
+            return 0, 0, 0
+        if offsets is None or index is None or offsets.dtype != torch.int32 or index.dtype != torch.int32 or offsets.numel() != index.numel() + 1:
+            raise ValueError("offsets: int32, one more than index; index: int32, an adapter for each run")
+        return index.numel(), lbt._at(offsets, self.device), lbt._at(index, self.device)
+
+    def _plan(self, names, acts, widths, runs):
+        """Addresses of the activations (None: 0) and the descriptor of a call on tensors of these sizes."""
+        addresses, lds, M = [], [], None
+        for name, t, width in zip(names, acts, widths):
+            if t is None:
+                addresses.append(0)
+                lds.append(0)
+                continue
+            address, _, ld, rows = lbt._rows(t, name, width, self.device)
+            if t.dtype != self.dtype or (M is not None and rows != M):
+                raise ValueError(f"{name}: one row per token, of the adapters' type {self.dtype}")
+            M = rows
+            addresses.append(address)
+            lds.append(ld)
+        key = (M, runs, *names, *lds)
+        plan = self._plans.get(key)
+        if plan is None:
+            d = lbt.AdaptersDesc(M, self.I, self.O, runs, self.n, self.rank, lbt.TYPES[self.dtype], 0)
+            for name, ld in zip(names, lds):
+                setattr(d, "ld_" + name, ld)
+            if len(self._plans) >= 256:   # many lengths: the plans are cheap to make again
+                self._plans.clear()
+            plan = self._plans[key] = (d, C.addressof(d), lbt.adapters_workspace_bytes(d))
+        return M, addresses, plan
+
+    def forward(self, x, base, offsets=None, index=None, out=None, keep=False, stream=None):
+        """out for x [M, I] and base [M, O] (the layer's output; out None: added in place).  keep: x, the runs and h stay for `backward`,
+        until the next forward pass with keep=True."""
+        on = x.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(x, stream):
+                return self.forward(x, base, offsets, index, out, keep)
+        if on != self.device:
+            raise ValueError(f"the adapters are on device {self.device}")
+        out = base if out is None else out
+        runs, at_offsets, at_index = self._runs(offsets, index)
+        M, at, (_, desc, _) = self._plan(("x", "base", "out"), (x, base, out), (self.I, self.O, self.O), runs)
+        raw, h = lbt._current_raw_stream(on), None
+        if keep:   # a buffer for each stream, shared by one forward pass after the other
+            held = not _capturing(raw)
+            h = self._own_kept.get(raw) if held else None
+            if h is None or h.shape[0] != M:
+                h = torch.empty(M, self.rank, dtype=torch.float32, device=x.device)
+                if held:
+                    self._own_kept[raw] = h
+        a, b, scale = self._weights
+        status = lbt.lib().lbt_adapters_forward(desc, at[0], a, b, scale, at_offsets, at_index, at[1], at[2], h.data_ptr() if keep else 0, raw)
+        if status:
+            raise lbt.LbtError(status, "lbt_adapters_forward")
+        if keep:
+            self.kept = (x, h, offsets, index)
+        return out
+
+    def backward(self, dy, dbase=None, dx=None, da=None, db=None, grad_dtype=torch.float32, stream=None):
+        """{"dx", "da", "db"} of the last forward pass with keep=True.  dbase: the layer's gradient of x, to which the adapters' is
+        added (dx None: in place); without it there is no dx.  da, db: buffers to write into, else new ones of grad_dtype (fp32, or the adapters' type)."""
+        if self.kept is None:
+            raise RuntimeError("backward needs a forward pass with keep=True")
+        on = dy.get_device()
+        if stream is not None or on != lbt._device():
+            with lbt._place(dy, stream):
+                return self.backward(dy, dbase, dx, da, db, grad_dtype)
+        if on != self.device:
+            raise ValueError(f"the adapters are on device {self.device}")
+        x, h, offsets, index = self.kept
+        if dx is not None and dbase is None:
+            raise ValueError("dx is the layer's gradient dbase and the adapters' part: it needs dbase")
+        dx = dbase if dx is None else dx
+        kinds = {t.dtype for t in (da, db) if t is not None} or {grad_dtype}
+        if len(kinds) != 1 or not kinds <= {torch.float32, self.dtype}:
+            raise ValueError("da and db: both fp32, or both of the adapters' type")
+        kind = kinds.pop()
+        out = {"dx": dx} if dx is not None else {}
+        for name, given, like in (("da", da, self.a), ("db", db, self.b)):
+            out[name] = torch.empty_like(like, dtype=kind) if given is None else given
+            if out[name].shape != like.shape:
+                raise ValueError(f"{name}: of the shape {tuple(like.shape)}")
+        runs, at_offsets, at_index = self._runs(offsets, index)
+        M, at, (_, desc, size) = self._plan(("dy", "x", "dbase", "dx"), (dy, x, dbase, dx), (self.O, self.I, self.I, self.I), runs)
+        raw = lbt._current_raw_stream(on)
+        held = not _capturing(raw)
+        ws = self._space.get(raw) if held else None
+        if ws is None or ws.numel() < size:
+            ws = torch.empty(size, dtype=torch.uint8, device=dy.device)
+            if held:
+                self._space[raw] = ws
+        a, b, scale = self._weights
+        status = lbt.lib().lbt_adapters_backward(desc, at[0], at[1], h.data_ptr(), a, b, scale, at_offsets, at_index, at[2], at[3], lbt._at(out["da"], on),
+                                                 lbt._at(out["db"], on), lbt.TYPES[kind], ws.data_ptr(), size, raw)
+        if status:
+            raise lbt.LbtError(status, "lbt_adapters_backward")
+        return out
+
+
 class ResNorm:
     """What happens between two blocks: r = scale_x x + scale_h gate N_post(h), y = N_pre(r), in one pass.
 
@@ -310,6 +432,86 @@ class ResNorm:
         if status:
             raise lbt.LbtError(status, "lbt_resnorm_backward")
         return out
+
+
+class GradClip:
+    """The norm of all gradients in `grads` (fixed storage), and clipping to `max_norm` by it.
+
+    `measure` leaves `norm`, `scale` = min(1, max_norm / norm), `skip` (1: a gradient is not finite) and each tensor's norm in `norms`,
+    all on the device; scale and skip go to AdamW.step(grad_scale=clip.scale, skip=clip.skip), which then needs no pass over the
+    gradients more than it makes anyway.  `clip` also writes the clipped gradients, for an optimizer that takes them as they are: into
+    `out` (tensors of the gradients' sizes, of any type), by default in place; with skip set it writes nothing.  An object is used
+    by one thread and one stream at a time."""
+
+    def __init__(self, grads, max_norm=float("inf"), out=None):
+        n = len(grads)
+        if out is not None and len(out) != n:
+            raise ValueError("one output for each gradient")
+        if not max_norm > 0:
+            raise ValueError("max_norm is positive")
+        self.grads, self.out, self.max_norm = list(grads), list(out) if out is not None else list(grads), float(max_norm)
+        self.device = self.grads[0].get_device() if n else None
+        if n and self.device < 0:
+            raise ValueError("gradients are CUDA tensors")
+        self.table = (lbt.GradTensor * n)()
+        for e, g, o in zip(self.table, self.grads, self.out):
+            if g.dtype not in lbt.TYPES or o.dtype not in lbt.TYPES or g.numel() != o.numel():
+                raise ValueError("gradients and outputs: fp32, bf16 or fp16, of equal sizes")
+            e.g, e.out = lbt._at(g, self.device), lbt._at(o, self.device)
+            e.n, e.g_type, e.out_type = g.numel(), lbt.TYPES[g.dtype], lbt.TYPES[o.dtype]
+            if e.g == e.out and g.dtype != o.dtype:
+                raise ValueError("an output in its gradient's place has its type")
+        places = [e.out for e in self.table if e.n]
+        if len(set(places)) != len(places):
+            raise ValueError("every tensor once: a gradient given twice would be clipped twice")
+        where = self.grads[0].device if n else "cpu"
+        self._result = torch.zeros(4, dtype=torch.int32, device=where)
+        parts = self._result.view(torch.float32)
+        self.norm, self.scale, self.skip = parts[0:1], parts[1:2], self._result[2:3]
+        self.norms = torch.zeros(n, dtype=torch.float32, device=where)
+        if n == 0:
+            self.scale.fill_(1.0)
+        else:
+            with lbt._place(self.grads[0]):
+                self._addresses = (lbt._at(self._result), lbt._at(self.norms))
+            self._bytes, self._space = lbt.grad_norm_workspace_bytes(self.table), {}
+
+    def measure(self, grad_scale=None, stream=None):
+        """Enqueues the measurement; returns `norm` (a device float).  grad_scale: device float that the gradients are still to be
+        multiplied by (a loss scale's reciprocal): norm is of the products, and `scale` contains it."""
+        if not self.grads:
+            return self.norm
+        if stream is not None or self.device != lbt._device():
+            with lbt._place(self.grads[0], stream):
+                return self.measure(grad_scale)
+        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+            raise ValueError("grad_scale: one fp32 value")
+        raw = lbt._current_raw_stream(self.device)
+        held = not _capturing(raw)
+        ws = self._space.get(raw) if held else None
+        if ws is None:
+            ws = torch.empty(self._bytes, dtype=torch.uint8, device=self.norms.device)
+            if held:
+                self._space[raw] = ws
+        result, norms = self._addresses
+        status = lbt.lib().lbt_grad_norm(self.table, len(self.table), self.max_norm, lbt._at(grad_scale, self.device) if grad_scale is not None else 0,
+                                         result, norms, ws.data_ptr(), self._bytes, raw)
+        if status:
+            raise lbt.LbtError(status, "lbt_grad_norm")
+        return self.norm
+
+    def clip(self, grad_scale=None, stream=None):
+        """`measure`, and the gradients times `scale` into `out`."""
+        if not self.grads:
+            return self.norm
+        if stream is not None or self.device != lbt._device():
+            with lbt._place(self.grads[0], stream):
+                return self.clip(grad_scale)
+        self.measure(grad_scale)
+        status = lbt.lib().lbt_grad_clip(self.table, len(self.table), self._addresses[0], lbt._current_raw_stream(self.device))
+        if status:
+            raise lbt.LbtError(status, "lbt_grad_clip")
+        return self.norm
 
 
 class AdamW:
