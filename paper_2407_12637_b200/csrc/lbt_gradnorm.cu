@@ -22,7 +22,7 @@ constexpr int kNormMax = 800;       // tensors per launch: the table fits the 32
 constexpr int kNormFew = 40;        // smaller tables for fewer tensors (less to copy at a launch)
 constexpr int kNormSome = 128;
 constexpr uint64_t kNormChunk = 2048;                       // elements of the smallest chunk: eight accesses a lane
-constexpr uint64_t kNormChunks = (uint64_t)kNumSMs * 64;    // chunks that fill the SMs: larger inputs take larger chunks
+constexpr uint64_t kNormChunks = (uint64_t)kNumSMs * 16;    // chunks that fill the SMs once: larger inputs take larger chunks
 
 struct NormEntry {
     const void* g;
@@ -77,10 +77,10 @@ __device__ __forceinline__ void norm_store(void* p, int type, uint64_t i, float 
     else static_cast<__half*>(p)[i] = from_f32<__half>(v);
 }
 
-// The chunk's sum over this lane's elements [at, end) of an aligned tensor; four accesses under way at a time.
+// The chunk's sum over this lane's elements [at, end) of an aligned tensor; 128 bytes a lane under way at a time.
 template <typename G>
 __device__ __forceinline__ double chunk_squares(const G* g, uint64_t at, uint64_t end, int lane) {
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 16 / sizeof(G);
     double sum = 0.0;
     uint64_t i = at + 8 * lane;
     for (; i + 256 * (kAhead - 1) + 8 <= end; i += 256 * kAhead) {
@@ -151,6 +151,7 @@ struct NormCall {
 
 template <int kCap>
 __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_constant__ NormTable<kCap> t, const __grid_constant__ NormCall c) {
+    extern __shared__ double staged[];   // a word for each chunk, one for each tensor
     __shared__ uint32_t first[kCap + 1];
     __shared__ double space[kNormThreads / 32];
     __shared__ bool is_last;
@@ -188,31 +189,28 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
     }
     __syncthreads();
     if (!is_last) return;
-    constexpr uint32_t kWide = 512;   // tensors of more chunks are added by the whole block
-    double total = 0.0;               // of the tensors that this warp has added (in its lane 0)
+    // All partial sums come on chip in one sweep; a tensor of many chunks is then added by a warp, one of few by a thread.
+    constexpr uint32_t kFew = 32;
+    double* sums = reinterpret_cast<double*>(staged + all);
+    for (uint32_t k = threadIdx.x; k < all; k += kNormThreads) staged[k] = __ldcg(c.partial + k);
+    __syncthreads();
     for (int i = warp; i < t.count; i += kNormThreads / 32) {
-        const uint32_t lo = first[i], hi = first[i + 1];
-        if (hi - lo > kWide) continue;
+        if (first[i + 1] - first[i] <= kFew) continue;
         double sum = 0.0;
-        for (uint32_t k = lo + lane; k < hi; k += 32) sum += __ldcg(c.partial + k);
+        for (uint32_t k = first[i] + lane; k < first[i + 1]; k += 32) sum += staged[k];
         sum = warp_sum(sum);
-        if (lane == 0) {
-            total += sum;
-            if (c.norms != nullptr) c.norms[i] = (float)sqrt(sum);
-        }
+        if (lane == 0) sums[i] = sum;
     }
-    for (int i = 0; i < t.count; ++i) {
-        const uint32_t lo = first[i], hi = first[i + 1];
-        if (hi - lo <= kWide) continue;
+    __syncthreads();
+    double total = 0.0;
+    for (int i = threadIdx.x; i < t.count; i += kNormThreads) {
         double sum = 0.0;
-        for (uint32_t k = lo + threadIdx.x; k < hi; k += kNormThreads) sum += __ldcg(c.partial + k);
-        sum = block_sum(sum, space);
-        if (threadIdx.x == 0) {
-            total += sum;
-            if (c.norms != nullptr) c.norms[i] = (float)sqrt(sum);
-        }
+        if (first[i + 1] - first[i] > kFew) sum = sums[i];
+        else for (uint32_t k = first[i]; k < first[i + 1]; ++k) sum += staged[k];
+        total += sum;
+        if (c.norms != nullptr) c.norms[i] = (float)sqrt(sum);
     }
-    total = block_sum(lane == 0 ? total : 0.0, space);
+    total = block_sum(total, space);
     if (threadIdx.x != 0) return;
     c.out->reserved = 0;
     if (c.launch < c.last) {
@@ -324,7 +322,8 @@ template <int kCap>
 static lbt_status norm_launch(const lbt_grad_tensor* tensors, int count, uint64_t chunk, const NormCall& c, uint32_t* chunks, cudaStream_t stream) {
     NormTable<kCap> t;
     *chunks = norm_table(t, tensors, count, chunk, false);
-    grad_norm_kernel<kCap><<<std::max(1, norm_grid(*chunks)), kNormThreads, 0, stream>>>(t, c);
+    // (chunks: kNormChunks and one more for each tensor at most, 25 KB with their tensors' sums)
+    grad_norm_kernel<kCap><<<std::max(1, norm_grid(*chunks)), kNormThreads, sizeof(double) * (*chunks + count), stream>>>(t, c);
     return launch_status();
 }
 

@@ -4,11 +4,14 @@
 //   k = (x - mean) rstd,  z = k w + b,  y = act(z);   e = dy act'(z),  db = sum e,  dw = sum e k,
 //   dx = rstd (w e - mean_g(w e) - k mean_g(w e k))
 //
-// Bound by memory: x and y, then x, dy and dx.  Two kernels a direction: the first leaves sums of its share of an image's pixels for each
-// channel, the second adds them up for its image (a few KB from L2), and streams.  Sums are kept by channel, whatever groups
-// the channels fall into, so a thread owns eight (or, where rows are not aligned, one) neighbouring channels and
-// walks over pixels.  The variance must not lose itself in a mean far from 0: a thread sums differences from the first value it
-// reads of each channel, and shares are combined from their means and centred sums of squares.
+// Bound by memory: x and y, then x, dy and dx.  Sums are kept by channel, whatever groups the channels fall into, so a thread owns
+// eight (or, where rows are not aligned, one) neighbouring channels and walks over pixels.  Two forms:
+//   an image that fits the shared memory of a cluster (8 or 16 CTAs) is read once: each CTA keeps its share of the pixels on chip, the
+//   CTAs' sums of each channel meet through the cluster, and the output is formed from what is kept;
+//   a larger one is read twice: the first kernel leaves the sums of its share of an image's pixels for each channel, the second adds
+//   them up for its image (a few KB from L2), and streams.
+// The variance must not lose itself in a mean far from 0: shares are combined from their means and centred sums of squares, which
+// are formed around the share's own mean (what is kept can be read again) or around the first value that a thread reads.
 #include <math.h>
 
 #include <algorithm>
@@ -20,6 +23,7 @@ namespace lbt {
 
 constexpr int kGnThreads = 256;
 constexpr int kGnAhead = 4;             // pixels whose loads a thread has under way together
+constexpr int kGnPairs = 2;             // the same for two tensors at once
 constexpr int kGnMaxChunks = 148;       // shares of an image's pixels
 
 struct GroupNormArgs {
@@ -33,10 +37,13 @@ struct GroupNormArgs {
     float* stats;           // [N, G, 2] mean, rstd (null: not kept)
     const void* dy;
     void* dx;
+    void* dw;
+    void* db;
     float* partial;         // [N, chunks, C, 2]
     int64_t ld_x, ld_y, ld_dy, ld_dx;
-    int P, C, G, chunks, act, bits, param_type;
+    int N, P, C, G, chunks, share, act, bits, param_type;   // share: pixels of a chunk (the last one's may be fewer)
     float eps;
+    int kept;   // where the packs that are kept begin in shared memory
 };
 
 // kVec consecutive values of a row.
@@ -68,87 +75,21 @@ template <typename T> __device__ __forceinline__ float sigmoid(float z) {
 }
 
 // How a thread block covers rows of `vecs` packs: this block's first pack, its packs, and pixels side by side.
-template <int kVec> struct Cover {
+template <int kVec, int kThreads = kGnThreads> struct Cover {
     int vec0, vecs, lanes, vec, lane;
     bool active;
     __device__ __forceinline__ Cover(int C) {
         const int all = (C + kVec - 1) / kVec;
-        vec0 = blockIdx.z * kGnThreads;
-        vecs = min(kGnThreads, all - vec0);
-        lanes = kGnThreads / vecs;
-        vec = threadIdx.x % vecs;
+        vec0 = blockIdx.z * kThreads;
+        vecs = min(kThreads, all - vec0);
+        lanes = kThreads / vecs;
         lane = threadIdx.x / vecs;
+        vec = threadIdx.x - lane * vecs;
         active = lane < lanes;
     }
     __device__ __forceinline__ int channel() const { return (vec0 + vec) * kVec; }
+    __device__ __forceinline__ int width() const { return vecs * kVec; }
 };
-
-// Pixels [lo, hi) of share c.
-__device__ __forceinline__ void gn_share(int P, int chunks, int c, int& lo, int& hi) {
-    lo = (int)((int64_t)P * c / chunks);
-    hi = (int)((int64_t)P * (c + 1) / chunks);
-}
-
-template <typename T, int kVec>
-__global__ void __launch_bounds__(kGnThreads) groupnorm_stats_kernel(const __grid_constant__ GroupNormArgs g) {
-    __shared__ float2 part[kGnThreads * kVec];   // mean and centred sum of squares by pixel lane and channel
-    const Cover<kVec> cover(g.C);
-    const int n = blockIdx.y, chunk = blockIdx.x;
-    int lo, hi;
-    gn_share(g.P, g.chunks, chunk, lo, hi);
-    const T* x = static_cast<const T*>(g.x) + (int64_t)n * g.P * g.ld_x + cover.channel();
-    if (cover.active) {
-        float first[kVec], s1[kVec], s2[kVec];
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) first[i] = s1[i] = s2[i] = 0.0f;
-        int p = lo + cover.lane;
-        const int count = max(0, (hi - p + cover.lanes - 1) / cover.lanes);
-        if (p < hi) {
-            Pack<T, kVec> v;
-            v.load(x + p * g.ld_x);
-            v.get(first);
-        }
-        for (; p < hi; p += kGnAhead * cover.lanes) {
-            Pack<T, kVec> v[kGnAhead];
-#pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                const int at = p + u * cover.lanes;
-                v[u].load(x + (at < hi ? at : p) * g.ld_x);
-            }
-#pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                if (p + u * cover.lanes >= hi) break;
-                float f[kVec];
-                v[u].get(f);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    const float d = f[i] - first[i];
-                    s1[i] += d;
-                    s2[i] = fmaf(d, d, s2[i]);
-                }
-            }
-        }
-        const float inv = count > 0 ? 1.0f / (float)count : 0.0f;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            const float shift = s1[i] * inv;
-            part[(cover.lane * cover.vecs + cover.vec) * kVec + i] = make_float2(first[i] + shift, fmaxf(s2[i] - s1[i] * shift, 0.0f));
-        }
-    }
-    __syncthreads();
-    const int width = cover.vecs * kVec, size = hi - lo;
-    for (int i = threadIdx.x; i < width; i += kGnThreads) {
-        float mean = 0.0f, m2 = 0.0f;
-        for (int l = 0; l < cover.lanes; ++l) mean = fmaf((float)max(0, (size - l + cover.lanes - 1) / cover.lanes), part[l * width + i].x, mean);
-        mean /= (float)size;
-        for (int l = 0; l < cover.lanes; ++l) {
-            const float2 v = part[l * width + i];
-            const float d = v.x - mean;
-            m2 += fmaf((float)max(0, (size - l + cover.lanes - 1) / cover.lanes) * d, d, v.y);
-        }
-        reinterpret_cast<float2*>(g.partial)[((int64_t)n * g.chunks + chunk) * g.C + cover.vec0 * kVec + i] = make_float2(mean, m2);
-    }
-}
 
 __device__ __forceinline__ float warp_add(float v) {
 #pragma unroll
@@ -156,28 +97,145 @@ __device__ __forceinline__ float warp_add(float v) {
     return v;
 }
 
-// Mean and 1 / standard deviation of one group of image n from the shares' channels, by a warp.
-__device__ __forceinline__ float2 group_stats(const GroupNormArgs& g, int n, int group) {
-    const int lane = threadIdx.x & 31, cg = g.C / g.G, items = g.chunks * cg;
-    const float2* part = reinterpret_cast<const float2*>(g.partial) + (int64_t)n * g.chunks * g.C + group * cg;
-    float mean = 0.0f, m2 = 0.0f;
-    for (int i = lane; i < items; i += 32) {
-        int lo, hi;
-        gn_share(g.P, g.chunks, i / cg, lo, hi);
-        mean = fmaf((float)(hi - lo), part[(int64_t)(i / cg) * g.C + i % cg].x, mean);
+// Sums by channel from those of the pixel lanes (part[lane][channel]): several threads take a channel's lanes in turn where there are
+// more threads than channels, then one joins them.
+__device__ __forceinline__ void join_lanes(const float2* part, float2* joined, int width, int lanes, float2* out) {
+    const int parts = max(1, kGnThreads / width);
+    for (int j = threadIdx.x; j < parts * width; j += kGnThreads) {
+        const int own = j / width, i = j - own * width;
+        float2 sum = make_float2(0.0f, 0.0f);
+        for (int l = own; l < lanes; l += parts) {
+            sum.x += part[l * width + i].x;
+            sum.y += part[l * width + i].y;
+        }
+        if (parts == 1) out[i] = sum;
+        else joined[j] = sum;
     }
-    const float total = (float)g.P * (float)cg;
-    mean = warp_add(mean) / total;
-    for (int i = lane; i < items; i += 32) {
-        int lo, hi;
-        gn_share(g.P, g.chunks, i / cg, lo, hi);
-        const float2 v = part[(int64_t)(i / cg) * g.C + i % cg];
-        const float d = v.x - mean;
-        m2 += fmaf((float)(hi - lo) * d, d, v.y);
+    if (parts == 1) return;
+    __syncthreads();
+    if (threadIdx.x < width) {
+        float2 sum = joined[threadIdx.x];
+        for (int k = 1; k < parts; ++k) {
+            sum.x += joined[k * width + threadIdx.x].x;
+            sum.y += joined[k * width + threadIdx.x].y;
+        }
+        out[threadIdx.x] = sum;
     }
-    m2 = warp_add(m2) / total;
-    return make_float2(mean, rsqrtf(m2 + g.eps));
 }
+
+// A share's mean and centred sum of squares of each channel.  A thread sums differences from the first value that it reads; the block's
+// mean is formed from the threads' means, then every thread's sum of squares is moved to that mean.
+template <typename T, int kVec>
+__global__ void __launch_bounds__(kGnThreads, 4) groupnorm_stats_kernel(const __grid_constant__ GroupNormArgs g) {
+    __shared__ float2 joined[kGnThreads];
+    __shared__ float2 part[kGnThreads * kVec];
+    __shared__ float2 sums[kGnThreads * kVec];
+    sm100::griddep_launch_dependents();
+    const Cover<kVec> cover(g.C);
+    const int n = blockIdx.y, chunk = blockIdx.x, width = cover.width();
+    const int lo = chunk * g.share, hi = min(lo + g.share, g.P);
+    const T* x = static_cast<const T*>(g.x) + ((int64_t)n * g.P + lo + cover.lane) * g.ld_x + cover.channel();
+    const int count = cover.active ? max(0, (hi - lo - cover.lane + cover.lanes - 1) / cover.lanes) : 0;
+    const int64_t step = cover.lanes * g.ld_x;
+    float first[kVec], s1[kVec], s2[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) first[i] = s1[i] = s2[i] = 0.0f;
+    for (int p = 0; p < count; p += kGnAhead) {
+        Pack<T, kVec> v[kGnAhead];
+#pragma unroll
+        for (int u = 0; u < kGnAhead; ++u)
+            if (p + u < count) v[u].load(x + (p + u) * step);
+        if (p == 0) v[0].get(first);
+#pragma unroll
+        for (int u = 0; u < kGnAhead; ++u) {
+            if (p + u >= count) break;
+            float f[kVec];
+            v[u].get(f);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const float d = f[i] - first[i];
+                s1[i] += d;
+                s2[i] = fmaf(d, d, s2[i]);
+            }
+        }
+    }
+    const float inv = count > 0 ? 1.0f / (float)count : 0.0f;
+    if (cover.active) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {   // the thread's mean, times its count; centred squares
+            const float shift = s1[i] * inv;
+            s2[i] = fmaxf(fmaf(-s1[i], shift, s2[i]), 0.0f);
+            first[i] += shift;
+            part[cover.lane * width + cover.vec * kVec + i] = make_float2(first[i] * (float)count, 0.0f);
+        }
+    }
+    __syncthreads();
+    join_lanes(part, joined, width, cover.lanes, sums);
+    __syncthreads();
+    const float size = 1.0f / (float)(hi - lo);
+    if (cover.active) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float d = first[i] - sums[cover.vec * kVec + i].x * size;
+            part[cover.lane * width + cover.vec * kVec + i] = make_float2(0.0f, fmaf((float)count * d, d, s2[i]));
+        }
+    }
+    float2* out = reinterpret_cast<float2*>(g.partial) + ((int64_t)n * g.chunks + chunk) * g.C + cover.vec0 * kVec;
+    __syncthreads();
+    float2 mean[kVec];   // (of the channels threadIdx.x, + 256, ..: read before `sums` is written again)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) mean[i] = threadIdx.x + i * kGnThreads < width ? sums[threadIdx.x + i * kGnThreads] : make_float2(0.0f, 0.0f);
+    __syncthreads();
+    join_lanes(part, joined, width, cover.lanes, sums);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+        if (threadIdx.x + i * kGnThreads < width) out[threadIdx.x + i * kGnThreads] = make_float2(mean[i].x * size, sums[threadIdx.x + i * kGnThreads].y);
+}
+
+// A group's items (share, channel) as `lanes` neighbouring threads take them in turn, eight of them under way at a time.  f(value, pixels
+// of the share, channel of the group).
+constexpr int kGnItems = 8;
+template <typename F>
+__device__ __forceinline__ void each_item(const GroupNormArgs& g, const float2* part, int cg, int lane, int lanes, F f) {
+    const int whole = lanes / cg, more = lanes - whole * cg;
+    int share = lane / cg, channel = lane - share * cg;
+    while (share < g.chunks) {
+        float2 v[kGnItems];
+        int s[kGnItems], c[kGnItems];
+#pragma unroll
+        for (int u = 0; u < kGnItems; ++u) {
+            s[u] = share;
+            c[u] = channel;
+            if (share < g.chunks) v[u] = __ldcg(part + (int64_t)share * g.C + channel);
+            channel += more;
+            share += whole;
+            if (channel >= cg) { channel -= cg; ++share; }
+        }
+#pragma unroll
+        for (int u = 0; u < kGnItems; ++u)
+            if (s[u] < g.chunks) f(v[u], (float)min(g.share, g.P - s[u] * g.share), c[u]);
+    }
+}
+
+// How the threads of a block share its groups: `lanes` (a power of two) to a group, so that all groups are in hand at once where
+// there are no more groups than threads.
+template <int kThreads = kGnThreads> struct GroupCover {
+    int first, count, lanes, lane, own;
+    template <int kVec> __device__ __forceinline__ GroupCover(const Cover<kVec, kThreads>& cover, int C, int cg) {
+        first = cover.vec0 * kVec / cg;
+        count = min((cover.vec0 + cover.vecs) * kVec - 1, C - 1) / cg - first + 1;
+        lanes = 32;
+        while (lanes > 1 && lanes * count > kThreads) lanes >>= 1;
+        lane = threadIdx.x & (lanes - 1);
+        own = threadIdx.x / lanes;
+    }
+    __device__ __forceinline__ int stride() const { return kThreads / lanes; }
+    __device__ __forceinline__ float add(float v) const {
+        for (int d = lanes >> 1; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        return v;
+    }
+};
 
 // The quantizer of activations (lbt_quantize_act) for one value: clip to [0, c], steps of s = c / (2^bits - 1), ties to even.
 struct ActQuant {
@@ -187,23 +245,66 @@ struct ActQuant {
         if (zero) return 0u;
         return (uint32_t)fminf(rintf(__fdiv_rn(fminf(fmaxf(z, 0.0f), c), s)), levels);
     }
+    // eight neighbouring codes, the first of them element `at` (a multiple of 8)
+    __device__ __forceinline__ void store8(const float* z, int bits, uint8_t* out, int64_t at) const {
+        uint32_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = (*this)(z[i]);
+        if (bits <= 4) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) word |= q[i] << (4 * i);
+            *reinterpret_cast<uint32_t*>(out + at / 2) = word;
+        } else {
+            *reinterpret_cast<uint2*>(out + at) = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+        }
+    }
 };
 
+// The groups of neighbouring channels, one channel after the other (a division once, not for each).
+struct Owner {
+    int group, left;
+    const int cg;
+    __device__ __forceinline__ Owner(int channel, int cg_) : cg(cg_) {
+        group = channel / cg;
+        left = (group + 1) * cg - channel;
+    }
+    __device__ __forceinline__ int next() {
+        const int own = group;
+        if (--left == 0) { left = cg; ++group; }
+        return own;
+    }
+};
+
+// w and b of a block's channels, in shared memory (the kernel ahead does not write them).
+template <int kThreads = kGnThreads> __device__ __forceinline__ void load_params(const GroupNormArgs& g, int c0, int width, float2* params) {
+    for (int i = threadIdx.x; i < width; i += kThreads)
+        params[i] = make_float2(gn_param(g.w, g.param_type, c0 + i, 1.0f), gn_param(g.b, g.param_type, c0 + i, 0.0f));
+}
+
 template <typename T, int kVec, int kAct, bool kCodes>
-__global__ void __launch_bounds__(kGnThreads) groupnorm_apply_kernel(const __grid_constant__ GroupNormArgs g) {
+__global__ void __launch_bounds__(kGnThreads, 4) groupnorm_apply_kernel(const __grid_constant__ GroupNormArgs g) {
     extern __shared__ float2 group[];   // mean and rstd of the groups that this block's channels belong to
+    __shared__ float2 params[kGnThreads * kVec];
     const Cover<kVec> cover(g.C);
     const int n = blockIdx.y, cg = g.C / g.G;
-    const int group0 = cover.vec0 * kVec / cg, group1 = min((cover.vec0 + cover.vecs) * kVec - 1, g.C - 1) / cg;
+    const GroupCover<> groups(cover, g.C, cg);
+    load_params(g, cover.vec0 * kVec, cover.width(), params);
     sm100::griddep_wait();
-    for (int i = group0 + (threadIdx.x >> 5); i <= group1; i += kGnThreads / 32) {
-        const float2 s = group_stats(g, n, i);
-        if ((threadIdx.x & 31) == 0) {
-            group[i - group0] = s;
-            if (g.stats != nullptr && blockIdx.x == 0) {   // (a group on the border of two blocks' channels: both write the same)
-                g.stats[2 * ((int64_t)n * g.G + i)] = s.x;
-                g.stats[2 * ((int64_t)n * g.G + i) + 1] = s.y;
-            }
+    for (int i0 = 0; i0 < groups.count; i0 += groups.stride()) {   // (whole warps stay together)
+        const int i = min(i0 + groups.own, groups.count - 1);
+        const float2* part = reinterpret_cast<const float2*>(g.partial) + (int64_t)n * g.chunks * g.C + (groups.first + i) * cg;
+        const float total = 1.0f / ((float)g.P * (float)cg);
+        float mean = 0.0f, m2 = 0.0f;
+        each_item(g, part, cg, groups.lane, groups.lanes, [&](float2 v, float pixels, int) { mean = fmaf(pixels, v.x, mean); });
+        mean = groups.add(mean) * total;
+        each_item(g, part, cg, groups.lane, groups.lanes, [&](float2 v, float pixels, int) { m2 += fmaf(pixels * (v.x - mean), v.x - mean, v.y); });
+        m2 = groups.add(m2) * total;
+        if (groups.lane == 0 && i0 + groups.own < groups.count) {
+            const float rstd = rsqrtf(m2 + g.eps);
+            group[i] = make_float2(mean, rstd);
+            if (g.stats != nullptr && blockIdx.x == 0)   // (a group on the border of two blocks' channels: both write the same)
+                reinterpret_cast<float2*>(g.stats)[(int64_t)n * g.G + groups.first + i] = make_float2(mean, rstd);
         }
     }
     ActQuant quant{};
@@ -217,29 +318,27 @@ __global__ void __launch_bounds__(kGnThreads) groupnorm_apply_kernel(const __gri
     __syncthreads();
     if (!cover.active) return;
     float mean[kVec], a[kVec], b[kVec];
+    Owner owner(cover.channel(), cg);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-        const int c = cover.channel() + i;
-        const float2 s = group[c / cg - group0];
+        const float2 s = group[owner.next() - groups.first], p = params[cover.vec * kVec + i];
         mean[i] = s.x;
-        a[i] = s.y * gn_param(g.w, g.param_type, c, 1.0f);
-        b[i] = gn_param(g.b, g.param_type, c, 0.0f);
+        a[i] = s.y * p.x;
+        b[i] = p.y;
     }
-    int lo, hi;
-    gn_share(g.P, g.chunks, blockIdx.x, lo, hi);
-    const T* x = static_cast<const T*>(g.x) + (int64_t)n * g.P * g.ld_x + cover.channel();
-    T* y = static_cast<T*>(g.y) + (int64_t)n * g.P * g.ld_y + cover.channel();
-    for (int p = lo + cover.lane; p < hi; p += kGnAhead * cover.lanes) {
+    const int lo = blockIdx.x * g.share, hi = min(lo + g.share, g.P);
+    const int count = max(0, (hi - lo - cover.lane + cover.lanes - 1) / cover.lanes);
+    const T* x = static_cast<const T*>(g.x) + ((int64_t)n * g.P + lo + cover.lane) * g.ld_x + cover.channel();
+    T* y = static_cast<T*>(g.y) + ((int64_t)n * g.P + lo + cover.lane) * g.ld_y + cover.channel();
+    const int64_t step = cover.lanes * g.ld_x, y_step = cover.lanes * g.ld_y;
+    for (int p = 0; p < count; p += kGnAhead) {
         Pack<T, kVec> v[kGnAhead];
 #pragma unroll
-        for (int u = 0; u < kGnAhead; ++u) {
-            const int at = p + u * cover.lanes;
-            v[u].load(x + (at < hi ? at : p) * g.ld_x);
-        }
+        for (int u = 0; u < kGnAhead; ++u)
+            if (p + u < count) v[u].load(x + (p + u) * step);
 #pragma unroll
         for (int u = 0; u < kGnAhead; ++u) {
-            const int at = p + u * cover.lanes;
-            if (at >= hi) break;
+            if (p + u >= count) break;
             float f[kVec];
             v[u].get(f);
 #pragma unroll
@@ -247,20 +346,10 @@ __global__ void __launch_bounds__(kGnThreads) groupnorm_apply_kernel(const __gri
                 const float z = fmaf(f[i] - mean[i], a[i], b[i]);
                 f[i] = kAct == LBT_ACT_NONE ? z : kAct == LBT_ACT_RELU ? (z < 0.0f ? 0.0f : z) : z * sigmoid<T>(z);   // (NaN stays)
             }
-            if (!kCodes || g.y != nullptr) Pack<T, kVec>::store(y + at * g.ld_y, f);
+            if (!kCodes || g.y != nullptr) Pack<T, kVec>::store(y + (p + u) * y_step, f);
             if (kCodes && kVec == 8) {
-                const int64_t at8 = ((int64_t)n * g.P + at) * g.C + cover.channel();
-                uint32_t q[8];
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) q[i] = quant(f[i]);
-                if (g.bits <= 4) {
-                    uint32_t word = 0;
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) word |= q[i] << (4 * i);
-                    *reinterpret_cast<uint32_t*>(g.q + at8 / 2) = word;
-                } else {
-                    *reinterpret_cast<uint2*>(g.q + at8) = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4 % kVec], q[5 % kVec], q[6 % kVec], q[7 % kVec]));
-                }
+                const int64_t at = ((int64_t)n * g.P + lo + cover.lane + (p + u) * cover.lanes) * g.C + cover.channel();
+                quant.store8(f, g.bits, g.q, at);
             }
         }
     }
@@ -275,175 +364,558 @@ __device__ __forceinline__ float act_slope(float z) {
     return s * fmaf(z, 1.0f - s, 1.0f);
 }
 
+// A share's sums of e and e k of each channel.
 template <typename T, int kVec, int kAct>
-__global__ void __launch_bounds__(kGnThreads) groupnorm_sums_kernel(const __grid_constant__ GroupNormArgs g) {
-    __shared__ float2 part[kGnThreads * kVec];   // sums of e and e k by pixel lane and channel
+__global__ void __launch_bounds__(kGnThreads, 3) groupnorm_sums_kernel(const __grid_constant__ GroupNormArgs g) {
+    __shared__ float2 joined[kGnThreads];
+    __shared__ float2 part[kGnThreads * kVec];
+    __shared__ float2 params[kGnThreads * kVec];
+    sm100::griddep_launch_dependents();
     const Cover<kVec> cover(g.C);
-    const int n = blockIdx.y, cg = g.C / g.G;
-    int lo, hi;
-    gn_share(g.P, g.chunks, blockIdx.x, lo, hi);
+    const int n = blockIdx.y, cg = g.C / g.G, width = cover.width();
+    load_params(g, cover.vec0 * kVec, width, params);
+    __syncthreads();
     if (cover.active) {
-        float mean[kVec], rstd[kVec], w[kVec], b[kVec], s1[kVec], s2[kVec];
+        float mean[kVec], a[kVec], b[kVec], s1[kVec], s2[kVec];   // z = (x - mean) a + b; s2: of e (x - mean)
+        const float2* stats = reinterpret_cast<const float2*>(g.stats) + (int64_t)n * g.G;
+        Owner owner(cover.channel(), cg);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const int c = cover.channel() + i;
-            const float* s = g.stats + 2 * ((int64_t)n * g.G + c / cg);
-            mean[i] = s[0];
-            rstd[i] = s[1];
-            w[i] = gn_param(g.w, g.param_type, c, 1.0f);
-            b[i] = gn_param(g.b, g.param_type, c, 0.0f);
+            const float2 s = stats[owner.next()], p = params[cover.vec * kVec + i];
+            mean[i] = s.x;
+            a[i] = s.y * p.x;
+            b[i] = p.y;
             s1[i] = s2[i] = 0.0f;
         }
-        const T* x = static_cast<const T*>(g.x) + (int64_t)n * g.P * g.ld_x + cover.channel();
-        const T* dy = static_cast<const T*>(g.dy) + (int64_t)n * g.P * g.ld_dy + cover.channel();
-        for (int p = lo + cover.lane; p < hi; p += kGnAhead * cover.lanes) {
-            Pack<T, kVec> v[kGnAhead], d[kGnAhead];
+        const int lo = blockIdx.x * g.share, hi = min(lo + g.share, g.P);
+        const int count = max(0, (hi - lo - cover.lane + cover.lanes - 1) / cover.lanes);
+        const T* x = static_cast<const T*>(g.x) + ((int64_t)n * g.P + lo + cover.lane) * g.ld_x + cover.channel();
+        const T* dy = static_cast<const T*>(g.dy) + ((int64_t)n * g.P + lo + cover.lane) * g.ld_dy + cover.channel();
+        const int64_t step = cover.lanes * g.ld_x, dy_step = cover.lanes * g.ld_dy;
+        for (int p = 0; p < count; p += kGnPairs) {
+            Pack<T, kVec> v[kGnPairs], d[kGnPairs];
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                const int at = p + u * cover.lanes < hi ? p + u * cover.lanes : p;
-                v[u].load(x + at * g.ld_x);
-                d[u].load(dy + at * g.ld_dy);
-            }
+            for (int u = 0; u < kGnPairs; ++u)
+                if (p + u < count) {
+                    v[u].load(x + (p + u) * step);
+                    d[u].load(dy + (p + u) * dy_step);
+                }
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                if (p + u * cover.lanes >= hi) break;
+            for (int u = 0; u < kGnPairs; ++u) {
+                if (p + u >= count) break;
                 float f[kVec], e[kVec];
                 v[u].get(f);
                 d[u].get(e);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
-                    const float k = (f[i] - mean[i]) * rstd[i];
-                    if (kAct != LBT_ACT_NONE) e[i] *= act_slope<T, kAct>(fmaf(k, w[i], b[i]));
+                    const float k = f[i] - mean[i];
+                    if (kAct != LBT_ACT_NONE) e[i] *= act_slope<T, kAct>(fmaf(k, a[i], b[i]));
                     s1[i] += e[i];
                     s2[i] = fmaf(e[i], k, s2[i]);
                 }
             }
         }
+        Owner again(cover.channel(), cg);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) part[(cover.lane * cover.vecs + cover.vec) * kVec + i] = make_float2(s1[i], s2[i]);
+        for (int i = 0; i < kVec; ++i) part[cover.lane * width + cover.vec * kVec + i] = make_float2(s1[i], s2[i] * stats[again.next()].y);
     }
     __syncthreads();
-    const int width = cover.vecs * kVec;
-    for (int i = threadIdx.x; i < width; i += kGnThreads) {
-        float2 sum = make_float2(0.0f, 0.0f);
-        for (int l = 0; l < cover.lanes; ++l) {
-            sum.x += part[l * width + i].x;
-            sum.y += part[l * width + i].y;
-        }
-        reinterpret_cast<float2*>(g.partial)[((int64_t)n * g.chunks + blockIdx.x) * g.C + cover.vec0 * kVec + i] = sum;
-    }
+    join_lanes(part, joined, width, cover.lanes, reinterpret_cast<float2*>(g.partial) + ((int64_t)n * g.chunks + blockIdx.x) * g.C + cover.vec0 * kVec);
 }
 
-template <typename T, int kVec, int kAct>
-__global__ void __launch_bounds__(kGnThreads) groupnorm_dx_kernel(const __grid_constant__ GroupNormArgs g) {
-    extern __shared__ float2 group[];   // mean_g(w e) and mean_g(w e k) of this block's groups
-    const Cover<kVec> cover(g.C);
-    const int n = blockIdx.y, cg = g.C / g.G, items = g.chunks * cg;
-    const int group0 = cover.vec0 * kVec / cg, group1 = min((cover.vec0 + cover.vecs) * kVec - 1, g.C - 1) / cg;
-    sm100::griddep_wait();
-    for (int i = group0 + (threadIdx.x >> 5); i <= group1; i += kGnThreads / 32) {
-        const float2* part = reinterpret_cast<const float2*>(g.partial) + (int64_t)n * g.chunks * g.C + i * cg;
-        float e = 0.0f, ek = 0.0f;
-        for (int j = threadIdx.x & 31; j < items; j += 32) {
-            const float2 v = part[(int64_t)(j / cg) * g.C + j % cg];
-            const float w = gn_param(g.w, g.param_type, i * cg + j % cg, 1.0f);
-            e = fmaf(w, v.x, e);
-            ek = fmaf(w, v.y, ek);
-        }
-        const float total = (float)g.P * (float)cg;
-        e = warp_add(e) / total;
-        ek = warp_add(ek) / total;
-        if ((threadIdx.x & 31) == 0) group[i - group0] = make_float2(e, ek);
-    }
-    __syncthreads();
-    if (!cover.active) return;
-    float mean[kVec], rstd[kVec], w[kVec], b[kVec];
-    float2 back[kVec];
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        const int c = cover.channel() + i;
-        const float* s = g.stats + 2 * ((int64_t)n * g.G + c / cg);
-        mean[i] = s[0];
-        rstd[i] = s[1];
-        w[i] = gn_param(g.w, g.param_type, c, 1.0f);
-        b[i] = gn_param(g.b, g.param_type, c, 0.0f);
-        back[i] = group[c / cg - group0];
-    }
-    int lo, hi;
-    gn_share(g.P, g.chunks, blockIdx.x, lo, hi);
-    const T* x = static_cast<const T*>(g.x) + (int64_t)n * g.P * g.ld_x + cover.channel();
-    const T* dy = static_cast<const T*>(g.dy) + (int64_t)n * g.P * g.ld_dy + cover.channel();
-    T* dx = static_cast<T*>(g.dx) + (int64_t)n * g.P * g.ld_dx + cover.channel();
-    constexpr int kAhead = kGnAhead / 2;
-    for (int p = lo + cover.lane; p < hi; p += kAhead * cover.lanes) {
-        Pack<T, kVec> v[kAhead], d[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int at = p + u * cover.lanes < hi ? p + u * cover.lanes : p;
-            v[u].load(x + at * g.ld_x);
-            d[u].load(dy + at * g.ld_dy);
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int at = p + u * cover.lanes;
-            if (at >= hi) break;
-            float f[kVec], e[kVec];
-            v[u].get(f);
-            d[u].get(e);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                const float k = (f[i] - mean[i]) * rstd[i];
-                if (kAct != LBT_ACT_NONE) e[i] *= act_slope<T, kAct>(fmaf(k, w[i], b[i]));
-                f[i] = rstd[i] * (fmaf(e[i], w[i], -back[i].x) - k * back[i].y);
-            }
-            Pack<T, kVec>::store(dx + at * g.ld_dx, f);
-        }
-    }
-}
-
-// dw and db: sums over images and shares.  32 channels a block, eight rows of shares side by side.
-__global__ void __launch_bounds__(256) groupnorm_finish_kernel(const float2* partial, int rows, int C, void* dw, void* db, int type) {
-    __shared__ float2 part[8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
+// dw and db of 32 channels: sums over images and shares, eight rows of them side by side.
+__device__ __forceinline__ void param_grads(const GroupNormArgs& g, int rows, int c0, float2 (*part)[32]) {
+    const int lane = threadIdx.x >> 5, c = c0 + (threadIdx.x & 31);
     float2 sum = make_float2(0.0f, 0.0f);
-    sm100::griddep_wait();
-    if (c < C)
-        for (int r = lane; r < rows; r += 8) {
-            const float2 v = partial[(int64_t)r * C + c];
-            sum.x += v.x;
-            sum.y += v.y;
+    if (c < g.C)
+        for (int r = lane; r < rows; r += kGnItems * kGnThreads / 32) {
+            float2 v[kGnItems];
+#pragma unroll
+            for (int u = 0; u < kGnItems; ++u) {
+                const int at = r + u * (kGnThreads / 32);
+                v[u] = at < rows ? __ldcg(reinterpret_cast<const float2*>(g.partial) + (int64_t)at * g.C + c) : make_float2(0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int u = 0; u < kGnItems; ++u) {
+                sum.x += v[u].x;
+                sum.y += v[u].y;
+            }
         }
+    __syncthreads();
     part[lane][threadIdx.x & 31] = sum;
     __syncthreads();
-    if (lane != 0 || c >= C) return;
-    for (int l = 1; l < 8; ++l) {
+    if (lane != 0 || c >= g.C) return;
+    for (int l = 1; l < kGnThreads / 32; ++l) {
         sum.x += part[l][threadIdx.x].x;
         sum.y += part[l][threadIdx.x].y;
     }
     auto put = [&](void* p, float v) {
         if (p == nullptr) return;
-        if (type == LBT_F32) static_cast<float*>(p)[c] = v;
-        else if (type == LBT_BF16) static_cast<__nv_bfloat16*>(p)[c] = from_f32<__nv_bfloat16>(v);
+        if (g.param_type == LBT_F32) static_cast<float*>(p)[c] = v;
+        else if (g.param_type == LBT_BF16) static_cast<__nv_bfloat16*>(p)[c] = from_f32<__nv_bfloat16>(v);
         else static_cast<__half*>(p)[c] = from_f32<__half>(v);
     };
-    put(db, sum.x);
-    put(dw, sum.y);
+    put(g.db, sum.x);
+    put(g.dw, sum.y);
+}
+
+// The first row of blocks forms the parameters' gradients, the others an image's dx each.
+template <typename T, int kVec, int kAct>
+__global__ void __launch_bounds__(kGnThreads, 3) groupnorm_dx_kernel(const __grid_constant__ GroupNormArgs g) {
+    extern __shared__ float2 group[];   // mean_g(w e) and mean_g(w e k) of this block's groups
+    __shared__ float2 params[kGnThreads * kVec];
+    if (blockIdx.y == 0) {
+        __shared__ float2 part[kGnThreads / 32][32];
+        sm100::griddep_wait();
+        for (int c = 32 * (blockIdx.x + blockIdx.z * gridDim.x); c < g.C; c += 32 * gridDim.x * gridDim.z) param_grads(g, g.N * g.chunks, c, part);
+        return;
+    }
+    const Cover<kVec> cover(g.C);
+    const int n = blockIdx.y - 1, cg = g.C / g.G;
+    const GroupCover<> groups(cover, g.C, cg);
+    load_params(g, cover.vec0 * kVec, cover.width(), params);
+    sm100::griddep_wait();
+    for (int i0 = 0; i0 < groups.count; i0 += groups.stride()) {
+        const int i = min(i0 + groups.own, groups.count - 1);
+        const float2* part = reinterpret_cast<const float2*>(g.partial) + (int64_t)n * g.chunks * g.C + (groups.first + i) * cg;
+        float e = 0.0f, ek = 0.0f;
+        each_item(g, part, cg, groups.lane, groups.lanes, [&](float2 v, float, int c) {
+            const float w = gn_param(g.w, g.param_type, (groups.first + i) * cg + c, 1.0f);
+            e = fmaf(w, v.x, e);
+            ek = fmaf(w, v.y, ek);
+        });
+        const float total = 1.0f / ((float)g.P * (float)cg);
+        e = groups.add(e) * total;
+        ek = groups.add(ek) * total;
+        if (groups.lane == 0 && i0 + groups.own < groups.count) group[i] = make_float2(e, ek);
+    }
+    __syncthreads();
+    if (!cover.active) return;
+    float mean[kVec], a[kVec], b[kVec], c1[kVec], c2[kVec];   // dx = e a - c1 - (x - mean) c2
+    const float2* stats = reinterpret_cast<const float2*>(g.stats) + (int64_t)n * g.G;
+    Owner owner(cover.channel(), cg);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        const int own = owner.next();
+        const float2 s = stats[own], p = params[cover.vec * kVec + i], back = group[own - groups.first];
+        mean[i] = s.x;
+        a[i] = s.y * p.x;
+        b[i] = p.y;
+        c1[i] = s.y * back.x;
+        c2[i] = s.y * s.y * back.y;
+    }
+    const int lo = blockIdx.x * g.share, hi = min(lo + g.share, g.P);
+    const int count = max(0, (hi - lo - cover.lane + cover.lanes - 1) / cover.lanes);
+    const int64_t at = (int64_t)n * g.P + lo + cover.lane, step = cover.lanes * g.ld_x, dy_step = cover.lanes * g.ld_dy, dx_step = cover.lanes * g.ld_dx;
+    const T* x = static_cast<const T*>(g.x) + at * g.ld_x + cover.channel();
+    const T* dy = static_cast<const T*>(g.dy) + at * g.ld_dy + cover.channel();
+    T* dx = static_cast<T*>(g.dx) + at * g.ld_dx + cover.channel();
+    for (int p = 0; p < count; p += kGnPairs) {
+        Pack<T, kVec> v[kGnPairs], d[kGnPairs];
+#pragma unroll
+        for (int u = 0; u < kGnPairs; ++u)
+            if (p + u < count) {
+                v[u].load(x + (p + u) * step);
+                d[u].load(dy + (p + u) * dy_step);
+            }
+#pragma unroll
+        for (int u = 0; u < kGnPairs; ++u) {
+            if (p + u >= count) break;
+            float f[kVec], e[kVec];
+            v[u].get(f);
+            d[u].get(e);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const float k = f[i] - mean[i];
+                if (kAct != LBT_ACT_NONE) e[i] *= act_slope<T, kAct>(fmaf(k, a[i], b[i]));
+                f[i] = fmaf(e[i], a[i], -fmaf(k, c2[i], c1[i]));
+            }
+            Pack<T, kVec>::store(dx + (p + u) * dx_step, f);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- images kept on chip
+// kVec fp32 values.
+template <int kVec> struct Vals {
+    float f[kVec];
+    __device__ __forceinline__ void fill(float v) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) f[i] = v;
+    }
+};
+template <int kVec> __device__ __forceinline__ Vals<kVec> add(const Vals<kVec>& a, const Vals<kVec>& b) {
+    Vals<kVec> r;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) r.f[i] = a.f[i] + b.f[i];
+    return r;
+}
+template <int kVec> __device__ __forceinline__ Vals<kVec> mul(const Vals<kVec>& a, const Vals<kVec>& b) {
+    Vals<kVec> r;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) r.f[i] = a.f[i] * b.f[i];
+    return r;
+}
+template <int kVec> __device__ __forceinline__ Vals<kVec> fma(const Vals<kVec>& a, const Vals<kVec>& b, const Vals<kVec>& c) {
+    Vals<kVec> r;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) r.f[i] = fmaf(a.f[i], b.f[i], c.f[i]);
+    return r;
+}
+template <int kVec> __device__ __forceinline__ Vals<kVec> all(float v) {
+    Vals<kVec> r;
+    r.fill(v);
+    return r;
+}
+// 1 / (1 + exp(-z)); see sigmoid
+template <typename T, int kVec> __device__ __forceinline__ Vals<kVec> sigmoids(const Vals<kVec>& z) {
+    Vals<kVec> s;
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) s.f[i] = sigmoid<T>(z.f[i]);
+        return s;
+    }
+    s = mul(z, all<kVec>(-1.4426950408889634f));
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(s.f[i]) : "f"(s.f[i]));
+    s = add(s, all<kVec>(1.0f));
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.f[i]) : "f"(s.f[i]));
+    return s;
+}
+
+// What a thread keeps of an image in shared memory: its packs, one behind the other for all threads (pack k of the thread at
+// (k threads + thread)); nobody else reads them, so that they need no barrier.
+template <typename T, int kVec, int kThreads> struct Kept {
+    uint8_t* base;
+    __device__ __forceinline__ T* at(int k) const { return reinterpret_cast<T*>(base) + (k * kThreads + (int)threadIdx.x) * kVec; }
+    __device__ __forceinline__ void fetch(int k, const T* src) const {
+        if constexpr (kVec == 1) *at(k) = *src;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) * kVec / 16; ++i)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(at(k)) + 16 * i), "l"(reinterpret_cast<const uint8_t*>(src) + 16 * i) : "memory");
+    }
+    __device__ __forceinline__ Vals<kVec> get(int k) const {
+        Vals<kVec> v;
+        if constexpr (kVec == 1) {
+            v.f[0] = to_f32(*at(k));
+        } else {
+            Vec8<T> w;
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) * kVec / 16; ++i) {
+                const uint4 q = reinterpret_cast<const uint4*>(at(k))[i];
+                w.w[4 * i] = q.x; w.w[4 * i + 1] = q.y; w.w[4 * i + 2] = q.z; w.w[4 * i + 3] = q.w;
+            }
+            unpack(w, reinterpret_cast<float (&)[8]>(v.f));
+        }
+        return v;
+    }
+};
+
+// A thread's `count` packs are fetched in four parts, each worked on while the next are under way.
+template <typename Fetch> __device__ __forceinline__ void fetch_parts(int count, Fetch fetch) {
+    const int part = (count + 3) / 4;
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {
+        for (int k = q * part; k < min((q + 1) * part, count); ++k) fetch(k);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+}
+template <int kLeft> __device__ __forceinline__ void parts_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+template <typename F> __device__ __forceinline__ void as_they_come(int count, F f) {
+    const int part = (count + 3) / 4;
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {
+        if (q == 0) parts_wait<3>();
+        else if (q == 1) parts_wait<2>();
+        else if (q == 2) parts_wait<1>();
+        else parts_wait<0>();
+#pragma unroll 2
+        for (int k = q * part; k < min((q + 1) * part, count); ++k) f(k);
+    }
+}
+
+// The sum over the CTA's pixel lanes of kVec values a thread, into out[2 * channel].  `rows`: [image_rows][C].
+template <int kVec, int kThreads>
+__device__ __forceinline__ void lanes_sum(Vals<kVec> v, const Cover<kVec, kThreads>& cover, float* rows, float* out) {
+    const int width = cover.width();
+    const bool even = cover.vecs <= 32 && 32 % cover.vecs == 0;   // a warp holds whole pixels
+    if (even) {
+        for (int d = cover.vecs; d < 32; d <<= 1)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v.f[i] += __shfl_xor_sync(0xFFFFFFFFu, v.f[i], d);
+        if ((threadIdx.x & 31) < cover.vecs)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) rows[(threadIdx.x >> 5) * width + cover.vec * kVec + i] = v.f[i];
+    } else if (cover.active) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) rows[cover.lane * width + cover.vec * kVec + i] = v.f[i];
+    }
+    __syncthreads();
+    const int count = even ? kThreads / 32 : cover.lanes;
+    for (int i = threadIdx.x; i < width; i += kThreads) {
+        float s = 0.0f;
+#pragma unroll 4
+        for (int l = 0; l < count; ++l) s += rows[l * width + i];
+        out[2 * i] = s;
+    }
+    __syncthreads();
+}
+static int image_rows(int vecs, int threads) { return vecs <= 32 && 32 % vecs == 0 ? threads / 32 : threads / vecs; }
+
+__device__ __forceinline__ float2 ld_cluster2(const float2* p, int cta) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(sm100::map_to_cta(sm100::smem_u32(p), cta)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// How shared memory begins in both kernels below; the packs that are kept come behind it, at g.kept.
+struct ImageSpace {
+    float2* chan;     // [C] sums of this CTA's pixels by channel
+    float2* params;   // [C]
+    float2* own;      // [G] sums of this CTA's pixels by group: read by the other CTAs
+    float2* group;    // [G] of the whole image
+    float* rows;
+    __device__ __forceinline__ ImageSpace(uint8_t* at, int C, int G) {
+        chan = reinterpret_cast<float2*>(at);
+        params = chan + C;
+        own = params + C;
+        group = own + G;
+        rows = reinterpret_cast<float*>(group + G);
+    }
+};
+
+// One cluster an image.
+template <typename T, int kVec, int kAct, bool kCodes, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_kernel(const __grid_constant__ GroupNormArgs g) {
+    extern __shared__ __align__(16) uint8_t image[];
+    const Cover<kVec, kThreads> cover(g.C);
+    const ImageSpace space(image, g.C, g.G);
+    const Kept<T, kVec, kThreads> kept{image + g.kept};
+    const int n = blockIdx.y, cta = blockIdx.x, ctas = gridDim.x, cg = g.C / g.G;
+    const int lo = min(cta * g.share, g.P), hi = min(lo + g.share, g.P);
+    const int count = cover.active ? max(0, (hi - lo - cover.lane + cover.lanes - 1) / cover.lanes) : 0;
+    const T* x = static_cast<const T*>(g.x) + ((int64_t)n * g.P + lo + cover.lane) * g.ld_x + cover.channel();
+    const int64_t step = cover.lanes * g.ld_x;
+    fetch_parts(count, [&](int k) { kept.fetch(k, x + k * step); });
+    load_params<kThreads>(g, 0, g.C, space.params);
+    Vals<kVec> s1 = all<kVec>(0.0f), s2 = all<kVec>(0.0f);
+    as_they_come(count, [&](int k) { s1 = add(s1, kept.get(k)); });
+    lanes_sum(s1, cover, space.rows, &space.chan[0].x);
+    const float pixels = (float)(hi - lo), inv = hi > lo ? 1.0f / pixels : 0.0f;
+    Vals<kVec> centre = all<kVec>(0.0f);   // minus this CTA's mean
+    if (cover.active)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) centre.f[i] = -space.chan[cover.vec * kVec + i].x * inv;
+#pragma unroll 4
+    for (int k = 0; k < count; ++k) {
+        const Vals<kVec> d = add(kept.get(k), centre);
+        s2 = fma(d, d, s2);
+    }
+    lanes_sum(s2, cover, space.rows, &space.chan[0].y);
+    // this CTA's mean and centred sum of squares of each group, then the image's
+    const GroupCover<kThreads> groups(cover, g.C, cg);
+    for (int i0 = 0; i0 < groups.count; i0 += groups.stride()) {   // (whole warps stay together)
+        const int i = min(i0 + groups.own, groups.count - 1);
+        float mean = 0.0f, m2 = 0.0f;
+        for (int c = groups.lane; c < cg; c += groups.lanes) mean += space.chan[i * cg + c].x;
+        mean = groups.add(mean) * inv / (float)cg;
+        for (int c = groups.lane; c < cg; c += groups.lanes) {
+            const float2 v = space.chan[i * cg + c];
+            const float d = v.x * inv - mean;
+            m2 += fmaf(pixels * d, d, v.y);
+        }
+        m2 = groups.add(m2);
+        if (groups.lane == 0 && i0 + groups.own < groups.count) space.own[i] = make_float2(mean, m2);
+    }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    const float total = 1.0f / (float)g.P;
+    for (int i = threadIdx.x; i < g.G; i += kThreads) {
+        float2 v[16];
+        float mean = 0.0f, m2 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+            if (c < ctas) v[c] = ld_cluster2(space.own + i, c);
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+            if (c < ctas) mean = fmaf((float)max(0, min(g.share, g.P - c * g.share)), v[c].x, mean);
+        mean *= total;
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+            if (c < ctas) m2 += fmaf((float)max(0, min(g.share, g.P - c * g.share)) * (float)cg * (v[c].x - mean), v[c].x - mean, v[c].y);
+        space.group[i] = make_float2(mean, rsqrtf(m2 * total / (float)cg + g.eps));
+        if (g.stats != nullptr && cta == 0) reinterpret_cast<float2*>(g.stats)[(int64_t)n * g.G + i] = space.group[i];
+    }
+    __syncthreads();
+    cluster_arrive();   // this CTA reads no other's sums any more
+    ActQuant quant{};
+    if (kCodes) {
+        quant.c = *g.clip;
+        quant.levels = (float)((1 << g.bits) - 1);
+        quant.s = __fdiv_rn(quant.c, quant.levels);
+        quant.zero = !(quant.s > 0.0f) || isinf(quant.s);
+        if (cta == 0 && n == 0 && threadIdx.x == 0) *g.q_scale = quant.zero ? 0.0f : quant.s;
+    }
+    if (cover.active) {
+        Vals<kVec> a, b;
+        Owner owner(cover.channel(), cg);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float2 s = space.group[owner.next()], p = space.params[cover.vec * kVec + i];
+            centre.f[i] = -s.x;
+            a.f[i] = s.y * p.x;
+            b.f[i] = p.y;
+        }
+        T* y = static_cast<T*>(g.y) + ((int64_t)n * g.P + lo + cover.lane) * g.ld_y + cover.channel();
+        const int64_t y_step = cover.lanes * g.ld_y;
+#pragma unroll 2
+        for (int k = 0; k < count; ++k) {
+            Vals<kVec> z = fma(add(kept.get(k), centre), a, b);
+            if (kAct == LBT_ACT_SILU) z = mul(z, sigmoids<T>(z));
+            if (kAct == LBT_ACT_RELU)
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) z.f[i] = z.f[i] < 0.0f ? 0.0f : z.f[i];   // (NaN stays)
+            if (!kCodes || g.y != nullptr) Pack<T, kVec>::store(y + k * y_step, z.f);
+            if constexpr (kCodes && kVec == 8)
+                quant.store8(z.f, g.bits, g.q, ((int64_t)n * g.P + lo + cover.lane + k * cover.lanes) * g.C + cover.channel());
+        }
+    }
+    cluster_wait();
+}
+
+// dy act'(z) at k = x - mean, z = k a + b
+template <typename T, int kVec, int kAct>
+__device__ __forceinline__ Vals<kVec> slopes(Vals<kVec> e, const Vals<kVec>& k, const Vals<kVec>& a, const Vals<kVec>& b) {
+    if constexpr (kAct == LBT_ACT_SILU) {
+        const Vals<kVec> z = fma(k, a, b), s = sigmoids<T>(z);
+        e = mul(e, mul(s, fma(z, fma(s, all<kVec>(-1.0f), all<kVec>(1.0f)), all<kVec>(1.0f))));
+    } else if constexpr (kAct == LBT_ACT_RELU) {
+        const Vals<kVec> z = fma(k, a, b);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) e.f[i] = z.f[i] > 0.0f ? e.f[i] : 0.0f * e.f[i];
+    }
+    return e;
+}
+
+// Its gradients: x and dy are kept; partial: [N, C] sums of e and e k for the parameters' gradients.
+template <typename T, int kVec, int kAct, int kThreads>
+__global__ void __launch_bounds__(kThreads, 768 / kThreads) groupnorm_image_grad_kernel(const __grid_constant__ GroupNormArgs g) {
+    extern __shared__ __align__(16) uint8_t image[];
+    sm100::griddep_launch_dependents();
+    const Cover<kVec, kThreads> cover(g.C);
+    const ImageSpace space(image, g.C, g.G);   // sums of e and e k
+    const int n = blockIdx.y, cta = blockIdx.x, ctas = gridDim.x, cg = g.C / g.G;
+    const int lo = min(cta * g.share, g.P), hi = min(lo + g.share, g.P);
+    const int count = cover.active ? max(0, (hi - lo - cover.lane + cover.lanes - 1) / cover.lanes) : 0;
+    const int most = (g.share + cover.lanes - 1) / cover.lanes;   // packs that any thread keeps of one tensor
+    const Kept<T, kVec, kThreads> kept{image + g.kept}, kept_dy{image + g.kept + most * kThreads * kVec * (int)sizeof(T)};
+    const int64_t at = (int64_t)n * g.P + lo + cover.lane, step = cover.lanes * g.ld_x, dy_step = cover.lanes * g.ld_dy, dx_step = cover.lanes * g.ld_dx;
+    const T* x = static_cast<const T*>(g.x) + at * g.ld_x + cover.channel();
+    const T* dy = static_cast<const T*>(g.dy) + at * g.ld_dy + cover.channel();
+    fetch_parts(count, [&](int k) { kept.fetch(k, x + k * step); kept_dy.fetch(k, dy + k * dy_step); });
+    load_params<kThreads>(g, 0, g.C, space.params);
+    for (int i = threadIdx.x; i < g.G; i += kThreads) space.group[i] = reinterpret_cast<const float2*>(g.stats)[(int64_t)n * g.G + i];
+    __syncthreads();
+    Vals<kVec> centre, a, b, rstd, s1 = all<kVec>(0.0f), s2 = all<kVec>(0.0f);
+    Owner owner(cover.channel(), cg);
+    if (cover.active)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float2 s = space.group[owner.next()], p = space.params[cover.vec * kVec + i];
+            centre.f[i] = -s.x;
+            a.f[i] = s.y * p.x;
+            b.f[i] = p.y;
+            rstd.f[i] = s.y;
+        }
+    as_they_come(count, [&](int i) {
+        const Vals<kVec> k = add(kept.get(i), centre), e = slopes<T, kVec, kAct>(kept_dy.get(i), k, a, b);
+        s1 = add(s1, e);
+        s2 = fma(e, k, s2);
+    });
+    if (cover.active) s2 = mul(s2, rstd);
+    lanes_sum(s1, cover, space.rows, &space.chan[0].x);
+    lanes_sum(s2, cover, space.rows, &space.chan[0].y);
+    const GroupCover<kThreads> groups(cover, g.C, cg);
+    for (int i0 = 0; i0 < groups.count; i0 += groups.stride()) {   // (whole warps stay together)
+        const int i = min(i0 + groups.own, groups.count - 1);
+        float e = 0.0f, ek = 0.0f;
+        for (int c = groups.lane; c < cg; c += groups.lanes) {
+            e = fmaf(space.params[i * cg + c].x, space.chan[i * cg + c].x, e);
+            ek = fmaf(space.params[i * cg + c].x, space.chan[i * cg + c].y, ek);
+        }
+        e = groups.add(e);
+        ek = groups.add(ek);
+        if (groups.lane == 0 && i0 + groups.own < groups.count) space.own[i] = make_float2(e, ek);
+    }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    if (g.dw != nullptr || g.db != nullptr)   // each CTA adds up some of the channels for its image
+        for (int i = cta * kThreads + threadIdx.x; i < g.C; i += ctas * kThreads) {
+            float2 sum = make_float2(0.0f, 0.0f);
+            for (int c = 0; c < ctas; ++c) {
+                const float2 v = ld_cluster2(space.chan + i, c);
+                sum.x += v.x;
+                sum.y += v.y;
+            }
+            reinterpret_cast<float2*>(g.partial)[(int64_t)n * g.C + i] = sum;
+        }
+    const float total = 1.0f / ((float)g.P * (float)cg);
+    for (int i = threadIdx.x; i < g.G; i += kThreads) {   // rstd mean_g(w e), rstd^2 mean_g(w e k)
+        float2 sum = make_float2(0.0f, 0.0f);
+        for (int c = 0; c < ctas; ++c) {
+            const float2 v = ld_cluster2(space.own + i, c);
+            sum.x += v.x;
+            sum.y += v.y;
+        }
+        const float r = space.group[i].y;
+        space.group[i] = make_float2(sum.x * total * r, sum.y * total * r * r);
+    }
+    __syncthreads();
+    cluster_arrive();   // this CTA reads no other's sums any more
+    if (g.dx != nullptr && cover.active) {
+        Vals<kVec> c1, c2;   // dx = e a - c1 - (x - mean) c2
+        Owner again(cover.channel(), cg);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float2 back = space.group[again.next()];
+            c1.f[i] = -back.x;
+            c2.f[i] = -back.y;
+        }
+        T* dx = static_cast<T*>(g.dx) + at * g.ld_dx + cover.channel();
+        for (int i = 0; i < count; ++i) {
+            const Vals<kVec> k = add(kept.get(i), centre);
+            const Vals<kVec> d = fma(slopes<T, kVec, kAct>(kept_dy.get(i), k, a, b), a, fma(k, c2, c1));
+            Pack<T, kVec>::store(dx + i * dx_step, d.f);
+        }
+    }
+    cluster_wait();
+}
+
+__global__ void __launch_bounds__(kGnThreads) groupnorm_params_kernel(const __grid_constant__ GroupNormArgs g) {
+    __shared__ float2 part[kGnThreads / 32][32];
+    sm100::griddep_wait();
+    param_grads(g, g.N, 32 * blockIdx.x, part);
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-// Shares of an image's pixels: enough blocks to fill the SMs four times over, and four pixels a thread at least.
+// Shares of an image's pixels: four blocks to an SM, all resident at once, and four pixels a thread at least.
 static int gn_chunks(int64_t N, int64_t P, int64_t C, int vec) {
     const int64_t vecs = (C + vec - 1) / vec, tiles = (vecs + kGnThreads - 1) / kGnThreads, lanes = kGnThreads / std::min<int64_t>(vecs, kGnThreads);
-    const int64_t want = ((int64_t)kNumSMs * 4 + N * tiles - 1) / (N * tiles), most = (P + lanes * kGnAhead - 1) / (lanes * kGnAhead);
+    const int64_t want = (int64_t)kNumSMs * 4 / (N * tiles), most = (P + lanes * kGnAhead - 1) / (lanes * kGnAhead);
     return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, kGnMaxChunks}));
 }
 
 // The second kernel of a pair may set up while the first one ends.
 template <typename... Args>
-static lbt_status gn_chained(void (*kernel)(Args...), dim3 grid, size_t smem, cudaStream_t stream, Args... args) {
+static lbt_status gn_chained(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
     cudaLaunchConfig_t config{};
     config.gridDim = grid;
-    config.blockDim = dim3(kGnThreads);
+    config.blockDim = dim3(threads);
     config.dynamicSmemBytes = smem;
     config.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -455,21 +927,71 @@ static lbt_status gn_chained(void (*kernel)(Args...), dim3 grid, size_t smem, cu
     return launch_status();
 }
 
-template <typename T, int kVec, int kAct>
-static lbt_status gn_forward(const GroupNormArgs& g, dim3 grid, cudaStream_t stream) {
-    groupnorm_stats_kernel<T, kVec><<<grid, kGnThreads, 0, stream>>>(g);
-    if (launch_status() != LBT_OK) return LBT_ERR_CUDA;
-    const size_t smem = sizeof(float2) * std::min(g.G, kGnThreads * kVec);
-    if (g.q != nullptr) return gn_chained(groupnorm_apply_kernel<T, kVec, kAct, true>, grid, smem, stream, g);
-    return gn_chained(groupnorm_apply_kernel<T, kVec, kAct, false>, grid, smem, stream, g);
+constexpr size_t kGnSmem = 110 * 1024;   // shared memory of a CTA that keeps pixels: two of them to an SM
+// CTAs of the cluster that keeps an image on chip (`tensors` of its size) with blocks of so many threads, 0 if it does not fit one;
+// where the kept packs begin and the bytes of shared memory.
+static int gn_cluster(GroupNormArgs& g, int vec, int threads, size_t size, int tensors, size_t* smem) {
+    const int vecs = (g.C + vec - 1) / vec;
+    if (vecs > threads) return 0;
+    const int lanes = threads / vecs;
+    g.kept = (int)((sizeof(float2) * 2 * (g.C + g.G) + sizeof(float) * image_rows(vecs, threads) * g.C + 15) / 16 * 16);
+    for (int ctas : {8, 16}) {
+        const int share = (g.P + ctas - 1) / ctas;
+        *smem = g.kept + (size_t)tensors * ((share + lanes - 1) / lanes) * threads * vec * size;
+        if (*smem > kGnSmem) continue;
+        g.share = share;
+        return ctas;
+    }
+    return 0;
+}
+
+static lbt_status gn_image_launch(void (*kernel)(GroupNormArgs), const GroupNormArgs& g, int ctas, int threads, size_t smem, cudaStream_t stream) {
+    LBT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGnSmem));
+    if (ctas > 8) LBT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(ctas, g.N);
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    config.attrs = attr;
+    config.numAttrs = 1;
+    LBT_CUDA_TRY(cudaLaunchKernelEx(&config, kernel, g));
+    return launch_status();
 }
 
 template <typename T, int kVec, int kAct>
-static lbt_status gn_backward(const GroupNormArgs& g, dim3 grid, cudaStream_t stream) {
+static lbt_status gn_forward(const GroupNormArgs& args, dim3 grid, cudaStream_t stream) {
+    GroupNormArgs g = args;
+    size_t smem = 0;
+    if (const int ctas = gn_cluster(g, kVec, kGnThreads, sizeof(T), 1, &smem))
+        return gn_image_launch(g.q != nullptr ? groupnorm_image_kernel<T, kVec, kAct, true, kGnThreads> : groupnorm_image_kernel<T, kVec, kAct, false, kGnThreads>,
+                               g, ctas, kGnThreads, smem, stream);
+    g = args;
+    groupnorm_stats_kernel<T, kVec><<<grid, kGnThreads, 0, stream>>>(g);
+    if (launch_status() != LBT_OK) return LBT_ERR_CUDA;
+    smem = sizeof(float2) * std::min(g.G, kGnThreads * kVec);
+    if (g.q != nullptr) return gn_chained(groupnorm_apply_kernel<T, kVec, kAct, true>, grid, kGnThreads, smem, stream, g);
+    return gn_chained(groupnorm_apply_kernel<T, kVec, kAct, false>, grid, kGnThreads, smem, stream, g);
+}
+
+template <typename T, int kVec, int kAct>
+static lbt_status gn_backward(const GroupNormArgs& args, dim3 grid, cudaStream_t stream) {
+    GroupNormArgs g = args;
+    size_t smem = 0;
+    if (const int ctas = gn_cluster(g, kVec, kGnThreads, sizeof(T), 2, &smem)) {
+        const lbt_status s = gn_image_launch(groupnorm_image_grad_kernel<T, kVec, kAct, kGnThreads>, g, ctas, kGnThreads, smem, stream);
+        if (s != LBT_OK || (g.dw == nullptr && g.db == nullptr)) return s;
+        return gn_chained(groupnorm_params_kernel, dim3((g.C + 31) / 32), kGnThreads, 0, stream, g);
+    }
+    g = args;
     groupnorm_sums_kernel<T, kVec, kAct><<<grid, kGnThreads, 0, stream>>>(g);
     if (launch_status() != LBT_OK) return LBT_ERR_CUDA;
-    if (g.dx == nullptr) return LBT_OK;
-    return gn_chained(groupnorm_dx_kernel<T, kVec, kAct>, grid, sizeof(float2) * std::min(g.G, kGnThreads * kVec), stream, g);
+    grid.y = (g.dx != nullptr ? grid.y : 0) + 1;
+    return gn_chained(groupnorm_dx_kernel<T, kVec, kAct>, grid, kGnThreads, sizeof(float2) * std::min(g.G, kGnThreads * kVec), stream, g);
 }
 
 template <typename T, int kVec>
@@ -487,7 +1009,8 @@ static lbt_status gn_run_act(const GroupNormArgs& g, dim3 grid, bool forward, cu
 template <typename T>
 static lbt_status gn_run_vec(GroupNormArgs& g, int64_t N, bool wide, bool forward, cudaStream_t stream) {
     const int vec = wide ? 8 : 1, vecs = (g.C + vec - 1) / vec;
-    g.chunks = gn_chunks(N, g.P, g.C, vec);
+    g.share = (g.P + gn_chunks(N, g.P, g.C, vec) - 1) / gn_chunks(N, g.P, g.C, vec);
+    g.chunks = (g.P + g.share - 1) / g.share;   // (no share is empty)
     const dim3 grid(g.chunks, (unsigned)N, (vecs + kGnThreads - 1) / kGnThreads);
     return wide ? gn_run_act<T, 8>(g, grid, forward, stream) : gn_run_act<T, 1>(g, grid, forward, stream);
 }
@@ -509,7 +1032,7 @@ static lbt_status gn_check(const lbt_groupnorm_desc* desc, lbt_groupnorm_desc* d
         if (*ld == 0) *ld = d->C;
         if (*ld < d->C) return LBT_ERR_INVALID_ARG;
     }
-    if (d->N > 65535 || d->P > (1 << 30) || d->C > (1 << 20)) return LBT_ERR_UNSUPPORTED;
+    if (d->N > 65534 || d->P > (1 << 30) || d->C > (1 << 20)) return LBT_ERR_UNSUPPORTED;
     return LBT_OK;
 }
 
@@ -541,7 +1064,7 @@ extern "C" lbt_status lbt_groupnorm_forward(const lbt_groupnorm_desc* desc, cons
     if ((y == nullptr && q == nullptr) || (q != nullptr && (d_clip == nullptr || d_scale_out == nullptr))) return LBT_ERR_INVALID_ARG;
     if (q != nullptr && (bits < 2 || bits > 8)) return LBT_ERR_UNSUPPORTED_BITS;
     const size_t e = type_size(d.type), pe = type_size(d.param_type);
-    if (gn_off(x, e) || gn_off(y, e) || gn_off(w, pe) || gn_off(b, pe) || gn_off(stats, 4) || gn_off(d_clip, 4) || gn_off(d_scale_out, 4) ||
+    if (gn_off(x, e) || gn_off(y, e) || gn_off(w, pe) || gn_off(b, pe) || gn_off(stats, 8) || gn_off(d_clip, 4) || gn_off(d_scale_out, 4) ||
         gn_off(q, 16) || gn_off(ws, 8))
         return LBT_ERR_ALIGNMENT;
     const bool wide = gn_wide(d, {{x, d.ld_x}, {y, d.ld_y}});
@@ -552,7 +1075,7 @@ extern "C" lbt_status lbt_groupnorm_forward(const lbt_groupnorm_desc* desc, cons
     GroupNormArgs g{};
     g.x = x; g.w = w; g.b = b; g.y = y; g.q = static_cast<uint8_t*>(q); g.clip = d_clip; g.q_scale = d_scale_out; g.stats = stats;
     g.partial = static_cast<float*>(ws);
-    g.ld_x = d.ld_x; g.ld_y = d.ld_y;
+    g.ld_x = d.ld_x; g.ld_y = d.ld_y; g.N = (int)d.N;
     g.P = (int)d.P; g.C = (int)d.C; g.G = (int)d.G; g.act = d.act; g.bits = bits; g.param_type = d.param_type; g.eps = d.eps;
     return gn_run(g, d.N, d.type, wide, true, as_stream(cuda_stream));
 }
@@ -564,7 +1087,7 @@ extern "C" lbt_status lbt_groupnorm_backward(const lbt_groupnorm_desc* desc, con
     if (rc != LBT_OK) return rc;
     if (dx == nullptr && dw == nullptr && db == nullptr) return LBT_ERR_INVALID_ARG;
     const size_t e = type_size(d.type), pe = type_size(d.param_type);
-    if (gn_off(dy, e) || gn_off(x, e) || gn_off(dx, e) || gn_off(w, pe) || gn_off(b, pe) || gn_off(dw, pe) || gn_off(db, pe) || gn_off(stats, 4) || gn_off(ws, 8))
+    if (gn_off(dy, e) || gn_off(x, e) || gn_off(dx, e) || gn_off(w, pe) || gn_off(b, pe) || gn_off(dw, pe) || gn_off(db, pe) || gn_off(stats, 8) || gn_off(ws, 8))
         return LBT_ERR_ALIGNMENT;
     if (d.N > 0 && (dy == nullptr || x == nullptr || stats == nullptr)) return LBT_ERR_INVALID_ARG;
     if (ws == nullptr || ws_bytes < lbt_groupnorm_workspace_bytes(desc)) return LBT_ERR_WORKSPACE;
@@ -573,10 +1096,11 @@ extern "C" lbt_status lbt_groupnorm_backward(const lbt_groupnorm_desc* desc, con
     g.x = x; g.w = w; g.b = b; g.dy = dy; g.dx = dx; g.stats = const_cast<float*>(stats); g.partial = static_cast<float*>(ws);
     g.ld_x = d.ld_x; g.ld_dy = d.ld_dy; g.ld_dx = d.ld_dx;
     g.P = (int)d.P; g.C = (int)d.C; g.G = (int)d.G; g.act = d.act; g.param_type = d.param_type; g.eps = d.eps;
-    if (d.N > 0) {
-        const lbt_status s = gn_run(g, d.N, d.type, gn_wide(d, {{x, d.ld_x}, {dy, d.ld_dy}, {dx, d.ld_dx}}), false, stream);
-        if (s != LBT_OK) return s;
+    g.dw = dw; g.db = db; g.N = (int)d.N;
+    if (d.N == 0) {   // the sums of nothing
+        if (dw != nullptr) LBT_CUDA_TRY(cudaMemsetAsync(dw, 0, pe * d.C, stream));
+        if (db != nullptr) LBT_CUDA_TRY(cudaMemsetAsync(db, 0, pe * d.C, stream));
+        return LBT_OK;
     }
-    if (dw == nullptr && db == nullptr) return LBT_OK;
-    return gn_chained(groupnorm_finish_kernel, dim3((g.C + 31) / 32), 0, stream, static_cast<const float2*>(ws), (int)(d.N * g.chunks), g.C, dw, db, (int)d.param_type);
+    return gn_run(g, d.N, d.type, gn_wide(d, {{x, d.ld_x}, {dy, d.ld_dy}, {dx, d.ld_dx}}), false, stream);
 }
