@@ -6,7 +6,7 @@
 // share a stage's tokens and columns.  16-bit z enters the matrix instructions as it is, pairs of its rows joined; f is split into three
 // bf16 or two fp16 numbers (24 or 22 bits: the gradients are fp32).  fp32 z and f are split into two tf32 numbers each.  fp16 holds no
 // more than 65504: there f enters times a power of two that brings the largest value of the CTA's tokens to [512, 1024).
-// (The tensor core's own sums are cut off, not rounded: those of a stage are added up in fp32.)
+// (The tensor core's own sums are cut off, not rounded: those of four stages at most are added up in fp32.)
 #include <algorithm>
 
 #include "lbt_adapters.cuh"
@@ -106,6 +106,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
     const float* f = g.f[which] + rank0;
     const T* z = static_cast<const T*>(g.z[which]) + col;
     const int64_t ld = g.ld[which];
+    const bool even_ranks = g.rank % 4 == 0 && (reinterpret_cast<uintptr_t>(f) & 15) == 0;
 
     // ids: the tokens of the pieces under way; this CTA takes every `ctas`-th piece.
     __shared__ int ids[kStages + 1][kAgTokens], have[kStages + 1];
@@ -141,9 +142,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
                 const T* z0 = z - col;
                 const int n = min(kAgCols, cols - col);
                 for (int m = warp; m < kAgTokens; m += kAdWarps) {
-                    const T* p = z + (int64_t)max(tokens[m], 0) * ld;
-                    copy_word(to + m * kAgStride, p, lane, m < count ? n : 0, z0);
-                    copy_word(to + m * kAgStride, p, lane + 32, m < count ? n : 0, z0);
+                    copy_words<T, 2>(to + m * kAgStride, 0, z + (int64_t)max(tokens[m], 0) * ld, 0, 1, m < count ? n : 0, z0);
                 }
                 if constexpr (!kF32) {   // the 65th word of rows that begin odd
                     if (threadIdx.x < kAgTokens) {
@@ -156,16 +155,25 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
                 for (int q = 0; q < kAgTokens / 16; ++q) {
                     const int m = (threadIdx.x >> 4) + 16 * q, c = kAgCols / 16 * (threadIdx.x & 15);
                     const uint32_t bytes = m < count && col + c < cols ? 16 : 0;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + m * kAgStride + 16 * (threadIdx.x & 15)),
-                                 "l"(bytes ? z + (int64_t)tokens[m] * ld + c : z), "r"(bytes) : "memory");
+                    copy16(to + m * kAgStride + 16 * (threadIdx.x & 15), bytes ? z + (int64_t)tokens[m] * ld + c : z, bytes);
                 }
             }
+            if (even_ranks) {   // f's rows by 16 bytes
+                constexpr int kLine = kR / 4;
 #pragma unroll
-            for (int q = 0; q < kAgTokens * kR / kAdThreads; ++q) {
-                const int i = threadIdx.x + kAdThreads * q, m = i / kR, k = i % kR;
-                const uint32_t bytes = m < count && k < ranks ? 4 : 0;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + kAgTokens * kAgStride + 4 * (m * kRow + k)), "l"(bytes ? f + (int64_t)tokens[m] * g.rank + k : f),
-                             "r"(bytes) : "memory");
+                for (int q = 0; q < (kAgTokens * kLine + kAdThreads - 1) / kAdThreads; ++q) {
+                    const int i = threadIdx.x + kAdThreads * q, m = i / kLine, k = 4 * (i % kLine);
+                    const uint32_t bytes = m < count && k < ranks ? 16 : 0;
+                    copy16(to + kAgTokens * kAgStride + 4 * (m * kRow + k), bytes ? f + (int64_t)tokens[m] * g.rank + k : f, bytes);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < kAgTokens * kR / kAdThreads; ++q) {
+                    const int i = threadIdx.x + kAdThreads * q, m = i / kR, k = i % kR;
+                    const uint32_t bytes = m < count && k < ranks ? 4 : 0;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + kAgTokens * kAgStride + 4 * (m * kRow + k)),
+                                 "l"(bytes ? f + (int64_t)tokens[m] * g.rank + k : f), "r"(bytes) : "memory");
+                }
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -183,6 +191,8 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
         for (int j = 0; j < kNt; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[n][j][i] = 0.0f;
+    float sum[kNt][4];     // of up to four pieces (one, with several blocks of ranks)
+    int pieces = 0;
     int at = 0, now = 0;   // the piece's stage, and its place among the lists of tokens
     for (;;) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
@@ -208,11 +218,11 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
             }
 #pragma unroll
         for (int n = 0; n < kR16; ++n) {
-            float sum[kNt][4];
+            if (kR16 > 1 || pieces == 0)
 #pragma unroll
-            for (int j = 0; j < kNt; ++j)
+                for (int j = 0; j < kNt; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[j][i] = 0.0f;
+                    for (int i = 0; i < 4; ++i) sum[j][i] = 0.0f;
 #pragma unroll
             for (int h = 0; h < kEach; ++h) {
                 uint32_t hi[4], lo[4], rest[4];
@@ -230,12 +240,19 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
                     mma_ranks<T, kNt, !kHalf>(sum, hi, lo, r[h], rest);
                 }
             }
+            if (kR16 > 1 || pieces == 3)
 #pragma unroll
-            for (int j = 0; j < kNt; ++j)
+                for (int j = 0; j < kNt; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[n][j][i] += sum[j][i];
+                    for (int i = 0; i < 4; ++i) acc[n][j][i] += sum[j][i];
         }
+        pieces = (pieces + 1) & 3;
     }
+    if (kR16 == 1 && pieces != 0)
+#pragma unroll
+        for (int j = 0; j < kNt; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[0][j][i] += sum[j][i];
     // The warps' sums over their tokens meet in the ring's place, one after the other, then the CTAs'.
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     float* mine = reinterpret_cast<float*>(ring);   // [kR][kAgCols]

@@ -60,10 +60,8 @@ __global__ void __launch_bounds__(kAdThreads, kN <= 2 ? 4 : kN <= 8 ? 2 : 1) ada
         const uint32_t to = smem_u32(s);
         if constexpr (kWords) {   // a row at a time
             const int n = min(kStep, width - c0);
-#pragma unroll 4
-            for (int r = 0; r < rows; ++r) copy_word(to + r * kStride, left + r * ld + c0, lane, n, left0);
-#pragma unroll 4
-            for (int r = 0; r < g.rank; ++r) copy_word(to + (kAdTokens + r) * kStride, right + (int64_t)r * width + c0, lane, n, right0);
+            copy_words<T, 1>(to, kStride, left + c0, ld, rows, n, left0);
+            copy_words<T, 1>(to + kAdTokens * kStride, kStride, right + c0, width, g.rank, n, right0);
             if constexpr (!kF32) {   // the 33rd word of rows that begin odd
                 if (lane < rows && begins_odd(left + lane * ld + c0)) copy_word(to + lane * kStride, left + lane * ld + c0, 32, n, left0);
                 for (int r = lane; r < g.rank; r += 32)
@@ -75,8 +73,7 @@ __global__ void __launch_bounds__(kAdThreads, kN <= 2 ? 4 : kN <= 8 ? 2 : 1) ada
             for (int q = 0; q < (kAdTokens + kR) / 4; ++q) {
                 const int r = (lane >> 3) + 4 * q, k = r - kAdTokens;
                 const T* from = q < kAdTokens / 4 ? left + r * ld + c : right + (int64_t)k * width + c;
-                if (q < kAdTokens / 4 ? r < rows : k < g.rank)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + r * kStride + 16 * (lane & 7)), "l"(c < width ? from : left0), "r"(c < width ? 16 : 0) : "memory");
+                if (q < kAdTokens / 4 ? r < rows : k < g.rank) copy16(to + r * kStride + 16 * (lane & 7), c < width ? from : left0, c < width ? 16 : 0);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -226,49 +223,60 @@ __global__ void __launch_bounds__(kTileThreads<T, kN>, kN <= 4 ? 2 : 1) adapter_
     const T* b = static_cast<const T*>(g.b) + (int64_t)adapter * g.rank * g.O;
     const int n2 = g.out != nullptr ? group_hi - group_lo : 0, all = n1 + n2;
 
-    // Step i's columns.  Columns that do not exist are zeros; rows that do not are left as they are (their h is not used, or set to 0).
-    auto fetch = [&](int i) {
-        if (i < all) {
-            const bool second = i >= n1;
-            const int c0 = kStep * (second ? group_lo + i - n1 : step_lo + i), width = second ? g.O : g.I;
-            const T* left = second ? base : x;
-            const T* right = second ? b : a;
-            const int64_t ld = second ? g.ld_base : g.ld_x;
-            const uint32_t slot = smem_u32(ring) + (i % kStages) * kStage;
+    // The next step's columns.  Columns that do not exist are zeros; rows that do not are left as they are (their h is not used, or set to 0).
+    constexpr int kEach = kWords ? 1 : 16 / (int)sizeof(T), kLanes = kThreads / 8;   // aligned rows: eight threads a row, kLanes rows at a time
+    constexpr int kLeft = kTileTokens / kLanes, kRight = (kR + kLanes - 1) / kLanes;
+    const int own = kWords ? threadIdx.x >> 5 : threadIdx.x >> 3;                    // this thread's first row
+    int next = 0, column = kStep * step_lo + (kWords ? 0 : kEach * (threadIdx.x & 7)), width = g.I;
+    uint32_t slot = smem_u32(ring) + own * kStride + (kWords ? 0 : 16 * (threadIdx.x & 7));
+    const T* left = x + own * g.ld_x + column;
+    const T* right = a + (int64_t)own * g.I + column;
+    int64_t left_step = (kWords ? kThreads / 32 : kLanes) * g.ld_x;
+    const int mine_left = max(0, (rows - own + (kWords ? kThreads / 32 : kLanes) - 1) / (kWords ? kThreads / 32 : kLanes));
+    const int mine_right = max(0, (g.rank - own + (kWords ? kThreads / 32 : kLanes) - 1) / (kWords ? kThreads / 32 : kLanes));
+    auto fetch = [&]() {
+        if (next < all) {
+            if (next == n1) {   // on to the second product
+                column = kStep * group_lo + (kWords ? 0 : kEach * (threadIdx.x & 7));
+                width = g.O;
+                left = base + own * g.ld_base + column;
+                right = b + (int64_t)own * g.O + column;
+                left_step = (kWords ? kThreads / 32 : kLanes) * g.ld_base;
+            }
             if constexpr (kWords) {   // a warp a row
-                const int n = min(kStep, width - c0);
+                const bool second = next >= n1;
+                const int n = min(kStep, width - column);
                 const T* left0 = static_cast<const T*>(second ? g.base : g.x);
                 const T* right0 = static_cast<const T*>(second ? g.b : g.a);
-#pragma unroll 4
-                for (int r = threadIdx.x >> 5; r < rows; r += kThreads / 32) copy_word(slot + r * kStride, left + r * ld + c0, lane, n, left0);
-#pragma unroll 4
-                for (int r = threadIdx.x >> 5; r < g.rank; r += kThreads / 32) copy_word(slot + (kTileTokens + r) * kStride, right + (int64_t)r * width + c0, lane, n, right0);
+                copy_words<T, 1>(slot, kThreads / 32 * kStride, left, left_step, mine_left, n, left0);
+                copy_words<T, 1>(slot + kTileTokens * kStride, kThreads / 32 * kStride, right, (int64_t)(kThreads / 32) * width, mine_right, n, right0);
                 if constexpr (!kF32) {   // the 33rd word of rows that begin odd
+                    const T* l = second ? base : x;
+                    const T* r0 = second ? b : a;
+                    const int64_t ld = second ? g.ld_base : g.ld_x;
+                    const uint32_t to = slot - own * kStride;
                     for (int r = threadIdx.x; r < kTileTokens + kR; r += kThreads) {
                         const bool is_left = r < kTileTokens;
-                        const T* p = is_left ? left + r * ld + c0 : right + (int64_t)(r - kTileTokens) * width + c0;
-                        if ((is_left ? r < rows : r - kTileTokens < g.rank) && begins_odd(p)) copy_word(slot + r * kStride, p, 32, n, is_left ? left0 : right0);
+                        const T* p = is_left ? l + r * ld + column : r0 + (int64_t)(r - kTileTokens) * width + column;
+                        if ((is_left ? r < rows : r - kTileTokens < g.rank) && begins_odd(p)) copy_word(to + r * kStride, p, 32, n, is_left ? left0 : right0);
                     }
                 }
-            } else {                  // eight threads a row
-                constexpr int kEach = 16 / (int)sizeof(T);
-                const int c = c0 + kEach * (threadIdx.x & 7);
-                const uint32_t to = slot + (threadIdx.x >> 3) * kStride + 16 * (threadIdx.x & 7);
+            } else {
+                const uint32_t bytes = column < width ? 16 : 0;
+                const T* from = left;
 #pragma unroll
-                for (int q = 0; q < kTileTokens / (kThreads / 8); ++q) {
-                    const int m = (threadIdx.x >> 3) + kThreads / 8 * q;
-                    if (m < rows)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + kThreads / 8 * q * kStride), "l"(c < width ? left + m * ld + c : left),
-                                     "r"(c < width ? 16 : 0) : "memory");
-                }
+                for (int q = 0; q < kLeft; ++q, from += left_step)
+                    if (q < mine_left) copy16(slot + kLanes * q * kStride, bytes ? from : left, bytes);
+                from = right;
 #pragma unroll
-                for (int q = 0; q < (kR + kThreads / 8 - 1) / (kThreads / 8); ++q) {
-                    const int k = (threadIdx.x >> 3) + kThreads / 8 * q;
-                    if (k < g.rank)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (kTileTokens + kThreads / 8 * q) * kStride),
-                                     "l"(c < width ? right + (int64_t)k * width + c : right), "r"(c < width ? 16 : 0) : "memory");
-                }
+                for (int q = 0; q < kRight; ++q, from += (int64_t)kLanes * width)
+                    if (q < mine_right) copy16(slot + (kTileTokens + kLanes * q) * kStride, bytes ? from : right, bytes);
             }
+            ++next;
+            column += kStep;
+            left += kStep;
+            right += kStep;
+            slot = next % kStages == 0 ? slot - (kStages - 1) * kStage : slot + kStage;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -276,11 +284,11 @@ __global__ void __launch_bounds__(kTileThreads<T, kN>, kN <= 4 ? 2 : 1) adapter_
     auto stage = [&](int i) -> uint8_t* {
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
         __syncthreads();   // (all warps have left the stage that is filled next)
-        fetch(i + kStages - 1);
+        fetch();
         return ring + (i % kStages) * kStage;
     };
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) fetch(i);
+    for (int i = 0; i < kStages - 1; ++i) fetch();
 
     const int m0 = 16 * warp + gq, m1 = m0 + 8;
     float acc[kOwn][4];

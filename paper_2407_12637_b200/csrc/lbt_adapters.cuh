@@ -260,6 +260,39 @@ template <typename T> __device__ __forceinline__ void copy_word(uint32_t to, con
     }
 }
 
+// Rows p, p + step, .. (count of them, n elements each) to `to`, to + to_step, .., by a warp, a word a lane and block of 32 words.
+template <typename T, int kBlocks>
+__device__ __forceinline__ void copy_words(uint32_t to, uint32_t to_step, const T* p, int64_t step, int count, int n, const T* begin) {
+    const int lane = threadIdx.x & 31;
+    if (begins_odd(begin)) {   // (the tensor's first row may need care)
+        for (int r = 0; r < count; ++r, p += step, to += to_step)
+#pragma unroll
+            for (int k = 0; k < kBlocks; ++k) copy_word(to, p, lane + 32 * k, n, begin);
+        return;
+    }
+    uint32_t even[kBlocks], odd[kBlocks];   // bytes that exist of this lane's words
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) {
+        const int w = lane + 32 * k;
+        even[k] = sizeof(T) == 4 ? (w < n ? 4 : 0) : min(max(2 * (n - 2 * w), 0), 4);
+        odd[k] = min(max(2 * (n - 2 * w + 1), 0), 4);
+    }
+    to += 4 * lane;
+#pragma unroll 4
+    for (int r = 0; r < count; ++r, p += step, to += to_step) {
+        const uint8_t* from = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3) + 4 * lane;
+        const bool late = begins_odd(p);
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 128 * k), "l"(from + 128 * k), "r"(late ? odd[k] : even[k]) : "memory");
+    }
+}
+
+// 16 bytes of a row, `bytes` (16 or 0) of which exist.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+
 // kWords words of a row at p in shared memory, one element further on where the row began odd.
 template <int kWords> __device__ __forceinline__ void ld_shifted(const uint8_t* p, bool odd, uint32_t (&w)[kWords]) {
     ld_words(p, w);
@@ -275,7 +308,9 @@ template <typename T, bool kShift, int kWords> __device__ __forceinline__ void l
 // acc += the products of a lane's 32 bytes of two rows (v0, v1) and of a row of the other operand (w), with the other lanes' (the tensor
 // core's own sums are cut off, not rounded: they are added to acc in fp32).
 template <typename T> __device__ __forceinline__ void mma_step(float (&acc)[4], const uint32_t (&v0)[8], const uint32_t (&v1)[8], const uint32_t (&w)[8]) {
-    float sum[4] = {};
+    float sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = 0.0f;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         if constexpr (sizeof(T) == 4) {   // terms t and t + 4 of instruction p: the lane's elements 2 p and 2 p + 1
