@@ -96,7 +96,12 @@ template <> struct IsF32<float> { static constexpr bool value = true; };
 template <bool kSplitB>
 __device__ __forceinline__ void mma_split(float (&d)[4], const uint32_t (&hi)[4], const uint32_t (&lo)[4], float b0, float b1) {
     uint32_t h0 = __float_as_uint(b0), h1 = __float_as_uint(b1), l0 = 0, l1 = 0;
-    if (kSplitB) { split(b0, h0, l0); split(b1, h1, l1); }
+    if (kSplitB) {   // (the instruction cuts the second part to tf32 itself; an infinity ends as NaN)
+        asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(h0) : "f"(b0));
+        asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(h1) : "f"(b1));
+        l0 = __float_as_uint(b0 - __uint_as_float(h0));
+        l1 = __float_as_uint(b1 - __uint_as_float(h1));
+    }
     mma_tf32(d, lo[0], lo[1], lo[2], lo[3], h0, h1);
     if (kSplitB) mma_tf32(d, hi[0], hi[1], hi[2], hi[3], l0, l1);
     mma_tf32(d, hi[0], hi[1], hi[2], hi[3], h0, h1);

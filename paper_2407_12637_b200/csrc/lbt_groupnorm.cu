@@ -5,7 +5,7 @@
 //   dx = rstd (w e - mean_g(w e) - k mean_g(w e k))
 //
 // Bound by memory: x and y, then x, dy and dx.  Sums are kept by channel, whatever groups the channels fall into, so a thread owns
-// eight (or, where rows are not aligned, one) neighbouring channels and walks over pixels.  Two forms:
+// eight neighbouring channels (two, or one, where rows are not aligned) and walks over pixels.  Two forms:
 //   an image that fits the shared memory of a cluster (8 or 16 CTAs) is read once: each CTA keeps its share of the pixels on chip, the
 //   CTAs' sums of each channel meet through the cluster, and the output is formed from what is kept;
 //   a larger one is read twice: the first kernel leaves the sums of its share of an image's pixels for each channel, the second adds
@@ -53,6 +53,32 @@ template <typename T> struct Pack<T, 8> {
     __device__ __forceinline__ void load(const T* p) { ld_vec(p, v.w); }
     __device__ __forceinline__ void get(float (&f)[8]) const { unpack(v, f); }
     static __device__ __forceinline__ void store(T* p, const float (&f)[8]) { store8(p, f); }
+};
+template <typename T> struct Pack<T, 2> {
+    uint32_t w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    }
+    __device__ __forceinline__ void get(float (&f)[2]) const { get(w, f); }
+    static __device__ __forceinline__ void get(const uint32_t* w, float (&f)[2]) {
+        if constexpr (sizeof(T) == 4) {
+            f[0] = __uint_as_float(w[0]);
+            f[1] = __uint_as_float(w[1]);
+        } else {
+            const T* v = reinterpret_cast<const T*>(w);
+            f[0] = to_f32(v[0]);
+            f[1] = to_f32(v[1]);
+        }
+    }
+    static __device__ __forceinline__ void store(T* p, const float (&f)[2]) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
+        } else {
+            T v[2] = {from_f32<T>(f[0]), from_f32<T>(f[1])};
+            *reinterpret_cast<uint32_t*>(p) = *reinterpret_cast<const uint32_t*>(v);
+        }
+    }
 };
 template <typename T> struct Pack<T, 1> {
     T v;
@@ -591,6 +617,8 @@ template <typename T, int kVec, int kThreads> struct Kept {
     __device__ __forceinline__ T* at(int k) const { return reinterpret_cast<T*>(base) + (k * kThreads + (int)threadIdx.x) * kVec; }
     __device__ __forceinline__ void fetch(int k, const T* src) const {
         if constexpr (kVec == 1) *at(k) = *src;
+        if constexpr (kVec == 2)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(sm100::smem_u32(at(k))), "l"(src), "n"(2 * sizeof(T)) : "memory");
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) * kVec / 16; ++i)
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sm100::smem_u32(at(k)) + 16 * i), "l"(reinterpret_cast<const uint8_t*>(src) + 16 * i) : "memory");
@@ -599,6 +627,10 @@ template <typename T, int kVec, int kThreads> struct Kept {
         Vals<kVec> v;
         if constexpr (kVec == 1) {
             v.f[0] = to_f32(*at(k));
+        } else if constexpr (kVec == 2) {
+            Pack<T, 2> w;
+            w.load(at(k));
+            w.get(v.f);
         } else {
             Vec8<T> w;
 #pragma unroll
@@ -803,7 +835,7 @@ __device__ __forceinline__ Vals<kVec> slopes(Vals<kVec> e, const Vals<kVec>& k, 
 
 // Its gradients: x and dy are kept; partial: [N, C] sums of e and e k for the parameters' gradients.
 template <typename T, int kVec, int kAct, int kThreads>
-__global__ void __launch_bounds__(kThreads, 768 / kThreads) groupnorm_image_grad_kernel(const __grid_constant__ GroupNormArgs g) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 2) groupnorm_image_grad_kernel(const __grid_constant__ GroupNormArgs g) {
     extern __shared__ __align__(16) uint8_t image[];
     sm100::griddep_launch_dependents();
     const Cover<kVec, kThreads> cover(g.C);
@@ -906,7 +938,9 @@ __global__ void __launch_bounds__(kGnThreads) groupnorm_params_kernel(const __gr
 // Shares of an image's pixels: four blocks to an SM, all resident at once, and four pixels a thread at least.
 static int gn_chunks(int64_t N, int64_t P, int64_t C, int vec) {
     const int64_t vecs = (C + vec - 1) / vec, tiles = (vecs + kGnThreads - 1) / kGnThreads, lanes = kGnThreads / std::min<int64_t>(vecs, kGnThreads);
-    const int64_t want = (int64_t)kNumSMs * 4 / (N * tiles), most = (P + lanes * kGnAhead - 1) / (lanes * kGnAhead);
+    // (each share's channels are added up again by every block of the image: few of them, unless shares are large)
+    const int64_t width = std::min<int64_t>(C, kGnThreads * vec), few = std::max<int64_t>(4096 / width, P * C >> 18);
+    const int64_t want = std::min<int64_t>((int64_t)kNumSMs * 4 / (N * tiles), few), most = (P + lanes * kGnAhead - 1) / (lanes * kGnAhead);
     return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, kGnMaxChunks}));
 }
 
@@ -927,6 +961,8 @@ static lbt_status gn_chained(void (*kernel)(Args...), dim3 grid, int threads, si
     return launch_status();
 }
 
+// small packs need many threads to cover a row, and few registers each
+template <int kVec> constexpr int kImageThreads = kVec == 8 ? 256 : 512;
 constexpr size_t kGnSmem = 110 * 1024;   // shared memory of a CTA that keeps pixels: two of them to an SM
 // CTAs of the cluster that keeps an image on chip (`tensors` of its size) with blocks of so many threads, 0 if it does not fit one;
 // where the kept packs begin and the bytes of shared memory.
@@ -963,18 +999,25 @@ static lbt_status gn_image_launch(void (*kernel)(GroupNormArgs), const GroupNorm
     return launch_status();
 }
 
+// (codes are written eight at a time: only there is the kernel that writes them)
+template <typename T, int kVec, int kAct> static void (*gn_image(bool codes))(GroupNormArgs) {
+    if constexpr (kVec == 8)
+        if (codes) return groupnorm_image_kernel<T, kVec, kAct, true, kImageThreads<kVec>>;
+    return groupnorm_image_kernel<T, kVec, kAct, false, kImageThreads<kVec>>;
+}
+
 template <typename T, int kVec, int kAct>
 static lbt_status gn_forward(const GroupNormArgs& args, dim3 grid, cudaStream_t stream) {
     GroupNormArgs g = args;
     size_t smem = 0;
-    if (const int ctas = gn_cluster(g, kVec, kGnThreads, sizeof(T), 1, &smem))
-        return gn_image_launch(g.q != nullptr ? groupnorm_image_kernel<T, kVec, kAct, true, kGnThreads> : groupnorm_image_kernel<T, kVec, kAct, false, kGnThreads>,
-                               g, ctas, kGnThreads, smem, stream);
+    if (const int ctas = gn_cluster(g, kVec, kImageThreads<kVec>, sizeof(T), 1, &smem))
+        return gn_image_launch(gn_image<T, kVec, kAct>(g.q != nullptr), g, ctas, kImageThreads<kVec>, smem, stream);
     g = args;
     groupnorm_stats_kernel<T, kVec><<<grid, kGnThreads, 0, stream>>>(g);
     if (launch_status() != LBT_OK) return LBT_ERR_CUDA;
     smem = sizeof(float2) * std::min(g.G, kGnThreads * kVec);
-    if (g.q != nullptr) return gn_chained(groupnorm_apply_kernel<T, kVec, kAct, true>, grid, kGnThreads, smem, stream, g);
+    if constexpr (kVec == 8)
+        if (g.q != nullptr) return gn_chained(groupnorm_apply_kernel<T, kVec, kAct, true>, grid, kGnThreads, smem, stream, g);
     return gn_chained(groupnorm_apply_kernel<T, kVec, kAct, false>, grid, kGnThreads, smem, stream, g);
 }
 
@@ -982,8 +1025,8 @@ template <typename T, int kVec, int kAct>
 static lbt_status gn_backward(const GroupNormArgs& args, dim3 grid, cudaStream_t stream) {
     GroupNormArgs g = args;
     size_t smem = 0;
-    if (const int ctas = gn_cluster(g, kVec, kGnThreads, sizeof(T), 2, &smem)) {
-        const lbt_status s = gn_image_launch(groupnorm_image_grad_kernel<T, kVec, kAct, kGnThreads>, g, ctas, kGnThreads, smem, stream);
+    if (const int ctas = gn_cluster(g, kVec, kImageThreads<kVec>, sizeof(T), 2, &smem)) {
+        const lbt_status s = gn_image_launch(groupnorm_image_grad_kernel<T, kVec, kAct, kImageThreads<kVec>>, g, ctas, kImageThreads<kVec>, smem, stream);
         if (s != LBT_OK || (g.dw == nullptr && g.db == nullptr)) return s;
         return gn_chained(groupnorm_params_kernel, dim3((g.C + 31) / 32), kGnThreads, 0, stream, g);
     }
@@ -1007,17 +1050,18 @@ static lbt_status gn_run_act(const GroupNormArgs& g, dim3 grid, bool forward, cu
 }
 
 template <typename T>
-static lbt_status gn_run_vec(GroupNormArgs& g, int64_t N, bool wide, bool forward, cudaStream_t stream) {
-    const int vec = wide ? 8 : 1, vecs = (g.C + vec - 1) / vec;
+static lbt_status gn_run_vec(GroupNormArgs& g, int64_t N, int vec, bool forward, cudaStream_t stream) {
+    const int vecs = (g.C + vec - 1) / vec;
     g.share = (g.P + gn_chunks(N, g.P, g.C, vec) - 1) / gn_chunks(N, g.P, g.C, vec);
     g.chunks = (g.P + g.share - 1) / g.share;   // (no share is empty)
     const dim3 grid(g.chunks, (unsigned)N, (vecs + kGnThreads - 1) / kGnThreads);
-    return wide ? gn_run_act<T, 8>(g, grid, forward, stream) : gn_run_act<T, 1>(g, grid, forward, stream);
+    if (vec == 8) return gn_run_act<T, 8>(g, grid, forward, stream);
+    return vec == 2 ? gn_run_act<T, 2>(g, grid, forward, stream) : gn_run_act<T, 1>(g, grid, forward, stream);
 }
 
-static lbt_status gn_run(GroupNormArgs& g, int64_t N, int type, bool wide, bool forward, cudaStream_t stream) {
-    if (type == LBT_F32) return gn_run_vec<float>(g, N, wide, forward, stream);
-    return type == LBT_BF16 ? gn_run_vec<__nv_bfloat16>(g, N, wide, forward, stream) : gn_run_vec<__half>(g, N, wide, forward, stream);
+static lbt_status gn_run(GroupNormArgs& g, int64_t N, int type, int vec, bool forward, cudaStream_t stream) {
+    if (type == LBT_F32) return gn_run_vec<float>(g, N, vec, forward, stream);
+    return type == LBT_BF16 ? gn_run_vec<__nv_bfloat16>(g, N, vec, forward, stream) : gn_run_vec<__half>(g, N, vec, forward, stream);
 }
 
 static bool gn_off(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
@@ -1036,12 +1080,14 @@ static lbt_status gn_check(const lbt_groupnorm_desc* desc, lbt_groupnorm_desc* d
     return LBT_OK;
 }
 
-// Whether rows of all tensors begin where packs of eight may (fp32: 32 bytes, 16-bit types: 16).
-static bool gn_wide(const lbt_groupnorm_desc& d, std::initializer_list<std::pair<const void*, int64_t>> rows) {
-    if (d.C % 8 != 0) return false;
-    for (const auto& r : rows)
-        if (r.first != nullptr && (gn_off(r.first, 8 * type_size(d.type)) || r.second % 8 != 0)) return false;
-    return true;
+// Channels of a pack: eight or two where every pixel of all tensors begins on that many elements, else one.
+static int gn_vec(const lbt_groupnorm_desc& d, std::initializer_list<std::pair<const void*, int64_t>> rows) {
+    for (int vec : {8, 2}) {
+        bool ok = d.C % vec == 0;
+        for (const auto& r : rows) ok = ok && (r.first == nullptr || (!gn_off(r.first, vec * type_size(d.type)) && r.second % vec == 0));
+        if (ok) return vec;
+    }
+    return 1;
 }
 
 }  // namespace lbt
@@ -1051,8 +1097,8 @@ using namespace lbt;
 extern "C" size_t lbt_groupnorm_workspace_bytes(const lbt_groupnorm_desc* desc) {
     lbt_groupnorm_desc d;
     if (gn_check(desc, &d) != LBT_OK) return 0;
-    // two sums for each image, share and channel (either width of access), 256 bytes at least
-    const int64_t chunks = std::max(gn_chunks(std::max<int64_t>(d.N, 1), d.P, d.C, 1), gn_chunks(std::max<int64_t>(d.N, 1), d.P, d.C, 8));
+    // two sums for each image, share and channel (any width of access), 256 bytes at least
+    const int64_t n = std::max<int64_t>(d.N, 1), chunks = std::max({gn_chunks(n, d.P, d.C, 1), gn_chunks(n, d.P, d.C, 2), gn_chunks(n, d.P, d.C, 8)});
     return (size_t)std::max<int64_t>(256, d.N * chunks * d.C * (int64_t)sizeof(float2));
 }
 
@@ -1067,8 +1113,8 @@ extern "C" lbt_status lbt_groupnorm_forward(const lbt_groupnorm_desc* desc, cons
     if (gn_off(x, e) || gn_off(y, e) || gn_off(w, pe) || gn_off(b, pe) || gn_off(stats, 8) || gn_off(d_clip, 4) || gn_off(d_scale_out, 4) ||
         gn_off(q, 16) || gn_off(ws, 8))
         return LBT_ERR_ALIGNMENT;
-    const bool wide = gn_wide(d, {{x, d.ld_x}, {y, d.ld_y}});
-    if (q != nullptr && !wide) return d.C % 8 != 0 ? LBT_ERR_UNSUPPORTED : LBT_ERR_ALIGNMENT;
+    const int vec = gn_vec(d, {{x, d.ld_x}, {y, d.ld_y}});
+    if (q != nullptr && vec != 8) return d.C % 8 != 0 ? LBT_ERR_UNSUPPORTED : LBT_ERR_ALIGNMENT;
     if (d.N == 0) return LBT_OK;
     if (x == nullptr) return LBT_ERR_INVALID_ARG;
     if (ws == nullptr || ws_bytes < lbt_groupnorm_workspace_bytes(desc)) return LBT_ERR_WORKSPACE;
@@ -1077,7 +1123,7 @@ extern "C" lbt_status lbt_groupnorm_forward(const lbt_groupnorm_desc* desc, cons
     g.partial = static_cast<float*>(ws);
     g.ld_x = d.ld_x; g.ld_y = d.ld_y; g.N = (int)d.N;
     g.P = (int)d.P; g.C = (int)d.C; g.G = (int)d.G; g.act = d.act; g.bits = bits; g.param_type = d.param_type; g.eps = d.eps;
-    return gn_run(g, d.N, d.type, wide, true, as_stream(cuda_stream));
+    return gn_run(g, d.N, d.type, vec, true, as_stream(cuda_stream));
 }
 
 extern "C" lbt_status lbt_groupnorm_backward(const lbt_groupnorm_desc* desc, const void* dy, const void* x, const void* w, const void* b, const float* stats,
@@ -1102,5 +1148,5 @@ extern "C" lbt_status lbt_groupnorm_backward(const lbt_groupnorm_desc* desc, con
         if (db != nullptr) LBT_CUDA_TRY(cudaMemsetAsync(db, 0, pe * d.C, stream));
         return LBT_OK;
     }
-    return gn_run(g, d.N, d.type, gn_wide(d, {{x, d.ld_x}, {dy, d.ld_dy}, {dx, d.ld_dx}}), false, stream);
+    return gn_run(g, d.N, d.type, gn_vec(d, {{x, d.ld_x}, {dy, d.ld_dy}, {dx, d.ld_dx}}), false, stream);
 }
