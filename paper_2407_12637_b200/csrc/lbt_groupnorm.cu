@@ -24,7 +24,7 @@ namespace lbt {
 constexpr int kGnThreads = 256;
 constexpr int kGnAhead = 4;             // pixels whose loads a thread has under way together
 constexpr int kGnPairs = 2;             // the same for two tensors at once
-constexpr int kGnMaxChunks = 148;       // shares of an image's pixels
+constexpr int kGnJoined = 8;            // blocks of a cluster that add up their sums
 
 struct GroupNormArgs {
     const void* x;
@@ -39,9 +39,12 @@ struct GroupNormArgs {
     void* dx;
     void* dw;
     void* db;
-    float* partial;         // [N, chunks, C, 2]
+    float* partial;         // [N, parts, C, 2]
     int64_t ld_x, ld_y, ld_dy, ld_dx;
-    int N, P, C, G, chunks, share, act, bits, param_type;   // share: pixels of a chunk (the last one's may be fewer)
+    int N, P, C, G, act, bits, param_type;
+    int chunks, share;      // blocks that share an image's pixels, pixels of each (the last ones' may be fewer, or none)
+    int joined;             // neighbouring blocks whose sums are added up before they are left in partial
+    int parts, part_share;  // sums left of an image, pixels of each
     float eps;
     int kept;   // where the packs that are kept begin in shared memory
 };
@@ -149,6 +152,31 @@ __device__ __forceinline__ void join_lanes(const float2* part, float2* joined, i
     }
 }
 
+__device__ __forceinline__ float2 ld_cluster2(const float2* p, int cta) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(sm100::map_to_cta(sm100::smem_u32(p), cta)) : "memory");
+    return v;
+}
+
+// Leaves this block's sums of each channel (in shared memory) in partial, or, with clusters, those of the cluster's blocks joined one after
+// the other: join(all, pixels so far, a block's, its place among the image's).
+template <typename Join> __device__ __forceinline__ void join_blocks(const GroupNormArgs& g, int n, int c0, int width, const float2* sums, Join join) {
+    float2* out = reinterpret_cast<float2*>(g.partial) + ((int64_t)n * g.parts + blockIdx.x / g.joined) * g.C + c0;
+    const int rank = blockIdx.x % g.joined;
+    if (g.joined > 1) sm100::cluster_sync_all();
+    else __syncthreads();
+    for (int i = rank * kGnThreads + threadIdx.x; i < width; i += g.joined * kGnThreads) {
+        float2 all = make_float2(0.0f, 0.0f);
+        float pixels = 0.0f;
+        if (g.joined == 1) all = join(all, pixels, sums[i], blockIdx.x);
+        else
+            for (int c = 0; c < g.joined; ++c) all = join(all, pixels, ld_cluster2(sums + i, c), blockIdx.x - rank + c);
+        out[i] = all;
+    }
+    __syncwarp();
+    if (g.joined > 1) sm100::cluster_sync_all();   // nobody leaves before its sums have been fetched
+}
+
 // A share's mean and centred sum of squares of each channel.  A thread sums differences from the first value that it reads; the block's
 // mean is formed from the threads' means, then every thread's sum of squares is moved to that mean.
 template <typename T, int kVec>
@@ -198,7 +226,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) groupnorm_stats_kernel(const __
     __syncthreads();
     join_lanes(part, joined, width, cover.lanes, sums);
     __syncthreads();
-    const float size = 1.0f / (float)(hi - lo);
+    const float size = hi > lo ? 1.0f / (float)(hi - lo) : 0.0f;
     if (cover.active) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
@@ -206,7 +234,6 @@ __global__ void __launch_bounds__(kGnThreads, 4) groupnorm_stats_kernel(const __
             part[cover.lane * width + cover.vec * kVec + i] = make_float2(0.0f, fmaf((float)count * d, d, s2[i]));
         }
     }
-    float2* out = reinterpret_cast<float2*>(g.partial) + ((int64_t)n * g.chunks + chunk) * g.C + cover.vec0 * kVec;
     __syncthreads();
     float2 mean[kVec];   // (of the channels threadIdx.x, + 256, ..: read before `sums` is written again)
 #pragma unroll
@@ -216,7 +243,13 @@ __global__ void __launch_bounds__(kGnThreads, 4) groupnorm_stats_kernel(const __
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
-        if (threadIdx.x + i * kGnThreads < width) out[threadIdx.x + i * kGnThreads] = make_float2(mean[i].x * size, sums[threadIdx.x + i * kGnThreads].y);
+        if (threadIdx.x + i * kGnThreads < width) sums[threadIdx.x + i * kGnThreads].x = mean[i].x * size;
+    join_blocks(g, n, cover.vec0 * kVec, width, sums, [&](float2 all, float& pixels, float2 v, int c) {
+        const float own = (float)max(0, min(g.share, g.P - c * g.share)), d = v.x - all.x;
+        pixels += own;
+        const float share = pixels > 0.0f ? own / pixels : 0.0f;
+        return make_float2(fmaf(d, share, all.x), all.y + fmaf(d * d, (pixels - own) * share, v.y));
+    });
 }
 
 // A group's items (share, channel) as `lanes` neighbouring threads take them in turn, eight of them under way at a time.  f(value, pixels
@@ -226,21 +259,21 @@ template <typename F>
 __device__ __forceinline__ void each_item(const GroupNormArgs& g, const float2* part, int cg, int lane, int lanes, F f) {
     const int whole = lanes / cg, more = lanes - whole * cg;
     int share = lane / cg, channel = lane - share * cg;
-    while (share < g.chunks) {
+    while (share < g.parts) {
         float2 v[kGnItems];
         int s[kGnItems], c[kGnItems];
 #pragma unroll
         for (int u = 0; u < kGnItems; ++u) {
             s[u] = share;
             c[u] = channel;
-            if (share < g.chunks) v[u] = __ldcg(part + (int64_t)share * g.C + channel);
+            if (share < g.parts) v[u] = __ldcg(part + (int64_t)share * g.C + channel);
             channel += more;
             share += whole;
             if (channel >= cg) { channel -= cg; ++share; }
         }
 #pragma unroll
         for (int u = 0; u < kGnItems; ++u)
-            if (s[u] < g.chunks) f(v[u], (float)min(g.share, g.P - s[u] * g.share), c[u]);
+            if (s[u] < g.parts) f(v[u], (float)min(g.part_share, g.P - s[u] * g.part_share), c[u]);
     }
 }
 
@@ -319,7 +352,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) groupnorm_apply_kernel(const __
     sm100::griddep_wait();
     for (int i0 = 0; i0 < groups.count; i0 += groups.stride()) {   // (whole warps stay together)
         const int i = min(i0 + groups.own, groups.count - 1);
-        const float2* part = reinterpret_cast<const float2*>(g.partial) + (int64_t)n * g.chunks * g.C + (groups.first + i) * cg;
+        const float2* part = reinterpret_cast<const float2*>(g.partial) + (int64_t)n * g.parts * g.C + (groups.first + i) * cg;
         const float total = 1.0f / ((float)g.P * (float)cg);
         float mean = 0.0f, m2 = 0.0f;
         each_item(g, part, cg, groups.lane, groups.lanes, [&](float2 v, float pixels, int) { mean = fmaf(pixels, v.x, mean); });
@@ -446,7 +479,8 @@ __global__ void __launch_bounds__(kGnThreads, 3) groupnorm_sums_kernel(const __g
         for (int i = 0; i < kVec; ++i) part[cover.lane * width + cover.vec * kVec + i] = make_float2(s1[i], s2[i] * stats[again.next()].y);
     }
     __syncthreads();
-    join_lanes(part, joined, width, cover.lanes, reinterpret_cast<float2*>(g.partial) + ((int64_t)n * g.chunks + blockIdx.x) * g.C + cover.vec0 * kVec);
+    join_lanes(part, joined, width, cover.lanes, params);   // (in the parameters' place)
+    join_blocks(g, n, cover.vec0 * kVec, width, params, [](float2 all, float&, float2 v, int) { return make_float2(all.x + v.x, all.y + v.y); });
 }
 
 // dw and db of 32 channels: sums over images and shares, eight rows of them side by side.
@@ -493,7 +527,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) groupnorm_dx_kernel(const __gri
     if (blockIdx.y == 0) {
         __shared__ float2 part[kGnThreads / 32][32];
         sm100::griddep_wait();
-        for (int c = 32 * (blockIdx.x + blockIdx.z * gridDim.x); c < g.C; c += 32 * gridDim.x * gridDim.z) param_grads(g, g.N * g.chunks, c, part);
+        for (int c = 32 * (blockIdx.x + blockIdx.z * gridDim.x); c < g.C; c += 32 * gridDim.x * gridDim.z) param_grads(g, g.N * g.parts, c, part);
         return;
     }
     const Cover<kVec> cover(g.C);
@@ -503,7 +537,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) groupnorm_dx_kernel(const __gri
     sm100::griddep_wait();
     for (int i0 = 0; i0 < groups.count; i0 += groups.stride()) {
         const int i = min(i0 + groups.own, groups.count - 1);
-        const float2* part = reinterpret_cast<const float2*>(g.partial) + (int64_t)n * g.chunks * g.C + (groups.first + i) * cg;
+        const float2* part = reinterpret_cast<const float2*>(g.partial) + (int64_t)n * g.parts * g.C + (groups.first + i) * cg;
         float e = 0.0f, ek = 0.0f;
         each_item(g, part, cg, groups.lane, groups.lanes, [&](float2 v, float, int c) {
             const float w = gn_param(g.w, g.param_type, (groups.first + i) * cg + c, 1.0f);
@@ -695,11 +729,6 @@ __device__ __forceinline__ void lanes_sum(Vals<kVec> v, const Cover<kVec, kThrea
 }
 static int image_rows(int vecs, int threads) { return vecs <= 32 && 32 % vecs == 0 ? threads / 32 : threads / vecs; }
 
-__device__ __forceinline__ float2 ld_cluster2(const float2* p, int cta) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(sm100::map_to_cta(sm100::smem_u32(p), cta)) : "memory");
-    return v;
-}
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
@@ -935,13 +964,34 @@ __global__ void __launch_bounds__(kGnThreads) groupnorm_params_kernel(const __gr
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-// Shares of an image's pixels: four blocks to an SM, all resident at once, and four pixels a thread at least.
-static int gn_chunks(int64_t N, int64_t P, int64_t C, int vec) {
-    const int64_t vecs = (C + vec - 1) / vec, tiles = (vecs + kGnThreads - 1) / kGnThreads, lanes = kGnThreads / std::min<int64_t>(vecs, kGnThreads);
-    // (each share's channels are added up again by every block of the image: few of them, unless shares are large)
-    const int64_t width = std::min<int64_t>(C, kGnThreads * vec), few = std::max<int64_t>(4096 / width, P * C >> 18);
+// How an image's pixels are shared: four blocks to an SM, all resident at once, and four pixels a thread at least.  Every block of an image
+// adds up again what all of them have left: few sums, unless shares are large.
+static void gn_share(GroupNormArgs& g, int64_t N, int vec) {
+    const int64_t P = g.P, C = g.C, vecs = (C + vec - 1) / vec, tiles = (vecs + kGnThreads - 1) / kGnThreads, lanes = kGnThreads / std::min<int64_t>(vecs, kGnThreads);
+    const int64_t width = std::min<int64_t>(C, kGnThreads * vec), few = kGnJoined * std::max<int64_t>(2048 / width, P * C >> 20);
     const int64_t want = std::min<int64_t>((int64_t)kNumSMs * 4 / (N * tiles), few), most = (P + lanes * kGnAhead - 1) / (lanes * kGnAhead);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, kGnMaxChunks}));
+    const int64_t chunks = std::max<int64_t>(1, std::min(want, most));
+    g.share = (int)((P + chunks - 1) / chunks);
+    g.chunks = (int)((P + g.share - 1) / g.share);
+    g.joined = g.chunks >= 2 * kGnJoined ? kGnJoined : 1;
+    g.parts = (g.chunks + g.joined - 1) / g.joined;
+    g.chunks = g.parts * g.joined;
+    g.part_share = g.share * g.joined;
+}
+
+static lbt_status gn_first(void (*kernel)(GroupNormArgs), const GroupNormArgs& g, dim3 grid, cudaStream_t stream) {
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid;
+    config.blockDim = dim3(kGnThreads);
+    config.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = g.joined;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    config.attrs = attr;
+    config.numAttrs = 1;
+    LBT_CUDA_TRY(cudaLaunchKernelEx(&config, kernel, g));
+    return launch_status();
 }
 
 // The second kernel of a pair may set up while the first one ends.
@@ -1013,8 +1063,7 @@ static lbt_status gn_forward(const GroupNormArgs& args, dim3 grid, cudaStream_t 
     if (const int ctas = gn_cluster(g, kVec, kImageThreads<kVec>, sizeof(T), 1, &smem))
         return gn_image_launch(gn_image<T, kVec, kAct>(g.q != nullptr), g, ctas, kImageThreads<kVec>, smem, stream);
     g = args;
-    groupnorm_stats_kernel<T, kVec><<<grid, kGnThreads, 0, stream>>>(g);
-    if (launch_status() != LBT_OK) return LBT_ERR_CUDA;
+    if (gn_first(groupnorm_stats_kernel<T, kVec>, g, grid, stream) != LBT_OK) return LBT_ERR_CUDA;
     smem = sizeof(float2) * std::min(g.G, kGnThreads * kVec);
     if constexpr (kVec == 8)
         if (g.q != nullptr) return gn_chained(groupnorm_apply_kernel<T, kVec, kAct, true>, grid, kGnThreads, smem, stream, g);
@@ -1031,8 +1080,7 @@ static lbt_status gn_backward(const GroupNormArgs& args, dim3 grid, cudaStream_t
         return gn_chained(groupnorm_params_kernel, dim3((g.C + 31) / 32), kGnThreads, 0, stream, g);
     }
     g = args;
-    groupnorm_sums_kernel<T, kVec, kAct><<<grid, kGnThreads, 0, stream>>>(g);
-    if (launch_status() != LBT_OK) return LBT_ERR_CUDA;
+    if (gn_first(groupnorm_sums_kernel<T, kVec, kAct>, g, grid, stream) != LBT_OK) return LBT_ERR_CUDA;
     grid.y = (g.dx != nullptr ? grid.y : 0) + 1;
     return gn_chained(groupnorm_dx_kernel<T, kVec, kAct>, grid, kGnThreads, sizeof(float2) * std::min(g.G, kGnThreads * kVec), stream, g);
 }
@@ -1052,8 +1100,7 @@ static lbt_status gn_run_act(const GroupNormArgs& g, dim3 grid, bool forward, cu
 template <typename T>
 static lbt_status gn_run_vec(GroupNormArgs& g, int64_t N, int vec, bool forward, cudaStream_t stream) {
     const int vecs = (g.C + vec - 1) / vec;
-    g.share = (g.P + gn_chunks(N, g.P, g.C, vec) - 1) / gn_chunks(N, g.P, g.C, vec);
-    g.chunks = (g.P + g.share - 1) / g.share;   // (no share is empty)
+    gn_share(g, N, vec);
     const dim3 grid(g.chunks, (unsigned)N, (vecs + kGnThreads - 1) / kGnThreads);
     if (vec == 8) return gn_run_act<T, 8>(g, grid, forward, stream);
     return vec == 2 ? gn_run_act<T, 2>(g, grid, forward, stream) : gn_run_act<T, 1>(g, grid, forward, stream);
@@ -1098,8 +1145,14 @@ extern "C" size_t lbt_groupnorm_workspace_bytes(const lbt_groupnorm_desc* desc) 
     lbt_groupnorm_desc d;
     if (gn_check(desc, &d) != LBT_OK) return 0;
     // two sums for each image, share and channel (any width of access), 256 bytes at least
-    const int64_t n = std::max<int64_t>(d.N, 1), chunks = std::max({gn_chunks(n, d.P, d.C, 1), gn_chunks(n, d.P, d.C, 2), gn_chunks(n, d.P, d.C, 8)});
-    return (size_t)std::max<int64_t>(256, d.N * chunks * d.C * (int64_t)sizeof(float2));
+    int64_t parts = 1;
+    for (int vec : {1, 2, 8}) {
+        GroupNormArgs g{};
+        g.P = (int)d.P; g.C = (int)d.C;
+        gn_share(g, std::max<int64_t>(d.N, 1), vec);
+        parts = std::max<int64_t>(parts, g.parts);
+    }
+    return (size_t)std::max<int64_t>(256, d.N * parts * d.C * (int64_t)sizeof(float2));
 }
 
 extern "C" lbt_status lbt_groupnorm_forward(const lbt_groupnorm_desc* desc, const void* x, const void* w, const void* b, void* y, void* q, int bits,
