@@ -35,6 +35,8 @@ def _images(t, name, channels, device):
             elif stride != step:
                 raise ValueError(f"{name}: pixels and images evenly spaced")
             step *= size
+        if ld < channels:
+            raise ValueError(f"{name}: pixels that do not overlap")
     return t.data_ptr(), kind, ld, images, pixels
 
 

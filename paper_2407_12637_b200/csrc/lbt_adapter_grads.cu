@@ -29,7 +29,7 @@ struct Tokens {
         int hi = 0;
         lo = 0;
         if (r < g.runs) {
-            if (g.offsets == nullptr) hi = (int)g.M;
+            if (g.offsets == nullptr) hi = adapter == 0 ? (int)g.M : 0;
             else if (g.index[r] == adapter) run_range(g.offsets, r, g.M, lo, hi);
         }
         upto = hi - lo;

@@ -1160,7 +1160,7 @@ extern "C" lbt_status lbt_groupnorm_forward(const lbt_groupnorm_desc* desc, cons
     lbt_groupnorm_desc d;
     const lbt_status rc = gn_check(desc, &d);
     if (rc != LBT_OK) return rc;
-    if ((y == nullptr && q == nullptr) || (q != nullptr && (d_clip == nullptr || d_scale_out == nullptr))) return LBT_ERR_INVALID_ARG;
+    if ((d.N > 0 && y == nullptr && q == nullptr) || (q != nullptr && (d_clip == nullptr || d_scale_out == nullptr))) return LBT_ERR_INVALID_ARG;
     if (q != nullptr && (bits < 2 || bits > 8)) return LBT_ERR_UNSUPPORTED_BITS;
     const size_t e = type_size(d.type), pe = type_size(d.param_type);
     if (gn_off(x, e) || gn_off(y, e) || gn_off(w, pe) || gn_off(b, pe) || gn_off(stats, 8) || gn_off(d_clip, 4) || gn_off(d_scale_out, 4) ||
@@ -1184,7 +1184,7 @@ extern "C" lbt_status lbt_groupnorm_backward(const lbt_groupnorm_desc* desc, con
     lbt_groupnorm_desc d;
     const lbt_status rc = gn_check(desc, &d);
     if (rc != LBT_OK) return rc;
-    if (dx == nullptr && dw == nullptr && db == nullptr) return LBT_ERR_INVALID_ARG;
+    if (d.N > 0 && dx == nullptr && dw == nullptr && db == nullptr) return LBT_ERR_INVALID_ARG;
     const size_t e = type_size(d.type), pe = type_size(d.param_type);
     if (gn_off(dy, e) || gn_off(x, e) || gn_off(dx, e) || gn_off(w, pe) || gn_off(b, pe) || gn_off(dw, pe) || gn_off(db, pe) || gn_off(stats, 8) || gn_off(ws, 8))
         return LBT_ERR_ALIGNMENT;

@@ -209,6 +209,8 @@ class Adapters:
             address, _, ld, rows = lbt._rows(t, name, width, self.device)
             if t.dtype != self.dtype or (M is not None and rows != M):
                 raise ValueError(f"{name}: one row per token, of the adapters' type {self.dtype}")
+            if ld < width:   # (a leading dimension of 0 stands for the row's length in the descriptor)
+                raise ValueError(f"{name}: rows that do not overlap")
             M = rows
             addresses.append(address)
             lds.append(ld)
@@ -335,6 +337,8 @@ class ResNorm:
                 raise ValueError(f"{name}: {rows} rows of {dtype}")
             addresses.append(address)
             lds.append(ld)
+        if min(l for l, a in zip(lds, acts) if a is not None) < self.dim:   # (0 stands for the row's length in the descriptor)
+            raise ValueError("rows that do not overlap")
         pd = self.param_dtype or (gate.dtype if gate is not None else dtype)
         if gate is not None:
             gates = -(-rows // rows_per_gate) if rows_per_gate else 1
@@ -459,7 +463,7 @@ class GradClip:
                 raise ValueError("gradients and outputs: fp32, bf16 or fp16, of equal sizes")
             e.g, e.out = lbt._at(g, self.device), lbt._at(o, self.device)
             e.n, e.g_type, e.out_type = g.numel(), lbt.TYPES[g.dtype], lbt.TYPES[o.dtype]
-            if e.g == e.out and g.dtype != o.dtype:
+            if e.n and e.g == e.out and g.dtype != o.dtype:
                 raise ValueError("an output in its gradient's place has its type")
         places = [e.out for e in self.table if e.n]
         if len(set(places)) != len(places):
