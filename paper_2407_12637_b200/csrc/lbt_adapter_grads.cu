@@ -253,30 +253,38 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
         for (int j = 0; j < kNt; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[0][j][i] += sum[j][i];
-    // The warps' sums over their tokens meet in the ring's place, one after the other, then the CTAs'.
+    // The warps' sums over their tokens meet in the ring's place, those of warps on the same tokens in one slab, then the CTAs' sums.
     asm volatile("cp.async.wait_group 0;" ::: "memory");
-    float* mine = reinterpret_cast<float*>(ring);   // [kR][kAgCols]
+    constexpr int kSlabRow = kAgCols + 4, kSlab = kR * kSlabRow;
+    static_assert(kAlong * kSlab * sizeof(float) <= (size_t)kStages * kStage, "the slabs take the ring's place");
+    float* mine = reinterpret_cast<float*>(ring);   // [kR][kSlabRow]: the first slab, then the CTA's sums
     const float back = 1.0f / factor;
-    for (int w = 0; w < kAlong; ++w) {
-        __syncthreads();
-        if (along != w) continue;
+    __syncthreads();
 #pragma unroll
-        for (int n = 0; n < kR16; ++n)
+    for (int n = 0; n < kR16; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {   // instruction j's columns 2 t and 2 t + 1 are 2 kNt t + j and 2 kNt t + kNt + j
-                float* to = mine + (16 * n + gq + 8 * (i >> 1)) * kAgCols + 8 * kNt * across + 2 * kNt * t + kNt * (i & 1);
+        for (int i = 0; i < 4; ++i) {   // instruction j's columns 2 t and 2 t + 1 are 2 kNt t + j and 2 kNt t + kNt + j
+            float* to = mine + along * kSlab + (16 * n + gq + 8 * (i >> 1)) * kSlabRow + 8 * kNt * across + 2 * kNt * t + kNt * (i & 1);
 #pragma unroll
-                for (int j = 0; j < kNt; ++j) to[j] = (w == 0 ? 0.0f : to[j]) + acc[n][j][i] * back;
-            }
+            for (int j = 0; j < kNt; j += 4)
+                *reinterpret_cast<float4*>(to + j) = make_float4(acc[n][j][i] * back, acc[n][j + 1][i] * back, acc[n][j + 2][i] * back, acc[n][j + 3][i] * back);
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < ranks * kAgCols; i += kAdThreads) {
+        float* at = mine + i / kAgCols * kSlabRow + i % kAgCols;
+        float v = at[0];
+#pragma unroll
+        for (int w = 1; w < kAlong; ++w) v += at[w * kSlab];
+        at[0] = v;
     }
     __syncthreads();
     cluster_sync_all();
     const float scale = g.scale != nullptr ? g.scale[adapter] : 1.0f;
-    for (int i = cta * kAdThreads + threadIdx.x; i < kR * kAgCols; i += ctas * kAdThreads) {   // each CTA finishes some rows
+    for (int i = cta * kAdThreads + threadIdx.x; i < ranks * kAgCols; i += ctas * kAdThreads) {   // each CTA finishes some rows
         const int k = i / kAgCols, c = col + i % kAgCols;
-        if (k >= ranks || c >= cols) continue;
+        if (c >= cols) continue;
         float v = 0.0f;
-        for (int p = 0; p < ctas; ++p) v += ld_cluster(map_to_cta(smem_u32(mine + i), p));
+        for (int p = 0; p < ctas; ++p) v += ld_cluster(map_to_cta(smem_u32(mine + k * kSlabRow + i % kAgCols), p));
         static_cast<G*>(g.out[which])[((int64_t)adapter * g.rank + rank0 + k) * cols + c] = from_f32<G>(v * scale);
     }
     __syncwarp();
@@ -291,7 +299,6 @@ static lbt_status grad_launch(AdapterGradArgs g, cudaStream_t stream) {
     // two CTAs to an SM, and two pieces of 64 tokens for each
     g.ctas = (int)std::max<int64_t>(1, std::min<int64_t>({kAdCluster, 2 * kNumSMs / blocks, g.M / (2 * kAgTokens * std::max(1, std::min(g.adapters, g.runs)))}));
     constexpr size_t smem = (size_t)kAgStages<kR16> * kAgTokens * (kAgStride + 4 * (kR + 4));
-    static_assert(smem >= sizeof(float) * kR * kAgCols, "the sums take the ring's place");
     const dim3 grid((g.groups[0] + g.groups[1]) * g.ctas, g.adapters, (g.rank + kR - 1) / kR);
     return cluster_launch(adapter_grad_kernel<T, G, kR16, kWords>, g, grid, smem, stream, g.ctas);
 }

@@ -21,7 +21,7 @@
 
 namespace lbt {
 
-// Few tokens a run: 16 of them a tile; the weights are what is read.  A cluster of eight CTAs and its 64 warps share x's columns, then the
+// Few tokens a run: 16 of them a tile; the weights are what is read.  A cluster of one to eight CTAs and its warps share x's columns, then the
 // output's: a warp copies 128 bytes of each row (of x and A, then of base and B) into a buffer of its own, kStride bytes a row (no two
 // of the eight lanes of an access meet in a bank).  The second product's first columns are under way while the cluster adds up h.
 // kN: blocks of eight ranks.  kWords: rows that begin anywhere.
@@ -38,12 +38,12 @@ __global__ void __launch_bounds__(kAdThreads, kN <= 2 ? 4 : kN <= 8 ? 2 : 1) ada
     float* mine = reinterpret_cast<float*>(buffers + kAdWarps * kBuffer);   // [16][kR], read by the other CTAs
     float* hs = mine + kAdTokens * kR;                                      // [16][kRow]
     float* factor = hs + kAdTokens * kRow;                                  // [16], of fp16 rows
-    const int cta = (int)cluster_ctarank();
+    const int cta = (int)cluster_ctarank(), ctas = g.ctas;
     int row, rows, adapter;
-    if (!run_of_tile<kAdTokens>(g, blockIdx.x / kAdCluster, row, rows, adapter)) return;   // (all CTAs of the cluster)
+    if (!run_of_tile<kAdTokens>(g, blockIdx.x / ctas, row, rows, adapter)) return;   // (all CTAs of the cluster)
     const int groups = (g.O + kStep - 1) / kStep, steps = (g.I + kStep - 1) / kStep;       // this CTA's columns of the output and of x
-    const int group_lo = (int)((int64_t)groups * cta / kAdCluster), group_hi = (int)((int64_t)groups * (cta + 1) / kAdCluster);
-    const int step_lo = (int)((int64_t)steps * cta / kAdCluster), step_hi = (int)((int64_t)steps * (cta + 1) / kAdCluster);
+    const int group_lo = (int)((int64_t)groups * cta / ctas), group_hi = (int)((int64_t)groups * (cta + 1) / ctas);
+    const int step_lo = (int)((int64_t)steps * cta / ctas), step_hi = (int)((int64_t)steps * (cta + 1) / ctas);
     const T* base = static_cast<const T*>(g.base) + row * g.ld_base;
     T* out = static_cast<T*>(g.out) + row * g.ld_out;
     if (adapter < 0 || adapter >= g.adapters) {
@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(kAdThreads, kN <= 2 ? 4 : kN <= 8 ? 2 : 1) ada
             v[n] = 0.0f;
             if (m < rows && 8 * n + j < g.rank) {
 #pragma unroll
-                for (int c = 0; c < kAdCluster; ++c) v[n] += ld_cluster(map_to_cta(smem_u32(mine + m * kR + 8 * n + j), c));
+                for (int c = 0; c < kAdCluster; ++c)
+                    if (c < ctas) v[n] += ld_cluster(map_to_cta(smem_u32(mine + m * kR + 8 * n + j), c));
                 if (g.h != nullptr && cta == 0) g.h[(int64_t)(row + m) * g.rank + 8 * n + j] = v[n];
                 v[n] *= scale;
                 most = max(most, abs_bits(v[n]));
@@ -419,14 +420,17 @@ template <typename T, int kN, bool kWords>
 static lbt_status adapter_launch(AdapterArgs g, cudaStream_t stream) {
     const int64_t runs = g.offsets == nullptr ? 1 : g.runs;
     constexpr int kR = 8 * kN;
-    // 16 tokens a tile where runs are short on average, or where such tiles are few enough (up to one and three quarters of what the SMs hold at
-    // once: to there they are faster, as a tile of 128 takes the time of its steps one after the other; 4096 -> 4096 with rank 16:
-    // 1024 tokens 11 against 15 us, 2048 tokens 19 against 22, 4096 tokens 35 against 23; twice as many in fp32).
-    constexpr int kFewTiles = (kN <= 2 ? 128 : kN <= 8 ? 64 : 32) * (IsF32<T>::value ? 2 : 1);
+    // 16 tokens a tile where runs are short on average, or where such tiles are few: a tile of 128 takes the time of its steps one after the
+    // other, whatever its number.  4096 -> 4096, 16 against 128 tokens a tile: rank 16 with 1024 tokens 11 against 15 us, 2048 tokens 17 against
+    // 22, 4096 tokens 30 against 21; rank 64 with 1024 tokens 21 against 29, 4096 tokens 55 against 48; twice as many tokens in fp32.
+    constexpr int kFewTiles = kN <= 4 ? (IsF32<T>::value ? 256 : 128) : IsF32<T>::value && kN == 8 ? 128 : 64;
     const int64_t few_tiles = std::min<int64_t>(g.M, (g.M + (kAdTokens - 1) * runs) / kAdTokens);
     if (g.M < 48 * runs || few_tiles <= kFewTiles) {
         constexpr size_t smem = kAdWarps * (kAdTokens + kR) * kStride + sizeof(float) * kAdTokens * (kR + kR + 4 + 1);
-        return cluster_launch(adapter_few_kernel<T, kN, kWords>, g, dim3((unsigned)(few_tiles * kAdCluster)), smem, stream);
+        static std::atomic<int> fit[kAdCluster + 1];   // as many CTAs to a cluster as leave all clusters resident at once
+        g.ctas = kAdCluster;
+        while (g.ctas > 1 && few_tiles > clusters_fit(adapter_few_kernel<T, kN, kWords>, smem, g.ctas, kAdThreads, fit)) --g.ctas;
+        return cluster_launch(adapter_few_kernel<T, kN, kWords>, g, dim3((unsigned)(few_tiles * g.ctas)), smem, stream, g.ctas);
     }
     const int64_t tiles = (g.M + (kTileTokens - 1) * runs) / kTileTokens;   // at most
     constexpr size_t smem = kTileStages<kN> * (kTileTokens + kR) * kStride + sizeof(float) * kTileTokens * (kR + kR + 4 + 1);

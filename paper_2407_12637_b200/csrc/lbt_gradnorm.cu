@@ -13,6 +13,7 @@
 
 #include <algorithm>
 
+#include "lbt_sm100.cuh"
 #include "lbt_types.cuh"
 
 namespace lbt {
@@ -151,7 +152,8 @@ struct NormCall {
 
 template <int kCap>
 __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_constant__ NormTable<kCap> t, const __grid_constant__ NormCall c) {
-    extern __shared__ double staged[];   // a word for each chunk, one for each tensor
+    extern __shared__ double staged[];   // a word for each chunk
+    sm100::griddep_launch_dependents();   // (the clipping behind it may set up; it waits for this grid before it reads anything)
     __shared__ uint32_t first[kCap + 1];
     __shared__ double space[kNormThreads / 32];
     __shared__ bool is_last;
@@ -189,26 +191,33 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
     }
     __syncthreads();
     if (!is_last) return;
-    // All partial sums come on chip in one sweep; a tensor of many chunks is then added by a warp, one of few by a thread.
-    constexpr uint32_t kFew = 32;
-    double* sums = reinterpret_cast<double*>(staged + all);
-    for (uint32_t k = threadIdx.x; k < all; k += kNormThreads) staged[k] = __ldcg(c.partial + k);
-    __syncthreads();
-    for (int i = warp; i < t.count; i += kNormThreads / 32) {
-        if (first[i + 1] - first[i] <= kFew) continue;
-        double sum = 0.0;
-        for (uint32_t k = first[i] + lane; k < first[i + 1]; k += 32) sum += staged[k];
-        sum = warp_sum(sum);
-        if (lane == 0) sums[i] = sum;
+    // All partial sums come on chip in one sweep, eight loads of a thread under way at a time; eight lanes then add up a tensor's.
+    for (uint32_t k0 = threadIdx.x; k0 < all; k0 += 8 * kNormThreads) {
+        double v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = k0 + u * kNormThreads < all ? __ldcg(c.partial + k0 + u * kNormThreads) : 0.0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (k0 + u * kNormThreads < all) staged[k0 + u * kNormThreads] = v[u];
     }
     __syncthreads();
     double total = 0.0;
-    for (int i = threadIdx.x; i < t.count; i += kNormThreads) {
-        double sum = 0.0;
-        if (first[i + 1] - first[i] > kFew) sum = sums[i];
-        else for (uint32_t k = first[i]; k < first[i + 1]; ++k) sum += staged[k];
-        total += sum;
-        if (c.norms != nullptr) c.norms[i] = (float)sqrt(sum);
+    for (int i0 = 0; i0 < t.count; i0 += kNormThreads / 8) {   // (whole warps stay together)
+        const int i = i0 + threadIdx.x / 8, j = threadIdx.x & 7;
+        double sum = 0.0, more = 0.0;
+        if (i < t.count) {
+            uint32_t k = first[i] + j;
+            const uint32_t end = first[i + 1];
+            for (; k + 8 < end; k += 16) { sum += staged[k]; more += staged[k + 8]; }
+            if (k < end) sum += staged[k];
+        }
+        sum += more;
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+        if (j == 0 && i < t.count) {
+            total += sum;
+            if (c.norms != nullptr) c.norms[i] = (float)sqrt(sum);
+        }
     }
     total = block_sum(total, space);
     if (threadIdx.x != 0) return;
@@ -270,9 +279,10 @@ __device__ __forceinline__ void clip_chunk_out(const NormEntry& e, float scale, 
 template <int kCap>
 __global__ void __launch_bounds__(kNormThreads) grad_clip_kernel(const __grid_constant__ NormTable<kCap> t, const lbt_grad_norm_t* norm) {
     __shared__ uint32_t first[kCap + 1];
+    for (int i = threadIdx.x; i <= t.count; i += kNormThreads) first[i] = t.first[i];
+    sm100::griddep_wait();
     const float scale = norm->scale;
     if (norm->skip != 0) return;
-    for (int i = threadIdx.x; i <= t.count; i += kNormThreads) first[i] = t.first[i];
     __syncthreads();
     const int lane = threadIdx.x & 31;
     const uint32_t all = first[t.count];
@@ -322,8 +332,8 @@ template <int kCap>
 static lbt_status norm_launch(const lbt_grad_tensor* tensors, int count, uint64_t chunk, const NormCall& c, uint32_t* chunks, cudaStream_t stream) {
     NormTable<kCap> t;
     *chunks = norm_table(t, tensors, count, chunk, false);
-    // (chunks: kNormChunks and one more for each tensor at most, 25 KB with their tensors' sums)
-    grad_norm_kernel<kCap><<<std::max(1, norm_grid(*chunks)), kNormThreads, sizeof(double) * (*chunks + count), stream>>>(t, c);
+    // (chunks: kNormChunks and one more for each tensor at most: 25 KB)
+    grad_norm_kernel<kCap><<<std::max(1, norm_grid(*chunks)), kNormThreads, sizeof(double) * *chunks, stream>>>(t, c);
     return launch_status();
 }
 
@@ -332,7 +342,16 @@ static lbt_status clip_launch(const lbt_grad_tensor* tensors, int count, uint64_
     NormTable<kCap> t;
     const uint32_t chunks = norm_table(t, tensors, count, chunk, true);
     if (chunks == 0) return LBT_OK;
-    grad_clip_kernel<kCap><<<norm_grid(chunks), kNormThreads, 0, stream>>>(t, norm);
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(norm_grid(chunks));
+    config.blockDim = dim3(kNormThreads);
+    config.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    config.attrs = attr;
+    config.numAttrs = 1;
+    LBT_CUDA_TRY(cudaLaunchKernelEx(&config, grad_clip_kernel<kCap>, t, norm));
     return launch_status();
 }
 
