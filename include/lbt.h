@@ -511,7 +511,8 @@ lbt_status lbt_grad_clip(const lbt_grad_tensor *tensors, int count, const lbt_gr
  * of all M tokens with adapter 0.  An index outside [0, adapters) is a run without an adapter: out = base.  Rows of no run (ahead of
  * offsets[0], from offsets[runs] on) are not written; offsets are cut to [0, M].  out may be base.
  * h (may be NULL): [M, rank] floats, kept for the backward pass (rows without an adapter are not written).
- * Sums are fp32 in an order fixed by the sizes; h enters its second product with 22 bits.  rank <= 128.
+ * Sums are fp32 in an order fixed by the sizes; h enters its second product with 16 (bf16) or 22 bits.  rank <= 128.  dev_status (device int32,
+ * may be NULL) receives LBT_ERR_TIMEOUT if a bounded on-chip wait ran out; the outputs that hang on it are not written.
  */
 typedef struct lbt_adapters_desc {   /* HOST struct */
     int64_t M, I, O, runs;
@@ -519,7 +520,8 @@ typedef struct lbt_adapters_desc {   /* HOST struct */
     int64_t ld_x, ld_base, ld_out, ld_dy, ld_dbase, ld_dx;   /* 0 = the row's length */
 } lbt_adapters_desc;
 lbt_status lbt_adapters_forward(const lbt_adapters_desc *d, const void *x, const void *a, const void *b, const float *scale,
-                                const int32_t *offsets, const int32_t *index, const void *base, void *out, float *h, void *cuda_stream);
+                                const int32_t *offsets, const int32_t *index, const void *base, void *out, float *h, int32_t *dev_status,
+                                void *cuda_stream);
 
 /*
  * Its gradients: dh[m] = B_i dy[m], dx[m] = dbase[m] + s_i dh[m] A_i (dx may be dbase; rows as for out), and over all runs of adapter i
@@ -529,7 +531,7 @@ lbt_status lbt_adapters_forward(const lbt_adapters_desc *d, const void *x, const
 size_t lbt_adapters_workspace_bytes(const lbt_adapters_desc *d);
 lbt_status lbt_adapters_backward(const lbt_adapters_desc *d, const void *dy, const void *x, const float *h, const void *a, const void *b,
                                  const float *scale, const int32_t *offsets, const int32_t *index, const void *dbase, void *dx, void *da,
-                                 void *db, int grad_type, void *ws, size_t ws_bytes, void *cuda_stream);
+                                 void *db, int grad_type, int32_t *dev_status, void *ws, size_t ws_bytes, void *cuda_stream);
 
 /*
  * Group norm with an activation on channels-last images x[N,P,C] (P pixels, ld elements from one pixel to the next, images P ld apart):

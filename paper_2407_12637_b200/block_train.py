@@ -90,7 +90,7 @@ class Stack:
 
     def check(self):
         """Raises if a product's output is missing (waits for the device)."""
-        for layer in self.layers:
+        for layer in self.layers + self.adapters:
             layer.check()
 
 

@@ -5,15 +5,17 @@
 // A and B are both stored rank first, [rank, I] and [rank, O]: the gradient of x is then the same operator with A and B
 // exchanged (dx = dbase + s (B dy) A), and both weight gradients have one form, G[k,c] = s sum_m f[m,k] z[m,c].
 //
-// Bound by memory: a token's row of x, base and out and the weights of the adapters in use, 2 rank operations an element.
-// So one cluster of eight CTAs carries a tile of 16 tokens through both products: each CTA takes an eighth of x's columns,
-// the partial h meet through the cluster's shared memory, then each CTA takes an eighth of the output's columns.  h never
-// leaves the chip (it is written only where the backward pass asks for it).
+// Bound by memory: a token's row of x, base and out and the weights of the adapters in use, 2 rank operations an element.  One
+// launch carries a tile of tokens through both products: the CTAs of a cluster share x's columns, their partial h meet through the
+// cluster's shared memory, then they share the output's columns.  h never leaves the chip (it is written only where the backward
+// pass asks for it).  Three kernels: tiles of 16 tokens (few tokens, short runs), and tiles of 128 on the tensor cores' own memory
+// (16-bit rows that begin on 16 bytes: lbt_adapters_tc.cu) or, for fp32 and rows that begin anywhere, on fragments in registers.
+// The rule between them stands at the launch, with both sides' times.
 //
-// Products run as tf32 with fp32 sums: bf16 and fp16 values are exact in tf32, h enters its second product as the sum of two
-// tf32 numbers (22 bits), and fp32 tensors are split the same way.  Fragments come straight from global memory: the
-// reduced index may be taken in any order that both operands share, so a lane's 16 (or 32) contiguous bytes serve four
-// instructions, and a lane ends up with 16 contiguous columns of the output.
+// Here bf16 and fp16 products run on fragments as they lie in memory, h entering the second one as two 16-bit numbers (fp16: after a
+// power of two for each row); fp32 ones as tf32, both operands split into two.  The reduced index may be taken in any order that
+// both operands share, so a lane's 32 contiguous bytes of x and A serve four instructions, and a lane ends up with 16 contiguous columns of
+// the output.  mma.sync reaches about 1250 multiply-adds a clock and SM here.
 #include <algorithm>
 #include <atomic>
 
@@ -40,7 +42,7 @@ __global__ void __launch_bounds__(kAdThreads, kN <= 2 ? 4 : kN <= 8 ? 2 : 1) ada
     float* factor = hs + kAdTokens * kRow;                                  // [16], of fp16 rows
     const int cta = (int)cluster_ctarank(), ctas = g.ctas;
     int row, rows, adapter;
-    if (!run_of_tile<kAdTokens>(g, blockIdx.x / ctas, row, rows, adapter)) return;   // (all CTAs of the cluster)
+    if (!run_of_tile(g, kAdTokens, blockIdx.x / ctas, row, rows, adapter)) return;   // (all CTAs of the cluster)
     const int groups = (g.O + kStep - 1) / kStep, steps = (g.I + kStep - 1) / kStep;       // this CTA's columns of the output and of x
     const int group_lo = (int)((int64_t)groups * cta / ctas), group_hi = (int)((int64_t)groups * (cta + 1) / ctas);
     const int step_lo = (int)((int64_t)steps * cta / ctas), step_hi = (int)((int64_t)steps * (cta + 1) / ctas);
@@ -209,7 +211,7 @@ __global__ void __launch_bounds__(kTileThreads<T, kN>, kN <= 4 ? 2 : 1) adapter_
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 7, part = threadIdx.x >> 8, gq = lane >> 2, t = lane & 3;
     const int cta = (int)cluster_ctarank(), ctas = g.ctas;
     int row, rows, adapter;
-    if (!run_of_tile<kTileTokens>(g, blockIdx.x / ctas, row, rows, adapter)) return;   // (all CTAs of the cluster)
+    if (!run_of_tile(g, kTileTokens, blockIdx.x / ctas, row, rows, adapter)) return;   // (all CTAs of the cluster)
     const int groups = (g.O + kStep - 1) / kStep, steps = (g.I + kStep - 1) / kStep;
     const int group_lo = (int)((int64_t)groups * cta / ctas), group_hi = (int)((int64_t)groups * (cta + 1) / ctas);
     const int step_lo = (int)((int64_t)steps * cta / ctas), n1 = (int)((int64_t)steps * (cta + 1) / ctas) - step_lo;
@@ -421,24 +423,33 @@ static lbt_status adapter_launch(AdapterArgs g, cudaStream_t stream) {
     const int64_t runs = g.offsets == nullptr ? 1 : g.runs;
     constexpr int kR = 8 * kN;
     // 16 tokens a tile where runs are short on average, or where such tiles are few: a tile of 128 takes the time of its steps one after the
-    // other, whatever its number.  4096 -> 4096, 16 against 128 tokens a tile: rank 16 with 1024 tokens 11 against 15 us, 2048 tokens 17 against
-    // 22, 4096 tokens 30 against 21; rank 64 with 1024 tokens 21 against 29, 4096 tokens 55 against 48; twice as many tokens in fp32.
-    constexpr int kFewTiles = kN <= 4 ? (IsF32<T>::value ? 256 : 128) : IsF32<T>::value && kN == 8 ? 128 : 64;
+    // other, whatever its number.  4096 -> 4096, 16 against 128 tokens a tile on the tensor cores' own memory: rank 16 with 1024 tokens 12 against
+    // 14 us, 2048 tokens 17 against 16; rank 32 with 1024 tokens 15 against 15; rank 64 with 128 tokens 13 against 15, 256 tokens 16 against 15;
+    // rank 128 with 128 tokens 19 against 20; 2048 tokens in runs of 96: rank 16 17 against 34, rank 64 31 against 36, rank 128 60 against
+    // 45, in runs of 192: 17 against 17, 31 against 19, 60 against 24.  On the other kernel: rank 16 with 2048 tokens 16 against 20, 4096 tokens 31 against
+    // 22; rank 64 with 1024 tokens 21 against 29, 4096 tokens 54 against 48; twice as many tokens in fp32.
+    constexpr bool kTc = !IsF32<T>::value && !kWords;
+    constexpr int kFewTiles = kTc ? (kN <= 2 ? 80 : kN <= 4 ? 64 : kN <= 8 ? 12 : 8) : kN <= 4 ? (IsF32<T>::value ? 256 : 128) : IsF32<T>::value && kN == 8 ? 128 : 64;
+    constexpr int kShort = !kTc ? 48 : kN <= 2 ? 256 : kN <= 4 ? 64 : kN <= 8 ? 48 : 16;
     const int64_t few_tiles = std::min<int64_t>(g.M, (g.M + (kAdTokens - 1) * runs) / kAdTokens);
-    if (g.M < 48 * runs || few_tiles <= kFewTiles) {
+    if (few_tiles <= kFewTiles || (runs > 1 && g.M < kShort * runs)) {
         constexpr size_t smem = kAdWarps * (kAdTokens + kR) * kStride + sizeof(float) * kAdTokens * (kR + kR + 4 + 1);
         static std::atomic<int> fit[kAdCluster + 1];   // as many CTAs to a cluster as leave all clusters resident at once
         g.ctas = kAdCluster;
         while (g.ctas > 1 && few_tiles > clusters_fit(adapter_few_kernel<T, kN, kWords>, smem, g.ctas, kAdThreads, fit)) --g.ctas;
         return cluster_launch(adapter_few_kernel<T, kN, kWords>, g, dim3((unsigned)(few_tiles * g.ctas)), smem, stream, g.ctas);
     }
-    const int64_t tiles = (g.M + (kTileTokens - 1) * runs) / kTileTokens;   // at most
-    constexpr size_t smem = kTileStages<kN> * (kTileTokens + kR) * kStride + sizeof(float) * kTileTokens * (kR + kR + 4 + 1);
-    // As many CTAs to a cluster as leave all clusters resident at once, where every other run ends in the middle of a tile's half.
-    static std::atomic<int> fit[kAdCluster + 1];
-    g.ctas = kAdCluster;
-    while (g.ctas > 1 && (g.M + kTileTokens / 2 * runs) / kTileTokens > clusters_fit(adapter_tile_kernel<T, kN, kWords>, smem, g.ctas, kTileThreads<T, kN>, fit)) --g.ctas;
-    return cluster_launch(adapter_tile_kernel<T, kN, kWords>, g, dim3((unsigned)(tiles * g.ctas)), smem, stream, g.ctas, kTileThreads<T, kN>);
+    if constexpr (kTc) {
+        return adapter_tc(g, IsHalf<T>::value ? LBT_F16 : LBT_BF16, stream);
+    } else {
+        const int64_t tiles = (g.M + (kTileTokens - 1) * runs) / kTileTokens;   // at most
+        constexpr size_t smem = kTileStages<kN> * (kTileTokens + kR) * kStride + sizeof(float) * kTileTokens * (kR + kR + 4 + 1);
+        // As many CTAs to a cluster as leave all clusters resident at once, where every other run ends in the middle of a tile's half.
+        static std::atomic<int> fit[kAdCluster + 1];
+        g.ctas = kAdCluster;
+        while (g.ctas > 1 && (g.M + kTileTokens / 2 * runs) / kTileTokens > clusters_fit(adapter_tile_kernel<T, kN, kWords>, smem, g.ctas, kTileThreads<T, kN>, fit)) --g.ctas;
+        return cluster_launch(adapter_tile_kernel<T, kN, kWords>, g, dim3((unsigned)(tiles * g.ctas)), smem, stream, g.ctas, kTileThreads<T, kN>);
+    }
 }
 
 template <typename T, bool kWords>
@@ -485,17 +496,18 @@ static lbt_status adapter_check(const lbt_adapters_desc* desc, lbt_adapters_desc
 using namespace lbt;
 
 extern "C" lbt_status lbt_adapters_forward(const lbt_adapters_desc* desc, const void* x, const void* a, const void* b, const float* scale,
-                                           const int32_t* offsets, const int32_t* index, const void* base, void* out, float* h, void* cuda_stream) {
+                                           const int32_t* offsets, const int32_t* index, const void* base, void* out, float* h,
+                                           int32_t* dev_status, void* cuda_stream) {
     lbt_adapters_desc d;
     const lbt_status rc = adapter_check(desc, &d);
     if (rc != LBT_OK) return rc;
     if (a == nullptr || b == nullptr || (d.runs > 0 && (offsets == nullptr) != (index == nullptr))) return LBT_ERR_INVALID_ARG;
     const size_t e = type_size(d.type);
-    if (off(x, e) || off(a, e) || off(b, e) || off(base, e) || off(out, e) || off(scale, 4) || off(offsets, 4) || off(index, 4) || off(h, 4))
+    if (off(x, e) || off(a, e) || off(b, e) || off(base, e) || off(out, e) || off(scale, 4) || off(offsets, 4) || off(index, 4) || off(h, 4) || off(dev_status, 4))
         return LBT_ERR_ALIGNMENT;
     if (d.M == 0 || (offsets != nullptr && d.runs == 0)) return LBT_OK;
     if (x == nullptr || base == nullptr || out == nullptr) return LBT_ERR_INVALID_ARG;
-    const AdapterArgs g{x, a, b, scale, offsets, index, base, out, h, d.M, d.ld_x, d.ld_base, d.ld_out, (int)d.I, (int)d.O, (int)d.runs, d.adapters, d.rank};
+    const AdapterArgs g{x, a, b, scale, offsets, index, base, out, h, d.M, d.ld_x, d.ld_base, d.ld_out, (int)d.I, (int)d.O, (int)d.runs, d.adapters, d.rank, dev_status};
     return adapter_pass(g, d.type, as_stream(cuda_stream));
 }
 
@@ -506,7 +518,7 @@ extern "C" size_t lbt_adapters_workspace_bytes(const lbt_adapters_desc* desc) {
 
 extern "C" lbt_status lbt_adapters_backward(const lbt_adapters_desc* desc, const void* dy, const void* x, const float* h, const void* a, const void* b,
                                             const float* scale, const int32_t* offsets, const int32_t* index, const void* dbase, void* dx, void* da,
-                                            void* db, int grad_type, void* ws, size_t ws_bytes, void* cuda_stream) {
+                                            void* db, int grad_type, int32_t* dev_status, void* ws, size_t ws_bytes, void* cuda_stream) {
     lbt_adapters_desc d;
     const lbt_status rc = adapter_check(desc, &d);
     if (rc != LBT_OK) return rc;
@@ -515,7 +527,7 @@ extern "C" lbt_status lbt_adapters_backward(const lbt_adapters_desc* desc, const
         return LBT_ERR_INVALID_ARG;
     const size_t e = type_size(d.type), ge = type_size(grad_type);
     if (off(dy, e) || off(x, e) || off(a, e) || off(b, e) || off(dbase, e) || off(dx, e) || off(da, ge) || off(db, ge) || off(scale, 4) || off(h, 4) ||
-        off(offsets, 4) || off(index, 4) || off(ws, 4))
+        off(offsets, 4) || off(index, 4) || off(ws, 4) || off(dev_status, 4))
         return LBT_ERR_ALIGNMENT;
     const bool any = d.M > 0 && (offsets == nullptr || d.runs > 0);
     if (any && (dy == nullptr || (da != nullptr && x == nullptr) || (db != nullptr && h == nullptr))) return LBT_ERR_INVALID_ARG;
@@ -524,7 +536,7 @@ extern "C" lbt_status lbt_adapters_backward(const lbt_adapters_desc* desc, const
     float* dh = static_cast<float*>(ws);
     if (any && (dx != nullptr || da != nullptr)) {   // the same operator with A and B exchanged
         const AdapterArgs g{dy, b, a, scale, offsets, index, dbase, dx, da != nullptr ? dh : nullptr, d.M, d.ld_dy, d.ld_dbase, d.ld_dx, (int)d.O, (int)d.I,
-                            (int)d.runs, d.adapters, d.rank};
+                            (int)d.runs, d.adapters, d.rank, dev_status};
         const lbt_status s = adapter_pass(g, d.type, stream);
         if (s != LBT_OK) return s;
     }

@@ -2,6 +2,8 @@
 // parts that those hold, rows that begin anywhere, cluster launches.
 #pragma once
 
+#include <type_traits>
+
 #include "lbt_sm100.cuh"
 #include "lbt_types.cuh"
 
@@ -27,7 +29,8 @@ struct AdapterArgs {
     float* h;              // [M, rank], unscaled; null: not wanted
     int64_t M, ld_x, ld_base, ld_out;
     int I, O, runs, adapters, rank;
-    int ctas;     // of a cluster (adapter_tile_kernel)
+    int32_t* status;   // device status word (null: none)
+    int ctas;     // of a cluster
     bool wide;    // rows of x, a, base and out begin on 32 bytes
 };
 
@@ -39,11 +42,10 @@ __device__ __forceinline__ void run_range(const int32_t* offsets, int r, int64_t
 }
 
 // The run that holds a tile, by all lanes of a warp together: first token, tokens of the tile, adapter.
-template <int kTokens>
-__device__ __forceinline__ bool run_of_tile(const AdapterArgs& g, int tile, int& row, int& rows, int& adapter) {
+__device__ __forceinline__ bool run_of_tile(const AdapterArgs& g, int tokens, int tile, int& row, int& rows, int& adapter) {
     if (g.offsets == nullptr) {
-        row = tile * kTokens;
-        rows = (int)min((int64_t)kTokens, g.M - row);
+        row = tile * tokens;
+        rows = (int)min((int64_t)tokens, g.M - row);
         adapter = 0;
         return rows > 0;
     }
@@ -52,7 +54,7 @@ __device__ __forceinline__ bool run_of_tile(const AdapterArgs& g, int tile, int&
     for (int r0 = 0; r0 < g.runs; r0 += 32) {
         int lo = 0, hi = 0;
         if (r0 + lane < g.runs) run_range(g.offsets, r0 + lane, g.M, lo, hi);
-        const int tiles = (hi - lo + kTokens - 1) / kTokens;
+        const int tiles = (hi - lo + tokens - 1) / tokens;
         int upto = tiles;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -63,8 +65,8 @@ __device__ __forceinline__ bool run_of_tile(const AdapterArgs& g, int tile, int&
         if (who != 0) {
             const int src = __ffs(who) - 1;
             const int at = tile - before - __shfl_sync(0xFFFFFFFFu, upto - tiles, src);
-            row = __shfl_sync(0xFFFFFFFFu, lo, src) + at * kTokens;
-            rows = min(kTokens, __shfl_sync(0xFFFFFFFFu, hi, src) - row);
+            row = __shfl_sync(0xFFFFFFFFu, lo, src) + at * tokens;
+            rows = min(tokens, __shfl_sync(0xFFFFFFFFu, hi, src) - row);
             adapter = g.index[r0 + src];
             return true;
         }
@@ -113,6 +115,14 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
     return v;
 }
 
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ void st_cluster2(uint32_t addr, uint2 v) {
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
+}
 __device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
@@ -231,15 +241,25 @@ template <typename T, int kWords> __device__ __forceinline__ void st_row(T* to, 
     }
     if (valid > 0) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-// out = base for the tokens of a run without an adapter, columns [lo, hi)
+// out = base for the tokens of a run without an adapter, columns [lo, hi): eight loads of a lane are on their way at a time.
 template <typename T, bool kWords> __device__ __forceinline__ void copy_rows(const AdapterArgs& g, const T* base, T* out, int rows, int lo, int hi, int warps) {
     if (g.out == nullptr || g.out == g.base) return;
-    constexpr int kEach = kWords ? 1 : 16 / (int)sizeof(T);
-    for (int m = threadIdx.x >> 5; m < rows; m += warps)
-        for (int c = lo + kEach * (threadIdx.x & 31); c < min(hi, g.O); c += 32 * kEach) {
-            if constexpr (kWords) out[m * g.ld_out + c] = base[m * g.ld_base + c];
-            else *reinterpret_cast<uint4*>(out + m * g.ld_out + c) = *reinterpret_cast<const uint4*>(base + m * g.ld_base + c);
+    using V = std::conditional_t<kWords, T, uint4>;
+    constexpr int kEach = sizeof(V) / sizeof(T), kDeep = 8;
+    const int n = (max(min(hi, g.O) - lo, 0) + 32 * kEach - 1) / (32 * kEach), all = rows * n, end = min(hi, g.O);   // a warp takes 32 lanes' columns of a row
+    for (int i0 = threadIdx.x >> 5; i0 < all; i0 += kDeep * warps) {
+        V v[kDeep];
+#pragma unroll
+        for (int q = 0; q < kDeep; ++q) {
+            const int i = i0 + q * warps, m = i / n, c = lo + kEach * (32 * (i - m * n) + (threadIdx.x & 31));
+            if (i < all && c < end) v[q] = *reinterpret_cast<const V*>(base + m * g.ld_base + c);
         }
+#pragma unroll
+        for (int q = 0; q < kDeep; ++q) {
+            const int i = i0 + q * warps, m = i / n, c = lo + kEach * (32 * (i - m * n) + (threadIdx.x & 31));
+            if (i < all && c < end) *reinterpret_cast<V*>(out + m * g.ld_out + c) = v[q];
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- rows that begin anywhere
@@ -391,6 +411,9 @@ template <typename T, int kCount> __device__ __forceinline__ void store_rows(T* 
         for (int e = 0; e < kCount; e += 32)
             if (e + lane < n) out[m * ld + e + lane] = *reinterpret_cast<const T*>(rows + m * 144 + at + (e + lane) * (int)sizeof(T));
 }
+
+// Long runs of 16-bit rows that begin on 16 bytes (lbt_adapters_tc.cu).
+lbt_status adapter_tc(const AdapterArgs& g, int type, cudaStream_t stream);
 
 struct AdapterGradArgs {
     const float* f[2];     // [M, rank]: dh for da, h for db

@@ -180,8 +180,8 @@ def lib() -> C.CDLL:
         l.lbt_grad_norm.argtypes = [vp, i32, C.c_double, vp, vp, vp, vp, sz, vp]
         l.lbt_grad_clip.argtypes = [vp, i32, vp, vp]
         l.lbt_grad_norm_workspace_bytes.argtypes = [vp, i32]
-        l.lbt_adapters_forward.argtypes = [vp] * 11
-        l.lbt_adapters_backward.argtypes = [vp] * 13 + [i32, vp, sz, vp]
+        l.lbt_adapters_forward.argtypes = [vp] * 12
+        l.lbt_adapters_backward.argtypes = [vp] * 13 + [i32, vp, vp, sz, vp]
         l.lbt_adapters_workspace_bytes.argtypes = [vp]
         l.lbt_groupnorm_forward.argtypes = [vp] * 6 + [i32, vp, vp, vp, vp, sz, vp]
         l.lbt_groupnorm_backward.argtypes = [vp] * 10 + [sz, vp]
@@ -544,19 +544,19 @@ def adapters_workspace_bytes(desc) -> int:
     return int(lib().lbt_adapters_workspace_bytes(C.addressof(desc)))
 
 
-def adapters_forward(desc, x, a, b, scale, offsets, index, base, out, h=None, stream=None):
+def adapters_forward(desc, x, a, b, scale, offsets, index, base, out, h=None, dev_status=None, stream=None):
     """`lbt_adapters_forward` on tensors that match `desc` (marshalling only: lm.Adapters builds and checks them)."""
     _check(lib().lbt_adapters_forward(C.addressof(desc), x.data_ptr(), _at(a), _at(b), _at(scale), _at(offsets), _at(index), base.data_ptr(),
-                                      out.data_ptr(), _at(h), _raw_stream(x, stream)), "lbt_adapters_forward")
+                                      out.data_ptr(), _at(h), _at(dev_status), _raw_stream(x, stream)), "lbt_adapters_forward")
 
 
-def adapters_backward(desc, dy, x, h, a, b, scale, offsets, index, dbase=None, dx=None, da=None, db=None, grad_type=F32, ws=None, stream=None):
+def adapters_backward(desc, dy, x, h, a, b, scale, offsets, index, dbase=None, dx=None, da=None, db=None, grad_type=F32, ws=None, dev_status=None, stream=None):
     """`lbt_adapters_backward` on tensors that match `desc`.  ws None: from torch's allocator."""
     if ws is None:
         ws = _scratch(adapters_workspace_bytes(desc), dy.device, stream)
     _check(lib().lbt_adapters_backward(C.addressof(desc), dy.data_ptr(), x.data_ptr(), _at(h), _at(a), _at(b), _at(scale), _at(offsets), _at(index),
                                        dbase.data_ptr() if dbase is not None else 0, dx.data_ptr() if dx is not None else 0, _at(da), _at(db),
-                                       grad_type, _at(ws), ws.numel(), _raw_stream(dy, stream)), "lbt_adapters_backward")
+                                       grad_type, _at(dev_status), _at(ws), ws.numel(), _raw_stream(dy, stream)), "lbt_adapters_backward")
 
 
 def groupnorm_workspace_bytes(desc) -> int:

@@ -188,8 +188,17 @@ class Adapters:
         self.a, self.b, self.scale, self.dtype, self.device = a, b, scale, a.dtype, a.get_device()
         with lbt._place(a):   # (addresses of the adapters' own tensors, whose storage stays)
             self._weights = (lbt._at(a), lbt._at(b), lbt._floats(scale, self.n, "scale"))
+        self.status = torch.zeros(1, dtype=torch.int32, device=a.device)   # lbt.ERR_TIMEOUT if a bounded on-chip wait ran out (check)
+        self._status = self.status.data_ptr()
         self.kept = None
         self._plans, self._own_kept, self._space = {}, {}, {}   # descriptors by sizes; by stream: h that is kept, workspace of the backward pass
+
+    def check(self):
+        """Raises LbtError if a bounded on-chip wait ran out since the last check (waits for the device): see Linear8.check."""
+        status = int(self.status)
+        if status:
+            self.status.zero_()
+            raise lbt.LbtError(status, "Adapters")
 
     def _runs(self, offsets, index):
         if offsets is None and index is None:
@@ -246,7 +255,7 @@ class Adapters:
                 if held:
                     self._own_kept[raw] = h
         a, b, scale = self._weights
-        status = lbt.lib().lbt_adapters_forward(desc, at[0], a, b, scale, at_offsets, at_index, at[1], at[2], h.data_ptr() if keep else 0, raw)
+        status = lbt.lib().lbt_adapters_forward(desc, at[0], a, b, scale, at_offsets, at_index, at[1], at[2], h.data_ptr() if keep else 0, self._status, raw)
         if status:
             raise lbt.LbtError(status, "lbt_adapters_forward")
         if keep:
@@ -288,7 +297,7 @@ class Adapters:
                 self._space[raw] = ws
         a, b, scale = self._weights
         status = lbt.lib().lbt_adapters_backward(desc, at[0], at[1], h.data_ptr(), a, b, scale, at_offsets, at_index, at[2], at[3], lbt._at(out["da"], on),
-                                                 lbt._at(out["db"], on), lbt.TYPES[kind], ws.data_ptr(), size, raw)
+                                                 lbt._at(out["db"], on), lbt.TYPES[kind], self._status, ws.data_ptr(), size, raw)
         if status:
             raise lbt.LbtError(status, "lbt_adapters_backward")
         return out

@@ -59,24 +59,23 @@ def _adapters(**change):
     ({"ld_out": 31}, lbt.ERR_INVALID_ARG), ({"M": 1 << 29}, lbt.ERR_UNSUPPORTED), ({"adapters": 65536}, lbt.ERR_UNSUPPORTED), ({"M": 0}, lbt.OK), ({"runs": 0}, lbt.OK)])
 def test_adapters_desc(change, want):
     d = _adapters(**change)
-    assert lbt.lib().lbt_adapters_forward(C.addressof(d), A, A, A, A, A, A, A, A if want != lbt.OK else None, None, None) == want
+    assert lbt.lib().lbt_adapters_forward(C.addressof(d), A, A, A, A, A, A, A, A if want != lbt.OK else None, None, None, None) == want
     assert (lbt.adapters_workspace_bytes(d) > 0) == (want == lbt.OK)
 
 
 def test_adapters_pointers():
     f, b = lbt.lib().lbt_adapters_forward, lbt.lib().lbt_adapters_backward
-    d = C.addressof(_adapters())
     keep = _adapters()
     d = C.addressof(keep)
-    args = dict(x=A, a=A, b=A, scale=A, offsets=A, index=A, base=A, out=A, h=A)
+    args = dict(x=A, a=A, b=A, scale=A, offsets=A, index=A, base=A, out=A, h=A, status=A)
     call = lambda **k: f(d, *{**args, **k}.values(), None)  # noqa: E731
     for name in ("x", "a", "b", "base", "out"):
         assert call(**{name: None}) == lbt.ERR_INVALID_ARG and call(**{name: A + 1}) == lbt.ERR_ALIGNMENT
-    for name in ("scale", "offsets", "index", "h"):
+    for name in ("scale", "offsets", "index", "h", "status"):
         assert call(**{name: A + 2}) == lbt.ERR_ALIGNMENT
     assert call(index=None) == lbt.ERR_INVALID_ARG and call(offsets=None) == lbt.ERR_INVALID_ARG
     assert f(None, *args.values(), None) == lbt.ERR_INVALID_ARG
-    more = dict(dy=A, x=A, h=A, a=A, b=A, scale=None, offsets=A, index=A, dbase=A, dx=A, da=A, db=A, grad_type=lbt.F32, ws=A, ws_bytes=1 << 20)
+    more = dict(dy=A, x=A, h=A, a=A, b=A, scale=None, offsets=A, index=A, dbase=A, dx=A, da=A, db=A, grad_type=lbt.F32, status=None, ws=A, ws_bytes=1 << 20)
     call = lambda **k: b(d, *{**more, **k}.values(), None)  # noqa: E731
     for name in ("dy", "x", "h", "a", "b", "dbase", "index"):
         assert call(**{name: None}) == lbt.ERR_INVALID_ARG
