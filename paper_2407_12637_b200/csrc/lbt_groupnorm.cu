@@ -6,7 +6,7 @@
 //
 // Bound by memory: x and y, then x, dy and dx.  Sums are kept by channel, whatever groups the channels fall into, so a thread owns
 // eight neighbouring channels (two, or one, where rows are not aligned) and walks over pixels.  Two forms:
-//   an image that fits the shared memory of a cluster (8 or 16 CTAs) is read once: each CTA keeps its share of the pixels on chip, the
+//   an image that fits the shared memory of a cluster (8 to 16 CTAs) is read once: each CTA keeps its share of the pixels on chip, the
 //   CTAs' sums of each channel meet through the cluster, and the output is formed from what is kept;
 //   a larger one is read twice: the first kernel leaves the sums of its share of an image's pixels for each channel, the second adds
 //   them up for its image (a few KB from L2), and streams.
@@ -15,6 +15,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "lbt_sm100.cuh"
 #include "lbt_types.cuh"
@@ -24,6 +25,7 @@ namespace lbt {
 constexpr int kGnThreads = 256;
 constexpr int kGnAhead = 4;             // pixels whose loads a thread has under way together
 constexpr int kGnPairs = 2;             // the same for two tensors at once
+constexpr int kGnClusters = 16;         // CTAs that keep an image on chip, at most
 constexpr int kGnJoined = 8;            // blocks of a cluster that add up their sums
 
 struct GroupNormArgs {
@@ -748,7 +750,10 @@ struct ImageSpace {
     }
 };
 
-// One cluster an image.
+// One cluster an image.  Forward pass, against two kernels: 64 x 56 x 56 x 64 bf16 with SiLU 20 us against 26, 16 x 96 x 96 x 64 fp16 18 against
+// 34 (without an activation 14: issuing the sigmoids' instructions takes the rest), 8 x 28 x 28 x 91 bf16 9.5 against 16.  What is left is read
+// (5500 clocks of 23000), sums through the cluster (6000) and written (7500) one after the other: an image's sums need all of it.
+// Two fp32 operations an instruction, and one reciprocal for two sigmoids, gained nothing.
 template <typename T, int kVec, int kAct, bool kCodes, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_kernel(const __grid_constant__ GroupNormArgs g) {
     extern __shared__ __align__(16) uint8_t image[];
@@ -762,18 +767,45 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_ker
     const int64_t step = cover.lanes * g.ld_x;
     fetch_parts(count, [&](int k) { kept.fetch(k, x + k * step); });
     load_params<kThreads>(g, 0, g.C, space.params);
-    Vals<kVec> s1 = all<kVec>(0.0f), s2 = all<kVec>(0.0f);
-    as_they_come(count, [&](int k) { s1 = add(s1, kept.get(k)); });
+    // 16-bit values: sums of differences from a thread's first value and of their squares while the pixels come; the squares are then moved to
+    // the CTA's mean.  They lose at most 2^-24 of themselves a pixel (110 of them: 2^-17), and that value is one of the image's.  fp32 values
+    // are read again around the CTA's mean.
+    constexpr bool kOnce = sizeof(T) == 2;
+    Vals<kVec> s1 = all<kVec>(0.0f), s2 = all<kVec>(0.0f), first = all<kVec>(0.0f);
+    const float own = (float)count, each = count > 0 ? 1.0f / own : 0.0f;
+    as_they_come(count, [&](int k) {
+        const Vals<kVec> v = kept.get(k);
+        if constexpr (kOnce) {
+            if (k == 0) first = mul(v, all<kVec>(-1.0f));
+            const Vals<kVec> d = add(v, first);
+            s1 = add(s1, d);
+            s2 = fma(d, d, s2);
+        } else {
+            s1 = add(s1, v);
+        }
+    });
+    Vals<kVec> mean = s1;
+    if constexpr (kOnce) {
+        mean = fma(s1, all<kVec>(each), mul(first, all<kVec>(-1.0f)));   // of the thread's pixels
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) s2.f[i] = fmaxf(fmaf(-s1.f[i], s1.f[i] * each, s2.f[i]), 0.0f);
+        s1 = mul(mean, all<kVec>(own));
+    }
     lanes_sum(s1, cover, space.rows, &space.chan[0].x);
     const float pixels = (float)(hi - lo), inv = hi > lo ? 1.0f / pixels : 0.0f;
     Vals<kVec> centre = all<kVec>(0.0f);   // minus this CTA's mean
     if (cover.active)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) centre.f[i] = -space.chan[cover.vec * kVec + i].x * inv;
+    if constexpr (kOnce) {
+        const Vals<kVec> d = add(mean, centre);
+        if (count > 0) s2 = fma(mul(d, d), all<kVec>(own), s2);
+    } else {
 #pragma unroll 4
-    for (int k = 0; k < count; ++k) {
-        const Vals<kVec> d = add(kept.get(k), centre);
-        s2 = fma(d, d, s2);
+        for (int k = 0; k < count; ++k) {
+            const Vals<kVec> d = add(kept.get(k), centre);
+            s2 = fma(d, d, s2);
+        }
     }
     lanes_sum(s2, cover, space.rows, &space.chan[0].y);
     // this CTA's mean and centred sum of squares of each group, then the image's
@@ -795,21 +827,22 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_ker
     cluster_arrive();
     cluster_wait();
     const float total = 1.0f / (float)g.P;
-    for (int i = threadIdx.x; i < g.G; i += kThreads) {
-        float2 v[16];
-        float mean = 0.0f, m2 = 0.0f;
+    for (int i0 = 0; i0 < g.G; i0 += kThreads / kGnClusters) {   // a lane for each CTA's sums of a group (whole warps stay together)
+        const int i = i0 + threadIdx.x / kGnClusters, c = threadIdx.x % kGnClusters;
+        const bool here = i < g.G && c < ctas;
+        const float2 v = here ? ld_cluster2(space.own + i, c) : make_float2(0.0f, 0.0f);
+        const float size = here ? (float)max(0, min(g.share, g.P - c * g.share)) : 0.0f;
+        float mean = size * v.x;
 #pragma unroll
-        for (int c = 0; c < 16; ++c)
-            if (c < ctas) v[c] = ld_cluster2(space.own + i, c);
-#pragma unroll
-        for (int c = 0; c < 16; ++c)
-            if (c < ctas) mean = fmaf((float)max(0, min(g.share, g.P - c * g.share)), v[c].x, mean);
+        for (int d = 1; d < kGnClusters; d <<= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, d);
         mean *= total;
+        float m2 = here ? fmaf(size * (float)cg * (v.x - mean), v.x - mean, v.y) : 0.0f;
 #pragma unroll
-        for (int c = 0; c < 16; ++c)
-            if (c < ctas) m2 += fmaf((float)max(0, min(g.share, g.P - c * g.share)) * (float)cg * (v[c].x - mean), v[c].x - mean, v[c].y);
-        space.group[i] = make_float2(mean, rsqrtf(m2 * total / (float)cg + g.eps));
-        if (g.stats != nullptr && cta == 0) reinterpret_cast<float2*>(g.stats)[(int64_t)n * g.G + i] = space.group[i];
+        for (int d = 1; d < kGnClusters; d <<= 1) m2 += __shfl_xor_sync(0xFFFFFFFFu, m2, d);
+        if (here && c == 0) {
+            space.group[i] = make_float2(mean, rsqrtf(m2 * total / (float)cg + g.eps));
+            if (g.stats != nullptr && cta == 0) reinterpret_cast<float2*>(g.stats)[(int64_t)n * g.G + i] = space.group[i];
+        }
     }
     __syncthreads();
     cluster_arrive();   // this CTA reads no other's sums any more
@@ -862,7 +895,7 @@ __device__ __forceinline__ Vals<kVec> slopes(Vals<kVec> e, const Vals<kVec>& k, 
     return e;
 }
 
-// Its gradients: x and dy are kept; partial: [N, C] sums of e and e k for the parameters' gradients.
+// Its gradients (64 x 56 x 56 x 64 bf16 with SiLU: 37 us against 49 of two kernels; the sigmoids are formed twice): x and dy are kept; partial: [N, C] sums of e and e k for the parameters' gradients.
 template <typename T, int kVec, int kAct, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 2) groupnorm_image_grad_kernel(const __grid_constant__ GroupNormArgs g) {
     extern __shared__ __align__(16) uint8_t image[];
@@ -1014,21 +1047,54 @@ static lbt_status gn_chained(void (*kernel)(Args...), dim3 grid, int threads, si
 // small packs need many threads to cover a row, and few registers each
 template <int kVec> constexpr int kImageThreads = kVec == 8 ? 256 : 512;
 constexpr size_t kGnSmem = 110 * 1024;   // shared memory of a CTA that keeps pixels: two of them to an SM
+// Clusters of so many CTAs that are resident at once, with at most four `blocks` of those to an SM: asked once for each.
+template <int kThreads> static int gn_resident(void (*kernel)(GroupNormArgs), int ctas, int blocks) {
+    static std::atomic<int> known[kGnClusters + 1][5];
+    int n = known[ctas][blocks].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(ctas);
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = std::min<size_t>(kGnSmem, 228 * 1024 / blocks - 1024);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    config.attrs = attr;
+    config.numAttrs = 1;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGnSmem) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &config) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = 1;
+    }
+    known[ctas][blocks].store(n, std::memory_order_relaxed);
+    return n;
+}
 // CTAs of the cluster that keeps an image on chip (`tensors` of its size) with blocks of so many threads, 0 if it does not fit one;
-// where the kept packs begin and the bytes of shared memory.
-static int gn_cluster(GroupNormArgs& g, int vec, int threads, size_t size, int tensors, size_t* smem) {
+// where the kept packs begin and the bytes of shared memory.  Of eight and more those that take the images in the fewest turns: an SM group holds one
+// cluster of 16 less where its SMs are no multiple of it (16 x 96 x 96 x 64 fp16 with SiLU: 24 us with 16 CTAs an image, in two turns, against 18 with 12).
+template <int kThreads>
+static int gn_cluster(GroupNormArgs& g, void (*kernel)(GroupNormArgs), int vec, int resident, size_t size, int tensors, size_t* smem) {
+    constexpr int threads = kThreads;
     const int vecs = (g.C + vec - 1) / vec;
     if (vecs > threads) return 0;
     const int lanes = threads / vecs;
     g.kept = (int)((sizeof(float2) * 2 * (g.C + g.G) + sizeof(float) * image_rows(vecs, threads) * g.C + 15) / 16 * 16);
-    for (int ctas : {8, 16}) {
+    int best = 0, least = 0;
+    for (int ctas = 8; ctas <= kGnClusters && least != 1; ++ctas) {
         const int share = (g.P + ctas - 1) / ctas;
-        *smem = g.kept + (size_t)tensors * ((share + lanes - 1) / lanes) * threads * vec * size;
-        if (*smem > kGnSmem) continue;
-        g.share = share;
-        return ctas;
+        const size_t bytes = g.kept + (size_t)tensors * ((share + lanes - 1) / lanes) * threads * vec * size;
+        if (bytes > kGnSmem) continue;
+        const int blocks = (int)std::min<size_t>(resident, 228 * 1024 / (bytes + 1024)), n = gn_resident<kThreads>(kernel, ctas, blocks), turns = (g.N + n - 1) / n;
+        if (best == 0 || turns < least) {
+            best = ctas;
+            least = turns;
+            g.share = share;
+            *smem = bytes;
+        }
     }
-    return 0;
+    return best;
 }
 
 static lbt_status gn_image_launch(void (*kernel)(GroupNormArgs), const GroupNormArgs& g, int ctas, int threads, size_t smem, cudaStream_t stream) {
@@ -1060,8 +1126,9 @@ template <typename T, int kVec, int kAct>
 static lbt_status gn_forward(const GroupNormArgs& args, dim3 grid, cudaStream_t stream) {
     GroupNormArgs g = args;
     size_t smem = 0;
-    if (const int ctas = gn_cluster(g, kVec, kImageThreads<kVec>, sizeof(T), 1, &smem))
-        return gn_image_launch(gn_image<T, kVec, kAct>(g.q != nullptr), g, ctas, kImageThreads<kVec>, smem, stream);
+    const auto image = gn_image<T, kVec, kAct>(g.q != nullptr);
+    if (const int ctas = gn_cluster<kImageThreads<kVec>>(g, image, kVec, 1024 / kImageThreads<kVec>, sizeof(T), 1, &smem))
+        return gn_image_launch(image, g, ctas, kImageThreads<kVec>, smem, stream);
     g = args;
     if (gn_first(groupnorm_stats_kernel<T, kVec>, g, grid, stream) != LBT_OK) return LBT_ERR_CUDA;
     smem = sizeof(float2) * std::min(g.G, kGnThreads * kVec);
@@ -1074,8 +1141,9 @@ template <typename T, int kVec, int kAct>
 static lbt_status gn_backward(const GroupNormArgs& args, dim3 grid, cudaStream_t stream) {
     GroupNormArgs g = args;
     size_t smem = 0;
-    if (const int ctas = gn_cluster(g, kVec, kImageThreads<kVec>, sizeof(T), 2, &smem)) {
-        const lbt_status s = gn_image_launch(groupnorm_image_grad_kernel<T, kVec, kAct, kImageThreads<kVec>>, g, ctas, kImageThreads<kVec>, smem, stream);
+    const auto image = groupnorm_image_grad_kernel<T, kVec, kAct, kImageThreads<kVec>>;
+    if (const int ctas = gn_cluster<kImageThreads<kVec>>(g, image, kVec, kVec == 8 ? 3 : 2, sizeof(T), 2, &smem)) {
+        const lbt_status s = gn_image_launch(image, g, ctas, kImageThreads<kVec>, smem, stream);
         if (s != LBT_OK || (g.dw == nullptr && g.db == nullptr)) return s;
         return gn_chained(groupnorm_params_kernel, dim3((g.C + 31) / 32), kGnThreads, 0, stream, g);
     }
