@@ -426,11 +426,12 @@ static lbt_status adapter_launch(AdapterArgs g, cudaStream_t stream) {
     // other, whatever its number.  4096 -> 4096, 16 against 128 tokens a tile on the tensor cores' own memory: rank 16 with 1024 tokens 12 against
     // 14 us, 2048 tokens 17 against 16; rank 32 with 1024 tokens 15 against 15; rank 64 with 128 tokens 13 against 15, 256 tokens 16 against 15;
     // rank 128 with 128 tokens 19 against 20; 2048 tokens in runs of 96: rank 16 17 against 34, rank 64 31 against 36, rank 128 60 against
-    // 45, in runs of 192: 17 against 17, 31 against 19, 60 against 24.  On the other kernel: rank 16 with 2048 tokens 16 against 20, 4096 tokens 31 against
-    // 22; rank 64 with 1024 tokens 21 against 29, 4096 tokens 54 against 48; twice as many tokens in fp32.
+    // 45, in runs of 192: 17 against 17, 31 against 19, 60 against 24.  On the other kernel, 1023 -> 2047 bf16: rank 13 with 2048 tokens 18 against
+    // 21, 8192 tokens 49 against 38, in runs of 64 49 against 68, of 256 49 against 50; rank 64 28 against 36, 91 against 76, 92 against 147, 91 against
+    // 145; fp32 1024 -> 2048: rank 13 16 against 22, 49 against 43; rank 64 37 against 51, 120 against 126; rank 128 82 against 86, 312 against 215.
     constexpr bool kTc = !IsF32<T>::value && !kWords;
-    constexpr int kFewTiles = kTc ? (kN <= 2 ? 80 : kN <= 4 ? 64 : kN <= 8 ? 12 : 8) : kN <= 4 ? (IsF32<T>::value ? 256 : 128) : IsF32<T>::value && kN == 8 ? 128 : 64;
-    constexpr int kShort = !kTc ? 48 : kN <= 2 ? 256 : kN <= 4 ? 64 : kN <= 8 ? 48 : 16;
+    constexpr int kFewTiles = kTc ? (kN <= 2 ? 80 : kN <= 4 ? 64 : kN <= 8 ? 12 : 8) : kN == 16 ? 128 : IsF32<T>::value ? 256 : 160;
+    constexpr int kShort = !kTc ? (kN <= 4 ? 256 : 512) : kN <= 2 ? 256 : kN <= 4 ? 64 : kN <= 8 ? 48 : 16;
     const int64_t few_tiles = std::min<int64_t>(g.M, (g.M + (kAdTokens - 1) * runs) / kAdTokens);
     if (few_tiles <= kFewTiles || (runs > 1 && g.M < kShort * runs)) {
         constexpr size_t smem = kAdWarps * (kAdTokens + kR) * kStride + sizeof(float) * kAdTokens * (kR + kR + 4 + 1);
