@@ -512,7 +512,7 @@ lbt_status lbt_grad_clip(const lbt_grad_tensor *tensors, int count, const lbt_gr
  * offsets[0], from offsets[runs] on) are not written; offsets are cut to [0, M].  out may be base.
  * h (may be NULL): [M, rank] floats, kept for the backward pass (rows without an adapter are not written).
  * Sums are fp32 in an order fixed by the sizes; h enters its second product with 16 (bf16) or 22 bits.  rank <= 128.  dev_status (device int32,
- * may be NULL) receives LBT_ERR_TIMEOUT if a bounded on-chip wait ran out; the outputs that hang on it are not written.
+ * may be NULL) receives LBT_ERR_TIMEOUT if a bounded on-chip wait ran out: out (dx) and h are then not complete, nor is what is formed from them.
  */
 typedef struct lbt_adapters_desc {   /* HOST struct */
     int64_t M, I, O, runs;
@@ -606,6 +606,14 @@ lbt_status lbt_selftest_barrier_timeout(int32_t *dev_status, uint32_t limit_us, 
  */
 lbt_status lbt_selftest_linear8_timeout(const void *q_x, const float *s_x, const void *q_w, const float *s_w, float *y, int64_t M,
                                         int64_t O, int64_t I, int rank, uint32_t limit_us, int32_t *dev_status, void *cuda_stream);
+
+/*
+ * The same for the adapters' kernel of long runs (bf16 or fp16, rows that begin on eight elements, one run of all M tokens with adapter 0): CTA
+ * `rank` (0 .. 7) of each cluster is never told that its first product is done.  Where clusters have that CTA, *dev_status becomes
+ * LBT_ERR_TIMEOUT and their rows of out stay as they were.
+ */
+lbt_status lbt_selftest_adapters_timeout(const lbt_adapters_desc *d, const void *x, const void *a, const void *b, const void *base, void *out,
+                                         int rank, uint32_t limit_us, int32_t *dev_status, void *cuda_stream);
 
 /* Static, NUL-terminated name of a status code. */
 const char *lbt_status_string(lbt_status status);

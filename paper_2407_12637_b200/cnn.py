@@ -15,15 +15,11 @@ from .lm import _capturing
 ACTS = {"none": lbt.ACT_NONE, "relu": lbt.ACT_RELU, "silu": lbt.ACT_SILU}
 
 
-def _images(t, name, channels, device):
-    """Address, element type, distance of pixels, images and pixels of a channels-last tensor [N, ..., C] whose pixels lie evenly spaced."""
-    kind, shape = lbt.TYPES.get(t.dtype), t.shape
-    if kind is None or len(shape) < 2 or t.get_device() != device or shape[-1] != channels:
-        raise ValueError(f"{name}: a CUDA tensor [N, ..., {channels}] of fp32, bf16 or fp16, on the device of the call")
-    count = t.numel()
-    if count > 0 and t.is_contiguous():
-        return t.data_ptr(), kind, channels, shape[0], count // (shape[0] * channels)
-    strides = t.stride()
+_LAYOUTS = {}   # (shape, strides) of tensors -> distance of pixels, images and pixels
+
+
+def _layout(shape, strides, name):
+    channels = shape[-1]
     if channels > 1 and strides[-1] != 1:
         raise ValueError(f"{name}: channels last (contiguous)")
     ld, pixels, images = channels, 1, shape[0]
@@ -41,6 +37,22 @@ def _images(t, name, channels, device):
             step *= size
         if ld < channels:
             raise ValueError(f"{name}: pixels that do not overlap")
+    return ld, images, pixels
+
+
+def _images(t, name, channels, device):
+    """Address, element type, distance of pixels, images and pixels of a channels-last tensor [N, ..., C] whose pixels lie evenly spaced."""
+    kind, shape = lbt.TYPES.get(t.dtype), t.shape
+    if kind is None or len(shape) < 2 or t.get_device() != device or shape[-1] != channels:
+        raise ValueError(f"{name}: a CUDA tensor [N, ..., {channels}] of fp32, bf16 or fp16, on the device of the call")
+    key = (shape, t.stride())
+    layout = _LAYOUTS.get(key)
+    if layout is None:
+        layout = _layout(*key, name)
+        if len(_LAYOUTS) >= 256:   # many sizes: they are cheap to look at again
+            _LAYOUTS.clear()
+        _LAYOUTS[key] = layout
+    ld, images, pixels = layout
     return t.data_ptr(), kind, ld, images, pixels
 
 

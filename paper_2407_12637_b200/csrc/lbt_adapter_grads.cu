@@ -7,6 +7,8 @@
 // bf16 or two fp16 numbers (24 or 22 bits: the gradients are fp32).  fp32 z and f are split into two tf32 numbers each.  fp16 holds no
 // more than 65504: there f enters times a power of two that brings the largest value of the CTA's tokens to [512, 1024).
 // (The tensor core's own sums are cut off, not rounded: those of four stages at most are added up in fp32.)
+// 8192 tokens, 4096 and 4096 columns, bf16, rank 16: 41 us for both gradients (56 with cold caches; reading x and dy takes 20): issue slots are
+// 0.46 busy with joining rows, splitting f and the ring, and the two kernels' data meet in L2 only in part.
 #include <algorithm>
 
 #include "lbt_adapters.cuh"

@@ -462,11 +462,15 @@ static lbt_status adapter_run(const AdapterArgs& g, cudaStream_t stream) {
     return adapter_launch<T, 16, kWords>(g, stream);
 }
 
+// Rows that begin on eight elements
+static bool adapter_aligned(const AdapterArgs& g, int type) {
+    auto ok = [&](const void* p) { return (reinterpret_cast<uintptr_t>(p) & (8 * type_size(type) - 1)) == 0; };
+    return g.I % 8 == 0 && g.O % 8 == 0 && g.ld_x % 8 == 0 && g.ld_base % 8 == 0 && g.ld_out % 8 == 0 && ok(g.x) && ok(g.a) && ok(g.b) && ok(g.base) && ok(g.out);
+}
+
 // One pass through both products; g.M > 0 and something to do.
 static lbt_status adapter_pass(AdapterArgs g, int type, cudaStream_t stream) {
-    auto ok = [&](const void* p) { return (reinterpret_cast<uintptr_t>(p) & (8 * type_size(type) - 1)) == 0; };
-    const bool aligned = g.I % 8 == 0 && g.O % 8 == 0 && g.ld_x % 8 == 0 && g.ld_base % 8 == 0 && g.ld_out % 8 == 0 && ok(g.x) && ok(g.a) && ok(g.b) &&
-                         ok(g.base) && ok(g.out);
+    const bool aligned = adapter_aligned(g, type);
     auto wide = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; };
     g.wide = g.I % 16 == 0 && g.O % 16 == 0 && g.ld_x % 16 == 0 && g.ld_base % 16 == 0 && g.ld_out % 16 == 0 && wide(g.x) && wide(g.a) && wide(g.base) && wide(g.out);
     if (type == LBT_F32) return aligned ? adapter_run<float, false>(g, stream) : adapter_run<float, true>(g, stream);
@@ -510,6 +514,20 @@ extern "C" lbt_status lbt_adapters_forward(const lbt_adapters_desc* desc, const 
     if (x == nullptr || base == nullptr || out == nullptr) return LBT_ERR_INVALID_ARG;
     const AdapterArgs g{x, a, b, scale, offsets, index, base, out, h, d.M, d.ld_x, d.ld_base, d.ld_out, (int)d.I, (int)d.O, (int)d.runs, d.adapters, d.rank, dev_status};
     return adapter_pass(g, d.type, as_stream(cuda_stream));
+}
+
+extern "C" lbt_status lbt_selftest_adapters_timeout(const lbt_adapters_desc* desc, const void* x, const void* a, const void* b, const void* base, void* out,
+                                                    int rank, uint32_t limit_us, int32_t* dev_status, void* cuda_stream) {
+    if (dev_status == nullptr || rank < 0 || rank >= kAdCluster || limit_us == 0 || limit_us > 1000000u) return LBT_ERR_INVALID_ARG;
+    lbt_adapters_desc d;
+    const lbt_status rc = adapter_check(desc, &d);
+    if (rc != LBT_OK) return rc;
+    if (x == nullptr || a == nullptr || b == nullptr || base == nullptr || out == nullptr) return LBT_ERR_INVALID_ARG;
+    AdapterArgs g{x, a, b, nullptr, nullptr, nullptr, base, out, nullptr, d.M, d.ld_x, d.ld_base, d.ld_out, (int)d.I, (int)d.O, 1, d.adapters, d.rank, dev_status};
+    if (d.M == 0 || !adapter_aligned(g, d.type) || d.type == LBT_F32) return LBT_ERR_UNSUPPORTED;
+    g.limit_ns = (uint64_t)limit_us * 1000ull;
+    g.mute = rank;
+    return adapter_tc(g, d.type, as_stream(cuda_stream));
 }
 
 extern "C" size_t lbt_adapters_workspace_bytes(const lbt_adapters_desc* desc) {

@@ -30,6 +30,8 @@ struct AdapterArgs {
     int64_t M, ld_x, ld_base, ld_out;
     int I, O, runs, adapters, rank;
     int32_t* status;   // device status word (null: none)
+    uint64_t limit_ns = 2000000000ull;   // after which an on-chip wait gives up (adapter_tc_kernel)
+    int mute = -1;     // the CTA of each cluster whose first product is never said to be done (self-test)
     int ctas;     // of a cluster
     bool wide;    // rows of x, a, base and out begin on 32 bytes
 };

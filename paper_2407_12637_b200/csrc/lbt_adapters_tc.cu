@@ -30,7 +30,6 @@ namespace lbt {
 constexpr int kTcTokens = 128;   // of a tile at most
 constexpr int kTcLeft = kTcTokens * 128;
 constexpr int kTcThreads = 384;   // a warp that loads, one that issues products, two idle; two times four of the epilogue
-constexpr uint64_t kTcLimit = 2000000000ull;               // of a wait, ns
 
 // Ranks to kMax: bytes of a stage, stages, accumulators of the first product (the second one's two lie behind them in TMEM).
 template <int kMax> struct TcSizes {
@@ -60,8 +59,8 @@ template <typename T> __device__ __forceinline__ uint32_t idesc_16(int m, int n,
     return 1u << 4 | format << 7 | format << 10 | (b_mn_major ? 1u : 0u) << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
 
-template <int kStages> __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, TcBarriers<kStages>* b) {
-    if (mbar_wait_bounded(bar, parity, kTcLimit)) return true;
+template <int kStages> __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, TcBarriers<kStages>* b, uint64_t limit_ns) {
+    if (mbar_wait_bounded(bar, parity, limit_ns)) return true;
     *reinterpret_cast<volatile uint32_t*>(&b->lost) = 1u;
     return false;
 }
@@ -117,8 +116,8 @@ adapter_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         const int s = i % kStages, before = i - kStages;
         if (before >= n1) {
             const int first = n1 + (s - n1 % kStages + kStages) % kStages;   // the first of the second product's steps in this stage
-            if (!tc_wait(&b->done[s], ((before - first) / kStages) & 1, b)) return false;
-        } else if (before >= 0 && !tc_wait(&b->used[s], (before / kStages) & 1, b)) {
+            if (!tc_wait(&b->done[s], ((before - first) / kStages) & 1, b, g.limit_ns)) return false;
+        } else if (before >= 0 && !tc_wait(&b->used[s], (before / kStages) & 1, b, g.limit_ns)) {
             return false;
         }
         const bool second = i >= n1;
@@ -145,7 +144,7 @@ adapter_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             const uint32_t idesc = idesc_16<T>(kTcTokens, ranks, false);
             for (int i = 0; i < n1 && ok; ++i) {
                 const int s = i % kStages;
-                ok = tc_wait(&b->full[s], (i / kStages) & 1, b);
+                ok = tc_wait(&b->full[s], (i / kStages) & 1, b, g.limit_ns);
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint64_t left = smem_desc_sw128(smem_u32(ring + s * S::kStage), 16, 1024), right = left + (kTcLeft >> 4);   // (addresses in 16 bytes)
@@ -153,11 +152,11 @@ adapter_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
                 for (int k = 0; k < 4; ++k) mma_f16(tmem + kMax * (i % S::kSums), left + 2 * k, right + 2 * k, idesc, i >= S::kSums || k > 0);
                 mma_commit(&b->used[s]);
             }
-            if (ok) mma_commit(&b->h_sums);
+            if (ok && cta != g.mute) mma_commit(&b->h_sums);
         }
     } else if (warp >= 4) {
         const int m = 32 * (warp & 3) + lane;
-        ok = tc_wait(&b->h_sums, 0, b);
+        ok = tc_wait(&b->h_sums, 0, b, g.limit_ns);
         __syncwarp();
         tc_fence_after_sync();
         for (int c0 = warp >= 8 ? 32 : 0; c0 < ranks; c0 += 64) {
@@ -254,7 +253,7 @@ adapter_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
                 const uint64_t h = smem_desc_sw128(smem_u32(parts), 16, 1024);
                 for (int j = 0; j < n2 && ok; ++j) {
                     const int i = n1 + j, s = i % kStages, buffer = j & 1;
-                    ok = (j < 2 || tc_wait(&b->taken[buffer], (j / 2 - 1) & 1, b)) && tc_wait(&b->full[s], (i / kStages) & 1, b);
+                    ok = (j < 2 || tc_wait(&b->taken[buffer], (j / 2 - 1) & 1, b, g.limit_ns)) && tc_wait(&b->full[s], (i / kStages) & 1, b, g.limit_ns);
                     if (!ok) break;
                     tc_fence_after_sync();
                     const uint32_t d = tmem + S::kSums * kMax + 64 * buffer;
@@ -273,7 +272,7 @@ adapter_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             const int buffer = warp >= 8, sub = lane >> 3, chunk = lane & 7;   // four warps take every other step
             for (int j = buffer; j < n2 && ok; j += 2) {
                 const int i = n1 + j, s = i % kStages, col = 64 * (group_lo + j);
-                ok = tc_wait(&b->full[s], (i / kStages) & 1, b) && tc_wait(&b->sums[buffer], (j / 2) & 1, b);
+                ok = tc_wait(&b->full[s], (i / kStages) & 1, b, g.limit_ns) && tc_wait(&b->sums[buffer], (j / 2) & 1, b, g.limit_ns);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
@@ -320,7 +319,7 @@ adapter_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     // What was asked for and not waited for (a wait has run out) arrives before this CTA's memory goes.
     if ((warp == 0 || warp == 2) && lane == 0 && (!go_on || *reinterpret_cast<volatile uint32_t*>(&b->lost) != 0)) {
         if (g.status != nullptr) atomicCAS(g.status, (int32_t)LBT_OK, (int32_t)LBT_ERR_TIMEOUT);
-        for (int i = max(0, loaded - kStages); i < loaded; ++i) mbar_wait_bounded(&b->full[i % kStages], (i / kStages) & 1, kTcLimit);
+        for (int i = max(0, loaded - kStages); i < loaded; ++i) mbar_wait_bounded(&b->full[i % kStages], (i / kStages) & 1, g.limit_ns);
     }
     if (warp == 1) { tc_fence_after_sync(); tmem_dealloc(tmem, 512); }
 }

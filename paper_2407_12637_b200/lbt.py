@@ -36,7 +36,7 @@ EXPORTS = (
     "lbt_adapters_forward", "lbt_adapters_backward", "lbt_adapters_workspace_bytes",
     "lbt_groupnorm_forward", "lbt_groupnorm_backward", "lbt_groupnorm_workspace_bytes",
     "lbt_set_timing_events", "lbt_selftest_wait_timeout", "lbt_selftest_barrier_timeout",
-    "lbt_selftest_linear8_timeout", "lbt_status_string",
+    "lbt_selftest_linear8_timeout", "lbt_selftest_adapters_timeout", "lbt_status_string",
 )
 TIME_STATS, TIME_QUANTIZE, TIME_EXPAND, TIME_DGRAD, TIME_WGRAD, TIME_FORWARD, TIME_FWD_QUANT = range(7)
 
@@ -189,6 +189,7 @@ def lib() -> C.CDLL:
         l.lbt_set_timing_events.argtypes = [i32, vp, vp]
         l.lbt_selftest_wait_timeout.argtypes = [vp, C.c_uint32, vp]
         l.lbt_selftest_barrier_timeout.argtypes = [vp, C.c_uint32, vp]
+        l.lbt_selftest_adapters_timeout.argtypes = [vp] * 6 + [i32, C.c_uint32, vp, vp]
         l.lbt_selftest_linear8_timeout.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i32, C.c_uint32, vp, vp]
         for name in EXPORTS:
             getattr(l, name).restype = sz if name.endswith("workspace_bytes") else C.c_int32
@@ -557,6 +558,12 @@ def adapters_backward(desc, dy, x, h, a, b, scale, offsets, index, dbase=None, d
     _check(lib().lbt_adapters_backward(C.addressof(desc), dy.data_ptr(), x.data_ptr(), _at(h), _at(a), _at(b), _at(scale), _at(offsets), _at(index),
                                        dbase.data_ptr() if dbase is not None else 0, dx.data_ptr() if dx is not None else 0, _at(da), _at(db),
                                        grad_type, _at(dev_status), _at(ws), ws.numel(), _raw_stream(dy, stream)), "lbt_adapters_backward")
+
+
+def selftest_adapters_timeout(desc, x, a, b, base, out, rank, dev_status, limit_us: int, stream=None):
+    """adapters_forward of long runs in which CTA `rank` of each cluster waits in vain; *dev_status becomes ERR_TIMEOUT and out stays as it was."""
+    _check(lib().lbt_selftest_adapters_timeout(C.addressof(desc), x.data_ptr(), _at(a), _at(b), base.data_ptr(), out.data_ptr(), int(rank), int(limit_us),
+                                               _at(dev_status), _raw_stream(x, stream)), "lbt_selftest_adapters_timeout")
 
 
 def groupnorm_workspace_bytes(desc) -> int:

@@ -143,11 +143,28 @@ def test_in_place_captured_and_on_two_streams(dtype):
     ad.check()
 
 
-def test_check_reports_the_status_word():
-    t = _make(4, 64, 64, 8, 1, torch.bfloat16)
-    ad, _ = _forward(t)
-    ad.check()
-    ad.status.fill_(lbt.ERR_TIMEOUT)
-    with pytest.raises(lbt.LbtError):
+@pytest.mark.parametrize("M,rank,mute", [(300, 16, 0), (300, 64, 7), (2500, 128, 2), (20000, 40, 0)])
+def test_a_lost_signal_stores_nothing(M, rank, mute):
+    """One CTA of each cluster that waits in vain: an error code, no output from any CTA of the cluster, and a usable context."""
+    t = _make(M, 520, 1032, rank, 1, torch.bfloat16, seed=3)
+    ad, want = _forward(t)
+    out = torch.full_like(t["base"], 7.0)
+    desc = lbt.AdaptersDesc(M=M, I=520, O=1032, runs=0, adapters=1, rank=rank, type=lbt.BF16)
+    lbt.selftest_adapters_timeout(desc, t["x"], t["a"], t["b"], t["base"], out, mute, ad.status, 2000)
+    torch.cuda.synchronize()
+    assert (out == 7.0).all()
+    with pytest.raises(lbt.LbtError) as e:
         ad.check()
-    ad.check()
+    assert e.value.status == lbt.ERR_TIMEOUT
+    assert torch.equal(_forward(t, adapters=ad)[1], want)
+    ad.check()   # (said once)
+
+
+def test_a_self_test_without_such_rows_is_refused():
+    t = _make(8, 60, 64, 8, 1, torch.bfloat16)
+    desc = lbt.AdaptersDesc(M=8, I=60, O=64, runs=0, adapters=1, rank=8, type=lbt.BF16)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for mute, limit in ((0, 1000), (8, 1000), (0, 0)):   # rows of 120 bytes; no such CTA; no limit
+        with pytest.raises(lbt.LbtError):
+            lbt.selftest_adapters_timeout(desc, t["x"], t["a"], t["b"], t["base"], t["base"], mute, status, limit)
+    assert int(status) == 0
