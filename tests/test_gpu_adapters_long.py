@@ -143,6 +143,22 @@ def test_in_place_captured_and_on_two_streams(dtype):
     ad.check()
 
 
+@pytest.mark.parametrize("rank", [16, 72])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_weight_gradients_alone(dtype, rank):
+    """Without dx the second product is left out: dA keeps its bits."""
+    t = _make(2500, 264, 136, rank, 2, dtype, seed=22)
+    g = torch.Generator(device="cuda").manual_seed(23)
+    dy, dbase = (torch.randn(2500, w, generator=g, device="cuda").to(dtype) for w in (136, 264))
+    ad, _ = _forward(t, [0, 1100, 1300, 2500], [1, -1, 0])
+    all_of_them = ad.backward(dy, dbase, dx=torch.empty_like(dbase))
+    alone = ad.backward(dy)
+    assert set(alone) == {"da", "db"} and torch.equal(alone["da"], all_of_them["da"]) and torch.equal(alone["db"], all_of_them["db"])
+    back = lm.Adapters(t["b"], t["a"], t["scale"])   # dx is the operator with A and B exchanged
+    assert torch.equal(back.forward(dy, dbase, _i32([0, 1100, 1300, 2500]), _i32([1, -1, 0]), out=torch.empty_like(dbase)), all_of_them["dx"])
+    ad.check()
+
+
 @pytest.mark.parametrize("M,rank,mute", [(300, 16, 0), (300, 64, 7), (2500, 128, 2), (20000, 40, 0)])
 def test_a_lost_signal_stores_nothing(M, rank, mute):
     """One CTA of each cluster that waits in vain: an error code, no output from any CTA of the cluster, and a usable context."""
