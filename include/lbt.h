@@ -526,7 +526,7 @@ lbt_status lbt_adapters_forward(const lbt_adapters_desc *d, const void *x, const
 /*
  * Its gradients: dh[m] = B_i dy[m], dx[m] = dbase[m] + s_i dh[m] A_i (dx may be dbase; rows as for out), and over all runs of adapter i
  * dA_i = s_i sum_m dh[m] x[m]^T, dB_i = s_i sum_m h[m] dy[m]^T: whole tensors like a and b of grad_type (LBT_F32, or the type of a), zeros
- * for an adapter without tokens.  Any of dx, da, db may be NULL.  x, h, runs: the forward pass's.  ws: lbt_adapters_workspace_bytes(d).
+ * for an adapter without tokens.  Any of dx, da, db may be NULL; dx is written first, so it is not x where da is wanted, nor dy where db is.  x, h, runs: the forward pass's.  ws: lbt_adapters_workspace_bytes(d).
  */
 size_t lbt_adapters_workspace_bytes(const lbt_adapters_desc *d);
 lbt_status lbt_adapters_backward(const lbt_adapters_desc *d, const void *dy, const void *x, const float *h, const void *a, const void *b,

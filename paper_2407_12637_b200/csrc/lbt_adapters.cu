@@ -551,6 +551,7 @@ extern "C" lbt_status lbt_adapters_backward(const lbt_adapters_desc* desc, const
     const bool any = d.M > 0 && (offsets == nullptr || d.runs > 0);
     if (any && (dy == nullptr || (da != nullptr && x == nullptr) || (db != nullptr && h == nullptr))) return LBT_ERR_INVALID_ARG;
     if (ws == nullptr || ws_bytes < lbt_adapters_workspace_bytes(desc)) return LBT_ERR_WORKSPACE;
+    if (any && dx != nullptr && ((da != nullptr && dx == x) || (db != nullptr && dx == dy))) return LBT_ERR_INVALID_ARG;   // written ahead of what reads it
     const cudaStream_t stream = as_stream(cuda_stream);
     float* dh = static_cast<float*>(ws);
     if (any && (dx != nullptr || da != nullptr)) {   // the same operator with A and B exchanged

@@ -85,6 +85,15 @@ def test_adapters_pointers():
     assert call(ws=None) == lbt.ERR_WORKSPACE and call(ws_bytes=8 * 16 * 4 - 1) == lbt.ERR_WORKSPACE
 
 
+def test_adapters_gradient_in_the_place_of_what_is_read_behind_it():
+    """dx is written first: not in the place of x where da is wanted, nor in dy's where db is."""
+    d = _adapters()
+    B = A + (1 << 20)
+    for x, dy, dx, da, db in ((A, B, A, A, None), (A, B, A, A, A), (B, A, A, None, A), (B, A, A, A, A)):
+        status = lbt.lib().lbt_adapters_backward(C.addressof(d), dy, x, A, A, A, None, A, A, A, dx, da, db, lbt.F32, None, A, 1 << 20, None)
+        assert status == lbt.ERR_INVALID_ARG
+
+
 # ---------------------------------------------------------------------------------------------- group norm
 def _norm(**change):
     d = lbt.GroupnormDesc(2, 10, 24, 3, lbt.BF16, lbt.F32, lbt.ACT_RELU, 1e-5)
