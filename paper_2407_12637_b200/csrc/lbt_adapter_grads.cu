@@ -289,7 +289,6 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
         for (int p = 0; p < ctas; ++p) v += ld_cluster(map_to_cta(smem_u32(mine + k * kSlabRow + i % kAgCols), p));
         static_cast<G*>(g.out[which])[((int64_t)adapter * g.rank + rank0 + k) * cols + c] = from_f32<G>(v * scale);
     }
-    __syncwarp();
     cluster_sync_all();   // nobody leaves before its sums have been fetched
 }
 

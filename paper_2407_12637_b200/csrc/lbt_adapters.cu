@@ -153,7 +153,6 @@ __global__ void __launch_bounds__(kAdThreads, kN <= 2 ? 4 : kN <= 8 ? 2 : 1) ada
 #pragma unroll
         for (int n = 0; n < kN; ++n) hs[m * kRow + 8 * n + j] = v[n] * f;
     }
-    __syncwarp();
     cluster_sync_all();   // nobody leaves, and nobody's h is read, before the partial sums have been fetched
     if (g.out == nullptr) return;
 
@@ -357,7 +356,6 @@ __global__ void __launch_bounds__(kTileThreads<T, kN>, kN <= 4 ? 2 : 1) adapter_
             if (kHalf && j == 0) st_cluster(map_to_cta(smem_u32(factor + m), c), 1.0f / f);
         }
     }
-    __syncwarp();
     cluster_sync_all();   // nobody leaves before the partial sums have been fetched, nobody goes on before h is there
     if (n2 == 0) return;
 

@@ -176,7 +176,6 @@ adapter_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         }
         tc_fence_before_sync();
     }
-    __syncwarp();
     cluster_sync_all();
     if (threadIdx.x == 0) {
         uint32_t lost = 0;
@@ -236,7 +235,6 @@ adapter_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         }
     }
     fence_proxy_async();
-    __syncwarp();
     cluster_sync_all();   // nobody leaves before the partial sums have been fetched, nobody goes on before h is there
     fence_proxy_async();
     const bool go_on = b->dead == 0;

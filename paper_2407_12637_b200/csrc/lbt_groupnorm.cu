@@ -175,7 +175,6 @@ template <typename Join> __device__ __forceinline__ void join_blocks(const Group
             for (int c = 0; c < g.joined; ++c) all = join(all, pixels, ld_cluster2(sums + i, c), blockIdx.x - rank + c);
         out[i] = all;
     }
-    __syncwarp();
     if (g.joined > 1) sm100::cluster_sync_all();   // nobody leaves before its sums have been fetched
 }
 
@@ -731,8 +730,15 @@ __device__ __forceinline__ void lanes_sum(Vals<kVec> v, const Cover<kVec, kThrea
 }
 static int image_rows(int vecs, int threads) { return vecs <= 32 && 32 % vecs == 0 ? threads / 32 : threads / vecs; }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// (as cluster_sync_all: a warp's lanes come from loops of their own lengths and meet first)
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 // How shared memory begins in both kernels below; the packs that are kept come behind it, at g.kept.
 struct ImageSpace {
@@ -823,7 +829,6 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_ker
         m2 = groups.add(m2);
         if (groups.lane == 0 && i0 + groups.own < groups.count) space.own[i] = make_float2(mean, m2);
     }
-    __syncwarp();
     cluster_arrive();
     cluster_wait();
     const float total = 1.0f / (float)g.P;
@@ -945,7 +950,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 2) groupnorm_i
         ek = groups.add(ek);
         if (groups.lane == 0 && i0 + groups.own < groups.count) space.own[i] = make_float2(e, ek);
     }
-    __syncwarp();
     cluster_arrive();
     cluster_wait();
     if (g.dw != nullptr || g.db != nullptr)   // each CTA adds up some of the channels for its image

@@ -203,7 +203,9 @@ __device__ __forceinline__ uint32_t cluster_ctarank() {
     return r;
 }
 
+// (the instructions are of the kind that a whole warp executes together, wherever its lanes come from: they meet first)
 __device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 

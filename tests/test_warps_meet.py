@@ -1,0 +1,24 @@
+"""Instructions of the kind that a whole warp executes together, read in the kernels' sources: its lanes meet (`__syncwarp`) wherever they may come from
+loops of their own lengths.  Hardware need not join them by itself, and a barrier that part of a warp enters may never end."""
+import glob
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2407_12637_b200", "csrc")
+
+
+def _lines(name):
+    """The lines that hold code, without their comments."""
+    lines = [re.sub(r"//.*", "", line).strip() for line in open(os.path.join(CSRC, name))]
+    return [line for line in lines if line]
+
+
+def test_ahead_of_every_cluster_barrier():
+    found = 0
+    for path in glob.glob(os.path.join(CSRC, "*.cu*")):
+        lines = _lines(os.path.basename(path))
+        for before, line in zip(lines, lines[1:]):
+            if "barrier.cluster" in line and ".aligned" in line:
+                found += 1
+                assert before == "__syncwarp();", (os.path.basename(path), line)
+    assert found >= 3
