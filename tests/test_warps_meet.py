@@ -22,3 +22,15 @@ def test_ahead_of_every_cluster_barrier():
                 found += 1
                 assert before == "__syncwarp();", (os.path.basename(path), line)
     assert found >= 3
+
+
+def test_ahead_of_tensor_memory_taken_and_given_back():
+    """Taking it follows zero fills and set-up that some of a warp's lanes do; where it does not end, neither does the block."""
+    found = 0
+    for path in glob.glob(os.path.join(CSRC, "*.cu*")):
+        lines = _lines(os.path.basename(path))
+        for before, line in zip(lines, lines[1:]):
+            if re.search(r"tcgen05\.(alloc|dealloc)\.", line):
+                found += 1
+                assert before == "__syncwarp();", (os.path.basename(path), line)
+    assert found == 4
