@@ -203,6 +203,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
         const int ahead = now + kStages - 1 > kStages ? now - 2 : now + kStages - 1, last = now == 0 ? kStages : now - 1;
         fetch(at == 0 ? kStages - 1 : at - 1, ids[ahead], have[ahead]);
         produce(tokens, last);
+        __syncwarp();   // (lanes copied words of their own number; matrix instructions, a whole warp's, follow)
         const int* list = ids[now];
         const uint8_t* s = ring + at * kStage;
         const float* fs = reinterpret_cast<const float*>(s + kAgTokens * kAgStride);

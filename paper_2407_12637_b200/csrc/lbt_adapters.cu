@@ -281,6 +281,7 @@ __global__ void __launch_bounds__(kTileThreads<T, kN>, kN <= 4 ? 2 : 1) adapter_
             slot = next % kStages == 0 ? slot - (kStages - 1) * kStage : slot + kStage;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
+        __syncwarp();   // (lanes copied words of their own number; matrix instructions, a whole warp's, follow)
     };
     // Step i's stage, once it has come for all threads; the one behind the ring's end is then on its way.
     auto stage = [&](int i) -> uint8_t* {

@@ -34,3 +34,15 @@ def test_ahead_of_tensor_memory_taken_and_given_back():
                 found += 1
                 assert before == "__syncwarp();", (os.path.basename(path), line)
     assert found == 4
+
+
+def test_between_copies_and_matrix_instructions():
+    """Rows that begin anywhere are copied in loops whose lanes take words of their own number."""
+    for name in ("lbt_adapters.cu", "lbt_adapter_grads.cu"):
+        text = " ".join(_lines(name))
+        kernels = [k for k in text.split("__global__")[1:] if "copy_words<" in k]
+        assert kernels
+        for kernel in kernels:
+            copies = kernel.rindex("copy_words<")
+            product = min(at for at in (kernel.find(what, copies) for what in ("mma_step<", "rank_product<", "mma_split<")) if at >= 0)
+            assert "__syncwarp();" in kernel[copies:product], (name, kernel[:200])
