@@ -11,7 +11,7 @@
 //   a larger one is read twice: the first kernel leaves the sums of its share of an image's pixels for each channel, the second adds
 //   them up for its image (a few KB from L2), and streams.
 // The variance must not lose itself in a mean far from 0: shares are combined from their means and centred sums of squares, which
-// are formed around the share's own mean (what is kept can be read again) or around the first value that a thread reads.
+// are formed around the share's own mean (what is kept can be read again) or around the mean of what a thread has read so far.
 #include <math.h>
 
 #include <algorithm>
@@ -178,7 +178,23 @@ template <typename Join> __device__ __forceinline__ void join_blocks(const Group
     if (g.joined > 1) sm100::cluster_sync_all();   // nobody leaves before its sums have been fetched
 }
 
-// A share's mean and centred sum of squares of each channel.  A thread sums differences from the first value that it reads; the block's
+// The sums of differences (s1) and of their squares (s2) of a thread's `count` values, moved from the value c around which they were formed to
+// the values' mean: s1 is then 0 and s2 the centred sum.
+template <int kVec> __device__ __forceinline__ void move_to_mean(float (&c)[kVec], float (&s1)[kVec], float (&s2)[kVec], int count) {
+    const float each = 1.0f / (float)count;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        const float shift = s1[i] * each;
+        s2[i] = fmaf(-s1[i], shift, s2[i]);
+        c[i] += shift;
+        s1[i] = 0.0f;
+    }
+}
+// Where that is done: after 4, 8, 16, 32, 64, 96, .. values.  Around a first value that lies D away from the rest n squares add up to n D^2, of which D^2 is
+// the image's: n^2 2^-24 of it would be lost.  Four of them lose 2^-18; around the mean of four the next ones' differences are a quarter, and so on.
+__device__ __forceinline__ bool time_to_move(int count) { return count >= 4 && (count & min(count - 1, 31)) == 0; }
+
+// A share's mean and centred sum of squares of each channel.  A thread sums differences from the mean of what it has read; the block's
 // mean is formed from the threads' means, then every thread's sum of squares is moved to that mean.
 template <typename T, int kVec>
 __global__ void __launch_bounds__(kGnThreads, 4) groupnorm_stats_kernel(const __grid_constant__ GroupNormArgs g) {
@@ -213,14 +229,13 @@ __global__ void __launch_bounds__(kGnThreads, 4) groupnorm_stats_kernel(const __
                 s2[i] = fmaf(d, d, s2[i]);
             }
         }
+        if (p + kGnAhead <= count && time_to_move(p + kGnAhead)) move_to_mean(first, s1, s2, p + kGnAhead);
     }
-    const float inv = count > 0 ? 1.0f / (float)count : 0.0f;
+    if (count > 0) move_to_mean(first, s1, s2, count);
     if (cover.active) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {   // the thread's mean, times its count; centred squares
-            const float shift = s1[i] * inv;
-            s2[i] = fmaxf(fmaf(-s1[i], shift, s2[i]), 0.0f);
-            first[i] += shift;
+            s2[i] = fmaxf(s2[i], 0.0f);
             part[cover.lane * width + cover.vec * kVec + i] = make_float2(first[i] * (float)count, 0.0f);
         }
     }
@@ -689,7 +704,8 @@ template <typename Fetch> __device__ __forceinline__ void fetch_parts(int count,
     }
 }
 template <int kLeft> __device__ __forceinline__ void parts_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
-template <typename F> __device__ __forceinline__ void as_they_come(int count, F f) {
+// once(k): behind the first part, k packs.
+template <typename F, typename Once> __device__ __forceinline__ void as_they_come(int count, F f, Once once) {
     const int part = (count + 3) / 4;
 #pragma unroll 1
     for (int q = 0; q < 4; ++q) {
@@ -699,6 +715,7 @@ template <typename F> __device__ __forceinline__ void as_they_come(int count, F 
         else parts_wait<0>();
 #pragma unroll 2
         for (int k = q * part; k < min((q + 1) * part, count); ++k) f(k);
+        if (q == 0) once(part);
     }
 }
 
@@ -773,9 +790,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_ker
     const int64_t step = cover.lanes * g.ld_x;
     fetch_parts(count, [&](int k) { kept.fetch(k, x + k * step); });
     load_params<kThreads>(g, 0, g.C, space.params);
-    // 16-bit values: sums of differences from a thread's first value and of their squares while the pixels come; the squares are then moved to
-    // the CTA's mean.  They lose at most 2^-24 of themselves a pixel (110 of them: 2^-17), and that value is one of the image's.  fp32 values
-    // are read again around the CTA's mean.
+    // 16-bit values: sums of differences and of their squares while the pixels come, around a thread's first value for a quarter of its packs, then
+    // around the mean of that quarter: at most 28 single values (3 x 28^2 2^-24 = 2^-13 of the variance lost, see time_to_move), 14 pairs or 7 packs of
+    // eight (2^-17).  Moving more often gained no digit that 16 bits show and cost 5 % (16 x 96 x 96 x 64 fp16) to 9 % (31 x 4001 x 66 bf16); this
+    // costs 0.5 and 1.5 %.  The squares are then moved to the CTA's mean.  fp32 values are read again around the CTA's mean.
     constexpr bool kOnce = sizeof(T) == 2;
     Vals<kVec> s1 = all<kVec>(0.0f), s2 = all<kVec>(0.0f), first = all<kVec>(0.0f);
     const float own = (float)count, each = count > 0 ? 1.0f / own : 0.0f;
@@ -788,6 +806,17 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_ker
             s2 = fma(d, d, s2);
         } else {
             s1 = add(s1, v);
+        }
+    }, [&](int k) {
+        if constexpr (kOnce) {
+            const float each = __fdividef(1.0f, (float)max(k, 1));   // (2^-22: what it leaves of s1 weighs its square)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {   // (`first` is minus the value)
+                const float shift = s1.f[i] * each;
+                s2.f[i] = fmaf(-s1.f[i], shift, s2.f[i]);
+                first.f[i] -= shift;
+                s1.f[i] = 0.0f;
+            }
         }
     });
     Vals<kVec> mean = s1;
@@ -934,7 +963,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 2) groupnorm_i
         const Vals<kVec> k = add(kept.get(i), centre), e = slopes<T, kVec, kAct>(kept_dy.get(i), k, a, b);
         s1 = add(s1, e);
         s2 = fma(e, k, s2);
-    });
+    }, [](int) {});
     if (cover.active) s2 = mul(s2, rstd);
     lanes_sum(s1, cover, space.rows, &space.chan[0].x);
     lanes_sum(s2, cover, space.rows, &space.chan[0].y);
