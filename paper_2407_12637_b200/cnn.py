@@ -1,11 +1,13 @@
 """Layers between the quantized convolutions on the library's kernels: `GroupNorm`.
 
 As in `lm`, an object keeps what a program keeps between calls (parameters, scratch for each stream) and every step of arithmetic
-runs in the library (`lbt`); outputs may be handed in, work is enqueued on `stream` (default: torch's current stream).
+runs in the library (`lbt`); outputs may be handed in, work is enqueued on `stream` (default: torch's current stream).  Threads may
+share an object's forward passes without `keep`; what `keep` holds for `backward` belongs to one thread at a time.
 """
 from __future__ import annotations
 
 import ctypes as C
+import threading
 
 import torch
 
@@ -78,6 +80,7 @@ class GroupNorm:
         else:
             self._params = (0, 0)
         self._plans, self._stats, self._space = {}, {}, {}   # descriptors by sizes; by stream: statistics that are kept, workspace
+        self._lock = threading.Lock()   # a pass is two launches that meet in the workspace (the library's call lets other threads run)
 
     def _plan(self, names, acts, on):
         if self.device is not None and on != self.device:
@@ -119,21 +122,22 @@ class GroupNorm:
         at, (_, desc, size) = self._plan(("x", "y"), (x, y), on)
         raw, stats = lbt._current_raw_stream(on), None
         held = not _capturing(raw)
-        if keep:   # a buffer for each stream, shared by one forward pass after the other
-            stats = self._stats.get(raw) if held else None
-            if stats is None or stats.shape[0] != x.shape[0]:
-                stats = torch.empty(x.shape[0], self.groups, 2, dtype=torch.float32, device=x.device)
-                if held:
-                    self._stats[raw] = stats
-        ws = self._workspace(raw, held, size, x.device)
-        w, b = self._params
-        status = lbt.lib().lbt_groupnorm_forward(desc, at[0], w, b, at[1], q.data_ptr() if q is not None else 0, bits,
-                                                 lbt._floats(clip, 1, "clip", on), scale.data_ptr() if q is not None else 0,
-                                                 stats.data_ptr() if keep else 0, ws.data_ptr(), size, raw)
-        if status:
-            raise lbt.LbtError(status, "lbt_groupnorm_forward")
-        if keep:
-            self.kept = (x, stats)
+        with self._lock:
+            if keep:   # a buffer for each stream, shared by one forward pass after the other
+                stats = self._stats.get(raw) if held else None
+                if stats is None or stats.shape[0] != x.shape[0]:
+                    stats = torch.empty(x.shape[0], self.groups, 2, dtype=torch.float32, device=x.device)
+                    if held:
+                        self._stats[raw] = stats
+            ws = self._workspace(raw, held, size, x.device)
+            w, b = self._params
+            status = lbt.lib().lbt_groupnorm_forward(desc, at[0], w, b, at[1], q.data_ptr() if q is not None else 0, bits,
+                                                     lbt._floats(clip, 1, "clip", on), scale.data_ptr() if q is not None else 0,
+                                                     stats.data_ptr() if keep else 0, ws.data_ptr(), size, raw)
+            if status:
+                raise lbt.LbtError(status, "lbt_groupnorm_forward")
+            if keep:
+                self.kept = (x, stats)
 
     def forward(self, x, out=None, keep=False, stream=None):
         """y; keep: the statistics stay for `backward` (until the next forward pass with keep=True), which also needs x unchanged."""
@@ -181,9 +185,10 @@ class GroupNorm:
             grads.append(lbt._at(g, on))
         at, (_, desc, size) = self._plan(("dy", "x", "dx"), (dy, x, out["dx"]), on)
         raw = lbt._current_raw_stream(on)
-        ws = self._workspace(raw, not _capturing(raw), size, dy.device)
         w, b = self._params
-        status = lbt.lib().lbt_groupnorm_backward(desc, at[0], at[1], w, b, stats.data_ptr(), at[2], *grads, ws.data_ptr(), size, raw)
+        with self._lock:
+            ws = self._workspace(raw, not _capturing(raw), size, dy.device)
+            status = lbt.lib().lbt_groupnorm_backward(desc, at[0], at[1], w, b, stats.data_ptr(), at[2], *grads, ws.data_ptr(), size, raw)
         if status:
             raise lbt.LbtError(status, "lbt_groupnorm_backward")
         return out

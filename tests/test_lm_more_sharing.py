@@ -1,0 +1,51 @@
+"""Adapters, group norm and gradient clipping shared by threads, devices and tensors (no GPU): stand-in tensors and devices, the addresses handed to the
+library are never read."""
+import threading
+
+import torch
+
+from paper_2407_12637_b200 import cnn, lbt, lm
+from test_lm_more_host import A, _Devices, _objects, _Tensor
+
+
+def _two_at_once(work):
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(10)
+
+
+class _Calls:
+    """Library calls of a scratch address each: which of them were under way with the same one.  The first one stays until the second has come in, or for 0.3 s."""
+
+    def __init__(self):
+        self.inside, self.overlaps, self.entered = [], [], threading.Event()
+
+    def __call__(self, scratch):
+        self.overlaps.extend(s for s in self.inside if s == scratch)
+        self.inside.append(scratch)
+        if len(self.inside) == 1:
+            self.entered.wait(0.3)
+        else:
+            self.entered.set()
+        self.inside.remove(scratch)
+        return lbt.OK
+
+
+def test_threads_that_share_a_group_norm_take_turns(monkeypatch):
+    """A pass over large images is two launches that meet in the workspace: between the two no other thread's pass may use it."""
+    devices = _Devices(monkeypatch)
+    _, norm, half = _objects(0)
+    x, y, vec = half(2, 3, 16), half(2, 3, 16), _Tensor((16,), torch.float32)
+    calls = _Calls()
+    devices.lbt_groupnorm_forward = lambda *a: calls(a[10])
+    norm.forward(x, out=y)   # (the workspace is there from now on)
+    calls.entered.clear()
+    _two_at_once(lambda: norm.forward(x, out=y))
+    assert not calls.overlaps
+    norm.forward(x, out=y, keep=True)
+    calls = _Calls()
+    devices.lbt_groupnorm_backward = lambda *a: calls(a[9])
+    _two_at_once(lambda: norm.backward(y, dx=x, dw=vec, db=vec))
+    assert not calls.overlaps
