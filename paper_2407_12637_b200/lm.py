@@ -192,6 +192,7 @@ class Adapters:
         self._status = self.status.data_ptr()
         self.kept = None
         self._plans, self._own_kept, self._space = {}, {}, {}   # descriptors by sizes; by stream: h that is kept, workspace of the backward pass
+        self._lock = threading.Lock()   # a backward pass is two launches that meet in the workspace (the library's call lets other threads run)
 
     def check(self):
         """Raises LbtError if a bounded on-chip wait ran out since the last check (waits for the device): see Linear8.check."""
@@ -289,15 +290,17 @@ class Adapters:
         runs, at_offsets, at_index = self._runs(offsets, index)
         M, at, (_, desc, size) = self._plan(("dy", "x", "dbase", "dx"), (dy, x, dbase, dx), (self.O, self.I, self.I, self.I), runs)
         raw = lbt._current_raw_stream(on)
-        held = not _capturing(raw)
-        ws = self._space.get(raw) if held else None
-        if ws is None or ws.numel() < size:
-            ws = torch.empty(size, dtype=torch.uint8, device=dy.device)
-            if held:
-                self._space[raw] = ws
+        at_da, at_db = lbt._at(out["da"], on), lbt._at(out["db"], on)
         a, b, scale = self._weights
-        status = lbt.lib().lbt_adapters_backward(desc, at[0], at[1], h.data_ptr(), a, b, scale, at_offsets, at_index, at[2], at[3], lbt._at(out["da"], on),
-                                                 lbt._at(out["db"], on), lbt.TYPES[kind], self._status, ws.data_ptr(), size, raw)
+        with self._lock:
+            held = not _capturing(raw)
+            ws = self._space.get(raw) if held else None
+            if ws is None or ws.numel() < size:
+                ws = torch.empty(size, dtype=torch.uint8, device=dy.device)
+                if held:
+                    self._space[raw] = ws
+            status = lbt.lib().lbt_adapters_backward(desc, at[0], at[1], h.data_ptr(), a, b, scale, at_offsets, at_index, at[2], at[3], at_da, at_db,
+                                                     lbt.TYPES[kind], self._status, ws.data_ptr(), size, raw)
         if status:
             raise lbt.LbtError(status, "lbt_adapters_backward")
         return out

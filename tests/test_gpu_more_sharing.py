@@ -4,7 +4,7 @@ import threading
 import pytest
 import torch
 
-from paper_2407_12637_b200 import cnn
+from paper_2407_12637_b200 import cnn, lm
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +26,28 @@ def test_two_threads_share_a_group_norm():
         t.join()
     torch.cuda.synchronize()
     assert all(torch.equal(y, want[i]) for i in range(2) for y in got[i])
+
+
+def test_two_threads_share_adapters():
+    """Forward passes without `keep`, and gradients of two dy for one kept pass, on the default stream."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    adapters = lm.Adapters(randn(2, 8, 96), randn(2, 8, 64))
+    offsets, index = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([0, 100, 300], [1, 0]))
+    x, base, dys, xs = randn(300, 96), randn(300, 64), [randn(300, 64) * (i + 1) for i in range(2)], [randn(300, 96) for _ in range(2)]
+    adapters.forward(x, base.clone(), offsets, index, keep=True)
+    passes = [lambda i=i: (adapters.forward(xs[i], base, offsets, index, out=torch.empty_like(base)), *adapters.backward(dys[i], torch.zeros(300, 96, device="cuda")).values())
+              for i in range(2)]
+    want, got = [p() for p in passes], [[], []]
+
+    def work(i):
+        for _ in range(100):
+            got[i].append(passes[i]())
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in range(2) for out in got[i] for a, b in zip(out, want[i]))

@@ -49,3 +49,17 @@ def test_threads_that_share_a_group_norm_take_turns(monkeypatch):
     devices.lbt_groupnorm_backward = lambda *a: calls(a[9])
     _two_at_once(lambda: norm.backward(y, dx=x, dw=vec, db=vec))
     assert not calls.overlaps
+
+
+def test_threads_that_share_adapters_take_turns(monkeypatch):
+    """A backward pass leaves dh in the workspace, from which the weight gradients' launch reads it."""
+    devices = _Devices(monkeypatch)
+    adapters, _, half = _objects(0)
+    x, dy, da, db = half(5, 64), half(5, 32), _Tensor((2, 4, 64), torch.float32), _Tensor((2, 4, 32), torch.float32)
+    adapters.forward(x, half(5, 32), keep=True)
+    calls = _Calls()
+    devices.lbt_adapters_backward = lambda *a: calls(a[15])
+    adapters.backward(dy, half(5, 64), da=da, db=db)
+    calls.entered.clear()
+    _two_at_once(lambda: adapters.backward(dy, half(5, 64), da=da, db=db))
+    assert not calls.overlaps
