@@ -330,7 +330,7 @@ class ResNorm:
         with lbt._place(given[0]) if given else contextlib.nullcontext():   # (the layer's own tensors, whose storage stays)
             self._params = tuple(lbt._at(p) for p in (w_post, b_post, w_pre, b_pre))
         self._plans = {}   # (rows, types, leading dimensions) -> descriptor and its workspace size
-        self._space, self._stats = {}, {}   # stream -> workspace of the backward pass, statistics that were kept
+        self._space, self._stats = {}, {}   # device and stream (0 on each device) -> workspace of the backward pass, statistics that were kept
 
     def _plan(self, names, acts, gate, rows_per_gate, on):
         """Addresses of the activations and the descriptor of a call on tensors of these sizes (checked each time)."""
@@ -375,11 +375,11 @@ class ResNorm:
         raw, stats = lbt._current_raw_stream(on), None
         if keep:   # a buffer for each stream, shared by one forward pass after the other
             held = not _capturing(raw)
-            stats = self._stats.get(raw) if held else None
+            stats = self._stats.get((on, raw)) if held else None
             if stats is None or stats.shape[0] != x.shape[0]:
                 stats = torch.empty(x.shape[0], 4, dtype=torch.float32, device=x.device)
                 if held:
-                    self._stats[raw] = stats
+                    self._stats[on, raw] = stats
         w_post, b_post, w_pre, b_pre = self._params
         status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._at(gate, on) if gate is not None else 0, w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
                                                q.data_ptr() if q is not None else 0, q.shape[1] if q is not None else 0,
@@ -437,11 +437,11 @@ class ResNorm:
         at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate, on)
         raw = lbt._current_raw_stream(on)
         held = not _capturing(raw)
-        ws = self._space.get(raw) if held else None
+        ws = self._space.get((on, raw)) if held else None
         if ws is None or ws.numel() < size:
             ws = torch.empty(size, dtype=torch.uint8, device=x.device)
             if held:
-                self._space[raw] = ws
+                self._space[on, raw] = ws
         w_post, b_post, w_pre, _ = self._params
         status = lbt.lib().lbt_resnorm_backward(desc, at[2], at[3], at[0], at[1], lbt._at(gate, on) if gate is not None else 0, w_post, b_post, w_pre, stats.data_ptr(), at[4], at[5],
                                                 *grads, ws.data_ptr(), size, raw)

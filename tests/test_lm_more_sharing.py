@@ -63,3 +63,25 @@ def test_threads_that_share_adapters_take_turns(monkeypatch):
     calls.entered.clear()
     _two_at_once(lambda: adapters.backward(dy, half(5, 64), da=da, db=db))
     assert not calls.overlaps
+
+
+def test_norms_without_parameters_keep_scratch_for_each_device(monkeypatch):
+    """Such a norm belongs to no device, and the default stream's handle is 0 on every one of them."""
+    devices = _Devices(monkeypatch)
+    monkeypatch.setattr(lbt, "_current_raw_stream", lambda index: 0)
+    seen = {}
+    devices.lbt_groupnorm_forward = lambda *a: seen.setdefault("forward", []).append((a[9], a[10])) or lbt.OK     # (statistics, workspace)
+    devices.lbt_groupnorm_backward = lambda *a: seen.setdefault("backward", []).append((a[5], a[9])) or lbt.OK
+    devices.lbt_resnorm_forward = lambda *a: seen.setdefault("res forward", []).append((a[13],)) or lbt.OK
+    devices.lbt_resnorm_backward = lambda *a: seen.setdefault("res backward", []).append((a[9], a[17])) or lbt.OK
+    norm, res = cnn.GroupNorm(16, 2), lm.ResNorm(32)
+    for index in (0, 1):
+        x, y = (_Tensor((2, 3, 16), torch.bfloat16, index, at) for at in (A, 2 * A))
+        norm.forward(x, out=y, keep=True)
+        norm.backward(y, dx=_Tensor((2, 3, 16), torch.bfloat16, index, 3 * A))
+        x, y, z = (_Tensor((5, 32), torch.bfloat16, index, at) for at in (A, 2 * A, 3 * A))
+        res.forward(x, y, out=(z, z), keep=True)
+        res.backward(z, z, out={"dx": x, "dh": y})
+    assert len(seen) == 4
+    for calls in seen.values():
+        assert len(calls) == 2 and all(a != b for a, b in zip(*calls))
