@@ -119,7 +119,7 @@ class GroupNorm:
         return ws
 
     def _forward(self, x, y, q, bits, clip, scale, keep, on):
-        at, (_, desc, size) = self._plan(("x", "y"), (x, y), on)
+        at, (held_desc, desc, size) = self._plan(("x", "y"), (x, y), on)
         raw, stats = lbt._current_raw_stream(on), None
         held = not _capturing(raw)
         with self._lock:
@@ -183,7 +183,7 @@ class GroupNorm:
             if g.numel() != p.numel() or g.dtype != p.dtype:
                 raise ValueError(f"{name}: {p.numel()} values of {p.dtype}")
             grads.append(lbt._at(g, on))
-        at, (_, desc, size) = self._plan(("dy", "x", "dx"), (dy, x, out["dx"]), on)
+        at, (held_desc, desc, size) = self._plan(("dy", "x", "dx"), (dy, x, out["dx"]), on)
         raw = lbt._current_raw_stream(on)
         w, b = self._params
         with self._lock:

@@ -246,7 +246,7 @@ class Adapters:
             raise ValueError(f"the adapters are on device {self.device}")
         out = base if out is None else out
         runs, at_offsets, at_index = self._runs(offsets, index)
-        M, at, (_, desc, _) = self._plan(("x", "base", "out"), (x, base, out), (self.I, self.O, self.O), runs)
+        M, at, plan = self._plan(("x", "base", "out"), (x, base, out), (self.I, self.O, self.O), runs)   # (holds the descriptor while the library reads it)
         raw, h = lbt._current_raw_stream(on), None
         if keep:   # a buffer for each stream, shared by one forward pass after the other
             held = not _capturing(raw)
@@ -256,7 +256,7 @@ class Adapters:
                 if held:
                     self._own_kept[raw] = h
         a, b, scale = self._weights
-        status = lbt.lib().lbt_adapters_forward(desc, at[0], a, b, scale, at_offsets, at_index, at[1], at[2], h.data_ptr() if keep else 0, self._status, raw)
+        status = lbt.lib().lbt_adapters_forward(plan[1], at[0], a, b, scale, at_offsets, at_index, at[1], at[2], h.data_ptr() if keep else 0, self._status, raw)
         if status:
             raise lbt.LbtError(status, "lbt_adapters_forward")
         if keep:
@@ -288,7 +288,7 @@ class Adapters:
             if out[name].shape != like.shape:
                 raise ValueError(f"{name}: of the shape {tuple(like.shape)}")
         runs, at_offsets, at_index = self._runs(offsets, index)
-        M, at, (_, desc, size) = self._plan(("dy", "x", "dbase", "dx"), (dy, x, dbase, dx), (self.O, self.I, self.I, self.I), runs)
+        M, at, (held_desc, desc, size) = self._plan(("dy", "x", "dbase", "dx"), (dy, x, dbase, dx), (self.O, self.I, self.I, self.I), runs)
         raw = lbt._current_raw_stream(on)
         at_da, at_db = lbt._at(out["da"], on), lbt._at(out["db"], on)
         a, b, scale = self._weights
@@ -371,7 +371,7 @@ class ResNorm:
 
     def _forward(self, x, h, gate, rows_per_gate, r, y, q, q_scale, keep, on):
         names, acts = (("x", "h", "r", "y"), (x, h, r, y)) if y is not None else (("x", "h", "r"), (x, h, r))
-        at, (_, desc, _) = self._plan(names, acts, gate, rows_per_gate, on)
+        at, plan = self._plan(names, acts, gate, rows_per_gate, on)   # (holds the descriptor while the library reads it)
         raw, stats = lbt._current_raw_stream(on), None
         if keep:   # a buffer for each stream, shared by one forward pass after the other
             held = not _capturing(raw)
@@ -381,7 +381,7 @@ class ResNorm:
                 if held:
                     self._stats[on, raw] = stats
         w_post, b_post, w_pre, b_pre = self._params
-        status = lbt.lib().lbt_resnorm_forward(desc, at[0], at[1], lbt._at(gate, on) if gate is not None else 0, w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
+        status = lbt.lib().lbt_resnorm_forward(plan[1], at[0], at[1], lbt._at(gate, on) if gate is not None else 0, w_post, b_post, w_pre, b_pre, at[2], at[3] if y is not None else 0,
                                                q.data_ptr() if q is not None else 0, q.shape[1] if q is not None else 0,
                                                q_scale.data_ptr() if q is not None else 0, stats.data_ptr() if keep else 0, raw)
         if status:
@@ -434,7 +434,7 @@ class ResNorm:
                 grads.append(lbt._at(g, on))
             else:
                 grads.append(0)
-        at, (_, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate, on)
+        at, (held_desc, desc, size) = self._plan(("x", "h", "dr", "dy", "dx", "dh"), (x, h, dr, dy, out["dx"], out["dh"]), gate, rows_per_gate, on)
         raw = lbt._current_raw_stream(on)
         held = not _capturing(raw)
         ws = self._space.get((on, raw)) if held else None

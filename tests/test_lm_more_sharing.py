@@ -1,6 +1,8 @@
 """Adapters, group norm and gradient clipping shared by threads, devices and tensors (no GPU): stand-in tensors and devices, the addresses handed to the
 library are never read."""
+import gc
 import threading
+import weakref
 
 import torch
 
@@ -85,3 +87,32 @@ def test_norms_without_parameters_keep_scratch_for_each_device(monkeypatch):
     assert len(seen) == 4
     for calls in seen.values():
         assert len(calls) == 2 and all(a != b for a, b in zip(*calls))
+
+
+def test_a_descriptor_lives_as_long_as_the_call_that_reads_it(monkeypatch):
+    """The library's call lets other threads run; one of them may clear the plans (256 sizes) while this one's descriptor is read."""
+    devices = _Devices(monkeypatch)
+    adapters, norm, half = _objects(0)
+    res, alive, own = lm.ResNorm(32), [], []
+
+    def call(*args):
+        (plan,) = own[0]._plans.values()
+        descriptor = weakref.ref(plan[0])
+        del plan
+        own[0]._plans.clear()
+        gc.collect()
+        alive.append(descriptor() is not None)
+        return lbt.OK
+
+    for name in ("adapters", "groupnorm", "resnorm"):
+        for way in ("forward", "backward"):
+            setattr(devices, f"lbt_{name}_{way}", call)
+    x, y, z = half(2, 3, 16), half(5, 32), half(5, 64)
+    for obj, passes in ((adapters, (lambda: adapters.forward(z, y, keep=True), lambda: adapters.backward(y, z, da=_Tensor((2, 4, 64), torch.float32), db=_Tensor((2, 4, 32), torch.float32)))),
+                        (norm, (lambda: norm.forward(x, out=x), lambda: norm.forward(x, out=half(2, 3, 16, at=2 * A), keep=True),
+                                lambda: norm.backward(x, dx=x, dw=_Tensor((16,), torch.float32), db=_Tensor((16,), torch.float32)))),
+                        (res, (lambda: res.forward(y, y, out=(y, y), keep=True), lambda: res.backward(y, y, out={"dx": y, "dh": y})))):
+        own[:] = [obj]
+        for work in passes:
+            work()
+    assert len(alive) == 7 and all(alive)
