@@ -401,6 +401,11 @@ def _place(t, stream=None):
     return torch.cuda.stream(stream)
 
 
+def _in_place_of(out, t) -> bool:
+    """Whether `out` begins where `t` does (itself, or another tensor on the same memory), so that writing the one overwrites the other."""
+    return out is t or (isinstance(t, torch.Tensor) and t.numel() > 0 and out.data_ptr() == t.data_ptr())
+
+
 def _raw_stream(t, stream=None) -> int:
     """The stream a call on `t` goes to: the one given, else torch's current stream.  The library launches on the current device,
     so that has to be t's: the default streams of all devices share one handle."""

@@ -237,7 +237,7 @@ class Adapters:
 
     def forward(self, x, base, offsets=None, index=None, out=None, keep=False, stream=None):
         """out for x [M, I] and base [M, O] (the layer's output; out None: added in place).  keep: x, the runs and h stay for `backward`,
-        until the next forward pass with keep=True."""
+        until the next forward pass with keep=True; x is then not overwritten by out."""
         on = x.get_device()
         if stream is not None or on != lbt._device():
             with lbt._place(x, stream):
@@ -245,6 +245,8 @@ class Adapters:
         if on != self.device:
             raise ValueError(f"the adapters are on device {self.device}")
         out = base if out is None else out
+        if keep and lbt._in_place_of(out, x):
+            raise ValueError("out in the place of x, which backward reads")
         runs, at_offsets, at_index = self._runs(offsets, index)
         M, at, plan = self._plan(("x", "base", "out"), (x, base, out), (self.I, self.O, self.O), runs)   # (holds the descriptor while the library reads it)
         raw, h = lbt._current_raw_stream(on), None

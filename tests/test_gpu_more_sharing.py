@@ -51,3 +51,17 @@ def test_two_threads_share_adapters():
         t.join()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for i in range(2) for out in got[i] for a, b in zip(out, want[i]))
+
+
+def test_adapters_out_in_the_place_of_x():
+    """Refused where backward reads x, whatever tensor lies there; without `keep` the same as elsewhere."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    for M, I, dtype in ((5, 64, torch.float32), (300, 96, torch.bfloat16), (300, 63, torch.bfloat16), (700, 128, torch.float16)):
+        adapters, x, base = lm.Adapters(randn(1, 8, I).to(dtype), randn(1, 8, I).to(dtype)), randn(M, I).to(dtype), randn(M, I).to(dtype)
+        want, before = adapters.forward(x, base, out=torch.empty_like(x)), x.clone()
+        for bad in (lambda: adapters.forward(x, base, out=x, keep=True), lambda: adapters.forward(x, base, out=x.view(M, I), keep=True), lambda: adapters.forward(x, x[:], keep=True)):
+            with pytest.raises(ValueError):
+                bad()
+        assert torch.equal(x, before) and adapters.kept is None
+        assert torch.equal(adapters.forward(x, base, out=x), want)

@@ -4,6 +4,7 @@ import gc
 import threading
 import weakref
 
+import pytest
 import torch
 
 from paper_2407_12637_b200 import cnn, lbt, lm
@@ -116,3 +117,16 @@ def test_a_descriptor_lives_as_long_as_the_call_that_reads_it(monkeypatch):
         for work in passes:
             work()
     assert len(alive) == 7 and all(alive)
+
+
+def test_adapters_keep_no_x_that_is_overwritten(monkeypatch):
+    devices = _Devices(monkeypatch)
+    half = lambda *s: _Tensor(s, torch.bfloat16)  # noqa: E731
+    adapters = lm.Adapters(half(2, 4, 64), half(2, 4, 64))
+    x, base = half(5, 64), half(5, 64)
+    for bad in (lambda: adapters.forward(x, base, out=x, keep=True), lambda: adapters.forward(x, x, keep=True)):
+        with pytest.raises(ValueError):
+            bad()
+    assert not devices.calls and adapters.kept is None
+    adapters.forward(x, base, out=x)   # (without a backward pass x may go)
+    assert len(devices.calls) == 1
