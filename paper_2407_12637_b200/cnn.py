@@ -119,6 +119,8 @@ class GroupNorm:
         return ws
 
     def _forward(self, x, y, q, bits, clip, scale, keep, on):
+        if keep and y is not None and lbt._in_place_of(y, x):
+            raise ValueError("out in the place of x, which backward reads")
         at, (held_desc, desc, size) = self._plan(("x", "y"), (x, y), on)
         raw, stats = lbt._current_raw_stream(on), None
         held = not _capturing(raw)
@@ -140,7 +142,8 @@ class GroupNorm:
                 self.kept = (x, stats)
 
     def forward(self, x, out=None, keep=False, stream=None):
-        """y; keep: the statistics stay for `backward` (until the next forward pass with keep=True), which also needs x unchanged."""
+        """y; keep: the statistics stay for `backward` (until the next forward pass with keep=True), which also needs x unchanged: out is then
+        not in its place."""
         on = x.get_device()
         if stream is not None or on != lbt._device():
             with lbt._place(x, stream):   # outputs and scratch belong to the stream that uses them

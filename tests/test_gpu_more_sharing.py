@@ -65,3 +65,20 @@ def test_adapters_out_in_the_place_of_x():
                 bad()
         assert torch.equal(x, before) and adapters.kept is None
         assert torch.equal(adapters.forward(x, base, out=x), want)
+
+
+def test_group_norm_out_in_the_place_of_x():
+    for shape in ((2, 9, 16), (2, 40000, 24)):
+        x, clip = torch.randn(*shape, device="cuda"), torch.ones(1, device="cuda")
+        norm = cnn.GroupNorm(shape[-1], 2)
+        want, before = norm.forward(x), x.clone()
+        for bad in (lambda: norm.forward(x, out=x, keep=True), lambda: norm.forward(x, out=x[:], keep=True), lambda: norm.forward_codes(x, clip, out=x, keep=True)):
+            with pytest.raises(ValueError):
+                bad()
+        assert torch.equal(x, before) and norm.kept is None
+        norm.forward(x, out=torch.empty_like(x), keep=True)
+        q, s = norm.forward_codes(x, clip)
+        assert torch.equal(norm.forward(x, out=x), want)
+        x.copy_(before)
+        got = norm.forward_codes(x, clip, out=x)
+        assert torch.equal(x, want) and torch.equal(got[0], q) and torch.equal(got[1], s)

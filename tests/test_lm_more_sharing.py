@@ -130,3 +130,15 @@ def test_adapters_keep_no_x_that_is_overwritten(monkeypatch):
     assert not devices.calls and adapters.kept is None
     adapters.forward(x, base, out=x)   # (without a backward pass x may go)
     assert len(devices.calls) == 1
+
+
+def test_a_group_norm_keeps_no_x_that_is_overwritten(monkeypatch):
+    devices = _Devices(monkeypatch)
+    x, clip = _Tensor((2, 3, 16), torch.float32), _Tensor((1,), torch.float32)
+    norm = cnn.GroupNorm(16, 2)
+    for bad in (lambda: norm.forward(x, out=x, keep=True), lambda: norm.forward_codes(x, clip, out=x, keep=True)):
+        with pytest.raises(ValueError):
+            bad()
+    assert not devices.calls and norm.kept is None
+    norm.forward(x, out=x)   # (without a backward pass x may go)
+    assert len(devices.calls) == 1
