@@ -483,7 +483,7 @@ lbt_status lbt_adamw_step_ex(const lbt_adamw_tensor *tensors, int count, const l
  * out (device, 4-byte aligned): `reserved` is 0 before the first call and between calls; a struct belongs to one call at a time.
  * ws: lbt_grad_norm_workspace_bytes(tensors, count) bytes, 8-byte aligned.
  * lbt_grad_clip: out_i = g_i * norm->scale in fp32, rounded to out's type once, for every tensor of the table; skip != 0: nothing is
- * written.  out may be g (then a scale of 1 writes nothing) and may have another type where it is not.
+ * written.  out may be g (then a scale of 1 writes nothing) and may have another type where it is not; it overlaps no other tensor of the table.
  * `tensors` (HOST) is read during the call.  Tensors need their element type's alignment; 32 bytes (fp32) and 16 (16-bit types) are
  * read in wide accesses.  n = 0 and count = 0 are valid (the norm of nothing is 0).
  */

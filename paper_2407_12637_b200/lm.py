@@ -458,8 +458,8 @@ class GradClip:
     `measure` leaves `norm`, `scale` = min(1, max_norm / norm), `skip` (1: a gradient is not finite) and each tensor's norm in `norms`,
     all on the device; scale and skip go to AdamW.step(grad_scale=clip.scale, skip=clip.skip), which then needs no pass over the
     gradients more than it makes anyway.  `clip` also writes the clipped gradients, for an optimizer that takes them as they are: into
-    `out` (tensors of the gradients' sizes, of any type), by default in place; with skip set it writes nothing.  An object is used
-    by one thread and one stream at a time."""
+    `out` (tensors of the gradients' sizes, of any type), by default in place; with skip set it writes nothing.  Outputs overlap neither
+    each other nor the other gradients.  An object is used by one thread and one stream at a time."""
 
     def __init__(self, grads, max_norm=float("inf"), out=None):
         n = len(grads)
@@ -479,9 +479,18 @@ class GradClip:
             e.n, e.g_type, e.out_type = g.numel(), lbt.TYPES[g.dtype], lbt.TYPES[o.dtype]
             if e.n and e.g == e.out and g.dtype != o.dtype:
                 raise ValueError("an output in its gradient's place has its type")
-        places = [e.out for e in self.table if e.n]
-        if len(set(places)) != len(places):
-            raise ValueError("every tensor once: a gradient given twice would be clipped twice")
+        spans = []   # first byte, end, whether it is written
+        size = lambda kind: 4 if kind == lbt.F32 else 2  # noqa: E731
+        for e in self.table:
+            if e.n:
+                spans.append((e.out, e.out + e.n * size(e.out_type), True))
+                if e.g != e.out:
+                    spans.append((e.g, e.g + e.n * size(e.g_type), False))
+        end, end_written = 0, 0   # of the spans so far
+        for first, last, written in sorted(spans):
+            if first < (end if written else end_written):
+                raise ValueError("an output lies in its gradient's place or apart from all others: a gradient given twice would be clipped twice, another's might be read after it was written")
+            end, end_written = max(end, last), max(end_written, last) if written else end_written
         where = self.grads[0].device if n else "cpu"
         self._result = torch.zeros(4, dtype=torch.int32, device=where)
         parts = self._result.view(torch.float32)

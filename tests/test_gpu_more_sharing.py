@@ -82,3 +82,17 @@ def test_group_norm_out_in_the_place_of_x():
         x.copy_(before)
         got = norm.forward_codes(x, clip, out=x)
         assert torch.equal(x, want) and torch.equal(got[0], q) and torch.equal(got[1], s)
+
+
+def test_clipped_outputs_lie_apart():
+    """Outputs in other gradients' places are refused; in flat storage side by side, in place or elsewhere, they hold what each alone would."""
+    flat, other = torch.randn(300, device="cuda"), torch.zeros(300, device="cuda")
+    cut = lambda t: [t[0:100], t[100:101], t[101:300]]  # noqa: E731
+    before = flat.clone()
+    for out in ([flat[1:101], other[100:101], other[101:300]], [other[0:100], flat[0:1], other[101:300]], [other[0:100], other[99:100], other[101:300]]):
+        with pytest.raises(ValueError):
+            lm.GradClip(cut(flat), 1.0, out=out)
+    for out in (cut(other), cut(flat)):
+        lm.GradClip(cut(flat), 1.0, out=out).clip()
+    want = before * (1.0 / before.double().norm()).float()
+    assert torch.equal(other, flat) and ((other - want).abs() <= 2.0 ** -22 * want.abs()).all()

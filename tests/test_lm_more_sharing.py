@@ -142,3 +142,23 @@ def test_a_group_norm_keeps_no_x_that_is_overwritten(monkeypatch):
     assert not devices.calls and norm.kept is None
     norm.forward(x, out=x)   # (without a backward pass x may go)
     assert len(devices.calls) == 1
+
+
+def test_outputs_of_a_clip_lie_apart():
+    """In their own gradient's place or nowhere near another tensor: the order in which tensors are read and written is the device's."""
+    def clip(grads, out=None):   # (tensors as first byte, elements, type)
+        make = lambda spans: [_Tensor((n,), dtype, 0, A + at) for at, n, dtype in spans]  # noqa: E731
+        return lm.GradClip(make(grads), 1.0, make(out) if out is not None else None)
+
+    f, h = torch.float32, torch.bfloat16
+    two = [(0, 64, f), (256, 64, f)]
+    with pytest.MonkeyPatch.context() as patch:
+        _Devices(patch)
+        patch.setattr(lbt, "_at", lambda t, device=None: t.data_ptr())   # (an object's own result is on the host here)
+        for grads, out in ((two, [(256, 64, f), (0, 64, f)]), (two, [(256, 64, f), (512, 64, f)]), (two, [(1024, 64, f), (1200, 64, f)]), (two, [(0, 64, f), (508, 64, f)]),
+                           (two, [(4, 64, f), (512, 64, f)]), (two, [(1024, 64, f), (128, 64, h)]), ([(0, 64, f), (252, 64, f)], None), ([(0, 64, f), (0, 8, h)], None)):
+            with pytest.raises(ValueError):
+                clip(grads, out)
+        for grads, out in ((two, None), (two, two), (two, [(0, 64, f), (512, 64, h)]), (two, [(512, 64, f), (768, 64, f)]), ([two[0]] * 2, [(512, 64, f), (768, 64, f)]),
+                           (two + [(0, 0, f)], None), (two, [(768, 64, h), (896, 64, h)]), ([(0, 64, f), (4, 0, f)], None)):
+            clip(grads, out)
