@@ -538,7 +538,7 @@ lbt_status lbt_adapters_backward(const lbt_adapters_desc *d, const void *dy, con
  * for each image and each group of C / G neighbouring channels, mean and (biased) variance over the group's P C / G values,
  *   k = (x - mean) rstd, rstd = (var + eps)^(-1/2);  z = k w + b;  y = act(z): z, max(z, 0) or z / (1 + exp(-z)).
  * w, b: [C] of param_type (NULL: ones, zeros).  y or q may be NULL.  q: what lbt_quantize_act makes of the fp32 y with `bits` and d_clip
- * (dense, the storage of this header's codes: what lbt_qconv_forward takes), d_scale_out: its scale; needs C a multiple of 8 and aligned rows.
+ * (dense, the storage of this header's codes: what lbt_qconv_forward takes), d_scale_out: its scale (of no images too); needs C a multiple of 8 and aligned rows.
  * stats (may be NULL): [N,G,2] floats, 8-byte aligned, mean and rstd, kept for the backward pass.  ws: lbt_groupnorm_workspace_bytes(d), 8-byte aligned.
  * No sum crosses images.  Sums are fp32 (of differences from a value of the channel) in an order fixed by the sizes.  y may be x.
  */

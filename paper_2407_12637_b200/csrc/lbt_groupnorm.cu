@@ -1269,7 +1269,8 @@ extern "C" lbt_status lbt_groupnorm_forward(const lbt_groupnorm_desc* desc, cons
         return LBT_ERR_ALIGNMENT;
     const int vec = gn_vec(d, {{x, d.ld_x}, {y, d.ld_y}});
     if (q != nullptr && vec != 8) return d.C % 8 != 0 ? LBT_ERR_UNSUPPORTED : LBT_ERR_ALIGNMENT;
-    if (d.N == 0) return LBT_OK;
+    if (d.N == 0)   // (the codes of nothing have a scale all the same)
+        return d_clip != nullptr && d_scale_out != nullptr ? lbt_quantize_act(nullptr, 0, d_clip, bits, nullptr, d_scale_out, cuda_stream) : LBT_OK;
     if (x == nullptr) return LBT_ERR_INVALID_ARG;
     if (ws == nullptr || ws_bytes < lbt_groupnorm_workspace_bytes(desc)) return LBT_ERR_WORKSPACE;
     GroupNormArgs g{};

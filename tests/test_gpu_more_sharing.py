@@ -4,7 +4,7 @@ import threading
 import pytest
 import torch
 
-from paper_2407_12637_b200 import cnn, lm
+from paper_2407_12637_b200 import cnn, lbt, lm
 
 pytestmark = pytest.mark.gpu
 
@@ -96,3 +96,13 @@ def test_clipped_outputs_lie_apart():
         lm.GradClip(cut(flat), 1.0, out=out).clip()
     want = before * (1.0 / before.double().norm()).float()
     assert torch.equal(other, flat) and ((other - want).abs() <= 2.0 ** -22 * want.abs()).all()
+
+
+@pytest.mark.parametrize("clip", [1.5, 0.0])
+def test_codes_of_no_images(clip):
+    c, x, want = torch.tensor([clip], device="cuda"), torch.empty(0, 5, 16, device="cuda"), torch.empty(1, device="cuda")
+    used = torch.full((1,), 7.0, device="cuda")   # (what the next allocation of that size may find)
+    del used
+    q, scale = cnn.GroupNorm(16, 2).forward_codes(x, c, bits=4)
+    lbt.quantize_act(x, c, 4, torch.empty_like(q), want)
+    assert q.numel() == 0 and torch.equal(scale, want) and float(want) == torch.tensor(clip / 15).float()

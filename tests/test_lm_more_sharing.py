@@ -1,5 +1,6 @@
 """Adapters, group norm and gradient clipping shared by threads, devices and tensors (no GPU): stand-in tensors and devices, the addresses handed to the
 library are never read."""
+import ctypes as C
 import gc
 import threading
 import weakref
@@ -162,3 +163,11 @@ def test_outputs_of_a_clip_lie_apart():
         for grads, out in ((two, None), (two, two), (two, [(0, 64, f), (512, 64, h)]), (two, [(512, 64, f), (768, 64, f)]), ([two[0]] * 2, [(512, 64, f), (768, 64, f)]),
                            (two + [(0, 0, f)], None), (two, [(768, 64, h), (896, 64, h)]), ([(0, 64, f), (4, 0, f)], None)):
             clip(grads, out)
+
+
+def test_the_scale_of_no_images():
+    """q is then an empty tensor, whose address is 0: the scale is asked for all the same, by the quantizer's rules."""
+    d = lbt.GroupnormDesc(0, 10, 24, 3, lbt.F32, lbt.F32, lbt.ACT_RELU, 1e-5)
+    call = lambda **k: lbt.lib().lbt_groupnorm_forward(C.addressof(d), *{**dict(x=None, w=A, b=A, y=None, q=None, bits=4, clip=A, scale=A, stats=None, ws=A, ws_bytes=1 << 20), **k}.values(), None)  # noqa: E731
+    assert call(bits=9) == call(bits=1) == lbt.ERR_UNSUPPORTED_BITS and call(scale=A + 2) == lbt.ERR_ALIGNMENT
+    assert call(clip=None, scale=None) == lbt.OK
