@@ -5,7 +5,8 @@
 // 64 ranks; its CTAs take 64 tokens at a time in turn, z's rows and f's through a ring of stages in shared memory.  The warps of a CTA
 // share a stage's tokens and columns.  16-bit z enters the matrix instructions as it is, pairs of its rows joined; f is split into three
 // bf16 or two fp16 numbers (24 or 22 bits: the gradients are fp32).  fp32 z and f are split into two tf32 numbers each.  fp16 holds no
-// more than 65504: there f enters times a power of two that brings the largest value of the CTA's tokens to [512, 1024).
+// more than 65504: there f enters times a power of two that brings the largest finite value of the CTA's tokens to [512, 1024) (an infinity or
+// NaN spoils its own rank's gradient alone).
 // (The tensor core's own sums are cut off, not rounded: those of four stages at most are added up in fp32.)
 // 8192 tokens, 4096 and 4096 columns, bf16, rank 16: 41 us for both gradients (56 with cold caches; reading x and dy takes 20): issue slots are
 // 0.46 busy with joining rows, splitting f and the ring, and the two kernels' data meet in L2 only in part.
@@ -127,7 +128,10 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapter_grad_kernel(const __gri
             produce(tokens, 0);
             __syncthreads();
             const int n = have[0] * ranks;
-            for (int i = threadIdx.x; i < n; i += kAdThreads) most = max(most, abs_bits(f[(int64_t)ids[0][i / ranks] * g.rank + i % ranks]));
+            for (int i = threadIdx.x; i < n; i += kAdThreads) {
+                const uint32_t v = abs_bits(f[(int64_t)ids[0][i / ranks] * g.rank + i % ranks]);
+                if (v < kNonFinite) most = max(most, v);
+            }
             __syncthreads();
             if (n == 0) break;
         }
