@@ -472,20 +472,19 @@ class GradClip:
         if n and self.device < 0:
             raise ValueError("gradients are CUDA tensors")
         self.table = (lbt.GradTensor * n)()
-        for e, g, o in zip(self.table, self.grads, self.out):
-            if g.dtype not in lbt.TYPES or o.dtype not in lbt.TYPES or g.numel() != o.numel():
-                raise ValueError("gradients and outputs: fp32, bf16 or fp16, of equal sizes")
-            e.g, e.out = lbt._at(g, self.device), lbt._at(o, self.device)
-            e.n, e.g_type, e.out_type = g.numel(), lbt.TYPES[g.dtype], lbt.TYPES[o.dtype]
-            if e.n and e.g == e.out and g.dtype != o.dtype:
-                raise ValueError("an output in its gradient's place has its type")
         spans = []   # first byte, end, whether it is written
-        size = lambda kind: 4 if kind == lbt.F32 else 2  # noqa: E731
-        for e in self.table:
-            if e.n:
-                spans.append((e.out, e.out + e.n * size(e.out_type), True))
-                if e.g != e.out:
-                    spans.append((e.g, e.g + e.n * size(e.g_type), False))
+        for e, g, o in zip(self.table, self.grads, self.out):
+            kind, count, at = lbt.TYPES.get(g.dtype), g.numel(), lbt._at(g, self.device)
+            to_kind, to = (kind, at) if o is g else (lbt.TYPES.get(o.dtype), lbt._at(o, self.device))
+            if kind is None or to_kind is None or (o is not g and count != o.numel()):
+                raise ValueError("gradients and outputs: fp32, bf16 or fp16, of equal sizes")
+            e.g, e.out, e.n, e.g_type, e.out_type = at, to, count, kind, to_kind
+            if count:
+                if at == to and kind != to_kind:
+                    raise ValueError("an output in its gradient's place has its type")
+                spans.append((to, to + (count << 2 if to_kind == lbt.F32 else count << 1), True))
+                if at != to:
+                    spans.append((at, at + (count << 2 if kind == lbt.F32 else count << 1), False))
         end, end_written = 0, 0   # of the spans so far
         for first, last, written in sorted(spans):
             if first < (end if written else end_written):
