@@ -40,11 +40,11 @@ def _check(x, G, n, q=0):
         assert (err <= tol).all(), (float(err.max()), float((err / tol).max()))
 
 
-def _image(N, P, C, dtype, first, mean):
+def _image(N, P, C, dtype, first, mean, std=1.0):
     g = torch.Generator(device="cuda").manual_seed(P)
     x = torch.empty(N, P, C, dtype=dtype, device="cuda")
     for image in x:
-        image.copy_(torch.randn(P, C, generator=g, device="cuda") + mean)
+        image.copy_(torch.randn(P, C, generator=g, device="cuda") * std + mean)
     x[:, 0] = first
     return x
 
@@ -65,3 +65,11 @@ def test_images_read_twice(shape, G, dtype, first, mean):
 def test_images_kept_on_chip(dtype, C, G, first, mean):
     """As large as a cluster keeps: 110 KB a CTA, up to 27 pixels a thread by eights, 55 by twos, 110 one by one."""
     _check(_image(3, 10000, C, dtype, first, mean), G, *{64: (27, 7), 66: (55, 14), 65: (110, 28)}[C])
+
+
+@pytest.mark.parametrize("shape,G,n", [((3, 10000, 64), 8, (27, 7)), ((3, 10000, 66), 11, (55, 14)), ((3, 10000, 65), 5, (110, 28)), ((40, 2001, 2049), 683, (2001, 0))])
+@pytest.mark.parametrize("dtype,std", [(torch.bfloat16, 8.0), (torch.float16, 1.0)], ids=str)
+def test_a_mean_far_from_zero(dtype, std, shape, G, n):
+    """2000 +- 1 (+- 8, a step of bf16): the mean of the squares less the square of the mean, in fp32, is off by 1.7 times the tolerance and more here (sums of
+    25 values, then of 400 such), or negative."""
+    _check(_image(*shape, dtype, 2000.0, 2000.0, std), G, *n)
