@@ -511,7 +511,8 @@ lbt_status lbt_grad_clip(const lbt_grad_tensor *tensors, int count, const lbt_gr
  * of all M tokens with adapter 0.  An index outside [0, adapters) is a run without an adapter: out = base.  Rows of no run (ahead of
  * offsets[0], from offsets[runs] on) are not written; offsets are cut to [0, M].  out may be base.
  * h (may be NULL): [M, rank] floats, kept for the backward pass (rows without an adapter are not written).
- * Sums are fp32 in an order fixed by the sizes; h enters its second product with 16 (bf16) or 22 bits.  rank <= 128.  dev_status (device int32,
+ * Sums are fp32 in an order fixed by the sizes; h enters its second product with 16 (bf16) or 22 bits.  rank <= 128, adapters <= 65535, M and
+ * runs <= 2^28, I and O <= 2^30 (LBT_ERR_UNSUPPORTED above).  dev_status (device int32,
  * may be NULL) receives LBT_ERR_TIMEOUT if a bounded on-chip wait ran out: out (dx) and h are then not complete, nor is what is formed from them.
  */
 typedef struct lbt_adapters_desc {   /* HOST struct */
@@ -540,7 +541,8 @@ lbt_status lbt_adapters_backward(const lbt_adapters_desc *d, const void *dy, con
  * w, b: [C] of param_type (NULL: ones, zeros).  y or q may be NULL.  q: what lbt_quantize_act makes of the fp32 y with `bits` and d_clip
  * (dense, the storage of this header's codes: what lbt_qconv_forward takes), d_scale_out: its scale (of no images too); needs C a multiple of 8 and aligned rows.
  * stats (may be NULL): [N,G,2] floats, 8-byte aligned, mean and rstd, kept for the backward pass.  ws: lbt_groupnorm_workspace_bytes(d), 8-byte aligned.
- * No sum crosses images.  Sums are fp32 (of differences from a value of the channel) in an order fixed by the sizes.  y may be x.
+ * N <= 65534, P <= 2^30, C <= 2^20 (LBT_ERR_UNSUPPORTED above).  No sum crosses images.  Sums are fp32 (of differences from a mean or a value of the channel) in an order fixed by the sizes.  y may be x (which
+ * the backward pass reads, though).
  */
 enum { LBT_ACT_NONE = 0, LBT_ACT_RELU = 1, LBT_ACT_SILU = 2 };
 typedef struct lbt_groupnorm_desc {   /* HOST struct */

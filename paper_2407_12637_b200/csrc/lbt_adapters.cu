@@ -422,8 +422,8 @@ static lbt_status adapter_launch(AdapterArgs g, cudaStream_t stream) {
     const int64_t runs = g.offsets == nullptr ? 1 : g.runs;
     constexpr int kR = 8 * kN;
     // 16 tokens a tile where runs are short on average, or where such tiles are few: a tile of 128 takes the time of its steps one after the
-    // other, whatever its number.  4096 -> 4096, 16 against 128 tokens a tile on the tensor cores' own memory: rank 16 with 1024 tokens 12 against
-    // 14 us, 2048 tokens 17 against 16; rank 32 with 1024 tokens 15 against 15; rank 64 with 128 tokens 13 against 15, 256 tokens 16 against 15;
+    // other, whatever its number.  (Both sides were timed at the widths below alone.)
+    // 4096 -> 4096, 16 against 128 tokens a tile on the tensor cores' own memory: rank 16 with 1024 tokens 12 against 14 us, 2048 tokens 17 against 16; rank 32 with 1024 tokens 15 against 15; rank 64 with 128 tokens 13 against 15, 256 tokens 16 against 15;
     // rank 128 with 128 tokens 19 against 20; 2048 tokens in runs of 96: rank 16 17 against 34, rank 64 31 against 36, rank 128 60 against
     // 45, in runs of 192: 17 against 17, 31 against 19, 60 against 24.  On the other kernel, 1023 -> 2047 bf16: rank 13 with 2048 tokens 18 against
     // 21, 8192 tokens 49 against 38, in runs of 64 49 against 68, of 256 49 against 50; rank 64 28 against 36, 91 against 76, 92 against 147, 91 against

@@ -11,14 +11,14 @@
 // contiguous (MN-major).  Its sums go to one of two accumulators; four warps each add them to base's stage, in place, and store whole 128 bytes of a row.
 // Roles: a thread for each side's copies, one that issues products, two times four warps of the epilogue; all warps add up h.
 //
-// 4096 -> 4096, bf16, against fragments in registers: 8192 tokens, rank 16 43 us (45), rank 64 44 (84), rank 128 60 (127); 2085 tokens in 11
-// runs, rank 64 20 (37); 16384 tokens, rank 16 78 (79): 5.2 TB/s of the 6.6 that a copy reaches.  What is left is the time in which nothing
+// 4096 -> 4096, bf16, replayed on the same inputs, against fragments in registers: 8192 tokens, rank 16 43 us (45), rank 64 43 (84), rank 128 59 (127), with
+// nothing of them in L2 beforehand 50, 51 and 65; 2085 tokens in 11 runs, rank 64 20 (37); 16384 tokens, rank 16 78 (79): 5.2 TB/s of the 6.6 that a copy reaches.  What is left is the time in which nothing
 // streams: 13000 clocks a tile (start 2000, first columns 3000, h through the cluster 6000, the last columns 2000).
 // One thread's instructions are what the products wait for: descriptors are made once a stage and stepped by constants (rank 64: 48 -> 44 us).
 // Tiles of fewer tokens, so that clusters of two fill all SMs, gained nothing (8192 tokens: 43).
 //
-// Every wait on a barrier is bounded: where one runs out, the status word says so, no CTA of the cluster goes on to the second product, what is
-// in flight is waited for, and the kernel ends.
+// Every wait on a barrier is bounded: where one runs out, the status word says so, what is in flight is waited for, and the kernel ends.  In the first
+// product no CTA of the cluster goes on to the second one; in the second one the warps that waited store nothing more.
 #include <algorithm>
 #include <atomic>
 #include <mutex>

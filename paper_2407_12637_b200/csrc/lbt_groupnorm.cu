@@ -773,8 +773,8 @@ struct ImageSpace {
     }
 };
 
-// One cluster an image.  Forward pass, against two kernels: 64 x 56 x 56 x 64 bf16 with SiLU 20 us against 26, 16 x 96 x 96 x 64 fp16 18 against
-// 34 (without an activation 14: issuing the sigmoids' instructions takes the rest), 8 x 28 x 28 x 91 bf16 9.5 against 16.  What is left is read
+// One cluster an image.  Forward pass, against two kernels, inputs in L2: 64 x 56 x 56 x 64 bf16 with SiLU 21 us against 26 (27 from memory), 16 x 96 x 96 x 64
+// fp16 18 against 34 (24 from memory; without an activation 14: issuing the sigmoids' instructions takes the rest), 8 x 28 x 28 x 91 bf16 9 against 16.  What is left is read
 // (5500 clocks of 23000), sums through the cluster (6000) and written (7500) one after the other: an image's sums need all of it.
 // Two fp32 operations an instruction, and one reciprocal for two sigmoids, gained nothing.
 template <typename T, int kVec, int kAct, bool kCodes, int kThreads>
@@ -929,7 +929,7 @@ __device__ __forceinline__ Vals<kVec> slopes(Vals<kVec> e, const Vals<kVec>& k, 
     return e;
 }
 
-// Its gradients (64 x 56 x 56 x 64 bf16 with SiLU: 37 us against 49 of two kernels; the sigmoids are formed twice): x and dy are kept; partial: [N, C] sums of e and e k for the parameters' gradients.
+// Its gradients (64 x 56 x 56 x 64 bf16 with SiLU, inputs in L2: 37 us against 49 of two kernels, 47 from memory; the sigmoids are formed twice): x and dy are kept; partial: [N, C] sums of e and e k for the parameters' gradients.
 template <typename T, int kVec, int kAct, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 2) groupnorm_image_grad_kernel(const __grid_constant__ GroupNormArgs g) {
     extern __shared__ __align__(16) uint8_t image[];

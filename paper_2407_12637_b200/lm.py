@@ -453,7 +453,8 @@ class ResNorm:
 
 
 class GradClip:
-    """The norm of all gradients in `grads` (fixed storage), and clipping to `max_norm` by it.
+    """The norm of all gradients in `grads` (fixed storage, read where it lay when the object was made: gradients that are allocated anew
+    need a new object), and clipping to `max_norm` by it.
 
     `measure` leaves `norm`, `scale` = min(1, max_norm / norm), `skip` (1: a gradient is not finite) and each tensor's norm in `norms`,
     all on the device; scale and skip go to AdamW.step(grad_scale=clip.scale, skip=clip.skip), which then needs no pass over the
