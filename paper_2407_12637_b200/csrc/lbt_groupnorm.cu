@@ -790,10 +790,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_ker
     const int64_t step = cover.lanes * g.ld_x;
     fetch_parts(count, [&](int k) { kept.fetch(k, x + k * step); });
     load_params<kThreads>(g, 0, g.C, space.params);
-    // 16-bit values: sums of differences and of their squares while the pixels come, around a thread's first value for a quarter of its packs, then
-    // around the mean of that quarter: at most 28 single values (3 x 28^2 2^-24 = 2^-13 of the variance lost, see time_to_move), 14 pairs or 7 packs of
-    // eight (2^-17).  Moving more often gained no digit that 16 bits show and cost 5 % (16 x 96 x 96 x 64 fp16) to 9 % (31 x 4001 x 66 bf16); this
-    // costs 0.5 and 1.5 %.  The squares are then moved to the CTA's mean.  fp32 values are read again around the CTA's mean.
+    // 16-bit values: sums of differences and of their squares while the pixels come, around a thread's first value.  Of packs of eight a thread has 27
+    // at most; of pairs and single values (55, 110), the sums go on around the mean of the first quarter.  So at most 28 values stand around one of
+    // them, which loses 3 x 28^2 2^-24 = 2^-13 of the variance (see time_to_move), half of that in rstd: below what 16 bits show.  Moving packs of
+    // eight as well costs 3 % (16 x 96 x 96 x 64 fp16: 21.4 -> 22.0 us a call), moving pairs more often 9 % (31 x 4001 x 66 bf16; once: 1.5 %).  The squares are
+    // then moved to the CTA's mean.  fp32 values are read again around the CTA's mean.
     constexpr bool kOnce = sizeof(T) == 2;
     Vals<kVec> s1 = all<kVec>(0.0f), s2 = all<kVec>(0.0f), first = all<kVec>(0.0f);
     const float own = (float)count, each = count > 0 ? 1.0f / own : 0.0f;
@@ -808,7 +809,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) groupnorm_image_ker
             s1 = add(s1, v);
         }
     }, [&](int k) {
-        if constexpr (kOnce) {
+        if constexpr (kOnce && kVec < 8) {
             const float each = __fdividef(1.0f, (float)max(k, 1));   // (2^-22: what it leaves of s1 weighs its square)
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {   // (`first` is minus the value)
