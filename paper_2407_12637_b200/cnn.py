@@ -79,7 +79,7 @@ class GroupNorm:
                 self._params = (lbt._at(weight), lbt._at(bias))
         else:
             self._params = (0, 0)
-        self._plans, self._stats, self._space = {}, {}, {}   # descriptors by sizes; by device and stream (0 on each device): statistics that are kept, workspace
+        self._plans, self._stats, self._space = {}, {}, {}   # descriptors by sizes; by stream (without parameters by device and stream: the default one is 0 on each): statistics that are kept, workspace
         self._lock = threading.Lock()   # a pass is two launches that meet in the workspace (the library's call lets other threads run)
 
     def _plan(self, names, acts, on):
@@ -119,22 +119,22 @@ class GroupNorm:
         return ws
 
     def _forward(self, x, y, q, bits, clip, scale, keep, on):
-        if keep and y is not None and lbt._in_place_of(y, x):
-            raise ValueError("out in the place of x, which backward reads")
         at, (held_desc, desc, size) = self._plan(("x", "y"), (x, y), on)
+        if keep and at[0] == at[1] and lbt._in_place_of(y, x):
+            raise ValueError("out in the place of x, which backward reads")
         raw, stats = lbt._current_raw_stream(on), None
-        held = not _capturing(raw)
+        held, place = not _capturing(raw), raw if self.device is not None else (on, raw)
         with self._lock:
             if keep:   # a buffer for each stream, shared by one forward pass after the other
-                stats = self._stats.get((on, raw)) if held else None
+                stats = self._stats.get(place) if held else None
                 if stats is None or stats.shape[0] != x.shape[0]:
                     stats = torch.empty(x.shape[0], self.groups, 2, dtype=torch.float32, device=x.device)
                     if held:
-                        self._stats[on, raw] = stats
-            ws = self._workspace((on, raw), held, size, x.device)
+                        self._stats[place] = stats
+            ws = self._workspace(place, held, size, x.device)
             w, b = self._params
             status = lbt.lib().lbt_groupnorm_forward(desc, at[0], w, b, at[1], q.data_ptr() if q is not None else 0, bits,
-                                                     lbt._floats(clip, 1, "clip", on), scale.data_ptr() if q is not None else 0,
+                                                     lbt._floats(clip, 1, "clip", on) if q is not None else 0, scale.data_ptr() if q is not None else 0,
                                                      stats.data_ptr() if keep else 0, ws.data_ptr(), size, raw)
             if status:
                 raise lbt.LbtError(status, "lbt_groupnorm_forward")
@@ -190,7 +190,7 @@ class GroupNorm:
         raw = lbt._current_raw_stream(on)
         w, b = self._params
         with self._lock:
-            ws = self._workspace((on, raw), not _capturing(raw), size, dy.device)
+            ws = self._workspace(raw if self.device is not None else (on, raw), not _capturing(raw), size, dy.device)
             status = lbt.lib().lbt_groupnorm_backward(desc, at[0], at[1], w, b, stats.data_ptr(), at[2], *grads, ws.data_ptr(), size, raw)
         if status:
             raise lbt.LbtError(status, "lbt_groupnorm_backward")

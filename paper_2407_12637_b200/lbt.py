@@ -402,7 +402,7 @@ def _place(t, stream=None):
 
 
 def _in_place_of(out, t) -> bool:
-    """Whether `out` begins where `t` does (itself, or another tensor on the same memory), so that writing the one overwrites the other."""
+    """Whether `out` is `t` or another tensor that begins where `t` does, so that writing the one overwrites the other (empty ones begin nowhere)."""
     return out is t or (isinstance(t, torch.Tensor) and t.numel() > 0 and out.data_ptr() == t.data_ptr())
 
 

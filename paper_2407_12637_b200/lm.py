@@ -245,10 +245,10 @@ class Adapters:
         if on != self.device:
             raise ValueError(f"the adapters are on device {self.device}")
         out = base if out is None else out
-        if keep and lbt._in_place_of(out, x):
-            raise ValueError("out in the place of x, which backward reads")
         runs, at_offsets, at_index = self._runs(offsets, index)
         M, at, plan = self._plan(("x", "base", "out"), (x, base, out), (self.I, self.O, self.O), runs)   # (holds the descriptor while the library reads it)
+        if keep and at[0] == at[2] and lbt._in_place_of(out, x):
+            raise ValueError("out in the place of x, which backward reads")
         raw, h = lbt._current_raw_stream(on), None
         if keep:   # a buffer for each stream, shared by one forward pass after the other
             held = not _capturing(raw)
